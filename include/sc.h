@@ -347,6 +347,121 @@ int sc_conv_up_fwd(const void* d_feat_coarse, int64_t n_map,
                    int K, int C_in, int C_out, int dtype_in, int dtype_out,
                    void* stream);
 
+/* ---- row layers: what a network runs on the rows of a sparse tensor between its convolutions ----------
+ *
+ * Linear layers with bias, activation and residual; layers whose weights differ by group of rows
+ * (experts, class heads, scenes of a batch, kernel offsets of a rulebook); the norm and the rotation by
+ * voxel coordinates of an attention's queries and keys; and the gradients of all of them.
+ *
+ * Conventions beside those above: rows are `ld` elements apart (ld >= the row's channels, so a row may be
+ * a slice of a wider one), every pointer needs the alignment of its elements only, and any number
+ * of channels 1 <= C <= SC_CHANNELS_MAX is taken.  16-byte alignment of rows and channels that are multiples of 16
+ * bytes are faster.  Types are SC_F32, SC_F16 and SC_BF16; sums are held in 32 bits.  Outputs must not overlap inputs,
+ * except that d_y may be d_residual.  Every sum's order is fixed by the sizes: repeated calls give the same bits. */
+#define SC_CHANNELS_MAX 65536
+#define SC_GROUPS_MAX   65536
+#define SC_ENTRIES_MAX  2147483647LL
+
+/* activations */
+#define SC_ACT_NONE  0
+#define SC_ACT_RELU  1     /* max(v, 0) */
+#define SC_ACT_GELU  2     /* v Phi(v), Phi the normal distribution's integral */
+#define SC_ACT_SILU  3     /* v / (1 + exp(-v)) */
+
+/* d_y[p][:] = act(d_x[p][:] . d_weight + d_bias) + d_residual[p][:]
+ *   d_x        [rows][C_in] of dtype_in, ldx apart; 0 <= rows <= SC_N_MAX
+ *   d_weight   [C_in][C_out] of dtype_in, contiguous; d_bias [C_out] of dtype_in or NULL
+ *   d_residual [rows][C_out] of dtype_out or NULL
+ *   d_y        [rows][C_out] of dtype_out: SC_F32 or dtype_in (one rounding at the end)
+ *   d_pre      NULL, or [rows][C_out] of dtype_out: receives x W + bias, what sc_linear_bwd needs for act != none */
+int sc_linear_fwd(const void* d_x, int64_t ldx, int64_t rows,
+                  const void* d_weight, const void* d_bias, int act,
+                  const void* d_residual, int64_t ld_residual,
+                  void* d_y, int64_t ldy, void* d_pre, int64_t ld_pre,
+                  int C_in, int C_out, int dtype_in, int dtype_out, void* stream);
+
+/* Gradients of sc_linear_fwd, all of one dtype: with dpre = dy * act'(pre),
+ *   d_dx = dpre W^T [rows][C_in],  d_dweight = x^T dpre [C_in][C_out],  d_dbias = column sums of dpre [C_out]
+ * each skipped where NULL (one at least is asked for).  The residual's gradient is dy itself.  dpre of 16-bit layers is rounded
+ * once to the rows' type before the products (not with act = SC_ACT_NONE, where it is dy).
+ *   d_pre      what the forward call stored; ignored for SC_ACT_NONE
+ *   d_x, d_weight may be NULL where d_dweight, d_dx are
+ *   d_workspace  workspace_bytes >= sc_linear_workspace_bytes(...), 16-byte aligned; contents undefined afterwards */
+size_t sc_linear_workspace_bytes(int64_t rows, int C_in, int C_out, int dtype);
+int sc_linear_bwd(const void* d_dy, int64_t lddy, const void* d_x, int64_t ldx, int64_t rows,
+                  const void* d_weight, const void* d_pre, int64_t ld_pre, int act,
+                  void* d_dx, int64_t lddx, void* d_dweight, void* d_dbias,
+                  int C_in, int C_out, int dtype, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* The same with a weight matrix for every group of entries: for d_starts[g] <= p < d_starts[g + 1],
+ *   d_y[p][:] = act(d_x[d_rows[p]][:] . d_weight[g] + d_bias[g])
+ *   d_starts   [groups + 1] on the device, ascending, values in [0, n]; groups may be empty.  (Starts that do not ascend give
+ *              wrong results, but no access outside the arrays.)  Rows of d_y of no group are left untouched.
+ *   d_rows     [n] row of d_x of each entry, or NULL: entry p reads row p.  An index outside [0, x_rows)
+ *              stands for a row of zeros.
+ *   d_weight   [groups][C_in][C_out], d_bias [groups][C_out] or NULL
+ * A rulebook from sc_kmap_export is such a set of entries: d_offset_start, and d_pairs_in / d_pairs_out as rows. */
+int sc_grouped_fwd(const void* d_x, int64_t ldx, int64_t x_rows, const int32_t* d_rows, int64_t n,
+                   const int32_t* d_starts, int groups,
+                   const void* d_weight, const void* d_bias, int act,
+                   void* d_y, int64_t ldy, void* d_pre, int64_t ld_pre,
+                   int C_in, int C_out, int dtype_in, int dtype_out, void* stream);
+
+/* Gradients of sc_grouped_fwd: with dpre[p] = dy[grad_rows[p]] * act'(pre[p]) (d_grad_rows NULL: row p),
+ *   d_dx[p] = dpre[p] d_weight[g]^T          one row per entry [n][C_in] (not added up over entries with the same row)
+ *   d_dweight[g] = sum over the group's p of x[rows[p]]^T dpre[p],  d_dbias[g] = sum of dpre[p]
+ * A group without entries gets zeros.  With the rulebook of a convolution (rows = pairs_in, grad_rows = pairs_out, dy the
+ * gradient of its output rows) d_dweight is the gradient of its weights. */
+size_t sc_grouped_workspace_bytes(int64_t n, int groups, int C_in, int C_out, int dtype);
+int sc_grouped_bwd(const void* d_dy, int64_t lddy, int64_t dy_rows, const int32_t* d_grad_rows,
+                   const void* d_x, int64_t ldx, int64_t x_rows, const int32_t* d_rows, int64_t n,
+                   const int32_t* d_starts, int groups,
+                   const void* d_weight, const void* d_pre, int64_t ld_pre, int act,
+                   void* d_dx, int64_t lddx, void* d_dweight, void* d_dbias,
+                   int C_in, int C_out, int dtype, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* Queries and keys of an attention over voxels: every head's D channels are normalised by their root mean
+ * square, scaled by a gain, and turned pairwise by angles that follow from the row's integer coordinates:
+ *   n = v / sqrt(mean(v^2) + eps) * gain        (gain NULL: n = v)
+ *   (n_a, n_b) -> (n_a cos t - n_b sin t, n_a sin t + n_b cos t),  t = pos[axis(j)] * f_j  for pair j
+ * Pair j is channels (j, j + D/2) with SC_PAIRS_HALVES, (2j, 2j + 1) with SC_PAIRS_ADJACENT.  The first pairs[0] pairs belong to axis
+ * 0, the next pairs[1] to axis 1 and so on; pairs left over are not turned.  Pair i of an axis with m pairs has
+ * f = base^(-i/m).  Statistics, angles and the rotation are in 32 bits, angles reduced exactly to a turn first
+ * (|pos| < 2^24), with one rounding at the end.
+ *   q, k        rows x heads x D, `row` and `head` elements apart (any order of rows and heads); k NULL or k->heads = 0: queries only.
+ *               q_out and k_out have the same numbers of heads; they may be q and k themselves (same strides).
+ *   d_pos       [rows][axes] int32, ld_pos apart: with voxel rows (b, x, y, z), d_coords + 1 and ld_pos 4
+ *   d_table     from sc_rope_table, sc_rope_table_bytes(D) bytes, 16-byte aligned
+ *   D           even, 2 <= D <= SC_HEAD_MAX; 1 <= axes <= SC_AXES_MAX; 0 <= rows <= SC_N_MAX; at most SC_GROUPS_MAX heads */
+#define SC_HEAD_MAX       1024
+#define SC_AXES_MAX       4
+#define SC_PAIRS_HALVES   0
+#define SC_PAIRS_ADJACENT 1
+typedef struct sc_heads {
+    void* data;                /* device memory */
+    int64_t row, head;         /* elements from row to row, from head to head */
+    int32_t heads;
+} sc_heads;
+
+size_t sc_rope_table_bytes(int D);
+/* h_pairs [axes] on the host, their sum at most D/2; base > 0 and finite.  Asynchronous on `stream`. */
+int sc_rope_table(int D, int axes, const int32_t* h_pairs, double base, void* d_table, size_t table_bytes, void* stream);
+
+int sc_qk_rope_fwd(const sc_heads* q, const sc_heads* k, int64_t rows, int D,
+                   const int32_t* d_pos, int64_t ld_pos, int axes, const void* d_table, int pairing,
+                   const void* d_gain_q, const void* d_gain_k, float eps,
+                   const sc_heads* q_out, const sc_heads* k_out, int dtype, void* stream);
+
+/* Gradients: of q and k from those of q_out and k_out (dq, dk may be dq_out, dk_out themselves), and of the gains, [D] each, summed over rows and heads
+ * (NULL where the gain is NULL or its gradient is not wanted).  q and k are the forward call's inputs, read only where there is a gain.
+ *   d_workspace  workspace_bytes >= sc_qk_rope_workspace_bytes(...), 16-byte aligned (needed with gains only) */
+size_t sc_qk_rope_workspace_bytes(int64_t rows, int q_heads, int k_heads, int D);
+int sc_qk_rope_bwd(const sc_heads* dq_out, const sc_heads* dk_out, const sc_heads* q, const sc_heads* k, int64_t rows, int D,
+                   const int32_t* d_pos, int64_t ld_pos, int axes, const void* d_table, int pairing,
+                   const void* d_gain_q, const void* d_gain_k, float eps,
+                   const sc_heads* dq, const sc_heads* dk, void* d_dgain_q, void* d_dgain_k,
+                   int dtype, void* d_workspace, size_t workspace_bytes, void* stream);
+
 /* ---- reading results back ------------------------------------------------------------------ */
 
 /* Fill n_pairs and per_offset from the kernel map (d_kmap may be NULL to skip that), copy the

@@ -31,13 +31,20 @@ DTYPES = {"f32": SC_F32, "f16": SC_F16, "bf16": SC_BF16,
           torch.float32: SC_F32, torch.float16: SC_F16, torch.bfloat16: SC_BF16}
 TORCH_DTYPES = {SC_F32: torch.float32, SC_F16: torch.float16, SC_BF16: torch.bfloat16}
 
+SC_CHANNELS_MAX, SC_GROUPS_MAX, SC_ENTRIES_MAX, SC_HEAD_MAX, SC_AXES_MAX = 65536, 65536, (1 << 31) - 1, 1024, 4
+ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, 0: 0, 1: 1, 2: 2, 3: 3}
+PAIRINGS = {"halves": 0, "adjacent": 1, 0: 0, 1: 1}
+
 # every symbol include/sc.h declares
 SYMBOLS = ["sc_hash_bytes", "sc_hash_build", "sc_hash_rebuild", "sc_hash_lookup", "sc_out_bound", "sc_kmap_bytes",
            "sc_kmap_scratch_bytes", "sc_kmap_build", "sc_kmap_transpose", "sc_conv_workspace_bytes", "sc_conv_fwd",
            "sc_counts_read", "sc_kmap_export", "sc_strerror", "sc_profile_enable", "sc_profile_read",
            "sc_grid_bytes", "sc_grid_clear", "sc_grid_build", "sc_grid_lookup", "sc_kmap_build_grid",
            "sc_conv_fwd_grid", "sc_conv_up_fwd", "sc_kmap_build_noalloc", "sc_profile_mfma_peak",
-           "sc_conv_packed_bytes", "sc_conv_weight_pack", "sc_conv_fwd_packed", "sc_hash_probe_slot"]
+           "sc_conv_packed_bytes", "sc_conv_weight_pack", "sc_conv_fwd_packed", "sc_hash_probe_slot",
+           "sc_linear_fwd", "sc_linear_workspace_bytes", "sc_linear_bwd", "sc_grouped_fwd", "sc_grouped_workspace_bytes",
+           "sc_grouped_bwd", "sc_rope_table_bytes", "sc_rope_table", "sc_qk_rope_fwd", "sc_qk_rope_workspace_bytes",
+           "sc_qk_rope_bwd"]
 
 
 class ScCounts(ctypes.Structure):
@@ -51,6 +58,10 @@ COUNTS_BYTES = ctypes.sizeof(ScCounts)
 class ScProfileEntry(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char_p), ("launches", ctypes.c_int64), ("total_ms", ctypes.c_double),
                 ("median_ms", ctypes.c_double)]
+
+
+class ScHeads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row", ctypes.c_int64), ("head", ctypes.c_int64), ("heads", ctypes.c_int32)]
 
 
 class ScError(RuntimeError):
@@ -75,6 +86,7 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         _build.build()
     lib = ctypes.CDLL(LIB_PATH)
     vp, i64, i32, sz = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_size_t
+    heads = ctypes.POINTER(ScHeads)
     sig = {
         "sc_hash_bytes": (sz, [i64]),
         "sc_hash_build": (i32, [vp, i64, vp, sz, vp, vp]),
@@ -106,6 +118,18 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         "sc_kmap_build_grid": (i32, [vp, i64, vp, sz, i32, i32, i32, i32, ctypes.c_uint32, i32, vp, sz, vp, vp]),
         "sc_conv_fwd_grid": (i32, [vp, vp, i64, vp, sz, i32, i32, i32, i32, ctypes.c_uint32, vp, vp, i32, i32, i32, i32, i32,
                                    vp, sz, vp]),
+        "sc_linear_fwd": (i32, [vp, i64, i64, vp, vp, i32, vp, i64, vp, i64, vp, i64, i32, i32, i32, i32, vp]),
+        "sc_linear_workspace_bytes": (sz, [i64, i32, i32, i32]),
+        "sc_linear_bwd": (i32, [vp, i64, vp, i64, i64, vp, vp, i64, i32, vp, i64, vp, vp, i32, i32, i32, vp, sz, vp]),
+        "sc_grouped_fwd": (i32, [vp, i64, i64, vp, i64, vp, i32, vp, vp, i32, vp, i64, vp, i64, i32, i32, i32, i32, vp]),
+        "sc_grouped_workspace_bytes": (sz, [i64, i32, i32, i32, i32]),
+        "sc_grouped_bwd": (i32, [vp, i64, i64, vp, vp, i64, i64, vp, i64, vp, i32, vp, vp, i64, i32, vp, i64, vp, vp, i32, i32, i32, vp, sz, vp]),
+        "sc_rope_table_bytes": (sz, [i32]),
+        "sc_rope_table": (i32, [i32, i32, ctypes.POINTER(ctypes.c_int32), ctypes.c_double, vp, sz, vp]),
+        "sc_qk_rope_fwd": (i32, [heads, heads, i64, i32, vp, i64, i32, vp, i32, vp, vp, ctypes.c_float, heads, heads, i32, vp]),
+        "sc_qk_rope_workspace_bytes": (sz, [i64, i32, i32, i32]),
+        "sc_qk_rope_bwd": (i32, [heads, heads, heads, heads, i64, i32, vp, i64, i32, vp, i32, vp, vp, ctypes.c_float, heads, heads, vp, vp, i32,
+                                 vp, sz, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -118,6 +142,8 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
 # the functions _native calls, in the order its bind() takes their addresses
 _NATIVE_CALLS = ["sc_hash_build", "sc_hash_rebuild", "sc_kmap_build", "sc_kmap_build_noalloc", "sc_kmap_transpose", "sc_conv_fwd",
                  "sc_conv_fwd_packed", "sc_conv_up_fwd", "sc_conv_fwd_grid", "sc_grid_build", "sc_kmap_build_grid"]
+# ... and of its bind_rows()
+_NATIVE_ROW_CALLS = ["sc_linear_fwd", "sc_linear_bwd", "sc_grouped_fwd", "sc_grouped_bwd", "sc_qk_rope_fwd", "sc_qk_rope_bwd"]
 
 
 class _NativeOnFirstUse:
@@ -138,6 +164,7 @@ def _load_native(lib: ctypes.CDLL):
     module = importlib.util.module_from_spec(spec)
     loader.exec_module(module)
     module.bind(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _NATIVE_CALLS))
+    module.bind_rows(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _NATIVE_ROW_CALLS))
     _native = module
 
 
@@ -317,6 +344,82 @@ def sc_kmap_export(kmap, n, K, stride, mode, h_counts: ScCounts, stream=None):
     _check(load().sc_kmap_export(_ptr(kmap), n, K, stride, MODES[mode], ctypes.byref(h_counts), _ptr(pin), _ptr(pout),
                                  _ptr(ost), _stream(stream)), "sc_kmap_export")
     return pin[:P], pout[:P], ost
+
+
+# ---- row layers ------------------------------------------------------------------------------
+# Matrices are [rows, channels] tensors whose rows may be slices of wider ones (x[:, :C]); weights, biases and their
+# gradients are contiguous.  Outputs are given by the caller, here as everywhere.
+def sc_linear_fwd(x, weight, out, bias=None, act="none", residual=None, pre=None, stream=None):
+    """out = act(x . weight + bias) + residual: x [rows, C_in], weight [C_in, C_out], out [rows, C_out] of x's
+    dtype or float32; `pre`, like out, receives x . weight + bias (what sc_linear_bwd needs for an activation)."""
+    rc = _native.linear_fwd(x, weight, out, bias, ACTS[act], residual, pre, stream)
+    if rc:
+        _check(rc, "sc_linear_fwd")
+
+
+def sc_linear_workspace_bytes(rows: int, C_in: int, C_out: int, dtype) -> int:
+    return load().sc_linear_workspace_bytes(rows, C_in, C_out, DTYPES[dtype])
+
+
+def sc_linear_bwd(grad_out, x, weight, grad_x=None, grad_weight=None, grad_bias=None, pre=None, act="none", workspace=None, stream=None):
+    """Gradients of sc_linear_fwd where a tensor is given for them (the residual's is grad_out itself);
+    workspace uint8 [>= sc_linear_workspace_bytes(...)]."""
+    rc = _native.linear_bwd(grad_out, x, weight, grad_x, grad_weight, grad_bias, pre, ACTS[act], workspace, stream)
+    if rc:
+        _check(rc, "sc_linear_bwd")
+
+
+def sc_grouped_fwd(x, weight, starts, out, rows=None, bias=None, act="none", pre=None, stream=None):
+    """out[p] = act(x[rows[p]] . weight[g] + bias[g]) for starts[g] <= p < starts[g + 1]: weight [groups, C_in, C_out],
+    starts int32 [groups + 1], rows int32 [n] or None (entry p reads row p), out [n, C_out]."""
+    rc = _native.grouped_fwd(x, weight, starts, out, rows, bias, ACTS[act], pre, stream)
+    if rc:
+        _check(rc, "sc_grouped_fwd")
+
+
+def sc_grouped_workspace_bytes(n: int, groups: int, C_in: int, C_out: int, dtype) -> int:
+    return load().sc_grouped_workspace_bytes(n, groups, C_in, C_out, DTYPES[dtype])
+
+
+def sc_grouped_bwd(grad_out, x, weight, starts, grad_x=None, grad_weight=None, grad_bias=None, rows=None, grad_rows=None, pre=None,
+                   act="none", workspace=None, stream=None):
+    """Gradients of sc_grouped_fwd; entry p's output gradient is grad_out[grad_rows[p]] (None: grad_out[p]), grad_x has one row
+    per entry.  With the lists of sc_kmap_export, grad_weight is a convolution's weight gradient."""
+    rc = _native.grouped_bwd(grad_out, x, weight, starts, grad_x, grad_weight, grad_bias, rows, grad_rows, pre, ACTS[act], workspace, stream)
+    if rc:
+        _check(rc, "sc_grouped_bwd")
+
+
+def sc_rope_table(D: int, pairs, base: float = 10000.0, table=None, device="cuda:0", stream=None):
+    """Frequencies of a head's D/2 pairs, `pairs[a]` of them turned by axis a: the table that sc_qk_rope_* take (a uint8
+    tensor; allocated here unless `table` is given)."""
+    pairs = [int(n) for n in pairs]
+    if table is None:
+        table = torch.empty(max(load().sc_rope_table_bytes(D), 16), dtype=torch.uint8, device=device)
+    _check(load().sc_rope_table(D, len(pairs), (ctypes.c_int32 * len(pairs))(*pairs), base, _ptr(table),
+                                table.numel() * table.element_size(), _stream(stream)), "sc_rope_table")
+    return table
+
+
+def sc_qk_rope_fwd(q, k, pos, table, q_out, k_out, gain_q=None, gain_k=None, eps=1e-6, pairing="halves", stream=None):
+    """Norm (where a gain [D] is given) and rotation of queries [rows, heads, D] and keys (or None) by int32 positions
+    [rows, axes]; with voxel rows (b, x, y, z) these are coords[:, 1:].  In place with q_out = q, k_out = k."""
+    rc = _native.qk_rope_fwd(q, k, pos, table, q_out, k_out, gain_q, gain_k, eps, PAIRINGS[pairing], stream)
+    if rc:
+        _check(rc, "sc_qk_rope_fwd")
+
+
+def sc_qk_rope_workspace_bytes(rows: int, q_heads: int, k_heads: int, D: int) -> int:
+    return load().sc_qk_rope_workspace_bytes(rows, q_heads, k_heads, D)
+
+
+def sc_qk_rope_bwd(grad_q_out, grad_k_out, q, k, pos, table, grad_q, grad_k, gain_q=None, gain_k=None, grad_gain_q=None, grad_gain_k=None,
+                   eps=1e-6, pairing="halves", workspace=None, stream=None):
+    """Gradients of sc_qk_rope_fwd: q and k are that call's inputs (None where there is no gain)."""
+    rc = _native.qk_rope_bwd(grad_q_out, grad_k_out, q, k, pos, table, grad_q, grad_k, gain_q, gain_k, grad_gain_q, grad_gain_k, eps,
+                             PAIRINGS[pairing], workspace, stream)
+    if rc:
+        _check(rc, "sc_qk_rope_bwd")
 
 
 def sc_profile_enable(enable: bool):

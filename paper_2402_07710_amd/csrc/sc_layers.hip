@@ -1,0 +1,316 @@
+// Linear layers and layers whose weights differ by group of rows, forward and backward: argument checks, the gradient of the
+// activation, and the sums of a weight gradient's parts.  The products themselves are in sc_product.h; a linear layer is one group.
+#include "sc_product.h"
+
+namespace sc {
+namespace {
+
+// dpre[p][n] = dy[row(p)][n] act'(pre[p][n]), rounded once to the rows' type: the matrix cores take it as an operand.  A pass over three
+// arrays; both products that follow read the result, which the last-level cache holds unless it is larger.
+template <int DT>
+__global__ void __launch_bounds__(256)
+k_act_grad(const void* __restrict__ grad, int64_t ldg, int64_t grad_rows, const int32_t* __restrict__ list, const void* __restrict__ pre,
+           int64_t ldp, int act, void* __restrict__ out, int64_t n, int N, int rows_each) {
+    const int chunks = (N + 7) / 8;
+    const int64_t first = (int64_t)blockIdx.x * rows_each;
+    for (int t = threadIdx.x; t < rows_each * chunks; t += 256) {
+        const int r = t / chunks, col = (t - r * chunks) * 8;
+        const int64_t e = first + r;
+        if (e >= n) break;
+        int64_t row = e;
+        if (list != nullptr) row = list[e];
+        const int there = N - col < 8 ? N - col : 8;
+        float g[8], v[8];
+        const bool ok = row >= 0 && row < grad_rows;
+        if (ok) load8<DT>(grad, row * ldg + col, there, g);
+        load8<DT>(pre, e * ldp + col, there, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = ok ? g[j] * slope<DT>(v[j], act) : 0.f;
+        store8<DT>(out, e * N + col, there, v);
+    }
+}
+
+// Sums of the parts of a group, in a fixed order: 16 threads take every 16th part of 64 consecutive values, then their 16 sums.
+template <int DT>
+__global__ void __launch_bounds__(256)
+k_product_join(const float* __restrict__ partial, const int32_t* __restrict__ starts, int groups, int64_t n, int64_t per, int M, int N,
+               void* __restrict__ out, void* __restrict__ out_bias, int64_t slots, int64_t blocks_each) {
+    __shared__ float4 sums[16][16];
+    const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    const int g = (int)(block / blocks_each);
+    if (g >= groups) return;
+    const int64_t values = (int64_t)(M + 1) * N;
+    const int lane = threadIdx.x & 63;
+    int64_t slot = 0;
+    int parts = 0;
+    if (starts == nullptr) {
+        parts = (int)((n + per - 1) / per);
+    } else {
+        for (int g0 = 0; g0 <= g; g0 += WAVE) {
+            const int at = g0 + lane;
+            int64_t lo = 0, hi = 0;
+            if (at <= g) {
+                lo = starts[at];
+                hi = starts[at + 1];
+                lo = lo < 0 ? 0 : lo > n ? n : lo;
+                hi = hi < lo ? lo : hi > n ? n : hi;
+            }
+            const uint32_t len = (uint32_t)(hi - lo), step = (uint32_t)per;
+            const int count = (int)(len / step + (len % step != 0));
+            if (g - g0 < WAVE) parts = __shfl(count, g - g0);
+            int before = count > 1 && at < g ? count : 0;
+#pragma unroll
+            for (int d = 1; d < WAVE; d <<= 1) before += __shfl_xor(before, d);
+            slot += before;
+        }
+    }
+    if (parts <= 1 || slot + parts > slots) return;    // written by the product itself; starts that do not ascend
+    const int64_t at = (block - (int64_t)g * blocks_each) * 64 + 4 * (threadIdx.x & 15);
+    const int which = threadIdx.x >> 4;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    const bool whole = at + 4 <= values;
+    const float* src = partial + slot * values + at;
+    if (whole) {
+#pragma unroll 8
+        for (int s = which; s < parts; s += 16) {
+            const uint4 v = load_chunk(src + s * values);
+            sum.x += __builtin_bit_cast(float, v.x);
+            sum.y += __builtin_bit_cast(float, v.y);
+            sum.z += __builtin_bit_cast(float, v.z);
+            sum.w += __builtin_bit_cast(float, v.w);
+        }
+    } else {
+        for (int s = which; s < parts; s += 16) {
+            if (at < values) sum.x += src[s * values];
+            if (at + 1 < values) sum.y += src[s * values + 1];
+            if (at + 2 < values) sum.z += src[s * values + 2];
+        }
+    }
+    sums[which][threadIdx.x & 15] = sum;
+    __syncthreads();
+    if (threadIdx.x >= 64) return;
+    const int64_t mine = at - 4 * (threadIdx.x & 15) + threadIdx.x;
+    if (mine >= values) return;
+    float total = 0.f;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) total += reinterpret_cast<const float*>(&sums[w][0])[threadIdx.x];
+    const int64_t weights = (int64_t)M * N;
+    if (mine < weights) store_elem<DT>(out, g * weights + mine, total);
+    else if (out_bias != nullptr) store_elem<DT>(out_bias, g * (int64_t)N + mine - weights, total);
+}
+
+int elem(int dtype) { return dtype == SC_F32 ? 4 : 2; }
+bool dtype_ok(int dtype) { return dtype == SC_F32 || dtype == SC_F16 || dtype == SC_BF16; }
+bool aligned_to(const void* p, int bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
+bool channels_ok(int C) { return C >= 1 && C <= SC_CHANNELS_MAX; }
+// `n` rows `ld` elements apart; no rows need no memory
+bool rows_ok(const void* p, int64_t n, int64_t ld, int C, int dtype) {
+    return (p != nullptr || n == 0) && aligned_to(p, elem(dtype)) && ld >= C && ld <= INT32_MAX;
+}
+// every row starts and ends at a 16-byte boundary
+bool whole_chunks(const void* p, int64_t ld, int C, int dtype) {
+    const int per = 16 / elem(dtype);
+    return aligned16(p) && ld % per == 0 && C % per == 0;
+}
+
+int launch(int dtype, int mode, const Product& p, bool whole, hipStream_t s) {
+    const int cus = compute_units();
+    if (dtype == SC_F32) return launch_product_f32(mode, p, whole, cus, s);
+    if (dtype == SC_F16) return launch_product_f16(mode, p, whole, cus, s);
+    return launch_product_bf16(mode, p, whole, cus, s);
+}
+
+struct Entries {                   // what tells a grouped layer from a linear one
+    const int32_t* starts;
+    int groups;
+    int64_t n;
+    const int32_t* rows;
+    int64_t x_rows;
+    const int32_t* grad_rows;
+    int64_t grad_n;
+};
+
+int forward(const void* x, int64_t ldx, const Entries& e, const void* weight, const void* bias, int act, const void* residual, int64_t ldr, void* y,
+            int64_t ldy, void* pre, int64_t ldp, int C_in, int C_out, int dtype_in, int dtype_out, hipStream_t s) {
+    if (!channels_ok(C_in) || !channels_ok(C_out) || !dtype_ok(dtype_in) || (dtype_out != SC_F32 && dtype_out != dtype_in)) return SC_EINVAL;
+    if (act < SC_ACT_NONE || act > SC_ACT_SILU) return SC_EINVAL;
+    if (e.n < 0 || e.n > SC_ENTRIES_MAX || e.x_rows < 0 || e.x_rows > SC_N_MAX || e.groups < 1 || e.groups > SC_GROUPS_MAX) return SC_EINVAL;
+    if (weight == nullptr || !aligned_to(weight, elem(dtype_in)) || !aligned_to(bias, elem(dtype_in))) return SC_EINVAL;
+    if (!rows_ok(x, e.x_rows, ldx, C_in, dtype_in) || !rows_ok(y, e.n, ldy, C_out, dtype_out)) return SC_EINVAL;
+    if (residual != nullptr && !rows_ok(residual, e.n, ldr, C_out, dtype_out)) return SC_EINVAL;
+    if (pre != nullptr && !rows_ok(pre, e.n, ldp, C_out, dtype_out)) return SC_EINVAL;
+    if (e.n == 0) return SC_OK;
+    Product p{};
+    p.a = x;
+    p.lda = ldx;
+    p.a_rows = e.x_rows;
+    p.a_list = e.rows;
+    p.b = weight;
+    p.ldb = C_out;
+    p.starts = e.starts;
+    p.groups = e.groups;
+    p.n = e.n;
+    p.N = C_out;
+    p.K = C_in;
+    p.bias = bias;
+    p.act = act;
+    p.residual = residual;
+    p.ldr = ldr;
+    p.pre = pre;
+    p.ldp = ldp;
+    p.out = y;
+    p.ldo = ldy;
+    p.out_f32 = dtype_out == SC_F32 && dtype_in != SC_F32;
+    return launch(dtype_in, PRODUCT_FWD, p, whole_chunks(x, ldx, C_in, dtype_in) && whole_chunks(weight, C_out, C_out, dtype_in), s);
+}
+
+size_t grad_bytes(int64_t n, int C_out, int dtype) { return align_up((size_t)n * C_out * elem(dtype), 256); }
+size_t partial_bytes(int64_t n, int C_in, int C_out) {
+    return (size_t)weight_slots(n, weight_part(n, C_in, C_out)) * (C_in + 1) * C_out * sizeof(float);
+}
+size_t workspace_bytes(int64_t n, int groups, int C_in, int C_out, int dtype) {
+    if (n < 0 || n > SC_ENTRIES_MAX || groups < 1 || groups > SC_GROUPS_MAX || !channels_ok(C_in) || !channels_ok(C_out) || !dtype_ok(dtype)) return 0;
+    return grad_bytes(n, C_out, dtype) + partial_bytes(n, C_in, C_out);
+}
+
+int backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const Entries& e, const void* weight, const void* pre, int64_t ldp, int act,
+             void* dx, int64_t lddx, void* dweight, void* dbias, int C_in, int C_out, int dtype, void* workspace, size_t bytes, hipStream_t s) {
+    if (!channels_ok(C_in) || !channels_ok(C_out) || !dtype_ok(dtype)) return SC_EINVAL;
+    if (act < SC_ACT_NONE || act > SC_ACT_SILU) return SC_EINVAL;
+    if (e.n < 0 || e.n > SC_ENTRIES_MAX || e.x_rows < 0 || e.x_rows > SC_N_MAX || e.grad_n < 0 || e.grad_n > SC_N_MAX || e.groups < 1 ||
+        e.groups > SC_GROUPS_MAX)
+        return SC_EINVAL;
+    const int size = elem(dtype);
+    if (dx == nullptr && dweight == nullptr && dbias == nullptr) return SC_EINVAL;
+    if (!rows_ok(dy, e.grad_n, lddy, C_out, dtype)) return SC_EINVAL;
+    if (act != SC_ACT_NONE && !rows_ok(pre, e.n, ldp, C_out, dtype)) return SC_EINVAL;
+    if (dx != nullptr && (!rows_ok(dx, e.n, lddx, C_in, dtype) || weight == nullptr || !aligned_to(weight, size))) return SC_EINVAL;
+    if (dweight != nullptr && (!aligned_to(dweight, size) || !rows_ok(x, e.x_rows, ldx, C_in, dtype))) return SC_EINVAL;
+    if (!aligned_to(dbias, size)) return SC_EINVAL;
+    const bool sums = dweight != nullptr || dbias != nullptr;
+    const size_t own = act != SC_ACT_NONE ? grad_bytes(e.n, C_out, dtype) : 0;
+    const size_t need = own + (sums ? partial_bytes(e.n, C_in, C_out) : 0);
+    if (need > 0 && (workspace == nullptr || !aligned16(workspace))) return SC_EINVAL;
+    if (need > bytes) return SC_ECAP;
+    if (e.n == 0 && !sums) return SC_OK;
+
+    const void* grad = dy;
+    int64_t ldg = lddy, grad_rows = e.grad_n;
+    const int32_t* grad_list = e.grad_rows;
+    if (act != SC_ACT_NONE && e.n > 0) {
+        const int chunks = (C_out + 7) / 8, each = chunks >= 2048 ? 1 : 2048 / chunks;
+        const dim3 grid((unsigned)((e.n + each - 1) / each));
+#define SC_ACT_GRAD(DT) SC_LAUNCH(KID_ACT_GRAD, k_act_grad<DT>, grid, dim3(256), 0, s, dy, lddy, e.grad_n, e.grad_rows, pre, ldp, act, workspace, e.n, C_out, each)
+        if (dtype == SC_F32) SC_ACT_GRAD(SC_F32);
+        else if (dtype == SC_F16) SC_ACT_GRAD(SC_F16);
+        else SC_ACT_GRAD(SC_BF16);
+#undef SC_ACT_GRAD
+        grad = workspace;
+        ldg = C_out;
+        grad_rows = e.n;
+        grad_list = nullptr;
+    }
+    if (dx != nullptr && e.n > 0) {
+        Product p{};
+        p.a = grad;
+        p.lda = ldg;
+        p.a_rows = grad_rows;
+        p.a_list = grad_list;
+        p.b = weight;
+        p.ldb = C_out;
+        p.starts = e.starts;
+        p.groups = e.groups;
+        p.n = e.n;
+        p.N = C_in;
+        p.K = C_out;
+        p.out = dx;
+        p.ldo = lddx;
+        const int rc = launch(dtype, PRODUCT_DX, p, whole_chunks(grad, ldg, C_out, dtype) && whole_chunks(weight, C_out, C_out, dtype), s);
+        if (rc != SC_OK) return rc;
+    }
+    if (sums) {
+        Product p{};
+        p.a = x;
+        p.lda = ldx;
+        p.a_rows = e.x_rows;
+        p.a_list = e.rows;
+        p.b = grad;
+        p.ldb = ldg;
+        p.b_rows = grad_rows;
+        p.b_list = grad_list;
+        p.starts = e.starts;
+        p.groups = e.groups;
+        p.n = e.n;
+        p.M = dweight != nullptr ? C_in : 0;
+        p.N = C_out;
+        p.per = weight_part(e.n, C_in, C_out);
+        p.units = e.starts == nullptr ? (e.n > p.per ? (e.n + p.per - 1) / p.per : 1) : e.n / p.per + e.groups;
+        p.out = dweight;
+        p.out_bias = dbias;
+        p.partial = (float*)((char*)workspace + own);
+        p.slots = weight_slots(e.n, p.per);
+        const bool whole = whole_chunks(grad, ldg, C_out, dtype) && (dweight == nullptr || whole_chunks(x, ldx, C_in, dtype));
+        int rc = launch(dtype, PRODUCT_DW, p, whole, s);
+        if (rc != SC_OK) return rc;
+        if (e.n > p.per) {
+            const int64_t each = ((int64_t)(p.M + 1) * p.N + 63) / 64, blocks = each * e.groups;
+            if (blocks > INT32_MAX) return SC_EINVAL;
+            const dim3 grid((unsigned)grid_columns(blocks), (unsigned)grid_rows(blocks));
+#define SC_JOIN(DT) SC_LAUNCH(KID_PRODUCT_JOIN, k_product_join<DT>, grid, dim3(256), 0, s, p.partial, e.starts, e.groups, e.n, p.per, p.M, p.N, dweight, dbias, p.slots, each)
+            if (dtype == SC_F32) SC_JOIN(SC_F32);
+            else if (dtype == SC_F16) SC_JOIN(SC_F16);
+            else SC_JOIN(SC_BF16);
+#undef SC_JOIN
+        }
+    }
+    return SC_OK;
+}
+
+}  // namespace
+}  // namespace sc
+
+using namespace sc;
+
+extern "C" int sc_linear_fwd(const void* d_x, int64_t ldx, int64_t rows, const void* d_weight, const void* d_bias, int act, const void* d_residual,
+                             int64_t ld_residual, void* d_y, int64_t ldy, void* d_pre, int64_t ld_pre, int C_in, int C_out, int dtype_in,
+                             int dtype_out, void* stream) {
+    if (rows < 0 || rows > SC_N_MAX) return SC_EINVAL;
+    const Entries e{nullptr, 1, rows, nullptr, rows, nullptr, rows};
+    return forward(d_x, ldx, e, d_weight, d_bias, act, d_residual, ld_residual, d_y, ldy, d_pre, ld_pre, C_in, C_out, dtype_in, dtype_out,
+                   (hipStream_t)stream);
+}
+
+extern "C" size_t sc_linear_workspace_bytes(int64_t rows, int C_in, int C_out, int dtype) {
+    return rows > SC_N_MAX ? 0 : workspace_bytes(rows, 1, C_in, C_out, dtype);
+}
+
+extern "C" int sc_linear_bwd(const void* d_dy, int64_t lddy, const void* d_x, int64_t ldx, int64_t rows, const void* d_weight, const void* d_pre,
+                             int64_t ld_pre, int act, void* d_dx, int64_t lddx, void* d_dweight, void* d_dbias, int C_in, int C_out, int dtype,
+                             void* d_workspace, size_t bytes, void* stream) {
+    if (rows < 0 || rows > SC_N_MAX) return SC_EINVAL;
+    const Entries e{nullptr, 1, rows, nullptr, rows, nullptr, rows};
+    return backward(d_dy, lddy, d_x, ldx, e, d_weight, d_pre, ld_pre, act, d_dx, lddx, d_dweight, d_dbias, C_in, C_out, dtype, d_workspace, bytes,
+                    (hipStream_t)stream);
+}
+
+extern "C" int sc_grouped_fwd(const void* d_x, int64_t ldx, int64_t x_rows, const int32_t* d_rows, int64_t n, const int32_t* d_starts, int groups,
+                              const void* d_weight, const void* d_bias, int act, void* d_y, int64_t ldy, void* d_pre, int64_t ld_pre, int C_in,
+                              int C_out, int dtype_in, int dtype_out, void* stream) {
+    if (d_starts == nullptr || !aligned_to(d_starts, 4) || !aligned_to(d_rows, 4)) return SC_EINVAL;
+    const Entries e{d_starts, groups, n, d_rows, x_rows, nullptr, 0};
+    return forward(d_x, ldx, e, d_weight, d_bias, act, nullptr, 0, d_y, ldy, d_pre, ld_pre, C_in, C_out, dtype_in, dtype_out, (hipStream_t)stream);
+}
+
+extern "C" size_t sc_grouped_workspace_bytes(int64_t n, int groups, int C_in, int C_out, int dtype) {
+    return workspace_bytes(n, groups, C_in, C_out, dtype);
+}
+
+extern "C" int sc_grouped_bwd(const void* d_dy, int64_t lddy, int64_t dy_rows, const int32_t* d_grad_rows, const void* d_x, int64_t ldx, int64_t x_rows,
+                              const int32_t* d_rows, int64_t n, const int32_t* d_starts, int groups, const void* d_weight, const void* d_pre,
+                              int64_t ld_pre, int act, void* d_dx, int64_t lddx, void* d_dweight, void* d_dbias, int C_in, int C_out, int dtype,
+                              void* d_workspace, size_t bytes, void* stream) {
+    if (d_starts == nullptr || !aligned_to(d_starts, 4) || !aligned_to(d_rows, 4) || !aligned_to(d_grad_rows, 4)) return SC_EINVAL;
+    const Entries e{d_starts, groups, n, d_rows, x_rows, d_grad_rows, dy_rows};
+    return backward(d_dy, lddy, d_x, ldx, e, d_weight, d_pre, ld_pre, act, d_dx, lddx, d_dweight, d_dbias, C_in, C_out, dtype, d_workspace, bytes,
+                    (hipStream_t)stream);
+}

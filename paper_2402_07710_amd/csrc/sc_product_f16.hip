@@ -1,0 +1,6 @@
+// The product kernels on f16 rows.
+#include "sc_product.h"
+
+namespace sc {
+int launch_product_f16(int mode, const Product& p, bool whole, int cus, hipStream_t s) { return launch_product<SC_F16>(mode, p, whole, cus, s); }
+}  // namespace sc

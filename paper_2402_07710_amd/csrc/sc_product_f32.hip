@@ -1,0 +1,6 @@
+// The product kernels on f32 rows.
+#include "sc_product.h"
+
+namespace sc {
+int launch_product_f32(int mode, const Product& p, bool whole, int cus, hipStream_t s) { return launch_product<SC_F32>(mode, p, whole, cus, s); }
+}  // namespace sc

@@ -25,7 +25,8 @@ const char* const KERNEL_NAMES[KID_COUNT] = {
     "k_table_fill", "k_hash_insert", "k_hash_lookup", "k_kmap_header", "k_kmap_subm", "k_strided_fill",
     "k_strided_insert", "k_strided_flags", "k_scan_blocks", "k_strided_pairs", "k_masks_from_table",
     "k_count_pairs", "k_export", "k_weight_pack", "k_conv_mfma", "k_conv_f32", "k_grid_clear", "k_grid_insert",
-    "k_grid_lookup", "k_kmap_subm_grid", "misc"};
+    "k_grid_lookup", "k_kmap_subm_grid", "k_product", "k_product_join", "k_act_grad", "k_rope_table", "k_rope", "k_rope_grad",
+    "k_gain_join", "misc"};
 
 hipEvent_t take_event() {
     if (!g_pool.empty()) {

@@ -11,6 +11,9 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <algorithm>
+#include <initializer_list>
+
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -31,6 +34,16 @@ struct Lib {
     decltype(&sc_grid_build) grid_build;
     decltype(&sc_kmap_build_grid) kmap_build_grid;
 } lib;
+
+// the row layers, bound apart by bind_rows()
+struct RowLib {
+    decltype(&sc_linear_fwd) linear_fwd;
+    decltype(&sc_linear_bwd) linear_bwd;
+    decltype(&sc_grouped_fwd) grouped_fwd;
+    decltype(&sc_grouped_bwd) grouped_bwd;
+    decltype(&sc_qk_rope_fwd) qk_rope_fwd;
+    decltype(&sc_qk_rope_bwd) qk_rope_bwd;
+} row_lib;
 
 struct PyFailure {};      // a Python exception is set
 
@@ -201,6 +214,189 @@ int conv_fwd_grid(Args a) {              // feat_in, coords, grid, dims, epoch, 
                              dtype(a[6]), ptr(a[8]), nbytes(a[8]), stream(a[9]));
 }
 
+// A matrix whose rows may be a slice of wider ones: [n, C], a row's elements next to each other.
+struct Rows {
+    void* data = nullptr;
+    int64_t n = 0, C = 0, ld = 0;
+};
+[[noreturn]] void fail_on(PyObject* kind, const char* name, const char* what) {
+    PyErr_Format(kind, "%s %s", name, what);
+    throw PyFailure{};
+}
+// every tensor among a call's arguments, behind the checks of their shapes
+void all_on_device(Args a, int n) {
+    for (int i = 0; i < n; ++i)
+        if (THPVariable_Check(a[i]) && !THPVariable_Unpack(a[i]).is_cuda()) fail(PyExc_ValueError, "device tensor expected");
+}
+Rows rows_of(PyObject* o, const char* name) {
+    if (o == Py_None) return Rows{};
+    const at::Tensor& t = tensor(o);
+    if (t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1)) fail_on(PyExc_ValueError, name, "must be [rows, channels], a row's channels contiguous");
+    Rows r;
+    r.n = t.size(0);
+    r.C = t.size(1);
+    r.ld = r.n > 1 ? t.stride(0) : r.C;                // torch leaves the stride of a single row undefined
+    if (r.ld < r.C) fail_on(PyExc_ValueError, name, "has rows that overlap");
+    r.data = t.data_ptr();
+    return r;
+}
+// a contiguous tensor of `dims` dimensions, sizes -1 unchecked
+void check_block(PyObject* o, const char* name, std::initializer_list<int64_t> sizes) {
+    if (o == Py_None) return;
+    const at::Tensor& t = tensor(o);
+    bool fits = t.dim() == (int64_t)sizes.size();
+    int d = 0;
+    for (const int64_t s : sizes) fits = fits && t.size(d++) == s;
+    if (!fits) fail_on(PyExc_ValueError, name, "has the wrong shape");
+    if (!t.is_contiguous()) fail_on(PyExc_ValueError, name, "must be contiguous");
+}
+void check_dtype(PyObject* o, const char* name, PyObject* like) {
+    if (o != Py_None && !same_dtype(o, like)) fail_on(PyExc_ValueError, name, "has the wrong dtype");
+}
+const int32_t* list_of(PyObject* o, const char* name, int64_t n) {
+    if (o == Py_None) return nullptr;
+    const at::Tensor& t = tensor(o);
+    if (t.scalar_type() != at::kInt) fail_on(PyExc_ValueError, name, "must be int32");
+    check_block(o, name, {n});
+    return (const int32_t*)t.data_ptr();
+}
+void check_rows(const Rows& r, PyObject* o, const char* name, int64_t n, int64_t C) {
+    if (o != Py_None && (r.n != n || r.C != C)) fail_on(PyExc_ValueError, name, "has the wrong shape");
+}
+void check_out_dtype(PyObject* out, PyObject* in) {
+    if (!same_dtype(out, in) && tensor(out).scalar_type() != at::kFloat) fail(PyExc_ValueError, "out must be of the rows' dtype or float32");
+}
+
+int linear_fwd(Args a) {                 // x, weight, out, bias, act, residual, pre, stream
+    const Rows x = rows_of(a[0], "x"), out = rows_of(a[2], "out"), residual = rows_of(a[5], "residual"), pre = rows_of(a[6], "pre");
+    const int64_t C_out = out.C;
+    check_block(a[1], "weight", {x.C, C_out});
+    check_block(a[3], "bias", {C_out});
+    check_dtype(a[1], "weight", a[0]);
+    check_dtype(a[3], "bias", a[0]);
+    check_out_dtype(a[2], a[0]);
+    check_dtype(a[5], "residual", a[2]);
+    check_dtype(a[6], "pre", a[2]);
+    check_rows(out, a[2], "out", x.n, C_out);
+    check_rows(residual, a[5], "residual", x.n, C_out);
+    check_rows(pre, a[6], "pre", x.n, C_out);
+    all_on_device(a, 8);
+    return unlocked(row_lib.linear_fwd, x.data, x.ld, x.n, ptr(a[1]), ptr(a[3]), small_int(a[4]), residual.data, residual.ld, out.data, out.ld, pre.data,
+                    pre.ld, (int)x.C, (int)C_out, dtype(a[0]), dtype(a[2]), stream(a[7]));
+}
+int linear_bwd(Args a) {                 // grad, x, weight, grad_x, grad_weight, grad_bias, pre, act, workspace, stream
+    const Rows grad = rows_of(a[0], "grad_out"), x = rows_of(a[1], "x"), grad_x = rows_of(a[3], "grad_x"), pre = rows_of(a[6], "pre");
+    check_block(a[2], "weight", {x.C, grad.C});
+    check_block(a[4], "grad_weight", {x.C, grad.C});
+    check_block(a[5], "grad_bias", {grad.C});
+    for (int i = 1; i <= 6; ++i) check_dtype(a[i], "an argument", a[0]);
+    check_rows(x, a[1], "x", grad.n, x.C);
+    check_rows(grad_x, a[3], "grad_x", grad.n, x.C);
+    check_rows(pre, a[6], "pre", grad.n, grad.C);
+    all_on_device(a, 10);
+    return unlocked(row_lib.linear_bwd, grad.data, grad.ld, x.data, x.ld, grad.n, ptr(a[2]), pre.data, pre.ld, small_int(a[7]), grad_x.data, grad_x.ld,
+                    ptr(a[4]), ptr(a[5]), (int)x.C, (int)grad.C, dtype(a[0]), ptr(a[8]), nbytes(a[8]), stream(a[9]));
+}
+int grouped_fwd(Args a) {                // x, weight, starts, out, rows, bias, act, pre, stream
+    const Rows x = rows_of(a[0], "x"), out = rows_of(a[3], "out"), pre = rows_of(a[7], "pre");
+    const int64_t groups = size(a[2], 0) - 1, n = out.n, C_out = out.C;
+    check_block(a[1], "weight", {groups, x.C, C_out});
+    check_block(a[5], "bias", {groups, C_out});
+    check_dtype(a[1], "weight", a[0]);
+    check_dtype(a[5], "bias", a[0]);
+    check_out_dtype(a[3], a[0]);
+    check_dtype(a[7], "pre", a[3]);
+    check_rows(pre, a[7], "pre", n, C_out);
+    const int32_t* starts = list_of(a[2], "starts", groups + 1);
+    const int32_t* rows = list_of(a[4], "rows", n);
+    all_on_device(a, 9);
+    return unlocked(row_lib.grouped_fwd, x.data, x.ld, x.n, rows, n, starts, (int)groups, ptr(a[1]), ptr(a[5]), small_int(a[6]), out.data, out.ld, pre.data,
+                    pre.ld, (int)x.C, (int)C_out, dtype(a[0]), dtype(a[3]), stream(a[8]));
+}
+int grouped_bwd(Args a) {                // grad, x, weight, starts, grad_x, grad_weight, grad_bias, rows, grad_rows, pre, act, workspace, stream
+    const Rows grad = rows_of(a[0], "grad_out"), x = rows_of(a[1], "x"), grad_x = rows_of(a[4], "grad_x"), pre = rows_of(a[9], "pre");
+    const int64_t groups = size(a[3], 0) - 1;
+    int64_t n = grad.n;                  // entries: as many as there are gradient rows, or as the list has
+    if (a[8] != Py_None) n = size(a[8], 0);
+    check_block(a[2], "weight", {groups, x.C, grad.C});
+    check_block(a[5], "grad_weight", {groups, x.C, grad.C});
+    check_block(a[6], "grad_bias", {groups, grad.C});
+    for (const int i : {1, 2, 4, 5, 6, 9}) check_dtype(a[i], "an argument", a[0]);
+    check_rows(grad_x, a[4], "grad_x", n, x.C);
+    check_rows(pre, a[9], "pre", n, grad.C);
+    const int32_t* starts = list_of(a[3], "starts", groups + 1);
+    const int32_t* rows = list_of(a[7], "rows", n);
+    const int32_t* grad_rows = list_of(a[8], "grad_rows", n);
+    all_on_device(a, 13);
+    return unlocked(row_lib.grouped_bwd, grad.data, grad.ld, grad.n, grad_rows, x.data, x.ld, x.n, rows, n, starts, (int)groups, ptr(a[2]), pre.data, pre.ld,
+                    small_int(a[10]), grad_x.data, grad_x.ld, ptr(a[5]), ptr(a[6]), (int)x.C, (int)grad.C, dtype(a[0]), ptr(a[11]), nbytes(a[11]),
+                    stream(a[12]));
+}
+
+// [rows, heads, D] in any order of rows and heads, a head's channels contiguous
+sc_heads heads_of(PyObject* o, const char* name, int64_t rows, int64_t D) {
+    sc_heads h{};
+    if (o == Py_None) return h;
+    const at::Tensor& t = tensor(o);
+    if (t.dim() != 3 || t.size(0) != rows || t.size(2) != D) fail_on(PyExc_ValueError, name, "has the wrong shape");
+    if (t.size(2) > 1 && t.stride(2) != 1) fail_on(PyExc_ValueError, name, "must have a head's channels contiguous");
+    if (t.size(1) > INT32_MAX) fail_on(PyExc_ValueError, name, "has too many heads");
+    h.row = t.size(0) > 1 ? t.stride(0) : 0;
+    h.head = t.size(1) > 1 ? t.stride(1) : 0;
+    h.heads = (int32_t)t.size(1);
+    h.data = t.data_ptr();
+    return h;
+}
+struct Positions {
+    const int32_t* data;
+    int64_t ld;
+    int axes;
+};
+Positions positions(PyObject* o, int64_t rows) {
+    const at::Tensor& t = tensor(o);
+    if (t.dim() != 2 || t.size(0) != rows || t.scalar_type() != at::kInt) fail(PyExc_ValueError, "pos must be int32 [rows, axes]");
+    if (t.size(1) > 1 && t.stride(1) != 1) fail(PyExc_ValueError, "pos must have a row's coordinates contiguous");
+    const int64_t ld = t.size(0) > 1 ? t.stride(0) : t.size(1);
+    return Positions{(const int32_t*)t.data_ptr(), ld, (int)std::min<int64_t>(t.size(1), INT32_MAX)};
+}
+float number(PyObject* o) {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw PyFailure{};
+    return (float)v;
+}
+void check_table(PyObject* table, int64_t D) {
+    if ((int64_t)nbytes(table) < 8 * D) fail(PyExc_ValueError, "table is not one of sc_rope_table for this head size");
+}
+int qk_rope_fwd(Args a) {                // q, k, pos, table, q_out, k_out, gain_q, gain_k, eps, pairing, stream
+    if (tensor(a[0]).dim() != 3) fail(PyExc_ValueError, "q must be [rows, heads, D]");
+    const int64_t rows = size(a[0], 0), D = size(a[0], 2);
+    const sc_heads q = heads_of(a[0], "q", rows, D), k = heads_of(a[1], "k", rows, D), q_out = heads_of(a[4], "q_out", rows, D),
+                   k_out = heads_of(a[5], "k_out", rows, D);
+    for (const int i : {1, 4, 5, 6, 7}) check_dtype(a[i], "an argument", a[0]);
+    check_block(a[6], "gain_q", {D});
+    check_block(a[7], "gain_k", {D});
+    check_table(a[3], D);
+    const Positions pos = positions(a[2], rows);
+    all_on_device(a, 11);
+    return unlocked(row_lib.qk_rope_fwd, &q, a[1] == Py_None ? nullptr : &k, rows, (int)D, pos.data, pos.ld, pos.axes, (const void*)ptr(a[3]), small_int(a[9]),
+                    ptr(a[6]), ptr(a[7]), number(a[8]), &q_out, a[5] == Py_None ? nullptr : &k_out, dtype(a[0]), stream(a[10]));
+}
+int qk_rope_bwd(Args a) {                // grad_q_out, grad_k_out, q, k, pos, table, grad_q, grad_k, gain_q, gain_k, grad_gain_q, grad_gain_k, eps, pairing, workspace, stream
+    if (tensor(a[0]).dim() != 3) fail(PyExc_ValueError, "grad_q_out must be [rows, heads, D]");
+    const int64_t rows = size(a[0], 0), D = size(a[0], 2);
+    const sc_heads dq_out = heads_of(a[0], "grad_q_out", rows, D), dk_out = heads_of(a[1], "grad_k_out", rows, D), q = heads_of(a[2], "q", rows, D),
+                   k = heads_of(a[3], "k", rows, D), dq = heads_of(a[6], "grad_q", rows, D), dk = heads_of(a[7], "grad_k", rows, D);
+    for (const int i : {1, 2, 3, 6, 7, 8, 9, 10, 11}) check_dtype(a[i], "an argument", a[0]);
+    const char* const names[4] = {"gain_q", "gain_k", "grad_gain_q", "grad_gain_k"};
+    for (int i = 0; i < 4; ++i) check_block(a[8 + i], names[i], {D});
+    check_table(a[5], D);
+    const Positions pos = positions(a[4], rows);
+    all_on_device(a, 16);
+    return unlocked(row_lib.qk_rope_bwd, &dq_out, a[1] == Py_None ? nullptr : &dk_out, &q, a[3] == Py_None ? nullptr : &k, rows, (int)D, pos.data, pos.ld,
+                    pos.axes, (const void*)ptr(a[5]), small_int(a[13]), ptr(a[8]), ptr(a[9]), number(a[12]), &dq, a[7] == Py_None ? nullptr : &dk,
+                    ptr(a[10]), ptr(a[11]), dtype(a[0]), ptr(a[14]), nbytes(a[14]), stream(a[15]));
+}
+
 template <int (*F)(Args), int N>
 PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (nargs != N) {
@@ -217,10 +413,11 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     }
 }
 
-// the addresses of the C functions, in the order of Lib's members
+// the addresses of the C functions, in the order of L's members
+template <class L, L& TARGET>
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-    void* addr[sizeof(Lib) / sizeof(void*)];
-    if (nargs != (Py_ssize_t)(sizeof(Lib) / sizeof(void*))) {
+    void* addr[sizeof(L) / sizeof(void*)];
+    if (nargs != (Py_ssize_t)(sizeof(L) / sizeof(void*))) {
         PyErr_SetString(PyExc_TypeError, "one address per function expected");
         return nullptr;
     }
@@ -231,13 +428,14 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
             return nullptr;
         }
     }
-    memcpy(&lib, addr, sizeof lib);
+    memcpy(&TARGET, addr, sizeof TARGET);
     Py_RETURN_NONE;
 }
 
 #define SC_METHOD(name, nargs) {#name, (PyCFunction)(void (*)(void))call<name, nargs>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
-    {"bind", (PyCFunction)(void (*)(void))bind, METH_FASTCALL, nullptr},
+    {"bind", (PyCFunction)(void (*)(void))bind<Lib, lib>, METH_FASTCALL, nullptr},
+    {"bind_rows", (PyCFunction)(void (*)(void))bind<RowLib, row_lib>, METH_FASTCALL, nullptr},
     SC_METHOD(hash_build, 4),
     SC_METHOD(hash_rebuild, 5),
     SC_METHOD(kmap_build, 10),
@@ -249,6 +447,12 @@ PyMethodDef methods[] = {
     SC_METHOD(conv_fwd_packed, 11),
     SC_METHOD(conv_up_fwd, 8),
     SC_METHOD(conv_fwd_grid, 10),
+    SC_METHOD(linear_fwd, 8),
+    SC_METHOD(linear_bwd, 10),
+    SC_METHOD(grouped_fwd, 9),
+    SC_METHOD(grouped_bwd, 13),
+    SC_METHOD(qk_rope_fwd, 11),
+    SC_METHOD(qk_rope_bwd, 16),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "argument marshalling for libsc's calls", -1, methods,

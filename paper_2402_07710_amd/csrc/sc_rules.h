@@ -176,4 +176,31 @@ constexpr bool grid_fits(int64_t columns, int64_t threads) { return columns * th
 constexpr int64_t grid_columns(int64_t groups) { return groups < GRID_COLUMNS ? groups : GRID_COLUMNS; }
 constexpr int64_t grid_rows(int64_t groups) { return (groups + GRID_COLUMNS - 1) / GRID_COLUMNS; }
 
+// ---- products of rows and weights (sc_product.h) --------------------------------------------------------
+// Tile of the result that a workgroup owns, by the rows and columns there are.  Few rows a group: 16 rows, four wavefronts share the summed axis.
+enum RowTile { ROWS_FEW, COLUMNS_32, COLUMNS_64, TILE_128 };
+constexpr RowTile row_tile(int64_t entries, int64_t groups, int64_t columns, int64_t depth) {
+    (void)depth;
+    if (entries <= 32 * (groups < entries ? groups : entries)) return ROWS_FEW;
+    return columns <= 32 ? COLUMNS_32 : columns <= 64 ? COLUMNS_64 : TILE_128;
+}
+// Tile of a weight gradient.
+constexpr int weight_tile(int64_t c_in, int64_t c_out) { return c_in <= 64 && c_out <= 64 ? 64 : 128; }
+constexpr int64_t weight_tiles(int64_t c_in, int64_t c_out) {
+    const int64_t t = weight_tile(c_in, c_out);
+    return (c_in > t ? (c_in + t - 1) / t : 1) * ((c_out + t - 1) / t);
+}
+// Entries that one workgroup sums of a group for a tile of its weight gradient: the groups are cut into parts so that there are about two
+// workgroups for each of 256 compute units, but parts of 512 entries at least, whose sums are written once and read once.
+constexpr int64_t weight_part(int64_t entries, int64_t c_in, int64_t c_out) {
+    const int64_t want = (entries * weight_tiles(c_in, c_out) + 511) / 512;
+    return ((want > 512 ? want : 512) + 63) / 64 * 64;
+}
+// Parts of groups that have several: a group of e entries has fewer than 2 e / part of them.
+constexpr int64_t weight_slots(int64_t entries, int64_t part) { return entries <= part ? 0 : 2 * entries / part + 1; }
+
+// ---- norm and rotation (sc_rope.hip) ----------------------------------------------------------------------
+// Workgroups of 256 threads for the queries, and as many for the keys, at most.
+constexpr int64_t ROPE_BLOCKS_MAX = 2048;
+
 }  // namespace sc
