@@ -30,12 +30,14 @@ k_act_grad(const void* __restrict__ grad, int64_t ldg, int64_t grad_rows, const 
     }
 }
 
-// Sums of the parts of a group, in a fixed order: 16 threads take every 16th part of 64 consecutive values, then their 16 sums.
-template <int DT>
+// Sums of the parts of a group, in a fixed order.  LANES threads take 4 LANES consecutive values, 256 / LANES of them every so many'th part each, then their sums:
+// few parts many values a workgroup, many parts many loads in flight.
+template <int DT, int LANES>
 __global__ void __launch_bounds__(256)
 k_product_join(const float* __restrict__ partial, const int32_t* __restrict__ starts, int groups, int64_t n, int64_t per, int M, int N,
                void* __restrict__ out, void* __restrict__ out_bias, int64_t slots, int64_t blocks_each) {
-    __shared__ float4 sums[16][16];
+    constexpr int SHARES = 256 / LANES;
+    __shared__ float4 sums[SHARES][LANES];
     const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     const int g = (int)(block / blocks_each);
     if (g >= groups) return;
@@ -65,14 +67,13 @@ k_product_join(const float* __restrict__ partial, const int32_t* __restrict__ st
         }
     }
     if (parts <= 1 || slot + parts > slots) return;    // written by the product itself; starts that do not ascend
-    const int64_t at = (block - (int64_t)g * blocks_each) * 64 + 4 * (threadIdx.x & 15);
-    const int which = threadIdx.x >> 4;
+    const int64_t first = (block - (int64_t)g * blocks_each) * (4 * LANES), at = first + 4 * (threadIdx.x % LANES);
+    const int which = threadIdx.x / LANES;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    const bool whole = at + 4 <= values;
     const float* src = partial + slot * values + at;
-    if (whole) {
+    if (at + 4 <= values) {
 #pragma unroll 8
-        for (int s = which; s < parts; s += 16) {
+        for (int s = which; s < parts; s += SHARES) {
             const uint4 v = load_chunk(src + s * values);
             sum.x += __builtin_bit_cast(float, v.x);
             sum.y += __builtin_bit_cast(float, v.y);
@@ -80,23 +81,24 @@ k_product_join(const float* __restrict__ partial, const int32_t* __restrict__ st
             sum.w += __builtin_bit_cast(float, v.w);
         }
     } else {
-        for (int s = which; s < parts; s += 16) {
+        for (int s = which; s < parts; s += SHARES) {
             if (at < values) sum.x += src[s * values];
             if (at + 1 < values) sum.y += src[s * values + 1];
             if (at + 2 < values) sum.z += src[s * values + 2];
         }
     }
-    sums[which][threadIdx.x & 15] = sum;
+    sums[which][threadIdx.x % LANES] = sum;
     __syncthreads();
-    if (threadIdx.x >= 64) return;
-    const int64_t mine = at - 4 * (threadIdx.x & 15) + threadIdx.x;
-    if (mine >= values) return;
-    float total = 0.f;
-#pragma unroll
-    for (int w = 0; w < 16; ++w) total += reinterpret_cast<const float*>(&sums[w][0])[threadIdx.x];
     const int64_t weights = (int64_t)M * N;
-    if (mine < weights) store_elem<DT>(out, g * weights + mine, total);
-    else if (out_bias != nullptr) store_elem<DT>(out_bias, g * (int64_t)N + mine - weights, total);
+    for (int t = threadIdx.x; t < 4 * LANES; t += 256) {
+        const int64_t mine = first + t;
+        if (mine >= values) return;
+        float total = 0.f;
+#pragma unroll
+        for (int w = 0; w < SHARES; ++w) total += reinterpret_cast<const float*>(&sums[w][0])[t];
+        if (mine < weights) store_elem<DT>(out, g * weights + mine, total);
+        else if (out_bias != nullptr) store_elem<DT>(out_bias, g * (int64_t)N + mine - weights, total);
+    }
 }
 
 int elem(int dtype) { return dtype == SC_F32 ? 4 : 2; }
@@ -253,10 +255,19 @@ int backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const Ent
         int rc = launch(dtype, PRODUCT_DW, p, whole, s);
         if (rc != SC_OK) return rc;
         if (e.n > p.per) {
-            const int64_t each = ((int64_t)(p.M + 1) * p.N + 63) / 64, blocks = each * e.groups;
+            // 1024 values a workgroup leave most of the chip idle below some thousands of them (narrow / wide: 27 groups of 64 x 64 5 / 10 us)
+            const int64_t values = (int64_t)(p.M + 1) * p.N;
+            const bool many = (values + 1023) / 1024 * e.groups < 2048;
+            const int64_t wide = many ? 64 : 1024, each = (values + wide - 1) / wide, blocks = each * e.groups;
             if (blocks > INT32_MAX) return SC_EINVAL;
             const dim3 grid((unsigned)grid_columns(blocks), (unsigned)grid_rows(blocks));
-#define SC_JOIN(DT) SC_LAUNCH(KID_PRODUCT_JOIN, k_product_join<DT>, grid, dim3(256), 0, s, p.partial, e.starts, e.groups, e.n, p.per, p.M, p.N, dweight, dbias, p.slots, each)
+#define SC_JOIN(DT)                                                                                                                             \
+    do {                                                                                                                                        \
+        if (many) SC_LAUNCH(KID_PRODUCT_JOIN, (k_product_join<DT, 16>), grid, dim3(256), 0, s, p.partial, e.starts, e.groups, e.n, p.per, p.M,  \
+                            p.N, dweight, dbias, p.slots, each);                                                                                \
+        else SC_LAUNCH(KID_PRODUCT_JOIN, (k_product_join<DT, 256>), grid, dim3(256), 0, s, p.partial, e.starts, e.groups, e.n, p.per, p.M, p.N, \
+                       dweight, dbias, p.slots, each);                                                                                          \
+    } while (0)
             if (dtype == SC_F32) SC_JOIN(SC_F32);
             else if (dtype == SC_F16) SC_JOIN(SC_F16);
             else SC_JOIN(SC_BF16);

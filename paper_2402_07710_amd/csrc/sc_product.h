@@ -69,6 +69,16 @@ __device__ inline float to_float(uint32_t bits16) {
     if constexpr (DT == SC_F16) return (float)__builtin_bit_cast(_Float16, (uint16_t)bits16);
     else return __builtin_bit_cast(float, bits16 << 16);
 }
+// two values rounded to nearest even, one instruction of gfx950
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+template <int DT>
+__device__ inline uint32_t round2(float lo, float hi) {
+    const f32x2 v{lo, hi};
+    if constexpr (DT == SC_F16) return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
+    else return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+}
 template <int DT>
 __device__ inline float load_elem(const void* p, int64_t i) {
     if constexpr (DT == SC_F32) return reinterpret_cast<const float*>(p)[i];
@@ -77,7 +87,7 @@ __device__ inline float load_elem(const void* p, int64_t i) {
 template <int DT>
 __device__ inline void store_elem(void* p, int64_t i, float v) {
     if constexpr (DT == SC_F32) reinterpret_cast<float*>(p)[i] = v;
-    else reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)pack2<DT>(v, 0.f);
+    else reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)round2<DT>(v, 0.f);
 }
 // up to eight consecutive elements, those from `count` on are zeros / left alone
 template <int DT>
@@ -114,7 +124,7 @@ __device__ inline void store8(void* base, int64_t i, int count, const float (&v)
             store_chunk(p, make_uint4(w[0], w[1], w[2], w[3]));
             store_chunk(p + 16, make_uint4(w[4], w[5], w[6], w[7]));
         } else {
-            store_chunk(p, make_uint4(pack2<DT>(v[0], v[1]), pack2<DT>(v[2], v[3]), pack2<DT>(v[4], v[5]), pack2<DT>(v[6], v[7])));
+            store_chunk(p, make_uint4(round2<DT>(v[0], v[1]), round2<DT>(v[2], v[3]), round2<DT>(v[4], v[5]), round2<DT>(v[6], v[7])));
         }
     } else {
 #pragma unroll
@@ -149,14 +159,14 @@ __device__ inline float sigmoid(float v) {
     if constexpr (DT == SC_F32) return 1.f / (1.f + expf(-v));
     else return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -1.44269504f));
 }
-// v times the weight of its activation.  Minus infinity times a weight of zero is the limit, zero.
+// v times the weight of its activation.  Minus infinity counts as the lowest number: times its weight of zero it is zero, the limit.
 template <int DT>
 __device__ inline float activate(float v, int act) {
     if (act == SC_ACT_RELU) return v > 0.f || v != v ? v : 0.f;
     if (act == SC_ACT_NONE) return v;
     float density;
     const float w = act == SC_ACT_GELU ? gauss_cdf<DT>(v, density) : sigmoid<DT>(v);
-    return w == 0.f ? 0.f : v * w;
+    return fmaxf(v, -3.4e38f) * w;                      // a NaN is in w as well
 }
 template <int DT>
 __device__ inline float slope(float v, int act) {
@@ -314,7 +324,7 @@ struct Loader {
     const int32_t* list;
     int limit, col0;               // channels there are; ACROSS: first of them here
     const char* row[ACROSS ? 1 : PASSES];      // ALONG: the lines' rows, null: none
-    int32_t at[ACROSS ? PASSES : 1];           // ACROSS: rows of the step that is loaded next, -1: none
+    int32_t at[ACROSS ? PASSES : 1];           // ACROSS: rows of the step that is loaded next, negative: none
     uint4 held[WHOLE ? 1 : PASSES];
 
     __device__ static int line_of(int i) { return (i * NTH + (int)threadIdx.x) / LINE; }
@@ -340,9 +350,9 @@ struct Loader {
 #pragma unroll
             for (int i = 0; i < PASSES; ++i) {
                 const int64_t e = first + line_of(i);
-                int64_t r = e < last ? e : -1;
-                if (r >= 0 && list != nullptr) r = list[e];
-                at[i] = r >= 0 && r < rows ? (int32_t)r : -1;
+                at[i] = e < last ? (int32_t)e : -1;
+                // not looked at before it is used, a step later: a comparison here would wait for it, and for the chunks ahead of it
+                if (list != nullptr && e < last) at[i] = list[e];
             }
         }
     }
@@ -355,7 +365,7 @@ struct Loader {
             const char* line;
             bool ok;
             if constexpr (ACROSS) {
-                ok = at[i] >= 0;
+                ok = at[i] >= 0 && at[i] < rows;
                 line = base + (int64_t)(ok ? at[i] : 0) * ld;
             } else {
                 ok = row[i] != nullptr;
