@@ -16,6 +16,8 @@
 // columns are dealt to pairs of 16-column blocks such that there are eight of them: 16 bytes of 16-bit results, a row's 64 bytes by four lanes.
 #pragma once
 
+#include <type_traits>
+
 #include "sc_conv.h"
 
 namespace sc {
@@ -34,6 +36,7 @@ struct Product {
     int64_t n, per;                // entries; DW: entries per part of a group
     int M, N, K;                   // channels: FWD K -> N, DX K -> N, DW M x N
     int64_t units;                 // row tiles there can be at most (DW: parts)
+    int run;                       // consecutive tiles that one XCD takes: product_run
     const void* bias;
     int act;
     const void* residual;
@@ -251,56 +254,68 @@ __device__ inline Part find_part(const int32_t* __restrict__ starts, int groups,
 // Stands in for chunks that lie beyond an operand's rows or channels.
 __device__ __align__(16) uint4 g_no_chunk;
 
-// ALONG: lines are rows of the tile, LINE chunks of the summed axis.  A lane's operand is one chunk of one line.
+// Where a chunk of a line lies in it: its number, turned by the line's, so that what an access of 16 lanes (operands along) or 32 (across) reads
+// fills the 64 banks once.
+// ALONG: lines are rows of the tile, LINE chunks of the summed axis; 16 lanes read one chunk of 16 lines.
 template <int LINE>
 __device__ constexpr int along_turn(int line) { return LINE == 8 ? (line >> 1) & 7 : line & 7; }
-// ACROSS: lines are places on the summed axis, LINE chunks of tile rows.  A 16-bit read takes 8 bytes from each of four lines and four
-// chunks, a 32-bit one words of lines four apart.
+// ACROSS: lines are places on the summed axis, LINE chunks of tile rows.  32 lanes of a 16-bit read take 32 bytes of four lines and of the four that
+// are 8 further on, 64 lanes of a 32-bit one 64 bytes of lines 0, 4, 8 and 12.
 template <int DT, int LINE>
 __device__ constexpr int across_turn(int line) {
-    if (DT == SC_F32) return LINE >= 16 ? ((line >> 2) & 1) | (line & 8) : LINE >= 8 ? (line >> 2) & 1 : 0;
-    return LINE >= 16 ? 4 * (line & 3) : LINE == 8 ? 4 * ((line >> 1) & 1) : 0;
+    if (DT == SC_F32) return LINE >= 16 ? line & 12 : LINE == 8 ? line & 4 : 0;
+    return LINE >= 16 ? 2 * (line & 3) + (line & 8) : LINE == 8 ? (line & 2) + (line & 8) / 2 : (line & 8) / 4;
 }
-
-// Row or column `i` (0..15) of block t of a wavefront's share: blocks of 16 in a row, or DEALT by pairs so that a result's lane has
-// eight consecutive ones.
-template <bool DEALT>
-__device__ constexpr int place(int t, int i) { return DEALT ? 32 * (t >> 1) + 8 * (i >> 2) + 4 * (t & 1) + (i & 3) : 16 * t + i; }
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
-typedef __attribute__((address_space(3))) const char* lds_bytes;
+typedef __attribute__((address_space(3))) const u32x4* lds_u32x4;
+typedef __attribute__((address_space(3))) const uint32_t* lds_uint32;
 
-// the operand of lane (i = lane % 16, o = lane / 16) for block t and chunks 4 s .. 4 s + 3 of the summed axis (from chunk or line `at0` on)
-template <int DT, int LINE, bool DEALT>
-__device__ inline uint4 operand_along(const uint4* tile, int row0, int t, int chunk0, int s, int i, int o) {
-    const int line = row0 + place<DEALT>(t, i), c = chunk0 + 4 * s + o;
-    return tile[line * LINE + (c ^ along_turn<LINE>(line))];
-}
-template <int DT, int LINE, bool DEALT>
-__device__ inline uint4 operand_across(const uint4* tile, int col0, int t, int line0, int s, int i, int o) {
-    if constexpr (DT == SC_F32) {
-        const int col = col0 + place<DEALT>(t, i);
-        uint32_t v[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int line = line0 + 16 * s + 4 * o + j;
-            v[j] = reinterpret_cast<const uint32_t*>(tile)[(line * LINE + ((col >> 2) ^ across_turn<DT, LINE>(line))) * 4 + (col & 3)];
-        }
-        return make_uint4(v[0], v[1], v[2], v[3]);
-    } else {
-        // lane i hands in 4 columns of line i / 4 and gets column i of the four lines
-        const int col = col0 + place<DEALT>(t, 4 * (i & 3));
-        uint2 v[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int line = line0 + 32 * s + 8 * o + 4 * h + (i >> 2);
-            const char* p = reinterpret_cast<const char*>(tile + line * LINE + ((col >> 3) ^ across_turn<DT, LINE>(line))) + (col & 4) * 2;
-            v[h] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(lds_bytes)p));
-        }
-        return make_uint4(v[0].x, v[0].y, v[1].x, v[1].y);
+// LDS addresses from which a lane reads its operands of T blocks of 16 rows, in the first buffer
+template <int DT, int LINE, int T>
+struct AlongReader {
+    uint32_t at[2];
+    // row0: the wavefront's first row; chunk0: its set's first chunk; both multiples that leave the turn alone
+    __device__ AlongReader(uint32_t tile, int row0, int chunk0) {
+        const int i = threadIdx.x & 15, o = (threadIdx.x >> 4) & 3;
+        for (int c = 0; c < 2; ++c) at[c] = tile + ((row0 + i) * LINE + chunk0 + ((4 * c + o) ^ along_turn<LINE>(i))) * 16;
     }
-}
+    // block t, chunks 4 c .. 4 c + 3, a chunk for each 16 lanes
+    __device__ uint4 read(uint32_t buffer, int t, int c) const { return __builtin_bit_cast(uint4, *(lds_u32x4)(at[c] + buffer + t * (16 * LINE * 16))); }
+};
+template <int DT, int LINE, int T>
+struct AcrossReader {
+    uint32_t at[T];
+    __device__ AcrossReader(uint32_t tile, int col0, int line0) {
+        const int i = threadIdx.x & 15, o = (threadIdx.x >> 4) & 3;
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            if constexpr (DT == SC_F32) {
+                const int line = line0 + 4 * o, col = col0 + 16 * t + i;
+                at[t] = tile + (line * LINE + ((col >> 2) ^ across_turn<DT, LINE>(line))) * 16 + (col & 3) * 4;
+            } else {                        // a lane hands in 4 columns of line i / 4 and gets column i of the four lines
+                const int line = line0 + 8 * o + (i >> 2), col = col0 + 16 * t + 4 * (i & 3);
+                at[t] = tile + (line * LINE + ((col >> 3) ^ across_turn<DT, LINE>(line))) * 16 + (col & 4) * 2;
+            }
+        }
+    }
+    __device__ uint4 read(uint32_t buffer, int t, int c) const {
+        const uint32_t p = at[t] + buffer;
+        if constexpr (DT == SC_F32) {
+            uint32_t v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = *(lds_uint32)(p + (16 * c + j) * (LINE * 16));
+            return make_uint4(v[0], v[1], v[2], v[3]);
+        } else {
+            uint2 v[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                v[h] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(p + (32 * c + 4 * h) * (LINE * 16))));
+            return make_uint4(v[0].x, v[0].y, v[1].x, v[1].y);
+        }
+    }
+};
 template <int DT>
 __device__ inline f32x4 multiply(uint4 a, uint4 b, f32x4 c) {
     if constexpr (DT == SC_F32) {
@@ -314,17 +329,19 @@ __device__ inline f32x4 multiply(uint4 a, uint4 b, f32x4 c) {
     }
 }
 
-// What the chunks that one thread brings of a tile have in common over the steps.  PASSES chunks each, `LINES` lines.
-template <int DT, bool ACROSS, int LINES, int LINE, int NTH, bool WHOLE>
+// What one thread brings of an operand's tiles: PASSES chunks a step.  `end` is where the summed axis ends (ALONG: channels, ACROSS: rows
+// of the operand that count), STRIDE how much of it a step takes.
+template <int DT, bool ACROSS, int LINES, int LINE, int NTH, int STRIDE, bool WHOLE>
 struct Loader {
     static constexpr int PASSES = LINES * LINE / NTH, PER = 16 / ELEM<DT>;
     static_assert(LINES * LINE % NTH == 0 && NTH % LINE == 0, "whole passes of whole lines");
+    int64_t ld, rows;                          // bytes from row to row; rows of the operand
+    int64_t first, end;                        // ACROSS: the summed entries; ALONG: first is 0
     const char* base;
-    int64_t ld, rows, last;        // bytes from row to row; rows of the operand; ACROSS: end of the entries
-    const int32_t* list;
-    int limit, col0;               // channels there are; ACROSS: first of them here
-    const char* row[ACROSS ? 1 : PASSES];      // ALONG: the lines' rows, null: none
-    int32_t at[ACROSS ? PASSES : 1];           // ACROSS: rows of the step that is loaded next, negative: none
+    const int32_t* list;                       // ACROSS
+    int limit, col0;                           // ACROSS: channels there are, and the tile's first
+    const char* ptr[PASSES];                   // of the step that is fetched next; ACROSS with a list: unused
+    int32_t at[ACROSS ? PASSES : 1];           // ACROSS with a list: its rows
     uint4 held[WHOLE ? 1 : PASSES];
 
     __device__ static int line_of(int i) { return (i * NTH + (int)threadIdx.x) / LINE; }
@@ -332,66 +349,104 @@ struct Loader {
         const int line = line_of(i), c = (int)threadIdx.x % LINE;
         return c ^ (ACROSS ? across_turn<DT, LINE>(line) : along_turn<LINE>(line));
     }
-    // ALONG: rows first .. of the operand, or of the list
-    __device__ void rows_along(int64_t first, int64_t end) {
-        if constexpr (!ACROSS) {
+    // ALONG: lines are rows begin .. of the operand, or those that the list names from there on.  Beyond the last, and for a row that is none,
+    // some other row is read: the results are not used.
+    __device__ void start_along(const int32_t* rows_list, int64_t begin, int64_t stop) {
+        first = 0;
 #pragma unroll
-            for (int i = 0; i < PASSES; ++i) {
-                const int64_t e = first + line_of(i);
-                int64_t r = e < end ? e : -1;
-                if (r >= 0 && list != nullptr) r = list[e];
-                row[i] = r >= 0 && r < rows ? base + r * ld : nullptr;
-            }
+        for (int i = 0; i < PASSES; ++i) {
+            int64_t r = begin + line_of(i);
+            if (r >= stop) r = stop - 1;
+            if (rows_list != nullptr) r = rows_list[r];
+            if (r < 0 || r >= rows) r = 0;
+            ptr[i] = base + r * ld + (int64_t)chunk_of(i) * 16;
         }
     }
-    // ACROSS: the rows of the lines of the step that starts at entry `first`
-    __device__ void rows_across(int64_t first) {
+    // ACROSS: columns beyond the last read some other chunk
+    __device__ const char* column(int i) const {
+        const int channel = col0 + chunk_of(i) * PER;
+        return base + (int64_t)(WHOLE && channel >= limit ? 0 : channel) * ELEM<DT>;
+    }
+    __device__ void start_across() {
+        if (list != nullptr) {
+            take_rows(0);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i) ptr[i] = column(i) + (first + line_of(i)) * ld;
+    }
+    __device__ void take_rows(int s) {
         if constexpr (ACROSS) {
 #pragma unroll
             for (int i = 0; i < PASSES; ++i) {
-                const int64_t e = first + line_of(i);
-                at[i] = e < last ? (int32_t)e : -1;
+                const int64_t e = first + (int64_t)s * STRIDE + line_of(i);
                 // not looked at before it is used, a step later: a comparison here would wait for it, and for the chunks ahead of it
-                if (list != nullptr && e < last) at[i] = list[e];
+                at[i] = -1;
+                if (e < end) at[i] = list[e];
             }
         }
     }
-    // ALONG: `k` is the step's first channel
-    __device__ void fetch(int k, uint32_t lds) {
+    __device__ void fetch(int s, uint32_t lds) {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int64_t from = first + (int64_t)s * STRIDE;
+        const bool listed = ACROSS && list != nullptr;
+        if constexpr (WHOLE) {             // channels are whole chunks, rows aligned
+            const void* const none = &g_no_chunk;
+            if (listed) {
 #pragma unroll
-        for (int i = 0; i < PASSES; ++i) {
-            const int channel = (ACROSS ? col0 : k) + chunk_of(i) * PER;
-            const char* line;
-            bool ok;
-            if constexpr (ACROSS) {
-                ok = at[i] >= 0 && at[i] < rows;
-                line = base + (int64_t)(ok ? at[i] : 0) * ld;
+                for (int i = 0; i < PASSES; ++i) {
+                    const int32_t r = at[ACROSS ? i : 0];
+                    load_to_lds((uint32_t)r < (uint32_t)rows ? (const void*)(column(i) + (int64_t)r * ld) : none, lds + (i * NTH + wave * 64) * 16);
+                }
+            } else if (from + STRIDE <= end) {
+                const int64_t step = ACROSS ? STRIDE * ld : STRIDE * ELEM<DT>;
+#pragma unroll
+                for (int i = 0; i < PASSES; ++i) {
+                    load_to_lds(ptr[i], lds + (i * NTH + wave * 64) * 16);
+                    ptr[i] += step;
+                }
             } else {
-                ok = row[i] != nullptr;
-                line = row[i];
+                const int left = end > from ? (int)(end - from) : 0;
+#pragma unroll
+                for (int i = 0; i < PASSES; ++i)
+                    load_to_lds((ACROSS ? line_of(i) : chunk_of(i) * PER) < left ? (const void*)ptr[i] : none, lds + (i * NTH + wave * 64) * 16);
             }
-            const char* p = line + (int64_t)channel * ELEM<DT>;
-            if constexpr (WHOLE) {         // channels are whole chunks
-                const void* src = ok && channel < limit ? (const void*)p : (const void*)&g_no_chunk;
-                load_to_lds(src, __builtin_amdgcn_readfirstlane(lds + (i * NTH + wave * 64) * 16));
-            } else {
+        } else {
+            const int64_t step = ACROSS ? STRIDE * ld : STRIDE * ELEM<DT>;
+#pragma unroll
+            for (int i = 0; i < PASSES; ++i) {
+                const char* p = ptr[i];
+                int there;                 // elements of the chunk
+                if (ACROSS) {
+                    there = limit - (col0 + chunk_of(i) * PER);
+                    bool ok = from + line_of(i) < end;
+                    if (listed) {
+                        const int32_t r = at[ACROSS ? i : 0];
+                        ok = (uint32_t)r < (uint32_t)rows;
+                        p = column(i) + (int64_t)r * ld;
+                    }
+                    if (!ok) there = 0;
+                } else {
+                    there = (int)(end - from) - chunk_of(i) * PER;
+                }
                 uint4 v = make_uint4(0, 0, 0, 0);
-                if (ok && channel + PER <= limit) {
+                if (there >= PER) {
                     v = load_chunk(p);
-                } else if (ok) {
+                } else if (there > 0) {
                     uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
                     for (int j = 0; j < PER; ++j)
-                        if (channel + j < limit) {
+                        if (j < there) {
                             if constexpr (DT == SC_F32) w[j] = reinterpret_cast<const uint32_t*>(p)[j];
                             else w[j / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[j] << (16 * (j & 1));
                         }
                     v = make_uint4(w[0], w[1], w[2], w[3]);
                 }
                 held[i] = v;
+                ptr[i] += step;
             }
         }
+        if (listed) take_rows(s + 1);
     }
     __device__ void put(uint4* tile) {
         if constexpr (!WHOLE) {
@@ -423,19 +478,20 @@ __global__ void __launch_bounds__(64 * WM * WN * KW)
 k_product(const Product p) {
     using S = ProductShape<DT, MODE, BM, BN, WM, WN, KW>;
     constexpr int NTH = S::NTH, TM = S::TM, TN = S::TN;
-    constexpr bool DEALT = TN % 2 == 0;
     extern __shared__ __align__(16) uint4 product_lds[];
 
-    const int64_t unit = xcd_unit(blockIdx.y * gridDim.x + blockIdx.x, gridDim.x * gridDim.y);
-    const int n_tiles = (p.N + BN - 1) / BN;
-    int64_t row_unit;
+    // runs of consecutive tiles, which share rows, go to one XCD; those that do not exist after all are the last of every XCD
+    const uint32_t block = blockIdx.y * gridDim.x + blockIdx.x, turn = block / NUM_XCD, run = (uint32_t)p.run;
+    const uint32_t unit = (turn / run * NUM_XCD + block % NUM_XCD) * run + turn % run;
+    const uint32_t n_tiles = (uint32_t)(p.N + BN - 1) / BN;
+    uint32_t row_unit;
     int m_tile = 0, n_tile;
     if constexpr (MODE == PRODUCT_DW) {
-        const int m_tiles = p.M > BM ? (p.M + BM - 1) / BM : 1;
+        const uint32_t m_tiles = p.M > BM ? (uint32_t)(p.M + BM - 1) / BM : 1u;
         row_unit = unit / (m_tiles * n_tiles);
-        const int tile = (int)(unit - row_unit * (m_tiles * n_tiles));
-        m_tile = tile / n_tiles;
-        n_tile = tile - m_tile * n_tiles;
+        const uint32_t tile = unit - row_unit * (m_tiles * n_tiles);
+        m_tile = (int)(tile / n_tiles);
+        n_tile = (int)(tile - m_tile * n_tiles);
     } else {
         row_unit = unit / n_tiles;
         n_tile = (int)(unit - row_unit * n_tiles);
@@ -451,57 +507,79 @@ k_product(const Product p) {
     const int n0 = n_tile * BN, m0 = m_tile * BM;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)product_lds;
 
-    Loader<DT, S::A_ACROSS, S::A_LINES, S::A_LINE, NTH, WHOLE> la;
-    Loader<DT, S::B_ACROSS, S::B_LINES, S::B_LINE, NTH, WHOLE> lb;
+    constexpr int STRIDE = S::STEP * KW;
+    Loader<DT, S::A_ACROSS, S::A_LINES, S::A_LINE, NTH, STRIDE, WHOLE> la;
+    Loader<DT, S::B_ACROSS, S::B_LINES, S::B_LINE, NTH, STRIDE, WHOLE> lb;
     la.base = (const char*)p.a;
     la.ld = p.lda * ELEM<DT>;
     la.rows = p.a_rows;
-    la.list = p.a_list;
-    la.last = part.last;
-    la.limit = MODE == PRODUCT_DW ? p.M : p.K;
-    la.col0 = m0;
     lb.ld = p.ldb * ELEM<DT>;
-    lb.col0 = n0;
     int64_t depth;                                      // of the summed axis
+    int32_t row_of[TM];                                 // the lane's rows of the operand, as the list has them
     if constexpr (MODE == PRODUCT_DW) {
+        depth = part.last - part.first;
+        la.list = p.a_list;
+        la.first = part.first;
+        la.end = p.a_list != nullptr || p.a_rows > part.last ? part.last : p.a_rows;
+        la.limit = p.M;
+        la.col0 = m0;
+        if (p.M == 0) {                                 // sums of b's rows only: zeros for a
+            la.base = (const char*)&g_no_chunk;
+            la.ld = 0;
+            la.list = nullptr;
+            la.end = part.last;
+        }
+        la.start_across();
         lb.base = (const char*)p.b;
         lb.rows = p.b_rows;
         lb.list = p.b_list;
-        lb.last = part.last;
+        lb.first = part.first;
+        lb.end = p.b_list != nullptr || p.b_rows > part.last ? part.last : p.b_rows;
         lb.limit = p.N;
-        depth = part.last - part.first;
-        la.rows_across(part.first);
-        lb.rows_across(part.first);
+        lb.col0 = n0;
+        lb.start_across();
     } else {
-        lb.base = (const char*)p.b + (int64_t)g * p.K * p.N * ELEM<DT>;
-        lb.list = nullptr;
-        depth = p.K;
-        la.rows_along(part.first, part.last);
-        if constexpr (MODE == PRODUCT_FWD) {
-            lb.rows = p.K;
-            lb.last = p.K;
-            lb.limit = p.N;
-            lb.rows_across(0);
-        } else {
-            lb.rows = p.N;
-            lb.limit = p.K;
-            lb.rows_along(n0, p.N);
+        depth = p.a_rows > 0 ? p.K : 0;
+#pragma unroll
+        for (int tm = 0; tm < TM; ++tm) {
+            const int64_t e = part.first + wm * TM * 16 + tm * 16 + i;
+            row_of[tm] = (int32_t)e;
+            if (p.a_list != nullptr && e < part.last) row_of[tm] = p.a_list[e];
+        }
+        if (depth > 0) {
+            la.list = nullptr;
+            la.end = p.K;
+            la.start_along(p.a_list, part.first, part.last);
+            lb.base = (const char*)p.b + (int64_t)g * p.K * p.N * ELEM<DT>;
+            lb.list = nullptr;
+            lb.first = 0;
+            lb.end = p.K;
+            if constexpr (MODE == PRODUCT_FWD) {
+                lb.rows = p.K;
+                lb.limit = p.N;
+                lb.col0 = n0;
+                lb.start_across();
+            } else {
+                lb.rows = p.N;
+                lb.start_along(nullptr, n0, p.N);
+            }
         }
     }
-    constexpr int STRIDE = S::STEP * KW;
     const int steps = (int)((depth + STRIDE - 1) / STRIDE);
     auto fetch = [&](int s) __attribute__((always_inline)) {
         const uint32_t at = lds0 + (s & 1) * S::BUFFER;
-        la.fetch(s * STRIDE, at);
-        lb.fetch(s * STRIDE, at + S::A_CHUNKS * 16);
-        if constexpr (S::A_ACROSS) la.rows_across(part.first + (int64_t)(s + 1) * STRIDE);
-        if constexpr (S::B_ACROSS) lb.rows_across((MODE == PRODUCT_DW ? part.first : 0) + (int64_t)(s + 1) * STRIDE);
+        la.fetch(s, at);
+        lb.fetch(s, at + S::A_CHUNKS * 16);
     };
     auto put = [&](int s) __attribute__((always_inline)) {
         uint4* at = product_lds + (s & 1) * (S::BUFFER / 16);
         la.put(at);
         lb.put(at + S::A_CHUNKS);
     };
+    typename std::conditional<S::A_ACROSS, AcrossReader<DT, S::A_LINE, TM>, AlongReader<DT, S::A_LINE, TM>>::type ra(
+        lds0, wm * TM * 16, set * (S::A_ACROSS ? S::STEP : 8));
+    typename std::conditional<S::B_ACROSS, AcrossReader<DT, S::B_LINE, TN>, AlongReader<DT, S::B_LINE, TN>>::type rb(
+        lds0 + S::A_CHUNKS * 16, wn * TN * 16, set * (S::B_ACROSS ? S::STEP : 8));
 
     f32x4 acc[TM][TN], ones_sum[TN];
 #pragma unroll
@@ -521,21 +599,14 @@ k_product(const Product p) {
         if constexpr (WHOLE) __builtin_amdgcn_s_waitcnt(0x0f70);       // vmcnt(0): the step's chunks are in LDS
         lds_barrier();                                 // ... of all wavefronts, which are done with the other buffer
         if (s + 1 < steps) fetch(s + 1);
-        const uint4* ta = product_lds + (s & 1) * (S::BUFFER / 16);
-        const uint4* tb = ta + S::A_CHUNKS;
+        const uint32_t buffer = (s & 1) * S::BUFFER;
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             uint4 fa[TM], fb[TN];
 #pragma unroll
-            for (int tn = 0; tn < TN; ++tn) {
-                if constexpr (S::B_ACROSS) fb[tn] = operand_across<DT, S::B_LINE, DEALT>(tb, wn * TN * 16, tn, set * S::STEP, c, i, o);
-                else fb[tn] = operand_along<DT, S::B_LINE, DEALT>(tb, wn * TN * 16, tn, set * 8, c, i, o);
-            }
+            for (int tn = 0; tn < TN; ++tn) fb[tn] = rb.read(buffer, tn, c);
 #pragma unroll
-            for (int tm = 0; tm < TM; ++tm) {
-                if constexpr (S::A_ACROSS) fa[tm] = operand_across<DT, S::A_LINE, false>(ta, wm * TM * 16, tm, set * S::STEP, c, i, o);
-                else fa[tm] = operand_along<DT, S::A_LINE, false>(ta, wm * TM * 16, tm, set * 8, c, i, o);
-            }
+            for (int tm = 0; tm < TM; ++tm) fa[tm] = ra.read(buffer, tm, c);
 #pragma unroll
             for (int tm = 0; tm < TM; ++tm)
 #pragma unroll
@@ -578,13 +649,26 @@ k_product(const Product p) {
                 }
     }
 
-    // A lane has columns 4 o .. 4 o + 3 of every block's 16 and row i: eight in a row from two blocks.
-    constexpr int PAIRS = DEALT ? TN / 2 : TN, WIDTH = DEALT ? 8 : 4;
-    const int col_lane = n0 + wn * TN * 16 + WIDTH * o;
+    // A lane has columns 4 o .. 4 o + 3 of every block's 16 and row i.  Two blocks' odd rows of lanes and even ones change places, and it has eight in a row.
+    static_assert(TN % 2 == 0, "blocks by pairs");
+    auto eight = [](const f32x4& x, const f32x4& y, float (&v)[8]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int u = 0; u < PAIRS; ++u) {
-        const int col = col_lane + (DEALT ? 32 : 16) * u;
-        const int there = p.N - col < WIDTH ? p.N - col : WIDTH;
+        for (int j = 0; j < 4; ++j) {
+            const auto pair = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, (float)x[j]), __builtin_bit_cast(uint32_t, (float)y[j]), false, false);
+            v[j] = __builtin_bit_cast(float, (uint32_t)pair[0]);
+            v[4 + j] = __builtin_bit_cast(float, (uint32_t)pair[1]);
+        }
+    };
+    const int col_lane = n0 + wn * TN * 16 + 16 * (o & 1) + 8 * (o >> 1);
+#pragma unroll
+    for (int u = 0; u < TN / 2; ++u) {
+        const int col = col_lane + 32 * u;
+        const int there = p.N - col < 8 ? p.N - col : 8;
+        float sum[8];
+        if constexpr (MODE == PRODUCT_DW) eight(ones_sum[2 * u], ones_sum[2 * u + 1], sum);
+        float vs[TM][8];
+#pragma unroll
+        for (int tm = 0; tm < TM; ++tm) eight(acc[tm][2 * u], acc[tm][2 * u + 1], vs[tm]);
         if (there <= 0) continue;
         float bias[8];
         if constexpr (MODE == PRODUCT_FWD) {
@@ -594,19 +678,14 @@ k_product(const Product p) {
         }
         if constexpr (MODE == PRODUCT_DW) {
             if (sums && i == 0) {
-                float v[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = j < WIDTH ? ones_sum[DEALT ? 2 * u + (j >> 2) : u][j & 3] : 0.f;
-                if (part.parts > 1) store8<SC_F32>(p.partial, (part.slot * (p.M + 1) + p.M) * p.N + col, there, v);
-                else store8<DT>(p.out_bias, (int64_t)g * p.N + col, there, v);
+                if (part.parts > 1) store8<SC_F32>(p.partial, (part.slot * (p.M + 1) + p.M) * p.N + col, there, sum);
+                else store8<DT>(p.out_bias, (int64_t)g * p.N + col, there, sum);
             }
         }
 #pragma unroll
         for (int tm = 0; tm < TM; ++tm) {
             const int r = wm * TM * 16 + tm * 16 + i;
-            float v[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = j < WIDTH ? acc[tm][DEALT ? 2 * u + (j >> 2) : u][j & 3] : 0.f;
+            float (&v)[8] = vs[tm];
             if constexpr (MODE == PRODUCT_DW) {
                 const int m = m0 + r;
                 if (m >= p.M) continue;
@@ -615,6 +694,10 @@ k_product(const Product p) {
             } else {
                 const int64_t e = part.first + r;
                 if (e >= part.last) continue;
+                if (row_of[tm] < 0 || row_of[tm] >= p.a_rows) {         // no such row: zeros
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] = 0.f;
+                }
                 if constexpr (MODE == PRODUCT_FWD) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) v[j] += bias[j];
@@ -655,11 +738,12 @@ int run_product(Product p, hipStream_t s) {
     using S = ProductShape<DT, MODE, BM, BN, WM, WN, KW>;
     const int64_t n_tiles = (p.N + BN - 1) / BN, m_tiles = MODE == PRODUCT_DW && p.M > BM ? (p.M + BM - 1) / BM : 1;
     if (MODE != PRODUCT_DW) {
-        const int64_t tails = p.starts == nullptr ? 1 : p.groups < p.n ? p.groups : p.n;
-        p.units = p.n / BM + tails;                    // a tile that is not full per group, and those that are
+        // groups: the tiles that are full, and one that is not of every group that there can be
+        p.units = p.starts == nullptr ? (p.n + BM - 1) / BM : p.n / BM + (p.groups < p.n ? p.groups : p.n);
     }
-    const int64_t blocks = (p.units * n_tiles * m_tiles + NUM_XCD - 1) / NUM_XCD * NUM_XCD;
-    if (blocks > INT32_MAX) return SC_EINVAL;
+    p.run = (int)product_run(p.units, n_tiles * m_tiles);
+    const int64_t turns = NUM_XCD * (int64_t)p.run, blocks = (p.units * n_tiles * m_tiles + turns - 1) / turns * turns;
+    if (blocks > INT32_MAX - 2 * GRID_COLUMNS) return SC_EINVAL;
     const dim3 grid((unsigned)grid_columns(blocks), (unsigned)grid_rows(blocks));
     const int64_t depth = MODE == PRODUCT_DW ? p.per : p.K;
     const size_t lds = S::lds(depth > S::STEP * KW);
@@ -680,14 +764,20 @@ int choose_product(const Product& p, bool whole, int cus, hipStream_t s) {
     if constexpr (MODE == PRODUCT_DW) {
         switch (weight_tile(p.M, p.N)) {
             case 64: return run_product<DT, MODE, 64, 64, 2, 2, 1>(p, whole, s);
-            default: return run_product<DT, MODE, 128, 128, 2, 2, 1>(p, whole, s);
+            case 128: return run_product<DT, MODE, 128, 128, 2, 2, 1>(p, whole, s);
+            default:
+                if constexpr (DT != SC_F32) return run_product<DT, MODE, 256, 256, 2, 4, 1>(p, whole, s);
+                else return run_product<DT, MODE, 128, 128, 2, 2, 1>(p, whole, s);
         }
     } else {
         switch (row_tile(p.n, p.starts == nullptr ? 1 : p.groups, p.N, p.K)) {
             case ROWS_FEW: return run_product<DT, MODE, 16, 64, 1, 1, 4>(p, whole, s);
             case COLUMNS_32: return run_product<DT, MODE, 128, 32, 4, 1, 1>(p, whole, s);
             case COLUMNS_64: return run_product<DT, MODE, 128, 64, 4, 1, 1>(p, whole, s);
-            default: return run_product<DT, MODE, 128, 128, 2, 2, 1>(p, whole, s);
+            case TILE_128: return run_product<DT, MODE, 128, 128, 2, 2, 1>(p, whole, s);
+            default:
+                if constexpr (DT != SC_F32) return run_product<DT, MODE, 256, 256, 2, 4, 1>(p, whole, s);
+                else return run_product<DT, MODE, 128, 128, 2, 2, 1>(p, whole, s);
         }
     }
 }

@@ -178,11 +178,16 @@ constexpr int64_t grid_rows(int64_t groups) { return (groups + GRID_COLUMNS - 1)
 
 // ---- products of rows and weights (sc_product.h) --------------------------------------------------------
 // Tile of the result that a workgroup owns, by the rows and columns there are.  Few rows a group: 16 rows, four wavefronts share the summed axis.
-enum RowTile { ROWS_FEW, COLUMNS_32, COLUMNS_64, TILE_128 };
+enum RowTile { ROWS_FEW, COLUMNS_32, COLUMNS_64, TILE_128, TILE_256 };
 constexpr RowTile row_tile(int64_t entries, int64_t groups, int64_t columns, int64_t depth) {
-    (void)depth;
     if (entries <= 32 * (groups < entries ? groups : entries)) return ROWS_FEW;
-    return columns <= 32 ? COLUMNS_32 : columns <= 64 ? COLUMNS_64 : TILE_128;
+    if (columns <= 64) return columns <= 32 ? COLUMNS_32 : COLUMNS_64;
+    return depth >= 512 && columns >= 256 && (entries / 256) * (columns / 256) >= 192 ? TILE_256 : TILE_128;
+}
+// Consecutive tiles that one XCD takes: those of the same rows, which its L2 then holds, as long as every XCD has eight runs.
+constexpr int64_t product_run(int64_t units, int64_t tiles_each) {
+    const int64_t run = units * tiles_each / 64;
+    return run < 1 ? 1 : run < tiles_each ? run : tiles_each;
 }
 // Tile of a weight gradient.
 constexpr int weight_tile(int64_t c_in, int64_t c_out) { return c_in <= 64 && c_out <= 64 ? 64 : 128; }
