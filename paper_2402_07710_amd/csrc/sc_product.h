@@ -12,8 +12,8 @@
 // read turns into operand order on the way to the registers, so nothing is ever re-laid out in memory.  Chunks of 16 bytes are permuted inside a
 // line by the line's number so that the lanes of one LDS access meet different banks; the permutation is in the address that a lane
 // loads from, because a load into LDS fills it in the order of the lanes.
-// The weights' side is the matrix instruction's first operand, so that a lane ends up with consecutive columns of one row; the
-// columns are dealt to pairs of 16-column blocks such that there are eight of them: 16 bytes of 16-bit results, a row's 64 bytes by four lanes.
+// The weights' side is the matrix instruction's first operand, so that a lane ends up with four consecutive columns of one row, which
+// pass through LDS once more on their way out.
 #pragma once
 
 #include <type_traits>
@@ -172,6 +172,19 @@ __device__ inline float activate(float v, int act) {
     return fmaxf(v, -3.4e38f) * w;                      // a NaN is in w as well
 }
 template <int DT>
+__device__ inline void activate8(float (&v)[8], int act) {       // one look at the kind for all of them
+    if (act == SC_ACT_GELU) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = activate<DT>(v[j], SC_ACT_GELU);
+    } else if (act == SC_ACT_SILU) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = activate<DT>(v[j], SC_ACT_SILU);
+    } else if (act == SC_ACT_RELU) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = activate<DT>(v[j], SC_ACT_RELU);
+    }
+}
+template <int DT>
 __device__ inline float slope(float v, int act) {
     if (act == SC_ACT_RELU) return v > 0.f || v != v ? 1.f : 0.f;
     if (act == SC_ACT_NONE) return 1.f;
@@ -258,7 +271,7 @@ __device__ __align__(16) uint4 g_no_chunk;
 // fills the 64 banks once.
 // ALONG: lines are rows of the tile, LINE chunks of the summed axis; 16 lanes read one chunk of 16 lines.
 template <int LINE>
-__device__ constexpr int along_turn(int line) { return LINE == 8 ? (line >> 1) & 7 : line & 7; }
+__device__ constexpr int along_turn(int line) { return LINE == 4 ? (line >> 2) & 3 : LINE == 8 ? (line >> 1) & 7 : line & 7; }
 // ACROSS: lines are places on the summed axis, LINE chunks of tile rows.  32 lanes of a 16-bit read take 32 bytes of four lines and of the four that
 // are 8 further on, 64 lanes of a 32-bit one 64 bytes of lines 0, 4, 8 and 12.
 template <int DT, int LINE>
@@ -273,18 +286,18 @@ typedef __attribute__((address_space(3))) const u32x4* lds_u32x4;
 typedef __attribute__((address_space(3))) const uint32_t* lds_uint32;
 
 // LDS addresses from which a lane reads its operands of T blocks of 16 rows, in the first buffer
-template <int DT, int LINE, int T>
+template <int DT, int LINE, int T, int PARTS>
 struct AlongReader {
-    uint32_t at[2];
+    uint32_t at[PARTS];
     // row0: the wavefront's first row; chunk0: its set's first chunk; both multiples that leave the turn alone
     __device__ AlongReader(uint32_t tile, int row0, int chunk0) {
         const int i = threadIdx.x & 15, o = (threadIdx.x >> 4) & 3;
-        for (int c = 0; c < 2; ++c) at[c] = tile + ((row0 + i) * LINE + chunk0 + ((4 * c + o) ^ along_turn<LINE>(i))) * 16;
+        for (int c = 0; c < PARTS; ++c) at[c] = tile + ((row0 + i) * LINE + chunk0 + ((4 * c + o) ^ along_turn<LINE>(i))) * 16;
     }
     // block t, chunks 4 c .. 4 c + 3, a chunk for each 16 lanes
     __device__ uint4 read(uint32_t buffer, int t, int c) const { return __builtin_bit_cast(uint4, *(lds_u32x4)(at[c] + buffer + t * (16 * LINE * 16))); }
 };
-template <int DT, int LINE, int T>
+template <int DT, int LINE, int T, int PARTS>
 struct AcrossReader {
     uint32_t at[T];
     __device__ AcrossReader(uint32_t tile, int col0, int line0) {
@@ -457,26 +470,36 @@ struct Loader {
 };
 
 // ---- the kernel -----------------------------------------------------------------------------------------
-// WM x WN wavefronts share a tile, KW sets of them the summed axis.  WHOLE: rows and channels are whole chunks of 16 bytes, aligned;
-// otherwise chunks pass through registers, by unaligned loads, element by element at the end of a row.
-template <int DT, int MODE, int BM_, int BN_, int WM_, int WN_, int KW_>
+// WM x WN wavefronts share a tile, KW sets of them the summed axis, of which a set takes SB bytes a step; STAGES buffers.  WHOLE: rows and
+// channels are whole chunks of 16 bytes, aligned; otherwise chunks pass through registers, by unaligned loads, element by element at the end of a row.
+template <int DT, int MODE, int BM_, int BN_, int WM_, int WN_, int KW_, int SB_, int STAGES_>
 struct ProductShape {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KW = KW_;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KW = KW_, SB = SB_, STAGES = STAGES_;
     static constexpr int NTH = 64 * WM * WN * KW, TM = BM / 16 / WM, TN = BN / 16 / WN;
-    static constexpr int STEP = 128 / ELEM<DT>;                       // places on the summed axis per set and step
+    static constexpr int STEP = SB / ELEM<DT>;                        // places on the summed axis per set and step
     static constexpr bool A_ACROSS = MODE == PRODUCT_DW, B_ACROSS = MODE != PRODUCT_DX;
-    static constexpr int A_LINES = A_ACROSS ? STEP * KW : BM, A_LINE = A_ACROSS ? BM * ELEM<DT> / 16 : 8 * KW;
-    static constexpr int B_LINES = B_ACROSS ? STEP * KW : BN, B_LINE = B_ACROSS ? BN * ELEM<DT> / 16 : 8 * KW;
+    static constexpr int A_LINES = A_ACROSS ? STEP * KW : BM, A_LINE = A_ACROSS ? BM * ELEM<DT> / 16 : SB / 16 * KW;
+    static constexpr int B_LINES = B_ACROSS ? STEP * KW : BN, B_LINE = B_ACROSS ? BN * ELEM<DT> / 16 : SB / 16 * KW;
     static constexpr int A_CHUNKS = A_LINES * A_LINE, B_CHUNKS = B_LINES * B_LINE;
     static constexpr int BUFFER = (A_CHUNKS + B_CHUNKS) * 16;
     static constexpr int SUMS = (KW - 1) * WM * WN * TM * TN * 64 * 16;  // what the sets hand over in the end
-    static constexpr int lds(bool several_steps) { return (several_steps ? 2 : 1) * BUFFER > SUMS ? (several_steps ? 2 : 1) * BUFFER : SUMS; }
+    static constexpr int PIECES = WM * WN * 16 * (TN * 16 + 4) * 4;      // results on their way out
+    static constexpr int lds(int64_t steps) {
+        const int buffers = (steps < STAGES ? (int)steps : STAGES) * BUFFER, end = SUMS > PIECES ? SUMS : PIECES;
+        return buffers > end ? buffers : end;
+    }
 };
 
-template <int DT, int MODE, int BM, int BN, int WM, int WN, int KW, bool WHOLE>
+// entry m names no row of a
+__device__ inline bool no_row(const Product& p, int64_t m) {
+    const int64_t r = p.a_list != nullptr ? p.a_list[m] : m;
+    return r < 0 || r >= p.a_rows;
+}
+
+template <int DT, int MODE, int BM, int BN, int WM, int WN, int KW, int SB, int STAGES, bool WHOLE>
 __global__ void __launch_bounds__(64 * WM * WN * KW)
 k_product(const Product p) {
-    using S = ProductShape<DT, MODE, BM, BN, WM, WN, KW>;
+    using S = ProductShape<DT, MODE, BM, BN, WM, WN, KW, SB, STAGES>;
     constexpr int NTH = S::NTH, TM = S::TM, TN = S::TN;
     extern __shared__ __align__(16) uint4 product_lds[];
 
@@ -515,7 +538,6 @@ k_product(const Product p) {
     la.rows = p.a_rows;
     lb.ld = p.ldb * ELEM<DT>;
     int64_t depth;                                      // of the summed axis
-    int32_t row_of[TM];                                 // the lane's rows of the operand, as the list has them
     if constexpr (MODE == PRODUCT_DW) {
         depth = part.last - part.first;
         la.list = p.a_list;
@@ -540,12 +562,6 @@ k_product(const Product p) {
         lb.start_across();
     } else {
         depth = p.a_rows > 0 ? p.K : 0;
-#pragma unroll
-        for (int tm = 0; tm < TM; ++tm) {
-            const int64_t e = part.first + wm * TM * 16 + tm * 16 + i;
-            row_of[tm] = (int32_t)e;
-            if (p.a_list != nullptr && e < part.last) row_of[tm] = p.a_list[e];
-        }
         if (depth > 0) {
             la.list = nullptr;
             la.end = p.K;
@@ -567,19 +583,19 @@ k_product(const Product p) {
     }
     const int steps = (int)((depth + STRIDE - 1) / STRIDE);
     auto fetch = [&](int s) __attribute__((always_inline)) {
-        const uint32_t at = lds0 + (s & 1) * S::BUFFER;
+        const uint32_t at = lds0 + s % STAGES * S::BUFFER;
         la.fetch(s, at);
         lb.fetch(s, at + S::A_CHUNKS * 16);
     };
     auto put = [&](int s) __attribute__((always_inline)) {
-        uint4* at = product_lds + (s & 1) * (S::BUFFER / 16);
+        uint4* at = product_lds + s % STAGES * (S::BUFFER / 16);
         la.put(at);
         lb.put(at + S::A_CHUNKS);
     };
-    typename std::conditional<S::A_ACROSS, AcrossReader<DT, S::A_LINE, TM>, AlongReader<DT, S::A_LINE, TM>>::type ra(
-        lds0, wm * TM * 16, set * (S::A_ACROSS ? S::STEP : 8));
-    typename std::conditional<S::B_ACROSS, AcrossReader<DT, S::B_LINE, TN>, AlongReader<DT, S::B_LINE, TN>>::type rb(
-        lds0 + S::A_CHUNKS * 16, wn * TN * 16, set * (S::B_ACROSS ? S::STEP : 8));
+    typename std::conditional<S::A_ACROSS, AcrossReader<DT, S::A_LINE, TM, SB / 64>, AlongReader<DT, S::A_LINE, TM, SB / 64>>::type ra(
+        lds0, wm * TM * 16, set * (S::A_ACROSS ? S::STEP : SB / 16));
+    typename std::conditional<S::B_ACROSS, AcrossReader<DT, S::B_LINE, TN, SB / 64>, AlongReader<DT, S::B_LINE, TN, SB / 64>>::type rb(
+        lds0 + S::A_CHUNKS * 16, wn * TN * 16, set * (S::B_ACROSS ? S::STEP : SB / 16));
 
     f32x4 acc[TM][TN], ones_sum[TN];
 #pragma unroll
@@ -591,17 +607,26 @@ k_product(const Product p) {
     const bool sums = MODE == PRODUCT_DW && p.out_bias != nullptr && m_tile == 0 && wm == 0;
     const uint32_t one = DT == SC_F32 ? 0x3f800000u : DT == SC_F16 ? 0x3c003c00u : 0x3f803f80u;
 
+    // A step's chunks are asked for STAGES - 1 steps ahead, into the buffer that was read last.
+    static_assert(STAGES == 2 || (STAGES == 3 && WHOLE), "chunks in registers: one step ahead");
+    constexpr int LOADS = S::A_CHUNKS / NTH + S::B_CHUNKS / NTH;
     if (steps > 0) {
         fetch(0);
         put(0);
+        if (STAGES == 3 && steps > 1) fetch(1);
     }
+    int at_stage = 0;
     for (int s = 0; s < steps; ++s) {
-        if constexpr (WHOLE) __builtin_amdgcn_s_waitcnt(0x0f70);       // vmcnt(0): the step's chunks are in LDS
+        if constexpr (WHOLE) {                         // the step's chunks are in LDS; those of the next may still be on their way
+            if (STAGES == 3 && s + 1 < steps) __builtin_amdgcn_s_waitcnt(0x0f70 | (LOADS & 15) | (LOADS >> 4) << 14);
+            else __builtin_amdgcn_s_waitcnt(0x0f70);
+        }
         lds_barrier();                                 // ... of all wavefronts, which are done with the other buffer
-        if (s + 1 < steps) fetch(s + 1);
-        const uint32_t buffer = (s & 1) * S::BUFFER;
+        if (s + STAGES - 1 < steps) fetch(s + STAGES - 1);
+        const uint32_t buffer = at_stage * S::BUFFER;
+        at_stage = at_stage + 1 < STAGES ? at_stage + 1 : 0;
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
+        for (int c = 0; c < SB / 64; ++c) {
             uint4 fa[TM], fb[TN];
 #pragma unroll
             for (int tn = 0; tn < TN; ++tn) fb[tn] = rb.read(buffer, tn, c);
@@ -618,7 +643,7 @@ k_product(const Product p) {
                 }
             }
         }
-        if (s + 1 < steps) put(s + 1);
+        if (!WHOLE && s + 1 < steps) put(s + 1);
     }
 
     if constexpr (KW > 1) {                            // the sets' sums, in the order of the sets
@@ -647,54 +672,45 @@ k_product(const Product p) {
                     acc[tm][tn][2] += v.z;
                     acc[tm][tn][3] += v.w;
                 }
+        static_assert(WM * WN == 1, "the pieces lie over the sums, which other wavefronts may still read");
     }
 
-    // A lane has columns 4 o .. 4 o + 3 of every block's 16 and row i.  Two blocks' odd rows of lanes and even ones change places, and it has eight in a row.
+    // A lane has columns 4 o .. 4 o + 3 of every block's 16 and row i.  Two blocks' odd and even rows of lanes change places, and it has eight
+    // columns in a row of one block; four lanes have 32 columns of a row.
+    constexpr int COLS = TN * 16;
     static_assert(TN % 2 == 0, "blocks by pairs");
-    auto eight = [](const f32x4& x, const f32x4& y, float (&v)[8]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const auto pair = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, (float)x[j]), __builtin_bit_cast(uint32_t, (float)y[j]), false, false);
-            v[j] = __builtin_bit_cast(float, (uint32_t)pair[0]);
-            v[4 + j] = __builtin_bit_cast(float, (uint32_t)pair[1]);
-        }
-    };
-    const int col_lane = n0 + wn * TN * 16 + 16 * (o & 1) + 8 * (o >> 1);
+    const int col_wave = n0 + wn * COLS;
+    const int64_t first_row = (MODE == PRODUCT_DW ? m0 : part.first) + wm * TM * 16, end_row = MODE == PRODUCT_DW ? p.M : part.last;
+    const int64_t slot_row = part.slot * (p.M + 1);    // DW, several parts: rows of sums in front of this part's
+    const bool to_partial = MODE == PRODUCT_DW && part.parts > 1;
+    const void* const bias_row = MODE == PRODUCT_FWD && p.bias != nullptr ? (const char*)p.bias + (int64_t)g * p.N * ELEM<DT> : nullptr;
+    int whole_cols = 0;                                // of the wavefront's columns, those in whole pairs of blocks
 #pragma unroll
     for (int u = 0; u < TN / 2; ++u) {
-        const int col = col_lane + 32 * u;
-        const int there = p.N - col < 8 ? p.N - col : 8;
-        float sum[8];
-        if constexpr (MODE == PRODUCT_DW) eight(ones_sum[2 * u], ones_sum[2 * u + 1], sum);
-        float vs[TM][8];
-#pragma unroll
-        for (int tm = 0; tm < TM; ++tm) eight(acc[tm][2 * u], acc[tm][2 * u + 1], vs[tm]);
-        if (there <= 0) continue;
+        if (col_wave + 32 * u + 32 > p.N) break;
+        whole_cols = 32 * u + 32;
+        const int col = col_wave + 32 * u + 16 * (o & 1) + 8 * (o >> 1);
         float bias[8];
-        if constexpr (MODE == PRODUCT_FWD) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) bias[j] = 0.f;
-            if (p.bias != nullptr) load8<DT>(p.bias, (int64_t)g * p.N + col, there, bias);
-        }
-        if constexpr (MODE == PRODUCT_DW) {
-            if (sums && i == 0) {
-                if (part.parts > 1) store8<SC_F32>(p.partial, (part.slot * (p.M + 1) + p.M) * p.N + col, there, sum);
-                else store8<DT>(p.out_bias, (int64_t)g * p.N + col, there, sum);
-            }
-        }
+        for (int j = 0; j < 8; ++j) bias[j] = 0.f;
+        if (bias_row != nullptr) load8<DT>(bias_row, col, 8, bias);
 #pragma unroll
         for (int tm = 0; tm < TM; ++tm) {
-            const int r = wm * TM * 16 + tm * 16 + i;
-            float (&v)[8] = vs[tm];
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const auto pair = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, (float)acc[tm][2 * u][j]),
+                                                                   __builtin_bit_cast(uint32_t, (float)acc[tm][2 * u + 1][j]), false, false);
+                v[j] = __builtin_bit_cast(float, (uint32_t)pair[0]);
+                v[4 + j] = __builtin_bit_cast(float, (uint32_t)pair[1]);
+            }
+            const int64_t m = first_row + tm * 16 + i;
+            if (m >= end_row) continue;
             if constexpr (MODE == PRODUCT_DW) {
-                const int m = m0 + r;
-                if (m >= p.M) continue;
-                if (part.parts > 1) store8<SC_F32>(p.partial, (part.slot * (p.M + 1) + m) * p.N + col, there, v);
-                else store8<DT>(p.out, ((int64_t)g * p.M + m) * p.N + col, there, v);
+                if (to_partial) store8<SC_F32>(p.partial, (slot_row + m) * p.N + col, 8, v);
+                else store8<DT>(p.out, ((int64_t)g * p.M + m) * p.N + col, 8, v);
             } else {
-                const int64_t e = part.first + r;
-                if (e >= part.last) continue;
-                if (row_of[tm] < 0 || row_of[tm] >= p.a_rows) {         // no such row: zeros
+                if (no_row(p, m)) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) v[j] = 0.f;
                 }
@@ -702,28 +718,92 @@ k_product(const Product p) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) v[j] += bias[j];
                     if (p.pre != nullptr) {
-                        if (p.out_f32) store8<SC_F32>(p.pre, e * p.ldp + col, there, v);
-                        else store8<DT>(p.pre, e * p.ldp + col, there, v);
+                        if (p.out_f32) store8<SC_F32>(p.pre, m * p.ldp + col, 8, v);
+                        else store8<DT>(p.pre, m * p.ldp + col, 8, v);
                     }
-                    if (p.act != SC_ACT_NONE) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) v[j] = activate<DT>(v[j], p.act);
-                    }
+                    activate8<DT>(v, p.act);
                     if (p.residual != nullptr) {
                         float add[8];
-                        if (p.out_f32) load8<SC_F32>(p.residual, e * p.ldr + col, there, add);
-                        else load8<DT>(p.residual, e * p.ldr + col, there, add);
+                        if (p.out_f32) load8<SC_F32>(p.residual, m * p.ldr + col, 8, add);
+                        else load8<DT>(p.residual, m * p.ldr + col, 8, add);
 #pragma unroll
                         for (int j = 0; j < 8; ++j) v[j] += add[j];
                     }
                     if (p.out_f32) {
-                        store8<SC_F32>(p.out, e * p.ldo + col, there, v);
+                        store8<SC_F32>(p.out, m * p.ldo + col, 8, v);
                         continue;
                     }
                 }
-                store8<DT>(p.out, e * p.ldo + col, there, v);
+                store8<DT>(p.out, m * p.ldo + col, 8, v);
             }
         }
+    }
+    // The columns that are left: 16 rows at a time through LDS, a wavefront's own piece of it, then element by element; one copy of the code.
+    const int rest = p.N - col_wave - whole_cols < COLS - whole_cols ? p.N - col_wave - whole_cols : COLS - whole_cols;
+    const bool column_sums = MODE == PRODUCT_DW && sums;
+    if constexpr (KW == 1) lds_barrier();              // the operands have been read
+    if (rest <= 0 && !column_sums) return;
+    constexpr int PITCH = COLS + 4;
+    float* const piece = reinterpret_cast<float*>(product_lds) + (wave % (WM * WN)) * (16 * PITCH);
+    if (column_sums) {
+        if (i == 0) {
+#pragma unroll
+            for (int tn = 0; tn < TN; ++tn)
+                *reinterpret_cast<float4*>(piece + 16 * tn + 4 * o) = make_float4(ones_sum[tn][0], ones_sum[tn][1], ones_sum[tn][2], ones_sum[tn][3]);
+        }
+        asm volatile("" ::: "memory");                 // a wavefront's LDS accesses keep their order
+        for (int c = lane; c < COLS && col_wave + c < p.N; c += 64) {
+            if (to_partial) p.partial[(slot_row + p.M) * p.N + col_wave + c] = piece[c];
+            else store_elem<DT>(p.out_bias, (int64_t)g * p.N + col_wave + c, piece[c]);
+        }
+        asm volatile("" ::: "memory");
+    }
+#pragma unroll 1
+    for (int tm = 0; tm < TM && rest > 0; ++tm) {
+#pragma unroll
+        for (int k = 0; k < TM; ++k)
+            if (tm == k) {
+#pragma unroll
+                for (int tn = 0; tn < TN; ++tn)
+                    *reinterpret_cast<float4*>(piece + i * PITCH + 16 * tn + 4 * o) = make_float4(acc[k][tn][0], acc[k][tn][1], acc[k][tn][2], acc[k][tn][3]);
+            }
+        asm volatile("" ::: "memory");
+        int r = lane / rest, c = lane - r * rest;      // 64 elements a turn, along the rows
+        const int turn_rows = 64 / rest, turn_cols = 64 - turn_rows * rest;
+#pragma unroll 1
+        for (int t = lane; t < 16 * rest; t += 64) {
+            const int64_t m = first_row + tm * 16 + r;
+            const int col = col_wave + whole_cols + c;
+            float v = piece[r * PITCH + whole_cols + c];
+            r += turn_rows;
+            c += turn_cols;
+            if (c >= rest) {
+                c -= rest;
+                ++r;
+            }
+            if (m >= end_row) continue;
+            if constexpr (MODE == PRODUCT_DW) {
+                if (to_partial) p.partial[(slot_row + m) * p.N + col] = v;
+                else store_elem<DT>(p.out, ((int64_t)g * p.M + m) * p.N + col, v);
+            } else {
+                if (no_row(p, m)) v = 0.f;
+                if constexpr (MODE == PRODUCT_FWD) {
+                    if (bias_row != nullptr) v += load_elem<DT>(bias_row, col);
+                    if (p.pre != nullptr) {
+                        if (p.out_f32) store_elem<SC_F32>(p.pre, m * p.ldp + col, v);
+                        else store_elem<DT>(p.pre, m * p.ldp + col, v);
+                    }
+                    v = activate<DT>(v, p.act);
+                    if (p.residual != nullptr) v += p.out_f32 ? load_elem<SC_F32>(p.residual, m * p.ldr + col) : load_elem<DT>(p.residual, m * p.ldr + col);
+                    if (p.out_f32) {
+                        store_elem<SC_F32>(p.out, m * p.ldo + col, v);
+                        continue;
+                    }
+                }
+                store_elem<DT>(p.out, m * p.ldo + col, v);
+            }
+        }
+        asm volatile("" ::: "memory");
     }
 }
 
@@ -733,9 +813,10 @@ int launch_product_f32(int mode, const Product& p, bool whole, int cus, hipStrea
 int launch_product_f16(int mode, const Product& p, bool whole, int cus, hipStream_t s);
 int launch_product_bf16(int mode, const Product& p, bool whole, int cus, hipStream_t s);
 
-template <int DT, int MODE, int BM, int BN, int WM, int WN, int KW, bool WHOLE>
+template <int DT, int MODE, int BM, int BN, int WM, int WN, int KW, int SB, int STAGES, bool WHOLE>
 int run_product(Product p, hipStream_t s) {
-    using S = ProductShape<DT, MODE, BM, BN, WM, WN, KW>;
+    using S = ProductShape<DT, MODE, BM, BN, WM, WN, KW, SB, STAGES>;
+    constexpr auto kernel = k_product<DT, MODE, BM, BN, WM, WN, KW, SB, STAGES, WHOLE>;
     const int64_t n_tiles = (p.N + BN - 1) / BN, m_tiles = MODE == PRODUCT_DW && p.M > BM ? (p.M + BM - 1) / BM : 1;
     if (MODE != PRODUCT_DW) {
         // groups: the tiles that are full, and one that is not of every group that there can be
@@ -746,16 +827,16 @@ int run_product(Product p, hipStream_t s) {
     if (blocks > INT32_MAX - 2 * GRID_COLUMNS) return SC_EINVAL;
     const dim3 grid((unsigned)grid_columns(blocks), (unsigned)grid_rows(blocks));
     const int64_t depth = MODE == PRODUCT_DW ? p.per : p.K;
-    const size_t lds = S::lds(depth > S::STEP * KW);
+    const size_t lds = S::lds((depth + S::STEP * KW - 1) / (S::STEP * KW));
     static bool done[MAX_DEVICES];
-    const int rc = allow_lds((const void*)k_product<DT, MODE, BM, BN, WM, WN, KW, WHOLE>, S::lds(true), done);
+    const int rc = allow_lds((const void*)kernel, S::lds(STAGES), done);
     if (rc != SC_OK) return rc;
-    SC_LAUNCH(KID_PRODUCT, (k_product<DT, MODE, BM, BN, WM, WN, KW, WHOLE>), grid, dim3(S::NTH), lds, s, p);
+    SC_LAUNCH(KID_PRODUCT, kernel, grid, dim3(S::NTH), lds, s, p);
     return SC_OK;
 }
-template <int DT, int MODE, int BM, int BN, int WM, int WN, int KW>
+template <int DT, int MODE, int BM, int BN, int WM, int WN, int KW, int SB = 128, int STAGES = 2>
 int run_product(const Product& p, bool whole, hipStream_t s) {
-    return whole ? run_product<DT, MODE, BM, BN, WM, WN, KW, true>(p, s) : run_product<DT, MODE, BM, BN, WM, WN, KW, false>(p, s);
+    return whole ? run_product<DT, MODE, BM, BN, WM, WN, KW, SB, STAGES, true>(p, s) : run_product<DT, MODE, BM, BN, WM, WN, KW, SB, 2, false>(p, s);
 }
 // Which tile: product_tile.
 template <int DT, int MODE>
