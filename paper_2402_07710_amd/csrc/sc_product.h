@@ -136,16 +136,40 @@ __device__ inline void store8(void* base, int64_t i, int count, const float (&v)
     }
 }
 
+// eight consecutive elements on their way
+template <int DT>
+struct Eight {
+    uint4 raw[DT == SC_F32 ? 2 : 1];
+    __device__ void load(const void* base, int64_t i) {
+        const char* p = reinterpret_cast<const char*>(base) + i * ELEM<DT>;
+        raw[0] = load_chunk(p);
+        if constexpr (DT == SC_F32) raw[1] = load_chunk(p + 16);
+    }
+    __device__ void add_to(float (&v)[8]) const {
+        if constexpr (DT == SC_F32) {
+            const uint32_t w[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += __builtin_bit_cast(float, w[j]);
+        } else {
+            const uint32_t w[4] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[2 * j] += to_float<DT>(w[j] & 0xffffu);
+                v[2 * j + 1] += to_float<DT>(w[j] >> 16);
+            }
+        }
+    }
+};
+
 // ---- activations ------------------------------------------------------------------------------------
 // Phi(v) = (1 + erf(v / sqrt 2)) / 2.  32-bit layers: the library's erf.  16-bit ones: the rational approximation 7.1.26 of Abramowitz and
 // Stegun, erfc(x) = t (a1 + t (a2 + ...)) exp(-x^2) with t = 1 / (1 + 0.3275911 x) for x >= 0, off by 1.5e-7 at most, far below a rounding
 // to 16 bits; a third of the instructions, and its exponential is the density that the derivative needs.
 __device__ inline float gauss_tail(float v, float& density) {          // Phi(-|v|), exp(-v^2 / 2)
-    const float x = fabsf(v) * 0.70710678f;
-    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f));
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678f, fminf(fabsf(v), 64.f), 1.f));
     density = __builtin_amdgcn_exp2f(v * v * -0.72134752f);
-    const float poly = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-    return 0.5f * poly * density;
+    const float poly = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f), 0.5f * 1.421413741f), 0.5f * -0.284496736f), 0.5f * 0.254829592f);
+    return poly * density;
 }
 template <int DT>
 __device__ inline float gauss_cdf(float v, float& density) {
@@ -168,6 +192,8 @@ __device__ inline float activate(float v, int act) {
     if (act == SC_ACT_RELU) return v > 0.f || v != v ? v : 0.f;
     if (act == SC_ACT_NONE) return v;
     float density;
+    // v Phi(v) = max(v, 0) - |v| Phi(-|v|); beyond 64 the last factor is zero (a NaN is in the density)
+    if (DT != SC_F32 && act == SC_ACT_GELU) return fmaf(-fminf(fabsf(v), 64.f), gauss_tail(v, density), fmaxf(v, 0.f));
     const float w = act == SC_ACT_GELU ? gauss_cdf<DT>(v, density) : sigmoid<DT>(v);
     return fmaxf(v, -3.4e38f) * w;                      // a NaN is in w as well
 }
@@ -472,6 +498,7 @@ struct Loader {
 // ---- the kernel -----------------------------------------------------------------------------------------
 // WM x WN wavefronts share a tile, KW sets of them the summed axis, of which a set takes SB bytes a step; STAGES buffers.  WHOLE: rows and
 // channels are whole chunks of 16 bytes, aligned; otherwise chunks pass through registers, by unaligned loads, element by element at the end of a row.
+// RESIDUAL: there is one; what is held of it costs the others wavefronts (128 x 128: 174 registers or 123).
 template <int DT, int MODE, int BM_, int BN_, int WM_, int WN_, int KW_, int SB_, int STAGES_>
 struct ProductShape {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KW = KW_, SB = SB_, STAGES = STAGES_;
@@ -496,8 +523,8 @@ __device__ inline bool no_row(const Product& p, int64_t m) {
     return r < 0 || r >= p.a_rows;
 }
 
-template <int DT, int MODE, int BM, int BN, int WM, int WN, int KW, int SB, int STAGES, bool WHOLE>
-__global__ void __launch_bounds__(64 * WM * WN * KW)
+template <int DT, int MODE, int BM, int BN, int WM, int WN, int KW, int SB, int STAGES, bool WHOLE, bool RESIDUAL>
+__global__ void __launch_bounds__(64 * WM * WN * KW, 2)
 k_product(const Product p) {
     using S = ProductShape<DT, MODE, BM, BN, WM, WN, KW, SB, STAGES>;
     constexpr int NTH = S::NTH, TM = S::TM, TN = S::TN;
@@ -538,6 +565,7 @@ k_product(const Product p) {
     la.rows = p.a_rows;
     lb.ld = p.ldb * ELEM<DT>;
     int64_t depth;                                      // of the summed axis
+    int32_t row_of[TM];                                 // rows of a that the lane's results are of
     if constexpr (MODE == PRODUCT_DW) {
         depth = part.last - part.first;
         la.list = p.a_list;
@@ -562,6 +590,12 @@ k_product(const Product p) {
         lb.start_across();
     } else {
         depth = p.a_rows > 0 ? p.K : 0;
+#pragma unroll
+        for (int tm = 0; tm < TM; ++tm) {
+            const int64_t e = part.first + (wm * TM + tm) * 16 + i;
+            row_of[tm] = (int32_t)e;
+            if (p.a_list != nullptr && e < part.last) row_of[tm] = p.a_list[e];
+        }
         if (depth > 0) {
             la.list = nullptr;
             la.end = p.K;
@@ -684,16 +718,37 @@ k_product(const Product p) {
     const int64_t slot_row = part.slot * (p.M + 1);    // DW, several parts: rows of sums in front of this part's
     const bool to_partial = MODE == PRODUCT_DW && part.parts > 1;
     const void* const bias_row = MODE == PRODUCT_FWD && p.bias != nullptr ? (const char*)p.bias + (int64_t)g * p.N * ELEM<DT> : nullptr;
-    int whole_cols = 0;                                // of the wavefront's columns, those in whole pairs of blocks
+    // Whatever is loaded is asked for ahead of the stores of the columns before: loads and stores are waited for in one order.
+    constexpr int PAIRS = TN / 2;
+    const int left = (p.N - col_wave) / 32, pairs = left < PAIRS ? (left > 0 ? left : 0) : PAIRS;
+    const int whole_cols = 32 * pairs;
+    const int col_lane = col_wave + 16 * (o & 1) + 8 * (o >> 1);
+    Eight<DT> bias[MODE == PRODUCT_FWD ? PAIRS : 1], add[RESIDUAL ? 2 : 1][RESIDUAL ? TM : 1];
+    const bool early = RESIDUAL && p.out_f32 == 0;
+    if constexpr (MODE == PRODUCT_FWD) {
+        if (bias_row != nullptr) {
 #pragma unroll
-    for (int u = 0; u < TN / 2; ++u) {
-        if (col_wave + 32 * u + 32 > p.N) break;
-        whole_cols = 32 * u + 32;
-        const int col = col_wave + 32 * u + 16 * (o & 1) + 8 * (o >> 1);
-        float bias[8];
+            for (int u = 0; u < PAIRS; ++u)
+                if (u < pairs) bias[u].load(bias_row, col_lane + 32 * u);
+        }
+    }
+    auto ask = [&](int u) __attribute__((always_inline)) {
+        if constexpr (RESIDUAL) {
+            if (early && u < pairs) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) bias[j] = 0.f;
-        if (bias_row != nullptr) load8<DT>(bias_row, col, 8, bias);
+                for (int tm = 0; tm < TM; ++tm) {
+                    const int64_t m = first_row + tm * 16 + i;
+                    if (m < end_row) add[u & 1][tm].load(p.residual, m * p.ldr + col_lane + 32 * u);
+                }
+            }
+        }
+    };
+    ask(0);
+#pragma unroll
+    for (int u = 0; u < PAIRS; ++u) {
+        if (u >= pairs) break;
+        if (u + 1 < PAIRS) ask(u + 1);
+        const int col = col_lane + 32 * u;
 #pragma unroll
         for (int tm = 0; tm < TM; ++tm) {
             float v[8];
@@ -710,24 +765,25 @@ k_product(const Product p) {
                 if (to_partial) store8<SC_F32>(p.partial, (slot_row + m) * p.N + col, 8, v);
                 else store8<DT>(p.out, ((int64_t)g * p.M + m) * p.N + col, 8, v);
             } else {
-                if (no_row(p, m)) {
+                if (row_of[tm] < 0 || row_of[tm] >= p.a_rows) {          // no such row: zeros
 #pragma unroll
                     for (int j = 0; j < 8; ++j) v[j] = 0.f;
                 }
                 if constexpr (MODE == PRODUCT_FWD) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] += bias[j];
+                    if (bias_row != nullptr) bias[u].add_to(v);
                     if (p.pre != nullptr) {
                         if (p.out_f32) store8<SC_F32>(p.pre, m * p.ldp + col, 8, v);
                         else store8<DT>(p.pre, m * p.ldp + col, 8, v);
                     }
                     activate8<DT>(v, p.act);
-                    if (p.residual != nullptr) {
-                        float add[8];
-                        if (p.out_f32) load8<SC_F32>(p.residual, m * p.ldr + col, 8, add);
-                        else load8<DT>(p.residual, m * p.ldr + col, 8, add);
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) v[j] += add[j];
+                    if constexpr (RESIDUAL) {
+                        if (early) {
+                            add[u & 1][tm].add_to(v);
+                        } else {
+                            Eight<SC_F32> late;
+                            late.load(p.residual, m * p.ldr + col);
+                            late.add_to(v);
+                        }
                     }
                     if (p.out_f32) {
                         store8<SC_F32>(p.out, m * p.ldo + col, 8, v);
@@ -794,7 +850,7 @@ k_product(const Product p) {
                         else store_elem<DT>(p.pre, m * p.ldp + col, v);
                     }
                     v = activate<DT>(v, p.act);
-                    if (p.residual != nullptr) v += p.out_f32 ? load_elem<SC_F32>(p.residual, m * p.ldr + col) : load_elem<DT>(p.residual, m * p.ldr + col);
+                    if (RESIDUAL) v += p.out_f32 ? load_elem<SC_F32>(p.residual, m * p.ldr + col) : load_elem<DT>(p.residual, m * p.ldr + col);
                     if (p.out_f32) {
                         store_elem<SC_F32>(p.out, m * p.ldo + col, v);
                         continue;
@@ -813,10 +869,10 @@ int launch_product_f32(int mode, const Product& p, bool whole, int cus, hipStrea
 int launch_product_f16(int mode, const Product& p, bool whole, int cus, hipStream_t s);
 int launch_product_bf16(int mode, const Product& p, bool whole, int cus, hipStream_t s);
 
-template <int DT, int MODE, int BM, int BN, int WM, int WN, int KW, int SB, int STAGES, bool WHOLE>
+template <int DT, int MODE, int BM, int BN, int WM, int WN, int KW, int SB, int STAGES, bool WHOLE, bool RESIDUAL>
 int run_product(Product p, hipStream_t s) {
     using S = ProductShape<DT, MODE, BM, BN, WM, WN, KW, SB, STAGES>;
-    constexpr auto kernel = k_product<DT, MODE, BM, BN, WM, WN, KW, SB, STAGES, WHOLE>;
+    constexpr auto kernel = k_product<DT, MODE, BM, BN, WM, WN, KW, SB, STAGES, WHOLE, RESIDUAL>;
     const int64_t n_tiles = (p.N + BN - 1) / BN, m_tiles = MODE == PRODUCT_DW && p.M > BM ? (p.M + BM - 1) / BM : 1;
     if (MODE != PRODUCT_DW) {
         // groups: the tiles that are full, and one that is not of every group that there can be
@@ -836,28 +892,33 @@ int run_product(Product p, hipStream_t s) {
 }
 template <int DT, int MODE, int BM, int BN, int WM, int WN, int KW, int SB = 128, int STAGES = 2>
 int run_product(const Product& p, bool whole, hipStream_t s) {
-    return whole ? run_product<DT, MODE, BM, BN, WM, WN, KW, SB, STAGES, true>(p, s) : run_product<DT, MODE, BM, BN, WM, WN, KW, SB, 2, false>(p, s);
+    if constexpr (MODE == PRODUCT_FWD) {
+        if (p.residual != nullptr)
+            return whole ? run_product<DT, MODE, BM, BN, WM, WN, KW, SB, STAGES, true, true>(p, s)
+                         : run_product<DT, MODE, BM, BN, WM, WN, KW, SB, 2, false, true>(p, s);
+    }
+    return whole ? run_product<DT, MODE, BM, BN, WM, WN, KW, SB, STAGES, true, false>(p, s)
+                 : run_product<DT, MODE, BM, BN, WM, WN, KW, SB, 2, false, false>(p, s);
 }
-// Which tile: product_tile.
+// Which tile: row_tile, weight_tile.
 template <int DT, int MODE>
 int choose_product(const Product& p, bool whole, int cus, hipStream_t s) {
-    (void)cus;
     if constexpr (MODE == PRODUCT_DW) {
-        switch (weight_tile(p.M, p.N)) {
-            case 64: return run_product<DT, MODE, 64, 64, 2, 2, 1>(p, whole, s);
-            case 128: return run_product<DT, MODE, 128, 128, 2, 2, 1>(p, whole, s);
-            default:
-                if constexpr (DT != SC_F32) return run_product<DT, MODE, 256, 256, 2, 4, 1>(p, whole, s);
-                else return run_product<DT, MODE, 128, 128, 2, 2, 1>(p, whole, s);
-        }
+        if (weight_tile(p.M, p.N) == 64) return run_product<DT, MODE, 64, 64, 2, 2, 1>(p, whole, s);
+        return run_product<DT, MODE, 128, 128, 2, 2, 1>(p, whole, s);
     } else {
-        switch (row_tile(p.n, p.starts == nullptr ? 1 : p.groups, p.N, p.K)) {
-            case ROWS_FEW: return run_product<DT, MODE, 16, 64, 1, 1, 4>(p, whole, s);
-            case COLUMNS_32: return run_product<DT, MODE, 128, 32, 4, 1, 1>(p, whole, s);
-            case COLUMNS_64: return run_product<DT, MODE, 128, 64, 4, 1, 1>(p, whole, s);
-            case TILE_128: return run_product<DT, MODE, 128, 128, 2, 2, 1>(p, whole, s);
+        switch (row_tile(p.n, p.starts == nullptr ? 1 : p.groups, p.N, p.K, cus)) {
+            case ROWS_16: return run_product<DT, MODE, 16, 64, 1, 1, 4>(p, whole, s);
+            case TILE_128_32: return run_product<DT, MODE, 128, 32, 4, 1, 1>(p, whole, s);
+            case TILE_64_64: return run_product<DT, MODE, 64, 64, 2, 2, 1>(p, whole, s);
+            case TILE_128_64: return run_product<DT, MODE, 128, 64, 4, 1, 1>(p, whole, s);
+            case TILE_128_128_LONG: return run_product<DT, MODE, 128, 128, 2, 2, 1>(p, whole, s);
+            case TILE_128_256:
+                if constexpr (DT != SC_F32 && MODE == PRODUCT_FWD) return run_product<DT, MODE, 128, 256, 2, 2, 1, 64>(p, whole, s);
+                else if constexpr (DT != SC_F32) return run_product<DT, MODE, 256, 256, 2, 4, 1>(p, whole, s);
+                else return run_product<DT, MODE, 128, 128, 2, 2, 1>(p, whole, s);
             default:
-                if constexpr (DT != SC_F32) return run_product<DT, MODE, 256, 256, 2, 4, 1>(p, whole, s);
+                if constexpr (MODE == PRODUCT_FWD) return run_product<DT, MODE, 128, 128, 2, 2, 1, 64, 3>(p, whole, s);
                 else return run_product<DT, MODE, 128, 128, 2, 2, 1>(p, whole, s);
         }
     }
