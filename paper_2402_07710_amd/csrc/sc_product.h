@@ -140,24 +140,34 @@ __device__ inline void store8(void* base, int64_t i, int count, const float (&v)
 template <int DT>
 struct Eight {
     uint4 raw[DT == SC_F32 ? 2 : 1];
+    __device__ void clear() {
+        raw[0] = make_uint4(0, 0, 0, 0);
+        if constexpr (DT == SC_F32) raw[1] = make_uint4(0, 0, 0, 0);
+    }
     __device__ void load(const void* base, int64_t i) {
         const char* p = reinterpret_cast<const char*>(base) + i * ELEM<DT>;
         raw[0] = load_chunk(p);
         if constexpr (DT == SC_F32) raw[1] = load_chunk(p + 16);
     }
-    __device__ void add_to(float (&v)[8]) const {
+    __device__ void to_floats(float (&v)[8]) const {
         if constexpr (DT == SC_F32) {
             const uint32_t w[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] += __builtin_bit_cast(float, w[j]);
+            for (int j = 0; j < 8; ++j) v[j] = __builtin_bit_cast(float, w[j]);
         } else {
             const uint32_t w[4] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                v[2 * j] += to_float<DT>(w[j] & 0xffffu);
-                v[2 * j + 1] += to_float<DT>(w[j] >> 16);
+                v[2 * j] = to_float<DT>(w[j] & 0xffffu);
+                v[2 * j + 1] = to_float<DT>(w[j] >> 16);
             }
         }
+    }
+    __device__ void add_to(float (&v)[8]) const {
+        float mine[8];
+        to_floats(mine);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += mine[j];
     }
 };
 

@@ -76,45 +76,85 @@ __device__ inline void turn_of(const PairTurn& t, float at, float& c, float& s) 
     }
 }
 
-// a lane's pairs of one head: a[i], b[i] for the pairs first + i
-template <int DT, bool ADJACENT>
-__device__ inline void load_pairs(const char* head, int first, int half, float (&a)[8], float (&b)[8]) {
-    if constexpr (ADJACENT) {
-        float v[2][8];
-        load8<DT>(head, 2 * first, 2 * (half - first), v[0]);
-        load8<DT>(head, 2 * first + 8, 2 * (half - first) - 8, v[1]);
+// A lane's eight pairs of one head: a[i], b[i].  It takes chunk c (of eight channels) of the lower half of the head's lanes' and the one as many further on as
+// the head has lanes, or (halves) pairs 8 c .. 8 c + 7 with their partners, so that the lanes of a head read consecutive chunks.
+template <bool ADJACENT>
+__device__ inline int pair_of(int c, int lanes, int i) { return ADJACENT ? 4 * (i < 4 ? c : c + lanes) + (i & 3) : 8 * c + i; }
+// Its channels on their way: two chunks.  WHOLE: heads are whole chunks (halves: both sides).
+template <int DT, bool WHOLE>
+struct Pairs {
+    Eight<DT> raw[WHOLE ? 2 : 1];
+    float parts[WHOLE ? 1 : 2][8];
+    __device__ void clear() {
+        if constexpr (WHOLE) {
+            raw[0].clear();
+            raw[1].clear();
+        } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            a[i] = v[i >> 2][(2 * i) & 7];
-            b[i] = v[i >> 2][(2 * i + 1) & 7];
+            for (int i = 0; i < 8; ++i) parts[0][i] = parts[1][i] = 0.f;
         }
-    } else {
-        load8<DT>(head, first, half - first, a);
-        load8<DT>(head, half + first, half - first, b);
     }
-}
-template <int DT, bool ADJACENT>
-__device__ inline void store_pairs(char* head, int first, int half, const float (&a)[8], const float (&b)[8]) {
-    if constexpr (ADJACENT) {
+    // channels at and at2 on, of the `count` and `count2` that there are
+    __device__ void load(const char* head, int at, int count, int at2, int count2) {
+        if constexpr (WHOLE) {
+            raw[0].load(head, at);
+            if (count2 > 0) raw[1].load(head, at2);
+            else raw[1].clear();
+        } else {
+            load8<DT>(head, at, count, parts[0]);
+            load8<DT>(head, at2, count2, parts[1]);
+        }
+    }
+    template <bool ADJACENT>
+    __device__ void take(float (&a)[8], float (&b)[8]) const {
         float v[2][8];
+        if constexpr (WHOLE) {
+            raw[0].to_floats(v[0]);
+            raw[1].to_floats(v[1]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[0][i] = parts[0][i];
+                v[1][i] = parts[1][i];
+            }
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
+            a[i] = ADJACENT ? v[i >> 2][(2 * i) & 7] : v[0][i];
+            b[i] = ADJACENT ? v[i >> 2][(2 * i + 1) & 7] : v[1][i];
+        }
+    }
+};
+template <int DT, bool ADJACENT, bool WHOLE>
+__device__ inline void store_pairs(char* head, int at, int count, int at2, int count2, const float (&a)[8], const float (&b)[8]) {
+    float v[2][8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (ADJACENT) {
             v[i >> 2][(2 * i) & 7] = a[i];
             v[i >> 2][(2 * i + 1) & 7] = b[i];
+        } else {
+            v[0][i] = a[i];
+            v[1][i] = b[i];
         }
-        store8<DT>(head, 2 * first, 2 * (half - first), v[0]);
-        store8<DT>(head, 2 * first + 8, 2 * (half - first) - 8, v[1]);
-    } else {
-        store8<DT>(head, first, half - first, a);
-        store8<DT>(head, half + first, half - first, b);
     }
+    store8<DT>(head, at, WHOLE ? 8 : count, v[0]);
+    if (!WHOLE || count2 > 0) store8<DT>(head, at2, WHOLE ? 8 : count2, v[1]);
 }
+template <int CONTROL>
+__device__ inline float from_lane(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CONTROL, 0xf, 0xf, true)); }
+// The sum over 2^log2 neighbouring lanes, the same bits in all of them.
 __device__ inline float sum_of_lanes(float v, int log2) {
-    for (int d = 0; d < log2; ++d) v += __shfl_xor(v, 1 << d);
+    if (log2 > 0) v += from_lane<0xb1>(v);             // the other of two, the other two of four
+    if (log2 > 1) v += from_lane<0x4e>(v);
+    if (log2 > 2) v += from_lane<0x141>(v);            // mirrored in 8 and in 16 lanes: fours, and then eights, are alike by now
+    if (log2 > 3) v += from_lane<0x140>(v);
+    if (log2 > 4) v += __shfl_xor(v, 16);
+    if (log2 > 5) v += __shfl_xor(v, 32);
     return v;
 }
 
-template <int DT, bool ADJACENT, bool BACKWARD, int TOGETHER>
+template <int DT, bool ADJACENT, bool BACKWARD, int TOGETHER, bool WHOLE>
 __global__ void __launch_bounds__(ROPE_THREADS)
 k_rope(const Rope p) {
     const int which = blockIdx.x < (unsigned)p.blocks[0] ? 0 : 1;
@@ -122,18 +162,23 @@ k_rope(const Rope p) {
     const Heads in = p.in[which], out = p.out[which], grad = p.grad[which];
     const void* const gain = p.gain[which];
     const int half = p.D / 2, lanes = 1 << p.lanes_log2;
-    const int first = ((int)threadIdx.x & (lanes - 1)) * PAIRS_A_LANE;
-    const bool on = first < half;                       // heads whose lanes are not a power of two leave some idle
+    const int c0 = (int)threadIdx.x & (lanes - 1);
+    // the lane's two chunks, and how much of them there is; heads whose lanes are not a power of two leave some idle
+    const int at = 8 * c0, at2 = ADJACENT ? 8 * (c0 + lanes) : half + 8 * c0;
+    const int count = (ADJACENT ? p.D : half) - at, count2 = p.D - at2;
+    const bool on = count > 0;
     const float per_channel = 1.f / (float)p.D;
     PairTurn turn[8];
-    float gain_a[8], gain_b[8], sum_a[8], sum_b[8];
+    Pairs<DT, WHOLE> gains;
+    float sum_a[BACKWARD ? 8 : 1], sum_b[BACKWARD ? 8 : 1];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        turn[i] = on && first + i < half ? p.table[first + i] : PairTurn{0.f, 0.f, 0, 0};
-        gain_a[i] = gain_b[i] = 1.f;
-        sum_a[i] = sum_b[i] = 0.f;
+        const int pair = pair_of<ADJACENT>(c0, lanes, i);
+        turn[i] = pair < half ? p.table[pair] : PairTurn{0.f, 0.f, 0, 0};
+        if (BACKWARD) sum_a[BACKWARD ? i : 0] = sum_b[BACKWARD ? i : 0] = 0.f;
     }
-    if (on && gain != nullptr) load_pairs<DT, ADJACENT>((const char*)gain, first, half, gain_a, gain_b);
+    gains.clear();
+    if (on && gain != nullptr) gains.load((const char*)gain, at, count, at2, count2);
 
     const int shares = (in.heads + TOGETHER - 1) / TOGETHER;     // groups of heads of a row
     const int64_t items = p.rows * shares, step = blocks * (ROPE_THREADS >> p.lanes_log2);
@@ -144,77 +189,81 @@ k_rope(const Rope p) {
         const int64_t item = start + n * step;
         const bool there = on && item < items;
         const int64_t row = there ? (shares == 1 ? item : item / shares) : 0;
-        const int head0 = there ? (int)(item - row * shares) * TOGETHER : 0;
-        float a[TOGETHER][8], b[TOGETHER][8], ga[BACKWARD ? TOGETHER : 1][8], gb[BACKWARD ? TOGETHER : 1][8];
+        const int share = there ? (int)(item - row * shares) : 0;           // heads share, share + shares, ...: neighbouring lanes, neighbouring heads
+        Pairs<DT, WHOLE> value[TOGETHER], slope[BACKWARD ? TOGETHER : 1];
 #pragma unroll
         for (int h = 0; h < TOGETHER; ++h) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) a[h][i] = b[h][i] = 0.f;
-            if (BACKWARD) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) ga[BACKWARD ? h : 0][i] = gb[BACKWARD ? h : 0][i] = 0.f;
-            }
-            if (there && head0 + h < in.heads) {
-                if (!BACKWARD || gain != nullptr) load_pairs<DT, ADJACENT>(in.data + row * in.row + (head0 + h) * in.head, first, half, a[h], b[h]);
-                if (BACKWARD)
-                    load_pairs<DT, ADJACENT>(grad.data + row * grad.row + (head0 + h) * grad.head, first, half, ga[BACKWARD ? h : 0], gb[BACKWARD ? h : 0]);
+            const int head = share + h * shares;
+            value[h].clear();
+            if (BACKWARD) slope[BACKWARD ? h : 0].clear();
+            if (there && head < in.heads) {
+                if (!BACKWARD || gain != nullptr) value[h].load(in.data + row * in.row + head * in.head, at, count, at2, count2);
+                if (BACKWARD) slope[BACKWARD ? h : 0].load(grad.data + row * grad.row + head * grad.head, at, count, at2, count2);
             }
         }
-        float at[SC_AXES_MAX];
+        float place[SC_AXES_MAX];
 #pragma unroll
-        for (int x = 0; x < SC_AXES_MAX; ++x) at[x] = there && x < p.axes ? (float)p.pos[row * p.ld_pos + x] : 0.f;
+        for (int x = 0; x < SC_AXES_MAX; ++x) place[x] = there && x < p.axes ? (float)p.pos[row * p.ld_pos + x] : 0.f;
         float c[8], s[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int axis = turn[i].axis;
-            turn_of<DT>(turn[i], axis == 0 ? at[0] : axis == 1 ? at[1] : axis == 2 ? at[2] : at[3], c[i], s[i]);
+            turn_of<DT>(turn[i], axis == 0 ? place[0] : axis == 1 ? place[1] : axis == 2 ? place[2] : place[3], c[i], s[i]);
         }
+        float gain_a[8], gain_b[8];
+        gains.template take<ADJACENT>(gain_a, gain_b);
 #pragma unroll
         for (int h = 0; h < TOGETHER; ++h) {
+            const int head = share + h * shares;
+            float a[8], b[8];
+            value[h].template take<ADJACENT>(a, b);
             float scale = 1.f;
             if (gain != nullptr) {
                 float squares = 0.f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) squares = fmaf(a[h][i], a[h][i], fmaf(b[h][i], b[h][i], squares));
+                for (int i = 0; i < 8; ++i) squares = fmaf(a[i], a[i], fmaf(b[i], b[i], squares));
                 scale = rsqrtf(fmaf(sum_of_lanes(squares, p.lanes_log2), per_channel, p.eps));
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    a[i] *= scale;                      // the unit row
+                    b[i] *= scale;
+                }
             }
             float x[8], y[8];
             if constexpr (!BACKWARD) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float u = a[h][i] * scale * gain_a[i], v = b[h][i] * scale * gain_b[i];
+                    const float u = gain != nullptr ? a[i] * gain_a[i] : a[i], v = gain != nullptr ? b[i] * gain_b[i] : b[i];
                     x[i] = u * c[i] - v * s[i];
                     y[i] = u * s[i] + v * c[i];
                 }
             } else {
+                float ga[8], gb[8];
+                slope[h].template take<ADJACENT>(ga, gb);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    x[i] = ga[h][i] * c[i] + gb[h][i] * s[i];
-                    y[i] = gb[h][i] * c[i] - ga[h][i] * s[i];
+                    x[i] = ga[i] * c[i] + gb[i] * s[i];
+                    y[i] = gb[i] * c[i] - ga[i] * s[i];
                 }
                 if (gain != nullptr) {
                     float along = 0.f;
-                    const bool mine = there && head0 + h < in.heads;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float u = a[h][i] * scale, v = b[h][i] * scale;        // of the unit row
-                        if (mine) {
-                            sum_a[i] = fmaf(x[i], u, sum_a[i]);
-                            sum_b[i] = fmaf(y[i], v, sum_b[i]);
-                        }
+                    for (int i = 0; i < 8; ++i) {        // a head that is not there has zeros for its gradient
+                        sum_a[i] = fmaf(x[i], a[i], sum_a[i]);
+                        sum_b[i] = fmaf(y[i], b[i], sum_b[i]);
                         x[i] *= gain_a[i];
                         y[i] *= gain_b[i];
-                        along = fmaf(x[i], u, fmaf(y[i], v, along));
+                        along = fmaf(x[i], a[i], fmaf(y[i], b[i], along));
                     }
-                    along = sum_of_lanes(along, p.lanes_log2) * per_channel * scale;
+                    along = sum_of_lanes(along, p.lanes_log2) * per_channel;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        x[i] = (x[i] - a[h][i] * along) * scale;
-                        y[i] = (y[i] - b[h][i] * along) * scale;
+                        x[i] = (x[i] - a[i] * along) * scale;
+                        y[i] = (y[i] - b[i] * along) * scale;
                     }
                 }
             }
-            if (there && head0 + h < in.heads) store_pairs<DT, ADJACENT>(out.data + row * out.row + (head0 + h) * out.head, first, half, x, y);
+            if (there && head < in.heads) store_pairs<DT, ADJACENT, WHOLE>(out.data + row * out.row + head * out.head, at, count, at2, count2, x, y);
         }
     }
     if constexpr (BACKWARD) {                           // the workgroup's share of the gain's gradient, groups of lanes in order
@@ -224,8 +273,9 @@ k_rope(const Rope p) {
         float* mine = sums + (threadIdx.x >> p.lanes_log2) * width;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            mine[first + i] = sum_a[i];
-            mine[width / 2 + first + i] = sum_b[i];
+            const int pair = pair_of<ADJACENT>(c0, lanes, i);          // below 8 lanes
+            mine[pair] = sum_a[i];
+            mine[width / 2 + pair] = sum_b[i];
         }
         __syncthreads();
         for (int j = threadIdx.x; j < p.D; j += ROPE_THREADS) {
@@ -238,11 +288,11 @@ k_rope(const Rope p) {
     }
 }
 
-// Gradients of the gains: sums over the workgroups' shares, every 16th by one of 16 threads, in a fixed order.
+// Gradients of the gains: sums over the workgroups' shares, every 64th by one of 64 threads, in a fixed order.
 template <int DT>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(1024)
 k_gain_join(const float* __restrict__ q, int q_blocks, void* __restrict__ dq, const float* __restrict__ k, int k_blocks, void* __restrict__ dk, int D) {
-    __shared__ float sums[16][16];
+    __shared__ float sums[64][16];
     const float* src = blockIdx.y ? k : q;
     void* dst = blockIdx.y ? dk : dq;
     const int blocks = blockIdx.y ? k_blocks : q_blocks;
@@ -251,14 +301,14 @@ k_gain_join(const float* __restrict__ q, int q_blocks, void* __restrict__ dq, co
     float total = 0.f;
     if (j < D) {
 #pragma unroll 8
-        for (int b = which; b < blocks; b += 16) total += src[(int64_t)b * D + j];
+        for (int b = which; b < blocks; b += 64) total += src[(int64_t)b * D + j];
     }
     sums[which][threadIdx.x & 15] = total;
     __syncthreads();
     if (which != 0 || j >= D) return;
     total = 0.f;
 #pragma unroll
-    for (int w = 0; w < 16; ++w) total += sums[w][threadIdx.x];
+    for (int w = 0; w < 64; ++w) total += sums[w][threadIdx.x];
     store_elem<DT>(dst, j, total);
 }
 
@@ -306,10 +356,12 @@ int launch_rope(const Rope& p, int pairing, int dtype, hipStream_t s) {
     constexpr int TOGETHER = BACKWARD ? BACKWARD_TOGETHER : FORWARD_TOGETHER;
     const dim3 grid((unsigned)(p.blocks[0] + p.blocks[1]));
     const int kid = BACKWARD ? KID_ROPE_GRAD : KID_ROPE;
-#define SC_ROPE(DT)                                                                                                                       \
-    do {                                                                                                                                  \
-        if (pairing == SC_PAIRS_ADJACENT) SC_LAUNCH(kid, (k_rope<DT, true, BACKWARD, TOGETHER>), grid, dim3(ROPE_THREADS), 0, s, p);      \
-        else SC_LAUNCH(kid, (k_rope<DT, false, BACKWARD, TOGETHER>), grid, dim3(ROPE_THREADS), 0, s, p);                                  \
+    const bool whole = (pairing == SC_PAIRS_ADJACENT ? p.D : p.D / 2) % 8 == 0;
+#define SC_ROPE(DT)                                                                                                                              \
+    do {                                                                                                                                         \
+        const auto kernel = pairing == SC_PAIRS_ADJACENT ? (whole ? k_rope<DT, true, BACKWARD, TOGETHER, true> : k_rope<DT, true, BACKWARD, TOGETHER, false>)  \
+                                                         : (whole ? k_rope<DT, false, BACKWARD, TOGETHER, true> : k_rope<DT, false, BACKWARD, TOGETHER, false>); \
+        SC_LAUNCH(kid, kernel, grid, dim3(ROPE_THREADS), 0, s, p);                                                                               \
     } while (0)
     if (dtype == SC_F32) SC_ROPE(SC_F32);
     else if (dtype == SC_F16) SC_ROPE(SC_F16);
@@ -424,7 +476,7 @@ extern "C" int sc_qk_rope_bwd(const sc_heads* dq_out, const sc_heads* dk_out, co
     }
     if (gains) {                                        // no rows: zeros
         const dim3 grid((unsigned)((D + 15) / 16), 2);
-#define SC_GAIN_JOIN(DT) SC_LAUNCH(KID_GAIN_JOIN, k_gain_join<DT>, grid, dim3(256), 0, s, p.partial[0], p.blocks[0], d_dgain_q, p.partial[1], p.blocks[1], d_dgain_k, D)
+#define SC_GAIN_JOIN(DT) SC_LAUNCH(KID_GAIN_JOIN, k_gain_join<DT>, grid, dim3(1024), 0, s, p.partial[0], p.blocks[0], d_dgain_q, p.partial[1], p.blocks[1], d_dgain_k, D)
         if (dtype == SC_F32) SC_GAIN_JOIN(SC_F32);
         else if (dtype == SC_F16) SC_GAIN_JOIN(SC_F16);
         else SC_GAIN_JOIN(SC_BF16);

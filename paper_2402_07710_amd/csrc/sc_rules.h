@@ -210,6 +210,6 @@ constexpr int64_t weight_slots(int64_t entries, int64_t part) { return entries <
 
 // ---- norm and rotation (sc_rope.hip) ----------------------------------------------------------------------
 // Workgroups of 256 threads for the queries, and as many for the keys, at most.
-constexpr int64_t ROPE_BLOCKS_MAX = 2048;
+constexpr int64_t ROPE_BLOCKS_MAX = 1024;
 
 }  // namespace sc
