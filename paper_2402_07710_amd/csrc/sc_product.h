@@ -445,20 +445,20 @@ struct Loader {
 #pragma unroll
                 for (int i = 0; i < PASSES; ++i) {
                     const int32_t r = at[ACROSS ? i : 0];
-                    load_to_lds((uint32_t)r < (uint32_t)rows ? (const void*)(column(i) + (int64_t)r * ld) : none, lds + (i * NTH + wave * 64) * 16);
+                    load_to_lds((uint32_t)r < (uint32_t)rows ? (const void*)(column(i) + (int64_t)r * ld) : none, __builtin_amdgcn_readfirstlane(lds + (i * NTH + wave * 64) * 16));
                 }
             } else if (from + STRIDE <= end) {
                 const int64_t step = ACROSS ? STRIDE * ld : STRIDE * ELEM<DT>;
 #pragma unroll
                 for (int i = 0; i < PASSES; ++i) {
-                    load_to_lds(ptr[i], lds + (i * NTH + wave * 64) * 16);
+                    load_to_lds(ptr[i], __builtin_amdgcn_readfirstlane(lds + (i * NTH + wave * 64) * 16));
                     ptr[i] += step;
                 }
             } else {
                 const int left = end > from ? (int)(end - from) : 0;
 #pragma unroll
                 for (int i = 0; i < PASSES; ++i)
-                    load_to_lds((ACROSS ? line_of(i) : chunk_of(i) * PER) < left ? (const void*)ptr[i] : none, lds + (i * NTH + wave * 64) * 16);
+                    load_to_lds((ACROSS ? line_of(i) : chunk_of(i) * PER) < left ? (const void*)ptr[i] : none, __builtin_amdgcn_readfirstlane(lds + (i * NTH + wave * 64) * 16));
             }
         } else {
             const int64_t step = ACROSS ? STRIDE * ld : STRIDE * ELEM<DT>;
@@ -508,7 +508,7 @@ struct Loader {
 // ---- the kernel -----------------------------------------------------------------------------------------
 // WM x WN wavefronts share a tile, KW sets of them the summed axis, of which a set takes SB bytes a step; STAGES buffers.  WHOLE: rows and
 // channels are whole chunks of 16 bytes, aligned; otherwise chunks pass through registers, by unaligned loads, element by element at the end of a row.
-// RESIDUAL: there is one; what is held of it costs the others wavefronts (128 x 128: 174 registers or 123).
+// RESIDUAL: there may be one; what is held of it costs the others wavefronts (128 x 128: 174 registers or 123).
 template <int DT, int MODE, int BM_, int BN_, int WM_, int WN_, int KW_, int SB_, int STAGES_>
 struct ProductShape {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KW = KW_, SB = SB_, STAGES = STAGES_;
@@ -716,7 +716,6 @@ k_product(const Product p) {
                     acc[tm][tn][2] += v.z;
                     acc[tm][tn][3] += v.w;
                 }
-        static_assert(WM * WN == 1, "the pieces lie over the sums, which other wavefronts may still read");
     }
 
     // A lane has columns 4 o .. 4 o + 3 of every block's 16 and row i.  Two blocks' odd and even rows of lanes change places, and it has eight
@@ -734,7 +733,7 @@ k_product(const Product p) {
     const int whole_cols = 32 * pairs;
     const int col_lane = col_wave + 16 * (o & 1) + 8 * (o >> 1);
     Eight<DT> bias[MODE == PRODUCT_FWD ? PAIRS : 1], add[RESIDUAL ? 2 : 1][RESIDUAL ? TM : 1];
-    const bool early = RESIDUAL && p.out_f32 == 0;
+    const bool early = RESIDUAL && p.residual != nullptr && p.out_f32 == 0;
     if constexpr (MODE == PRODUCT_FWD) {
         if (bias_row != nullptr) {
 #pragma unroll
@@ -789,7 +788,7 @@ k_product(const Product p) {
                     if constexpr (RESIDUAL) {
                         if (early) {
                             add[u & 1][tm].add_to(v);
-                        } else {
+                        } else if (p.residual != nullptr) {
                             Eight<SC_F32> late;
                             late.load(p.residual, m * p.ldr + col);
                             late.add_to(v);
@@ -807,7 +806,7 @@ k_product(const Product p) {
     // The columns that are left: 16 rows at a time through LDS, a wavefront's own piece of it, then element by element; one copy of the code.
     const int rest = p.N - col_wave - whole_cols < COLS - whole_cols ? p.N - col_wave - whole_cols : COLS - whole_cols;
     const bool column_sums = MODE == PRODUCT_DW && sums;
-    if constexpr (KW == 1) lds_barrier();              // the operands have been read
+    if constexpr (KW == 1 || WM * WN > 1) lds_barrier();     // the operands, or the sums, have been read by all
     if (rest <= 0 && !column_sums) return;
     constexpr int PITCH = COLS + 4;
     float* const piece = reinterpret_cast<float*>(product_lds) + (wave % (WM * WN)) * (16 * PITCH);
@@ -860,7 +859,7 @@ k_product(const Product p) {
                         else store_elem<DT>(p.pre, m * p.ldp + col, v);
                     }
                     v = activate<DT>(v, p.act);
-                    if (RESIDUAL) v += p.out_f32 ? load_elem<SC_F32>(p.residual, m * p.ldr + col) : load_elem<DT>(p.residual, m * p.ldr + col);
+                    if (RESIDUAL && p.residual != nullptr) v += p.out_f32 ? load_elem<SC_F32>(p.residual, m * p.ldr + col) : load_elem<DT>(p.residual, m * p.ldr + col);
                     if (p.out_f32) {
                         store_elem<SC_F32>(p.out, m * p.ldo + col, v);
                         continue;
@@ -900,15 +899,23 @@ int run_product(Product p, hipStream_t s) {
     SC_LAUNCH(KID_PRODUCT, kernel, grid, dim3(S::NTH), lds, s, p);
     return SC_OK;
 }
-template <int DT, int MODE, int BM, int BN, int WM, int WN, int KW, int SB = 128, int STAGES = 2>
+// MANY: large tiles have a kernel without residual apart, and none for rows that are not whole chunks.
+template <int DT, int MODE, int BM, int BN, int WM, int WN, int KW, int SB = 128, int STAGES = 2, bool MANY = false>
 int run_product(const Product& p, bool whole, hipStream_t s) {
     if constexpr (MODE == PRODUCT_FWD) {
-        if (p.residual != nullptr)
+        if constexpr (MANY) {
+            if (p.residual == nullptr) return run_product<DT, MODE, BM, BN, WM, WN, KW, SB, STAGES, true, false>(p, s);
+            return run_product<DT, MODE, BM, BN, WM, WN, KW, SB, STAGES, true, true>(p, s);
+        } else {
             return whole ? run_product<DT, MODE, BM, BN, WM, WN, KW, SB, STAGES, true, true>(p, s)
                          : run_product<DT, MODE, BM, BN, WM, WN, KW, SB, 2, false, true>(p, s);
+        }
+    } else if constexpr (MANY) {
+        return run_product<DT, MODE, BM, BN, WM, WN, KW, SB, STAGES, true, false>(p, s);
+    } else {
+        return whole ? run_product<DT, MODE, BM, BN, WM, WN, KW, SB, STAGES, true, false>(p, s)
+                     : run_product<DT, MODE, BM, BN, WM, WN, KW, SB, 2, false, false>(p, s);
     }
-    return whole ? run_product<DT, MODE, BM, BN, WM, WN, KW, SB, STAGES, true, false>(p, s)
-                 : run_product<DT, MODE, BM, BN, WM, WN, KW, SB, 2, false, false>(p, s);
 }
 // Which tile: row_tile, weight_tile.
 template <int DT, int MODE>
@@ -917,20 +924,31 @@ int choose_product(const Product& p, bool whole, int cus, hipStream_t s) {
         if (weight_tile(p.M, p.N) == 64) return run_product<DT, MODE, 64, 64, 2, 2, 1>(p, whole, s);
         return run_product<DT, MODE, 128, 128, 2, 2, 1>(p, whole, s);
     } else {
-        switch (row_tile(p.n, p.starts == nullptr ? 1 : p.groups, p.N, p.K, cus)) {
-            case ROWS_16: return run_product<DT, MODE, 16, 64, 1, 1, 4>(p, whole, s);
-            case TILE_128_32: return run_product<DT, MODE, 128, 32, 4, 1, 1>(p, whole, s);
+        constexpr bool FWD = MODE == PRODUCT_FWD, WIDE = DT != SC_F32;
+        const RowTile tile = row_tile(p.n, p.starts == nullptr ? 0 : p.groups, p.N, p.K, FWD, WIDE && whole, cus);
+        switch (tile) {
+            case TILE_16_32: return run_product<DT, MODE, 16, 32, 1, 1, 4>(p, whole, s);
+            case TILE_16_32_DEEP: return run_product<DT, MODE, 16, 32, 1, 1, 8>(p, whole, s);
+            case TILE_32_64: return run_product<DT, MODE, 32, 64, 2, 2, 2>(p, whole, s);
             case TILE_64_64: return run_product<DT, MODE, 64, 64, 2, 2, 1>(p, whole, s);
+            case TILE_64_64_DEEP: return run_product<DT, MODE, 64, 64, 2, 2, 2>(p, whole, s);
+            case TILE_128_32: return run_product<DT, MODE, 128, 32, 4, 1, 1>(p, whole, s);
             case TILE_128_64: return run_product<DT, MODE, 128, 64, 4, 1, 1>(p, whole, s);
-            case TILE_128_128_LONG: return run_product<DT, MODE, 128, 128, 2, 2, 1>(p, whole, s);
-            case TILE_128_256:
-                if constexpr (DT != SC_F32 && MODE == PRODUCT_FWD) return run_product<DT, MODE, 128, 256, 2, 2, 1, 64>(p, whole, s);
-                else if constexpr (DT != SC_F32) return run_product<DT, MODE, 256, 256, 2, 4, 1>(p, whole, s);
-                else return run_product<DT, MODE, 128, 128, 2, 2, 1>(p, whole, s);
-            default:
-                if constexpr (MODE == PRODUCT_FWD) return run_product<DT, MODE, 128, 128, 2, 2, 1, 64, 3>(p, whole, s);
-                else return run_product<DT, MODE, 128, 128, 2, 2, 1>(p, whole, s);
+            default: break;
         }
+        if (!whole) return run_product<DT, MODE, 128, 128, 2, 2, 1>(p, false, s);
+        switch (tile) {
+            case TILE_64_128:
+                if constexpr (FWD) return run_product<DT, MODE, 64, 128, 2, 2, 1, 64, 2, true>(p, true, s);
+                break;
+            case TILE_128_128_SHORT: return run_product<DT, MODE, 128, 128, 2, 2, 1, 64, 2, true>(p, true, s);
+            case TILE_LARGE:
+                if constexpr (WIDE && FWD) return run_product<DT, MODE, 128, 256, 2, 2, 1, 64, 2, true>(p, true, s);
+                else if constexpr (WIDE) return run_product<DT, MODE, 256, 256, 2, 4, 1, 128, 2, true>(p, true, s);
+                break;
+            default: break;
+        }
+        return run_product<DT, MODE, 128, 128, 2, 2, 1, 128, 2, true>(p, true, s);
     }
 }
 template <int DT>

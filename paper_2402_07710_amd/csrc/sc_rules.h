@@ -178,15 +178,20 @@ constexpr int64_t grid_rows(int64_t groups) { return (groups + GRID_COLUMNS - 1)
 
 // ---- products of rows and weights (sc_product.h) --------------------------------------------------------
 // Tile of the result that a workgroup owns, by the rows and columns there are.  Few rows a group: 16 rows, four wavefronts share the summed axis.
-enum RowTile { ROWS_16, TILE_128_32, TILE_64_64, TILE_128_64, TILE_128_128, TILE_128_128_LONG, TILE_128_256 };
-constexpr RowTile row_tile(int64_t entries, int64_t groups, int64_t columns, int64_t depth, int64_t cus) {
-    if (entries <= 32 * (groups < entries ? groups : entries)) return ROWS_16;
+enum RowTile { TILE_16_32, TILE_16_32_DEEP, TILE_32_64, TILE_64_64, TILE_64_64_DEEP, TILE_128_32, TILE_128_64, TILE_64_128, TILE_128_128, TILE_128_128_SHORT, TILE_LARGE };
+// `groups` 0: a linear layer.
+constexpr RowTile row_tile(int64_t entries, int64_t groups, int64_t columns, int64_t depth, bool forward, bool large_too, int64_t cus) {
+    const int64_t parts = groups == 0 ? 1 : groups < entries ? groups : entries, each = entries / parts;
+    const int64_t tiles = (entries + 15 * parts) / 16 * ((columns + 31) / 32);       // of 16 x 32
+    if (tiles <= 2 * cus) return depth >= 1024 && tiles <= cus ? TILE_16_32_DEEP : TILE_16_32;
+    if (tiles <= 8 * cus || each <= 32) return TILE_32_64;
     if (columns <= 32) return TILE_128_32;
-    const int64_t rows128 = (entries + 127) / 128, columns64 = (columns + 63) / 64;
-    if (rows128 * columns64 <= cus) return TILE_64_64;
-    if (columns <= 64 || rows128 * ((columns + 127) / 128) < 2 * cus) return TILE_128_64;
-    if (depth >= 512 && columns >= 256 && rows128 * (columns / 256) >= 2 * cus) return TILE_128_256;
-    return depth > 512 ? TILE_128_128_LONG : TILE_128_128;
+    if (tiles <= 16 * cus || each <= 64) return depth >= 512 ? TILE_64_64_DEEP : TILE_64_64;
+    if (tiles <= 32 * cus || columns <= 64) return TILE_128_64;
+    if (groups == 0 && large_too && depth >= 256 && columns >= 256 && (entries / 128) * (columns / 256) >= 2 * cus) return TILE_LARGE;
+    if (!forward) return groups > 0 && depth >= 1024 ? TILE_128_128_SHORT : TILE_128_128;
+    if (groups > 0) return TILE_128_128_SHORT;
+    return depth <= 256 ? TILE_64_128 : TILE_128_128;
 }
 // Consecutive tiles that one XCD takes: those of the same rows, which its L2 then holds, as long as every XCD has eight runs.
 constexpr int64_t product_run(int64_t units, int64_t tiles_each) {
