@@ -353,12 +353,13 @@ int sc_conv_up_fwd(const void* d_feat_coarse, int64_t n_map,
  * (experts, class heads, scenes of a batch, kernel offsets of a rulebook); the norm and the rotation by
  * voxel coordinates of an attention's queries and keys; and the gradients of all of them.
  *
- * Conventions beside those above: rows are `ld` elements apart (ld >= the row's channels, so a row may be
+ * Conventions beside those above: rows are `ld` elements apart (the row's channels <= ld <= SC_LD_MAX, so a row may be
  * a slice of a wider one), every pointer needs the alignment of its elements only, and any number
  * of channels 1 <= C <= SC_CHANNELS_MAX is taken.  16-byte alignment of rows and channels that are multiples of 16
  * bytes are faster.  Types are SC_F32, SC_F16 and SC_BF16; sums are held in 32 bits.  Outputs must not overlap inputs,
  * except that d_y may be d_residual.  Every sum's order is fixed by the sizes: repeated calls give the same bits. */
 #define SC_CHANNELS_MAX 65536
+#define SC_LD_MAX       536870912LL    /* 2^29 */
 #define SC_GROUPS_MAX   65536
 #define SC_ENTRIES_MAX  2147483647LL
 

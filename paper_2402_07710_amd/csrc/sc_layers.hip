@@ -107,7 +107,7 @@ bool aligned_to(const void* p, int bytes) { return ((uintptr_t)p & (uintptr_t)(b
 bool channels_ok(int C) { return C >= 1 && C <= SC_CHANNELS_MAX; }
 // `n` rows `ld` elements apart; no rows need no memory
 bool rows_ok(const void* p, int64_t n, int64_t ld, int C, int dtype) {
-    return (p != nullptr || n == 0) && aligned_to(p, elem(dtype)) && ld >= C && ld <= INT32_MAX;
+    return (p != nullptr || n == 0) && aligned_to(p, elem(dtype)) && ld >= C && ld <= SC_LD_MAX;
 }
 // every row starts and ends at a 16-byte boundary
 bool whole_chunks(const void* p, int64_t ld, int C, int dtype) {

@@ -239,13 +239,12 @@ struct Part {
     int64_t first, last;           // its entries here
     int parts;                     // of the group
     int64_t slot;                  // DW: of this part among the parts of groups that have several
-    int64_t group_slot;            // of the group's first part
 };
 // Unit u of the groups cut into parts of `per` entries; DW: a group without entries is one empty part, since its result is zero.
-// Called by whole wavefronts.  Starts that do not ascend make parts of wrong entries, never of entries outside [0, n).
+// Called by whole wavefronts; the result is in scalar registers.  Starts that do not ascend make parts of wrong entries, never of entries outside [0, n).
 template <bool EMPTY_TOO>
 __device__ inline Part find_part(const int32_t* __restrict__ starts, int groups, int64_t n, int64_t per, int64_t u) {
-    Part p{-1, 0, 0, 1, 0, 0};
+    Part p{-1, 0, 0, 1, 0};
     if (starts == nullptr) {
         const int64_t parts = (n + per - 1) / per;
         p.parts = (int)(parts > 1 ? parts : 1);
@@ -279,22 +278,21 @@ __device__ inline Part find_part(const int32_t* __restrict__ starts, int groups,
                 upto_slots += other_slots;
             }
         }
-        const int total = __shfl(upto, 63);
+        const int total = __builtin_amdgcn_readlane(upto, 63);
         if (u < base + total) {
             const uint64_t beyond = __ballot((int64_t)upto + base > u);
             const int at = __builtin_ctzll(beyond);
             p.g = g0 + at;
-            p.parts = __shfl(count, at);
-            const int64_t nth = u - base - (__shfl(upto, at) - p.parts);
-            const int64_t first = __shfl((int)lo, at), end = __shfl((int)hi, at);
+            p.parts = __builtin_amdgcn_readlane(count, at);
+            const int64_t nth = u - base - (__builtin_amdgcn_readlane(upto, at) - p.parts);
+            const int64_t first = __builtin_amdgcn_readlane((int)lo, at), end = __builtin_amdgcn_readlane((int)hi, at);
             p.first = first + nth * per;
             p.last = p.first + per < end ? p.first + per : end;
-            p.group_slot = slots + __shfl(upto_slots, at) - (p.parts > 1 ? p.parts : 0);
-            p.slot = p.group_slot + nth;
+            p.slot = slots + __builtin_amdgcn_readlane(upto_slots, at) - (p.parts > 1 ? p.parts : 0) + nth;
             return p;
         }
         base += total;
-        slots += __shfl(upto_slots, 63);
+        slots += __builtin_amdgcn_readlane(upto_slots, 63);
     }
     return p;
 }
@@ -303,11 +301,14 @@ __device__ inline Part find_part(const int32_t* __restrict__ starts, int groups,
 // Stands in for chunks that lie beyond an operand's rows or channels.
 __device__ __align__(16) uint4 g_no_chunk;
 
-// Where a chunk of a line lies in it: its number, turned by the line's, so that what an access of 16 lanes (operands along) or 32 (across) reads
-// fills the 64 banks once.
-// ALONG: lines are rows of the tile, LINE chunks of the summed axis; 16 lanes read one chunk of 16 lines.
+// Where a chunk of a line lies in it: its number, turned by the line's, so that what the LDS hands out in one cycle fills its 64 banks once.
+// ALONG: lines are rows of the tile, LINE chunks of the summed axis.  16-byte reads go 16 lanes a cycle, lanes 0-3, 12-15, 20-23 and 24-27 (or the others of 32): one
+// chunk of lines 0-3 and 12-15 and the next chunk of lines 4-11.
 template <int LINE>
-__device__ constexpr int along_turn(int line) { return LINE == 4 ? (line >> 2) & 3 : LINE == 8 ? (line >> 1) & 7 : line & 7; }
+__device__ constexpr int along_turn(int line) {
+    if (LINE == 4) return (((line >> 2) ^ (line >> 3)) & 1) * 2 + ((line >> 3) & 1);
+    return LINE == 8 ? (line >> 1) & 7 : line & 15;
+}
 // ACROSS: lines are places on the summed axis, LINE chunks of tile rows.  32 lanes of a 16-bit read take 32 bytes of four lines and of the four that
 // are 8 further on, 64 lanes of a 32-bit one 64 bytes of lines 0, 4, 8 and 12.
 template <int DT, int LINE>
@@ -328,7 +329,7 @@ struct AlongReader {
     // row0: the wavefront's first row; chunk0: its set's first chunk; both multiples that leave the turn alone
     __device__ AlongReader(uint32_t tile, int row0, int chunk0) {
         const int i = threadIdx.x & 15, o = (threadIdx.x >> 4) & 3;
-        for (int c = 0; c < PARTS; ++c) at[c] = tile + ((row0 + i) * LINE + chunk0 + ((4 * c + o) ^ along_turn<LINE>(i))) * 16;
+        for (int c = 0; c < PARTS; ++c) at[c] = tile + ((row0 + i) * LINE + ((chunk0 + 4 * c + o) ^ along_turn<LINE>(i))) * 16;
     }
     // block t, chunks 4 c .. 4 c + 3, a chunk for each 16 lanes
     __device__ uint4 read(uint32_t buffer, int t, int c) const { return __builtin_bit_cast(uint4, *(lds_u32x4)(at[c] + buffer + t * (16 * LINE * 16))); }
@@ -384,7 +385,7 @@ template <int DT, bool ACROSS, int LINES, int LINE, int NTH, int STRIDE, bool WH
 struct Loader {
     static constexpr int PASSES = LINES * LINE / NTH, PER = 16 / ELEM<DT>;
     static_assert(LINES * LINE % NTH == 0 && NTH % LINE == 0, "whole passes of whole lines");
-    int64_t ld, rows;                          // bytes from row to row; rows of the operand
+    uint32_t ld, rows;                         // bytes from row to row; rows of the operand
     int64_t first, end;                        // ACROSS: the summed entries; ALONG: first is 0
     const char* base;
     const int32_t* list;                       // ACROSS
@@ -408,7 +409,7 @@ struct Loader {
             if (r >= stop) r = stop - 1;
             if (rows_list != nullptr) r = rows_list[r];
             if (r < 0 || r >= rows) r = 0;
-            ptr[i] = base + r * ld + (int64_t)chunk_of(i) * 16;
+            ptr[i] = base + (uint64_t)(uint32_t)r * ld + chunk_of(i) * 16;
         }
     }
     // ACROSS: columns beyond the last read some other chunk
@@ -422,7 +423,7 @@ struct Loader {
             return;
         }
 #pragma unroll
-        for (int i = 0; i < PASSES; ++i) ptr[i] = column(i) + (first + line_of(i)) * ld;
+        for (int i = 0; i < PASSES; ++i) ptr[i] = column(i) + (uint64_t)(uint32_t)(first + line_of(i)) * ld;
     }
     __device__ void take_rows(int s) {
         if constexpr (ACROSS) {
@@ -445,10 +446,10 @@ struct Loader {
 #pragma unroll
                 for (int i = 0; i < PASSES; ++i) {
                     const int32_t r = at[ACROSS ? i : 0];
-                    load_to_lds((uint32_t)r < (uint32_t)rows ? (const void*)(column(i) + (int64_t)r * ld) : none, __builtin_amdgcn_readfirstlane(lds + (i * NTH + wave * 64) * 16));
+                    load_to_lds((uint32_t)r < rows ? (const void*)(column(i) + (uint64_t)(uint32_t)r * ld) : none, __builtin_amdgcn_readfirstlane(lds + (i * NTH + wave * 64) * 16));
                 }
             } else if (from + STRIDE <= end) {
-                const int64_t step = ACROSS ? STRIDE * ld : STRIDE * ELEM<DT>;
+                const uint64_t step = ACROSS ? (uint64_t)STRIDE * ld : STRIDE * ELEM<DT>;
 #pragma unroll
                 for (int i = 0; i < PASSES; ++i) {
                     load_to_lds(ptr[i], __builtin_amdgcn_readfirstlane(lds + (i * NTH + wave * 64) * 16));
@@ -461,7 +462,7 @@ struct Loader {
                     load_to_lds((ACROSS ? line_of(i) : chunk_of(i) * PER) < left ? (const void*)ptr[i] : none, __builtin_amdgcn_readfirstlane(lds + (i * NTH + wave * 64) * 16));
             }
         } else {
-            const int64_t step = ACROSS ? STRIDE * ld : STRIDE * ELEM<DT>;
+            const uint64_t step = ACROSS ? (uint64_t)STRIDE * ld : STRIDE * ELEM<DT>;
 #pragma unroll
             for (int i = 0; i < PASSES; ++i) {
                 const char* p = ptr[i];
@@ -471,8 +472,8 @@ struct Loader {
                     bool ok = from + line_of(i) < end;
                     if (listed) {
                         const int32_t r = at[ACROSS ? i : 0];
-                        ok = (uint32_t)r < (uint32_t)rows;
-                        p = column(i) + (int64_t)r * ld;
+                        ok = (uint32_t)r < rows;
+                        p = column(i) + (uint64_t)(uint32_t)r * ld;
                     }
                     if (!ok) there = 0;
                 } else {
@@ -571,9 +572,9 @@ k_product(const Product p) {
     Loader<DT, S::A_ACROSS, S::A_LINES, S::A_LINE, NTH, STRIDE, WHOLE> la;
     Loader<DT, S::B_ACROSS, S::B_LINES, S::B_LINE, NTH, STRIDE, WHOLE> lb;
     la.base = (const char*)p.a;
-    la.ld = p.lda * ELEM<DT>;
-    la.rows = p.a_rows;
-    lb.ld = p.ldb * ELEM<DT>;
+    la.ld = (uint32_t)(p.lda * ELEM<DT>);
+    la.rows = (uint32_t)p.a_rows;
+    lb.ld = (uint32_t)(p.ldb * ELEM<DT>);
     int64_t depth;                                      // of the summed axis
     int32_t row_of[TM];                                 // rows of a that the lane's results are of
     if constexpr (MODE == PRODUCT_DW) {
@@ -591,7 +592,7 @@ k_product(const Product p) {
         }
         la.start_across();
         lb.base = (const char*)p.b;
-        lb.rows = p.b_rows;
+        lb.rows = (uint32_t)p.b_rows;
         lb.list = p.b_list;
         lb.first = part.first;
         lb.end = p.b_list != nullptr || p.b_rows > part.last ? part.last : p.b_rows;
