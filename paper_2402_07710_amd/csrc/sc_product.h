@@ -550,9 +550,11 @@ k_product(const Product p) {
     if constexpr (MODE == PRODUCT_DW) {
         const uint32_t m_tiles = p.M > BM ? (uint32_t)(p.M + BM - 1) / BM : 1u;
         row_unit = unit / (m_tiles * n_tiles);
-        const uint32_t tile = unit - row_unit * (m_tiles * n_tiles);
-        m_tile = (int)(tile / n_tiles);
-        n_tile = (int)(tile - m_tile * n_tiles);
+        // bands of four tiles of m, across n: a run of them reads few columns of both sides
+        const uint32_t tile = unit - row_unit * (m_tiles * n_tiles), band = tile / (4 * n_tiles), in_band = tile - band * (4 * n_tiles);
+        const uint32_t high = m_tiles - 4 * band < 4 ? m_tiles - 4 * band : 4;
+        n_tile = (int)(in_band / high);
+        m_tile = (int)(4 * band + in_band - n_tile * high);
     } else {
         row_unit = unit / n_tiles;
         n_tile = (int)(unit - row_unit * n_tiles);
