@@ -109,17 +109,11 @@ bool channels_ok(int C) { return C >= 1 && C <= SC_CHANNELS_MAX; }
 bool rows_ok(const void* p, int64_t n, int64_t ld, int C, int dtype) {
     return (p != nullptr || n == 0) && aligned_to(p, elem(dtype)) && ld >= C && ld <= SC_LD_MAX;
 }
-// every row starts and ends at a 16-byte boundary
-bool whole_chunks(const void* p, int64_t ld, int C, int dtype) {
-    const int per = 16 / elem(dtype);
-    return aligned16(p) && ld % per == 0 && C % per == 0;
-}
-
-int launch(int dtype, int mode, const Product& p, bool whole, hipStream_t s) {
+int launch(int dtype, int mode, const Product& p, hipStream_t s) {
     const int cus = compute_units();
-    if (dtype == SC_F32) return launch_product_f32(mode, p, whole, cus, s);
-    if (dtype == SC_F16) return launch_product_f16(mode, p, whole, cus, s);
-    return launch_product_bf16(mode, p, whole, cus, s);
+    if (dtype == SC_F32) return launch_product_f32(mode, p, cus, s);
+    if (dtype == SC_F16) return launch_product_f16(mode, p, cus, s);
+    return launch_product_bf16(mode, p, cus, s);
 }
 
 struct Entries {                   // what tells a grouped layer from a linear one
@@ -163,7 +157,7 @@ int forward(const void* x, int64_t ldx, const Entries& e, const void* weight, co
     p.out = y;
     p.ldo = ldy;
     p.out_f32 = dtype_out == SC_F32 && dtype_in != SC_F32;
-    return launch(dtype_in, PRODUCT_FWD, p, whole_chunks(x, ldx, C_in, dtype_in) && whole_chunks(weight, C_out, C_out, dtype_in), s);
+    return launch(dtype_in, PRODUCT_FWD, p, s);
 }
 
 size_t grad_bytes(int64_t n, int C_out, int dtype) { return align_up((size_t)n * C_out * elem(dtype), 256); }
@@ -227,7 +221,7 @@ int backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const Ent
         p.K = C_out;
         p.out = dx;
         p.ldo = lddx;
-        const int rc = launch(dtype, PRODUCT_DX, p, whole_chunks(grad, ldg, C_out, dtype) && whole_chunks(weight, C_out, C_out, dtype), s);
+        const int rc = launch(dtype, PRODUCT_DX, p, s);
         if (rc != SC_OK) return rc;
     }
     if (sums) {
@@ -251,8 +245,7 @@ int backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const Ent
         p.out_bias = dbias;
         p.partial = (float*)((char*)workspace + own);
         p.slots = weight_slots(e.n, p.per);
-        const bool whole = whole_chunks(grad, ldg, C_out, dtype) && (dweight == nullptr || whole_chunks(x, ldx, C_in, dtype));
-        int rc = launch(dtype, PRODUCT_DW, p, whole, s);
+        int rc = launch(dtype, PRODUCT_DW, p, s);
         if (rc != SC_OK) return rc;
         if (e.n > p.per) {
             // 1024 values a workgroup leave most of the chip idle below some thousands of them (narrow / wide: 27 groups of 64 x 64 5 / 10 us)

@@ -300,6 +300,13 @@ __device__ inline Part find_part(const int32_t* __restrict__ starts, int groups,
 // ---- tiles in LDS ---------------------------------------------------------------------------------------
 // Stands in for chunks that lie beyond an operand's rows or channels.
 __device__ __align__(16) uint4 g_no_chunk;
+// Stands in for entries of a list beyond its end.
+__device__ int32_t g_no_row = -1;
+constexpr int RING = 256;          // bytes of LDS for the rows of a step's entries; two of them for each operand
+// 4 bytes per lane from global memory straight into LDS, as load_to_lds does with 16
+__device__ inline void load_word_to_lds(const void* src, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(src), "s"(lds) : "m0", "memory");
+}
 
 // Where a chunk of a line lies in it: its number, turned by the line's, so that what the LDS hands out in one cycle fills its 64 banks once.
 // ALONG: lines are rows of the tile, LINE chunks of the summed axis.  16-byte reads go 16 lanes a cycle, lanes 0-3, 12-15, 20-23 and 24-27 (or the others of 32): one
@@ -379,8 +386,10 @@ __device__ inline f32x4 multiply(uint4 a, uint4 b, f32x4 c) {
     }
 }
 
-// What one thread brings of an operand's tiles: PASSES chunks a step.  `end` is where the summed axis ends (ALONG: channels, ACROSS: rows
-// of the operand that count), STRIDE how much of it a step takes.
+// What one thread brings of an operand's tiles: PASSES chunks a step, straight into LDS and from any address that suits their elements.  `end` is where the
+// summed axis ends (ALONG: channels, ACROSS: rows of the operand that count), STRIDE how much of it a step takes.  Zeros stand for what lies beyond it: other
+// values there, infinities among them, would be in every sum.  Beyond a line's other end they are in sums that are not stored, so there whatever follows in
+// memory is read, except behind the operand's last element, where nothing may follow.  WHOLE: lines are whole chunks.
 template <int DT, bool ACROSS, int LINES, int LINE, int NTH, int STRIDE, bool WHOLE>
 struct Loader {
     static constexpr int PASSES = LINES * LINE / NTH, PER = 16 / ELEM<DT>;
@@ -391,17 +400,16 @@ struct Loader {
     const int32_t* list;                       // ACROSS
     int limit, col0;                           // ACROSS: channels there are, and the tile's first
     const char* ptr[PASSES];                   // of the step that is fetched next; ACROSS with a list: unused
-    int32_t at[ACROSS ? PASSES : 1];           // ACROSS with a list: its rows
-    uint4 held[WHOLE ? 1 : PASSES];
+    uint32_t ring;                             // ACROSS with a list: its rows of the steps ahead, in LDS
 
-    __device__ static int line_of(int i) { return (i * NTH + (int)threadIdx.x) / LINE; }
-    __device__ static int chunk_of(int i) {
+    __device__ __forceinline__ static int line_of(int i) { return (i * NTH + (int)threadIdx.x) / LINE; }
+    __device__ __forceinline__ static int chunk_of(int i) {
         const int line = line_of(i), c = (int)threadIdx.x % LINE;
         return c ^ (ACROSS ? across_turn<DT, LINE>(line) : along_turn<LINE>(line));
     }
     // ALONG: lines are rows begin .. of the operand, or those that the list names from there on.  Beyond the last, and for a row that is none,
     // some other row is read: the results are not used.
-    __device__ void start_along(const int32_t* rows_list, int64_t begin, int64_t stop) {
+    __device__ __forceinline__ void start_along(const int32_t* rows_list, int64_t begin, int64_t stop) {
         first = 0;
 #pragma unroll
         for (int i = 0; i < PASSES; ++i) {
@@ -412,118 +420,98 @@ struct Loader {
             ptr[i] = base + (uint64_t)(uint32_t)r * ld + chunk_of(i) * 16;
         }
     }
-    // ACROSS: columns beyond the last read some other chunk
-    __device__ const char* column(int i) const {
+    // ACROSS: the channels of a pass's chunk that there are; a chunk beyond the last reads the first
+    __device__ __forceinline__ int channels(int i) const { return limit - (col0 + chunk_of(i) * PER); }
+    __device__ __forceinline__ const char* column(int i) const {
         const int channel = col0 + chunk_of(i) * PER;
-        return base + (int64_t)(WHOLE && channel >= limit ? 0 : channel) * ELEM<DT>;
+        return base + (int64_t)(channel < limit ? channel : 0) * ELEM<DT>;
     }
-    __device__ void start_across() {
-        if (list != nullptr) {
-            take_rows(0);
-            return;
-        }
+    // ... whose 16 bytes, `offset` bytes from the base, may reach beyond the operand's last element
+    __device__ __forceinline__ int64_t extent() const { return (int64_t)(rows - 1) * ld + (int64_t)limit * ELEM<DT>; }
+    __device__ __forceinline__ int readable(int i, int64_t offset) const { return WHOLE || offset + 16 <= extent() ? PER : channels(i); }
+    __device__ __forceinline__ void start_across() {
+        if (list != nullptr) return;
 #pragma unroll
         for (int i = 0; i < PASSES; ++i) ptr[i] = column(i) + (uint64_t)(uint32_t)(first + line_of(i)) * ld;
     }
-    __device__ void take_rows(int s) {
-        if constexpr (ACROSS) {
+    // The rows of step s, by one wavefront, a step before its chunks are asked for.  They go through LDS like the chunks: in registers the compiler
+    // moves them at the end of the loop, and waits for them and for all that was asked for since.
+    __device__ __forceinline__ void ask_rows(int s) {
+        static_assert(!ACROSS || STRIDE <= WAVE, "a step's rows are one load");
+        const int lane = threadIdx.x & 63;
+        const int64_t e = first + (int64_t)s * STRIDE + lane;
+        load_word_to_lds(lane < STRIDE && e < end ? list + e : &g_no_row, __builtin_amdgcn_readfirstlane(ring + (s & 1) * RING));
+    }
+    // one chunk of which `there` elements are to be read, PER or more: all
+    __device__ __forceinline__ static void bring(const char* p, int there, uint32_t lds, int i) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const uint32_t pass = lds + i * NTH * 16;
+        if (WHOLE || there >= PER || there <= 0) {
+            load_to_lds(there > 0 ? (const void*)p : (const void*)&g_no_chunk, __builtin_amdgcn_readfirstlane(pass + wave * 1024));
+        } else {
+            uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < PASSES; ++i) {
-                const int64_t e = first + (int64_t)s * STRIDE + line_of(i);
-                // not looked at before it is used, a step later: a comparison here would wait for it, and for the chunks ahead of it
-                at[i] = -1;
-                if (e < end) at[i] = list[e];
-            }
+            for (int j = 0; j < PER; ++j)
+                if (j < there) {
+                    if constexpr (DT == SC_F32) w[j] = reinterpret_cast<const uint32_t*>(p)[j];
+                    else w[j / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[j] << (16 * (j & 1));
+                }
+            *(__attribute__((address_space(3))) u32x4*)(pass + threadIdx.x * 16) = u32x4{w[0], w[1], w[2], w[3]};
         }
     }
-    __device__ void fetch(int s, uint32_t lds) {
+    __device__ __forceinline__ void fetch(int s, uint32_t lds) {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const int64_t from = first + (int64_t)s * STRIDE;
-        const bool listed = ACROSS && list != nullptr;
-        if constexpr (WHOLE) {             // channels are whole chunks, rows aligned
-            const void* const none = &g_no_chunk;
-            if (listed) {
+        if (ACROSS && list != nullptr) {
+            uint32_t r[PASSES];
 #pragma unroll
-                for (int i = 0; i < PASSES; ++i) {
-                    const int32_t r = at[ACROSS ? i : 0];
-                    load_to_lds((uint32_t)r < rows ? (const void*)(column(i) + (uint64_t)(uint32_t)r * ld) : none, __builtin_amdgcn_readfirstlane(lds + (i * NTH + wave * 64) * 16));
-                }
-            } else if (from + STRIDE <= end) {
-                const uint64_t step = ACROSS ? (uint64_t)STRIDE * ld : STRIDE * ELEM<DT>;
+            for (int i = 0; i < PASSES; ++i) r[i] = *(lds_uint32)(ring + (s & 1) * RING + line_of(i) * 4);
 #pragma unroll
-                for (int i = 0; i < PASSES; ++i) {
-                    load_to_lds(ptr[i], __builtin_amdgcn_readfirstlane(lds + (i * NTH + wave * 64) * 16));
-                    ptr[i] += step;
-                }
-            } else {
-                const int left = end > from ? (int)(end - from) : 0;
-#pragma unroll
-                for (int i = 0; i < PASSES; ++i)
-                    load_to_lds((ACROSS ? line_of(i) : chunk_of(i) * PER) < left ? (const void*)ptr[i] : none, __builtin_amdgcn_readfirstlane(lds + (i * NTH + wave * 64) * 16));
+            for (int i = 0; i < PASSES; ++i) {
+                const char* p = column(i) + (uint64_t)r[i] * ld;
+                bring(p, r[i] < rows ? readable(i, p - base) : 0, lds, i);
             }
-        } else {
+        } else if (from + STRIDE <= end &&
+                   (!ACROSS || WHOLE || (from + STRIDE - 1) * ld + (int64_t)((limit + PER - 1) / PER) * 16 <= extent())) {
             const uint64_t step = ACROSS ? (uint64_t)STRIDE * ld : STRIDE * ELEM<DT>;
 #pragma unroll
             for (int i = 0; i < PASSES; ++i) {
-                const char* p = ptr[i];
-                int there;                 // elements of the chunk
-                if (ACROSS) {
-                    there = limit - (col0 + chunk_of(i) * PER);
-                    bool ok = from + line_of(i) < end;
-                    if (listed) {
-                        const int32_t r = at[ACROSS ? i : 0];
-                        ok = (uint32_t)r < rows;
-                        p = column(i) + (uint64_t)(uint32_t)r * ld;
-                    }
-                    if (!ok) there = 0;
-                } else {
-                    there = (int)(end - from) - chunk_of(i) * PER;
-                }
-                uint4 v = make_uint4(0, 0, 0, 0);
-                if (there >= PER) {
-                    v = load_chunk(p);
-                } else if (there > 0) {
-                    uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-                    for (int j = 0; j < PER; ++j)
-                        if (j < there) {
-                            if constexpr (DT == SC_F32) w[j] = reinterpret_cast<const uint32_t*>(p)[j];
-                            else w[j / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[j] << (16 * (j & 1));
-                        }
-                    v = make_uint4(w[0], w[1], w[2], w[3]);
-                }
-                held[i] = v;
+                load_to_lds(ptr[i], __builtin_amdgcn_readfirstlane(lds + (i * NTH + wave * 64) * 16));
                 ptr[i] += step;
             }
-        }
-        if (listed) take_rows(s + 1);
-    }
-    __device__ void put(uint4* tile) {
-        if constexpr (!WHOLE) {
+        } else {
+            const int left = end > from ? (int)(end - from < STRIDE ? end - from : STRIDE) : 0;
 #pragma unroll
-            for (int i = 0; i < PASSES; ++i) tile[i * NTH + threadIdx.x] = held[i];
+            for (int i = 0; i < PASSES; ++i) {
+                if constexpr (ACROSS) {
+                    bring(ptr[i], line_of(i) < left ? readable(i, ptr[i] - base) : 0, lds, i);
+                    ptr[i] += (uint64_t)STRIDE * ld;
+                } else {
+                    bring(ptr[i], left - chunk_of(i) * PER, lds, i);
+                }
+            }
         }
     }
 };
 
 // ---- the kernel -----------------------------------------------------------------------------------------
-// WM x WN wavefronts share a tile, KW sets of them the summed axis, of which a set takes SB bytes a step; STAGES buffers.  WHOLE: rows and
-// channels are whole chunks of 16 bytes, aligned; otherwise chunks pass through registers, by unaligned loads, element by element at the end of a row.
+// WM x WN wavefronts share a tile, KW sets of them the summed axis, of which a set takes SB bytes a step.  WHOLE: the operands' lines are whole chunks
+// of 16 bytes, at any alignment of their elements (what the others need is in registers through the whole loop: weight gradients 36 us or 29).
 // RESIDUAL: there may be one; what is held of it costs the others wavefronts (128 x 128: 174 registers or 123).
-template <int DT, int MODE, int BM_, int BN_, int WM_, int WN_, int KW_, int SB_, int STAGES_>
+template <int DT, int MODE, int BM_, int BN_, int WM_, int WN_, int KW_, int SB_>
 struct ProductShape {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KW = KW_, SB = SB_, STAGES = STAGES_;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KW = KW_, SB = SB_;
     static constexpr int NTH = 64 * WM * WN * KW, TM = BM / 16 / WM, TN = BN / 16 / WN;
     static constexpr int STEP = SB / ELEM<DT>;                        // places on the summed axis per set and step
     static constexpr bool A_ACROSS = MODE == PRODUCT_DW, B_ACROSS = MODE != PRODUCT_DX;
     static constexpr int A_LINES = A_ACROSS ? STEP * KW : BM, A_LINE = A_ACROSS ? BM * ELEM<DT> / 16 : SB / 16 * KW;
     static constexpr int B_LINES = B_ACROSS ? STEP * KW : BN, B_LINE = B_ACROSS ? BN * ELEM<DT> / 16 : SB / 16 * KW;
     static constexpr int A_CHUNKS = A_LINES * A_LINE, B_CHUNKS = B_LINES * B_LINE;
-    static constexpr int BUFFER = (A_CHUNKS + B_CHUNKS) * 16;
+    static constexpr int BUFFER = (A_CHUNKS + B_CHUNKS) * 16, RINGS = MODE == PRODUCT_DW ? 4 * RING : 0;
     static constexpr int SUMS = (KW - 1) * WM * WN * TM * TN * 64 * 16;  // what the sets hand over in the end
     static constexpr int PIECES = WM * WN * 16 * (TN * 16 + 4) * 4;      // results on their way out
     static constexpr int lds(int64_t steps) {
-        const int buffers = (steps < STAGES ? (int)steps : STAGES) * BUFFER, end = SUMS > PIECES ? SUMS : PIECES;
+        const int buffers = RINGS + (steps > 1 ? 2 : 1) * BUFFER, end = SUMS > PIECES ? SUMS : PIECES;
         return buffers > end ? buffers : end;
     }
 };
@@ -534,10 +522,10 @@ __device__ inline bool no_row(const Product& p, int64_t m) {
     return r < 0 || r >= p.a_rows;
 }
 
-template <int DT, int MODE, int BM, int BN, int WM, int WN, int KW, int SB, int STAGES, bool WHOLE, bool RESIDUAL>
+template <int DT, int MODE, int BM, int BN, int WM, int WN, int KW, int SB, bool WHOLE, bool RESIDUAL>
 __global__ void __launch_bounds__(64 * WM * WN * KW, 2)
 k_product(const Product p) {
-    using S = ProductShape<DT, MODE, BM, BN, WM, WN, KW, SB, STAGES>;
+    using S = ProductShape<DT, MODE, BM, BN, WM, WN, KW, SB>;
     constexpr int NTH = S::NTH, TM = S::TM, TN = S::TN;
     extern __shared__ __align__(16) uint4 product_lds[];
 
@@ -568,7 +556,7 @@ k_product(const Product p) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int set = wave / (WM * WN), wm = wave % (WM * WN) / WN, wn = wave % WN;
     const int n0 = n_tile * BN, m0 = m_tile * BM;
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)product_lds;
+    const uint32_t rings = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)product_lds, lds0 = rings + S::RINGS;
 
     constexpr int STRIDE = S::STEP * KW;
     Loader<DT, S::A_ACROSS, S::A_LINES, S::A_LINE, NTH, STRIDE, WHOLE> la;
@@ -582,6 +570,7 @@ k_product(const Product p) {
     if constexpr (MODE == PRODUCT_DW) {
         depth = part.last - part.first;
         la.list = p.a_list;
+        la.ring = rings;
         la.first = part.first;
         la.end = p.a_list != nullptr || p.a_rows > part.last ? part.last : p.a_rows;
         la.limit = p.M;
@@ -596,6 +585,7 @@ k_product(const Product p) {
         lb.base = (const char*)p.b;
         lb.rows = (uint32_t)p.b_rows;
         lb.list = p.b_list;
+        lb.ring = rings + 2 * RING;
         lb.first = part.first;
         lb.end = p.b_list != nullptr || p.b_rows > part.last ? part.last : p.b_rows;
         lb.limit = p.N;
@@ -629,15 +619,18 @@ k_product(const Product p) {
         }
     }
     const int steps = (int)((depth + STRIDE - 1) / STRIDE);
+    auto ask_rows = [&](int s) __attribute__((always_inline)) {
+        if constexpr (MODE == PRODUCT_DW) {
+            static_assert(WM * WN > 1, "a wavefront for each side's list");
+            if (wave == 0 && la.list != nullptr) la.ask_rows(s);
+            if (wave == 1 && lb.list != nullptr) lb.ask_rows(s);
+        }
+    };
     auto fetch = [&](int s) __attribute__((always_inline)) {
-        const uint32_t at = lds0 + s % STAGES * S::BUFFER;
+        const uint32_t at = lds0 + (s & 1) * S::BUFFER;
         la.fetch(s, at);
         lb.fetch(s, at + S::A_CHUNKS * 16);
-    };
-    auto put = [&](int s) __attribute__((always_inline)) {
-        uint4* at = product_lds + s % STAGES * (S::BUFFER / 16);
-        la.put(at);
-        lb.put(at + S::A_CHUNKS);
+        ask_rows(s + 1);
     };
     typename std::conditional<S::A_ACROSS, AcrossReader<DT, S::A_LINE, TM, SB / 64>, AlongReader<DT, S::A_LINE, TM, SB / 64>>::type ra(
         lds0, wm * TM * 16, set * (S::A_ACROSS ? S::STEP : SB / 16));
@@ -654,24 +647,19 @@ k_product(const Product p) {
     const bool sums = MODE == PRODUCT_DW && p.out_bias != nullptr && m_tile == 0 && wm == 0;
     const uint32_t one = DT == SC_F32 ? 0x3f800000u : DT == SC_F16 ? 0x3c003c00u : 0x3f803f80u;
 
-    // A step's chunks are asked for STAGES - 1 steps ahead, into the buffer that was read last.
-    static_assert(STAGES == 2 || (STAGES == 3 && WHOLE), "chunks in registers: one step ahead");
-    constexpr int LOADS = S::A_CHUNKS / NTH + S::B_CHUNKS / NTH;
-    if (steps > 0) {
-        fetch(0);
-        put(0);
-        if (STAGES == 3 && steps > 1) fetch(1);
-    }
-    int at_stage = 0;
-    for (int s = 0; s < steps; ++s) {
-        if constexpr (WHOLE) {                         // the step's chunks are in LDS; those of the next may still be on their way
-            if (STAGES == 3 && s + 1 < steps) __builtin_amdgcn_s_waitcnt(0x0f70 | (LOADS & 15) | (LOADS >> 4) << 14);
-            else __builtin_amdgcn_s_waitcnt(0x0f70);
+    if constexpr (MODE == PRODUCT_DW) {
+        if (la.list != nullptr || lb.list != nullptr) {
+            ask_rows(0);
+            __builtin_amdgcn_s_waitcnt(0x0f70);
+            lds_barrier();
         }
+    }
+    if (steps > 0) fetch(0);
+    for (int s = 0; s < steps; ++s) {
+        __builtin_amdgcn_s_waitcnt(0x0f70);            // vmcnt(0): the step's chunks are in LDS
         lds_barrier();                                 // ... of all wavefronts, which are done with the other buffer
-        if (s + STAGES - 1 < steps) fetch(s + STAGES - 1);
-        const uint32_t buffer = at_stage * S::BUFFER;
-        at_stage = at_stage + 1 < STAGES ? at_stage + 1 : 0;
+        if (s + 1 < steps) fetch(s + 1);
+        const uint32_t buffer = (s & 1) * S::BUFFER;
 #pragma unroll
         for (int c = 0; c < SB / 64; ++c) {
             uint4 fa[TM], fb[TN];
@@ -690,7 +678,6 @@ k_product(const Product p) {
                 }
             }
         }
-        if (!WHOLE && s + 1 < steps) put(s + 1);
     }
 
     if constexpr (KW > 1) {                            // the sets' sums, in the order of the sets
@@ -877,14 +864,14 @@ k_product(const Product p) {
 
 // ---- host ----------------------------------------------------------------------------------------------
 // The three products for one element type (sc_product_*.hip, one translation unit each).
-int launch_product_f32(int mode, const Product& p, bool whole, int cus, hipStream_t s);
-int launch_product_f16(int mode, const Product& p, bool whole, int cus, hipStream_t s);
-int launch_product_bf16(int mode, const Product& p, bool whole, int cus, hipStream_t s);
+int launch_product_f32(int mode, const Product& p, int cus, hipStream_t s);
+int launch_product_f16(int mode, const Product& p, int cus, hipStream_t s);
+int launch_product_bf16(int mode, const Product& p, int cus, hipStream_t s);
 
-template <int DT, int MODE, int BM, int BN, int WM, int WN, int KW, int SB, int STAGES, bool WHOLE, bool RESIDUAL>
-int run_product(Product p, hipStream_t s) {
-    using S = ProductShape<DT, MODE, BM, BN, WM, WN, KW, SB, STAGES>;
-    constexpr auto kernel = k_product<DT, MODE, BM, BN, WM, WN, KW, SB, STAGES, WHOLE, RESIDUAL>;
+template <int DT, int MODE, int BM, int BN, int WM, int WN, int KW, int SB, bool WHOLE, bool RESIDUAL>
+int start_product(Product p, hipStream_t s) {
+    using S = ProductShape<DT, MODE, BM, BN, WM, WN, KW, SB>;
+    constexpr auto kernel = k_product<DT, MODE, BM, BN, WM, WN, KW, SB, WHOLE, RESIDUAL>;
     const int64_t n_tiles = (p.N + BN - 1) / BN, m_tiles = MODE == PRODUCT_DW && p.M > BM ? (p.M + BM - 1) / BM : 1;
     if (MODE != PRODUCT_DW) {
         // groups: the tiles that are full, and one that is not of every group that there can be
@@ -897,68 +884,66 @@ int run_product(Product p, hipStream_t s) {
     const int64_t depth = MODE == PRODUCT_DW ? p.per : p.K;
     const size_t lds = S::lds((depth + S::STEP * KW - 1) / (S::STEP * KW));
     static bool done[MAX_DEVICES];
-    const int rc = allow_lds((const void*)kernel, S::lds(STAGES), done);
+    const int rc = allow_lds((const void*)kernel, S::lds(2), done);
     if (rc != SC_OK) return rc;
     SC_LAUNCH(KID_PRODUCT, kernel, grid, dim3(S::NTH), lds, s, p);
     return SC_OK;
 }
-// MANY: large tiles have a kernel without residual apart, and none for rows that are not whole chunks.
-template <int DT, int MODE, int BM, int BN, int WM, int WN, int KW, int SB = 128, int STAGES = 2, bool MANY = false>
-int run_product(const Product& p, bool whole, hipStream_t s) {
-    if constexpr (MODE == PRODUCT_FWD) {
-        if constexpr (MANY) {
-            if (p.residual == nullptr) return run_product<DT, MODE, BM, BN, WM, WN, KW, SB, STAGES, true, false>(p, s);
-            return run_product<DT, MODE, BM, BN, WM, WN, KW, SB, STAGES, true, true>(p, s);
-        } else {
-            return whole ? run_product<DT, MODE, BM, BN, WM, WN, KW, SB, STAGES, true, true>(p, s)
-                         : run_product<DT, MODE, BM, BN, WM, WN, KW, SB, 2, false, true>(p, s);
-        }
-    } else if constexpr (MANY) {
-        return run_product<DT, MODE, BM, BN, WM, WN, KW, SB, STAGES, true, false>(p, s);
-    } else {
-        return whole ? run_product<DT, MODE, BM, BN, WM, WN, KW, SB, STAGES, true, false>(p, s)
-                     : run_product<DT, MODE, BM, BN, WM, WN, KW, SB, 2, false, false>(p, s);
-    }
+// TWO: large tiles have a kernel without residual apart.
+template <int DT, int MODE, int BM, int BN, int WM, int WN, int KW, int SB, bool RESIDUAL>
+int start_product(const Product& p, hipStream_t s) {
+    constexpr int PER = 16 / ELEM<DT>;
+    const bool whole = p.N % PER == 0 && (MODE == PRODUCT_DW ? p.M : p.K) % PER == 0;      // DX: its weights' lines are K long
+    const bool along = MODE == PRODUCT_DX && p.K % PER == 0;
+    return whole || along ? start_product<DT, MODE, BM, BN, WM, WN, KW, SB, true, RESIDUAL>(p, s)
+                          : start_product<DT, MODE, BM, BN, WM, WN, KW, SB, false, RESIDUAL>(p, s);
+}
+template <int DT, int MODE, int BM, int BN, int WM, int WN, int KW, int SB = 128, bool TWO = false>
+int run_product(const Product& p, hipStream_t s) {
+    if constexpr (MODE != PRODUCT_FWD) return start_product<DT, MODE, BM, BN, WM, WN, KW, SB, false>(p, s);
+    else if (TWO && p.residual == nullptr) return start_product<DT, MODE, BM, BN, WM, WN, KW, SB, !TWO>(p, s);
+    else return start_product<DT, MODE, BM, BN, WM, WN, KW, SB, true>(p, s);
 }
 // Which tile: row_tile, weight_tile.
 template <int DT, int MODE>
-int choose_product(const Product& p, bool whole, int cus, hipStream_t s) {
+int choose_product(const Product& p, int cus, hipStream_t s) {
     if constexpr (MODE == PRODUCT_DW) {
-        if (weight_tile(p.M, p.N) == 64) return run_product<DT, MODE, 64, 64, 2, 2, 1>(p, whole, s);
-        return run_product<DT, MODE, 128, 128, 2, 2, 1>(p, whole, s);
+        switch (weight_tile(p.n, p.M, p.N)) {
+            case WEIGHTS_64_64: return run_product<DT, MODE, 64, 64, 2, 2, 1>(p, s);
+            case WEIGHTS_32_128: return run_product<DT, MODE, 32, 128, 1, 4, 1>(p, s);
+            case WEIGHTS_128_32: return run_product<DT, MODE, 128, 32, 4, 1, 1>(p, s);
+            case WEIGHTS_64_128: return run_product<DT, MODE, 64, 128, 2, 2, 1>(p, s);
+            case WEIGHTS_128_64: return run_product<DT, MODE, 128, 64, 2, 2, 1>(p, s);
+            default: return run_product<DT, MODE, 128, 128, 2, 2, 1>(p, s);
+        }
     } else {
         constexpr bool FWD = MODE == PRODUCT_FWD, WIDE = DT != SC_F32;
-        const RowTile tile = row_tile(p.n, p.starts == nullptr ? 0 : p.groups, p.N, p.K, FWD, WIDE && whole, cus);
-        switch (tile) {
-            case TILE_16_32: return run_product<DT, MODE, 16, 32, 1, 1, 4>(p, whole, s);
-            case TILE_16_32_DEEP: return run_product<DT, MODE, 16, 32, 1, 1, 8>(p, whole, s);
-            case TILE_32_64: return run_product<DT, MODE, 32, 64, 2, 2, 2>(p, whole, s);
-            case TILE_64_64: return run_product<DT, MODE, 64, 64, 2, 2, 1>(p, whole, s);
-            case TILE_64_64_DEEP: return run_product<DT, MODE, 64, 64, 2, 2, 2>(p, whole, s);
-            case TILE_128_32: return run_product<DT, MODE, 128, 32, 4, 1, 1>(p, whole, s);
-            case TILE_128_64: return run_product<DT, MODE, 128, 64, 4, 1, 1>(p, whole, s);
-            default: break;
-        }
-        if (!whole) return run_product<DT, MODE, 128, 128, 2, 2, 1>(p, false, s);
-        switch (tile) {
+        switch (row_tile(p.n, p.starts == nullptr ? 0 : p.groups, p.N, p.K, FWD, WIDE, cus)) {
+            case TILE_16_32: return run_product<DT, MODE, 16, 32, 1, 1, 4>(p, s);
+            case TILE_16_32_DEEP: return run_product<DT, MODE, 16, 32, 1, 1, 8>(p, s);
+            case TILE_32_64: return run_product<DT, MODE, 32, 64, 2, 2, 2>(p, s);
+            case TILE_64_64: return run_product<DT, MODE, 64, 64, 2, 2, 1>(p, s);
+            case TILE_64_64_DEEP: return run_product<DT, MODE, 64, 64, 2, 2, 2>(p, s);
+            case TILE_128_32: return run_product<DT, MODE, 128, 32, 4, 1, 1>(p, s);
+            case TILE_128_64: return run_product<DT, MODE, 128, 64, 4, 1, 1>(p, s);
             case TILE_64_128:
-                if constexpr (FWD) return run_product<DT, MODE, 64, 128, 2, 2, 1, 64, 2, true>(p, true, s);
+                if constexpr (FWD) return run_product<DT, MODE, 64, 128, 2, 2, 1, 64, true>(p, s);
                 break;
-            case TILE_128_128_SHORT: return run_product<DT, MODE, 128, 128, 2, 2, 1, 64, 2, true>(p, true, s);
+            case TILE_128_128_SHORT: return run_product<DT, MODE, 128, 128, 2, 2, 1, 64, true>(p, s);
             case TILE_LARGE:
-                if constexpr (WIDE && FWD) return run_product<DT, MODE, 128, 256, 2, 2, 1, 64, 2, true>(p, true, s);
-                else if constexpr (WIDE) return run_product<DT, MODE, 256, 256, 2, 4, 1, 128, 2, true>(p, true, s);
+                if constexpr (WIDE && FWD) return run_product<DT, MODE, 128, 256, 2, 2, 1, 64, true>(p, s);
+                else if constexpr (WIDE) return run_product<DT, MODE, 256, 256, 2, 4, 1, 128, true>(p, s);
                 break;
             default: break;
         }
-        return run_product<DT, MODE, 128, 128, 2, 2, 1, 128, 2, true>(p, true, s);
+        return run_product<DT, MODE, 128, 128, 2, 2, 1, 128, true>(p, s);
     }
 }
 template <int DT>
-int launch_product(int mode, const Product& p, bool whole, int cus, hipStream_t s) {
-    if (mode == PRODUCT_FWD) return choose_product<DT, PRODUCT_FWD>(p, whole, cus, s);
-    if (mode == PRODUCT_DX) return choose_product<DT, PRODUCT_DX>(p, whole, cus, s);
-    return choose_product<DT, PRODUCT_DW>(p, whole, cus, s);
+int launch_product(int mode, const Product& p, int cus, hipStream_t s) {
+    if (mode == PRODUCT_FWD) return choose_product<DT, PRODUCT_FWD>(p, cus, s);
+    if (mode == PRODUCT_DX) return choose_product<DT, PRODUCT_DX>(p, cus, s);
+    return choose_product<DT, PRODUCT_DW>(p, cus, s);
 }
 
 }  // namespace sc

@@ -2,5 +2,5 @@
 #include "sc_product.h"
 
 namespace sc {
-int launch_product_f16(int mode, const Product& p, bool whole, int cus, hipStream_t s) { return launch_product<SC_F16>(mode, p, whole, cus, s); }
+int launch_product_f16(int mode, const Product& p, int cus, hipStream_t s) { return launch_product<SC_F16>(mode, p, cus, s); }
 }  // namespace sc

@@ -180,7 +180,7 @@ constexpr int64_t grid_rows(int64_t groups) { return (groups + GRID_COLUMNS - 1)
 // Tile of the result that a workgroup owns, by the rows and columns there are.  Few rows a group: 16 rows, four wavefronts share the summed axis.
 enum RowTile { TILE_16_32, TILE_16_32_DEEP, TILE_32_64, TILE_64_64, TILE_64_64_DEEP, TILE_128_32, TILE_128_64, TILE_64_128, TILE_128_128, TILE_128_128_SHORT, TILE_LARGE };
 // `groups` 0: a linear layer.
-constexpr RowTile row_tile(int64_t entries, int64_t groups, int64_t columns, int64_t depth, bool forward, bool large_too, int64_t cus) {
+constexpr RowTile row_tile(int64_t entries, int64_t groups, int64_t columns, int64_t depth, bool forward, bool half, int64_t cus) {
     const int64_t parts = groups == 0 ? 1 : groups < entries ? groups : entries, each = entries / parts;
     const int64_t tiles = (entries + 15 * parts) / 16 * ((columns + 31) / 32);       // of 16 x 32
     if (tiles <= 2 * cus) return depth >= 1024 && tiles <= cus ? TILE_16_32_DEEP : TILE_16_32;
@@ -188,7 +188,7 @@ constexpr RowTile row_tile(int64_t entries, int64_t groups, int64_t columns, int
     if (columns <= 32) return TILE_128_32;
     if (tiles <= 16 * cus || each <= 64) return depth >= 512 ? TILE_64_64_DEEP : TILE_64_64;
     if (tiles <= 32 * cus || columns <= 64) return TILE_128_64;
-    if (groups == 0 && large_too && depth >= 256 && columns >= 256 && (entries / 128) * (columns / 256) >= 2 * cus) return TILE_LARGE;
+    if (groups == 0 && half && depth >= 256 && columns >= 256 && (entries / 128) * (columns / 256) >= 2 * cus) return TILE_LARGE;
     if (!forward) return groups > 0 && depth >= 1024 ? TILE_128_128_SHORT : TILE_128_128;
     if (groups > 0) return TILE_128_128_SHORT;
     return depth <= 256 ? TILE_64_128 : TILE_128_128;
@@ -198,17 +198,26 @@ constexpr int64_t product_run(int64_t units, int64_t tiles_each) {
     const int64_t run = units * tiles_each / 64;
     return run < 1 ? 1 : run < tiles_each ? run : tiles_each;
 }
-// Tile of a weight gradient.
-constexpr int weight_tile(int64_t c_in, int64_t c_out) { return c_in <= 64 && c_out <= 64 ? 64 : 128; }
-constexpr int64_t weight_tiles(int64_t c_in, int64_t c_out) {
-    const int64_t t = weight_tile(c_in, c_out);
-    return (c_in > t ? (c_in + t - 1) / t : 1) * ((c_out + t - 1) / t);
+// Tile of a weight gradient, rows by columns of the matrix.
+enum WeightTile { WEIGHTS_64_64, WEIGHTS_32_128, WEIGHTS_128_32, WEIGHTS_64_128, WEIGHTS_128_64, WEIGHTS_128_128 };
+constexpr WeightTile weight_tile(int64_t entries, int64_t c_in, int64_t c_out) {
+    (void)entries;
+    if (c_in <= 64 && c_out <= 64) return WEIGHTS_64_64;
+    if (c_in <= 32) return WEIGHTS_32_128;
+    if (c_out <= 32) return WEIGHTS_128_32;
+    return c_in <= 64 ? WEIGHTS_64_128 : c_out <= 64 ? WEIGHTS_128_64 : WEIGHTS_128_128;
+}
+constexpr int64_t weight_tiles(int64_t entries, int64_t c_in, int64_t c_out) {
+    const WeightTile t = weight_tile(entries, c_in, c_out);
+    const int64_t m = t == WEIGHTS_32_128 ? 32 : t == WEIGHTS_64_64 || t == WEIGHTS_64_128 ? 64 : 128;
+    const int64_t n = t == WEIGHTS_128_32 ? 32 : t == WEIGHTS_64_64 || t == WEIGHTS_128_64 ? 64 : 128;
+    return (c_in > m ? (c_in + m - 1) / m : 1) * ((c_out + n - 1) / n);
 }
 // Entries that one workgroup sums of a group for a tile of its weight gradient: the groups are cut into parts so that there are about two
-// workgroups for each of 256 compute units, but parts of 512 entries at least, whose sums are written once and read once.
+// workgroups for each of 256 compute units, but parts of 128 entries at least, whose sums are written once and read once.
 constexpr int64_t weight_part(int64_t entries, int64_t c_in, int64_t c_out) {
-    const int64_t want = (entries * weight_tiles(c_in, c_out) + 511) / 512;
-    return ((want > 512 ? want : 512) + 63) / 64 * 64;
+    const int64_t want = (entries * weight_tiles(entries, c_in, c_out) + 511) / 512;
+    return ((want > 128 ? want : 128) + 63) / 64 * 64;
 }
 // Parts of groups that have several: a group of e entries has fewer than 2 e / part of them.
 constexpr int64_t weight_slots(int64_t entries, int64_t part) { return entries <= part ? 0 : 2 * entries / part + 1; }
