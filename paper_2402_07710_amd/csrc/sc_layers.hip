@@ -194,7 +194,7 @@ int backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const Ent
     int64_t ldg = lddy, grad_rows = e.grad_n;
     const int32_t* grad_list = e.grad_rows;
     if (act != SC_ACT_NONE && e.n > 0) {
-        const int chunks = (C_out + 7) / 8, each = chunks >= 2048 ? 1 : 2048 / chunks;
+        const int chunks = (C_out + 7) / 8, each = (int)act_grad_rows(e.n, chunks);
         const dim3 grid((unsigned)((e.n + each - 1) / each));
 #define SC_ACT_GRAD(DT) SC_LAUNCH(KID_ACT_GRAD, k_act_grad<DT>, grid, dim3(256), 0, s, dy, lddy, e.grad_n, e.grad_rows, pre, ldp, act, workspace, e.n, C_out, each)
         if (dtype == SC_F32) SC_ACT_GRAD(SC_F32);

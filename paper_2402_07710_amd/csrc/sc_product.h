@@ -793,7 +793,7 @@ k_product(const Product p) {
             }
         }
     }
-    // The columns that are left: 16 rows at a time through LDS, a wavefront's own piece of it, then element by element; one copy of the code.
+    // The columns that are left: 16 rows at a time through LDS, a wavefront's own piece of it, up to eight columns a lane; one copy of the code.
     const int rest = p.N - col_wave - whole_cols < COLS - whole_cols ? p.N - col_wave - whole_cols : COLS - whole_cols;
     const bool column_sums = MODE == PRODUCT_DW && sums;
     if constexpr (KW == 1 || WM * WN > 1) lds_barrier();     // the operands, or the sums, have been read by all
@@ -813,8 +813,15 @@ k_product(const Product p) {
         }
         asm volatile("" ::: "memory");
     }
+    if (rest <= 0) return;
+    const int chunks = (rest + 7) / 8, turn_rows = 64 / chunks, row0 = lane / chunks, c = (lane - row0 * chunks) * 8;
+    const int col = col_wave + whole_cols + c, there = rest - c < 8 ? rest - c : 8;
+    float bias_late[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) bias_late[j] = 0.f;
+    if (bias_row != nullptr) load8<DT>(bias_row, col, there, bias_late);
 #pragma unroll 1
-    for (int tm = 0; tm < TM && rest > 0; ++tm) {
+    for (int tm = 0; tm < TM; ++tm) {
 #pragma unroll
         for (int k = 0; k < TM; ++k)
             if (tm == k) {
@@ -823,39 +830,44 @@ k_product(const Product p) {
                     *reinterpret_cast<float4*>(piece + i * PITCH + 16 * tn + 4 * o) = make_float4(acc[k][tn][0], acc[k][tn][1], acc[k][tn][2], acc[k][tn][3]);
             }
         asm volatile("" ::: "memory");
-        int r = lane / rest, c = lane - r * rest;      // 64 elements a turn, along the rows
-        const int turn_rows = 64 / rest, turn_cols = 64 - turn_rows * rest;
 #pragma unroll 1
-        for (int t = lane; t < 16 * rest; t += 64) {
+        for (int r = row0; r < 16 && row0 < turn_rows; r += turn_rows) {
             const int64_t m = first_row + tm * 16 + r;
-            const int col = col_wave + whole_cols + c;
-            float v = piece[r * PITCH + whole_cols + c];
-            r += turn_rows;
-            c += turn_cols;
-            if (c >= rest) {
-                c -= rest;
-                ++r;
-            }
-            if (m >= end_row) continue;
+            if (m >= end_row) break;
+            const float4 lo = *reinterpret_cast<const float4*>(piece + r * PITCH + whole_cols + c), hi = *reinterpret_cast<const float4*>(piece + r * PITCH + whole_cols + c + 4);
+            float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
             if constexpr (MODE == PRODUCT_DW) {
-                if (to_partial) p.partial[(slot_row + m) * p.N + col] = v;
-                else store_elem<DT>(p.out, ((int64_t)g * p.M + m) * p.N + col, v);
+                if (to_partial) store8<SC_F32>(p.partial, (slot_row + m) * p.N + col, there, v);
+                else store8<DT>(p.out, ((int64_t)g * p.M + m) * p.N + col, there, v);
             } else {
-                if (no_row(p, m)) v = 0.f;
+                if (no_row(p, m)) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] = 0.f;
+                }
                 if constexpr (MODE == PRODUCT_FWD) {
-                    if (bias_row != nullptr) v += load_elem<DT>(bias_row, col);
-                    if (p.pre != nullptr) {
-                        if (p.out_f32) store_elem<SC_F32>(p.pre, m * p.ldp + col, v);
-                        else store_elem<DT>(p.pre, m * p.ldp + col, v);
+                    float add[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        v[j] += bias_late[j];
+                        add[j] = 0.f;
                     }
-                    v = activate<DT>(v, p.act);
-                    if (RESIDUAL && p.residual != nullptr) v += p.out_f32 ? load_elem<SC_F32>(p.residual, m * p.ldr + col) : load_elem<DT>(p.residual, m * p.ldr + col);
+                    if (RESIDUAL && p.residual != nullptr) {
+                        if (p.out_f32) load8<SC_F32>(p.residual, m * p.ldr + col, there, add);
+                        else load8<DT>(p.residual, m * p.ldr + col, there, add);
+                    }
+                    if (p.pre != nullptr) {
+                        if (p.out_f32) store8<SC_F32>(p.pre, m * p.ldp + col, there, v);
+                        else store8<DT>(p.pre, m * p.ldp + col, there, v);
+                    }
+                    activate8<DT>(v, p.act);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] += add[j];
                     if (p.out_f32) {
-                        store_elem<SC_F32>(p.out, m * p.ldo + col, v);
+                        store8<SC_F32>(p.out, m * p.ldo + col, there, v);
                         continue;
                     }
                 }
-                store_elem<DT>(p.out, m * p.ldo + col, v);
+                store8<DT>(p.out, m * p.ldo + col, there, v);
             }
         }
         asm volatile("" ::: "memory");

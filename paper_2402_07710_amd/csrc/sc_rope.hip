@@ -193,6 +193,7 @@ k_rope(const Rope p) {
         Pairs<DT, WHOLE> value[TOGETHER], slope[BACKWARD ? TOGETHER : 1];
 #pragma unroll
         for (int h = 0; h < TOGETHER; ++h) {
+            if (!BACKWARD && h * shares >= in.heads) break;    // no lane has one (backward: the branch costs a third of the wavefronts)
             const int head = share + h * shares;
             value[h].clear();
             if (BACKWARD) slope[BACKWARD ? h : 0].clear();
@@ -214,6 +215,7 @@ k_rope(const Rope p) {
         gains.template take<ADJACENT>(gain_a, gain_b);
 #pragma unroll
         for (int h = 0; h < TOGETHER; ++h) {
+            if (!BACKWARD && h * shares >= in.heads) break;
             const int head = share + h * shares;
             float a[8], b[8];
             value[h].template take<ADJACENT>(a, b);

@@ -222,6 +222,13 @@ constexpr int64_t weight_part(int64_t entries, int64_t c_in, int64_t c_out) {
 // Parts of groups that have several: a group of e entries has fewer than 2 e / part of them.
 constexpr int64_t weight_slots(int64_t entries, int64_t part) { return entries <= part ? 0 : 2 * entries / part + 1; }
 
+// Rows of a workgroup of the activation's gradient, by their chunks of eight channels: one turn of its 256 threads while that makes
+// fewer than 2048 workgroups, up to eight turns (3192 rows of 160 channels: 18 us in eight turns, which wait for their loads one after the other).
+constexpr int64_t act_grad_rows(int64_t rows, int64_t chunks) {
+    const int64_t one = (256 + chunks - 1) / chunks, eight = 2048 / chunks > 1 ? 2048 / chunks : 1, spread = (rows + 2047) / 2048;
+    return spread < one ? one : spread < eight ? spread : eight > one ? eight : one;
+}
+
 // ---- norm and rotation (sc_rope.hip) ----------------------------------------------------------------------
 // Workgroups of 256 threads for the queries, and as many for the keys, at most.
 constexpr int64_t ROPE_BLOCKS_MAX = 1024;
