@@ -10,7 +10,7 @@ namespace {
 template <int DT>
 __global__ void __launch_bounds__(256)
 k_act_grad(const void* __restrict__ grad, int64_t ldg, int64_t grad_rows, const int32_t* __restrict__ list, const void* __restrict__ pre,
-           int64_t ldp, int act, void* __restrict__ out, int64_t n, int N, int rows_each) {
+           int64_t ldp, int act, void* __restrict__ out, int64_t ldo, int64_t n, int N, int rows_each) {
     const int chunks = (N + 7) / 8;
     const int64_t first = (int64_t)blockIdx.x * rows_each;
     for (int t = threadIdx.x; t < rows_each * chunks; t += 256) {
@@ -26,7 +26,7 @@ k_act_grad(const void* __restrict__ grad, int64_t ldg, int64_t grad_rows, const 
         load8<DT>(pre, e * ldp + col, there, v);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = ok ? g[j] * slope<DT>(v[j], act) : 0.f;
-        store8<DT>(out, e * N + col, there, v);
+        store8<DT>(out, e * ldo + col, there, v);
     }
 }
 
@@ -160,7 +160,9 @@ int forward(const void* x, int64_t ldx, const Entries& e, const void* weight, co
     return launch(dtype_in, PRODUCT_FWD, p, s);
 }
 
-size_t grad_bytes(int64_t n, int C_out, int dtype) { return align_up((size_t)n * C_out * elem(dtype), 256); }
+// The gradient ahead of the activation: rows 64 bytes aligned, whatever their channels.
+int64_t grad_pitch(int C_out, int dtype) { return (int64_t)align_up((size_t)C_out * elem(dtype), 64) / elem(dtype); }
+size_t grad_bytes(int64_t n, int C_out, int dtype) { return align_up((size_t)n * grad_pitch(C_out, dtype) * elem(dtype), 256); }
 size_t partial_bytes(int64_t n, int C_in, int C_out) {
     return (size_t)weight_slots(n, weight_part(n, C_in, C_out)) * (C_in + 1) * C_out * sizeof(float);
 }
@@ -191,21 +193,26 @@ int backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const Ent
     if (e.n == 0 && !sums) return SC_OK;
 
     const void* grad = dy;
+    const int64_t pitch = grad_pitch(C_out, dtype);
     int64_t ldg = lddy, grad_rows = e.grad_n;
     const int32_t* grad_list = e.grad_rows;
-    if (act != SC_ACT_NONE && e.n > 0) {
+    const bool fused = act != SC_ACT_NONE && e.n > 0 && dx != nullptr && e.grad_n > 0 && act_in_product(e.n, e.groups, C_in, C_out, compute_units());
+    if (act != SC_ACT_NONE && e.n > 0 && !fused) {
         const int chunks = (C_out + 7) / 8, each = (int)act_grad_rows(e.n, chunks);
         const dim3 grid((unsigned)((e.n + each - 1) / each));
-#define SC_ACT_GRAD(DT) SC_LAUNCH(KID_ACT_GRAD, k_act_grad<DT>, grid, dim3(256), 0, s, dy, lddy, e.grad_n, e.grad_rows, pre, ldp, act, workspace, e.n, C_out, each)
+#define SC_ACT_GRAD(DT) SC_LAUNCH(KID_ACT_GRAD, k_act_grad<DT>, grid, dim3(256), 0, s, dy, lddy, e.grad_n, e.grad_rows, pre, ldp, act, workspace, pitch, e.n, C_out, each)
         if (dtype == SC_F32) SC_ACT_GRAD(SC_F32);
         else if (dtype == SC_F16) SC_ACT_GRAD(SC_F16);
         else SC_ACT_GRAD(SC_BF16);
 #undef SC_ACT_GRAD
+    }
+    auto after_activation = [&] {
         grad = workspace;
-        ldg = C_out;
+        ldg = pitch;
         grad_rows = e.n;
         grad_list = nullptr;
-    }
+    };
+    if (act != SC_ACT_NONE && !fused) after_activation();
     if (dx != nullptr && e.n > 0) {
         Product p{};
         p.a = grad;
@@ -221,8 +228,14 @@ int backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const Ent
         p.K = C_out;
         p.out = dx;
         p.ldo = lddx;
-        const int rc = launch(dtype, PRODUCT_DX, p, s);
+        p.pre = const_cast<void*>(pre);
+        p.ldp = ldp;
+        p.act = act;
+        p.kept = workspace;
+        p.ldk = pitch;
+        const int rc = launch(dtype, fused ? PRODUCT_DX_ACT : PRODUCT_DX, p, s);
         if (rc != SC_OK) return rc;
+        if (fused) after_activation();
     }
     if (sums) {
         Product p{};

@@ -3,6 +3,7 @@
 //
 //     FWD   out[p][n] = act(sum_k a[row(p)][k] w[g][k][n] + bias[g][n]) + residual[p][n]     k: C_in,  n: C_out
 //     DX    out[p][n] = sum_k a[row(p)][k] w[g][n][k]                                        k: C_out, n: C_in
+//     DX_ACT  the same with a[row(p)][k] act'(pre[p][k]) in place of a, rounded to its type, which is kept in kept[p][k]
 //     DW    out[g][m][n] = sum_p a[row(p)][m] b[row'(p)][n],  bias[g][n] = sum_p b[row'(p)][n]   p: entries of group g
 //
 // A workgroup owns a BM x BN tile of the result and walks the summed axis in steps of 128 bytes (KW times that where KW sets of
@@ -22,7 +23,7 @@
 
 namespace sc {
 
-enum ProductMode { PRODUCT_FWD, PRODUCT_DX, PRODUCT_DW };
+enum ProductMode { PRODUCT_FWD, PRODUCT_DX, PRODUCT_DX_ACT, PRODUCT_DW };
 
 struct Product {
     const void* a;                 // rows
@@ -41,11 +42,13 @@ struct Product {
     int act;
     const void* residual;
     int64_t ldr;
-    void* pre;
+    void* pre;                     // DX_ACT: read
     int64_t ldp;
     void* out;
     int64_t ldo;
     int out_f32;                   // FWD
+    void* kept;                    // DX_ACT
+    int64_t ldk;
     void* out_bias;                // DW
     float* partial;                // DW: [slot][(M + 1) N], null if no group can have two parts
     int64_t slots;                 // ... how many
@@ -139,6 +142,11 @@ __device__ inline void store8(void* base, int64_t i, int count, const float (&v)
     }
 }
 
+template <int DT>
+__device__ inline void store_row(void* base, int64_t i, const float (&v)[8], bool streamed) {
+    if (streamed) store8<DT, true>(base, i, 8, v);
+    else store8<DT>(base, i, 8, v);
+}
 // eight consecutive elements on their way
 template <int DT>
 struct Eight {
@@ -497,6 +505,101 @@ struct Loader {
     }
 };
 
+// The rows of DX_ACT: gradient and value ahead of the activation come through registers a step ahead, their product goes to LDS and, by the first of the
+// workgroups with these rows (`keep`), to memory for the weight gradient that follows.
+template <int DT, int LINES, int LINE, int NTH, int STRIDE, bool WHOLE>
+struct GradLoader {
+    static constexpr int PASSES = LINES * LINE / NTH, PER = 16 / ELEM<DT>;
+    const char* grad[PASSES];          // at the next step's chunk
+    const char* pre[PASSES];
+    char* kept[PASSES];
+    bool row_ok[PASSES], entry_ok[PASSES];
+    uint4 g[PASSES], v[PASSES];
+    int depth, act;
+    bool keep;
+
+    __device__ __forceinline__ static int line_of(int i) { return (i * NTH + (int)threadIdx.x) / LINE; }
+    __device__ __forceinline__ static int chunk_of(int i) { return (int)threadIdx.x % LINE ^ along_turn<LINE>(line_of(i)); }
+    __device__ __forceinline__ void start(const Product& p, int64_t begin, int64_t stop) {
+        depth = p.K;
+        act = p.act;
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i) {
+            const int64_t e = begin + line_of(i);
+            entry_ok[i] = e < stop;
+            const int64_t at = entry_ok[i] ? e : begin;
+            const int64_t r = p.a_list != nullptr ? p.a_list[at] : at;
+            row_ok[i] = r >= 0 && r < p.a_rows;
+            const int offset = chunk_of(i) * 16;
+            grad[i] = (const char*)p.a + (row_ok[i] ? r : 0) * (p.lda * ELEM<DT>) + offset;
+            pre[i] = (const char*)p.pre + at * (p.ldp * ELEM<DT>) + offset;
+            kept[i] = (char*)p.kept + at * (p.ldk * ELEM<DT>) + offset;
+        }
+    }
+    __device__ __forceinline__ static uint4 some(const char* p, int there) {
+        uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+            if (j < there) {
+                if constexpr (DT == SC_F32) w[j] = reinterpret_cast<const uint32_t*>(p)[j];
+                else w[j / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[j] << (16 * (j & 1));
+            }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    __device__ __forceinline__ void fetch(int s) {
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i) {
+            const int there = depth - s * STRIDE - chunk_of(i) * PER;
+            g[i] = v[i] = make_uint4(0, 0, 0, 0);
+            if (there >= PER || (WHOLE && there > 0)) {
+                if (row_ok[i]) g[i] = load_chunk(grad[i]);
+                v[i] = load_chunk(pre[i]);
+            } else if (!WHOLE && there > 0) {
+                if (row_ok[i]) g[i] = some(grad[i], there);
+                v[i] = some(pre[i], there);
+            }
+            grad[i] += STRIDE * ELEM<DT>;
+            pre[i] += STRIDE * ELEM<DT>;
+        }
+    }
+    __device__ __forceinline__ void finish(int s, uint32_t lds) {
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i) {
+            const int there = depth - s * STRIDE - chunk_of(i) * PER;
+            const uint32_t gw[4] = {g[i].x, g[i].y, g[i].z, g[i].w}, vw[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (DT == SC_F32) {
+                    w[j] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(float, gw[j]) * slope<DT>(__builtin_bit_cast(float, vw[j]), act));
+                } else {
+                    const float lo = to_float<DT>(gw[j] & 0xffffu) * slope<DT>(to_float<DT>(vw[j] & 0xffffu), act);
+                    const float hi = to_float<DT>(gw[j] >> 16) * slope<DT>(to_float<DT>(vw[j] >> 16), act);
+                    w[j] = round2<DT>(lo, hi);
+                }
+            }
+            // no row, no channel: zeros, whatever the value ahead of the activation
+            const bool some_of_it = row_ok[i] && there > 0;
+            const uint4 d = some_of_it ? make_uint4(w[0], w[1], w[2], w[3]) : make_uint4(0, 0, 0, 0);
+            *(__attribute__((address_space(3))) u32x4*)(lds + (i * NTH + threadIdx.x) * 16) = u32x4{d.x, d.y, d.z, d.w};
+            if (keep && entry_ok[i] && there > 0) {
+                if (WHOLE || there >= PER) {
+                    store_chunk(kept[i], d);
+                } else {
+                    const uint32_t dw[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+                    for (int j = 0; j < PER; ++j)
+                        if (j < there) {
+                            if constexpr (DT == SC_F32) reinterpret_cast<uint32_t*>(kept[i])[j] = dw[j];
+                            else reinterpret_cast<uint16_t*>(kept[i])[j] = (uint16_t)(dw[j / 2] >> (16 * (j & 1)));
+                        }
+                }
+            }
+            kept[i] += STRIDE * ELEM<DT>;
+        }
+    }
+};
+
 // ---- the kernel -----------------------------------------------------------------------------------------
 // WM x WN wavefronts share a tile, KW sets of them the summed axis, of which a set takes SB bytes a step.  WHOLE: the operands' lines are whole chunks
 // of 16 bytes, at any alignment of their elements (what the others need is in registers through the whole loop: weight gradients 36 us or 29).
@@ -506,7 +609,7 @@ struct ProductShape {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KW = KW_, SB = SB_;
     static constexpr int NTH = 64 * WM * WN * KW, TM = BM / 16 / WM, TN = BN / 16 / WN;
     static constexpr int STEP = SB / ELEM<DT>;                        // places on the summed axis per set and step
-    static constexpr bool A_ACROSS = MODE == PRODUCT_DW, B_ACROSS = MODE != PRODUCT_DX;
+    static constexpr bool A_ACROSS = MODE == PRODUCT_DW, B_ACROSS = MODE == PRODUCT_FWD || MODE == PRODUCT_DW;
     static constexpr int A_LINES = A_ACROSS ? STEP * KW : BM, A_LINE = A_ACROSS ? BM * ELEM<DT> / 16 : SB / 16 * KW;
     static constexpr int B_LINES = B_ACROSS ? STEP * KW : BN, B_LINE = B_ACROSS ? BN * ELEM<DT> / 16 : SB / 16 * KW;
     static constexpr int A_CHUNKS = A_LINES * A_LINE, B_CHUNKS = B_LINES * B_LINE;
@@ -563,6 +666,7 @@ k_product(const Product p) {
 
     constexpr int STRIDE = S::STEP * KW;
     Loader<DT, S::A_ACROSS, S::A_LINES, S::A_LINE, NTH, STRIDE, WHOLE> la;
+    GradLoader<DT, MODE == PRODUCT_DX_ACT ? S::A_LINES : 0, S::A_LINE, NTH, STRIDE, WHOLE> lg;
     Loader<DT, S::B_ACROSS, S::B_LINES, S::B_LINE, NTH, STRIDE, WHOLE> lb;
     la.base = (const char*)p.a;
     la.ld = (uint32_t)(p.lda * ELEM<DT>);
@@ -603,9 +707,14 @@ k_product(const Product p) {
             if (p.a_list != nullptr && e < part.last) row_of[tm] = p.a_list[e];
         }
         if (depth > 0) {
-            la.list = nullptr;
-            la.end = p.K;
-            la.start_along(p.a_list, part.first, part.last);
+            if constexpr (MODE == PRODUCT_DX_ACT) {
+                lg.keep = n_tile == 0;
+                lg.start(p, part.first, part.last);
+            } else {
+                la.list = nullptr;
+                la.end = p.K;
+                la.start_along(p.a_list, part.first, part.last);
+            }
             lb.base = (const char*)p.b + (int64_t)g * p.K * p.N * ELEM<DT>;
             lb.list = nullptr;
             lb.first = 0;
@@ -631,9 +740,17 @@ k_product(const Product p) {
     };
     auto fetch = [&](int s) __attribute__((always_inline)) {
         const uint32_t at = lds0 + (s & 1) * S::BUFFER;
-        la.fetch(s, at);
+        if constexpr (MODE != PRODUCT_DX_ACT) la.fetch(s, at);
         lb.fetch(s, at + S::A_CHUNKS * 16);
+        if constexpr (MODE == PRODUCT_DX_ACT) lg.fetch(s);
         ask_rows(s + 1);
+    };
+    // DX_ACT: what a step's registers hold goes to LDS, and the step is complete
+    auto finish = [&](int s) __attribute__((always_inline)) {
+        if constexpr (MODE == PRODUCT_DX_ACT) {
+            __builtin_amdgcn_s_waitcnt(0x0f70);
+            lg.finish(s, lds0 + (s & 1) * S::BUFFER);
+        }
     };
     typename std::conditional<S::A_ACROSS, AcrossReader<DT, S::A_LINE, TM, SB / 64>, AlongReader<DT, S::A_LINE, TM, SB / 64>>::type ra(
         lds0, wm * TM * 16, set * (S::A_ACROSS ? S::STEP : SB / 16));
@@ -657,9 +774,12 @@ k_product(const Product p) {
             lds_barrier();
         }
     }
-    if (steps > 0) fetch(0);
+    if (steps > 0) {
+        fetch(0);
+        finish(0);
+    }
     for (int s = 0; s < steps; ++s) {
-        __builtin_amdgcn_s_waitcnt(0x0f70);            // vmcnt(0): the step's chunks are in LDS
+        if constexpr (MODE != PRODUCT_DX_ACT) __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0): the step's chunks are in LDS
         lds_barrier();                                 // ... of all wavefronts, which are done with the other buffer
         if (s + 1 < steps) fetch(s + 1);
         const uint32_t buffer = (s & 1) * S::BUFFER;
@@ -681,6 +801,7 @@ k_product(const Product p) {
                 }
             }
         }
+        if (s + 1 < steps) finish(s + 1);
     }
 
     if constexpr (KW > 1) {                            // the sets' sums, in the order of the sets
@@ -721,7 +842,10 @@ k_product(const Product p) {
     const bool to_partial = MODE == PRODUCT_DW && part.parts > 1;
     const void* const bias_row = MODE == PRODUCT_FWD && p.bias != nullptr ? (const char*)p.bias + (int64_t)g * p.N * ELEM<DT> : nullptr;
     // Rows of results are streamed: their lines, written in two halves, otherwise leave the L2 in halves too, a third more of them than there are (10^6 rows 128 -> 128
-    // 129 us and 95, which is the rate of a copy; 110545 x 256 -> 256 39.8 and 35.5).  Partial sums are not, they are read back at once.
+    // 129 us and 95, which is the rate of a copy; 110545 x 256 -> 256 39.8 and 35.5).  Not where rows start inside a 64-byte half.  Partial sums are not,
+    // they are read back at once.
+    const int out_size = MODE == PRODUCT_FWD && p.out_f32 ? 4 : ELEM<DT>;
+    const bool stream_out = (((uintptr_t)p.out | (uintptr_t)(p.ldo * out_size)) & 63) == 0, stream_pre = (((uintptr_t)p.pre | (uintptr_t)(p.ldp * out_size)) & 63) == 0;
     // Whatever is loaded is asked for ahead of the stores of the columns before: loads and stores are waited for in one order.
     constexpr int PAIRS = TN / 2;
     const int left = (p.N - col_wave) / 32, pairs = left < PAIRS ? (left > 0 ? left : 0) : PAIRS;
@@ -776,8 +900,8 @@ k_product(const Product p) {
                 if constexpr (MODE == PRODUCT_FWD) {
                     if (bias_row != nullptr) bias[u].add_to(v);
                     if (p.pre != nullptr) {
-                        if (p.out_f32) store8<SC_F32, true>(p.pre, m * p.ldp + col, 8, v);
-                        else store8<DT, true>(p.pre, m * p.ldp + col, 8, v);
+                        if (p.out_f32) store_row<SC_F32>(p.pre, m * p.ldp + col, v, stream_pre);
+                        else store_row<DT>(p.pre, m * p.ldp + col, v, stream_pre);
                     }
                     activate8<DT>(v, p.act);
                     if constexpr (RESIDUAL) {
@@ -790,11 +914,11 @@ k_product(const Product p) {
                         }
                     }
                     if (p.out_f32) {
-                        store8<SC_F32, true>(p.out, m * p.ldo + col, 8, v);
+                        store_row<SC_F32>(p.out, m * p.ldo + col, v, stream_out);
                         continue;
                     }
                 }
-                store8<DT, true>(p.out, m * p.ldo + col, 8, v);
+                store_row<DT>(p.out, m * p.ldo + col, v, stream_out);
             }
         }
     }
@@ -911,7 +1035,7 @@ template <int DT, int MODE, int BM, int BN, int WM, int WN, int KW, int SB, bool
 int start_product(const Product& p, hipStream_t s) {
     constexpr int PER = 16 / ELEM<DT>;
     const bool whole = p.N % PER == 0 && (MODE == PRODUCT_DW ? p.M : p.K) % PER == 0;      // DX: its weights' lines are K long
-    const bool along = MODE == PRODUCT_DX && p.K % PER == 0;
+    const bool along = (MODE == PRODUCT_DX || MODE == PRODUCT_DX_ACT) && p.K % PER == 0;
     return whole || along ? start_product<DT, MODE, BM, BN, WM, WN, KW, SB, true, RESIDUAL>(p, s)
                           : start_product<DT, MODE, BM, BN, WM, WN, KW, SB, false, RESIDUAL>(p, s);
 }
@@ -932,6 +1056,13 @@ int choose_product(const Product& p, int cus, hipStream_t s) {
             case WEIGHTS_64_128: return run_product<DT, MODE, 64, 128, 2, 2, 1>(p, s);
             case WEIGHTS_128_64: return run_product<DT, MODE, 128, 64, 2, 2, 1>(p, s);
             default: return run_product<DT, MODE, 128, 128, 2, 2, 1>(p, s);
+        }
+    } else if constexpr (MODE == PRODUCT_DX_ACT) {     // the tiles that act_in_product leaves
+        switch (row_tile(p.n, p.starts == nullptr ? 0 : p.groups, p.N, p.K, false, false, cus)) {
+            case TILE_16_32: return run_product<DT, MODE, 16, 32, 1, 1, 4>(p, s);
+            case TILE_16_32_DEEP: return run_product<DT, MODE, 16, 32, 1, 1, 8>(p, s);
+            case TILE_32_64: return run_product<DT, MODE, 32, 64, 2, 2, 2>(p, s);
+            default: return run_product<DT, MODE, 128, 32, 4, 1, 1>(p, s);
         }
     } else {
         constexpr bool FWD = MODE == PRODUCT_FWD, WIDE = DT != SC_F32;
@@ -960,6 +1091,7 @@ template <int DT>
 int launch_product(int mode, const Product& p, int cus, hipStream_t s) {
     if (mode == PRODUCT_FWD) return choose_product<DT, PRODUCT_FWD>(p, cus, s);
     if (mode == PRODUCT_DX) return choose_product<DT, PRODUCT_DX>(p, cus, s);
+    if (mode == PRODUCT_DX_ACT) return choose_product<DT, PRODUCT_DX_ACT>(p, cus, s);
     return choose_product<DT, PRODUCT_DW>(p, cus, s);
 }
 

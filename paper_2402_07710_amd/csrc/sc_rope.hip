@@ -78,9 +78,7 @@ __device__ inline void turn_of(const PairTurn& t, float at, float& c, float& s) 
 
 // A lane's eight pairs of one head: a[i], b[i].  It takes chunk c (of eight channels) of the lower half of the head's lanes' and the one as many further on as
 // the head has lanes, or (halves) pairs 8 c .. 8 c + 7 with their partners, so that the lanes of a head read consecutive chunks.
-template <bool ADJACENT>
-__device__ inline int pair_of(int c, int lanes, int i) { return ADJACENT ? 4 * (i < 4 ? c : c + lanes) + (i & 3) : 8 * c + i; }
-// Its channels on their way: two chunks.  WHOLE: heads are whole chunks (halves: both sides).
+// Its channels on their way: two chunks.  WHOLE: they are whole.
 template <int DT, bool WHOLE>
 struct Pairs {
     Eight<DT> raw[WHOLE ? 2 : 1];
@@ -154,7 +152,10 @@ __device__ inline float sum_of_lanes(float v, int log2) {
     return v;
 }
 
-template <int DT, bool ADJACENT, bool BACKWARD, int TOGETHER, bool WHOLE>
+// How heads divide into chunks: evenly; with a last chunk that reaches back over the one before it (both lanes come to the same values and store them, one
+// of them counts them in the sums); or there is not one whole chunk.
+enum HeadShape { HEAD_EVEN, HEAD_OVERLAP, HEAD_SMALL };
+template <int DT, bool ADJACENT, bool BACKWARD, int TOGETHER, int SHAPE>
 __global__ void __launch_bounds__(ROPE_THREADS)
 k_rope(const Rope p) {
     const int which = blockIdx.x < (unsigned)p.blocks[0] ? 0 : 1;
@@ -164,17 +165,31 @@ k_rope(const Rope p) {
     const int half = p.D / 2, lanes = 1 << p.lanes_log2;
     const int c0 = (int)threadIdx.x & (lanes - 1);
     // the lane's two chunks, and how much of them there is; heads whose lanes are not a power of two leave some idle
-    const int at = 8 * c0, at2 = ADJACENT ? 8 * (c0 + lanes) : half + 8 * c0;
-    const int count = (ADJACENT ? p.D : half) - at, count2 = p.D - at2;
+    constexpr bool WHOLE = SHAPE != HEAD_SMALL;
+    const int side = ADJACENT ? p.D : half;             // channels that chunks of one kind cover
+    int at = 8 * c0, at2 = ADJACENT ? 8 * (c0 + lanes) : half + 8 * c0;
+    const int count = side - at, count2 = p.D - at2;
     const bool on = count > 0;
+    int twice = 0, twice2 = 0;                          // channels of the chunks that the lane before has too
+    if constexpr (SHAPE == HEAD_OVERLAP) {
+        if (on && count < 8) twice = 8 - count;
+        if (on && count2 > 0 && count2 < 8) twice2 = 8 - count2;
+        at -= twice;
+        at2 -= twice2;
+    }
+    // pair i of the lane, of a and b; whether it counts
+    auto pair_at = [&](int i) __attribute__((always_inline)) { return ADJACENT ? (i < 4 ? at : at2) / 2 + (i & 3) : at + i; };
+    auto counts = [&](int i) __attribute__((always_inline)) {
+        return SHAPE != HEAD_OVERLAP || (ADJACENT ? 2 * (i & 3) >= (i < 4 ? twice : twice2) : i >= twice);
+    };
     const float per_channel = 1.f / (float)p.D;
     PairTurn turn[8];
     Pairs<DT, WHOLE> gains;
     float sum_a[BACKWARD ? 8 : 1], sum_b[BACKWARD ? 8 : 1];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int pair = pair_of<ADJACENT>(c0, lanes, i);
-        turn[i] = pair < half ? p.table[pair] : PairTurn{0.f, 0.f, 0, 0};
+        const int pair = pair_at(i);
+        turn[i] = on && pair < half ? p.table[pair] : PairTurn{0.f, 0.f, 0, 0};
         if (BACKWARD) sum_a[BACKWARD ? i : 0] = sum_b[BACKWARD ? i : 0] = 0.f;
     }
     gains.clear();
@@ -223,7 +238,7 @@ k_rope(const Rope p) {
             if (gain != nullptr) {
                 float squares = 0.f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) squares = fmaf(a[i], a[i], fmaf(b[i], b[i], squares));
+                for (int i = 0; i < 8; ++i) squares = counts(i) ? fmaf(a[i], a[i], fmaf(b[i], b[i], squares)) : squares;
                 scale = rsqrtf(fmaf(sum_of_lanes(squares, p.lanes_log2), per_channel, p.eps));
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -255,7 +270,7 @@ k_rope(const Rope p) {
                         sum_b[i] = fmaf(y[i], b[i], sum_b[i]);
                         x[i] *= gain_a[i];
                         y[i] *= gain_b[i];
-                        along = fmaf(x[i], a[i], fmaf(y[i], b[i], along));
+                        along = counts(i) ? fmaf(x[i], a[i], fmaf(y[i], b[i], along)) : along;
                     }
                     along = sum_of_lanes(along, p.lanes_log2) * per_channel;
 #pragma unroll
@@ -275,9 +290,11 @@ k_rope(const Rope p) {
         float* mine = sums + (threadIdx.x >> p.lanes_log2) * width;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int pair = pair_of<ADJACENT>(c0, lanes, i);          // below 8 lanes
-            mine[pair] = sum_a[i];
-            mine[width / 2 + pair] = sum_b[i];
+            const int pair = pair_at(i);                // below 8 lanes
+            if (on && pair < half && counts(i)) {
+                mine[pair] = sum_a[i];
+                mine[width / 2 + pair] = sum_b[i];
+            }
         }
         __syncthreads();
         for (int j = threadIdx.x; j < p.D; j += ROPE_THREADS) {
@@ -358,17 +375,21 @@ int launch_rope(const Rope& p, int pairing, int dtype, hipStream_t s) {
     constexpr int TOGETHER = BACKWARD ? BACKWARD_TOGETHER : FORWARD_TOGETHER;
     const dim3 grid((unsigned)(p.blocks[0] + p.blocks[1]));
     const int kid = BACKWARD ? KID_ROPE_GRAD : KID_ROPE;
-    const bool whole = (pairing == SC_PAIRS_ADJACENT ? p.D : p.D / 2) % 8 == 0;
-#define SC_ROPE(DT)                                                                                                                              \
-    do {                                                                                                                                         \
-        const auto kernel = pairing == SC_PAIRS_ADJACENT ? (whole ? k_rope<DT, true, BACKWARD, TOGETHER, true> : k_rope<DT, true, BACKWARD, TOGETHER, false>)  \
-                                                         : (whole ? k_rope<DT, false, BACKWARD, TOGETHER, true> : k_rope<DT, false, BACKWARD, TOGETHER, false>); \
-        SC_LAUNCH(kid, kernel, grid, dim3(ROPE_THREADS), 0, s, p);                                                                               \
+    const int side = pairing == SC_PAIRS_ADJACENT ? p.D : p.D / 2;
+    const int shape = side % 8 == 0 ? HEAD_EVEN : side > 8 ? HEAD_OVERLAP : HEAD_SMALL;
+#define SC_ROPE_SHAPE(DT, ADJACENT)                                                                                                     \
+    (shape == HEAD_EVEN ? k_rope<DT, ADJACENT, BACKWARD, TOGETHER, HEAD_EVEN>                                                            \
+                        : shape == HEAD_OVERLAP ? k_rope<DT, ADJACENT, BACKWARD, TOGETHER, HEAD_OVERLAP> : k_rope<DT, ADJACENT, BACKWARD, TOGETHER, HEAD_SMALL>)
+#define SC_ROPE(DT)                                                                                                                     \
+    do {                                                                                                                                \
+        const auto kernel = pairing == SC_PAIRS_ADJACENT ? SC_ROPE_SHAPE(DT, true) : SC_ROPE_SHAPE(DT, false);                          \
+        SC_LAUNCH(kid, kernel, grid, dim3(ROPE_THREADS), 0, s, p);                                                                      \
     } while (0)
     if (dtype == SC_F32) SC_ROPE(SC_F32);
     else if (dtype == SC_F16) SC_ROPE(SC_F16);
     else SC_ROPE(SC_BF16);
 #undef SC_ROPE
+#undef SC_ROPE_SHAPE
     return SC_OK;
 }
 

@@ -229,6 +229,16 @@ constexpr int64_t act_grad_rows(int64_t rows, int64_t chunks) {
     return spread < one ? one : spread < eight ? spread : eight > one ? eight : one;
 }
 
+// The activation's gradient inside the product with the weights, or a pass of its own ahead of it.  Inside, one tile of columns or few rows: what is read is read
+// once and a launch is spared; otherwise the slopes keep the matrix cores waiting, which a pass over memory hides (us of the whole backward pass, bf16 GELU, apart / inside:
+// 300 k x 32 -> 128 95 / 82, 53 k x 64 -> 256 45.5 / 47.7, 110 k x 128 -> 512 140 / 157, 8 k x 128 -> 128 SiLU 18.8 / 16.8, 1 k x 64 -> 256 14.9 / 14.1, 64 x 512 -> 512 12.1 / 13.8).
+// Few rows with many channels have too long a way through the registers (66 x 96 -> 3456 28 us, apart 14).
+constexpr bool act_in_product(int64_t entries, int64_t groups, int64_t c_in, int64_t c_out, int64_t cus) {
+    const int64_t parts = groups < entries ? groups : entries;
+    const int64_t tiles = (entries + 15 * parts) / 16 * ((c_in + 31) / 32);
+    return (c_in <= 32 && tiles > 8 * cus) || (c_in <= 128 && c_out <= 512 && tiles <= 8 * cus);
+}
+
 // ---- norm and rotation (sc_rope.hip) ----------------------------------------------------------------------
 // Workgroups of 256 threads for the queries, and as many for the keys, at most.
 constexpr int64_t ROPE_BLOCKS_MAX = 1024;

@@ -202,7 +202,7 @@ def test_activations_at_their_ends(dtype):
         want = act64(finite, act)
         close(out[1:-1, 0], want, forward_bound(want, finite, finite.abs(), 1, act, dt), act)
         assert float(out[0]) == 0.0 and float(out[-1]) == math.inf
-        ws = torch.empty(1024, dtype=torch.uint8, device=DEV)
+        ws = torch.empty(sc.sc_linear_workspace_bytes(len(v), 1, 1, dt), dtype=torch.uint8, device=DEV)
         sc.sc_linear_bwd(torch.ones(len(v), 1, dtype=dt, device=DEV), v[:, None].to(DEV), one, grad_x=gx, pre=v[:, None].to(DEV), act=act, workspace=ws)
         want = slope64(finite, act)
         close(gx[1:-1, 0], want, 2 * ACT_ERROR * (1 + finite.abs()).clamp(max=30.0) + 2 * UNIT[dt] * (want.abs() + 1e-5) + TINY[dt], act + " slope")
@@ -355,6 +355,7 @@ def rope_bound(want, D, dt, terms=1.0):
 ROPE = [  # D, pairs, q heads, k heads, rows
     (2, (1,), 1, 1, 1), (6, (1, 1, 1), 2, 1, 5), (16, (3, 3, 2), 4, 4, 33), (32, (6, 5, 5), 8, 2, 257), (44, (8, 7, 7), 3, 1, 65), (64, (10, 11, 11), 5, 0, 130),
     (64, (32,), 8, 8, 70), (96, (16, 16, 16), 7, 3, 40), (128, (20, 22, 22), 16, 4, 1), (130, (20, 22, 20), 2, 2, 9), (256, (42, 43), 4, 1, 19),
+    (10, (2, 2, 1), 3, 2, 11), (18, (3, 3, 3), 5, 1, 21), (36, (18,), 8, 4, 50), (50, (9, 8, 8), 4, 2, 30),
     (1024, (128, 128, 128, 128), 1, 2, 7), (64, (10, 10, 11), 8, 2, 3000),
 ]
 
