@@ -144,8 +144,13 @@ __device__ inline void store8(void* base, int64_t i, int count, const float (&v)
 
 template <int DT>
 __device__ inline void store_row(void* base, int64_t i, const float (&v)[8], bool streamed) {
-    if (streamed) store8<DT, true>(base, i, 8, v);
-    else store8<DT>(base, i, 8, v);
+    if (streamed) {
+        asm volatile("; streamed");                    // or the compiler takes the two stores for one
+        store8<DT, true>(base, i, 8, v);
+        asm volatile("; streamed");
+    } else {
+        store8<DT>(base, i, 8, v);
+    }
 }
 // eight consecutive elements on their way
 template <int DT>
@@ -1049,10 +1054,8 @@ int run_product(const Product& p, hipStream_t s) {
 template <int DT, int MODE>
 int choose_product(const Product& p, int cus, hipStream_t s) {
     if constexpr (MODE == PRODUCT_DW) {
-        switch (weight_tile(p.n, p.M, p.N)) {
+        switch (weight_tile(p.M, p.N)) {
             case WEIGHTS_64_64: return run_product<DT, MODE, 64, 64, 2, 2, 1>(p, s);
-            case WEIGHTS_32_128: return run_product<DT, MODE, 32, 128, 1, 4, 1>(p, s);
-            case WEIGHTS_128_32: return run_product<DT, MODE, 128, 32, 4, 1, 1>(p, s);
             case WEIGHTS_64_128: return run_product<DT, MODE, 64, 128, 2, 2, 1>(p, s);
             case WEIGHTS_128_64: return run_product<DT, MODE, 128, 64, 2, 2, 1>(p, s);
             default: return run_product<DT, MODE, 128, 128, 2, 2, 1>(p, s);
@@ -1073,11 +1076,10 @@ int choose_product(const Product& p, int cus, hipStream_t s) {
             case TILE_64_64: return run_product<DT, MODE, 64, 64, 2, 2, 1>(p, s);
             case TILE_64_64_DEEP: return run_product<DT, MODE, 64, 64, 2, 2, 2>(p, s);
             case TILE_128_32: return run_product<DT, MODE, 128, 32, 4, 1, 1>(p, s);
-            case TILE_128_64: return run_product<DT, MODE, 128, 64, 4, 1, 1>(p, s);
-            case TILE_64_128:
-                if constexpr (FWD) return run_product<DT, MODE, 64, 128, 2, 2, 1, 64, true>(p, s);
+            case TILE_128_64: return run_product<DT, MODE, 128, 64, 4, 1, 1, 128, true>(p, s);
+            case TILE_128_128_SHORT:
+                if constexpr (FWD) return run_product<DT, MODE, 128, 128, 2, 2, 1, 64, true>(p, s);
                 break;
-            case TILE_128_128_SHORT: return run_product<DT, MODE, 128, 128, 2, 2, 1, 64, true>(p, s);
             case TILE_LARGE:
                 if constexpr (WIDE && FWD) return run_product<DT, MODE, 128, 256, 2, 2, 1, 64, true>(p, s);
                 else if constexpr (WIDE) return run_product<DT, MODE, 256, 256, 2, 4, 1, 128, true>(p, s);

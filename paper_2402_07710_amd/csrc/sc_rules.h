@@ -177,46 +177,62 @@ constexpr int64_t grid_columns(int64_t groups) { return groups < GRID_COLUMNS ? 
 constexpr int64_t grid_rows(int64_t groups) { return (groups + GRID_COLUMNS - 1) / GRID_COLUMNS; }
 
 // ---- products of rows and weights (sc_product.h) --------------------------------------------------------
-// Tile of the result that a workgroup owns, by the rows and columns there are.  Few rows a group: 16 rows, four wavefronts share the summed axis.
-enum RowTile { TILE_16_32, TILE_16_32_DEEP, TILE_32_64, TILE_64_64, TILE_64_64_DEEP, TILE_128_32, TILE_128_64, TILE_64_128, TILE_128_128, TILE_128_128_SHORT, TILE_LARGE };
-// `groups` 0: a linear layer.
+// Tile of the result that a workgroup owns, rows by columns; DEEP and the two smallest: two, four or eight sets of wavefronts share the summed axis, SHORT: steps
+// of 64 bytes and not 128, four workgroups on a CU.  LARGE: 128 x 256 forward, 256 x 256 for the input's gradient.
+enum RowTile { TILE_16_32, TILE_16_32_DEEP, TILE_32_64, TILE_64_64, TILE_64_64_DEEP, TILE_128_32, TILE_128_64, TILE_128_128, TILE_128_128_SHORT, TILE_LARGE };
+// By the 16 x 32 tiles that there would be: few of them, and small tiles with short ways through the summed axis fill the chip; many, and what counts is how often the
+// operands are read.  `groups` 0: a linear layer.  us of the call, bf16, no epilogue, rows x summed x columns, 256 CUs, on either side of each line:
+//   16 x 32, eight sets / four     1 x 1024 x 4096 4.2 / 4.4, 1 x 4096 x 256 7.0 / 8.1, 64 x 2048 x 2048 (256 tiles) 6.9 / 7.1, 128 x 2048 x 2048 12.7 / 8.7, 1024 x 256 x 256 4.4 / 4.0
+//   16 x 32 / 32 x 64              256 x 1024 x 1024 (512) 5.6 / 6.2, 1024 x 256 x 256 4.0 / 4.1, 512 x 1024 x 1024 (1024) 9.7 / 6.6, 2048 x 256 x 256 4.6 / 4.2
+//   32 x 64 / 64 x 64, two sets    512 x 512 x 2048 (2048) 6.0 / 5.7, 1024 x 1024 x 1024 8.2 / 8.6, 2048 x 1024 x 1024 (4096) 13.9 / 10.0; one set 2048 x 256 x 1024 6.9 / 5.3
+//   64 x 64, two sets / one        2048 x 1024 x 1024 10.0 / 11.1, 512 x 512 x 2048 5.7 / 6.2, 2048 x 256 x 1024 5.6 / 5.3
+//   64 x 64 / 128 x 64             2048 x 1024 x 1024 11.1 / 13.1, 2048 x 2048 x 2048 (8192) 28.7 / 24.7, 8192 x 128 x 512 5.8 / 6.2, 4096 x 256 x 1024 7.0 / 7.4, 20 k x 128 x 128 5.1 / 6.0
+//   128 x 64 / 128 x 128           4096 x 256 x 1024 7.4 / 8.9, 8192 x 128 x 512 6.2 / 7.2, 8192 x 1024 x 1024 (16384) 29.3 / 25.3, 261 k x 64 x 64 12.8 / 15.3; short steps 53 k x 64 x 256 GELU 16.5 / 19.3
+//   128 x 32 / 128 x 64            200 k x 128 x 32 14.4 / 16.3
+//   128 x 128, short / long steps  53 k x 128 x 512 19.9 / 26.8, 110 k x 256 x 256 32.3 / 34.6, 10^6 x 128 x 128 87.7 / 105, 110 k x 512 x 128 37.5 / 35.6, 16384 x 512 x 512 15.7 / 14.4
+//   128 x 128 / large              156 k x 336 x 448 81.6 / 82.4, 53 k x 256 x 1024 46.0 / 53.2, 32768 x 512 x 512 27.5 / 22.5, 32768 x 2048 x 2048 298 / 261, 8192 x 1024 x 1024 25.3 / 28.6;
+//                                  input's gradient 32768 x 2048 x 2048 284 / 253, 110 k x 1024 x 256 92 / 80, 16384 x 2048 x 512 43.1 / 57.9 (256 tiles of 128 x 256)
+//   groups, 128 x 128 short / long / large   53 k in 8, 128 -> 512 SiLU 26.4 / 34.3 / 31.4, 16384 in 16, 2048 -> 512 52.2 / 63.1 / 53.1; input's gradient 53 k in 8, 512 -> 128
+//                                  16.5 / 14.5 / 21.6, 1024 -> 256 56.1 / 48.8 / 37.2, 16384 in 16, 2048 -> 512 68.6 / 71.1 / 58.9
 constexpr RowTile row_tile(int64_t entries, int64_t groups, int64_t columns, int64_t depth, bool forward, bool half, int64_t cus) {
     const int64_t parts = groups == 0 ? 1 : groups < entries ? groups : entries, each = entries / parts;
-    const int64_t tiles = (entries + 15 * parts) / 16 * ((columns + 31) / 32);       // of 16 x 32
+    const int64_t tiles = (entries + 15 * parts) / 16 * ((columns + 31) / 32);
     if (tiles <= 2 * cus) return depth >= 1024 && tiles <= cus ? TILE_16_32_DEEP : TILE_16_32;
-    if (tiles <= 8 * cus || each <= 32) return TILE_32_64;
+    if (tiles <= 8 * cus) return TILE_32_64;
     if (columns <= 32) return TILE_128_32;
-    if (tiles <= 16 * cus || each <= 64) return depth >= 512 ? TILE_64_64_DEEP : TILE_64_64;
-    if (tiles <= 32 * cus || columns <= 64) return TILE_128_64;
-    if (groups == 0 && half && depth >= 256 && columns >= 256 && (entries / 128) * (columns / 256) >= 2 * cus) return TILE_LARGE;
-    if (!forward) return groups > 0 && depth >= 1024 ? TILE_128_128_SHORT : TILE_128_128;
-    if (groups > 0) return TILE_128_128_SHORT;
-    return depth <= 256 ? TILE_64_128 : TILE_128_128;
+    if (tiles <= (depth <= 256 ? 32 : 16) * cus || each <= 64) return depth >= 512 ? TILE_64_64_DEEP : TILE_64_64;
+    if (tiles <= 32 * cus || columns <= 64 || depth <= 64) return TILE_128_64;
+    const bool large = half && depth >= 512 && columns >= 256;
+    if (large && (groups == 0 ? (entries / 128) * (columns / 256) >= 2 * cus : !forward && each >= 512)) return TILE_LARGE;
+    return forward && (groups > 0 || depth < 512) ? TILE_128_128_SHORT : TILE_128_128;
 }
-// Consecutive tiles that one XCD takes: those of the same rows, which its L2 then holds, as long as every XCD has eight runs.
+// Consecutive tiles that one XCD takes: those of the same rows, which its L2 then holds, as long as every XCD has eight runs
+// (us with one tile / all of the rows / this, bf16: 53 k x 256 x 1024 56.8 / 48.1 / 48.4, 8192 x 1024 x 1024 25.7 / 23.0 / 22.9, 64 x 2048 x 2048 7.4 / 16.9 / 7.2).
 constexpr int64_t product_run(int64_t units, int64_t tiles_each) {
     const int64_t run = units * tiles_each / 64;
     return run < 1 ? 1 : run < tiles_each ? run : tiles_each;
 }
-// Tile of a weight gradient, rows by columns of the matrix.
-enum WeightTile { WEIGHTS_64_64, WEIGHTS_32_128, WEIGHTS_128_32, WEIGHTS_64_128, WEIGHTS_128_64, WEIGHTS_128_128 };
-constexpr WeightTile weight_tile(int64_t entries, int64_t c_in, int64_t c_out) {
-    (void)entries;
-    if (c_in <= 64 && c_out <= 64) return WEIGHTS_64_64;
-    if (c_in <= 32) return WEIGHTS_32_128;
-    if (c_out <= 32) return WEIGHTS_128_32;
+// Tile of a weight gradient, rows by columns of the matrix: as wide as the matrix, up to 128, as the tiles along one axis read the other axis' operand once each
+// (us, bf16, 64 x 64 / 64 x 128 or 128 x 64 / 128 x 128: 53 k x 256 x 1024 77.8 / 71.3 / 50.8, 110 k x 64 x 256 24.8 / 23.4 / 23.6, 261 k x 64 x 64 21.4 / 21.6 / 22.5).
+// Narrower than 64 gains nothing (261 k x 128 x 32 in 128 x 32 28.1, in 64 x 64 27.4; 53 k x 32 x 64 in 32 x 128 10.6, in 64 x 64 10.5).
+enum WeightTile { WEIGHTS_64_64, WEIGHTS_64_128, WEIGHTS_128_64, WEIGHTS_128_128 };
+constexpr WeightTile weight_tile(int64_t c_in, int64_t c_out) {
+    if (c_in <= 32 || c_out <= 32 || (c_in <= 64 && c_out <= 64)) return WEIGHTS_64_64;
     return c_in <= 64 ? WEIGHTS_64_128 : c_out <= 64 ? WEIGHTS_128_64 : WEIGHTS_128_128;
 }
-constexpr int64_t weight_tiles(int64_t entries, int64_t c_in, int64_t c_out) {
-    const WeightTile t = weight_tile(entries, c_in, c_out);
-    const int64_t m = t == WEIGHTS_32_128 ? 32 : t == WEIGHTS_64_64 || t == WEIGHTS_64_128 ? 64 : 128;
-    const int64_t n = t == WEIGHTS_128_32 ? 32 : t == WEIGHTS_64_64 || t == WEIGHTS_128_64 ? 64 : 128;
+constexpr int64_t weight_tiles(int64_t c_in, int64_t c_out) {
+    const WeightTile t = weight_tile(c_in, c_out);
+    const int64_t m = t == WEIGHTS_64_64 || t == WEIGHTS_64_128 ? 64 : 128, n = t == WEIGHTS_64_64 || t == WEIGHTS_128_64 ? 64 : 128;
     return (c_in > m ? (c_in + m - 1) / m : 1) * ((c_out + n - 1) / n);
 }
 // Entries that one workgroup sums of a group for a tile of its weight gradient: the groups are cut into parts so that there are about two
-// workgroups for each of 256 compute units, but parts of 128 entries at least, whose sums are written once and read once.
+// workgroups for each of 256 compute units, or one where one large tile holds the whole matrix, as each part's sums are written and read again.
+// Us of the gradient, bf16, 256 / 512 / 1024 workgroups: 16384 x 512 x 2048 78.9 / 65.9 / 71.9, 110 k x 256 x 256 40.7 / 38.6 / -, 261 k x 64 x 64 22.7 / 22.5 / -, rulebook of 360 k pairs
+// 64 x 64 29.8 / 25.4 / 29.6; one tile 261 k x 64 x 128 26.8 / 31.4 / 37.8, 53 k x 128 x 128 16.4 / 19.8 / -, 360 k pairs 128 x 128 58.1 / 68.1 / -.
+// Parts of 128 entries at least (4000 x 256 x 256, at least 64 / 128 / 256: 16.5 / 13.4 / 12.9, 1000 x 64 x 256 8.5 / 8.4 / 9.7).
 constexpr int64_t weight_part(int64_t entries, int64_t c_in, int64_t c_out) {
-    const int64_t want = (entries * weight_tiles(entries, c_in, c_out) + 511) / 512;
+    const int64_t tiles = weight_tiles(c_in, c_out), workgroups = tiles == 1 && weight_tile(c_in, c_out) != WEIGHTS_64_64 ? 256 : 512;
+    const int64_t want = (entries * tiles + workgroups - 1) / workgroups;
     return ((want > 128 ? want : 128) + 63) / 64 * 64;
 }
 // Parts of groups that have several: a group of e entries has fewer than 2 e / part of them.
