@@ -1,5 +1,5 @@
 // Products of feature rows with weights, and of feature rows with gradient rows: one tile kernel for linear layers and for
-// layers whose weights differ by group of rows (sc_linear.hip, sc_grouped.hip).
+// layers whose weights differ by group of rows (sc_layers.hip).
 //
 //     FWD   out[p][n] = act(sum_k a[row(p)][k] w[g][k][n] + bias[g][n]) + residual[p][n]     k: C_in,  n: C_out
 //     DX    out[p][n] = sum_k a[row(p)][k] w[g][n][k]                                        k: C_out, n: C_in
@@ -13,8 +13,18 @@
 // read turns into operand order on the way to the registers, so nothing is ever re-laid out in memory.  Chunks of 16 bytes are permuted inside a
 // line by the line's number so that the lanes of one LDS access meet different banks; the permutation is in the address that a lane
 // loads from, because a load into LDS fills it in the order of the lanes.
-// The weights' side is the matrix instruction's first operand, so that a lane ends up with four consecutive columns of one row, which
-// pass through LDS once more on their way out.
+// The weights' side is the matrix instruction's first operand, so that a lane ends up with four consecutive columns of one row; one exchange between
+// lanes makes them eight, which go out with bias, activation and residual in the registers they were summed in.
+//
+// What bounds it: memory up to some hundred channels, the matrix cores from about 1000 x 1000 on, a way through LDS in between (an operand's byte is read BM or BN
+// over 16 times from there), and the launch with one trip to memory for few rows.  bf16, us, a copy on this card 5.1 TB/s, the library's largest product 1135 TFLOP/s:
+//     one row 1024 -> 4096                  5.1     8.4 MB of weights, launch and latency; 4.2 in a row of calls (2.0 TB/s)
+//     53 k x 64 -> 256, f16, both outputs  17.4     61.5 MB, 3.5 TB/s: one step of the axis, then GELU and the stores; nothing to hide them behind but other workgroups
+//     10^6 x 128 -> 128                    87.7     512 MB, 5.8 TB/s
+//     32768 x 2048 -> 2048                  261     1054 TFLOP/s (with residual and cold 290)
+//     16384 rows in 16 groups, 512 -> 2048 SiLU 61.2   562 TFLOP/s
+//     the gradients: 16384 in 16 groups 2048 -> 512  58.9   583 TFLOP/s; weights 16384 x 512 x 2048 65.4   525 TFLOP/s; 10^6 x 128 -> 128 107   4.8 TB/s
+// Steps of 128 bytes two deep leave room for two to four workgroups on a CU, which hide each other's barriers: three steps deep was slower everywhere (fewer of them).
 #pragma once
 
 #include <type_traits>

@@ -9,6 +9,9 @@
 // LDS.  A group of lanes takes several heads of one row at a time: their loads are in flight together and the row's angles are
 // made once for them.  Angles are counted in turns: a coordinate times a frequency of 48 bits, of which the whole turns are
 // dropped before the sine, so a coordinate of 65534 is as exact as one of 1.
+// 261574 rows of 8 + 8 heads of 32, bf16: 540 MB in 108 to 116 us, 4.7 to 5.0 TB/s, the rate of a copy (heads at a time 4 / 2 / 1: 108 / 109 / 130); backward 110545
+// rows of 8 + 2 heads of 64, f16: 425 MB in 94 us, 4.5 TB/s (2 / 1 at a time 97 / 116; four hold too many registers), and 5 us for the gains.
+// Stores past the caches were slower (119 and 166).
 #include "sc_product.h"
 
 namespace sc {

@@ -256,7 +256,8 @@ constexpr bool act_in_product(int64_t entries, int64_t groups, int64_t c_in, int
 }
 
 // ---- norm and rotation (sc_rope.hip) ----------------------------------------------------------------------
-// Workgroups of 256 threads for the queries, and as many for the keys, at most.
+// Workgroups of 256 threads for the queries, and as many for the keys, at most: each writes a share of the gain's gradient (backward, 110545 rows of 8 + 2 heads of 64, f16,
+// 1024 / 2048 / 4096: 94.8 / 97.2 / 104.8 us; forward the same to the per cent).
 constexpr int64_t ROPE_BLOCKS_MAX = 1024;
 
 }  // namespace sc

@@ -1,6 +1,5 @@
 """CPU tests of what the row layers refuse, at the C boundary and in the marshalling of tensors, before anything is launched."""
 import ctypes
-import random
 
 import pytest
 import torch
@@ -68,25 +67,6 @@ def test_grouped_refuses(lib):
     for bad in (dict(starts=None), dict(grad_rows=18), dict(rows=18), dict(groups=0), dict(n=-1), dict(dy_rows=-1), dict(dy_rows=sc.SC_N_MAX + 1), dict(dx=None), dict(w=None)):
         assert grouped_bwd(lib, **bad) == EINVAL, bad
     assert lib.sc_grouped_workspace_bytes(10, 0, 32, 64, F16) == 0 and lib.sc_grouped_workspace_bytes(1 << 31, 2, 32, 64, F16) == 0
-
-
-def test_workspace_holds_the_parts_of_any_groups(lib):
-    """Whatever the sizes of the groups, those that are cut into several parts have room for all of them."""
-    rng = random.Random(1)
-    for _ in range(400):
-        n, groups = int(10 ** rng.uniform(0, 6.5)), rng.choice([1, 2, 27, 125, 1000])
-        c_in, c_out = rng.randint(1, 700), rng.randint(1, 700)
-        tile = 64 if c_in <= 64 and c_out <= 64 else 128
-        tiles = -(-c_in // tile) * -(-c_out // tile)
-        part = (max(512, (n * tiles + 511) // 512) + 63) // 64 * 64
-        need = lib.sc_grouped_workspace_bytes(n, groups, c_in, c_out, F32) - (n * c_out * 4 + 255) // 256 * 256
-        slots, left = need // ((c_in + 1) * c_out * 4), 0
-        cuts = sorted(rng.randint(0, n) for _ in range(groups - 1))
-        sizes = [b - a for a, b in zip([0] + cuts, cuts + [n])] if rng.random() < 0.5 else [min(part + 1, n - min(n, i * (part + 1))) for i in range(n // (part + 1) + 1)]
-        for e in sizes:
-            parts = -(-e // part)
-            left += parts if parts > 1 else 0
-        assert left <= slots, (n, groups, c_in, c_out, part)
 
 
 def heads(data=16, row=128, head=64, n=2):
