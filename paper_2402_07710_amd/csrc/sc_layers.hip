@@ -31,8 +31,8 @@ k_act_grad(const void* __restrict__ grad, int64_t ldg, int64_t grad_rows, const 
 }
 
 // Sums of the parts of a group, in a fixed order.  LANES threads take 4 LANES consecutive values, 256 / LANES of them every so many'th part each, then their sums:
-// few parts many values a workgroup, many parts many loads in flight.  Bound by the trip to memory: 124 parts of 129 x 512 sums, 33 MB, 8.1 us; 16 groups of
-// 513 x 2048, of which the largest have parts, 16.6 us.
+// few parts many values a workgroup, many parts many loads in flight.  Bound by the trip to memory: 124 parts of 129 x 512 sums, 33 MB, 8.0 us; 16 groups of
+// 513 x 2048, of which the largest have parts, 11.5 us (16.6 with workgroups for the groups that have one part, too).
 template <int DT, int LANES>
 __global__ void __launch_bounds__(256)
 k_product_join(const float* __restrict__ partial, const int32_t* __restrict__ starts, int groups, int64_t n, int64_t per, int M, int N,
@@ -40,19 +40,19 @@ k_product_join(const float* __restrict__ partial, const int32_t* __restrict__ st
     constexpr int SHARES = 256 / LANES;
     __shared__ float4 sums[SHARES][LANES];
     const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-    const int g = (int)(block / blocks_each);
-    if (g >= groups) return;
+    const int nth = (int)(block / blocks_each);        // of the groups that have several parts
     const int64_t values = (int64_t)(M + 1) * N;
     const int lane = threadIdx.x & 63;
     int64_t slot = 0;
-    int parts = 0;
+    int g = 0, parts = 0;
     if (starts == nullptr) {
-        parts = (int)((n + per - 1) / per);
+        if (nth == 0) parts = (int)((n + per - 1) / per);
     } else {
-        for (int g0 = 0; g0 <= g; g0 += WAVE) {
+        int seen = 0;
+        for (int g0 = 0; g0 < groups && seen <= nth; g0 += WAVE) {
             const int at = g0 + lane;
             int64_t lo = 0, hi = 0;
-            if (at <= g) {
+            if (at < groups) {
                 lo = starts[at];
                 hi = starts[at + 1];
                 lo = lo < 0 ? 0 : lo > n ? n : lo;
@@ -60,15 +60,22 @@ k_product_join(const float* __restrict__ partial, const int32_t* __restrict__ st
             }
             const uint32_t len = (uint32_t)(hi - lo), step = (uint32_t)per;
             const int count = (int)(len / step + (len % step != 0));
-            if (g - g0 < WAVE) parts = __shfl(count, g - g0);
-            int before = count > 1 && at < g ? count : 0;
+            const uint64_t several = __ballot(count > 1), mine = (uint64_t)1 << lane;
+            const int rank = seen + __popcll(several & (mine - 1));       // of this lane's group among those
+            const uint64_t found = __ballot(count > 1 && rank == nth);
+            int before = count > 1 && rank < nth ? count : 0;
 #pragma unroll
             for (int d = 1; d < WAVE; d <<= 1) before += __shfl_xor(before, d);
             slot += before;
+            if (found != 0) {
+                g = g0 + __builtin_ctzll(found);
+                parts = __shfl(count, g - g0);
+            }
+            seen += __popcll(several);
         }
     }
-    if (parts <= 1 || slot + parts > slots) return;    // written by the product itself; starts that do not ascend
-    const int64_t first = (block - (int64_t)g * blocks_each) * (4 * LANES), at = first + 4 * (threadIdx.x % LANES);
+    if (parts <= 1 || slot + parts > slots) return;    // no more such groups: the product itself has written the others; starts that do not ascend
+    const int64_t first = (block - (int64_t)nth * blocks_each) * (4 * LANES), at = first + 4 * (threadIdx.x % LANES);
     const int which = threadIdx.x / LANES;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
     const float* src = partial + slot * values + at;
@@ -264,8 +271,9 @@ int backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const Ent
         if (e.n > p.per) {
             // 1024 values a workgroup leave most of the chip idle below some thousands of them (narrow / wide: 27 groups of 64 x 64 5 / 10 us)
             const int64_t values = (int64_t)(p.M + 1) * p.N;
-            const bool many = (values + 1023) / 1024 * e.groups < 2048;
-            const int64_t wide = many ? 64 : 1024, each = (values + wide - 1) / wide, blocks = each * e.groups;
+            const int64_t cut = e.groups < e.n / p.per ? e.groups : e.n / p.per;       // groups that can have several parts
+            const bool many = (values + 1023) / 1024 * cut < 2048;
+            const int64_t wide = many ? 64 : 1024, each = (values + wide - 1) / wide, blocks = each * cut;
             if (blocks > INT32_MAX) return SC_EINVAL;
             const dim3 grid((unsigned)grid_columns(blocks), (unsigned)grid_rows(blocks));
 #define SC_JOIN(DT)                                                                                                                             \

@@ -283,6 +283,27 @@ def test_grouped(kind, c_in, c_out, listed, dtype):
             close(gb[k], dk.sum(0), bound(dk.sum(0), dk.abs().sum(0), ek.sum(0), count), f"db[{k}]")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("c_in,c_out", [(8, 8), (256, 260)])
+def test_weight_gradients_of_many_groups_in_parts(c_in, c_out, dtype):
+    """140 groups, of which every third is summed in several parts, with whole and empty ones between them: sums by few and by many values a workgroup."""
+    dt, g = DT[dtype], gen(c_in)
+    sizes = [(400 + k, 1, 128 - k % 3, 0, 300, 64)[k % 6] for k in range(140)]
+    starts = [0]
+    for e in sizes:
+        starts.append(starts[-1] + e)
+    n = starts[-1]
+    x, grad = normal(g, n, c_in, dtype=dt), normal(g, n, c_out, dtype=dt, scale=1 / 16)
+    gw, gb = torch.full((140, c_in, c_out), 7.0, dtype=dt, device=DEV), torch.full((140, c_out), 7.0, dtype=dt, device=DEV)
+    ws = torch.empty(sc.sc_grouped_workspace_bytes(n, 140, c_in, c_out, dt), dtype=torch.uint8, device=DEV)
+    sc.sc_grouped_bwd(grad.to(DEV), x.to(DEV), None, torch.tensor(starts, dtype=torch.int32, device=DEV), grad_weight=gw, grad_bias=gb, workspace=ws)
+    for k, count in enumerate(sizes):
+        xt, d = x[starts[k]:starts[k + 1]].double().t(), grad[starts[k]:starts[k + 1]].double()
+        for got, want, size in ((gw[k], xt @ d, xt.abs() @ d.abs()), (gb[k], d.sum(0), d.abs().sum(0))):
+            off = (count + 8) * 2.0 ** -23 * size
+            close(got, want, off + UNIT[dt] * (want.abs() + off) + TINY[dt], f"group {k}")
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_weight_gradient_of_a_convolution(dtype):
     """From the rulebook that a kernel map exports: both sides gathered, 27 groups, against the sum over pairs."""
