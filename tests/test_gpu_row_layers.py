@@ -212,6 +212,76 @@ def test_activations_at_their_ends(dtype):
         assert math.isnan(float(out[0]))
 
 
+# rows and channels that take every tile of row_tile and weight_tile in sc_rules.h, in whole chunks of 16 bytes and not
+LARGE_SHAPES = [(1900, 1032, 1000), (7000, 131, 521), (8200, 131, 521), (70000, 48, 136), (70001, 136, 45), (140000, 24, 72), (140000, 96, 30), (9000, 600, 1030), (66000, 520, 264),
+                (34000, 530, 520), (33000, 513, 777)]
+
+
+def there(got, want, bound, what):
+    bad = ~((got.double() - want).abs() <= bound)
+    assert not bool(bad.any()), (what, int(bad.sum()), bad.numel())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,c_in,c_out", LARGE_SHAPES)
+def test_linear_large(rows, c_in, c_out, dtype):
+    """Every element of large layers and of their gradients, against products in 64 bits on the device."""
+    dt = DT[dtype]
+    torch.manual_seed(rows + c_in)
+    x, w = torch.randn(rows, c_in, device=DEV).to(dt), (torch.randn(c_in, c_out, device=DEV) / math.sqrt(c_in)).to(dt)
+    b, r, grad = torch.randn(c_out, device=DEV).to(dt), torch.randn(rows, c_out, device=DEV).to(dt), (torch.randn(rows, c_out, device=DEV) / 16).to(dt)
+    plain, size = x.double() @ w.double(), x.double().abs() @ w.double().abs()
+    for act, extra in (("none", False), ("gelu", True)):
+        print(f"linear large {rows} {c_in} {c_out} {dtype} {act}", flush=True)
+        pre = plain + b.double() if extra else plain
+        total = size + b.double().abs() if extra else size
+        out, whole = spread(torch.zeros(rows, c_out, dtype=dt), 8)
+        kept = torch.zeros(rows, c_out, dtype=dt, device=DEV)
+        sc.sc_linear_fwd(x, w, out, bias=b if extra else None, act=act, residual=r if extra else None, pre=kept if extra else None)
+        want = act64(pre, act) + (r.double() if extra else 0.0)
+        there(out, want, forward_bound(want, pre, total + (r.double().abs() if extra else 0.0), c_in, act, dt), "out")
+        assert bool((whole[:, c_out:] == 7.0).all())
+        if extra:
+            there(kept, pre, forward_bound(pre, pre, total, c_in, "none", dt), "pre")
+        d = grad.double() * slope64(kept.double(), act)
+        d_err = torch.zeros_like(d) if act == "none" else 2 * ACT_ERROR * grad.double().abs() * (1 + kept.double().abs()) + UNIT[dt] * d.abs() + TINY[dt]
+        gx, gx_whole = spread(torch.zeros(rows, c_in, dtype=dt), 5)
+        gw, gb = torch.full((c_in, c_out), 7.0, dtype=dt, device=DEV), torch.full((c_out,), 7.0, dtype=dt, device=DEV)
+        ws = torch.empty(sc.sc_linear_workspace_bytes(rows, c_in, c_out, dt), dtype=torch.uint8, device=DEV)
+        sc.sc_linear_bwd(grad, x, w, gx, gw, gb, pre=kept if extra else None, act=act, workspace=ws)
+
+        def bound(want, size, err, K):
+            off = (K + 8) * 2.0 ** -23 * size + err
+            return off + UNIT[dt] * (want.abs() + off) + TINY[dt]
+        wt, xt = w.double().t(), x.double().t()
+        there(gx, d @ wt, bound(d @ wt, d.abs() @ wt.abs(), d_err @ wt.abs(), c_out), "dx")
+        assert bool((gx_whole[:, c_in:] == 7.0).all())
+        there(gw, xt @ d, bound(xt @ d, xt.abs() @ d.abs(), xt.abs() @ d_err, rows), "dw")
+        there(gb, d.sum(0), bound(d.sum(0), d.abs().sum(0), d_err.sum(0), rows), "db")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("c_in,c_out", [(520, 528), (521, 1030)])
+def test_grouped_large(c_in, c_out, dtype):
+    """Groups that take the large tiles, their last rows among few and many; rows from a list."""
+    dt, starts = DT[dtype], [0, 4097, 4098, 9300, 12700]
+    torch.manual_seed(c_in)
+    n, table = starts[-1], 5000
+    x, w = torch.randn(table, c_in, device=DEV).to(dt), (torch.randn(4, c_in, c_out, device=DEV) / math.sqrt(c_in)).to(dt)
+    rows, grad = torch.randint(0, table, (n,), device=DEV, dtype=torch.int32), (torch.randn(n, c_out, device=DEV) / 16).to(dt)
+    d_starts = torch.tensor(starts, dtype=torch.int32, device=DEV)
+    out, gx, gw = torch.zeros(n, c_out, dtype=dt, device=DEV), torch.zeros(n, c_in, dtype=dt, device=DEV), torch.full_like(w, 7.0)
+    sc.sc_grouped_fwd(x, w, d_starts, out, rows=rows)
+    ws = torch.empty(sc.sc_grouped_workspace_bytes(n, 4, c_in, c_out, dt), dtype=torch.uint8, device=DEV)
+    sc.sc_grouped_bwd(grad, x, w, d_starts, gx, gw, rows=rows, workspace=ws)
+    for k in range(4):
+        m = slice(starts[k], starts[k + 1])
+        xs, wk, d = x[rows[m].long()].double(), w[k].double(), grad[m].double()
+        for got, a, c, K in ((out[m], xs, wk, c_in), (gx[m], d, wk.t(), c_out), (gw[k], xs.t(), d, starts[k + 1] - starts[k])):
+            want, off = a @ c, (K + 8) * 2.0 ** -23 * (a.abs() @ c.abs())
+            there(got, want, off + UNIT[dt] * (want.abs() + off) + TINY[dt], (k, K))
+
+
 # ---- grouped ------------------------------------------------------------------------------------------------
 GROUPS = {
     "one": [0, 200],
