@@ -1073,7 +1073,6 @@ int choose_product(const Product& p, int cus, hipStream_t s) {
     } else if constexpr (MODE == PRODUCT_DX_ACT) {     // the tiles that act_in_product leaves
         switch (row_tile(p.n, p.starts == nullptr ? 0 : p.groups, p.N, p.K, false, false, cus)) {
             case TILE_16_32: return run_product<DT, MODE, 16, 32, 1, 1, 4>(p, s);
-            case TILE_16_32_DEEP: return run_product<DT, MODE, 16, 32, 1, 1, 8>(p, s);
             case TILE_32_64: return run_product<DT, MODE, 32, 64, 2, 2, 2>(p, s);
             default: return run_product<DT, MODE, 128, 32, 4, 1, 1>(p, s);
         }

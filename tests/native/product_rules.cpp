@@ -53,8 +53,8 @@ int main() {
         // slopes inside the product: only the tiles that have it
         if (act_in_product(n, groups, c_in, c_out, 256)) {
             const RowTile t = row_tile(n, groups, c_in, c_out, false, false, 256), linear = row_tile(n, 0, c_in, c_out, false, false, 256);
-            HOLDS(t == TILE_16_32 || t == TILE_16_32_DEEP || t == TILE_32_64 || t == TILE_128_32);
-            HOLDS(groups > 1 || linear == TILE_16_32 || linear == TILE_16_32_DEEP || linear == TILE_32_64 || linear == TILE_128_32);
+            HOLDS(t == TILE_16_32 || t == TILE_32_64 || t == TILE_128_32);
+            HOLDS(groups > 1 || linear == TILE_16_32 || linear == TILE_32_64 || linear == TILE_128_32);
         }
         const bool forward = rng() & 1, half = rng() & 1;
         const RowTile t = row_tile(n, i % 3 ? groups : 0, c_out, c_in, forward, half, 256);
