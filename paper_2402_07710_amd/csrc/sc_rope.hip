@@ -243,6 +243,7 @@ k_rope(const Rope p) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) squares = counts(i) ? fmaf(a[i], a[i], fmaf(b[i], b[i], squares)) : squares;
                 scale = rsqrtf(fmaf(sum_of_lanes(squares, p.lanes_log2), per_channel, p.eps));
+                if (BACKWARD && !(there && head < in.heads)) scale = 0.f;          // infinite for eps = 0: its zeros would be NaN in the gain's sums
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     a[i] *= scale;                      // the unit row
@@ -268,7 +269,7 @@ k_rope(const Rope p) {
                 if (gain != nullptr) {
                     float along = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {        // a head that is not there has zeros for its gradient
+                    for (int i = 0; i < 8; ++i) {        // a head that is not there has zeros for its gradient and its unit row
                         sum_a[i] = fmaf(x[i], a[i], sum_a[i]);
                         sum_b[i] = fmaf(y[i], b[i], sum_b[i]);
                         x[i] *= gain_a[i];

@@ -1,0 +1,60 @@
+"""GPU tests of the row layers where sizes, lists or values come to an end: no rows, heads that fill no group of lanes, epsilon zero, gradients taken by a
+list through an activation, tables with fewer rows than entries, the activation's tail, arguments that a call may leave out.  Against the definitions in 64 bits;
+bounds as in test_gpu_row_layers.py unless a test derives its own."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+from paper_2402_07710_amd import binding as sc
+from tests.test_gpu_row_layers import (ACT_ERROR, DEV, DT, TINY, UNIT, act64, close, forward_bound, gen, normal, rope64, slope64, spread)
+
+pytestmark = pytest.mark.gpu
+EVERY = pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+
+
+def product_bound(want, size, err, K, dt):
+    off = (K + 8) * 2.0 ** -23 * size + err
+    return off + UNIT[dt] * (want.abs() + off) + TINY[dt]
+
+
+# ---- norm and rotation ---------------------------------------------------------------------------------------
+def check_rope_gradients(D, pairs, heads, rows, pairing, dt, eps, v, c, gain, pos, table, keys):
+    """Gradients of `v` [rows, heads, D] (as queries, or as keys behind one head of queries) and of the gain."""
+    back, dgain = torch.full((rows, heads, D), 7.0, dtype=dt, device=DEV), torch.full((D,), 7.0, dtype=dt, device=DEV)
+    one, one_grad = (v[:, :1] + 1).to(DEV).contiguous(), c[:, :1].to(DEV).contiguous()
+    dv, dc, dg = v.to(DEV), c.to(DEV), gain.to(DEV)
+    ws = torch.empty(sc.sc_qk_rope_workspace_bytes(rows, 1 if keys else heads, heads if keys else 0, D), dtype=torch.uint8, device=DEV)
+    if keys:
+        sc.sc_qk_rope_bwd(one_grad, dc, one, dv, pos.to(DEV), table, torch.empty_like(one), back, gain_k=dg, grad_gain_k=dgain, eps=eps, pairing=pairing, workspace=ws)
+    else:
+        sc.sc_qk_rope_bwd(dc, None, dv, None, pos.to(DEV), table, back, None, gain_q=dg, grad_gain_q=dgain, eps=eps, pairing=pairing, workspace=ws)
+    v64, g64 = v.double().requires_grad_(True), gain.double().requires_grad_(True)
+    rope64(v64, pos, pairs, 10000.0, pairing, g64, eps).backward(c.double())
+    turned = rope64(c.double(), -pos, pairs, 10000.0, pairing, None, eps)
+    rms = torch.sqrt((v.double() ** 2).mean(-1, keepdim=True) + eps)
+    unit, u = v.double() / rms, turned * gain.double()
+    size = (u.abs().amax(-1, keepdim=True) + unit.abs().amax(-1, keepdim=True) * (u * unit).abs().mean(-1, keepdim=True)) / rms
+    off = 3 * (2e-6 + (D + 16) * 2.0 ** -23) * size
+    close(back, v64.grad, off + UNIT[dt] * (v64.grad.abs() + off) + TINY[dt], "dv")
+    terms = turned.abs().amax(-1, keepdim=True).expand_as(turned) * unit.abs()
+    off = (4e-6 + (D + 16) * 2.0 ** -23 + (rows * heads + 8) * 2.0 ** -23) * terms.sum((0, 1))
+    close(dgain, g64.grad, off + UNIT[dt] * (g64.grad.abs() + off) + TINY[dt], "dgain")
+
+
+@EVERY
+@pytest.mark.parametrize("pairing", ["halves", "adjacent"])
+@pytest.mark.parametrize("D,pairs", [(64, (10, 11, 11)), (36, (6, 6, 6)), (6, (1, 1, 1)), (24, (4, 4, 4))])
+@pytest.mark.parametrize("eps", [0.0, 1e-6])
+def test_rope_gradients_of_heads_that_fill_no_group(D, pairs, pairing, eps, dtype):
+    """Heads in odd numbers, one among them, and rows that leave the last lanes without work, also with an epsilon of zero: what has no head adds nothing."""
+    dt, table = DT[dtype], sc.sc_rope_table(D, pairs)
+    for heads, rows in ((1, 1), (3, 5), (1, 333), (5, 130), (2, 77)):
+        g = gen(D + 10 * heads + rows)
+        v, c = normal(g, rows, heads, D, dtype=dt), normal(g, rows, heads, D, dtype=dt)
+        gain = (1 + normal(g, D, dtype=torch.float64, scale=0.2)).to(dt)
+        pos = torch.randint(0, 2000, (rows, 3), generator=g).to(torch.int32)
+        for keys in (False, True):
+            print(f"rope bwd {D} {heads} {rows} {pairing} {dtype} eps {eps} keys {keys}", flush=True)
+            check_rope_gradients(D, pairs, heads, rows, pairing, dt, eps, v, c, gain, pos, table, keys)
