@@ -357,7 +357,9 @@ int sc_conv_up_fwd(const void* d_feat_coarse, int64_t n_map,
  * a slice of a wider one), every pointer needs the alignment of its elements only, and any number
  * of channels 1 <= C <= SC_CHANNELS_MAX is taken.  16-byte alignment of rows and channels that are multiples of 16
  * bytes are faster.  Types are SC_F32, SC_F16 and SC_BF16; sums are held in 32 bits.  Outputs must not overlap inputs,
- * except that d_y may be d_residual.  Every sum's order is fixed by the sizes: repeated calls give the same bits. */
+ * except that d_y may be d_residual.  Every sum's order is fixed by the sizes: repeated calls give the same bits.
+ * No rows, no entries: nothing is written but the gradients of weights, biases and gains, which are zeros.  Rows may then be NULL in the linear
+ * and grouped calls, but not a gradient that is asked for, nor the data of queries and keys and d_pos in sc_qk_rope_*. */
 #define SC_CHANNELS_MAX 65536
 #define SC_LD_MAX       536870912LL    /* 2^29 */
 #define SC_GROUPS_MAX   65536

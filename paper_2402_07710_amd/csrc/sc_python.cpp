@@ -223,6 +223,12 @@ struct Rows {
     PyErr_Format(kind, "%s %s", name, what);
     throw PyFailure{};
 }
+// Where a tensor's elements are.  One without elements has no address, but is not the same as none that is given, for which null stands: it gets one that
+// nothing is read from or written to.
+void* address(const at::Tensor& t) {
+    alignas(64) static char nothing[64];
+    return t.numel() == 0 ? nothing : t.data_ptr();
+}
 // every tensor among a call's arguments, behind the checks of their shapes
 void all_on_device(Args a, int n) {
     for (int i = 0; i < n; ++i)
@@ -237,7 +243,7 @@ Rows rows_of(PyObject* o, const char* name) {
     r.C = t.size(1);
     r.ld = r.n > 1 ? t.stride(0) : r.C;                // torch leaves the stride of a single row undefined
     if (r.ld < r.C) fail_on(PyExc_ValueError, name, "has rows that overlap");
-    r.data = t.data_ptr();
+    r.data = address(t);
     return r;
 }
 // a contiguous tensor of `dims` dimensions, sizes -1 unchecked
@@ -344,7 +350,7 @@ sc_heads heads_of(PyObject* o, const char* name, int64_t rows, int64_t D) {
     h.row = t.size(0) > 1 ? t.stride(0) : 0;
     h.head = t.size(1) > 1 ? t.stride(1) : 0;
     h.heads = (int32_t)t.size(1);
-    h.data = t.data_ptr();
+    h.data = address(t);
     return h;
 }
 struct Positions {
@@ -357,7 +363,7 @@ Positions positions(PyObject* o, int64_t rows) {
     if (t.dim() != 2 || t.size(0) != rows || t.scalar_type() != at::kInt) fail(PyExc_ValueError, "pos must be int32 [rows, axes]");
     if (t.size(1) > 1 && t.stride(1) != 1) fail(PyExc_ValueError, "pos must have a row's coordinates contiguous");
     const int64_t ld = t.size(0) > 1 ? t.stride(0) : t.size(1);
-    return Positions{(const int32_t*)t.data_ptr(), ld, (int)std::min<int64_t>(t.size(1), INT32_MAX)};
+    return Positions{(const int32_t*)address(t), ld, (int)std::min<int64_t>(t.size(1), INT32_MAX)};
 }
 float number(PyObject* o) {
     const double v = PyFloat_AsDouble(o);

@@ -58,3 +58,36 @@ def test_rope_gradients_of_heads_that_fill_no_group(D, pairs, pairing, eps, dtyp
         for keys in (False, True):
             print(f"rope bwd {D} {heads} {rows} {pairing} {dtype} eps {eps} keys {keys}", flush=True)
             check_rope_gradients(D, pairs, heads, rows, pairing, dt, eps, v, c, gain, pos, table, keys)
+
+
+@EVERY
+def test_rope_of_no_rows(dtype):
+    """Nothing to turn: outputs without elements, and gains whose gradients are zeros."""
+    dt, D = DT[dtype], 32
+    table, pos = sc.sc_rope_table(D, (5, 5, 6)), torch.empty(0, 3, dtype=torch.int32, device=DEV)
+
+    def none(heads):
+        return torch.empty(0, heads, D, dtype=dt, device=DEV)
+    gain, dgq, dgk = torch.ones(D, dtype=dt, device=DEV), torch.full((D,), 7.0, dtype=dt, device=DEV), torch.full((D,), 7.0, dtype=dt, device=DEV)
+    sc.sc_qk_rope_fwd(none(4), none(2), pos, table, none(4), none(2), gain_q=gain, gain_k=gain)
+    sc.sc_qk_rope_fwd(none(4), None, pos, table, none(4), None)
+    ws = torch.empty(16, dtype=torch.uint8, device=DEV)
+    sc.sc_qk_rope_bwd(none(4), none(2), none(4), none(2), pos, table, none(4), none(2), gain_q=gain, gain_k=gain, grad_gain_q=dgq, grad_gain_k=dgk, workspace=ws)
+    assert not dgq.any() and not dgk.any()
+    dgq.fill_(7.0)
+    sc.sc_qk_rope_bwd(none(4), None, none(4), None, pos, table, none(4), None, gain_q=gain, grad_gain_q=dgq, workspace=ws)
+    assert not dgq.any()
+    sc.sc_qk_rope_bwd(none(4), None, None, None, pos, table, none(4), None)
+
+
+@EVERY
+def test_no_rows_and_their_gradient_alone(dtype):
+    """A gradient of rows that has no elements is asked for all the same: nothing is to be done."""
+    dt = DT[dtype]
+    w = torch.ones(16, 24, dtype=dt, device=DEV)
+    x, grad = torch.empty(0, 16, dtype=dt, device=DEV), torch.empty(0, 24, dtype=dt, device=DEV)
+    ws, starts = torch.empty(16, dtype=torch.uint8, device=DEV), torch.zeros(3, dtype=torch.int32, device=DEV)
+    for act in ("none", "gelu"):
+        pre = grad if act != "none" else None
+        sc.sc_linear_bwd(grad, x, w, grad_x=torch.empty_like(x), pre=pre, act=act, workspace=ws)
+        sc.sc_grouped_bwd(grad, x, torch.stack([w, w]), starts, grad_x=torch.empty_like(x), pre=pre, act=act, workspace=ws)
