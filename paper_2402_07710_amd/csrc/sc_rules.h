@@ -229,10 +229,11 @@ constexpr int64_t weight_tiles(int64_t c_in, int64_t c_out) {
 // workgroups for each of 256 compute units, or one where one large tile holds the whole matrix, as each part's sums are written and read again.
 // Us of the gradient, bf16, 256 / 512 / 1024 workgroups: 16384 x 512 x 2048 78.9 / 65.9 / 71.9, 110 k x 256 x 256 40.7 / 38.6 / -, 261 k x 64 x 64 22.7 / 22.5 / -, rulebook of 360 k pairs
 // 64 x 64 29.8 / 25.4 / 29.6; one tile 261 k x 64 x 128 26.8 / 31.4 / 37.8, 53 k x 128 x 128 16.4 / 19.8 / -, 360 k pairs 128 x 128 58.1 / 68.1 / -.
-// Parts of 128 entries at least (4000 x 256 x 256, at least 64 / 128 / 256: 16.5 / 13.4 / 12.9, 1000 x 64 x 256 8.5 / 8.4 / 9.7).
+// Parts of 128 entries at least (4000 x 256 x 256, at least 64 / 128 / 256: 16.5 / 13.4 / 12.9, 1000 x 64 x 256 8.5 / 8.4 / 9.7), and no more than there are:
+// the kernels divide by them in 32 bits.
 constexpr int64_t weight_part(int64_t entries, int64_t c_in, int64_t c_out) {
     const int64_t tiles = weight_tiles(c_in, c_out), workgroups = tiles == 1 && weight_tile(c_in, c_out) != WEIGHTS_64_64 ? 256 : 512;
-    const int64_t want = (entries * tiles + workgroups - 1) / workgroups;
+    const int64_t even = (entries * tiles + workgroups - 1) / workgroups, want = even < entries ? even : entries;
     return ((want > 128 ? want : 128) + 63) / 64 * 64;
 }
 // Parts of groups that have several: a group of e entries has fewer than 2 e / part of them.
