@@ -91,3 +91,22 @@ def test_no_rows_and_their_gradient_alone(dtype):
         pre = grad if act != "none" else None
         sc.sc_linear_bwd(grad, x, w, grad_x=torch.empty_like(x), pre=pre, act=act, workspace=ws)
         sc.sc_grouped_bwd(grad, x, torch.stack([w, w]), starts, grad_x=torch.empty_like(x), pre=pre, act=act, workspace=ws)
+
+
+# ---- the activation's tail --------------------------------------------------------------------------------------
+@EVERY
+def test_gelu_in_relative_terms(dtype):
+    """v Phi(v) and Phi(v) + v phi(v) down to -12, where 16-bit types still have all their digits.  The weight of the tail is within 2.1e-5 of itself, the
+    exponential's argument within 3 2^-24 of itself (v^2 / 2 of at most 72: 1.3e-5): 4e-5 of the terms, and one rounding."""
+    dt = DT[dtype]
+    v = torch.cat([torch.linspace(-12, 6, 40001, dtype=torch.float64), -torch.logspace(-6, 1, 2000, dtype=torch.float64)]).to(dt)
+    one, exact = torch.ones(1, 1, dtype=dt, device=DEV), v.double()
+    phi, cdf = torch.exp(-exact ** 2 / 2) / math.sqrt(2 * math.pi), torch.special.erfc(-exact / math.sqrt(2)) / 2
+    out, gx = torch.empty(len(v), 1, dtype=dt, device=DEV), torch.empty(len(v), 1, dtype=dt, device=DEV)
+    sc.sc_linear_fwd(v[:, None].to(DEV), one, out, act="gelu")
+    ws = torch.empty(sc.sc_linear_workspace_bytes(len(v), 1, 1, dt), dtype=torch.uint8, device=DEV)
+    sc.sc_linear_bwd(torch.ones(len(v), 1, dtype=dt, device=DEV), v[:, None].to(DEV), one, grad_x=gx, pre=v[:, None].to(DEV), act="gelu", workspace=ws)
+    want, off = exact * cdf, 4e-5 * exact.abs() * cdf
+    close(out[:, 0], want, off + UNIT[dt] * (want.abs() + off) + TINY[dt], "gelu")
+    want, off = cdf + exact * phi, 4e-5 * (cdf + exact.abs() * phi)
+    close(gx[:, 0], want, off + UNIT[dt] * (want.abs() + off) + TINY[dt], "gelu's slope")
