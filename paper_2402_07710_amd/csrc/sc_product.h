@@ -199,7 +199,7 @@ struct Eight {
 
 // ---- activations ------------------------------------------------------------------------------------
 // Phi(v) = (1 + erf(v / sqrt 2)) / 2.  32-bit layers: the library's erf.  16-bit ones: Phi(-x) = t (a1 + t (a2 + ...)) exp(-x^2 / 2) with t = 1 / (1 + 0.2975 x) for
-// x >= 0, six coefficients fitted by weighted least squares (Lawson's iteration) on [0, 13.5] so that it is off by 4e-7 at most and by 2.2e-5 of itself at most, a tenth of
+// x >= 0, six coefficients fitted by weighted least squares (Lawson's iteration) on [0, 13.5] so that it is off by 4e-7 at most and by 2.2e-5 of itself at most, a twentieth of
 // a rounding to f16, wherever the exponential is no smaller than 32 bits hold.  A third of the instructions, and its exponential is the density that the derivative needs.
 __device__ inline float gauss_tail(float v, float& density) {          // Phi(-|v|), exp(-v^2 / 2)
     const float t = __builtin_amdgcn_rcpf(fmaf(0.2975f, fminf(fabsf(v), 64.f), 1.f));
