@@ -371,7 +371,7 @@ def sc_linear_bwd(grad_out, x, weight, grad_x=None, grad_weight=None, grad_bias=
 
 def sc_grouped_fwd(x, weight, starts, out, rows=None, bias=None, act="none", pre=None, stream=None):
     """out[p] = act(x[rows[p]] . weight[g] + bias[g]) for starts[g] <= p < starts[g + 1]: weight [groups, C_in, C_out],
-    starts int32 [groups + 1], rows int32 [n] or None (entry p reads row p), out [n, C_out]."""
+    starts int32 [groups + 1], rows int32 [n] or None (entry p reads row p, and there is one), out [n, C_out]."""
     rc = _native.grouped_fwd(x, weight, starts, out, rows, bias, ACTS[act], pre, stream)
     if rc:
         _check(rc, "sc_grouped_fwd")

@@ -273,6 +273,11 @@ void check_out_dtype(PyObject* out, PyObject* in) {
     if (!same_dtype(out, in) && tensor(out).scalar_type() != at::kFloat) fail(PyExc_ValueError, "out must be of the rows' dtype or float32");
 }
 
+// Without a list entry p reads row p.  (The library itself takes rows past the last for zeros.)
+void check_entries(const Rows& x, PyObject* list, int64_t n) {
+    if (list == Py_None && x.n < n) fail(PyExc_ValueError, "x has fewer rows than there are entries");
+}
+
 int linear_fwd(Args a) {                 // x, weight, out, bias, act, residual, pre, stream
     const Rows x = rows_of(a[0], "x"), out = rows_of(a[2], "out"), residual = rows_of(a[5], "residual"), pre = rows_of(a[6], "pre");
     const int64_t C_out = out.C;
@@ -315,6 +320,7 @@ int grouped_fwd(Args a) {                // x, weight, starts, out, rows, bias, 
     check_rows(pre, a[7], "pre", n, C_out);
     const int32_t* starts = list_of(a[2], "starts", groups + 1);
     const int32_t* rows = list_of(a[4], "rows", n);
+    check_entries(x, a[4], n);
     all_on_device(a, 9);
     return unlocked(row_lib.grouped_fwd, x.data, x.ld, x.n, rows, n, starts, (int)groups, ptr(a[1]), ptr(a[5]), small_int(a[6]), out.data, out.ld, pre.data,
                     pre.ld, (int)x.C, (int)C_out, dtype(a[0]), dtype(a[3]), stream(a[8]));
@@ -332,6 +338,7 @@ int grouped_bwd(Args a) {                // grad, x, weight, starts, grad_x, gra
     check_rows(pre, a[9], "pre", n, grad.C);
     const int32_t* starts = list_of(a[3], "starts", groups + 1);
     const int32_t* rows = list_of(a[7], "rows", n);
+    if (a[5] != Py_None) check_entries(x, a[7], n);         // rows are read for weight gradients only
     const int32_t* grad_rows = list_of(a[8], "grad_rows", n);
     all_on_device(a, 13);
     return unlocked(row_lib.grouped_bwd, grad.data, grad.ld, grad.n, grad_rows, x.data, x.ld, x.n, rows, n, starts, (int)groups, ptr(a[2]), pre.data, pre.ld,

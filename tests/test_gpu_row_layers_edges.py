@@ -93,6 +93,30 @@ def test_no_rows_and_their_gradient_alone(dtype):
         sc.sc_grouped_bwd(grad, x, torch.stack([w, w]), starts, grad_x=torch.empty_like(x), pre=pre, act=act, workspace=ws)
 
 
+# ---- grouped --------------------------------------------------------------------------------------------------
+@EVERY
+def test_fewer_rows_than_entries(dtype):
+    """At the C boundary entry p reads row p, and rows past the last are zeros: forward and in the weights' gradient."""
+    dt, g, n, x_rows, c_in, c_out = DT[dtype], gen(3), 300, 210, 40, 24
+    lib, starts = sc.load(), [0, 100, 205, 300]
+    x, w, b, grad = normal(g, x_rows, c_in, dtype=dt), normal(g, 3, c_in, c_out, dtype=dt), normal(g, 3, c_out, dtype=dt), normal(g, n, c_out, dtype=dt)
+    d_x, d_w, d_b, d_grad, s = x.to(DEV), w.to(DEV), b.to(DEV), grad.to(DEV), torch.tensor(starts, dtype=torch.int32, device=DEV)
+    out, gw = torch.empty(n, c_out, dtype=dt, device=DEV), torch.empty_like(d_w)
+    ws = torch.empty(sc.sc_grouped_workspace_bytes(n, 3, c_in, c_out, dt), dtype=torch.uint8, device=DEV)
+    p, stream = (lambda t: ctypes.c_void_p(t.data_ptr())), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    kind = sc.DTYPES[dt]
+    assert lib.sc_grouped_fwd(p(d_x), c_in, x_rows, None, n, p(s), 3, p(d_w), p(d_b), 0, p(out), c_out, None, 0, c_in, c_out, kind, kind, stream) == sc.SC_OK
+    assert lib.sc_grouped_bwd(p(d_grad), c_out, n, None, p(d_x), c_in, x_rows, None, n, p(s), 3, None, None, 0, 0, None, 0, p(gw), None, c_in, c_out, kind, p(ws),
+                              ws.numel(), stream) == sc.SC_OK
+    full = torch.cat([x, torch.zeros(n - x_rows, c_in, dtype=dt)]).double()
+    for k in range(3):
+        m = slice(starts[k], starts[k + 1])
+        want, size = full[m] @ w[k].double() + b[k].double(), full[m].abs() @ w[k].double().abs() + b[k].double().abs()
+        close(out[m], want, forward_bound(want, want, size, c_in, "none", dt), f"out[{k}]")
+        xt, d = full[m].t(), grad[m].double()
+        close(gw[k], xt @ d, product_bound(xt @ d, xt.abs() @ d.abs(), 0.0, starts[k + 1] - starts[k], dt), f"dw[{k}]")
+
+
 # ---- the activation's tail --------------------------------------------------------------------------------------
 @EVERY
 def test_gelu_in_relative_terms(dtype):

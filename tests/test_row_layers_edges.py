@@ -1,0 +1,23 @@
+"""CPU tests of refusals of the row layers that depend on how arguments fit together, before anything is launched."""
+import pytest
+import torch
+
+from paper_2402_07710_amd import binding as sc
+from tests.test_row_layers_arguments import half, heads, rope_bwd, rope_fwd
+
+EINVAL = sc.SC_EINVAL
+
+
+def test_fewer_rows_than_entries():
+    """Without a list entry p reads row p, so there has to be one."""
+    starts, w = torch.zeros(4, dtype=torch.int32), half(3, 32, 64)
+    with pytest.raises(ValueError, match="x has fewer rows than there are entries"):
+        sc.sc_grouped_fwd(half(9, 32), w, starts, half(10, 64), stream=0)
+    with pytest.raises(ValueError, match="x has fewer rows than there are entries"):
+        sc.sc_grouped_bwd(half(10, 64), half(9, 32), None, starts, grad_weight=w, stream=0)
+    rows = torch.zeros(10, dtype=torch.int32)
+    for x, kw in ((half(11, 32), {}), (half(9, 32), dict(rows=rows))):
+        with pytest.raises(ValueError, match="device tensor expected"):
+            sc.sc_grouped_fwd(x, w, starts, half(10, 64), stream=0, **kw)
+        with pytest.raises(ValueError, match="device tensor expected"):
+            sc.sc_grouped_bwd(half(10, 64), x, None, starts, grad_weight=w, stream=0, **kw)
