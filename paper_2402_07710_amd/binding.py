@@ -398,12 +398,13 @@ def sc_rope_table(D: int, pairs, base: float = 10000.0, table=None, device="cuda
         table = torch.empty(max(load().sc_rope_table_bytes(D), 16), dtype=torch.uint8, device=device)
     _check(load().sc_rope_table(D, len(pairs), (ctypes.c_int32 * len(pairs))(*pairs), base, _ptr(table),
                                 table.numel() * table.element_size(), _stream(stream)), "sc_rope_table")
+    table.rope_axes = len(pairs)            # what sc_qk_rope_* hold the positions against
     return table
 
 
 def sc_qk_rope_fwd(q, k, pos, table, q_out, k_out, gain_q=None, gain_k=None, eps=1e-6, pairing="halves", stream=None):
     """Norm (where a gain [D] is given) and rotation of queries [rows, heads, D] and keys (or None) by int32 positions
-    [rows, axes]; with voxel rows (b, x, y, z) these are coords[:, 1:].  In place with q_out = q, k_out = k."""
+    [rows, axes], all of the table's axes; with voxel rows (b, x, y, z) these are coords[:, 1:].  In place with q_out = q, k_out = k."""
     rc = _native.qk_rope_fwd(q, k, pos, table, q_out, k_out, gain_q, gain_k, eps, PAIRINGS[pairing], stream)
     if rc:
         _check(rc, "sc_qk_rope_fwd")

@@ -377,8 +377,20 @@ float number(PyObject* o) {
     if (v == -1.0 && PyErr_Occurred()) throw PyFailure{};
     return (float)v;
 }
-void check_table(PyObject* table, int64_t D) {
+// Large enough, and with a coordinate for every axis: sc_rope_table leaves their number on the tensors it gives.  (Those from elsewhere are taken as they are.)
+void check_table(PyObject* table, int64_t D, const Positions& pos) {
     if ((int64_t)nbytes(table) < 8 * D) fail(PyExc_ValueError, "table is not one of sc_rope_table for this head size");
+    static PyObject* const name = PyUnicode_InternFromString("rope_axes");
+    PyObject* const axes = PyObject_GetAttr(table, name);
+    if (axes == nullptr) {
+        if (!PyErr_ExceptionMatches(PyExc_AttributeError)) throw PyFailure{};
+        PyErr_Clear();
+        return;
+    }
+    const long n = PyLong_AsLong(axes);
+    Py_DECREF(axes);
+    if (n == -1 && PyErr_Occurred()) throw PyFailure{};
+    if (n > pos.axes) fail(PyExc_ValueError, "table turns by more axes than pos has");
 }
 int qk_rope_fwd(Args a) {                // q, k, pos, table, q_out, k_out, gain_q, gain_k, eps, pairing, stream
     if (tensor(a[0]).dim() != 3) fail(PyExc_ValueError, "q must be [rows, heads, D]");
@@ -388,8 +400,8 @@ int qk_rope_fwd(Args a) {                // q, k, pos, table, q_out, k_out, gain
     for (const int i : {1, 4, 5, 6, 7}) check_dtype(a[i], "an argument", a[0]);
     check_block(a[6], "gain_q", {D});
     check_block(a[7], "gain_k", {D});
-    check_table(a[3], D);
     const Positions pos = positions(a[2], rows);
+    check_table(a[3], D, pos);
     all_on_device(a, 11);
     return unlocked(row_lib.qk_rope_fwd, &q, a[1] == Py_None ? nullptr : &k, rows, (int)D, pos.data, pos.ld, pos.axes, (const void*)ptr(a[3]), small_int(a[9]),
                     ptr(a[6]), ptr(a[7]), number(a[8]), &q_out, a[5] == Py_None ? nullptr : &k_out, dtype(a[0]), stream(a[10]));
@@ -402,8 +414,8 @@ int qk_rope_bwd(Args a) {                // grad_q_out, grad_k_out, q, k, pos, t
     for (const int i : {1, 2, 3, 6, 7, 8, 9, 10, 11}) check_dtype(a[i], "an argument", a[0]);
     const char* const names[4] = {"gain_q", "gain_k", "grad_gain_q", "grad_gain_k"};
     for (int i = 0; i < 4; ++i) check_block(a[8 + i], names[i], {D});
-    check_table(a[5], D);
     const Positions pos = positions(a[4], rows);
+    check_table(a[5], D, pos);
     all_on_device(a, 16);
     return unlocked(row_lib.qk_rope_bwd, &dq_out, a[1] == Py_None ? nullptr : &dk_out, &q, a[3] == Py_None ? nullptr : &k, rows, (int)D, pos.data, pos.ld,
                     pos.axes, (const void*)ptr(a[5]), small_int(a[13]), ptr(a[8]), ptr(a[9]), number(a[12]), &dq, a[7] == Py_None ? nullptr : &dk,

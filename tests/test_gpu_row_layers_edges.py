@@ -93,6 +93,26 @@ def test_no_rows_and_their_gradient_alone(dtype):
         sc.sc_grouped_bwd(grad, x, torch.stack([w, w]), starts, grad_x=torch.empty_like(x), pre=pre, act=act, workspace=ws)
 
 
+def test_rope_axis_without_a_coordinate():
+    """A table of three axes and positions of two: refused; positions of more axes than the table's are not."""
+    rows, D, g = 40, 32, gen(6)
+    q = normal(g, rows, 3, D, dtype=torch.float32).to(DEV)
+    pos = torch.randint(0, 900, (rows, 4), generator=g).to(torch.int32).to(DEV)
+    out, want = torch.empty_like(q), torch.empty_like(q)
+    table = sc.sc_rope_table(D, (5, 5, 4))
+    for axes in (1, 2):
+        with pytest.raises(ValueError, match="more axes than pos has"):
+            sc.sc_qk_rope_fwd(q, None, pos[:, :axes], table, out, None)
+        with pytest.raises(ValueError, match="more axes than pos has"):
+            sc.sc_qk_rope_bwd(q, None, None, None, pos[:, :axes], table, out, None)
+    sc.sc_qk_rope_fwd(q, None, pos[:, :3], table, want, None)
+    sc.sc_qk_rope_fwd(q, None, pos, table, out, None)
+    assert torch.equal(out, want)
+    sc.sc_rope_table(D, (5, 5), table=table)                   # the same memory, two axes now
+    sc.sc_qk_rope_fwd(q, None, pos[:, :2], table, out, None)
+    assert bool(torch.isfinite(out).all())
+
+
 # ---- grouped --------------------------------------------------------------------------------------------------
 @EVERY
 def test_fewer_rows_than_entries(dtype):

@@ -21,3 +21,21 @@ def test_fewer_rows_than_entries():
             sc.sc_grouped_fwd(x, w, starts, half(10, 64), stream=0, **kw)
         with pytest.raises(ValueError, match="device tensor expected"):
             sc.sc_grouped_bwd(half(10, 64), x, None, starts, grad_weight=w, stream=0, **kw)
+
+
+def test_positions_without_the_axes_of_the_table():
+    """The table says by how many axes it turns; one that does not is taken as it is."""
+    q, table = half(5, 2, 64), torch.zeros(512, dtype=torch.uint8)
+    two, three = (torch.zeros(5, n, dtype=torch.int32) for n in (2, 3))
+    with pytest.raises(ValueError, match="device tensor expected"):
+        sc.sc_qk_rope_fwd(q, None, two, table, q, None, stream=0)
+    table.rope_axes = 3
+    with pytest.raises(ValueError, match="table turns by more axes than pos has"):
+        sc.sc_qk_rope_fwd(q, None, two, table, q, None, stream=0)
+    with pytest.raises(ValueError, match="table turns by more axes than pos has"):
+        sc.sc_qk_rope_bwd(q, None, None, None, two, table, q, None, stream=0)
+    with pytest.raises(ValueError, match="device tensor expected"):
+        sc.sc_qk_rope_fwd(q, None, three, table, q, None, stream=0)
+    table.rope_axes = "three"
+    with pytest.raises(TypeError):
+        sc.sc_qk_rope_fwd(q, None, three, table, q, None, stream=0)
