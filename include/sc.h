@@ -432,7 +432,7 @@ int sc_grouped_bwd(const void* d_dy, int64_t lddy, int64_t dy_rows, const int32_
  * f = base^(-i/m).  Statistics, angles and the rotation are in 32 bits, angles reduced exactly to a turn first
  * (|pos| < 2^24), with one rounding at the end.
  *   q, k        rows x heads x D, `row` and `head` elements apart (any order of rows and heads); k NULL or k->heads = 0: queries only.
- *               q_out and k_out have the same numbers of heads; they may be q and k themselves (same strides).
+ *               q_out and k_out have the same numbers of heads, none of which overlap; they may be q and k themselves (same strides).
  *   d_pos       [rows][axes] int32, ld_pos apart: with voxel rows (b, x, y, z), d_coords + 1 and ld_pos 4
  *   d_table     from sc_rope_table, sc_rope_table_bytes(D) bytes, 16-byte aligned.  Pairs of an axis that d_pos does not have are not turned
  *   D           even, 2 <= D <= SC_HEAD_MAX; 1 <= axes <= SC_AXES_MAX; 0 <= rows <= SC_N_MAX; at most SC_GROUPS_MAX heads */

@@ -359,6 +359,17 @@ Heads heads_of(const sc_heads* h, int dtype) {
     const int size = dtype == SC_F32 ? 4 : 2;
     return Heads{(char*)h->data, h->row * size, h->head * size, h->heads};
 }
+// No element of an output belongs to two heads.  Mostly the heads of a row lie within it, or the rows of a head within that; rows and heads that
+// interleave otherwise are gone through.
+bool heads_apart(const sc_heads* h, int64_t rows, int D) {
+    const int64_t row = h->row, head = h->head, heads = h->heads;
+    if ((rows > 1 && row < D) || (heads > 1 && head < D)) return false;
+    if (rows <= 1 || heads <= 1 || row >= head * (heads - 1) + D || head >= row * (rows - 1) + D) return true;
+    for (int64_t j = 1; j < heads; ++j)                // row i and head j of another: i row - j head
+        for (int64_t i = j * head / row; i <= j * head / row + 1; ++i)
+            if (i > 0 && i < rows && i * row - j * head < D && j * head - i * row < D) return false;
+    return true;
+}
 bool has_keys(const sc_heads* k) { return k != nullptr && k->heads > 0; }
 
 int check_rope(const sc_heads* q, const sc_heads* k, int64_t rows, int D, const int32_t* d_pos, int64_t ld_pos, int axes, const void* d_table, int pairing,
@@ -371,6 +382,7 @@ int check_rope(const sc_heads* q, const sc_heads* k, int64_t rows, int D, const 
     if (((uintptr_t)gain_q & off) != 0 || ((uintptr_t)gain_k & off) != 0) return SC_EINVAL;
     if (!heads_ok(q, dtype) || !heads_ok(q_out, dtype) || q->heads < 1 || q_out->heads != q->heads) return SC_EINVAL;
     if (has_keys(k) && (!heads_ok(k, dtype) || !heads_ok(k_out, dtype) || k_out->heads != k->heads)) return SC_EINVAL;
+    if (!heads_apart(q_out, rows, D) || (has_keys(k) && !heads_apart(k_out, rows, D))) return SC_EINVAL;
     return SC_OK;
 }
 

@@ -113,6 +113,33 @@ def test_rope_axis_without_a_coordinate():
     assert bool(torch.isfinite(out).all())
 
 
+def test_rope_heads_between_each_other():
+    """Outputs whose rows and heads interleave without touching are as good as any; those that touch are refused."""
+    g, D = gen(4), 8
+    pos, table = torch.randint(0, 900, (3, 3), generator=g).to(torch.int32).to(DEV), sc.sc_rope_table(D, (1, 1, 1))
+    q = normal(g, 3, 2, D, dtype=torch.float32).to(DEV)
+    want = torch.empty_like(q)
+    sc.sc_qk_rope_fwd(q, None, pos, table, want, None)
+    for row, head in ((16, 8), (8, 24), (16, 40), (24, 16), (20, 50)):
+        space = torch.full((200,), 7.0, device=DEV)
+        out = space.as_strided((3, 2, D), (row, head, 1))
+        sc.sc_qk_rope_fwd(q, None, pos, table, out, None)
+        assert torch.equal(out, want), (row, head)
+        assert int((space == 7.0).sum()) == 200 - 3 * 2 * D
+    for row, head in ((0, 8), (8, 0), (7, 30), (16, 7), (8, 8), (8, 16), (20, 47), (16, 30)):
+        out = torch.empty(200, device=DEV).as_strided((3, 2, D), (row, head, 1))
+        with pytest.raises(sc.ScError):
+            sc.sc_qk_rope_fwd(q, None, pos, table, out, None)
+        with pytest.raises(sc.ScError):
+            sc.sc_qk_rope_bwd(q, None, None, None, pos, table, out, None)
+    # inputs may: one head's gradient for all of them
+    c = normal(g, 3, 1, D, dtype=torch.float32).to(DEV)
+    back, same = torch.empty_like(q), torch.empty_like(q)
+    sc.sc_qk_rope_bwd(c.expand(3, 2, D), None, None, None, pos, table, back, None)
+    sc.sc_qk_rope_bwd(c.expand(3, 2, D).contiguous(), None, None, None, pos, table, same, None)
+    assert torch.equal(back, same)
+
+
 # ---- grouped --------------------------------------------------------------------------------------------------
 @EVERY
 def test_fewer_rows_than_entries(dtype):

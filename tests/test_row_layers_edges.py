@@ -8,6 +8,21 @@ from tests.test_row_layers_arguments import half, heads, rope_bwd, rope_fwd
 EINVAL = sc.SC_EINVAL
 
 
+@pytest.fixture(scope="module")
+def lib():
+    return sc.load()
+
+
+def test_rope_outputs_that_overlap(lib):
+    """Rows 0, heads 0 apart; heads within each other; rows that start inside the heads of others.  (Inputs may: they are only read.)"""
+    for row, head, n in ((0, 64, 2), (128, 0, 2), (128, 63, 2), (127, 64, 2), (63, 1 << 20, 2), (64, 128, 3), (100, 350, 2), (150, 160, 2)):
+        out = heads(row=row, head=head, n=n)
+        assert rope_fwd(lib, rows=5, q=heads(n=n), qo=out) == EINVAL, (row, head, n)
+        assert rope_fwd(lib, rows=5, k=heads(n=n), ko=out) == EINVAL, (row, head, n)
+        assert rope_bwd(lib, rows=5, dqo=heads(n=n), dq=out) == EINVAL, (row, head, n)
+        assert rope_bwd(lib, rows=5, dko=heads(n=n), dk=out) == EINVAL, (row, head, n)
+
+
 def test_fewer_rows_than_entries():
     """Without a list entry p reads row p, so there has to be one."""
     starts, w = torch.zeros(4, dtype=torch.int32), half(3, 32, 64)
