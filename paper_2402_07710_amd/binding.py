@@ -362,7 +362,8 @@ def sc_linear_workspace_bytes(rows: int, C_in: int, C_out: int, dtype) -> int:
 
 
 def sc_linear_bwd(grad_out, x, weight, grad_x=None, grad_weight=None, grad_bias=None, pre=None, act="none", workspace=None, stream=None):
-    """Gradients of sc_linear_fwd where a tensor is given for them (the residual's is grad_out itself);
+    """Gradients of sc_linear_fwd where a tensor is given for them (the residual's is grad_out itself); without
+    grad_weight x may be None, without grad_x weight (not both);
     workspace uint8 [>= sc_linear_workspace_bytes(...)]."""
     rc = _native.linear_bwd(grad_out, x, weight, grad_x, grad_weight, grad_bias, pre, ACTS[act], workspace, stream)
     if rc:
@@ -384,7 +385,7 @@ def sc_grouped_workspace_bytes(n: int, groups: int, C_in: int, C_out: int, dtype
 def sc_grouped_bwd(grad_out, x, weight, starts, grad_x=None, grad_weight=None, grad_bias=None, rows=None, grad_rows=None, pre=None,
                    act="none", workspace=None, stream=None):
     """Gradients of sc_grouped_fwd; entry p's output gradient is grad_out[grad_rows[p]] (None: grad_out[p]), grad_x has one row
-    per entry.  With the lists of sc_kmap_export, grad_weight is a convolution's weight gradient."""
+    per entry.  x and weight may be None as in sc_linear_bwd.  With the lists of sc_kmap_export, grad_weight is a convolution's weight gradient."""
     rc = _native.grouped_bwd(grad_out, x, weight, starts, grad_x, grad_weight, grad_bias, rows, grad_rows, pre, ACTS[act], workspace, stream)
     if rc:
         _check(rc, "sc_grouped_bwd")

@@ -297,16 +297,17 @@ int linear_fwd(Args a) {                 // x, weight, out, bias, act, residual,
 }
 int linear_bwd(Args a) {                 // grad, x, weight, grad_x, grad_weight, grad_bias, pre, act, workspace, stream
     const Rows grad = rows_of(a[0], "grad_out"), x = rows_of(a[1], "x"), grad_x = rows_of(a[3], "grad_x"), pre = rows_of(a[6], "pre");
-    check_block(a[2], "weight", {x.C, grad.C});
-    check_block(a[4], "grad_weight", {x.C, grad.C});
+    const int64_t C_in = a[1] == Py_None && a[2] != Py_None ? size(a[2], 0) : x.C;         // x is read for the weight's gradient only
+    check_block(a[2], "weight", {C_in, grad.C});
+    check_block(a[4], "grad_weight", {C_in, grad.C});
     check_block(a[5], "grad_bias", {grad.C});
     for (int i = 1; i <= 6; ++i) check_dtype(a[i], "an argument", a[0]);
-    check_rows(x, a[1], "x", grad.n, x.C);
-    check_rows(grad_x, a[3], "grad_x", grad.n, x.C);
+    check_rows(x, a[1], "x", grad.n, C_in);
+    check_rows(grad_x, a[3], "grad_x", grad.n, C_in);
     check_rows(pre, a[6], "pre", grad.n, grad.C);
     all_on_device(a, 10);
     return unlocked(row_lib.linear_bwd, grad.data, grad.ld, x.data, x.ld, grad.n, ptr(a[2]), pre.data, pre.ld, small_int(a[7]), grad_x.data, grad_x.ld,
-                    ptr(a[4]), ptr(a[5]), (int)x.C, (int)grad.C, dtype(a[0]), ptr(a[8]), nbytes(a[8]), stream(a[9]));
+                    ptr(a[4]), ptr(a[5]), (int)C_in, (int)grad.C, dtype(a[0]), ptr(a[8]), nbytes(a[8]), stream(a[9]));
 }
 int grouped_fwd(Args a) {                // x, weight, starts, out, rows, bias, act, pre, stream
     const Rows x = rows_of(a[0], "x"), out = rows_of(a[3], "out"), pre = rows_of(a[7], "pre");
@@ -330,11 +331,12 @@ int grouped_bwd(Args a) {                // grad, x, weight, starts, grad_x, gra
     const int64_t groups = size(a[3], 0) - 1;
     int64_t n = grad.n;                  // entries: as many as there are gradient rows, or as the list has
     if (a[8] != Py_None) n = size(a[8], 0);
-    check_block(a[2], "weight", {groups, x.C, grad.C});
-    check_block(a[5], "grad_weight", {groups, x.C, grad.C});
+    const int64_t C_in = a[1] == Py_None && a[2] != Py_None ? size(a[2], 1) : x.C;
+    check_block(a[2], "weight", {groups, C_in, grad.C});
+    check_block(a[5], "grad_weight", {groups, C_in, grad.C});
     check_block(a[6], "grad_bias", {groups, grad.C});
     for (const int i : {1, 2, 4, 5, 6, 9}) check_dtype(a[i], "an argument", a[0]);
-    check_rows(grad_x, a[4], "grad_x", n, x.C);
+    check_rows(grad_x, a[4], "grad_x", n, C_in);
     check_rows(pre, a[9], "pre", n, grad.C);
     const int32_t* starts = list_of(a[3], "starts", groups + 1);
     const int32_t* rows = list_of(a[7], "rows", n);
@@ -342,7 +344,7 @@ int grouped_bwd(Args a) {                // grad, x, weight, starts, grad_x, gra
     const int32_t* grad_rows = list_of(a[8], "grad_rows", n);
     all_on_device(a, 13);
     return unlocked(row_lib.grouped_bwd, grad.data, grad.ld, grad.n, grad_rows, x.data, x.ld, x.n, rows, n, starts, (int)groups, ptr(a[2]), pre.data, pre.ld,
-                    small_int(a[10]), grad_x.data, grad_x.ld, ptr(a[5]), ptr(a[6]), (int)x.C, (int)grad.C, dtype(a[0]), ptr(a[11]), nbytes(a[11]),
+                    small_int(a[10]), grad_x.data, grad_x.ld, ptr(a[5]), ptr(a[6]), (int)C_in, (int)grad.C, dtype(a[0]), ptr(a[11]), nbytes(a[11]),
                     stream(a[12]));
 }
 

@@ -164,6 +164,25 @@ def test_fewer_rows_than_entries(dtype):
         close(gw[k], xt @ d, product_bound(xt @ d, xt.abs() @ d.abs(), 0.0, starts[k + 1] - starts[k], dt), f"dw[{k}]")
 
 
+# ---- what a call may leave out ----------------------------------------------------------------------------------
+@EVERY
+def test_rows_gradient_without_the_rows(dtype):
+    """The gradient of the rows needs the weights, not the rows: where no weight gradient is asked for, x may be None."""
+    dt, g, n, c_in, c_out = DT[dtype], gen(1), 200, 48, 40
+    w, grad, pre = (normal(g, *s, dtype=dt).to(DEV) for s in ((2, c_in, c_out), (n, c_out), (n, c_out)))
+    x, starts = normal(g, n, c_in, dtype=dt).to(DEV), torch.tensor([0, 90, n], dtype=torch.int32, device=DEV)
+    ws = torch.empty(sc.sc_grouped_workspace_bytes(n, 2, c_in, c_out, dt), dtype=torch.uint8, device=DEV)
+    for act in ("none", "gelu"):
+        got = [torch.full((n, c_in), 7.0, dtype=dt, device=DEV) for _ in range(4)]
+        gb = [torch.full((2, c_out), 7.0, dtype=dt, device=DEV) for _ in range(4)]
+        kw = dict(pre=pre if act != "none" else None, act=act, workspace=ws)
+        for i, rows in enumerate((x, None)):
+            sc.sc_linear_bwd(grad, rows, w[0], grad_x=got[i], grad_bias=gb[i][0], **kw)
+            sc.sc_grouped_bwd(grad, rows, w, starts, grad_x=got[2 + i], grad_bias=gb[2 + i], **kw)
+        assert torch.equal(got[0], got[1]) and torch.equal(got[2], got[3]) and torch.equal(gb[0], gb[1]) and torch.equal(gb[2], gb[3])
+        assert bool((got[0] != 7.0).any()) and bool((got[2] != 7.0).any())
+
+
 # ---- the activation's tail --------------------------------------------------------------------------------------
 @EVERY
 def test_gelu_in_relative_terms(dtype):

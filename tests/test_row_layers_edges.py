@@ -38,6 +38,24 @@ def test_fewer_rows_than_entries():
             sc.sc_grouped_bwd(half(10, 64), x, None, starts, grad_weight=w, stream=0, **kw)
 
 
+def test_weights_of_rows_that_are_not_given():
+    """x may be None where no weight gradient is asked for; shapes are then the weights'."""
+    grad = half(10, 64)
+    with pytest.raises(ValueError, match="device tensor expected"):
+        sc.sc_linear_bwd(grad, None, half(32, 64), grad_x=half(10, 32), stream=0)
+    with pytest.raises(ValueError, match="grad_x has the wrong shape"):
+        sc.sc_linear_bwd(grad, None, half(32, 64), grad_x=half(10, 31), stream=0)
+    with pytest.raises(ValueError, match="weight has the wrong shape"):
+        sc.sc_linear_bwd(grad, None, half(32, 63), grad_x=half(10, 32), stream=0)
+    starts = torch.zeros(4, dtype=torch.int32)
+    with pytest.raises(ValueError, match="device tensor expected"):
+        sc.sc_grouped_bwd(grad, None, half(3, 32, 64), starts, grad_x=half(10, 32), stream=0)
+    with pytest.raises(ValueError, match="grad_x has the wrong shape"):
+        sc.sc_grouped_bwd(grad, None, half(3, 32, 64), starts, grad_x=half(10, 31), stream=0)
+    with pytest.raises(ValueError, match="weight has the wrong shape"):
+        sc.sc_grouped_bwd(grad, None, half(2, 32, 64), starts, grad_x=half(10, 32), stream=0)
+
+
 def test_positions_without_the_axes_of_the_table():
     """The table says by how many axes it turns; one that does not is taken as it is."""
     q, table = half(5, 2, 64), torch.zeros(512, dtype=torch.uint8)
