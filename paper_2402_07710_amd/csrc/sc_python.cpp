@@ -243,6 +243,7 @@ Rows rows_of(PyObject* o, const char* name) {
     r.C = t.size(1);
     r.ld = r.n > 1 ? t.stride(0) : r.C;                // torch leaves the stride of a single row undefined
     if (r.ld < r.C) fail_on(PyExc_ValueError, name, "has rows that overlap");
+    if (r.C > INT32_MAX) fail_on(PyExc_ValueError, name, "has too many channels");         // the library counts them in an int
     r.data = address(t);
     return r;
 }
@@ -259,6 +260,8 @@ void check_block(PyObject* o, const char* name, std::initializer_list<int64_t> s
 void check_dtype(PyObject* o, const char* name, PyObject* like) {
     if (o != Py_None && !same_dtype(o, like)) fail_on(PyExc_ValueError, name, "has the wrong dtype");
 }
+// a count for the library, which holds it in an int; what does not fit is above every limit anyway
+int count32(int64_t n) { return (int)std::min<int64_t>(n, INT32_MAX); }
 const int32_t* list_of(PyObject* o, const char* name, int64_t n) {
     if (o == Py_None) return nullptr;
     const at::Tensor& t = tensor(o);
@@ -307,7 +310,7 @@ int linear_bwd(Args a) {                 // grad, x, weight, grad_x, grad_weight
     check_rows(pre, a[6], "pre", grad.n, grad.C);
     all_on_device(a, 10);
     return unlocked(row_lib.linear_bwd, grad.data, grad.ld, x.data, x.ld, grad.n, ptr(a[2]), pre.data, pre.ld, small_int(a[7]), grad_x.data, grad_x.ld,
-                    ptr(a[4]), ptr(a[5]), (int)C_in, (int)grad.C, dtype(a[0]), ptr(a[8]), nbytes(a[8]), stream(a[9]));
+                    ptr(a[4]), ptr(a[5]), count32(C_in), (int)grad.C, dtype(a[0]), ptr(a[8]), nbytes(a[8]), stream(a[9]));
 }
 int grouped_fwd(Args a) {                // x, weight, starts, out, rows, bias, act, pre, stream
     const Rows x = rows_of(a[0], "x"), out = rows_of(a[3], "out"), pre = rows_of(a[7], "pre");
@@ -323,7 +326,7 @@ int grouped_fwd(Args a) {                // x, weight, starts, out, rows, bias, 
     const int32_t* rows = list_of(a[4], "rows", n);
     check_entries(x, a[4], n);
     all_on_device(a, 9);
-    return unlocked(row_lib.grouped_fwd, x.data, x.ld, x.n, rows, n, starts, (int)groups, ptr(a[1]), ptr(a[5]), small_int(a[6]), out.data, out.ld, pre.data,
+    return unlocked(row_lib.grouped_fwd, x.data, x.ld, x.n, rows, n, starts, count32(groups), ptr(a[1]), ptr(a[5]), small_int(a[6]), out.data, out.ld, pre.data,
                     pre.ld, (int)x.C, (int)C_out, dtype(a[0]), dtype(a[3]), stream(a[8]));
 }
 int grouped_bwd(Args a) {                // grad, x, weight, starts, grad_x, grad_weight, grad_bias, rows, grad_rows, pre, act, workspace, stream
@@ -343,8 +346,8 @@ int grouped_bwd(Args a) {                // grad, x, weight, starts, grad_x, gra
     if (a[5] != Py_None) check_entries(x, a[7], n);         // rows are read for weight gradients only
     const int32_t* grad_rows = list_of(a[8], "grad_rows", n);
     all_on_device(a, 13);
-    return unlocked(row_lib.grouped_bwd, grad.data, grad.ld, grad.n, grad_rows, x.data, x.ld, x.n, rows, n, starts, (int)groups, ptr(a[2]), pre.data, pre.ld,
-                    small_int(a[10]), grad_x.data, grad_x.ld, ptr(a[5]), ptr(a[6]), (int)C_in, (int)grad.C, dtype(a[0]), ptr(a[11]), nbytes(a[11]),
+    return unlocked(row_lib.grouped_bwd, grad.data, grad.ld, grad.n, grad_rows, x.data, x.ld, x.n, rows, n, starts, count32(groups), ptr(a[2]), pre.data, pre.ld,
+                    small_int(a[10]), grad_x.data, grad_x.ld, ptr(a[5]), ptr(a[6]), count32(C_in), (int)grad.C, dtype(a[0]), ptr(a[11]), nbytes(a[11]),
                     stream(a[12]));
 }
 
@@ -372,7 +375,7 @@ Positions positions(PyObject* o, int64_t rows) {
     if (t.dim() != 2 || t.size(0) != rows || t.scalar_type() != at::kInt) fail(PyExc_ValueError, "pos must be int32 [rows, axes]");
     if (t.size(1) > 1 && t.stride(1) != 1) fail(PyExc_ValueError, "pos must have a row's coordinates contiguous");
     const int64_t ld = t.size(0) > 1 ? t.stride(0) : t.size(1);
-    return Positions{(const int32_t*)address(t), ld, (int)std::min<int64_t>(t.size(1), INT32_MAX)};
+    return Positions{(const int32_t*)address(t), ld, count32(t.size(1))};
 }
 float number(PyObject* o) {
     const double v = PyFloat_AsDouble(o);
@@ -405,7 +408,7 @@ int qk_rope_fwd(Args a) {                // q, k, pos, table, q_out, k_out, gain
     const Positions pos = positions(a[2], rows);
     check_table(a[3], D, pos);
     all_on_device(a, 11);
-    return unlocked(row_lib.qk_rope_fwd, &q, a[1] == Py_None ? nullptr : &k, rows, (int)D, pos.data, pos.ld, pos.axes, (const void*)ptr(a[3]), small_int(a[9]),
+    return unlocked(row_lib.qk_rope_fwd, &q, a[1] == Py_None ? nullptr : &k, rows, count32(D), pos.data, pos.ld, pos.axes, (const void*)ptr(a[3]), small_int(a[9]),
                     ptr(a[6]), ptr(a[7]), number(a[8]), &q_out, a[5] == Py_None ? nullptr : &k_out, dtype(a[0]), stream(a[10]));
 }
 int qk_rope_bwd(Args a) {                // grad_q_out, grad_k_out, q, k, pos, table, grad_q, grad_k, gain_q, gain_k, grad_gain_q, grad_gain_k, eps, pairing, workspace, stream
@@ -419,7 +422,7 @@ int qk_rope_bwd(Args a) {                // grad_q_out, grad_k_out, q, k, pos, t
     const Positions pos = positions(a[4], rows);
     check_table(a[5], D, pos);
     all_on_device(a, 16);
-    return unlocked(row_lib.qk_rope_bwd, &dq_out, a[1] == Py_None ? nullptr : &dk_out, &q, a[3] == Py_None ? nullptr : &k, rows, (int)D, pos.data, pos.ld,
+    return unlocked(row_lib.qk_rope_bwd, &dq_out, a[1] == Py_None ? nullptr : &dk_out, &q, a[3] == Py_None ? nullptr : &k, rows, count32(D), pos.data, pos.ld,
                     pos.axes, (const void*)ptr(a[5]), small_int(a[13]), ptr(a[8]), ptr(a[9]), number(a[12]), &dq, a[7] == Py_None ? nullptr : &dk,
                     ptr(a[10]), ptr(a[11]), dtype(a[0]), ptr(a[14]), nbytes(a[14]), stream(a[15]));
 }

@@ -38,6 +38,13 @@ def test_fewer_rows_than_entries():
             sc.sc_grouped_bwd(half(10, 64), x, None, starts, grad_weight=w, stream=0, **kw)
 
 
+def test_channels_that_no_int_holds():
+    """2^32 + 32 channels are not 32."""
+    wide, many = (torch.empty(shape, dtype=torch.float16, device="meta") for shape in ((1, (1 << 32) + 32), ((1 << 32) + 32, 64)))
+    with pytest.raises(ValueError, match="x has too many channels"):
+        sc.sc_linear_fwd(wide, many, half(1, 64), stream=0)
+
+
 def test_weights_of_rows_that_are_not_given():
     """x may be None where no weight gradient is asked for; shapes are then the weights'."""
     grad = half(10, 64)
