@@ -141,6 +141,48 @@ def test_rope_heads_between_each_other():
 
 
 # ---- grouped --------------------------------------------------------------------------------------------------
+# entries, starts, channels: with c_in = 32 and many entries and with few of both the slopes are inside the product with the weights, otherwise they are a pass of their own
+LISTED = [(300, [0, 130, 131, 131, 260, 290], 64, 40), (70000, [0, 40000, 40001, 69990], 32, 24), (70000, [0, 40000, 40001, 69990], 31, 25), (5000, [0, 2100, 2100, 4990], 136, 264)]
+
+
+@EVERY
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "silu"])
+@pytest.mark.parametrize("n,starts,c_in,c_out", LISTED)
+def test_gradients_taken_by_a_list(n, starts, c_in, c_out, act, dtype):
+    """Output gradients gathered by a list, some rows several times, some that are not there, through an activation whose arguments are one row per entry."""
+    dt, groups, g = DT[dtype], len(starts) - 1, gen(n + c_in)
+    print(f"listed gradients {n} {c_in} {c_out} {act} {dtype}", flush=True)
+    x_rows, dy_rows = 90, 70
+    x, w = normal(g, x_rows, c_in, dtype=dt), normal(g, groups, c_in, c_out, dtype=dt, scale=1 / math.sqrt(c_in))
+    dy, pre = normal(g, dy_rows, c_out, dtype=dt, scale=1 / 16), normal(g, n, c_out, dtype=dt)
+    rows, grad_rows = (torch.randint(0, m, (n,), generator=g).to(torch.int32) for m in (x_rows, dy_rows))
+    rows[5], rows[140] = -1, x_rows
+    grad_rows[0], grad_rows[7], grad_rows[8], grad_rows[131], grad_rows[starts[-1] - 1] = -1, dy_rows, -(1 << 31), (1 << 31) - 1, dy_rows + 3
+    pre[7] = math.inf                                          # of an entry whose gradient is not there: it adds nothing
+
+    def taken(t, list_):
+        ok = (list_ >= 0) & (list_ < len(t))
+        return t.double()[torch.where(ok, list_, 0).long()] * ok[:, None]
+    xs, grad = taken(x, rows), taken(dy, grad_rows)
+    slopes = slope64(torch.where(torch.isfinite(pre), pre, 0.0).double(), act)
+    d = grad * slopes
+    d_err = torch.zeros_like(d) if act == "none" else (2 * ACT_ERROR * grad.abs() * (1 + torch.where(torch.isfinite(pre), pre, 0.0).double().abs()) + UNIT[dt] * d.abs() +
+                                                        TINY[dt] * (d != 0))
+    gx = torch.full((n, c_in), 7.0, dtype=dt, device=DEV)
+    gw, gb = torch.full((groups, c_in, c_out), 7.0, dtype=dt, device=DEV), torch.full((groups, c_out), 7.0, dtype=dt, device=DEV)
+    ws = torch.empty(sc.sc_grouped_workspace_bytes(n, groups, c_in, c_out, dt), dtype=torch.uint8, device=DEV)
+    sc.sc_grouped_bwd(spread(dy, 8)[0], spread(x, 8)[0], w.to(DEV), torch.tensor(starts, dtype=torch.int32, device=DEV), gx, gw, gb, rows=rows.to(DEV),
+                      grad_rows=grad_rows.to(DEV), pre=spread(pre, 8)[0] if act != "none" else None, act=act, workspace=ws)
+    for k in range(groups):
+        m = slice(starts[k], starts[k + 1])
+        xk, dk, ek, wt = xs[m], d[m], d_err[m], w[k].double().t().contiguous()
+        close(gx[m], dk @ wt, product_bound(dk @ wt, dk.abs() @ wt.abs(), ek @ wt.abs(), c_out, dt), f"dx[{k}]")
+        xt, count = xk.t().contiguous(), starts[k + 1] - starts[k]
+        close(gw[k], xt @ dk, product_bound(xt @ dk, xt.abs() @ dk.abs(), xt.abs() @ ek, count, dt), f"dw[{k}]")
+        close(gb[k], dk.sum(0), product_bound(dk.sum(0), dk.abs().sum(0), ek.sum(0), count, dt), f"db[{k}]")
+    assert bool((gx[starts[-1]:] == 7.0).all())
+
+
 @EVERY
 def test_fewer_rows_than_entries(dtype):
     """At the C boundary entry p reads row p, and rows past the last are zeros: forward and in the weights' gradient."""
@@ -162,6 +204,51 @@ def test_fewer_rows_than_entries(dtype):
         close(out[m], want, forward_bound(want, want, size, c_in, "none", dt), f"out[{k}]")
         xt, d = full[m].t(), grad[m].double()
         close(gw[k], xt @ d, product_bound(xt @ d, xt.abs() @ d.abs(), 0.0, starts[k + 1] - starts[k], dt), f"dw[{k}]")
+
+
+def test_as_many_groups_as_there_may_be():
+    """SC_GROUPS_MAX of them, of 0 to 400 entries, some in several parts: forward and both gradients."""
+    groups, c, dt = sc.SC_GROUPS_MAX, 16, torch.float32
+    torch.manual_seed(4)
+    sizes = torch.randint(0, 3, (groups,))
+    sizes[[0, 77, 30000, 65535]] = torch.tensor([400, 0, 300, 129])
+    starts = torch.cat([torch.zeros(1, dtype=torch.int64), sizes.cumsum(0)])
+    n, owner = int(starts[-1]), torch.repeat_interleave(torch.arange(groups), sizes).to(DEV)
+    x, grad, w = torch.randn(n, c, device=DEV), torch.randn(n, c, device=DEV), torch.randn(groups, c, c, device=DEV)
+    out, gx, gw, gb = torch.empty_like(x), torch.empty_like(x), torch.full_like(w, 7.0), torch.full((groups, c), 7.0, device=DEV)
+    d_starts, ws = starts.to(DEV, torch.int32), torch.empty(sc.sc_grouped_workspace_bytes(n, groups, c, c, dt), dtype=torch.uint8, device=DEV)
+    sc.sc_grouped_fwd(x, w, d_starts, out)
+    sc.sc_grouped_bwd(grad, x, w, d_starts, gx, gw, gb, workspace=ws)
+
+    def by_group(t):
+        return torch.zeros(groups, *t.shape[1:], dtype=torch.float64, device=DEV).index_add(0, owner, t)
+    x, grad, w = x.double(), grad.double(), w.double()[owner]
+    for got, terms, axis, K in ((out, x[:, :, None] * w, 1, c), (gx, grad[:, None, :] * w, 2, c)):
+        close(got, terms.sum(axis).cpu(), product_bound(terms.sum(axis), terms.abs().sum(axis), 0.0, K, dt).cpu())
+    outer = x[:, :, None] * grad[:, None, :]
+    close(gw, by_group(outer).cpu(), product_bound(by_group(outer), by_group(outer.abs()), 0.0, 400, dt).cpu(), "dw")
+    close(gb, by_group(grad).cpu(), product_bound(by_group(grad), by_group(grad.abs()), 0.0, 400, dt).cpu(), "db")
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("c_in,c_out", [(64, 96), (33, 41)])
+def test_wide_outputs_with_the_value_ahead_of_the_activation(c_in, c_out, dtype):
+    """Both outputs in 32 bits from 16-bit rows: linear with a residual, and grouped."""
+    dt, g, n = DT[dtype], gen(c_in), 333
+    x, w, b, r = normal(g, n, c_in, dtype=dt), normal(g, 2, c_in, c_out, dtype=dt, scale=0.2), normal(g, 2, c_out, dtype=dt), normal(g, n, c_out, dtype=torch.float32)
+    for act in ("gelu", "silu"):
+        out, pre = torch.empty(n, c_out, device=DEV), torch.empty(n, c_out, device=DEV)
+        sc.sc_linear_fwd(x.to(DEV), w[0].to(DEV), out, bias=b[0].to(DEV), act=act, residual=r.to(DEV), pre=pre)
+        plain, size = x.double() @ w[0].double() + b[0].double(), x.double().abs() @ w[0].double().abs() + b[0].double().abs()
+        want = act64(plain, act) + r.double()
+        close(out, want, forward_bound(want, plain, size + r.double().abs(), c_in, act, torch.float32), "out")
+        close(pre, plain, forward_bound(plain, plain, size, c_in, "none", torch.float32), "pre")
+        sc.sc_grouped_fwd(x.to(DEV), w.to(DEV), torch.tensor([0, 120, n], dtype=torch.int32, device=DEV), out, bias=b.to(DEV), act=act, pre=pre)
+        for k, m in enumerate((slice(0, 120), slice(120, n))):
+            plain, size = x[m].double() @ w[k].double() + b[k].double(), x[m].double().abs() @ w[k].double().abs() + b[k].double().abs()
+            want = act64(plain, act)
+            close(out[m], want, forward_bound(want, plain, size, c_in, act, torch.float32), "grouped out")
+            close(pre[m], plain, forward_bound(plain, plain, size, c_in, "none", torch.float32), "grouped pre")
 
 
 # ---- what a call may leave out ----------------------------------------------------------------------------------
