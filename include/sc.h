@@ -386,7 +386,7 @@ int sc_linear_fwd(const void* d_x, int64_t ldx, int64_t rows,
 /* Gradients of sc_linear_fwd, all of one dtype: with dpre = dy * act'(pre),
  *   d_dx = dpre W^T [rows][C_in],  d_dweight = x^T dpre [C_in][C_out],  d_dbias = column sums of dpre [C_out]
  * each skipped where NULL (one at least is asked for).  The residual's gradient is dy itself.  dpre of 16-bit layers is rounded
- * once to the rows' type before the products (not with act = SC_ACT_NONE, where it is dy).
+ * once to the rows' type ahead of the products, whose operand it is (not with act = SC_ACT_NONE, where it is dy); d_dbias sums it as it is before that.
  *   d_pre      what the forward call stored; ignored for SC_ACT_NONE
  *   d_x, d_weight may be NULL where d_dweight, d_dx are
  *   d_workspace  workspace_bytes >= sc_linear_workspace_bytes(...), 16-byte aligned; contents undefined afterwards */
@@ -413,7 +413,7 @@ int sc_grouped_fwd(const void* d_x, int64_t ldx, int64_t x_rows, const int32_t* 
 /* Gradients of sc_grouped_fwd: with dpre[p] = dy[grad_rows[p]] * act'(pre[p]) (d_grad_rows NULL: row p),
  *   d_dx[p] = dpre[p] d_weight[g]^T          one row per entry [n][C_in] (not added up over entries with the same row)
  *   d_dweight[g] = sum over the group's p of x[rows[p]]^T dpre[p],  d_dbias[g] = sum of dpre[p]
- * A group without entries gets zeros.  With the rulebook of a convolution (rows = pairs_in, grad_rows = pairs_out, dy the
+ * dpre rounded as in sc_linear_bwd.  Rows of d_dx of entries of no group are left untouched.  A group without entries gets zeros.  With the rulebook of a convolution (rows = pairs_in, grad_rows = pairs_out, dy the
  * gradient of its output rows) d_dweight is the gradient of its weights. */
 size_t sc_grouped_workspace_bytes(int64_t n, int groups, int C_in, int C_out, int dtype);
 int sc_grouped_bwd(const void* d_dy, int64_t lddy, int64_t dy_rows, const int32_t* d_grad_rows,

@@ -3,7 +3,7 @@
 //
 //     FWD   out[p][n] = act(sum_k a[row(p)][k] w[g][k][n] + bias[g][n]) + residual[p][n]     k: C_in,  n: C_out
 //     DX    out[p][n] = sum_k a[row(p)][k] w[g][n][k]                                        k: C_out, n: C_in
-//     DX_ACT  the same with a[row(p)][k] act'(pre[p][k]) in place of a, rounded to its type, which is kept in kept[p][k]
+//     DX_ACT  the same with a[row(p)][k] act'(pre[p][k]) in place of a, rounded to its type, which is kept in kept[p][k]; sums over p before the rounding
 //     DW    out[g][m][n] = sum_p a[row(p)][m] b[row'(p)][n],  bias[g][n] = sum_p b[row'(p)][n]   p: entries of group g
 //
 // A workgroup owns a BM x BN tile of the result and walks the summed axis in steps of 128 bytes (KW times that where KW sets of
@@ -60,6 +60,8 @@ struct Product {
     void* kept;                    // DX_ACT
     int64_t ldk;
     void* out_bias;                // DW
+    float* bias_sums;              // DX_ACT: [bias_units][K], null: not wanted; DW: the same, null: the sums of b's rows instead
+    int bias_log2;                 // DW: 2^bias_log2 entries in a unit
     float* partial;                // DW: [slot][(M + 1) N], null if no group can have two parts
     int64_t slots;                 // ... how many
 };
@@ -522,22 +524,32 @@ struct Loader {
 
 // The rows of DX_ACT: gradient and value ahead of the activation come through registers a step ahead, their product goes to LDS and, by the first of the
 // workgroups with these rows (`keep`), to memory for the weight gradient that follows.
-template <int DT, int LINES, int LINE, int NTH, int STRIDE, bool WHOLE>
+template <int DT, int LINES, int LINE, int NTH, int STRIDE, bool WHOLE, bool SUMS>
 struct GradLoader {
     static constexpr int PASSES = LINES * LINE / NTH, PER = 16 / ELEM<DT>;
+    // SUMS: column sums before the rounding, a wavefront's lines the unit
+    static constexpr int WAVE_LINES = 64 / LINE, UNIT = PASSES * WAVE_LINES;
+    float* sums;                       // of this wavefront's unit, null: none
     const char* grad[PASSES];          // at the next step's chunk
     const char* pre[PASSES];
-    char* kept[PASSES];
+    char* kept;                        // of pass 0; the others' lines follow `kept_pass` bytes apart
+    int64_t kept_pass;
     bool row_ok[PASSES], entry_ok[PASSES];
     uint4 g[PASSES], v[PASSES];
     int depth, act;
     bool keep;
 
-    __device__ __forceinline__ static int line_of(int i) { return (i * NTH + (int)threadIdx.x) / LINE; }
-    __device__ __forceinline__ static int chunk_of(int i) { return (int)threadIdx.x % LINE ^ along_turn<LINE>(line_of(i)); }
-    __device__ __forceinline__ void start(const Product& p, int64_t begin, int64_t stop) {
+    __device__ __forceinline__ static int line_of(int i) { return (int)(threadIdx.x >> 6) * UNIT + i * WAVE_LINES + (int)(threadIdx.x & 63) / LINE; }
+    __device__ __forceinline__ static int chunk_of() { return (int)threadIdx.x % LINE; }
+    __device__ __forceinline__ static uint32_t place_of(int i) { return (line_of(i) * LINE + (chunk_of() ^ along_turn<LINE>(line_of(i)))) * 16; }
+    __device__ __forceinline__ void start(const Product& p, int g, int64_t begin, int64_t stop) {
         depth = p.K;
         act = p.act;
+        if constexpr (SUMS) {
+            static_assert(UNIT == 1 << bias_log2(true, LINES == 128 ? TILE_128_32 : LINES == 32 ? TILE_32_64 : TILE_16_32), "units of the rules");
+            const int64_t mine = begin + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * UNIT;
+            sums = keep && mine < stop ? p.bias_sums + (mine / UNIT + g) * p.K : nullptr;
+        }
 #pragma unroll
         for (int i = 0; i < PASSES; ++i) {
             const int64_t e = begin + line_of(i);
@@ -545,11 +557,12 @@ struct GradLoader {
             const int64_t at = entry_ok[i] ? e : begin;
             const int64_t r = p.a_list != nullptr ? p.a_list[at] : at;
             row_ok[i] = r >= 0 && r < p.a_rows;
-            const int offset = chunk_of(i) * 16;
+            const int offset = chunk_of() * 16;
             grad[i] = (const char*)p.a + (row_ok[i] ? r : 0) * (p.lda * ELEM<DT>) + offset;
             pre[i] = (const char*)p.pre + at * (p.ldp * ELEM<DT>) + offset;
-            kept[i] = (char*)p.kept + at * (p.ldk * ELEM<DT>) + offset;
         }
+        kept_pass = WAVE_LINES * (p.ldk * ELEM<DT>);
+        kept = (char*)p.kept + (begin + line_of(0)) * (p.ldk * ELEM<DT>) + chunk_of() * 16;
     }
     __device__ __forceinline__ static uint4 some(const char* p, int there) {
         uint32_t w[4] = {0, 0, 0, 0};
@@ -564,7 +577,7 @@ struct GradLoader {
     __device__ __forceinline__ void fetch(int s) {
 #pragma unroll
         for (int i = 0; i < PASSES; ++i) {
-            const int there = depth - s * STRIDE - chunk_of(i) * PER;
+            const int there = depth - s * STRIDE - chunk_of() * PER;
             g[i] = v[i] = make_uint4(0, 0, 0, 0);
             if (there >= PER || (WHOLE && there > 0)) {
                 if (row_ok[i]) g[i] = load_chunk(grad[i]);
@@ -577,12 +590,42 @@ struct GradLoader {
             pre[i] += STRIDE * ELEM<DT>;
         }
     }
+    // The sums of a wavefront's lines, of which lanes LINE apart have eight columns each: for 8 and 16 lanes a product with ones adds what is 16 lanes apart.
+    __device__ __forceinline__ void write_sums(int s, const float (&sum)[8]) const {
+        const int lane = threadIdx.x & 63, row = lane >> 4;
+        const int col = s * STRIDE + chunk_of() * PER;
+        float out[LINE / 8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float v;
+            if constexpr (LINE == 32) {
+                v = sum[j] + __shfl_xor(sum[j], 32);
+                if (j / 4 == lane >> 5) out[j % 4] = v;
+            } else {
+                v = __builtin_amdgcn_mfma_f32_16x16x4f32(1.f, sum[j], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0)[0];
+                if constexpr (LINE == 8) {                   // and the other eight of sixteen
+                    v += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x128, 0xf, 0xf, true));
+                    if (lane >> 3 == j) out[0] = v;
+                } else if (row == j % 4) {
+                    out[j / 4] = v;
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int k = 0; k < LINE / 8; ++k) {
+            const int c = col + (LINE == 32 ? 4 * (lane >> 5) + k : LINE == 16 ? 4 * k + row : lane >> 3);
+            if (sums != nullptr && c < depth) sums[c] = out[k];
+        }
+    }
     __device__ __forceinline__ void finish(int s, uint32_t lds) {
+        float sum[8];
 #pragma unroll
         for (int i = 0; i < PASSES; ++i) {
-            const int there = depth - s * STRIDE - chunk_of(i) * PER;
+            const int there = depth - s * STRIDE - chunk_of() * PER;
             const uint32_t gw[4] = {g[i].x, g[i].y, g[i].z, g[i].w}, vw[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
             uint32_t w[4];
+            float d32[8];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if constexpr (DT == SC_F32) {
@@ -591,34 +634,46 @@ struct GradLoader {
                     const float lo = to_float<DT>(gw[j] & 0xffffu) * slope<DT>(to_float<DT>(vw[j] & 0xffffu), act);
                     const float hi = to_float<DT>(gw[j] >> 16) * slope<DT>(to_float<DT>(vw[j] >> 16), act);
                     w[j] = round2<DT>(lo, hi);
+                    d32[2 * j] = lo;
+                    d32[2 * j + 1] = hi;
                 }
             }
             // no row, no channel: zeros, whatever the value ahead of the activation
             const bool some_of_it = row_ok[i] && there > 0;
             const uint4 d = some_of_it ? make_uint4(w[0], w[1], w[2], w[3]) : make_uint4(0, 0, 0, 0);
-            *(__attribute__((address_space(3))) u32x4*)(lds + (i * NTH + threadIdx.x) * 16) = u32x4{d.x, d.y, d.z, d.w};
+            if constexpr (SUMS) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float mine = some_of_it && entry_ok[i] ? d32[j] : 0.f;
+                    sum[j] = i == 0 ? mine : sum[j] + mine;
+                }
+                if (i == PASSES - 1) write_sums(s, sum);
+                __builtin_amdgcn_sched_barrier(0);         // one pass at a time: registers for four wavefronts
+            }
+            *(__attribute__((address_space(3))) u32x4*)(lds + place_of(i)) = u32x4{d.x, d.y, d.z, d.w};
             if (keep && entry_ok[i] && there > 0) {
+                char* const to = kept + i * kept_pass;
                 if (WHOLE || there >= PER) {
-                    store_chunk(kept[i], d);
+                    store_chunk(to, d);
                 } else {
                     const uint32_t dw[4] = {d.x, d.y, d.z, d.w};
 #pragma unroll
                     for (int j = 0; j < PER; ++j)
                         if (j < there) {
-                            if constexpr (DT == SC_F32) reinterpret_cast<uint32_t*>(kept[i])[j] = dw[j];
-                            else reinterpret_cast<uint16_t*>(kept[i])[j] = (uint16_t)(dw[j / 2] >> (16 * (j & 1)));
+                            if constexpr (DT == SC_F32) reinterpret_cast<uint32_t*>(to)[j] = dw[j];
+                            else reinterpret_cast<uint16_t*>(to)[j] = (uint16_t)(dw[j / 2] >> (16 * (j & 1)));
                         }
                 }
             }
-            kept[i] += STRIDE * ELEM<DT>;
         }
+        kept += STRIDE * ELEM<DT>;
     }
 };
 
 // ---- the kernel -----------------------------------------------------------------------------------------
 // WM x WN wavefronts share a tile, KW sets of them the summed axis, of which a set takes SB bytes a step.  WHOLE: the operands' lines are whole chunks
 // of 16 bytes, at any alignment of their elements (what the others need is in registers through the whole loop: weight gradients 36 us or 29).
-// RESIDUAL: there may be one; what is held of it costs the others wavefronts (128 x 128: 174 registers or 123).
+// RESIDUAL: there may be one; what is held of it costs the others wavefronts (128 x 128: 174 registers or 123).  DX_ACT: a bias wants the sums of the gradient's columns.
 template <int DT, int MODE, int BM_, int BN_, int WM_, int WN_, int KW_, int SB_>
 struct ProductShape {
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, KW = KW_, SB = SB_;
@@ -628,12 +683,13 @@ struct ProductShape {
     static constexpr int A_LINES = A_ACROSS ? STEP * KW : BM, A_LINE = A_ACROSS ? BM * ELEM<DT> / 16 : SB / 16 * KW;
     static constexpr int B_LINES = B_ACROSS ? STEP * KW : BN, B_LINE = B_ACROSS ? BN * ELEM<DT> / 16 : SB / 16 * KW;
     static constexpr int A_CHUNKS = A_LINES * A_LINE, B_CHUNKS = B_LINES * B_LINE;
+    static constexpr int SHARES = MODE == PRODUCT_DW ? NTH * 4 : 0;       // of a bias' sums, a float a thread
     static constexpr int BUFFER = (A_CHUNKS + B_CHUNKS) * 16, RINGS = MODE == PRODUCT_DW ? 4 * RING : 0;
     static constexpr int SUMS = (KW - 1) * WM * WN * TM * TN * 64 * 16;  // what the sets hand over in the end
     static constexpr int PIECES = WM * WN * 16 * (TN * 16 + 4) * 4;      // results on their way out
     static constexpr int lds(int64_t steps) {
         const int buffers = RINGS + (steps > 1 ? 2 : 1) * BUFFER, end = SUMS > PIECES ? SUMS : PIECES;
-        return buffers > end ? buffers : end;
+        return SHARES + (buffers > end ? buffers : end);
     }
 };
 
@@ -648,7 +704,8 @@ __global__ void __launch_bounds__(64 * WM * WN * KW, 2)
 k_product(const Product p) {
     using S = ProductShape<DT, MODE, BM, BN, WM, WN, KW, SB>;
     constexpr int NTH = S::NTH, TM = S::TM, TN = S::TN;
-    extern __shared__ __align__(16) uint4 product_lds[];
+    extern __shared__ __align__(16) uint4 all_lds[];
+    uint4* const product_lds = all_lds + S::SHARES / 16;
 
     // runs of consecutive tiles, which share rows, go to one XCD; those that do not exist after all are the last of every XCD
     const uint32_t block = blockIdx.y * gridDim.x + blockIdx.x, turn = block / NUM_XCD, run = (uint32_t)p.run;
@@ -681,7 +738,7 @@ k_product(const Product p) {
 
     constexpr int STRIDE = S::STEP * KW;
     Loader<DT, S::A_ACROSS, S::A_LINES, S::A_LINE, NTH, STRIDE, WHOLE> la;
-    GradLoader<DT, MODE == PRODUCT_DX_ACT ? S::A_LINES : 0, S::A_LINE, NTH, STRIDE, WHOLE> lg;
+    GradLoader<DT, MODE == PRODUCT_DX_ACT ? S::A_LINES : 0, S::A_LINE, NTH, STRIDE, WHOLE, MODE == PRODUCT_DX_ACT && RESIDUAL> lg;
     Loader<DT, S::B_ACROSS, S::B_LINES, S::B_LINE, NTH, STRIDE, WHOLE> lb;
     la.base = (const char*)p.a;
     la.ld = (uint32_t)(p.lda * ELEM<DT>);
@@ -690,7 +747,7 @@ k_product(const Product p) {
     int64_t depth;                                      // of the summed axis
     int32_t row_of[TM];                                 // rows of a that the lane's results are of
     if constexpr (MODE == PRODUCT_DW) {
-        depth = part.last - part.first;
+        depth = p.M == 0 && p.bias_sums != nullptr ? 0 : part.last - part.first;
         la.list = p.a_list;
         la.ring = rings;
         la.first = part.first;
@@ -724,7 +781,7 @@ k_product(const Product p) {
         if (depth > 0) {
             if constexpr (MODE == PRODUCT_DX_ACT) {
                 lg.keep = n_tile == 0;
-                lg.start(p, part.first, part.last);
+                lg.start(p, g, part.first, part.last);
             } else {
                 la.list = nullptr;
                 la.end = p.K;
@@ -779,7 +836,7 @@ k_product(const Product p) {
         for (int tn = 0; tn < TN; ++tn) acc[tm][tn] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int tn = 0; tn < TN; ++tn) ones_sum[tn] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const bool sums = MODE == PRODUCT_DW && p.out_bias != nullptr && m_tile == 0 && wm == 0;
+    const bool sums = MODE == PRODUCT_DW && p.out_bias != nullptr && p.bias_sums == nullptr && m_tile == 0 && wm == 0;
     const uint32_t one = DT == SC_F32 ? 0x3f800000u : DT == SC_F16 ? 0x3c003c00u : 0x3f803f80u;
 
     if constexpr (MODE == PRODUCT_DW) {
@@ -792,6 +849,30 @@ k_product(const Product p) {
     if (steps > 0) {
         fetch(0);
         finish(0);
+    }
+    // A bias' sums that are there already, by all wavefronts: every so many'th unit of a column, sixteen asked for at a time.
+    const bool ready_sums = MODE == PRODUCT_DW && p.out_bias != nullptr && p.bias_sums != nullptr && m_tile == 0;
+    if constexpr (MODE == PRODUCT_DW) {
+        if (ready_sums) {
+            constexpr int SHARES = NTH / BN;
+            const int col = n0 + (int)threadIdx.x % BN;
+            float share = 0.f;
+            if (col < p.N) {
+                const float* src = p.bias_sums + ((part.first >> p.bias_log2) + g) * p.N + col;
+                const int count = (int)((part.last - part.first + (1 << p.bias_log2) - 1) >> p.bias_log2);
+                for (int u = (int)threadIdx.x / BN; u < count; u += 16 * SHARES) {
+                    float term[16];
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        const uint32_t at = (uint32_t)(u + k * SHARES < count ? u + k * SHARES : u);
+                        term[k] = src[(uint64_t)at * (uint32_t)p.N];
+                    }
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) share += u + k * SHARES < count ? term[k] : 0.f;
+                }
+            }
+            reinterpret_cast<float*>(all_lds)[threadIdx.x] = share;
+        }
     }
     for (int s = 0; s < steps; ++s) {
         if constexpr (MODE != PRODUCT_DX_ACT) __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0): the step's chunks are in LDS
@@ -939,12 +1020,21 @@ k_product(const Product p) {
     }
     // The columns that are left: 16 rows at a time through LDS, a wavefront's own piece of it, up to eight columns a lane; one copy of the code.
     const int rest = p.N - col_wave - whole_cols < COLS - whole_cols ? p.N - col_wave - whole_cols : COLS - whole_cols;
-    const bool column_sums = MODE == PRODUCT_DW && sums;
     if constexpr (KW == 1 || WM * WN > 1) lds_barrier();     // the operands, or the sums, have been read by all
-    if (rest <= 0 && !column_sums) return;
+    if constexpr (MODE == PRODUCT_DW) {
+        const int col = n0 + (int)threadIdx.x;
+        if (ready_sums && threadIdx.x < BN && col < p.N) {       // their shares, in order
+            float total = 0.f;
+#pragma unroll
+            for (int k = 0; k < NTH / BN; ++k) total += reinterpret_cast<const float*>(all_lds)[k * BN + threadIdx.x];
+            if (to_partial) p.partial[(slot_row + p.M) * p.N + col] = total;
+            else store_elem<DT>(p.out_bias, (int64_t)g * p.N + col, total);
+        }
+    }
+    if (rest <= 0 && !sums) return;
     constexpr int PITCH = COLS + 4;
     float* const piece = reinterpret_cast<float*>(product_lds) + (wave % (WM * WN)) * (16 * PITCH);
-    if (column_sums) {
+    if (sums) {
         if (i == 0) {
 #pragma unroll
             for (int tn = 0; tn < TN; ++tn)
@@ -1056,6 +1146,9 @@ int start_product(const Product& p, hipStream_t s) {
 }
 template <int DT, int MODE, int BM, int BN, int WM, int WN, int KW, int SB = 128, bool TWO = false>
 int run_product(const Product& p, hipStream_t s) {
+    if constexpr (MODE == PRODUCT_DX_ACT && DT != SC_F32) {
+        if (p.bias_sums != nullptr) return start_product<DT, MODE, BM, BN, WM, WN, KW, SB, true>(p, s);
+    }
     if constexpr (MODE != PRODUCT_FWD) return start_product<DT, MODE, BM, BN, WM, WN, KW, SB, false>(p, s);
     else if (TWO && p.residual == nullptr) return start_product<DT, MODE, BM, BN, WM, WN, KW, SB, !TWO>(p, s);
     else return start_product<DT, MODE, BM, BN, WM, WN, KW, SB, true>(p, s);

@@ -246,6 +246,19 @@ constexpr int64_t act_grad_rows(int64_t rows, int64_t chunks) {
     return spread < one ? one : spread < eight ? spread : eight > one ? eight : one;
 }
 
+// A bias' gradient in 16-bit layers: the gradient ahead of the activation is summed before it is rounded, by units of 2^bias_log2 entries of a group.  A group's first unit
+// lies at its first entry / 2^bias_log2 + its number, which keeps any two apart.  A part of a weight gradient, whose workgroup adds its units up, is a whole number of them.
+// Inside the product with the weights a unit is what one wavefront of the tile loads.
+constexpr int bias_log2(bool in_product, RowTile tile) { return !in_product ? 6 : tile == TILE_128_32 ? 5 : 2; }
+constexpr int64_t bias_units(int64_t entries, int64_t groups, int log2) { return (entries >> log2) + groups; }
+// Channels, by eights, that a workgroup of 256 threads sums of a unit in a pass of its own: 32, or as few as make 1024 workgroups, down to 4
+// (us of the pass, bf16, 4 / 8 / 16 / 32: 64 rows of 512 5.2 / 6.8 / 9.3 / 15.1, 8192 of 512 12.0 / 9.8 / 12.2 / 17.2, 17007 of 512 22.5 / 17.1 / 16.3 / 20.2, 110 k of 512 105 / 75.3 / 68.6 / 68.3).
+constexpr int64_t sum_columns(int64_t units, int64_t chunks) {
+    int64_t wide = 32;
+    while (wide > 4 && units * ((chunks + wide - 1) / wide) < 1024) wide /= 2;
+    return chunks < wide ? chunks : wide;
+}
+
 // The activation's gradient inside the product with the weights, or a pass of its own ahead of it.  Inside, one tile of columns or few rows: what is read is read
 // once and a launch is spared; otherwise the slopes keep the matrix cores waiting, which a pass over memory hides (us of the whole backward pass, bf16 GELU, apart / inside:
 // 300 k x 32 -> 128 95 / 82, 53 k x 64 -> 256 45.5 / 47.7, 110 k x 128 -> 512 140 / 157, 8 k x 128 -> 128 SiLU 18.8 / 16.8, 1 k x 64 -> 256 14.9 / 14.1, 64 x 512 -> 512 12.1 / 13.8).

@@ -251,6 +251,71 @@ def test_wide_outputs_with_the_value_ahead_of_the_activation(c_in, c_out, dtype)
             close(pre[m], plain, forward_bound(plain, plain, size, c_in, "none", torch.float32), "grouped pre")
 
 
+# starts, channels: the slopes inside the product with the weights in each of its tiles (few rows, thousands, one tile of columns), in whole chunks and not, and ahead of it
+BIASES = [([0, 130], 24, 40), ([0, 4001], 128, 64), ([0, 70000], 24, 72), ([0, 70001], 31, 41), ([0, 5000], 200, 264), ([0, 40000], 96, 513), ([0, 300], 512, 9),
+          ([0, 1, 1, 66, 131, 400, 401], 48, 40), ([2, 700, 701, 3801], 130, 72), ([0, 33000, 33000, 33129, 70000], 30, 136), ([0] * 70 + [900, 900, 2400], 40, 1030)]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("starts,c_in,c_out", BIASES)
+def test_bias_gradient_of_values_before_their_rounding(starts, c_in, c_out, dtype):
+    """A group's last gradient takes back the sum of the others, which few rows have: what is left is as small as the rounding of the terms to 16 bits, and the bias'
+    gradient is within the error of a sum in 32 bits of it."""
+    dt, groups, n, g = DT[dtype], len(starts) - 1, starts[-1] + 3, gen(starts[-1] + c_out)
+    print(f"bias {starts[-1]} in {groups} {c_in} {c_out} {dtype}", flush=True)
+    pre, grad, taken = normal(g, n, c_out, dtype=dt), torch.zeros(n, c_out, dtype=dt), torch.randperm(n, generator=g).to(torch.int32)
+    want, bound = (torch.zeros(groups, c_out, dtype=torch.float64) for _ in range(2))
+    for k in range(groups):
+        lo, hi = starts[k], starts[k + 1]
+        if hi - lo < 2:
+            continue
+        some = lo + torch.randperm(hi - 1 - lo, generator=g)[:20]
+        grad[some] = normal(g, len(some), c_out, dtype=dt)
+        d = grad[some].double() * slope64(pre[some].double(), "silu")
+        grad[hi - 1], pre[hi - 1] = -d.sum(0).to(dt), 40.0     # where the slope is one
+        want[k] = d.sum(0) + grad[hi - 1].double()
+        size = d.abs().sum(0) + grad[hi - 1].double().abs()
+        off = (len(some) + 9) * 2.0 ** -23 * size + (ACT_ERROR * grad[some].double().abs() * (1 + pre[some].double().abs())).sum(0)
+        bound[k] = off + UNIT[dt] * (want[k].abs() + off) + TINY[dt]
+    x, w = normal(g, n, c_in, dtype=dt).to(DEV), normal(g, groups, c_in, c_out, dtype=dt, scale=0.1).to(DEV)
+    d_grad, d_pre, d_starts = grad.to(DEV), pre.to(DEV), torch.tensor(starts, dtype=torch.int32, device=DEV)
+    listed = torch.empty_like(d_grad)
+    listed[taken.long()] = d_grad                               # entry p's is row taken[p]
+    size = sc.sc_grouped_workspace_bytes(n, groups, c_in, c_out, dt)
+    ws = torch.full((size + 4096,), 77, dtype=torch.uint8, device=DEV)
+    gx, gw = torch.empty(n, c_in, dtype=dt, device=DEV), torch.empty(groups, c_in, c_out, dtype=dt, device=DEV)
+    for rows, kw in ((d_grad, {}), (listed, dict(grad_rows=taken.to(DEV)))):
+        for wanted in (dict(grad_x=gx, grad_weight=gw), dict(grad_x=gx), dict(grad_weight=gw), {}):
+            gb = torch.full((groups, c_out), 7.0, dtype=dt, device=DEV)
+            sc.sc_grouped_bwd(rows, x, w, d_starts, grad_bias=gb, pre=d_pre, act="silu", workspace=ws[:size], **kw, **wanted)
+            close(gb, want, bound, f"grouped {sorted(wanted)} {sorted(kw)}")
+    assert bool((ws[size:] == 77).all())
+    if groups == 1:
+        m = slice(starts[0], starts[1])
+        size = sc.sc_linear_workspace_bytes(starts[1], c_in, c_out, dt)
+        ws = torch.full((size + 4096,), 77, dtype=torch.uint8, device=DEV)
+        for wanted in (dict(grad_x=gx[m], grad_weight=gw[0]), dict(grad_x=gx[m]), dict(grad_weight=gw[0]), {}):
+            gb = torch.full((c_out,), 7.0, dtype=dt, device=DEV)
+            sc.sc_linear_bwd(d_grad[m], x[m], w[0], grad_bias=gb, pre=d_pre[m], act="silu", workspace=ws[:size], **wanted)
+            close(gb, want[0], bound[0], f"linear {sorted(wanted)}")
+        assert bool((ws[size:] == 77).all())
+
+
+def test_bias_gradient_of_starts_that_do_not_ascend():
+    """Wrong starts give wrong sums, but nothing outside the arrays is written."""
+    for n, c_in, c_out in ((2000, 32, 40), (70000, 24, 40), (3000, 160, 40)):
+        dt, groups = torch.float16, 5
+        x, grad, w = torch.ones(n, c_in, dtype=dt, device=DEV), torch.ones(n, c_out, dtype=dt, device=DEV), torch.ones(groups, c_in, c_out, dtype=dt, device=DEV)
+        size = sc.sc_grouped_workspace_bytes(n, groups, c_in, c_out, dt)
+        ws, gx = torch.full((size + 4096,), 77, dtype=torch.uint8, device=DEV), torch.full((n + 64, c_in), 7.0, dtype=dt, device=DEV)
+        gw, gb = torch.zeros(groups + 1, c_in, c_out, dtype=dt, device=DEV), torch.zeros(groups + 1, c_out, dtype=dt, device=DEV)
+        for starts in ([0, n, 0, n, 0, n], [-5, n + 1000, 1 << 30, -(1 << 31), 7, 100000], [n, n // 2, n // 3, n // 4, 0, 0]):
+            print(f"starts {n} {starts}", flush=True)
+            sc.sc_grouped_bwd(grad, x, w, torch.tensor(starts, dtype=torch.int32, device=DEV), gx[:n], gw[:groups], gb[:groups], pre=grad, act="gelu", workspace=ws[:size])
+            torch.cuda.synchronize()
+            assert bool((ws[size:] == 77).all()) and bool((gx[n:] == 7.0).all()) and not gw[groups].any() and not gb[groups].any()
+
+
 # ---- what a call may leave out ----------------------------------------------------------------------------------
 @EVERY
 def test_rows_gradient_without_the_rows(dtype):
