@@ -32,47 +32,79 @@ k_act_grad(const void* __restrict__ grad, int64_t ldg, int64_t grad_rows, const 
 
 // The same by units of a group's entries (bias_log2), with the sums of the unit's gradients before the rounding, which a bias takes: the sums of rounded values are off by half
 // as much again.  A thread keeps to its eight channels, `wide` threads side by side, and walks the unit's rows; their sums meet in LDS, in a fixed order.  110545 x 512 bf16
-// GELU 63 us (62 without sums), 64 x 512 5.1 (3.9).
+// GELU 63 us (60 without sums; one row at a time 66), 64 x 512 5.5 (4.0).
 template <int DT>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(512)
 k_act_grad_sums(const void* __restrict__ grad, int64_t ldg, int64_t grad_rows, const int32_t* __restrict__ list, const void* __restrict__ pre, int64_t ldp, int act,
                 void* __restrict__ out, int64_t ldo, const int32_t* __restrict__ starts, int groups, int64_t n, int N, int wide, int col_blocks, float* __restrict__ sums) {
     constexpr int ROWS = 1 << bias_log2(false, TILE_16_32);
-    __shared__ float lds[256 * 8];
+    extern __shared__ __align__(16) float row_sums[];  // eight a thread
     const uint32_t block = blockIdx.y * gridDim.x + blockIdx.x, unit = block / (uint32_t)col_blocks;
     const Part part = find_part<false>(starts, groups, n, ROWS, unit);
     if (part.g < 0) return;                            // the whole workgroup
-    const int first_col = (int)(block - unit * (uint32_t)col_blocks) * wide * 8, width = wide * 8, step = 256 / wide;
-    const int first_row = (int)threadIdx.x / wide, col = first_col + ((int)threadIdx.x - first_row * wide) * 8, there = N - col < 8 ? N - col : 8;
+    const int threads = (int)blockDim.x, step = threads / wide, width = wide * 8;
+    const int first_col = (int)(block - unit * (uint32_t)col_blocks) * width, first_row = (int)threadIdx.x / wide;
+    int col = first_col + ((int)threadIdx.x - first_row * wide) * 8, there = N - col < 8 ? N - col : 8;
+    // the last chunk reaches back over the one before it: the same values, stored by both and summed by one
+    const bool on = there > 0 && first_row < step;
+    const int twice = on && there < 8 && N >= 8 ? 8 - there : 0;
+    col -= twice;
+    there += twice;
     float sum[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) sum[j] = 0.f;
-    if (there > 0 && first_row < step) {
-        for (int64_t e = part.first + first_row; e < part.last; e += step) {
-            int64_t row = e;
-            if (list != nullptr) row = list[e];
+    if (on) {
+        int64_t e = part.first + first_row;
+        const auto row_of = [&](int64_t at) __attribute__((always_inline)) {
+            const int64_t row = list != nullptr ? list[at] : at;
+            return row < grad_rows ? row : -1;
+        };
+        for (; N >= 8 && e + step < part.last; e += 2 * step) {          // two rows on their way at a time
+            Eight<DT> g[2], x[2];
+            int64_t row[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                row[k] = row_of(e + k * step);
+                g[k].load(grad, (row[k] >= 0 ? row[k] : 0) * ldg + col);
+                x[k].load(pre, (e + k * step) * ldp + col);
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                float a[8], v[8];
+                g[k].to_floats(a);
+                x[k].to_floats(v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    v[j] = row[k] >= 0 ? a[j] * slope<DT>(v[j], act) : 0.f;
+                    sum[j] += v[j];
+                }
+                store8<DT>(out, (e + k * step) * ldo + col, 8, v);
+            }
+        }
+        for (; e < part.last; e += step) {
+            const int64_t row = row_of(e);
             float g[8], v[8];
-            const bool ok = row >= 0 && row < grad_rows;
-            if (ok) load8<DT>(grad, row * ldg + col, there, g);
+            if (row >= 0) load8<DT>(grad, row * ldg + col, there, g);
             load8<DT>(pre, e * ldp + col, there, v);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                v[j] = ok ? g[j] * slope<DT>(v[j], act) : 0.f;
+                v[j] = row >= 0 ? g[j] * slope<DT>(v[j], act) : 0.f;
                 sum[j] += v[j];
             }
             store8<DT>(out, e * ldo + col, there, v);
         }
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) lds[threadIdx.x * 8 + j] = sum[j];
+    for (int j = 0; j < 8; ++j)
+        if (j >= twice) row_sums[threadIdx.x * 8 + j - twice] = sum[j];
     __syncthreads();
     // of every column, shares of the rows by as many threads as there are for it, then the shares in order
-    const int shares = width < 256 ? 256 / width : 1, share = shares == 1 ? 0 : (int)threadIdx.x / width;
+    const int shares = width < threads ? threads / width : 1, share = shares == 1 ? 0 : (int)threadIdx.x / width;
     float* const at = sums + (part.first / ROWS + part.g) * N + first_col;
-    for (int j = (int)threadIdx.x - share * width; j < width && share < shares; j += 256) {
+    for (int j = (int)threadIdx.x - share * width; j < width && share < shares; j += threads) {
         float total = 0.f;
 #pragma unroll 8
-        for (int r = share; r < step; r += shares) total += lds[r * width + j];
+        for (int r = share; r < step; r += shares) total += row_sums[r * width + j];
         if (shares == 1) {
             if (first_col + j < N) at[j] = total;
         } else {
@@ -81,11 +113,11 @@ k_act_grad_sums(const void* __restrict__ grad, int64_t ldg, int64_t grad_rows, c
     }
     if (shares == 1) return;
     __syncthreads();
-    if (share < shares) lds[threadIdx.x] = sum[0];
+    if (share < shares) row_sums[threadIdx.x] = sum[0];
     __syncthreads();
     if ((int)threadIdx.x >= width || first_col + (int)threadIdx.x >= N) return;
     float total = 0.f;
-    for (int k = 0; k < shares; ++k) total += lds[k * width + threadIdx.x];
+    for (int k = 0; k < shares; ++k) total += row_sums[k * width + threadIdx.x];
     at[threadIdx.x] = total;
 }
 
@@ -280,9 +312,10 @@ int backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const Ent
         const int64_t chunks = (C_out + 7) / 8, most = e.starts == nullptr ? bias_units(e.n - 1, 1, log2) : bias_units(e.n, e.groups < e.n ? e.groups : e.n, log2);
         const int64_t wide = sum_columns(most, chunks), col_blocks = (chunks + wide - 1) / wide, blocks = most * col_blocks;
         if (blocks > INT32_MAX) return SC_EINVAL;
+        const unsigned threads = (unsigned)sum_threads(wide);
         const dim3 grid((unsigned)grid_columns(blocks), (unsigned)grid_rows(blocks));
 #define SC_ACT_GRAD(DT)                                                                                                                                       \
-    SC_LAUNCH(KID_ACT_GRAD, k_act_grad_sums<DT>, grid, dim3(256), 0, s, dy, lddy, e.grad_n, e.grad_rows, pre, ldp, act, workspace, pitch, e.starts, e.groups, \
+    SC_LAUNCH(KID_ACT_GRAD, k_act_grad_sums<DT>, grid, dim3(threads), threads * 8 * sizeof(float), s, dy, lddy, e.grad_n, e.grad_rows, pre, ldp, act, workspace, pitch, e.starts, e.groups, \
               e.n, C_out, (int)wide, (int)col_blocks, bias_terms)
         if (dtype == SC_F16) SC_ACT_GRAD(SC_F16);
         else SC_ACT_GRAD(SC_BF16);

@@ -251,12 +251,18 @@ constexpr int64_t act_grad_rows(int64_t rows, int64_t chunks) {
 // Inside the product with the weights a unit is what one wavefront of the tile loads.
 constexpr int bias_log2(bool in_product, RowTile tile) { return !in_product ? 6 : tile == TILE_128_32 ? 5 : 2; }
 constexpr int64_t bias_units(int64_t entries, int64_t groups, int log2) { return (entries >> log2) + groups; }
-// Channels, by eights, that a workgroup of 256 threads sums of a unit in a pass of its own: 32, or as few as make 1024 workgroups, down to 4
-// (us of the pass, bf16, 4 / 8 / 16 / 32: 64 rows of 512 5.2 / 6.8 / 9.3 / 15.1, 8192 of 512 12.0 / 9.8 / 12.2 / 17.2, 17007 of 512 22.5 / 17.1 / 16.3 / 20.2, 110 k of 512 105 / 75.3 / 68.6 / 68.3).
+// Channels, by eights, that a workgroup sums of a unit in a pass of its own: 32, or as few as make 512 workgroups, down to 4
+// (us of the pass, bf16, 4 / 8 / 16 / 32: 64 rows of 512 5.5 / 5.4 / 6.0 / 8.3, 8192 of 512 12.3 / 11.6 / 9.6 / 10.8, 17007 of 512 21.8 / 18.4 / 18.0 / 17.4, 53 k of 512 in 8 groups
+// 49.3 / 47.9 / 35.9 / 31.9, 110 k of 512 102 / 88.6 / 62.4 / 63.2).
 constexpr int64_t sum_columns(int64_t units, int64_t chunks) {
     int64_t wide = 32;
-    while (wide > 4 && units * ((chunks + wide - 1) / wide) < 1024) wide /= 2;
+    while (wide > 4 && units * ((chunks + wide - 1) / wide) < 512) wide /= 2;
     return chunks < wide ? chunks : wide;
+}
+// Threads of such a workgroup: its 64 rows in as few turns as 512 threads take, the turns of a size (256 threads 110 k of 512 65, 16384 of 2048 in 16 groups 38.2 us; 512 63 and 37.4).
+constexpr int64_t sum_threads(int64_t wide) {
+    const int64_t most = 512 / wide, turns = (64 + most - 1) / most, rows = (64 + turns - 1) / turns;
+    return (rows * wide + 63) / 64 * 64;
 }
 
 // The activation's gradient inside the product with the weights, or a pass of its own ahead of it.  Inside, one tile of columns or few rows: what is read is read

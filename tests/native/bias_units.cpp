@@ -9,7 +9,8 @@
 using namespace sc;
 
 static_assert(bias_log2(true, TILE_16_32) == 2 && bias_log2(true, TILE_32_64) == 2 && bias_log2(true, TILE_128_32) == 5 && bias_log2(false, TILE_16_32) == 6, "units");
-static_assert(sum_columns(1, 64) == 4 && sum_columns(128, 64) == 8 && sum_columns(266, 64) == 16 && sum_columns(1728, 64) == 32 && sum_columns(5000, 3) == 3, "columns");
+static_assert(sum_columns(1, 64) == 4 && sum_columns(47, 128) == 8 && sum_columns(128, 64) == 16 && sum_columns(266, 64) == 32 && sum_columns(5000, 3) == 3, "columns");
+static_assert(sum_threads(4) == 256 && sum_threads(8) == 512 && sum_threads(32) == 512 && sum_threads(20) == 448 && sum_threads(24) == 384 && sum_threads(3) == 192 && sum_threads(1) == 64, "threads");
 
 int main() {
     std::mt19937_64 rng(2);
@@ -35,7 +36,7 @@ int main() {
             return 1;
         }
         const int64_t chunks = 1 + rng() % 300, wide = sum_columns(1 + rng() % 3000, chunks);
-        if (wide < 1 || wide > 32 || wide > chunks) {
+        if (wide < 1 || wide > 32 || wide > chunks || sum_threads(wide) > 512 || sum_threads(wide) < wide) {
             std::printf("%lld of %lld chunks\n", (long long)wide, (long long)chunks);
             return 1;
         }

@@ -252,7 +252,7 @@ def test_wide_outputs_with_the_value_ahead_of_the_activation(c_in, c_out, dtype)
 
 
 # starts, channels: the slopes inside the product with the weights in each of its tiles (few rows, thousands, one tile of columns), in whole chunks and not, and ahead of it
-BIASES = [([0, 130], 24, 40), ([0, 4001], 128, 64), ([0, 70000], 24, 72), ([0, 70001], 31, 41), ([0, 5000], 200, 264), ([0, 40000], 96, 513), ([0, 300], 512, 9),
+BIASES = [([0, 130], 24, 40), ([0, 4001], 128, 64), ([0, 70000], 24, 72), ([0, 70001], 31, 41), ([0, 5000], 200, 264), ([0, 40000], 96, 513), ([0, 300], 512, 9), ([0, 40000], 200, 192), ([0, 3000], 160, 7),
           ([0, 1, 1, 66, 131, 400, 401], 48, 40), ([2, 700, 701, 3801], 130, 72), ([0, 33000, 33000, 33129, 70000], 30, 136), ([0] * 70 + [900, 900, 2400], 40, 1030)]
 
 
