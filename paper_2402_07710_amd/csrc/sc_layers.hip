@@ -94,9 +94,14 @@ k_act_grad_sums(const void* __restrict__ grad, int64_t ldg, int64_t grad_rows, c
             store8<DT>(out, e * ldo + col, there, v);
         }
     }
+    if (twice == 0) {
+        reinterpret_cast<float4*>(row_sums)[threadIdx.x * 2] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+        reinterpret_cast<float4*>(row_sums)[threadIdx.x * 2 + 1] = make_float4(sum[4], sum[5], sum[6], sum[7]);
+    } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (j >= twice) row_sums[threadIdx.x * 8 + j - twice] = sum[j];
+        for (int j = 1; j < 8; ++j)
+            if (j >= twice) row_sums[threadIdx.x * 8 + j - twice] = sum[j];
+    }
     __syncthreads();
     // of every column, shares of the rows by as many threads as there are for it, then the shares in order
     const int shares = width < threads ? threads / width : 1, share = shares == 1 ? 0 : (int)threadIdx.x / width;
