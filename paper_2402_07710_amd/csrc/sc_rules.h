@@ -180,6 +180,7 @@ constexpr int64_t grid_rows(int64_t groups) { return (groups + GRID_COLUMNS - 1)
 // Tile of the result that a workgroup owns, rows by columns; DEEP and the two smallest: two, four or eight sets of wavefronts share the summed axis, SHORT: steps
 // of 64 bytes and not 128, four workgroups on a CU.  LARGE: 128 x 256 forward, 256 x 256 for the input's gradient.
 enum RowTile { TILE_16_32, TILE_16_32_DEEP, TILE_32_64, TILE_64_64, TILE_64_64_DEEP, TILE_128_32, TILE_128_64, TILE_128_128, TILE_128_128_SHORT, TILE_LARGE };
+// (The lines were measured in bf16; f32 takes the same ones, but for LARGE, though its matrix cores are the bound from some hundred channels on and a padded tile costs it time.)
 // By the 16 x 32 tiles that there would be: few of them, and small tiles with short ways through the summed axis fill the chip; many, and what counts is how often the
 // operands are read.  `groups` 0: a linear layer.  us of the call, bf16, no epilogue, rows x summed x columns, 256 CUs, on either side of each line:
 //   16 x 32, eight sets / four     1 x 1024 x 4096 4.2 / 4.4, 1 x 4096 x 256 7.0 / 8.1, 64 x 2048 x 2048 (256 tiles) 6.9 / 7.1, 128 x 2048 x 2048 12.7 / 8.7, 1024 x 256 x 256 4.4 / 4.0
@@ -265,7 +266,7 @@ constexpr int64_t sum_threads(int64_t wide) {
     return (rows * wide + 63) / 64 * 64;
 }
 
-// The activation's gradient inside the product with the weights, or a pass of its own ahead of it.  Inside, one tile of columns or few rows: what is read is read
+// The activation's gradient inside the product with the weights, or a pass of its own ahead of it (bf16 figures, without a bias; f32 by the same lines).  Inside, one tile of columns or few rows: what is read is read
 // once and a launch is spared; otherwise the slopes keep the matrix cores waiting, which a pass over memory hides (us of the whole backward pass, bf16 GELU, apart / inside:
 // 300 k x 32 -> 128 95 / 82, 53 k x 64 -> 256 45.5 / 47.7, 110 k x 128 -> 512 140 / 157, 8 k x 128 -> 128 SiLU 18.8 / 16.8, 1 k x 64 -> 256 14.9 / 14.1, 64 x 512 -> 512 12.1 / 13.8).
 // Few rows with many channels have too long a way through the registers (66 x 96 -> 3456 28 us, apart 14).
