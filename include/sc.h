@@ -467,6 +467,36 @@ int sc_qk_rope_bwd(const sc_heads* dq_out, const sc_heads* dk_out, const sc_head
                    const sc_heads* dq, const sc_heads* dk, void* d_dgain_q, void* d_dgain_k,
                    int dtype, void* d_workspace, size_t workspace_bytes, void* stream);
 
+/* Attention of queries to the keys of their scene: for query row i of a scene with nq of them and nk keys, and each head,
+ *   s_j = scale q_i . k_j,   w = softmax of s over the keys seen,   out_i = sum of w_j v_j,   lse_i = log of the sum of exp(s_j)
+ * Queries see all keys of their scene, or with causal = 1 those with j - i <= nk - nq: a scene's queries are its last rows, so the next row of a
+ * sequence sees all that is kept of it.  A query that sees no key gets zeros and lse = minus infinity.  Head h of the queries goes with head h / (q->heads / k->heads) of keys and values.
+ *   q, out      q_rows x q->heads x D;  k, v  k_rows x k->heads x D; `row` and `head` elements apart, heads of `out` apart from each other
+ *   d_q_starts, d_k_starts  [scenes + 1] as d_starts above, in rows of queries and of keys; d_k_starts NULL: the same (then q_rows == k_rows); both NULL: one scene of all rows.
+ *              Rows of `out` and d_lse of no scene are left untouched
+ *   d_k_lens   [scenes] or NULL: only that many of a scene's keys count, the first ones (a cache with room behind them, which is not read)
+ *   scale      above 0
+ *   d_lse      [q_rows][q->heads] or NULL: what sc_attention_bwd needs
+ *   D          1 to SC_ATTENTION_HEAD_MAX; scenes 1 to SC_SCENES_MAX; rows up to SC_N_MAX, q_rows (q->heads / k->heads) below 2^31 - 4096
+ *   d_workspace  workspace_bytes >= sc_attention_workspace_bytes(...), which may be 0; 16-byte aligned
+ * 16-bit weights are rounded to the rows' type ahead of their product with the values; sums are in 32 bits. */
+#define SC_ATTENTION_HEAD_MAX 256
+#define SC_SCENES_MAX         SC_N_MAX
+size_t sc_attention_workspace_bytes(int64_t q_rows, int64_t k_rows, int scenes, int q_heads, int k_heads, int D, int dtype);
+int sc_attention_fwd(const sc_heads* q, const sc_heads* k, const sc_heads* v, int64_t q_rows, int64_t k_rows, int D,
+                     const int32_t* d_q_starts, const int32_t* d_k_starts, const int32_t* d_k_lens, int scenes,
+                     int causal, float scale, const sc_heads* out, float* d_lse,
+                     int dtype, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* Gradients of sc_attention_fwd: of q, k and v from that of out.  `out` and d_lse are what the forward call stored.  Heads of keys get the sum over their queries' heads;
+ * a key that no query sees gets zeros.  Rows of no scene, and keys beyond d_k_lens, are left untouched.  16-bit weights and their gradients are rounded to the rows' type ahead of their products. */
+size_t sc_attention_bwd_workspace_bytes(int64_t q_rows, int64_t k_rows, int scenes, int q_heads, int k_heads, int D, int dtype);
+int sc_attention_bwd(const sc_heads* dout, const sc_heads* q, const sc_heads* k, const sc_heads* v, const sc_heads* out, const float* d_lse,
+                     int64_t q_rows, int64_t k_rows, int D,
+                     const int32_t* d_q_starts, const int32_t* d_k_starts, const int32_t* d_k_lens, int scenes,
+                     int causal, float scale, const sc_heads* dq, const sc_heads* dk, const sc_heads* dv,
+                     int dtype, void* d_workspace, size_t workspace_bytes, void* stream);
+
 /* ---- reading results back ------------------------------------------------------------------ */
 
 /* Fill n_pairs and per_offset from the kernel map (d_kmap may be NULL to skip that), copy the

@@ -32,6 +32,7 @@ DTYPES = {"f32": SC_F32, "f16": SC_F16, "bf16": SC_BF16,
 TORCH_DTYPES = {SC_F32: torch.float32, SC_F16: torch.float16, SC_BF16: torch.bfloat16}
 
 SC_CHANNELS_MAX, SC_GROUPS_MAX, SC_ENTRIES_MAX, SC_HEAD_MAX, SC_AXES_MAX = 65536, 65536, (1 << 31) - 1, 1024, 4
+SC_ATTENTION_HEAD_MAX, SC_SCENES_MAX = 256, SC_N_MAX
 ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, 0: 0, 1: 1, 2: 2, 3: 3}
 PAIRINGS = {"halves": 0, "adjacent": 1, 0: 0, 1: 1}
 
@@ -44,7 +45,7 @@ SYMBOLS = ["sc_hash_bytes", "sc_hash_build", "sc_hash_rebuild", "sc_hash_lookup"
            "sc_conv_packed_bytes", "sc_conv_weight_pack", "sc_conv_fwd_packed", "sc_hash_probe_slot",
            "sc_linear_fwd", "sc_linear_workspace_bytes", "sc_linear_bwd", "sc_grouped_fwd", "sc_grouped_workspace_bytes",
            "sc_grouped_bwd", "sc_rope_table_bytes", "sc_rope_table", "sc_qk_rope_fwd", "sc_qk_rope_workspace_bytes",
-           "sc_qk_rope_bwd"]
+           "sc_qk_rope_bwd", "sc_attention_workspace_bytes", "sc_attention_fwd", "sc_attention_bwd_workspace_bytes", "sc_attention_bwd"]
 
 
 class ScCounts(ctypes.Structure):
@@ -130,6 +131,10 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         "sc_qk_rope_workspace_bytes": (sz, [i64, i32, i32, i32]),
         "sc_qk_rope_bwd": (i32, [heads, heads, heads, heads, i64, i32, vp, i64, i32, vp, i32, vp, vp, ctypes.c_float, heads, heads, vp, vp, i32,
                                  vp, sz, vp]),
+        "sc_attention_workspace_bytes": (sz, [i64, i64, i32, i32, i32, i32, i32]),
+        "sc_attention_fwd": (i32, [heads, heads, heads, i64, i64, i32, vp, vp, vp, i32, i32, ctypes.c_float, heads, vp, i32, vp, sz, vp]),
+        "sc_attention_bwd_workspace_bytes": (sz, [i64, i64, i32, i32, i32, i32, i32]),
+        "sc_attention_bwd": (i32, [heads, heads, heads, heads, heads, vp, i64, i64, i32, vp, vp, vp, i32, i32, ctypes.c_float, heads, heads, heads, i32, vp, sz, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -143,7 +148,8 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
 _NATIVE_CALLS = ["sc_hash_build", "sc_hash_rebuild", "sc_kmap_build", "sc_kmap_build_noalloc", "sc_kmap_transpose", "sc_conv_fwd",
                  "sc_conv_fwd_packed", "sc_conv_up_fwd", "sc_conv_fwd_grid", "sc_grid_build", "sc_kmap_build_grid"]
 # ... and of its bind_rows()
-_NATIVE_ROW_CALLS = ["sc_linear_fwd", "sc_linear_bwd", "sc_grouped_fwd", "sc_grouped_bwd", "sc_qk_rope_fwd", "sc_qk_rope_bwd"]
+_NATIVE_ROW_CALLS = ["sc_linear_fwd", "sc_linear_bwd", "sc_grouped_fwd", "sc_grouped_bwd", "sc_qk_rope_fwd", "sc_qk_rope_bwd", "sc_attention_fwd",
+                     "sc_attention_bwd"]
 
 
 class _NativeOnFirstUse:
@@ -424,14 +430,41 @@ def sc_qk_rope_bwd(grad_q_out, grad_k_out, q, k, pos, table, grad_q, grad_k, gai
         _check(rc, "sc_qk_rope_bwd")
 
 
+def sc_attention_workspace_bytes(q_rows: int, k_rows: int, scenes: int, q_heads: int, k_heads: int, D: int, dtype) -> int:
+    return load().sc_attention_workspace_bytes(q_rows, k_rows, scenes, q_heads, k_heads, D, DTYPES[dtype])
+
+
+def sc_attention_fwd(q, k, v, out, q_starts=None, k_starts=None, k_lens=None, causal=False, scale=None, lse=None, workspace=None, stream=None):
+    """Attention of queries [rows, heads, D] to keys and values [key rows, heads of keys, D] of their scene: starts int32 [scenes + 1] of queries
+    and keys (k_starts None: the same; both None: one scene), k_lens int32 [scenes] where only the first keys of a scene count.  causal: a scene's queries are
+    its last rows, and see no key behind them.  scale: 1/sqrt(D) if None.  lse float32 [rows, heads] receives what sc_attention_bwd needs;
+    workspace uint8 [>= sc_attention_workspace_bytes(...)], which may be 0."""
+    rc = _native.attention_fwd(q, k, v, out, q_starts, k_starts, k_lens, 1 if causal else 0, q.shape[-1] ** -0.5 if scale is None else scale, lse, workspace, stream)
+    if rc:
+        _check(rc, "sc_attention_fwd")
+
+
+def sc_attention_bwd_workspace_bytes(q_rows: int, k_rows: int, scenes: int, q_heads: int, k_heads: int, D: int, dtype) -> int:
+    return load().sc_attention_bwd_workspace_bytes(q_rows, k_rows, scenes, q_heads, k_heads, D, DTYPES[dtype])
+
+
+def sc_attention_bwd(grad_out, q, k, v, out, lse, grad_q, grad_k, grad_v, q_starts=None, k_starts=None, k_lens=None, causal=False, scale=None,
+                     workspace=None, stream=None):
+    """Gradients of sc_attention_fwd, whose out and lse these are; workspace uint8 [>= sc_attention_bwd_workspace_bytes(...)]."""
+    rc = _native.attention_bwd(grad_out, q, k, v, out, lse, grad_q, grad_k, grad_v, q_starts, k_starts, k_lens, 1 if causal else 0,
+                               q.shape[-1] ** -0.5 if scale is None else scale, workspace, stream)
+    if rc:
+        _check(rc, "sc_attention_bwd")
+
+
 def sc_profile_enable(enable: bool):
     _check(load().sc_profile_enable(1 if enable else 0), "sc_profile_enable")
 
 
 def sc_profile_read() -> dict:
     """{kernel name: (launches, total ms, median ms)} for the kernels that ran since sc_profile_enable(True)."""
-    arr = (ScProfileEntry * 32)()
-    n = load().sc_profile_read(arr, 32)
+    arr = (ScProfileEntry * 64)()
+    n = load().sc_profile_read(arr, 64)
     if n < 0:
         raise ScError(n, "sc_profile_read")
     return {arr[i].name.decode(): (int(arr[i].launches), float(arr[i].total_ms), float(arr[i].median_ms))

@@ -1,0 +1,956 @@
+// Attention of queries to the keys of their scene, forward and backward (entry points: sc_attention.hip).
+//
+//     S = scale q k^T,   P = softmax of S over the keys that a query sees,   o = P v,   lse = log of the sum of exp(S)
+//     backward: dv = P^T do,  dP = do v^T,  delta = sum(do o),  dS = P (dP - delta),  dq = scale dS k,  dk = scale dS^T q
+//
+// The heads of queries that share a head of keys are columns next to each other: column c of a scene and a head of keys is row c / per, head c % per.
+// A wavefront holds NB blocks of 16 columns in registers as the matrix instruction's second operand and walks the other side's rows through LDS,
+// two buffers deep, 16 bytes a lane straight from global memory.  S comes out transposed, rows of the walked side down a lane's registers, its column along the lanes:
+// the maximum and the sum of a column are then a lane's own (of its quarter of the rows), and four registers are four consecutive rows, which is how the
+// transposing LDS read hands out the second product's first operand.  So weights go from one product to the next without leaving their registers.
+#pragma once
+
+#include "sc_product.h"
+
+namespace sc {
+
+struct HeadRows {                      // rows of one of the operands' heads
+    char* data;
+    int64_t row, head;                 // bytes
+};
+struct Attention {
+    HeadRows q, k, v, out;             // backward: out is the forward call's
+    float* lse;                        // [q_rows][q_heads], may be null forward
+    const int32_t *q_starts, *k_starts, *k_lens;
+    int scenes;
+    int64_t q_rows, k_rows;
+    int D, per, k_heads;               // per: heads of queries that share one of keys
+    int causal;
+    float scale, scale_log2;           // ... times log2 e
+    int64_t units;                     // column tiles there can be at most
+    int parts;                         // of the walked rows; above 1 results go to the workspace
+    int part_keys;                     // keys that a part has at least
+    float2* part_sums;                 // [part][q_rows][q_heads]: exponent that the weights were taken against, sum
+    float* part_out;                   // [part][q_rows][q_heads][D]
+    // backward
+    HeadRows dout, dq, dk, dv;
+    int64_t k_units;
+    float *against, *delta;            // [q_heads][q_rows]: lse times log2 e, infinite for a row that sees nothing; sum(do o)
+};
+
+// ---- scenes -------------------------------------------------------------------------------------------
+struct Scene {
+    int64_t q0, k0;                    // first rows
+    int nq, nk;
+    int tile;                          // of the scene's columns; -1: none
+};
+__device__ inline int64_t clamp_row(int64_t v, int64_t rows) { return v < 0 ? 0 : v > rows ? rows : v; }
+
+// Unit u of the scenes' columns cut into tiles of `tile` columns, `per` columns a row.  Scene s has the units from A(s) = start(s) per / tile + s on: at least as many as
+// it has tiles, one too many at most, so the host knows how many units there can be without the starts, and the device finds a unit's scene by a search
+// 64 wide, one trip to memory up to 64 scenes and two up to 4096.  Called by whole wavefronts.  Starts that do not ascend give wrong scenes, but never rows outside [0, rows).
+__device__ inline Scene find_scene(const int32_t* __restrict__ starts, int scenes, int64_t rows, int per, int tile, int64_t u, int64_t& first, int& count, int& scene) {
+    Scene none{0, 0, 0, 0, -1};
+    const int lane = threadIdx.x & 63;
+    scene = 0;
+    if (starts == nullptr) {
+        first = 0;
+        count = (int)rows;
+        if (u * tile >= rows * per) return none;
+        none.tile = (int)u;
+        return none;
+    }
+    int lo = 0, hi = scenes;
+    int64_t at_lo = 0;
+    bool found = false;
+    while (!found || hi - lo > 1) {
+        const int step = (hi - lo + 63) / 64;
+        const int s = lo + lane * step;
+        int64_t at = 0;
+        bool below = false;
+        if (s < hi) {
+            at = clamp_row(starts[s], rows) * per / tile + s;
+            below = at <= u;
+        }
+        const int n = __popcll(__ballot(below));
+        if (n == 0) return none;
+        at_lo = ((int64_t)__builtin_amdgcn_readlane((int)(at >> 32), n - 1) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)at, n - 1);
+        lo += (n - 1) * step;
+        hi = lo + step < hi ? lo + step : hi;
+        found = true;
+    }
+    scene = lo;
+    first = clamp_row(starts[lo], rows);
+    const int64_t stop = clamp_row(starts[lo + 1], rows);
+    count = (int)(stop > first ? stop - first : 0);
+    const int64_t nth = u - at_lo;
+    if (nth < 0 || nth * tile >= (int64_t)count * per) return none;
+    none.tile = (int)nth;
+    return none;
+}
+__device__ inline void scene_rows(const int32_t* __restrict__ starts, const int32_t* __restrict__ lens, int64_t rows, int scene, int64_t& first, int& count) {
+    if (starts == nullptr) {
+        first = 0;
+        count = (int)rows;
+    } else {
+        first = clamp_row(starts[scene], rows);
+        const int64_t stop = clamp_row(starts[scene + 1], rows);
+        count = (int)(stop > first ? stop - first : 0);
+    }
+    if (lens != nullptr) {
+        const int n = lens[scene];
+        count = n < 0 ? 0 : n < count ? n : count;
+    }
+}
+__device__ inline int64_t uniform64(int64_t v) {
+    return ((int64_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
+}
+__device__ inline Scene scene_of_queries(const Attention& p, int tile, int64_t u) {
+    int64_t first = 0, first_k = 0;
+    int count = 0, count_k = 0, scene;
+    Scene s = find_scene(p.q_starts, p.scenes, p.q_rows, p.per, tile, u, first, count, scene);
+    s.tile = __builtin_amdgcn_readfirstlane(s.tile);
+    if (s.tile < 0) return s;
+    scene_rows(p.k_starts, p.k_lens, p.k_rows, scene, first_k, count_k);
+    s.q0 = uniform64(first);
+    s.nq = __builtin_amdgcn_readfirstlane(count);
+    s.k0 = uniform64(first_k);
+    s.nk = __builtin_amdgcn_readfirstlane(count_k);
+    return s;
+}
+
+// ---- tiles in LDS ---------------------------------------------------------------------------------------
+// A tile is rows of LINE chunks of 16 bytes.  Where a chunk lies in its line is turned by the line's number so that both reads meet every bank once: 16-byte reads along
+// the lines go 16 lanes a cycle, a chunk of lines 0-3 and 12-15 and its neighbour of lines 4-11; transposing reads 32 lanes, two chunks of eight consecutive lines;
+// 32-bit reads across 64 bytes of lines 0, 4, 8 and 12.
+template <int DT, int LINE>
+__device__ constexpr int tile_turn(int line) {
+    constexpr int WIDE = LINE < 16 ? LINE : 16;
+    const int m = (line / (16 / WIDE)) & (WIDE - 1);
+    if (DT == SC_F32) return m;
+    const int half = WIDE / 2;
+    return (((m & (half - 1)) ^ (m >= half ? half / 2 : 0)) << 1) | (m >= half ? 1 : 0);
+}
+
+template <int DT, int DPAD>
+struct HeadShape {
+    static constexpr int PER = 16 / ELEM<DT>, LINE = DPAD / PER, BYTES = DPAD * ELEM<DT>;
+    static constexpr int KS = LINE / 4;            // steps of 64 bytes along a row
+    static constexpr int CB = DPAD / 16;           // blocks of 16 channels
+    static constexpr int STEP = DT == SC_F32 ? 16 : 32;   // rows that a step of the second product takes
+};
+
+// The loads of one operand's tiles by NTH threads: rows first .. of a scene's head.  Zeros stand for rows that are not there and for channels beyond D.
+template <int DT, int DPAD, int ROWS, int NTH>
+struct TileLoader {
+    using H = HeadShape<DT, DPAD>;
+    static constexpr int PASSES = ROWS * H::LINE / NTH;
+    static_assert(ROWS * H::LINE % NTH == 0, "whole passes");
+    const char* base;                  // of the scene's first row
+    int64_t row;
+    int D;
+    __device__ __forceinline__ void fetch(int first, int left, uint32_t lds) const {
+        const int tid = (int)threadIdx.x % NTH, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const bool inside = left >= ROWS && D == DPAD;
+        const char* const from = base + (int64_t)first * row;
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i) {
+            const int slot = i * NTH + tid, line = slot / H::LINE, chunk = (slot % H::LINE) ^ tile_turn<DT, H::LINE>(line);
+            const char* src = from + (int64_t)line * row + chunk * 16;
+            const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (i * NTH + wave * 64) * 16);
+            if (inside) {
+                load_to_lds(src, to);
+                continue;
+            }
+            const int there = line < left ? D - chunk * H::PER : 0;
+            if (there >= H::PER || there <= 0) {
+                load_to_lds(there > 0 ? (const void*)src : (const void*)&g_no_chunk, to);
+            } else {
+                uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+                for (int j = 0; j < H::PER; ++j)
+                    if (j < there) {
+                        if constexpr (DT == SC_F32) w[j] = reinterpret_cast<const uint32_t*>(src)[j];
+                        else w[j / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(src)[j] << (16 * (j & 1));
+                    }
+                *(__attribute__((address_space(3))) u32x4*)(lds + slot * 16) = u32x4{w[0], w[1], w[2], w[3]};
+            }
+        }
+    }
+};
+// What a lane reads of a tile: rows as they lie (16 rows, 64 bytes of channels a step) ...
+template <int DT, int DPAD>
+struct RowReader {
+    using H = HeadShape<DT, DPAD>;
+    uint32_t at[H::KS];
+    __device__ explicit RowReader(uint32_t lds) {
+        const int i = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
+#pragma unroll
+        for (int k = 0; k < H::KS; ++k) at[k] = lds + (i * H::LINE + ((4 * k + g) ^ tile_turn<DT, H::LINE>(i))) * 16;
+    }
+    __device__ __forceinline__ uint4 read(uint32_t tile, int block, int k) const {
+        return __builtin_bit_cast(uint4, *(lds_u32x4)(at[k] + tile + block * (16 * H::BYTES)));
+    }
+};
+// ... or across them: a block of 16 channels, of the rows 4 g .. 4 g + 3 of each 16, which are the rows that the quarter g of the lanes holds of S.
+template <int DT, int DPAD>
+struct ChannelReader {
+    using H = HeadShape<DT, DPAD>;
+    uint32_t at[H::CB];
+    __device__ explicit ChannelReader(uint32_t lds) {
+        const int i = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
+#pragma unroll
+        for (int c = 0; c < H::CB; ++c) {
+            if constexpr (DT == SC_F32) {          // the turn of rows 4 g + 0 .. 3 differs in its lowest bits: read() adds them
+                at[c] = lds + 4 * g * H::BYTES + (i & 3) * 4;
+            } else {                               // a lane hands in 4 channels of row 4 g + i / 4 and gets channel i of the four rows
+                const int line = 4 * g + (i >> 2);
+                at[c] = lds + line * H::BYTES + ((2 * c + ((i >> 1) & 1)) ^ tile_turn<DT, H::LINE>(line)) * 16 + (i & 1) * 8;
+            }
+        }
+    }
+    __device__ __forceinline__ uint4 read(uint32_t tile, int step, int c) const {
+        const uint32_t p = at[c] + tile + step * (H::STEP * H::BYTES);
+        if constexpr (DT == SC_F32) {
+            const int i = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
+            uint32_t v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = *(lds_uint32)(p + j * H::BYTES + ((4 * c + (i >> 2)) ^ tile_turn<DT, H::LINE>(4 * g + j)) * 16);
+            return make_uint4(v[0], v[1], v[2], v[3]);
+        } else {
+            const uint2 a = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p));
+            const uint2 b = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(p + 16 * H::BYTES)));
+            return make_uint4(a.x, a.y, b.x, b.y);
+        }
+    }
+};
+// Weights of a step as the second product's second operand: rounded once to the rows' type (f32: as they are).
+template <int DT, int ST>
+__device__ __forceinline__ uint4 weights_of(const f32x4 (&p)[ST], int step) {
+    if constexpr (DT == SC_F32) {
+        return __builtin_bit_cast(uint4, p[step]);
+    } else {
+        const f32x4 a = p[2 * step], b = p[2 * step + 1];
+        return make_uint4(round2<DT>(a[0], a[1]), round2<DT>(a[2], a[3]), round2<DT>(b[0], b[1]), round2<DT>(b[2], b[3]));
+    }
+}
+// A row's channels as the first product's second operand; zeros for channels beyond D and for a column that is none (null).
+template <int DT, int DPAD>
+__device__ __forceinline__ void load_columns(const char* row, int D, uint4 (&q)[HeadShape<DT, DPAD>::KS]) {
+    using H = HeadShape<DT, DPAD>;
+    const int g = (threadIdx.x >> 4) & 3;
+#pragma unroll
+    for (int k = 0; k < H::KS; ++k) {
+        const int chunk = 4 * k + g, there = row != nullptr ? D - chunk * H::PER : 0;
+        q[k] = make_uint4(0, 0, 0, 0);
+        if (there >= H::PER) {
+            q[k] = load_chunk(row + chunk * 16);
+        } else if (there > 0) {
+            uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < H::PER; ++j)
+                if (j < there) {
+                    if constexpr (DT == SC_F32) w[j] = reinterpret_cast<const uint32_t*>(row + chunk * 16)[j];
+                    else w[j / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(row + chunk * 16)[j] << (16 * (j & 1));
+                }
+            q[k] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+}
+// Four consecutive channels of a row, those from D on left alone.
+template <int DT>
+__device__ __forceinline__ void store4(char* row, int channel, int D, f32x4 v) {
+    if (channel + 4 <= D) {
+        if constexpr (DT == SC_F32) {
+            store_chunk(row + channel * 4, __builtin_bit_cast(uint4, v));
+        } else {
+            typedef uint32_t half_chunk __attribute__((ext_vector_type(2), aligned(2)));
+            *reinterpret_cast<half_chunk*>(row + channel * 2) = half_chunk{round2<DT>(v[0], v[1]), round2<DT>(v[2], v[3])};
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (channel + j < D) store_elem<DT>(row, channel + j, v[j]);
+    }
+}
+__device__ inline float over_quarters_max(float v) {
+    v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ inline float over_quarters_sum(float v) {
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
+__device__ inline void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+constexpr float NO_SCORE = -__builtin_inff();
+
+// ---- forward --------------------------------------------------------------------------------------------
+// Weights are taken against an exponent that follows the largest score only when that is more than CALM beyond it: sums and results are then scaled anew, which is
+// rare behind the first tiles.  A weight is at most 2^(CALM + LIFT); the 16-bit floats of 5 exponent bits get their weights lifted so that small ones are not
+// rounded off (their least normal number is 2^-14).
+constexpr float CALM = 8.f;
+template <int DT>
+constexpr float LIFT = DT == SC_F16 ? 6.f : 0.f;
+
+// Of a column, the same in its four lanes but for the sum, of which each has its rows'.
+struct Running {
+    float top;                         // largest exponent (score times log2 e) followed so far, minus infinity: none seen
+    float against;                     // what exponents are taken against
+    float sum;
+};
+
+template <int DT, int DPAD, int NB, bool SPLIT>
+constexpr int attention_tile() {       // keys
+    return DPAD * ELEM<DT> >= 512 || SPLIT ? 32 : 64;
+}
+template <int DT, int DPAD, int WAVES, int NB, bool SPLIT>
+constexpr size_t attention_lds() {
+    return (size_t)(SPLIT ? WAVES : 1) * 4 * attention_tile<DT, DPAD, NB, SPLIT>() * DPAD * ELEM<DT>;
+}
+
+// SPLIT: the wavefronts share 16 NB columns and take every WAVES-th tile of the keys each; otherwise each has 16 NB columns of its own and all share the tiles.
+template <int DT, int DPAD, int WAVES, int NB, bool SPLIT>
+__global__ void __launch_bounds__(64 * WAVES, 2)
+k_attention(const Attention p) {
+    using H = HeadShape<DT, DPAD>;
+    constexpr int KT = attention_tile<DT, DPAD, NB, SPLIT>(), ST = KT / 16, TILE_BYTES = KT * H::BYTES;
+    constexpr int COLUMNS = 16 * NB * (SPLIT ? 1 : WAVES);
+    extern __shared__ __align__(16) uint4 attention_lds_words[];
+    // heads of keys first: workgroups that share keys and values go to one XCD where there are as many heads
+    const uint32_t block = blockIdx.y * gridDim.x + blockIdx.x, rest = block / (uint32_t)p.k_heads;
+    const int head_k = (int)(block - rest * (uint32_t)p.k_heads);
+    const int part = (int)(rest % (uint32_t)p.parts);
+    const int64_t unit = p.units - 1 - rest / (uint32_t)p.parts;  // the last first: behind a causal mask they take longest
+    if (unit < 0) return;
+    const Scene scene = scene_of_queries(p, COLUMNS, unit);
+    if (scene.tile < 0) return;
+
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int columns = scene.nq * p.per, column0 = scene.tile * COLUMNS + (SPLIT ? 0 : wave * 16 * NB);
+    const int ahead = scene.nk - scene.nq;
+    // keys that a column sees: those below its limit
+    auto limit_of = [&](int column) {
+        if (!p.causal) return scene.nk;
+        const int n = column / p.per + ahead + 1;
+        return n < 0 ? 0 : n < scene.nk ? n : scene.nk;
+    };
+    int row_of[NB], head_of[NB], limit[NB];
+    bool there[NB];
+    uint4 q[NB][H::KS];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+        const int c = column0 + 16 * n + i;
+        there[n] = c < columns;
+        row_of[n] = there[n] ? c / p.per : 0;
+        head_of[n] = head_k * p.per + (there[n] ? c % p.per : 0);
+        limit[n] = there[n] ? limit_of(c) : 0;
+        load_columns<DT, DPAD>(there[n] ? p.q.data + (scene.q0 + row_of[n]) * p.q.row + head_of[n] * p.q.head : nullptr, p.D, q[n]);
+    }
+    const int first_limit = column0 < columns ? __builtin_amdgcn_readfirstlane(limit_of(column0)) : 0;          // of the wavefront's columns the least and the largest
+    const int last_column = column0 + 16 * NB < columns ? column0 + 16 * NB - 1 : columns - 1;
+    const int wave_limit = column0 < columns ? __builtin_amdgcn_readfirstlane(limit_of(last_column)) : 0;
+    const int all_last = scene.tile * COLUMNS + COLUMNS < columns ? scene.tile * COLUMNS + COLUMNS - 1 : columns - 1;
+    const int tiles = (__builtin_amdgcn_readfirstlane(limit_of(all_last)) + KT - 1) / KT;
+    int from = 0, to = tiles;
+    if (p.parts > 1) {                                            // equal parts, not below a least number of tiles
+        int used = (tiles * KT + p.part_keys - 1) / p.part_keys;
+        used = used < p.parts ? used : p.parts;
+        from = part < used ? (int)((int64_t)tiles * part / used) : 0;
+        to = part < used ? (int)((int64_t)tiles * (part + 1) / used) : 0;
+    }
+
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)attention_lds_words;
+    const uint32_t mine = lds0 + (SPLIT ? wave * (4 * TILE_BYTES) : 0);
+    TileLoader<DT, DPAD, KT, SPLIT ? 64 : 64 * WAVES> keys{p.k.data + scene.k0 * p.k.row + head_k * p.k.head, p.k.row, p.D},
+        values{p.v.data + scene.k0 * p.v.row + head_k * p.v.head, p.v.row, p.D};
+    const RowReader<DT, DPAD> rows(mine);
+    const ChannelReader<DT, DPAD> channels(mine + TILE_BYTES);
+    f32x4 out[NB][H::CB];
+    Running run[NB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+        run[n] = Running{NO_SCORE, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < H::CB; ++c) out[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    constexpr int STRIDE = SPLIT ? WAVES : 1;
+    auto bring = [&](int t, uint32_t buffer) __attribute__((always_inline)) {
+        keys.fetch(t * KT, scene.nk - t * KT, mine + buffer);
+        values.fetch(t * KT, scene.nk - t * KT, mine + buffer + TILE_BYTES);
+    };
+    uint32_t buffer = 0;
+    const int begin = from + (SPLIT ? wave : 0);
+    if (begin < to) bring(begin, 0);
+    for (int t = begin; t < to; t += STRIDE) {
+        loads_done();
+        if constexpr (!SPLIT) lds_barrier();
+        else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (t + STRIDE < to) bring(t + STRIDE, buffer ^ (2 * TILE_BYTES));
+        const int key0 = t * KT;
+        if (key0 < wave_limit) {
+            f32x4 s[NB][ST];
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int b = 0; b < ST; ++b) s[n][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < H::KS; ++k)
+#pragma unroll
+                for (int b = 0; b < ST; ++b) {
+                    const uint4 a = rows.read(buffer, b, k);
+#pragma unroll
+                    for (int n = 0; n < NB; ++n) s[n][b] = multiply<DT>(a, q[n][k], s[n][b]);
+                }
+            if (key0 + KT > first_limit) {
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                    for (int b = 0; b < ST; ++b)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[n][b][r] = key0 + 16 * b + 4 * g + r < limit[n] ? s[n][b][r] : NO_SCORE;
+            }
+            float most[NB];
+            bool calm = true;
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                most[n] = s[n][0][0];
+#pragma unroll
+                for (int b = 0; b < ST; ++b)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) most[n] = fmaxf(most[n], s[n][b][r]);
+                most[n] *= p.scale_log2;
+                calm = calm && most[n] <= run[n].top + CALM;
+            }
+            if (!__all(calm)) {
+#pragma unroll
+                for (int n = 0; n < NB; ++n) {
+                    const float top = fmaxf(run[n].top, over_quarters_max(most[n]));
+                    const float against = top == NO_SCORE ? 0.f : top - LIFT<DT>;
+                    const float factor = run[n].top == NO_SCORE ? 0.f : __builtin_amdgcn_exp2f(run[n].against - against);
+                    run[n].top = top;
+                    run[n].against = against;
+                    run[n].sum *= factor;
+#pragma unroll
+                    for (int c = 0; c < H::CB; ++c)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) out[n][c][r] *= factor;
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int b = 0; b < ST; ++b)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        s[n][b][r] = __builtin_amdgcn_exp2f(fmaf(s[n][b][r], p.scale_log2, -run[n].against));
+                        run[n].sum += s[n][b][r];
+                    }
+#pragma unroll
+            for (int u = 0; u < KT / H::STEP; ++u) {
+                uint4 w[NB];
+#pragma unroll
+                for (int n = 0; n < NB; ++n) w[n] = weights_of<DT, ST>(s[n], u);
+#pragma unroll
+                for (int c = 0; c < H::CB; ++c) {
+                    const uint4 a = channels.read(buffer, u, c);
+#pragma unroll
+                    for (int n = 0; n < NB; ++n) out[n][c] = multiply<DT>(a, w[n], out[n][c]);
+                }
+            }
+        }
+        buffer ^= 2 * TILE_BYTES;
+    }
+#pragma unroll
+    for (int n = 0; n < NB; ++n) run[n].sum = over_quarters_sum(run[n].sum);
+
+    if constexpr (SPLIT) {                                        // the wavefronts' columns come together: wavefront w adds up every WAVES-th block of channels
+        static_assert(NB == 1, "a block of columns");
+        static_assert((16 * DPAD * 4 + 16 * 8) <= 4 * TILE_BYTES, "fits what the wavefront's tiles took");
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        float* const shared = reinterpret_cast<float*>(attention_lds_words);
+        constexpr int SHARE = TILE_BYTES;                         // floats from wavefront to wavefront: its own four tiles
+        float* const own = shared + wave * SHARE;
+        if (g == 0) {
+            own[2 * i] = run[0].top == NO_SCORE ? NO_SCORE : run[0].against;
+            own[2 * i + 1] = run[0].sum;
+        }
+#pragma unroll
+        for (int c = 0; c < H::CB; ++c)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) own[32 + (16 * c + 4 * g + r) * 16 + i] = out[0][c][r];
+        __syncthreads();
+        float top = NO_SCORE;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, shared[w * SHARE + 2 * i]);
+        float sum = 0.f, factor[WAVES];
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float theirs = shared[w * SHARE + 2 * i];
+            factor[w] = theirs == NO_SCORE ? 0.f : __builtin_amdgcn_exp2f(theirs - top);
+            sum += theirs == NO_SCORE ? 0.f : factor[w] * shared[w * SHARE + 2 * i + 1];
+        }
+        run[0].against = top == NO_SCORE ? 0.f : top;
+        run[0].sum = sum;
+#pragma unroll
+        for (int c = 0; c < H::CB; ++c) {
+            if (c % WAVES != wave) continue;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float v = 0.f;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) v += factor[w] == 0.f ? 0.f : factor[w] * shared[w * SHARE + 32 + (16 * c + 4 * g + r) * 16 + i];
+                out[0][c][r] = v;
+            }
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+        if (!there[n]) continue;
+        const int64_t row = scene.q0 + row_of[n], entry = row * (p.k_heads * p.per) + head_of[n];
+        const bool first_writer = SPLIT ? wave == 0 && g == 0 : g == 0;
+        if (p.parts > 1) {
+            const int64_t at = (int64_t)part * p.q_rows * (p.k_heads * p.per) + entry;
+            if (first_writer) p.part_sums[at] = make_float2(run[n].against, run[n].sum);
+            if (from < to) {
+#pragma unroll
+                for (int c = 0; c < H::CB; ++c)
+                    if (!SPLIT || c % WAVES == wave) store4<SC_F32>((char*)(p.part_out + at * p.D), 16 * c + 4 * g, p.D, out[n][c]);
+            }
+        } else {
+            const float inverse = run[n].sum == 0.f ? 0.f : 1.f / run[n].sum;
+            char* const to_row = p.out.data + row * p.out.row + head_of[n] * p.out.head;
+#pragma unroll
+            for (int c = 0; c < H::CB; ++c)
+                if (!SPLIT || c % WAVES == wave) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) out[n][c][r] *= inverse;
+                    store4<DT>(to_row, 16 * c + 4 * g, p.D, out[n][c]);
+                }
+            if (p.lse != nullptr && first_writer) p.lse[entry] = run[n].sum == 0.f ? NO_SCORE : (__log2f(run[n].sum) + run[n].against) * 0.69314718055994531f;
+        }
+    }
+}
+
+// ---- backward -------------------------------------------------------------------------------------------
+// Two kernels, so that every gradient is summed by one wavefront in one order: queries' columns walk the keys, keys' columns walk the queries.  The weights are made
+// again in both from lse: seven products where five would do, and no atomics, no sums in memory.
+// The walked rows go through the registers 32 at a time.
+constexpr int SUB = 32, SUB_BLOCKS = SUB / 16;
+
+template <int DT, int DPAD>
+constexpr int grad_tile() {            // rows of a tile: two operands, two buffers
+    return DPAD * ELEM<DT> >= 512 ? 32 : 64;
+}
+template <int DT, int DPAD>
+constexpr size_t grad_lds() {
+    return (size_t)4 * grad_tile<DT, DPAD>() * DPAD * ELEM<DT> + 4 * 64 * sizeof(float);
+}
+template <int DT, int DPAD, int NB>
+constexpr int grad_waves(int rows, int results) {                 // wavefronts on a SIMD that the registers leave room for
+    return NB * (rows * HeadShape<DT, DPAD>::KS * 4 + results * HeadShape<DT, DPAD>::CB * 4) > 200 ? 1 : 2;
+}
+
+template <int DT, int DPAD, int WAVES, int NB>
+__global__ void __launch_bounds__(64 * WAVES, (grad_waves<DT, DPAD, NB>(2, 1)))
+k_attention_dq(const Attention p) {
+    using H = HeadShape<DT, DPAD>;
+    constexpr int KT = grad_tile<DT, DPAD>(), TILE_BYTES = KT * H::BYTES, COLUMNS = 16 * NB * WAVES;
+    extern __shared__ __align__(16) uint4 attention_lds_words[];
+    const uint32_t block = blockIdx.y * gridDim.x + blockIdx.x, rest = block / (uint32_t)p.k_heads;
+    const int head_k = (int)(block - rest * (uint32_t)p.k_heads);
+    const int64_t unit = p.units - 1 - (int64_t)rest;
+    if (unit < 0) return;
+    const Scene scene = scene_of_queries(p, COLUMNS, unit);
+    if (scene.tile < 0) return;
+
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int columns = scene.nq * p.per, column0 = scene.tile * COLUMNS + wave * 16 * NB;
+    const int ahead = scene.nk - scene.nq;
+    auto limit_of = [&](int column) {
+        if (!p.causal) return scene.nk;
+        const int n = column / p.per + ahead + 1;
+        return n < 0 ? 0 : n < scene.nk ? n : scene.nk;
+    };
+    int row_of[NB], head_of[NB], limit[NB];
+    bool there[NB];
+    uint4 q[NB][H::KS], dout[NB][H::KS];
+    float against[NB], delta[NB];
+    f32x4 dq[NB][H::CB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+        const int c = column0 + 16 * n + i;
+        there[n] = c < columns;
+        row_of[n] = there[n] ? c / p.per : 0;
+        head_of[n] = head_k * p.per + (there[n] ? c % p.per : 0);
+        limit[n] = there[n] ? limit_of(c) : 0;
+        const int64_t row = scene.q0 + row_of[n];
+        load_columns<DT, DPAD>(there[n] ? p.q.data + row * p.q.row + head_of[n] * p.q.head : nullptr, p.D, q[n]);
+        load_columns<DT, DPAD>(there[n] ? p.dout.data + row * p.dout.row + head_of[n] * p.dout.head : nullptr, p.D, dout[n]);
+        const float lse = there[n] ? p.lse[row * (p.k_heads * p.per) + head_of[n]] : NO_SCORE;
+        against[n] = lse == NO_SCORE ? -NO_SCORE : lse * 1.4426950408889634f;
+        uint4 out[H::KS];
+        load_columns<DT, DPAD>(there[n] ? p.out.data + row * p.out.row + head_of[n] * p.out.head : nullptr, p.D, out);
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < H::KS; ++k) {
+            const uint32_t a[4] = {dout[n][k].x, dout[n][k].y, dout[n][k].z, dout[n][k].w}, b[4] = {out[k].x, out[k].y, out[k].z, out[k].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (DT == SC_F32) {
+                    sum = fmaf(__builtin_bit_cast(float, a[j]), __builtin_bit_cast(float, b[j]), sum);
+                } else {
+                    sum = fmaf(to_float<DT>(a[j] & 0xffffu), to_float<DT>(b[j] & 0xffffu), sum);
+                    sum = fmaf(to_float<DT>(a[j] >> 16), to_float<DT>(b[j] >> 16), sum);
+                }
+            }
+        }
+        delta[n] = over_quarters_sum(sum);
+        if (there[n] && g == 0) {                                 // for the keys' kernel, a head's rows together
+            p.against[(int64_t)head_of[n] * p.q_rows + row] = against[n];
+            p.delta[(int64_t)head_of[n] * p.q_rows + row] = delta[n];
+        }
+#pragma unroll
+        for (int c = 0; c < H::CB; ++c) dq[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int first_limit = column0 < columns ? __builtin_amdgcn_readfirstlane(limit_of(column0)) : 0;
+    const int last_column = column0 + 16 * NB < columns ? column0 + 16 * NB - 1 : columns - 1;
+    const int wave_limit = column0 < columns ? __builtin_amdgcn_readfirstlane(limit_of(last_column)) : 0;
+    const int all_last = scene.tile * COLUMNS + COLUMNS < columns ? scene.tile * COLUMNS + COLUMNS - 1 : columns - 1;
+    const int tiles = (__builtin_amdgcn_readfirstlane(limit_of(all_last)) + KT - 1) / KT;
+
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)attention_lds_words;
+    TileLoader<DT, DPAD, KT, 64 * WAVES> keys{p.k.data + scene.k0 * p.k.row + head_k * p.k.head, p.k.row, p.D},
+        values{p.v.data + scene.k0 * p.v.row + head_k * p.v.head, p.v.row, p.D};
+    const RowReader<DT, DPAD> rows(lds0);
+    const ChannelReader<DT, DPAD> channels(lds0);
+    auto bring = [&](int t, uint32_t buffer) __attribute__((always_inline)) {
+        keys.fetch(t * KT, scene.nk - t * KT, lds0 + buffer);
+        values.fetch(t * KT, scene.nk - t * KT, lds0 + buffer + TILE_BYTES);
+    };
+    uint32_t buffer = 0;
+    if (tiles > 0) bring(0, 0);
+    for (int t = 0; t < tiles; ++t) {
+        loads_done();
+        lds_barrier();
+        if (t + 1 < tiles) bring(t + 1, buffer ^ (2 * TILE_BYTES));
+#pragma unroll 1
+        for (int h = 0; h < KT / SUB; ++h) {
+            const int key0 = t * KT + h * SUB;
+            const uint32_t tile = buffer + h * (SUB * H::BYTES);
+            if (key0 >= wave_limit) break;
+            f32x4 s[NB][SUB_BLOCKS], dp[NB][SUB_BLOCKS];
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int b = 0; b < SUB_BLOCKS; ++b) s[n][b] = dp[n][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < H::KS; ++k)
+#pragma unroll
+                for (int b = 0; b < SUB_BLOCKS; ++b) {
+                    const uint4 a = rows.read(tile, b, k), v = rows.read(tile + TILE_BYTES, b, k);
+#pragma unroll
+                    for (int n = 0; n < NB; ++n) {
+                        s[n][b] = multiply<DT>(a, q[n][k], s[n][b]);
+                        dp[n][b] = multiply<DT>(v, dout[n][k], dp[n][b]);
+                    }
+                }
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int b = 0; b < SUB_BLOCKS; ++b)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        s[n][b][r] = __builtin_amdgcn_exp2f(fmaf(s[n][b][r], p.scale_log2, -against[n])) * (dp[n][b][r] - delta[n]);
+            if (key0 + SUB > first_limit) {
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                    for (int b = 0; b < SUB_BLOCKS; ++b)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[n][b][r] = key0 + 16 * b + 4 * g + r < limit[n] ? s[n][b][r] : 0.f;
+            }
+#pragma unroll
+            for (int u = 0; u < SUB / H::STEP; ++u) {
+                uint4 w[NB];
+#pragma unroll
+                for (int n = 0; n < NB; ++n) w[n] = weights_of<DT, SUB_BLOCKS>(s[n], u);
+#pragma unroll
+                for (int c = 0; c < H::CB; ++c) {
+                    const uint4 a = channels.read(tile, u, c);
+#pragma unroll
+                    for (int n = 0; n < NB; ++n) dq[n][c] = multiply<DT>(a, w[n], dq[n][c]);
+                }
+            }
+        }
+        buffer ^= 2 * TILE_BYTES;
+    }
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+        if (!there[n]) continue;
+        char* const to_row = p.dq.data + (scene.q0 + row_of[n]) * p.dq.row + head_of[n] * p.dq.head;
+#pragma unroll
+        for (int c = 0; c < H::CB; ++c) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) dq[n][c][r] *= p.scale;
+            store4<DT>(to_row, 16 * c + 4 * g, p.D, dq[n][c]);
+        }
+    }
+}
+
+// Stand for rows that are not there: a weight of zero.
+__device__ float g_no_weight = __builtin_inff();
+
+template <int DT, int DPAD, int WAVES, int NB>
+__global__ void __launch_bounds__(64 * WAVES, (grad_waves<DT, DPAD, NB>(2, 2)))
+k_attention_dkv(const Attention p) {
+    using H = HeadShape<DT, DPAD>;
+    constexpr int RT = grad_tile<DT, DPAD>(), TILE_BYTES = RT * H::BYTES, COLUMNS = 16 * NB * WAVES;
+    extern __shared__ __align__(16) uint4 attention_lds_words[];
+    const uint32_t block = blockIdx.y * gridDim.x + blockIdx.x, rest = block / (uint32_t)p.k_heads;
+    const int head_k = (int)(block - rest * (uint32_t)p.k_heads);
+    const int64_t unit = rest;                                    // behind a causal mask the first take longest
+    if (unit >= p.k_units) return;
+    int64_t k0 = 0, q0 = 0, first_all = 0;
+    int nk = 0, nq = 0, all = 0, scene_at;
+    const int at = __builtin_amdgcn_readfirstlane(find_scene(p.k_starts, p.scenes, p.k_rows, 1, COLUMNS, unit, first_all, all, scene_at).tile);
+    if (at < 0) return;
+    scene_rows(p.k_starts, p.k_lens, p.k_rows, scene_at, k0, nk);
+    scene_rows(p.q_starts, nullptr, p.q_rows, scene_at, q0, nq);
+    k0 = uniform64(k0);
+    q0 = uniform64(q0);
+    nk = __builtin_amdgcn_readfirstlane(nk);
+    nq = __builtin_amdgcn_readfirstlane(nq);
+    if (at * COLUMNS >= nk) return;
+
+    const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int column0 = at * COLUMNS + wave * 16 * NB, ahead = nk - nq;
+    uint4 k[NB][H::KS], v[NB][H::KS];
+    f32x4 dk[NB][H::CB], dv[NB][H::CB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+        const int c = column0 + 16 * n + i;
+        load_columns<DT, DPAD>(c < nk ? p.k.data + (k0 + c) * p.k.row + head_k * p.k.head : nullptr, p.D, k[n]);
+        load_columns<DT, DPAD>(c < nk ? p.v.data + (k0 + c) * p.v.row + head_k * p.v.head : nullptr, p.D, v[n]);
+#pragma unroll
+        for (int c = 0; c < H::CB; ++c) dk[n][c] = dv[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // rows that see key c: c - ahead on
+    const int tiles = (nq + RT - 1) / RT;
+    int first_row = p.causal ? at * COLUMNS - ahead : 0;
+    first_row = first_row < 0 ? 0 : first_row;
+    const int first_tile = first_row / RT < tiles ? first_row / RT : tiles;
+    const int last_column = column0 + 16 * NB - 1 < nk ? column0 + 16 * NB - 1 : nk - 1;
+
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)attention_lds_words;
+    constexpr uint32_t SUMS = 4 * TILE_BYTES;                     // exponents and deltas of a tile's rows, 64 words each, two buffers
+    const RowReader<DT, DPAD> rows(lds0);
+    const ChannelReader<DT, DPAD> channels(lds0);
+    const int each = tiles - first_tile, total = each * p.per;
+    auto bring = [&](int n, int which) __attribute__((always_inline)) {
+        const int h = n / each, t = first_tile + n - h * each, head = head_k * p.per + h, left = nq - t * RT;
+        const TileLoader<DT, DPAD, RT, 64 * WAVES> queries{p.q.data + q0 * p.q.row + head * p.q.head, p.q.row, p.D},
+            grads{p.dout.data + q0 * p.dout.row + head * p.dout.head, p.dout.row, p.D};
+        queries.fetch(t * RT, left, lds0 + which * (2 * TILE_BYTES));
+        grads.fetch(t * RT, left, lds0 + which * (2 * TILE_BYTES) + TILE_BYTES);
+        const int64_t from = (int64_t)head * p.q_rows + q0 + t * RT + lane;
+        if (wave == 0 && lane < RT)
+            load_word_to_lds(lane < left ? (const void*)(p.against + from) : (const void*)&g_no_weight, __builtin_amdgcn_readfirstlane(lds0 + SUMS + which * 512));
+        if (wave == WAVES - 1 && lane < RT)
+            load_word_to_lds(lane < left ? (const void*)(p.delta + from) : (const void*)&g_no_chunk, __builtin_amdgcn_readfirstlane(lds0 + SUMS + which * 512 + 256));
+    };
+    if (total > 0) bring(0, 0);
+    int which = 0;
+    for (int n = 0; n < total; ++n, which ^= 1) {
+        loads_done();
+        lds_barrier();
+        if (n + 1 < total) bring(n + 1, which ^ 1);
+        const int row_tile = (first_tile + n % each) * RT;
+#pragma unroll 1
+        for (int h = 0; h < RT / SUB; ++h) {
+            const int row0 = row_tile + h * SUB;
+            const uint32_t tile = which * (2 * TILE_BYTES) + h * (SUB * H::BYTES);
+            if (p.causal && row0 + SUB - 1 + ahead < column0) continue;       // none of the rows sees any of the keys
+            if (row0 >= nq || column0 >= nk) break;
+            f32x4 s[NB][SUB_BLOCKS], dp[NB][SUB_BLOCKS];
+#pragma unroll
+            for (int m = 0; m < NB; ++m)
+#pragma unroll
+                for (int b = 0; b < SUB_BLOCKS; ++b) s[m][b] = dp[m][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < H::KS; ++c)
+#pragma unroll
+                for (int b = 0; b < SUB_BLOCKS; ++b) {
+                    const uint4 a = rows.read(tile, b, c), d = rows.read(tile + TILE_BYTES, b, c);
+#pragma unroll
+                    for (int m = 0; m < NB; ++m) {
+                        s[m][b] = multiply<DT>(a, k[m][c], s[m][b]);
+                        dp[m][b] = multiply<DT>(d, v[m][c], dp[m][b]);
+                    }
+                }
+            const bool masked = p.causal && row0 + ahead < last_column;
+#pragma unroll
+            for (int b = 0; b < SUB_BLOCKS; ++b) {
+                const uint32_t sums = lds0 + SUMS + which * 512 + (h * SUB + 16 * b + 4 * g) * 4;
+                const f32x4 against = __builtin_bit_cast(f32x4, *(lds_u32x4)sums), delta = __builtin_bit_cast(f32x4, *(lds_u32x4)(sums + 256));
+#pragma unroll
+                for (int m = 0; m < NB; ++m)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        s[m][b][r] = __builtin_amdgcn_exp2f(fmaf(s[m][b][r], p.scale_log2, -against[r]));
+                        dp[m][b][r] = s[m][b][r] * (dp[m][b][r] - delta[r]);
+                    }
+            }
+            if (masked) {
+#pragma unroll
+                for (int m = 0; m < NB; ++m)
+#pragma unroll
+                    for (int b = 0; b < SUB_BLOCKS; ++b)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const bool seen = row0 + 16 * b + 4 * g + r + ahead >= column0 + 16 * m + i;
+                            s[m][b][r] = seen ? s[m][b][r] : 0.f;
+                            dp[m][b][r] = seen ? dp[m][b][r] : 0.f;
+                        }
+            }
+#pragma unroll
+            for (int u = 0; u < SUB / H::STEP; ++u) {
+                uint4 w[NB], z[NB];
+#pragma unroll
+                for (int m = 0; m < NB; ++m) {
+                    w[m] = weights_of<DT, SUB_BLOCKS>(s[m], u);
+                    z[m] = weights_of<DT, SUB_BLOCKS>(dp[m], u);
+                }
+#pragma unroll
+                for (int c = 0; c < H::CB; ++c) {
+                    const uint4 a = channels.read(tile + TILE_BYTES, u, c), b = channels.read(tile, u, c);
+#pragma unroll
+                    for (int m = 0; m < NB; ++m) {
+                        dv[m][c] = multiply<DT>(a, w[m], dv[m][c]);
+                        dk[m][c] = multiply<DT>(b, z[m], dk[m][c]);
+                    }
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+        const int c = column0 + 16 * n + i;
+        if (c >= nk) continue;
+        char* const to_k = p.dk.data + (k0 + c) * p.dk.row + head_k * p.dk.head;
+        char* const to_v = p.dv.data + (k0 + c) * p.dv.row + head_k * p.dv.head;
+#pragma unroll
+        for (int b = 0; b < H::CB; ++b) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) dk[n][b][r] *= p.scale;
+            store4<DT>(to_k, 16 * b + 4 * g, p.D, dk[n][b]);
+            store4<DT>(to_v, 16 * b + 4 * g, p.D, dv[n][b]);
+        }
+    }
+}
+
+// Parts joined: a thread has four channels of a row's head.
+template <int DT>
+__global__ void __launch_bounds__(256)
+k_attention_join(const Attention p, int64_t entries, int q_heads) {
+    const int fours = (p.D + 3) / 4;
+    const int64_t item = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t entry = item / fours;
+    if (entry >= entries) return;
+    const int64_t row = entry / q_heads;
+    if (p.q_starts != nullptr && (row < p.q_starts[0] || row >= p.q_starts[p.scenes])) return;        // a row of no scene stays as it is
+    const int channel = (int)(item - entry * fours) * 4;
+    float top = NO_SCORE;
+#pragma unroll 4
+    for (int k = 0; k < p.parts; ++k) {
+        const float2 s = p.part_sums[k * entries + entry];
+        top = s.y == 0.f ? top : fmaxf(top, s.x);
+    }
+    float sum = 0.f;
+    f32x4 v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int k = 0; k < p.parts; ++k) {
+        const float2 s = p.part_sums[k * entries + entry];
+        if (s.y == 0.f) continue;                                // nothing seen: its results were not written
+        const float factor = __builtin_amdgcn_exp2f(s.x - top);
+        sum = fmaf(factor, s.y, sum);
+        const float* from = p.part_out + (k * entries + entry) * p.D + channel;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = channel + j < p.D ? fmaf(factor, from[j], v[j]) : 0.f;
+    }
+    const float inverse = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] *= inverse;
+    store4<DT>(p.out.data + row * p.out.row + (entry - row * q_heads) * p.out.head, channel, p.D, v);
+    if (p.lse != nullptr && channel == 0) p.lse[entry] = sum == 0.f ? NO_SCORE : (__log2f(sum) + top) * 0.69314718055994531f;
+}
+
+// ---- launches -------------------------------------------------------------------------------------------
+template <int DT, int DPAD, int WAVES, int NB, bool SPLIT>
+int start_attention(Attention p, hipStream_t s) {
+    constexpr auto kernel = k_attention<DT, DPAD, WAVES, NB, SPLIT>;
+    constexpr size_t lds = attention_lds<DT, DPAD, WAVES, NB, SPLIT>();
+    p.units = scene_units(p.q_rows * p.per, p.scenes, 16 * NB * (SPLIT ? 1 : WAVES));
+    static bool done[MAX_DEVICES];
+    const int rc = allow_lds((const void*)kernel, lds, done);
+    if (rc != SC_OK) return rc;
+    const int64_t blocks = p.units * p.k_heads * p.parts;
+    if (blocks > INT32_MAX - 2 * GRID_COLUMNS) return SC_EINVAL;
+    SC_LAUNCH(KID_ATTENTION, kernel, dim3((unsigned)grid_columns(blocks), (unsigned)grid_rows(blocks)), dim3(64 * WAVES), lds, s, p);
+    return SC_OK;
+}
+template <int DT, int DPAD>
+int choose_attention(const Attention& p, AttentionShape shape, hipStream_t s) {
+    constexpr int NB = DT == SC_F32 && DPAD == 256 ? 1 : 2;
+    if (shape == ATTENTION_FEW) return start_attention<DT, DPAD, 4, 1, true>(p, s);
+    if (shape == ATTENTION_SHORT) return start_attention<DT, DPAD, 1, NB, false>(p, s);
+    return start_attention<DT, DPAD, 4, NB, false>(p, s);
+}
+template <int DT>
+int launch_attention(const Attention& p, AttentionShape shape, hipStream_t s) {
+    const int rc = p.D <= 32 ? choose_attention<DT, 32>(p, shape, s) : p.D <= 64 ? choose_attention<DT, 64>(p, shape, s)
+                 : p.D <= 128 ? choose_attention<DT, 128>(p, shape, s) : choose_attention<DT, 256>(p, shape, s);
+    if (rc != SC_OK || p.parts == 1) return rc;
+    const int q_heads = p.k_heads * p.per;
+    const int64_t entries = p.q_rows * q_heads, blocks = (entries * ((p.D + 3) / 4) + 255) / 256;
+    if (blocks > INT32_MAX / 256) return SC_EINVAL;
+    SC_LAUNCH(KID_ATTENTION_JOIN, k_attention_join<DT>, dim3((unsigned)blocks), dim3(256), 0, s, p, entries, q_heads);
+    return SC_OK;
+}
+
+template <int DT, int DPAD, int WAVES, int NB>
+int start_attention_grad(Attention p, hipStream_t s) {
+    constexpr auto of_queries = k_attention_dq<DT, DPAD, WAVES, NB>;
+    constexpr auto of_keys = k_attention_dkv<DT, DPAD, WAVES, NB>;
+    constexpr size_t lds = grad_lds<DT, DPAD>();
+    static bool done_queries[MAX_DEVICES], done_keys[MAX_DEVICES];
+    int rc = allow_lds((const void*)of_queries, lds, done_queries);
+    if (rc == SC_OK) rc = allow_lds((const void*)of_keys, lds, done_keys);
+    if (rc != SC_OK) return rc;
+    constexpr int COLUMNS = 16 * NB * WAVES;
+    p.units = scene_units(p.q_rows * p.per, p.scenes, COLUMNS);
+    p.k_units = scene_units(p.k_rows, p.scenes, COLUMNS);
+    const int64_t blocks = p.units * p.k_heads, key_blocks = p.k_units * p.k_heads;
+    if (blocks > INT32_MAX - 2 * GRID_COLUMNS || key_blocks > INT32_MAX - 2 * GRID_COLUMNS) return SC_EINVAL;
+    if (p.q_rows > 0)
+        SC_LAUNCH(KID_ATTENTION_DQ, of_queries, dim3((unsigned)grid_columns(blocks), (unsigned)grid_rows(blocks)), dim3(64 * WAVES), lds, s, p);
+    if (p.k_rows > 0)
+        SC_LAUNCH(KID_ATTENTION_DKV, of_keys, dim3((unsigned)grid_columns(key_blocks), (unsigned)grid_rows(key_blocks)), dim3(64 * WAVES), lds, s, p);
+    return SC_OK;
+}
+template <int DT, int DPAD>
+int choose_attention_grad(const Attention& p, bool shorts, hipStream_t s) {
+    constexpr int NB = DT == SC_F32 && DPAD == 256 ? 1 : 2;
+    if (shorts) return start_attention_grad<DT, DPAD, 1, NB>(p, s);
+    return start_attention_grad<DT, DPAD, 4, NB>(p, s);
+}
+template <int DT>
+int launch_attention_grad(const Attention& p, bool shorts, hipStream_t s) {
+    return p.D <= 32 ? choose_attention_grad<DT, 32>(p, shorts, s) : p.D <= 64 ? choose_attention_grad<DT, 64>(p, shorts, s)
+           : p.D <= 128 ? choose_attention_grad<DT, 128>(p, shorts, s) : choose_attention_grad<DT, 256>(p, shorts, s);
+}
+
+}  // namespace sc

@@ -402,7 +402,7 @@ enum KernelId {
     KID_STRIDED_INSERT, KID_STRIDED_FLAGS, KID_SCAN_BLOCKS, KID_STRIDED_PAIRS, KID_KMAP_FROM_OFT,
     KID_COUNT_PAIRS, KID_EXPORT, KID_WEIGHT_PACK, KID_CONV_MFMA, KID_CONV_F32, KID_GRID_CLEAR, KID_GRID_INSERT,
     KID_GRID_LOOKUP, KID_KMAP_GRID, KID_PRODUCT, KID_PRODUCT_JOIN, KID_ACT_GRAD, KID_ROPE_TABLE, KID_ROPE, KID_ROPE_GRAD,
-    KID_GAIN_JOIN, KID_MISC, KID_COUNT
+    KID_GAIN_JOIN, KID_ATTENTION, KID_ATTENTION_JOIN, KID_ATTENTION_DQ, KID_ATTENTION_DKV, KID_NORM, KID_NORM_SUMS, KID_NORM_GRAD, KID_NORM_JOIN, KID_MISC, KID_COUNT
 };
 extern bool g_profile_on;
 // A fresh pair of events for one launch of `kernel_id`; false if none could be created.

@@ -26,7 +26,7 @@ const char* const KERNEL_NAMES[KID_COUNT] = {
     "k_strided_insert", "k_strided_flags", "k_scan_blocks", "k_strided_pairs", "k_masks_from_table",
     "k_count_pairs", "k_export", "k_weight_pack", "k_conv_mfma", "k_conv_f32", "k_grid_clear", "k_grid_insert",
     "k_grid_lookup", "k_kmap_subm_grid", "k_product", "k_product_join", "k_act_grad", "k_rope_table", "k_rope", "k_rope_grad",
-    "k_gain_join", "misc"};
+    "k_gain_join", "k_attention", "k_attention_join", "k_attention_dq", "k_attention_dkv", "k_norm", "k_norm_sums", "k_norm_grad", "k_norm_join", "misc"};
 
 hipEvent_t take_event() {
     if (!g_pool.empty()) {

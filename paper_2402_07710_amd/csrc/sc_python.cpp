@@ -43,6 +43,8 @@ struct RowLib {
     decltype(&sc_grouped_bwd) grouped_bwd;
     decltype(&sc_qk_rope_fwd) qk_rope_fwd;
     decltype(&sc_qk_rope_bwd) qk_rope_bwd;
+    decltype(&sc_attention_fwd) attention_fwd;
+    decltype(&sc_attention_bwd) attention_bwd;
 } row_lib;
 
 struct PyFailure {};      // a Python exception is set
@@ -365,6 +367,10 @@ sc_heads heads_of(PyObject* o, const char* name, int64_t rows, int64_t D) {
     h.data = address(t);
     return h;
 }
+PyObject* tensor_given(PyObject* o, const char* name) {
+    if (o == Py_None) fail_on(PyExc_ValueError, name, "is needed");
+    return o;
+}
 struct Positions {
     const int32_t* data;
     int64_t ld;
@@ -427,6 +433,60 @@ int qk_rope_bwd(Args a) {                // grad_q_out, grad_k_out, q, k, pos, t
                     ptr(a[10]), ptr(a[11]), dtype(a[0]), ptr(a[14]), nbytes(a[14]), stream(a[15]));
 }
 
+// The scenes of attention's queries and keys: starts int32 [scenes + 1], lengths int32 [scenes], all of them optional.
+struct Scenes {
+    const int32_t *q_starts, *k_starts, *k_lens;
+    int scenes;
+};
+Scenes scenes_of(PyObject* q_starts, PyObject* k_starts, PyObject* k_lens, int64_t q_rows, int64_t k_rows) {
+    if (q_starts == Py_None && k_starts != Py_None) fail(PyExc_ValueError, "k_starts without q_starts");
+    if (q_starts != Py_None && k_starts == Py_None && q_rows != k_rows) fail(PyExc_ValueError, "as many keys as queries, or k_starts");
+    const int64_t scenes = q_starts == Py_None ? 1 : size(q_starts, 0) - 1;
+    if (scenes < 1 || scenes > SC_SCENES_MAX) fail(PyExc_ValueError, "q_starts must be int32 [scenes + 1]");
+    return Scenes{list_of(q_starts, "q_starts", scenes + 1), list_of(k_starts, "k_starts", scenes + 1), list_of(k_lens, "k_lens", scenes), (int)scenes};
+}
+float* floats_of(PyObject* o, const char* name, std::initializer_list<int64_t> sizes) {
+    if (o == Py_None) return nullptr;
+    if (tensor(o).scalar_type() != at::kFloat) fail_on(PyExc_ValueError, name, "must be float32");
+    check_block(o, name, sizes);
+    return (float*)address(tensor(o));
+}
+int attention_fwd(Args a) {              // q, k, v, out, q_starts, k_starts, k_lens, causal, scale, lse, workspace, stream
+    if (tensor(a[0]).dim() != 3) fail(PyExc_ValueError, "q must be [rows, heads, D]");
+    if (tensor(a[1]).dim() != 3) fail(PyExc_ValueError, "k must be [rows, heads, D]");
+    const int64_t rows = size(a[0], 0), D = size(a[0], 2), keys = size(a[1], 0);
+    const sc_heads q = heads_of(a[0], "q", rows, D), k = heads_of(a[1], "k", keys, D), v = heads_of(tensor_given(a[2], "v"), "v", keys, D),
+                   out = heads_of(tensor_given(a[3], "out"), "out", rows, D);
+    for (const int i : {1, 2, 3}) check_dtype(a[i], "an argument", a[0]);
+    if (k.heads != v.heads) fail(PyExc_ValueError, "v has another number of heads than k");
+    if (out.heads != q.heads) fail(PyExc_ValueError, "out has another number of heads than q");
+    const Scenes s = scenes_of(a[4], a[5], a[6], rows, keys);
+    float* lse = floats_of(a[9], "lse", {rows, q.heads});
+    all_on_device(a, 12);
+    return unlocked(row_lib.attention_fwd, &q, &k, &v, rows, keys, count32(D), s.q_starts, s.k_starts, s.k_lens, s.scenes, small_int(a[7]), number(a[8]), &out, lse,
+                    dtype(a[0]), ptr(a[10]), nbytes(a[10]), stream(a[11]));
+}
+int attention_bwd(Args a) {              // grad_out, q, k, v, out, lse, grad_q, grad_k, grad_v, q_starts, k_starts, k_lens, causal, scale, workspace, stream
+    if (tensor(a[1]).dim() != 3) fail(PyExc_ValueError, "q must be [rows, heads, D]");
+    if (tensor(a[2]).dim() != 3) fail(PyExc_ValueError, "k must be [rows, heads, D]");
+    const int64_t rows = size(a[1], 0), D = size(a[1], 2), keys = size(a[2], 0);
+    const char* const names[9] = {"grad_out", "q", "k", "v", "out", "lse", "grad_q", "grad_k", "grad_v"};
+    const bool of_keys[9] = {false, false, true, true, false, false, false, true, true};
+    sc_heads h[9];
+    for (int i = 0; i < 9; ++i) {
+        tensor_given(a[i], names[i]);
+        if (i == 5) continue;
+        h[i] = heads_of(a[i], names[i], of_keys[i] ? keys : rows, D);
+        check_dtype(a[i], names[i], a[1]);
+        if (h[i].heads != size(a[of_keys[i] ? 2 : 1], 1)) fail_on(PyExc_ValueError, names[i], "has another number of heads");
+    }
+    const Scenes s = scenes_of(a[9], a[10], a[11], rows, keys);
+    const float* lse = floats_of(a[5], "lse", {rows, size(a[1], 1)});
+    all_on_device(a, 16);
+    return unlocked(row_lib.attention_bwd, &h[0], &h[1], &h[2], &h[3], &h[4], lse, rows, keys, count32(D), s.q_starts, s.k_starts, s.k_lens, s.scenes, small_int(a[12]),
+                    number(a[13]), &h[6], &h[7], &h[8], dtype(a[1]), ptr(a[14]), nbytes(a[14]), stream(a[15]));
+}
+
 template <int (*F)(Args), int N>
 PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (nargs != N) {
@@ -483,6 +543,8 @@ PyMethodDef methods[] = {
     SC_METHOD(grouped_bwd, 13),
     SC_METHOD(qk_rope_fwd, 11),
     SC_METHOD(qk_rope_bwd, 16),
+    SC_METHOD(attention_fwd, 12),
+    SC_METHOD(attention_bwd, 16),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "argument marshalling for libsc's calls", -1, methods,

@@ -12,6 +12,7 @@
 // 261574 rows of 8 + 8 heads of 32, bf16: 540 MB in 108 to 116 us, 4.7 to 5.0 TB/s, the rate of a copy (heads at a time 4 / 2 / 1: 108 / 109 / 130); backward 110545
 // rows of 8 + 2 heads of 64, f16: 425 MB in 94 us, 4.5 TB/s (2 / 1 at a time 97 / 116; four hold too many registers), and 5 us for the gains.
 // Stores past the caches were slower (119 and 166).
+#include "sc_heads.h"
 #include "sc_product.h"
 
 namespace sc {
@@ -351,25 +352,9 @@ int lanes_log2(int D) {
 }
 constexpr int FORWARD_TOGETHER = 4, BACKWARD_TOGETHER = 2;
 
-bool heads_ok(const sc_heads* h, int dtype) {
-    const int size = dtype == SC_F32 ? 4 : 2;
-    return h != nullptr && h->data != nullptr && ((uintptr_t)h->data & (uintptr_t)(size - 1)) == 0 && h->heads >= 0 && h->heads <= SC_GROUPS_MAX &&
-           h->row >= 0 && h->head >= 0 && h->row <= INT32_MAX * (int64_t)64 && h->head <= INT32_MAX * (int64_t)64;
-}
 Heads heads_of(const sc_heads* h, int dtype) {
     const int size = dtype == SC_F32 ? 4 : 2;
     return Heads{(char*)h->data, h->row * size, h->head * size, h->heads};
-}
-// No element of an output belongs to two heads.  Mostly the heads of a row lie within it, or the rows of a head within that; rows and heads that
-// interleave otherwise are gone through.
-bool heads_apart(const sc_heads* h, int64_t rows, int D) {
-    const int64_t row = h->row, head = h->head, heads = h->heads;
-    if ((rows > 1 && row < D) || (heads > 1 && head < D)) return false;
-    if (rows <= 1 || heads <= 1 || row >= head * (heads - 1) + D || head >= row * (rows - 1) + D) return true;
-    for (int64_t j = 1; j < heads; ++j)                // row i and head j of another: i row - j head
-        for (int64_t i = j * head / row; i <= j * head / row + 1; ++i)
-            if (i > 0 && i < rows && i * row - j * head < D && j * head - i * row < D) return false;
-    return true;
 }
 bool has_keys(const sc_heads* k) { return k != nullptr && k->heads > 0; }
 

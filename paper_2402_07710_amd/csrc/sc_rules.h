@@ -281,4 +281,27 @@ constexpr bool act_in_product(int64_t entries, int64_t groups, int64_t c_in, int
 // 1024 / 2048 / 4096: 94.8 / 97.2 / 104.8 us; forward the same to the per cent).
 constexpr int64_t ROPE_BLOCKS_MAX = 1024;
 
+// ---- attention over packed scenes (sc_attention.h) --------------------------------------------------------
+// Units of work of scenes' columns cut into tiles: scene s has those from start(s) / tile + s on, one more than it needs at most.
+constexpr int64_t scene_units(int64_t columns, int64_t scenes, int64_t tile) { return columns / tile + scenes; }
+
+// FEW: 16 columns a workgroup, whose four wavefronts share the keys; SHORT: a wavefront alone; WIDE: four wavefronts, 128 columns.
+enum AttentionShape { ATTENTION_FEW, ATTENTION_SHORT, ATTENTION_WIDE };
+constexpr AttentionShape attention_shape(int64_t columns, int64_t scenes, int64_t k_rows) {
+    if (columns <= 32 * scenes && k_rows >= 256 * scenes) return ATTENTION_FEW;
+    return columns <= 64 * scenes ? ATTENTION_SHORT : ATTENTION_WIDE;
+}
+constexpr int attention_columns(AttentionShape shape) { return shape == ATTENTION_FEW ? 16 : shape == ATTENTION_SHORT ? 32 : 128; }
+// Parts that the keys of a scene are cut into where its columns alone do not fill the chip, and the keys that a part has at least.
+constexpr int ATTENTION_PARTS_MAX = 256;
+constexpr int attention_part_keys(AttentionShape) { return 256; }
+constexpr int attention_parts(AttentionShape shape, int64_t columns, int64_t scenes, int64_t k_heads, int64_t k_rows) {
+    const int64_t wanted = shape == ATTENTION_FEW ? 1024 : shape == ATTENTION_SHORT ? 2048 : 512;
+    const int64_t most = (k_rows / scenes + attention_part_keys(shape) - 1) / attention_part_keys(shape);
+    const int64_t there = (columns + attention_columns(shape) - 1) / attention_columns(shape) > scenes ? (columns + attention_columns(shape) - 1) / attention_columns(shape) : scenes;
+    int64_t parts = (wanted + there * k_heads - 1) / (there * k_heads);
+    parts = parts < most ? parts : most;
+    return (int)(parts < 1 ? 1 : parts < ATTENTION_PARTS_MAX ? parts : ATTENTION_PARTS_MAX);
+}
+
 }  // namespace sc
