@@ -497,6 +497,29 @@ int sc_attention_bwd(const sc_heads* dout, const sc_heads* q, const sc_heads* k,
                      int causal, float scale, const sc_heads* dq, const sc_heads* dk, const sc_heads* dv,
                      int dtype, void* d_workspace, size_t workspace_bytes, void* stream);
 
+/* Group norm with an activation, channels last: over the rows of a scene and the C / groups consecutive channels of a group,
+ *   u = (x - mean) / sqrt(var + eps),  y = act(u gain + bias)
+ * with the variance over all of them (not one less), statistics in 32 bits or more.  groups = C: every channel by itself; groups = 1: all channels together.
+ *   d_x, d_y   [rows][C], ldx and ldy apart; d_gain, d_bias [C] or NULL (1 and 0)
+ *   d_starts   [scenes + 1] as above, NULL: one scene of all rows.  Rows of d_y of no scene are left untouched
+ *   eps        above 0
+ *   d_stats    [scenes][groups][2] or NULL: receives mean and 1 / sqrt(var + eps), what sc_group_norm_bwd needs; of a scene without rows 0 and 1 / sqrt(eps). 8-byte aligned
+ *   groups divides C <= SC_CHANNELS_MAX; scenes * groups <= SC_NORM_PAIRS_MAX
+ *   d_workspace  workspace_bytes >= sc_group_norm_workspace_bytes(...), 16-byte aligned, for both calls */
+#define SC_NORM_PAIRS_MAX 8388608    /* 2^23 */
+size_t sc_group_norm_workspace_bytes(int64_t rows, int scenes, int C, int groups);
+int sc_group_norm_fwd(const void* d_x, int64_t ldx, int64_t rows, const int32_t* d_starts, int scenes, int C, int groups,
+                      const void* d_gain, const void* d_bias, float eps, int act, void* d_y, int64_t ldy, float* d_stats,
+                      int dtype, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* Gradients of sc_group_norm_fwd: with dz = dy act'(u gain + bias),
+ *   dx = (dz gain - mean(dz gain) - u mean(dz gain u)) / sqrt(var + eps),  dgain = sum of dz u,  dbias = sum of dz     over the rows of all scenes
+ * each skipped where NULL (one at least is asked for).  d_stats is what the forward call stored.  Rows of d_dx of no scene are left untouched. */
+int sc_group_norm_bwd(const void* d_dy, int64_t lddy, const void* d_x, int64_t ldx, int64_t rows, const int32_t* d_starts, int scenes, int C, int groups,
+                      const void* d_gain, const void* d_bias, int act, const float* d_stats,
+                      void* d_dx, int64_t lddx, void* d_dgain, void* d_dbias,
+                      int dtype, void* d_workspace, size_t workspace_bytes, void* stream);
+
 /* ---- reading results back ------------------------------------------------------------------ */
 
 /* Fill n_pairs and per_offset from the kernel map (d_kmap may be NULL to skip that), copy the

@@ -45,7 +45,8 @@ SYMBOLS = ["sc_hash_bytes", "sc_hash_build", "sc_hash_rebuild", "sc_hash_lookup"
            "sc_conv_packed_bytes", "sc_conv_weight_pack", "sc_conv_fwd_packed", "sc_hash_probe_slot",
            "sc_linear_fwd", "sc_linear_workspace_bytes", "sc_linear_bwd", "sc_grouped_fwd", "sc_grouped_workspace_bytes",
            "sc_grouped_bwd", "sc_rope_table_bytes", "sc_rope_table", "sc_qk_rope_fwd", "sc_qk_rope_workspace_bytes",
-           "sc_qk_rope_bwd", "sc_attention_workspace_bytes", "sc_attention_fwd", "sc_attention_bwd_workspace_bytes", "sc_attention_bwd"]
+           "sc_qk_rope_bwd", "sc_attention_workspace_bytes", "sc_attention_fwd", "sc_attention_bwd_workspace_bytes", "sc_attention_bwd",
+           "sc_group_norm_workspace_bytes", "sc_group_norm_fwd", "sc_group_norm_bwd"]
 
 
 class ScCounts(ctypes.Structure):
@@ -135,6 +136,9 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
         "sc_attention_fwd": (i32, [heads, heads, heads, i64, i64, i32, vp, vp, vp, i32, i32, ctypes.c_float, heads, vp, i32, vp, sz, vp]),
         "sc_attention_bwd_workspace_bytes": (sz, [i64, i64, i32, i32, i32, i32, i32]),
         "sc_attention_bwd": (i32, [heads, heads, heads, heads, heads, vp, i64, i64, i32, vp, vp, vp, i32, i32, ctypes.c_float, heads, heads, heads, i32, vp, sz, vp]),
+        "sc_group_norm_workspace_bytes": (sz, [i64, i32, i32, i32]),
+        "sc_group_norm_fwd": (i32, [vp, i64, i64, vp, i32, i32, i32, vp, vp, ctypes.c_float, i32, vp, i64, vp, i32, vp, sz, vp]),
+        "sc_group_norm_bwd": (i32, [vp, i64, vp, i64, i64, vp, i32, i32, i32, vp, vp, i32, vp, vp, i64, vp, vp, i32, vp, sz, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -149,7 +153,7 @@ _NATIVE_CALLS = ["sc_hash_build", "sc_hash_rebuild", "sc_kmap_build", "sc_kmap_b
                  "sc_conv_fwd_packed", "sc_conv_up_fwd", "sc_conv_fwd_grid", "sc_grid_build", "sc_kmap_build_grid"]
 # ... and of its bind_rows()
 _NATIVE_ROW_CALLS = ["sc_linear_fwd", "sc_linear_bwd", "sc_grouped_fwd", "sc_grouped_bwd", "sc_qk_rope_fwd", "sc_qk_rope_bwd", "sc_attention_fwd",
-                     "sc_attention_bwd"]
+                     "sc_attention_bwd", "sc_group_norm_fwd", "sc_group_norm_bwd"]
 
 
 class _NativeOnFirstUse:
@@ -455,6 +459,27 @@ def sc_attention_bwd(grad_out, q, k, v, out, lse, grad_q, grad_k, grad_v, q_star
                                q.shape[-1] ** -0.5 if scale is None else scale, workspace, stream)
     if rc:
         _check(rc, "sc_attention_bwd")
+
+
+def sc_group_norm_workspace_bytes(rows: int, scenes: int, C: int, groups: int) -> int:
+    return load().sc_group_norm_workspace_bytes(rows, scenes, C, groups)
+
+
+def sc_group_norm_fwd(x, out, groups, starts=None, gain=None, bias=None, act="none", eps=1e-5, stats=None, workspace=None, stream=None):
+    """out = act((x - mean) / sqrt(var + eps) * gain + bias), x [rows, C], mean and variance over the rows of a scene (starts int32 [scenes + 1];
+    None: one scene) and the C / groups channels of a group; gain and bias [C] or None.  stats float32 [scenes, groups, 2] receives mean and
+    1 / sqrt(var + eps), what sc_group_norm_bwd needs; workspace uint8 [>= sc_group_norm_workspace_bytes(...)]."""
+    rc = _native.group_norm_fwd(x, out, groups, starts, gain, bias, ACTS[act], eps, stats, workspace, stream)
+    if rc:
+        _check(rc, "sc_group_norm_fwd")
+
+
+def sc_group_norm_bwd(grad_out, x, stats, grad_x, groups, starts=None, gain=None, bias=None, act="none", grad_gain=None, grad_bias=None, workspace=None,
+                      stream=None):
+    """Gradients of sc_group_norm_fwd, of x, gain and bias where a tensor is given for them; x and stats are that call's."""
+    rc = _native.group_norm_bwd(grad_out, x, stats, grad_x, groups, starts, gain, bias, ACTS[act], grad_gain, grad_bias, workspace, stream)
+    if rc:
+        _check(rc, "sc_group_norm_bwd")
 
 
 def sc_profile_enable(enable: bool):

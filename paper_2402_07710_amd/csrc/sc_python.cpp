@@ -45,6 +45,8 @@ struct RowLib {
     decltype(&sc_qk_rope_bwd) qk_rope_bwd;
     decltype(&sc_attention_fwd) attention_fwd;
     decltype(&sc_attention_bwd) attention_bwd;
+    decltype(&sc_group_norm_fwd) group_norm_fwd;
+    decltype(&sc_group_norm_bwd) group_norm_bwd;
 } row_lib;
 
 struct PyFailure {};      // a Python exception is set
@@ -487,6 +489,40 @@ int attention_bwd(Args a) {              // grad_out, q, k, v, out, lse, grad_q,
                     number(a[13]), &h[6], &h[7], &h[8], dtype(a[1]), ptr(a[14]), nbytes(a[14]), stream(a[15]));
 }
 
+int scenes_of_starts(PyObject* starts) {
+    const int64_t scenes = starts == Py_None ? 1 : size(starts, 0) - 1;
+    if (scenes < 1 || scenes > SC_SCENES_MAX) fail(PyExc_ValueError, "starts must be int32 [scenes + 1]");
+    return (int)scenes;
+}
+int group_norm_fwd(Args a) {             // x, out, groups, starts, gain, bias, act, eps, stats, workspace, stream
+    const Rows x = rows_of(tensor_given(a[0], "x"), "x"), out = rows_of(tensor_given(a[1], "out"), "out");
+    const int scenes = scenes_of_starts(a[3]), groups = small_int(a[2]);
+    check_rows(out, a[1], "out", x.n, x.C);
+    check_block(a[4], "gain", {x.C});
+    check_block(a[5], "bias", {x.C});
+    for (const int i : {1, 4, 5}) check_dtype(a[i], "an argument", a[0]);
+    const int32_t* starts = list_of(a[3], "starts", scenes + 1);
+    float* stats = floats_of(a[8], "stats", {scenes, groups, 2});
+    all_on_device(a, 11);
+    return unlocked(row_lib.group_norm_fwd, x.data, x.ld, x.n, starts, scenes, (int)x.C, groups, ptr(a[4]), ptr(a[5]), number(a[7]), small_int(a[6]), out.data, out.ld,
+                    stats, dtype(a[0]), ptr(a[9]), nbytes(a[9]), stream(a[10]));
+}
+int group_norm_bwd(Args a) {             // grad_out, x, stats, grad_x, groups, starts, gain, bias, act, grad_gain, grad_bias, workspace, stream
+    const Rows grad = rows_of(tensor_given(a[0], "grad_out"), "grad_out"), x = rows_of(tensor_given(a[1], "x"), "x"), grad_x = rows_of(a[3], "grad_x");
+    const int scenes = scenes_of_starts(a[5]), groups = small_int(a[4]);
+    check_rows(grad, a[0], "grad_out", x.n, x.C);
+    check_rows(grad_x, a[3], "grad_x", x.n, x.C);
+    const char* const names[4] = {"gain", "bias", "grad_gain", "grad_bias"};
+    const int of_channels[4] = {6, 7, 9, 10};
+    for (int i = 0; i < 4; ++i) check_block(a[of_channels[i]], names[i], {x.C});
+    for (const int i : {0, 3, 6, 7, 9, 10}) check_dtype(a[i], "an argument", a[1]);
+    const int32_t* starts = list_of(a[5], "starts", scenes + 1);
+    const float* stats = floats_of(tensor_given(a[2], "stats"), "stats", {scenes, groups, 2});
+    all_on_device(a, 13);
+    return unlocked(row_lib.group_norm_bwd, grad.data, grad.ld, x.data, x.ld, x.n, starts, scenes, (int)x.C, groups, ptr(a[6]), ptr(a[7]), small_int(a[8]), stats,
+                    grad_x.data, grad_x.ld, ptr(a[9]), ptr(a[10]), dtype(a[1]), ptr(a[11]), nbytes(a[11]), stream(a[12]));
+}
+
 template <int (*F)(Args), int N>
 PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (nargs != N) {
@@ -545,6 +581,8 @@ PyMethodDef methods[] = {
     SC_METHOD(qk_rope_bwd, 16),
     SC_METHOD(attention_fwd, 12),
     SC_METHOD(attention_bwd, 16),
+    SC_METHOD(group_norm_fwd, 11),
+    SC_METHOD(group_norm_bwd, 13),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "argument marshalling for libsc's calls", -1, methods,

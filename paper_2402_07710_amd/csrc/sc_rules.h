@@ -304,4 +304,16 @@ constexpr int attention_parts(AttentionShape shape, int64_t columns, int64_t sce
     return (int)(parts < 1 ? 1 : parts < ATTENTION_PARTS_MAX ? parts : ATTENTION_PARTS_MAX);
 }
 
+// ---- group norm (sc_norm.hip) -------------------------------------------------------------------------------
+// Rows of a unit: some eight chunks of eight channels a thread, and no more than about 4096 units, whose sums are joined.
+constexpr int norm_rows(int64_t rows, int C) {
+    const int chunks = (C + 7) / 8;
+    int64_t per = 1;
+    while (per * chunks < 2048 && per < 1024) per *= 2;
+    while (rows / per > 4096) per *= 2;
+    return (int)per;
+}
+// One launch, a workgroup for a scene's group, whose rows may all be of one scene.
+constexpr bool norm_few(int64_t rows, int channels) { return rows * channels <= 8192; }
+
 }  // namespace sc

@@ -1,0 +1,133 @@
+"""GPU tests of the group norm with an activation, forward and backward, against the definition in 64 bits.
+
+Tolerances follow from the roundings, f = 2^-24.  A workgroup sums up to `per` deviations from its first row, at most 2 K each (K: the largest from the mean),
+so the mean is off by (per + 8) 2 K f and its own rounding, 2 f |mean|, and the variance by (per + 8) 8 K^2 f; 1 / deviation is off by half the variance's share.
+Activations of 16-bit rows are off by 1e-6 (1 + |v|), f32's by 8 f (1 + |v|), their slopes as much; no slope is above 1.13 or steeper than 1.  Then one rounding to the rows' type.
+"""
+import math
+
+import pytest
+import torch
+
+from paper_2402_07710_amd import binding as sc
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F = 2.0 ** -24
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+PER = 1024                          # rows of a unit at most
+
+
+def act_of(name):
+    return {"none": lambda t: t, "relu": torch.relu, "gelu": torch.nn.functional.gelu, "silu": torch.nn.functional.silu}[name]
+
+
+def starts_of(lens, at=0):
+    out = [at]
+    for n in lens:
+        out.append(out[-1] + n)
+    return torch.tensor(out, dtype=torch.int32, device=DEV)
+
+
+def inside(name, got, want, off):
+    got = got.double().cpu()
+    worst = float(((got - want).abs() / off).max()) if want.numel() else 0.0
+    print(f"{name} {worst:.3f} of its tolerance", flush=True)
+    assert torch.isfinite(got).all() and worst <= 1.0, (name, worst)
+
+
+def run(lens, C, groups, dt, act, *, lead=0, trail=0, pad=0, gains=True, mean=1.0, spread=1.0, eps=1e-5, seed=0, use_starts=True):
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(seed)
+    rows = lead + sum(lens) + trail
+
+    def normal(*shape, scale=1.0):
+        return (torch.randn(shape, generator=gen, device=DEV) * scale).to(dt)
+    x = (torch.randn((rows, C + pad), generator=gen, device=DEV) * spread + mean * torch.randn(C + pad, generator=gen, device=DEV)).to(dt)[:, :C]
+    grad = normal(rows, C + pad, scale=1 / 16)[:, :C]
+    gain, bias = ((1 + normal(C, scale=0.2).float()).to(dt), normal(C, scale=0.2)) if gains else (None, None)
+    starts = starts_of(lens, lead) if use_starts else None
+    workspace = torch.full((sc.sc_group_norm_workspace_bytes(rows, len(lens), C, groups),), 0xff, dtype=torch.uint8, device=DEV)
+    wide = torch.full((rows, C + pad), 7.0, dtype=dt, device=DEV)
+    out, stats = wide[:, :C], torch.full((len(lens), groups, 2), 7.0, device=DEV)
+    sc.sc_group_norm_fwd(x, out, groups, starts, gain, bias, act, eps, stats, workspace)
+    wide_grad = torch.full((rows, C + pad), 7.0, dtype=dt, device=DEV)
+    grad_x, grad_gain, grad_bias = wide_grad[:, :C], torch.full((C,), 7.0, dtype=dt, device=DEV), torch.full((C,), 7.0, dtype=dt, device=DEV)
+    workspace.fill_(0xff)
+    sc.sc_group_norm_bwd(grad, x, stats, grad_x, groups, starts, gain, bias, act, grad_gain, grad_bias, workspace)
+    for t in (wide, wide_grad):                     # rows of no scene and the channels behind the rows
+        assert (t[:lead] == 7).all() and (t[lead + sum(lens):] == 7).all() and (t[:, C:] == 7).all()
+
+    u16 = torch.finfo(dt).eps / 2
+    least = {torch.float32: 1e-37, torch.float16: 2.0 ** -25, torch.bfloat16: 1e-37}[dt]
+    fault = 8 * F if dt == torch.float32 else 1e-6
+    g64 = gain.double().cpu() if gains else torch.ones(C, dtype=torch.float64)
+    b64 = bias.double().cpu() if gains else torch.zeros(C, dtype=torch.float64)
+    total = torch.zeros(4, C, dtype=torch.float64)
+    at, n_ch = lead, C // groups
+    for s, n in enumerate(lens):
+        m = slice(at, at + n)
+        at += n
+        if n == 0:
+            assert torch.equal(stats[s, :, 0], torch.zeros(groups, device=DEV))
+            assert torch.allclose(stats[s, :, 1].double(), torch.full((groups,), eps ** -0.5, dtype=torch.float64, device=DEV), rtol=2 * F)
+            continue
+        X, dy = x[m].double().cpu().unflatten(1, (groups, n_ch)), grad[m].double().cpu()
+        mu, var = X.mean((0, 2), keepdim=True), X.var((0, 2), unbiased=False, keepdim=True)
+        K = (X - mu).abs().amax((0, 2), keepdim=True)
+        off_mu = (PER + 8) * 2 * K * F + 2 * F * mu.abs()
+        rel = ((PER + 8) * 8 * K * K * F + 2 * (off_mu * off_mu)) / (var + eps) / 2 + 4 * F
+        inside("mean", stats[s, :, 0], mu.flatten(), off_mu.flatten() + 1e-37)
+        scale = 1 / torch.sqrt(var + eps)
+        inside("scale", stats[s, :, 1], scale.flatten(), (rel * scale).flatten())
+        U = (X - mu) * scale
+        off_u = (off_mu + 2 * F * (X - mu).abs()) * scale * (1 + rel) + U.abs() * (rel + 2 * F)
+        U, off_u = U.flatten(1), off_u.flatten(1)
+        pre = (U * g64 + b64).requires_grad_(True)
+        off_pre = off_u * g64.abs() + 2 * F * ((U * g64).abs() + pre.detach().abs())
+        y = act_of(act)(pre)
+        off_y = 1.13 * off_pre + (fault * (1 + pre.detach().abs()) if act != "none" else 0.0)
+        inside("out", out[m], y.detach(), off_y + u16 * (y.detach().abs() + off_y) + least)
+        y.backward(dy)
+        dz = pre.grad
+        off_dz = dy.abs() * ((off_pre + fault) if act in ("gelu", "silu") else 0.0) + 2 * F * dz.abs()
+        total[0] += dz.sum(0)
+        total[1] += off_dz.sum(0) + (PER + 8) * F * dz.abs().sum(0)
+        along = dz * U
+        off_along = off_dz * (U.abs() + off_u) + dz.abs() * off_u + F * along.abs()
+        total[2] += along.sum(0)
+        total[3] += off_along.sum(0) + (PER + 8) * F * along.abs().sum(0)
+        count = n * n_ch
+
+        def mean_of(v):
+            return ((v.sum(0)).unflatten(0, (groups, n_ch)).sum(1) / count).repeat_interleave(n_ch)
+        m1, m2 = mean_of(dz * g64), mean_of(along * g64)
+        off_1 = mean_of((off_dz + (PER + 8) * F * dz.abs()) * g64.abs()) + F * m1.abs()
+        off_2 = mean_of((off_along + (PER + 8) * F * along.abs()) * g64.abs()) + F * m2.abs()
+        r, rel_r = scale.flatten().repeat_interleave(n_ch), rel.flatten().repeat_interleave(n_ch)
+        dx = (dz * g64 - m1 - U * m2) * r
+        size = (dz * g64).abs() + m1.abs() + (U * m2).abs()
+        off_dx = (off_dz * g64.abs() + off_1 + U.abs() * off_2 + off_u * (m2.abs() + off_2) + 4 * F * size) * r * (1 + rel_r) + rel_r * dx.abs()
+        inside("dx", grad_x[m], dx, off_dx + u16 * (dx.abs() + off_dx) + least)
+    inside("dbias", grad_bias, total[0], total[1] + u16 * (total[0].abs() + total[1]) + least)
+    inside("dgain", grad_gain, total[2], total[3] + u16 * (total[2].abs() + total[3]) + least)
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("C,groups", [(1, 1), (7, 7), (8, 2), (12, 3), (45, 9), (64, 8), (64, 1), (64, 64), (256, 32), (513, 3), (2056, 257), (4100, 2)])
+def test_channels(C, groups, dt):
+    run([70, 33], C, groups, dt, "silu")
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("act", ["none", "gelu", "silu"])
+@pytest.mark.parametrize("lens", [[1], [5], [0, 3, 0], [1, 1, 1, 1], [1000, 0, 1, 513, 64], [9000], [2] * 200])
+def test_scenes(lens, act, dt):
+    run(lens, 24, 6, dt, act, lead=3, trail=2, pad=3)
+
+
+@pytest.mark.parametrize("dt", TYPES)
+def test_far_from_zero_and_without_gains(dt):
+    run([800, 500], 32, 4, dt, "none", mean=100.0, spread=0.5)
+    run([800], 32, 32, dt, "gelu", gains=False, use_starts=False)
+    run([4000], 32, 2, dt, "silu", spread=1e-3, mean=0.0, eps=1e-3)
