@@ -471,7 +471,7 @@ int sc_qk_rope_bwd(const sc_heads* dq_out, const sc_heads* dk_out, const sc_head
  *   s_j = scale q_i . k_j,   w = softmax of s over the keys seen,   out_i = sum of w_j v_j,   lse_i = log of the sum of exp(s_j)
  * Queries see all keys of their scene, or with causal = 1 those with j - i <= nk - nq: a scene's queries are its last rows, so the next row of a
  * sequence sees all that is kept of it.  A query that sees no key gets zeros and lse = minus infinity.  Head h of the queries goes with head h / (q->heads / k->heads) of keys and values.
- *   q, out      q_rows x q->heads x D;  k, v  k_rows x k->heads x D; `row` and `head` elements apart, heads of `out` apart from each other
+ *   q, out      q_rows x q->heads x D;  k, v  k_rows x k->heads x D; `row` and `head` elements apart, rows by SC_ATTENTION_LD_MAX at most, heads of `out` apart from each other
  *   d_q_starts, d_k_starts  [scenes + 1] as d_starts above, in rows of queries and of keys; d_k_starts NULL: the same (then q_rows == k_rows); both NULL: one scene of all rows.
  *              Rows of `out` and d_lse of no scene are left untouched
  *   d_k_lens   [scenes] or NULL: only that many of a scene's keys count, the first ones (a cache with room behind them, which is not read)
@@ -481,6 +481,7 @@ int sc_qk_rope_bwd(const sc_heads* dq_out, const sc_heads* dk_out, const sc_head
  *   d_workspace  workspace_bytes >= sc_attention_workspace_bytes(...), which may be 0; 16-byte aligned
  * 16-bit weights are rounded to the rows' type ahead of their product with the values; sums are in 32 bits. */
 #define SC_ATTENTION_HEAD_MAX 256
+#define SC_ATTENTION_LD_MAX   16777216LL    /* 2^24 */
 #define SC_SCENES_MAX         SC_N_MAX
 size_t sc_attention_workspace_bytes(int64_t q_rows, int64_t k_rows, int scenes, int q_heads, int k_heads, int D, int dtype);
 int sc_attention_fwd(const sc_heads* q, const sc_heads* k, const sc_heads* v, int64_t q_rows, int64_t k_rows, int D,

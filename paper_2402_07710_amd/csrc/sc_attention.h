@@ -36,16 +36,22 @@ struct Attention {
     // backward
     HeadRows dout, dq, dk, dv;
     int64_t k_units;
+    int k_parts, part_rows;            // of the queries that the keys' columns walk
+    float *part_dk, *part_dv;          // [part][k_rows][k_heads][D]
     float *against, *delta;            // [q_heads][q_rows]: lse times log2 e, infinite for a row that sees nothing; sum(do o)
 };
 
-__device__ inline Scene scene_of_queries(const Attention& p, int tile, int64_t u) {
+// log2 of a tile of columns
+constexpr int log2_of(int tile) { return tile == 16 ? 4 : tile == 32 ? 5 : tile == 64 ? 6 : tile == 128 ? 7 : 8; }
+__device__ inline Scene scene_of_queries(const Attention& p, int log2, int64_t u) {
     int64_t first = 0, first_k = 0;
     int count = 0, count_k = 0, scene;
-    Scene s = find_scene(p.q_starts, p.scenes, p.q_rows, p.per, tile, u, first, count, scene);
+    Scene s = find_scene(p.q_starts, p.scenes, p.q_rows, p.per, log2, u, first, count, scene);
     s.tile = __builtin_amdgcn_readfirstlane(s.tile);
     if (s.tile < 0) return s;
-    scene_rows(p.k_starts, p.k_lens, p.k_rows, scene, first_k, count_k);
+    first_k = first;
+    count_k = count;
+    if (p.k_starts != p.q_starts || p.k_lens != nullptr || p.k_rows != p.q_rows) scene_rows(p.k_starts, p.k_lens, p.k_rows, scene, first_k, count_k);
     s.q0 = uniform64(first);
     s.nq = __builtin_amdgcn_readfirstlane(count);
     s.k0 = uniform64(first_k);
@@ -74,31 +80,50 @@ struct HeadShape {
     static constexpr int STEP = DT == SC_F32 ? 16 : 32;   // rows that a step of the second product takes
 };
 
-// The loads of one operand's tiles by NTH threads: rows first .. of a scene's head.  Zeros stand for rows that are not there and for channels beyond D.
+// 16 bytes a lane straight into LDS as load_to_lds, from an address that the wavefront shares and an offset of the lane's.
+__device__ inline void load_to_lds_at(const void* base, uint32_t offset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "m0", "memory");
+}
+// The loads of one operand's tiles by NTH threads: rows first .. of a scene's head.  Zeros stand for rows that are not there and for channels beyond D: whole chunks of those
+// are cleared once, by clear(), and never written again.
 template <int DT, int DPAD, int ROWS, int NTH>
 struct TileLoader {
     using H = HeadShape<DT, DPAD>;
-    static constexpr int PASSES = ROWS * H::LINE / NTH;
-    static_assert(ROWS * H::LINE % NTH == 0, "whole passes");
+    static constexpr int PASSES = ROWS * H::LINE / NTH, LINES = NTH / H::LINE;       // lines of a pass
+    static_assert(ROWS * H::LINE % NTH == 0 && NTH % H::LINE == 0 && PASSES > 0, "whole passes of whole lines");
     const char* base;                  // of the scene's first row
     int64_t row;
     int D;
-    __device__ __forceinline__ void fetch(int first, int left, uint32_t lds) const {
-        const int tid = (int)threadIdx.x % NTH, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-        const bool inside = left >= ROWS && D == DPAD;
-        const char* const from = base + (int64_t)first * row;
+    // The turn of a line is the exclusive or of its bits' turns, so that of a pass's line follows from the first pass's.
+    __device__ __forceinline__ static int chunk_of(int i) {
+        const int tid = (int)threadIdx.x % NTH;
+        return (tid % H::LINE) ^ tile_turn<DT, H::LINE>(tid / H::LINE) ^ tile_turn<DT, H::LINE>(i * LINES);
+    }
+    __device__ __forceinline__ void clear(uint32_t lds) const {
+        const int tid = (int)threadIdx.x % NTH;
 #pragma unroll
-        for (int i = 0; i < PASSES; ++i) {
-            const int slot = i * NTH + tid, line = slot / H::LINE, chunk = (slot % H::LINE) ^ tile_turn<DT, H::LINE>(line);
-            const char* src = from + (int64_t)line * row + chunk * 16;
-            const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (i * NTH + wave * 64) * 16);
-            if (inside) {
-                load_to_lds(src, to);
-                continue;
+        for (int i = 0; i < PASSES; ++i)
+            if (chunk_of(i) * H::PER >= D) *(__attribute__((address_space(3))) u32x4*)(lds + (i * NTH + tid) * 16) = u32x4{0, 0, 0, 0};
+    }
+    __device__ __forceinline__ void fetch(int first, int left, uint32_t lds) const {
+        const int tid = (int)threadIdx.x % NTH, wave = __builtin_amdgcn_readfirstlane(tid >> 6), line = tid / H::LINE;
+        const char* const from = (const char*)uniform64((int64_t)(base + (int64_t)first * row));
+        if (left >= ROWS && D % H::PER == 0) {
+            const uint32_t offset = (uint32_t)line * (uint32_t)row;
+#pragma unroll
+            for (int i = 0; i < PASSES; ++i) {
+                const int chunk = chunk_of(i);
+                if (D == DPAD || chunk * H::PER < D)
+                    load_to_lds_at((const void*)uniform64((int64_t)(from + (int64_t)(i * LINES) * row)), offset + chunk * 16, __builtin_amdgcn_readfirstlane(lds + (i * NTH + wave * 64) * 16));
             }
-            const int there = line < left ? D - chunk * H::PER : 0;
+            return;
+        }
+#pragma unroll 1
+        for (int i = 0; i < PASSES; ++i) {
+            const int at = line + i * LINES, chunk = (tid % H::LINE) ^ tile_turn<DT, H::LINE>(at), there = at < left ? D - chunk * H::PER : 0;
+            const char* const src = from + (int64_t)at * row + chunk * 16;
             if (there >= H::PER || there <= 0) {
-                load_to_lds(there > 0 ? (const void*)src : (const void*)&g_no_chunk, to);
+                load_to_lds(there > 0 ? (const void*)src : (const void*)&g_no_chunk, __builtin_amdgcn_readfirstlane(lds + (i * NTH + wave * 64) * 16));
             } else {
                 uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -107,7 +132,7 @@ struct TileLoader {
                         if constexpr (DT == SC_F32) w[j] = reinterpret_cast<const uint32_t*>(src)[j];
                         else w[j / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(src)[j] << (16 * (j & 1));
                     }
-                *(__attribute__((address_space(3))) u32x4*)(lds + slot * 16) = u32x4{w[0], w[1], w[2], w[3]};
+                *(__attribute__((address_space(3))) u32x4*)(lds + (i * NTH + tid) * 16) = u32x4{w[0], w[1], w[2], w[3]};
             }
         }
     }
@@ -234,35 +259,64 @@ struct Running {
     float sum;
 };
 
-template <int DT, int DPAD, int NB, bool SPLIT>
-constexpr int attention_tile() {       // keys
-    return DPAD * ELEM<DT> >= 512 || SPLIT ? 32 : 64;
+// SHARED: a wavefront has 16 NB columns of its own, and all walk the same tiles.  SPLIT: the wavefronts share 16 NB columns and take every WAVES-th tile each.
+// ALONE: a wavefront has columns and tiles to itself, neighbours the next head of the same scene: rows of short heads share lines of memory.
+enum Share { SHARED, SPLIT, ALONE };
+template <int DT, int DPAD, int SHARE>
+constexpr int walked_tile() {          // rows
+    constexpr int BYTES = DPAD * ELEM<DT>;
+    if (SHARE == SHARED) return BYTES >= 512 ? 32 : 64;
+    return DT == SC_F32 && BYTES >= 512 ? 16 : 32;
 }
-template <int DT, int DPAD, int WAVES, int NB, bool SPLIT>
-constexpr size_t attention_lds() {
-    return (size_t)(SPLIT ? WAVES : 1) * 4 * attention_tile<DT, DPAD, NB, SPLIT>() * DPAD * ELEM<DT>;
+template <int DT, int DPAD, int SHARE>
+constexpr int walked_bytes() {         // two operands, two buffers; of a wavefront if it has its own
+    return 4 * walked_tile<DT, DPAD, SHARE>() * DPAD * ELEM<DT>;
+}
+template <int DT, int DPAD, int SHARE>
+constexpr int wavefronts() {
+    constexpr int BYTES = walked_bytes<DT, DPAD, SHARE>();
+    if (SHARE == SHARED) return 4;
+    if (SHARE == SPLIT) return BYTES > 32768 ? 2 : 4;
+    return BYTES > 32768 ? 1 : BYTES > 16384 ? 2 : 4;
+}
+// What a workgroup, or a wavefront ALONE, works on: neighbours have the heads of one unit.
+struct Item {
+    int64_t unit;
+    int head, part;
+};
+template <int SHARE, int WAVES>
+__device__ inline Item item_of(int k_heads, int parts) {
+    uint32_t n = blockIdx.y * gridDim.x + blockIdx.x;
+    if constexpr (SHARE == ALONE) {    // runs of four workgroups to an XCD
+        n = ((n / (4 * NUM_XCD) * NUM_XCD + n % NUM_XCD) * 4 + n / NUM_XCD % 4) * WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    }
+    const uint32_t rest = n / (uint32_t)k_heads, unit = rest / (uint32_t)parts;
+    return Item{unit, (int)(n - rest * (uint32_t)k_heads), (int)(rest - unit * (uint32_t)parts)};
+}
+// The share of `all` steps that a part has: equal ones, but no more parts than there is `least` for.
+__device__ inline void part_of(int all, int part, int parts, int64_t used, int& from, int& to) {
+    used = used < parts ? used : parts;
+    from = part < used ? (int)((int64_t)all * part / used) : 0;
+    to = part < used ? (int)((int64_t)all * (part + 1) / used) : 0;
 }
 
-// SPLIT: the wavefronts share 16 NB columns and take every WAVES-th tile of the keys each; otherwise each has 16 NB columns of its own and all share the tiles.
-template <int DT, int DPAD, int WAVES, int NB, bool SPLIT>
-__global__ void __launch_bounds__(64 * WAVES, 2)
+template <int DT, int DPAD, int NB, int SHARE>
+__global__ void __launch_bounds__((64 * wavefronts<DT, DPAD, SHARE>()), (DT == SC_F32 && DPAD >= 128 ? 1 : 2))
 k_attention(const Attention p) {
     using H = HeadShape<DT, DPAD>;
-    constexpr int KT = attention_tile<DT, DPAD, NB, SPLIT>(), ST = KT / 16, TILE_BYTES = KT * H::BYTES;
-    constexpr int COLUMNS = 16 * NB * (SPLIT ? 1 : WAVES);
+    constexpr int WAVES = wavefronts<DT, DPAD, SHARE>(), KT = walked_tile<DT, DPAD, SHARE>(), ST = KT / 16, TILE_BYTES = KT * H::BYTES;
+    constexpr int COLUMNS = 16 * NB * (SHARE == SHARED ? WAVES : 1);
     extern __shared__ __align__(16) uint4 attention_lds_words[];
-    // heads of keys first: workgroups that share keys and values go to one XCD where there are as many heads
-    const uint32_t block = blockIdx.y * gridDim.x + blockIdx.x, rest = block / (uint32_t)p.k_heads;
-    const int head_k = (int)(block - rest * (uint32_t)p.k_heads);
-    const int part = (int)(rest % (uint32_t)p.parts);
-    const int64_t unit = p.units - 1 - rest / (uint32_t)p.parts;  // the last first: behind a causal mask they take longest
+    const Item item = item_of<SHARE, WAVES>(p.k_heads, p.parts);
+    const int head_k = item.head, part = item.part;
+    const int64_t unit = p.units - 1 - item.unit;                 // the last first: behind a causal mask they take longest
     if (unit < 0) return;
-    const Scene scene = scene_of_queries(p, COLUMNS, unit);
+    const Scene scene = scene_of_queries(p, log2_of(COLUMNS), unit);
     if (scene.tile < 0) return;
 
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int columns = scene.nq * p.per, column0 = scene.tile * COLUMNS + (SPLIT ? 0 : wave * 16 * NB);
+    const int columns = scene.nq * p.per, column0 = scene.tile * COLUMNS + (SHARE == SHARED ? wave * 16 * NB : 0);
     const int ahead = scene.nk - scene.nq;
     // keys that a column sees: those below its limit
     auto limit_of = [&](int column) {
@@ -288,16 +342,11 @@ k_attention(const Attention p) {
     const int all_last = scene.tile * COLUMNS + COLUMNS < columns ? scene.tile * COLUMNS + COLUMNS - 1 : columns - 1;
     const int tiles = (__builtin_amdgcn_readfirstlane(limit_of(all_last)) + KT - 1) / KT;
     int from = 0, to = tiles;
-    if (p.parts > 1) {                                            // equal parts, not below a least number of tiles
-        int used = (tiles * KT + p.part_keys - 1) / p.part_keys;
-        used = used < p.parts ? used : p.parts;
-        from = part < used ? (int)((int64_t)tiles * part / used) : 0;
-        to = part < used ? (int)((int64_t)tiles * (part + 1) / used) : 0;
-    }
+    if (p.parts > 1) part_of(tiles, part, p.parts, ((int64_t)tiles * KT + p.part_keys - 1) / p.part_keys, from, to);
 
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)attention_lds_words;
-    const uint32_t mine = lds0 + (SPLIT ? wave * (4 * TILE_BYTES) : 0);
-    TileLoader<DT, DPAD, KT, SPLIT ? 64 : 64 * WAVES> keys{p.k.data + scene.k0 * p.k.row + head_k * p.k.head, p.k.row, p.D},
+    const uint32_t mine = lds0 + (SHARE == SHARED ? 0 : wave * (4 * TILE_BYTES));
+    const TileLoader<DT, DPAD, KT, SHARE == SHARED ? 64 * WAVES : 64> keys{p.k.data + scene.k0 * p.k.row + head_k * p.k.head, p.k.row, p.D},
         values{p.v.data + scene.k0 * p.v.row + head_k * p.v.head, p.v.row, p.D};
     const RowReader<DT, DPAD> rows(mine);
     const ChannelReader<DT, DPAD> channels(mine + TILE_BYTES);
@@ -309,17 +358,21 @@ k_attention(const Attention p) {
 #pragma unroll
         for (int c = 0; c < H::CB; ++c) out[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    constexpr int STRIDE = SPLIT ? WAVES : 1;
+    constexpr int STRIDE = SHARE == SPLIT ? WAVES : 1;
+    if (p.D < DPAD) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) keys.clear(mine + b * TILE_BYTES);
+    }
     auto bring = [&](int t, uint32_t buffer) __attribute__((always_inline)) {
         keys.fetch(t * KT, scene.nk - t * KT, mine + buffer);
         values.fetch(t * KT, scene.nk - t * KT, mine + buffer + TILE_BYTES);
     };
     uint32_t buffer = 0;
-    const int begin = from + (SPLIT ? wave : 0);
+    const int begin = from + (SHARE == SPLIT ? wave : 0);
     if (begin < to) bring(begin, 0);
     for (int t = begin; t < to; t += STRIDE) {
         loads_done();
-        if constexpr (!SPLIT) lds_barrier();
+        if constexpr (SHARE == SHARED) lds_barrier();
         else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (t + STRIDE < to) bring(t + STRIDE, buffer ^ (2 * TILE_BYTES));
         const int key0 = t * KT;
@@ -399,13 +452,13 @@ k_attention(const Attention p) {
 #pragma unroll
     for (int n = 0; n < NB; ++n) run[n].sum = over_quarters_sum(run[n].sum);
 
-    if constexpr (SPLIT) {                                        // the wavefronts' columns come together: wavefront w adds up every WAVES-th block of channels
+    if constexpr (SHARE == SPLIT) {                                        // the wavefronts' columns come together: wavefront w adds up every WAVES-th block of channels
         static_assert(NB == 1, "a block of columns");
         static_assert((16 * DPAD * 4 + 16 * 8) <= 4 * TILE_BYTES, "fits what the wavefront's tiles took");
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         float* const shared = reinterpret_cast<float*>(attention_lds_words);
-        constexpr int SHARE = TILE_BYTES;                         // floats from wavefront to wavefront: its own four tiles
-        float* const own = shared + wave * SHARE;
+        constexpr int APART = TILE_BYTES;                         // floats from wavefront to wavefront: its own four tiles
+        float* const own = shared + wave * APART;
         if (g == 0) {
             own[2 * i] = run[0].top == NO_SCORE ? NO_SCORE : run[0].against;
             own[2 * i + 1] = run[0].sum;
@@ -417,13 +470,13 @@ k_attention(const Attention p) {
         __syncthreads();
         float top = NO_SCORE;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, shared[w * SHARE + 2 * i]);
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, shared[w * APART + 2 * i]);
         float sum = 0.f, factor[WAVES];
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-            const float theirs = shared[w * SHARE + 2 * i];
+            const float theirs = shared[w * APART + 2 * i];
             factor[w] = theirs == NO_SCORE ? 0.f : __builtin_amdgcn_exp2f(theirs - top);
-            sum += theirs == NO_SCORE ? 0.f : factor[w] * shared[w * SHARE + 2 * i + 1];
+            sum += theirs == NO_SCORE ? 0.f : factor[w] * shared[w * APART + 2 * i + 1];
         }
         run[0].against = top == NO_SCORE ? 0.f : top;
         run[0].sum = sum;
@@ -434,7 +487,7 @@ k_attention(const Attention p) {
             for (int r = 0; r < 4; ++r) {
                 float v = 0.f;
 #pragma unroll
-                for (int w = 0; w < WAVES; ++w) v += factor[w] == 0.f ? 0.f : factor[w] * shared[w * SHARE + 32 + (16 * c + 4 * g + r) * 16 + i];
+                for (int w = 0; w < WAVES; ++w) v += factor[w] == 0.f ? 0.f : factor[w] * shared[w * APART + 32 + (16 * c + 4 * g + r) * 16 + i];
                 out[0][c][r] = v;
             }
         }
@@ -443,21 +496,21 @@ k_attention(const Attention p) {
     for (int n = 0; n < NB; ++n) {
         if (!there[n]) continue;
         const int64_t row = scene.q0 + row_of[n], entry = row * (p.k_heads * p.per) + head_of[n];
-        const bool first_writer = SPLIT ? wave == 0 && g == 0 : g == 0;
+        const bool first_writer = g == 0 && (SHARE != SPLIT || wave == 0);
         if (p.parts > 1) {
             const int64_t at = (int64_t)part * p.q_rows * (p.k_heads * p.per) + entry;
             if (first_writer) p.part_sums[at] = make_float2(run[n].against, run[n].sum);
             if (from < to) {
 #pragma unroll
                 for (int c = 0; c < H::CB; ++c)
-                    if (!SPLIT || c % WAVES == wave) store4<SC_F32>((char*)(p.part_out + at * p.D), 16 * c + 4 * g, p.D, out[n][c]);
+                    if (SHARE != SPLIT || c % WAVES == wave) store4<SC_F32>((char*)(p.part_out + at * p.D), 16 * c + 4 * g, p.D, out[n][c]);
             }
         } else {
             const float inverse = run[n].sum == 0.f ? 0.f : 1.f / run[n].sum;
             char* const to_row = p.out.data + row * p.out.row + head_of[n] * p.out.head;
 #pragma unroll
             for (int c = 0; c < H::CB; ++c)
-                if (!SPLIT || c % WAVES == wave) {
+                if (SHARE != SPLIT || c % WAVES == wave) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) out[n][c][r] *= inverse;
                     store4<DT>(to_row, 16 * c + 4 * g, p.D, out[n][c]);
@@ -471,37 +524,31 @@ k_attention(const Attention p) {
 // Two kernels, so that every gradient is summed by one wavefront in one order: queries' columns walk the keys, keys' columns walk the queries.  The weights are made
 // again in both from lse: seven products where five would do, and no atomics, no sums in memory.
 // The walked rows go through the registers 32 at a time.
-constexpr int SUB = 32, SUB_BLOCKS = SUB / 16;
+template <int DT, int DPAD, int SHARE>
+constexpr int SUB = walked_tile<DT, DPAD, SHARE>() < 32 ? 16 : 32;
 
-template <int DT, int DPAD>
-constexpr int grad_tile() {            // rows of a tile: two operands, two buffers
-    return DPAD * ELEM<DT> >= 512 ? 32 : 64;
-}
-template <int DT, int DPAD>
-constexpr size_t grad_lds() {
-    return (size_t)4 * grad_tile<DT, DPAD>() * DPAD * ELEM<DT> + 4 * 64 * sizeof(float);
-}
 template <int DT, int DPAD, int NB>
 constexpr int grad_waves(int rows, int results) {                 // wavefronts on a SIMD that the registers leave room for
-    return NB * (rows * HeadShape<DT, DPAD>::KS * 4 + results * HeadShape<DT, DPAD>::CB * 4) > 200 ? 1 : 2;
+    return NB * (rows * HeadShape<DT, DPAD>::KS * 4 + results * HeadShape<DT, DPAD>::CB * 4) > (DT == SC_F32 ? 180 : 200) ? 1 : 2;
 }
 
-template <int DT, int DPAD, int WAVES, int NB>
-__global__ void __launch_bounds__(64 * WAVES, (grad_waves<DT, DPAD, NB>(2, 1)))
+template <int DT, int DPAD, int NB, int SHARE>
+__global__ void __launch_bounds__((64 * wavefronts<DT, DPAD, SHARE>()), (grad_waves<DT, DPAD, NB>(2, 1)))
 k_attention_dq(const Attention p) {
     using H = HeadShape<DT, DPAD>;
-    constexpr int KT = grad_tile<DT, DPAD>(), TILE_BYTES = KT * H::BYTES, COLUMNS = 16 * NB * WAVES;
+    constexpr int WAVES = wavefronts<DT, DPAD, SHARE>(), KT = walked_tile<DT, DPAD, SHARE>(), TILE_BYTES = KT * H::BYTES, COLUMNS = 16 * NB * (SHARE == SHARED ? WAVES : 1);
+    constexpr int SUB = sc::SUB<DT, DPAD, SHARE>, SUB_BLOCKS = SUB / 16;
     extern __shared__ __align__(16) uint4 attention_lds_words[];
-    const uint32_t block = blockIdx.y * gridDim.x + blockIdx.x, rest = block / (uint32_t)p.k_heads;
-    const int head_k = (int)(block - rest * (uint32_t)p.k_heads);
-    const int64_t unit = p.units - 1 - (int64_t)rest;
+    const Item item = item_of<SHARE, WAVES>(p.k_heads, p.parts);
+    const int head_k = item.head, part = item.part;
+    const int64_t unit = p.units - 1 - item.unit;
     if (unit < 0) return;
-    const Scene scene = scene_of_queries(p, COLUMNS, unit);
+    const Scene scene = scene_of_queries(p, log2_of(COLUMNS), unit);
     if (scene.tile < 0) return;
 
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int columns = scene.nq * p.per, column0 = scene.tile * COLUMNS + wave * 16 * NB;
+    const int columns = scene.nq * p.per, column0 = scene.tile * COLUMNS + (SHARE == SHARED ? wave * 16 * NB : 0);
     const int ahead = scene.nk - scene.nq;
     auto limit_of = [&](int column) {
         if (!p.causal) return scene.nk;
@@ -542,7 +589,7 @@ k_attention_dq(const Attention p) {
             }
         }
         delta[n] = over_quarters_sum(sum);
-        if (there[n] && g == 0) {                                 // for the keys' kernel, a head's rows together
+        if (there[n] && g == 0 && part == 0) {                    // for the keys' kernel, a head's rows together
             p.against[(int64_t)head_of[n] * p.q_rows + row] = against[n];
             p.delta[(int64_t)head_of[n] * p.q_rows + row] = delta[n];
         }
@@ -555,8 +602,11 @@ k_attention_dq(const Attention p) {
     const int all_last = scene.tile * COLUMNS + COLUMNS < columns ? scene.tile * COLUMNS + COLUMNS - 1 : columns - 1;
     const int tiles = (__builtin_amdgcn_readfirstlane(limit_of(all_last)) + KT - 1) / KT;
 
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)attention_lds_words;
-    TileLoader<DT, DPAD, KT, 64 * WAVES> keys{p.k.data + scene.k0 * p.k.row + head_k * p.k.head, p.k.row, p.D},
+    int from = 0, to = tiles;
+    if (p.parts > 1) part_of(tiles, part, p.parts, ((int64_t)tiles * KT + p.part_keys - 1) / p.part_keys, from, to);
+
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)attention_lds_words + (SHARE == SHARED ? 0 : wave * (4 * TILE_BYTES));
+    const TileLoader<DT, DPAD, KT, SHARE == SHARED ? 64 * WAVES : 64> keys{p.k.data + scene.k0 * p.k.row + head_k * p.k.head, p.k.row, p.D},
         values{p.v.data + scene.k0 * p.v.row + head_k * p.v.head, p.v.row, p.D};
     const RowReader<DT, DPAD> rows(lds0);
     const ChannelReader<DT, DPAD> channels(lds0);
@@ -564,12 +614,17 @@ k_attention_dq(const Attention p) {
         keys.fetch(t * KT, scene.nk - t * KT, lds0 + buffer);
         values.fetch(t * KT, scene.nk - t * KT, lds0 + buffer + TILE_BYTES);
     };
+    if (p.D < DPAD) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) keys.clear(lds0 + b * TILE_BYTES);
+    }
     uint32_t buffer = 0;
-    if (tiles > 0) bring(0, 0);
-    for (int t = 0; t < tiles; ++t) {
+    if (from < to) bring(from, 0);
+    for (int t = from; t < to; ++t) {
         loads_done();
-        lds_barrier();
-        if (t + 1 < tiles) bring(t + 1, buffer ^ (2 * TILE_BYTES));
+        if constexpr (SHARE == SHARED) lds_barrier();
+        else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (t + 1 < to) bring(t + 1, buffer ^ (2 * TILE_BYTES));
 #pragma unroll 1
         for (int h = 0; h < KT / SUB; ++h) {
             const int key0 = t * KT + h * SUB;
@@ -624,9 +679,15 @@ k_attention_dq(const Attention p) {
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
         if (!there[n]) continue;
-        char* const to_row = p.dq.data + (scene.q0 + row_of[n]) * p.dq.row + head_of[n] * p.dq.head;
+        const int64_t row = scene.q0 + row_of[n];
+        float* const to_part = p.parts > 1 ? p.part_out + (((int64_t)part * p.q_rows + row) * (p.k_heads * p.per) + head_of[n]) * p.D : nullptr;
+        char* const to_row = p.dq.data + row * p.dq.row + head_of[n] * p.dq.head;
 #pragma unroll
         for (int c = 0; c < H::CB; ++c) {
+            if (p.parts > 1) {
+                store4<SC_F32>((char*)to_part, 16 * c + 4 * g, p.D, dq[n][c]);
+                continue;
+            }
 #pragma unroll
             for (int r = 0; r < 4; ++r) dq[n][c][r] *= p.scale;
             store4<DT>(to_row, 16 * c + 4 * g, p.D, dq[n][c]);
@@ -637,22 +698,26 @@ k_attention_dq(const Attention p) {
 // Stand for rows that are not there: a weight of zero.
 __device__ float g_no_weight = __builtin_inff();
 
-template <int DT, int DPAD, int WAVES, int NB>
-__global__ void __launch_bounds__(64 * WAVES, (grad_waves<DT, DPAD, NB>(2, 2)))
+constexpr int SUMS_BYTES = 4 * 64 * sizeof(float);
+template <int DT, int DPAD, int NB, int SHARE>
+__global__ void __launch_bounds__((64 * wavefronts<DT, DPAD, SHARE>()), (grad_waves<DT, DPAD, NB>(2, 2)))
 k_attention_dkv(const Attention p) {
     using H = HeadShape<DT, DPAD>;
-    constexpr int RT = grad_tile<DT, DPAD>(), TILE_BYTES = RT * H::BYTES, COLUMNS = 16 * NB * WAVES;
+    constexpr int WAVES = wavefronts<DT, DPAD, SHARE>(), RT = walked_tile<DT, DPAD, SHARE>(), TILE_BYTES = RT * H::BYTES, COLUMNS = 16 * NB * (SHARE == SHARED ? WAVES : 1);
+    constexpr int SUB = sc::SUB<DT, DPAD, SHARE>, SUB_BLOCKS = SUB / 16;
     extern __shared__ __align__(16) uint4 attention_lds_words[];
-    const uint32_t block = blockIdx.y * gridDim.x + blockIdx.x, rest = block / (uint32_t)p.k_heads;
-    const int head_k = (int)(block - rest * (uint32_t)p.k_heads);
-    const int64_t unit = rest;                                    // behind a causal mask the first take longest
+    const Item item = item_of<SHARE, WAVES>(p.k_heads, p.k_parts);
+    const int head_k = item.head, part = item.part;
+    const int64_t unit = item.unit;                               // behind a causal mask the first take longest
     if (unit >= p.k_units) return;
     int64_t k0 = 0, q0 = 0, first_all = 0;
     int nk = 0, nq = 0, all = 0, scene_at;
-    const int at = __builtin_amdgcn_readfirstlane(find_scene(p.k_starts, p.scenes, p.k_rows, 1, COLUMNS, unit, first_all, all, scene_at).tile);
+    const int at = __builtin_amdgcn_readfirstlane(find_scene(p.k_starts, p.scenes, p.k_rows, 1, log2_of(COLUMNS), unit, first_all, all, scene_at).tile);
     if (at < 0) return;
-    scene_rows(p.k_starts, p.k_lens, p.k_rows, scene_at, k0, nk);
-    scene_rows(p.q_starts, nullptr, p.q_rows, scene_at, q0, nq);
+    k0 = q0 = first_all;
+    nk = nq = all;
+    if (p.k_lens != nullptr) scene_rows(p.k_starts, p.k_lens, p.k_rows, scene_at, k0, nk);
+    if (p.q_starts != p.k_starts || p.q_rows != p.k_rows) scene_rows(p.q_starts, nullptr, p.q_rows, scene_at, q0, nq);
     k0 = uniform64(k0);
     q0 = uniform64(q0);
     nk = __builtin_amdgcn_readfirstlane(nk);
@@ -661,7 +726,7 @@ k_attention_dkv(const Attention p) {
 
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int column0 = at * COLUMNS + wave * 16 * NB, ahead = nk - nq;
+    const int column0 = at * COLUMNS + (SHARE == SHARED ? wave * 16 * NB : 0), ahead = nk - nq;
     uint4 k[NB][H::KS], v[NB][H::KS];
     f32x4 dk[NB][H::CB], dv[NB][H::CB];
 #pragma unroll
@@ -679,29 +744,37 @@ k_attention_dkv(const Attention p) {
     const int first_tile = first_row / RT < tiles ? first_row / RT : tiles;
     const int last_column = column0 + 16 * NB - 1 < nk ? column0 + 16 * NB - 1 : nk - 1;
 
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)attention_lds_words;
     constexpr uint32_t SUMS = 4 * TILE_BYTES;                     // exponents and deltas of a tile's rows, 64 words each, two buffers
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)attention_lds_words + (SHARE == SHARED ? 0 : wave * (SUMS + SUMS_BYTES));
     const RowReader<DT, DPAD> rows(lds0);
     const ChannelReader<DT, DPAD> channels(lds0);
     const int each = tiles - first_tile, total = each * p.per;
+    int from = 0, to = total;
+    if (p.k_parts > 1) part_of(total, part, p.k_parts, ((int64_t)total * RT + p.part_rows - 1) / p.part_rows, from, to);
     auto bring = [&](int n, int which) __attribute__((always_inline)) {
         const int h = n / each, t = first_tile + n - h * each, head = head_k * p.per + h, left = nq - t * RT;
-        const TileLoader<DT, DPAD, RT, 64 * WAVES> queries{p.q.data + q0 * p.q.row + head * p.q.head, p.q.row, p.D},
+        const TileLoader<DT, DPAD, RT, SHARE == SHARED ? 64 * WAVES : 64> queries{p.q.data + q0 * p.q.row + head * p.q.head, p.q.row, p.D},
             grads{p.dout.data + q0 * p.dout.row + head * p.dout.head, p.dout.row, p.D};
         queries.fetch(t * RT, left, lds0 + which * (2 * TILE_BYTES));
         grads.fetch(t * RT, left, lds0 + which * (2 * TILE_BYTES) + TILE_BYTES);
         const int64_t from = (int64_t)head * p.q_rows + q0 + t * RT + lane;
-        if (wave == 0 && lane < RT)
+        if ((SHARE != SHARED || wave == 0) && lane < RT)
             load_word_to_lds(lane < left ? (const void*)(p.against + from) : (const void*)&g_no_weight, __builtin_amdgcn_readfirstlane(lds0 + SUMS + which * 512));
-        if (wave == WAVES - 1 && lane < RT)
+        if ((SHARE != SHARED || wave == WAVES - 1) && lane < RT)
             load_word_to_lds(lane < left ? (const void*)(p.delta + from) : (const void*)&g_no_chunk, __builtin_amdgcn_readfirstlane(lds0 + SUMS + which * 512 + 256));
     };
-    if (total > 0) bring(0, 0);
+    if (p.D < DPAD) {
+        const TileLoader<DT, DPAD, RT, SHARE == SHARED ? 64 * WAVES : 64> tile{nullptr, 0, p.D};
+#pragma unroll
+        for (int b = 0; b < 4; ++b) tile.clear(lds0 + b * TILE_BYTES);
+    }
+    if (from < to) bring(from, 0);
     int which = 0;
-    for (int n = 0; n < total; ++n, which ^= 1) {
+    for (int n = from; n < to; ++n, which ^= 1) {
         loads_done();
-        lds_barrier();
-        if (n + 1 < total) bring(n + 1, which ^ 1);
+        if constexpr (SHARE == SHARED) lds_barrier();
+        else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (n + 1 < to) bring(n + 1, which ^ 1);
         const int row_tile = (first_tile + n % each) * RT;
 #pragma unroll 1
         for (int h = 0; h < RT / SUB; ++h) {
@@ -774,10 +847,16 @@ k_attention_dkv(const Attention p) {
     for (int n = 0; n < NB; ++n) {
         const int c = column0 + 16 * n + i;
         if (c >= nk) continue;
+        const int64_t at_part = (((int64_t)part * p.k_rows + k0 + c) * p.k_heads + head_k) * p.D;
         char* const to_k = p.dk.data + (k0 + c) * p.dk.row + head_k * p.dk.head;
         char* const to_v = p.dv.data + (k0 + c) * p.dv.row + head_k * p.dv.head;
 #pragma unroll
         for (int b = 0; b < H::CB; ++b) {
+            if (p.k_parts > 1) {
+                store4<SC_F32>((char*)(p.part_dk + at_part), 16 * b + 4 * g, p.D, dk[n][b]);
+                store4<SC_F32>((char*)(p.part_dv + at_part), 16 * b + 4 * g, p.D, dv[n][b]);
+                continue;
+            }
 #pragma unroll
             for (int r = 0; r < 4; ++r) dk[n][b][r] *= p.scale;
             store4<DT>(to_k, 16 * b + 4 * g, p.D, dk[n][b]);
@@ -785,36 +864,85 @@ k_attention_dkv(const Attention p) {
         }
     }
 }
+// Parts of a gradient added up, in their order: a workgroup has 16 rows of a scene.
+template <int DT>
+__global__ void __launch_bounds__(256)
+k_attention_grad_join(const int32_t* __restrict__ starts, const int32_t* __restrict__ lens, int scenes, int64_t rows, int heads, int D, int parts,
+                      const float* __restrict__ a, HeadRows to_a, float scale_a, const float* __restrict__ b, HeadRows to_b) {
+    int64_t first = 0;
+    int count = 0, scene;
+    const int tile = __builtin_amdgcn_readfirstlane(find_scene(starts, scenes, rows, 1, 4, (int64_t)blockIdx.y * gridDim.x + blockIdx.x, first, count, scene).tile);
+    if (tile < 0) return;
+    if (lens != nullptr) scene_rows(starts, lens, rows, scene, first, count);
+    const int here = count - tile * 16 < 16 ? count - tile * 16 : 16, fours = (D + 3) / 4, row_items = heads * fours;
+    const int64_t row0 = first + tile * 16, apart = rows * heads * D;
+    for (int i = threadIdx.x; i < here * row_items; i += 256) {
+        const int r = i / row_items, head = (i - r * row_items) / fours, channel = (i - r * row_items - head * fours) * 4;
+        const int64_t at = ((row0 + r) * heads + head) * D + channel;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            const float* const from = w == 0 ? a : b;
+            if (from == nullptr) continue;
+            f32x4 v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+            for (int k = 0; k < parts; ++k) {
+                const float* const x = from + k * apart + at;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] += channel + j < D ? x[j] : 0.f;
+            }
+            const HeadRows to = w == 0 ? to_a : to_b;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] *= w == 0 ? scale_a : 1.f;
+            store4<DT>(to.data + (row0 + r) * to.row + head * to.head, channel, D, v);
+        }
+    }
+}
 
-// Parts joined: a thread has four channels of a row's head.
+// Parts joined: a workgroup has a row's head, its threads four channels and every so many of the parts.
 template <int DT>
 __global__ void __launch_bounds__(256)
 k_attention_join(const Attention p, int64_t entries, int q_heads) {
-    const int fours = (p.D + 3) / 4;
-    const int64_t item = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t entry = item / fours;
+    __shared__ float factors[ATTENTION_PARTS_MAX];
+    __shared__ float2 of_wave[4];
+    __shared__ f32x4 shared[256];
+    const int64_t entry = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
     if (entry >= entries) return;
     const int64_t row = entry / q_heads;
     if (p.q_starts != nullptr && (row < p.q_starts[0] || row >= p.q_starts[p.scenes])) return;        // a row of no scene stays as it is
-    const int channel = (int)(item - entry * fours) * 4;
-    float top = NO_SCORE;
-#pragma unroll 4
-    for (int k = 0; k < p.parts; ++k) {
-        const float2 s = p.part_sums[k * entries + entry];
-        top = s.y == 0.f ? top : fmaxf(top, s.x);
-    }
-    float sum = 0.f;
-    f32x4 v{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int k = 0; k < p.parts; ++k) {
-        const float2 s = p.part_sums[k * entries + entry];
-        if (s.y == 0.f) continue;                                // nothing seen: its results were not written
-        const float factor = __builtin_amdgcn_exp2f(s.x - top);
-        sum = fmaf(factor, s.y, sum);
-        const float* from = p.part_out + (k * entries + entry) * p.D + channel;
+    const int tid = threadIdx.x, wave = tid >> 6;
+    const float2 mine = tid < p.parts ? p.part_sums[tid * entries + entry] : make_float2(0.f, 0.f);
+    const bool seen = mine.y != 0.f;                             // nothing seen: its results were not written
+    float top = seen ? mine.x : NO_SCORE;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = channel + j < p.D ? fmaf(factor, from[j], v[j]) : 0.f;
+    for (int d = 1; d < WAVE; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+    if ((tid & 63) == 0) of_wave[wave].x = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(of_wave[0].x, of_wave[1].x), fmaxf(of_wave[2].x, of_wave[3].x));
+    const float factor = seen ? __builtin_amdgcn_exp2f(mine.x - top) : 0.f;
+    factors[tid] = factor;
+    float sum = seen ? factor * mine.y : 0.f;
+#pragma unroll
+    for (int d = 1; d < WAVE; d <<= 1) sum += __shfl_xor(sum, d);
+    if ((tid & 63) == 0) of_wave[wave].y = sum;
+    __syncthreads();
+    sum = (of_wave[0].y + of_wave[1].y) + (of_wave[2].y + of_wave[3].y);
+    int log2 = 0;
+    while (4 << log2 < p.D) ++log2;
+    const int channel = (tid & ((1 << log2) - 1)) * 4, first = tid >> log2, step = 256 >> log2;
+    f32x4 v{0.f, 0.f, 0.f, 0.f};
+    if (channel < p.D) {
+#pragma unroll 4
+        for (int k = first; k < p.parts; k += step) {
+            if (factors[k] == 0.f) continue;
+            const float* const from = p.part_out + (k * entries + entry) * p.D + channel;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = channel + j < p.D ? fmaf(factors[k], from[j], v[j]) : 0.f;
+        }
     }
+    shared[tid] = v;
+    __syncthreads();
+    if (first != 0 || channel >= p.D) return;
+    for (int k = 1; k < step; ++k) v += shared[tid + (k << log2)];
     const float inverse = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] *= inverse;
@@ -823,25 +951,38 @@ k_attention_join(const Attention p, int64_t entries, int q_heads) {
 }
 
 // ---- launches -------------------------------------------------------------------------------------------
-template <int DT, int DPAD, int WAVES, int NB, bool SPLIT>
+// Workgroups for so many items, of which a workgroup has one or each of its wavefronts ALONE.
+template <int SHARE, int WAVES>
+inline int64_t blocks_for(int64_t items) {
+    if (SHARE != ALONE) return items;
+    constexpr int64_t RUN = 4 * NUM_XCD;
+    return ((items + WAVES - 1) / WAVES + RUN - 1) / RUN * RUN;
+}
+inline dim3 grid_of(int64_t blocks) { return dim3((unsigned)grid_columns(blocks), (unsigned)grid_rows(blocks)); }
+constexpr int64_t BLOCKS_MAX = INT32_MAX / 4 - 2 * GRID_COLUMNS;
+
+template <int DT, int DPAD, int NB, int SHARE>
 int start_attention(Attention p, hipStream_t s) {
-    constexpr auto kernel = k_attention<DT, DPAD, WAVES, NB, SPLIT>;
-    constexpr size_t lds = attention_lds<DT, DPAD, WAVES, NB, SPLIT>();
-    p.units = scene_units(p.q_rows * p.per, p.scenes, 16 * NB * (SPLIT ? 1 : WAVES));
+    constexpr auto kernel = k_attention<DT, DPAD, NB, SHARE>;
+    constexpr int WAVES = wavefronts<DT, DPAD, SHARE>();
+    constexpr size_t lds = (size_t)(SHARE == SHARED ? 1 : WAVES) * walked_bytes<DT, DPAD, SHARE>();
+    static_assert(lds <= 163840, "of a CU");
+    p.units = scene_units(p.q_rows * p.per, p.scenes, 16 * NB * (SHARE == SHARED ? WAVES : 1));
+    const int64_t blocks = blocks_for<SHARE, WAVES>(p.units * p.k_heads * p.parts);
+    if (blocks > BLOCKS_MAX) return SC_EINVAL;
     static bool done[MAX_DEVICES];
     const int rc = allow_lds((const void*)kernel, lds, done);
     if (rc != SC_OK) return rc;
-    const int64_t blocks = p.units * p.k_heads * p.parts;
-    if (blocks > INT32_MAX - 2 * GRID_COLUMNS) return SC_EINVAL;
-    SC_LAUNCH(KID_ATTENTION, kernel, dim3((unsigned)grid_columns(blocks), (unsigned)grid_rows(blocks)), dim3(64 * WAVES), lds, s, p);
+    SC_LAUNCH(KID_ATTENTION, kernel, grid_of(blocks), dim3(64 * WAVES), lds, s, p);
     return SC_OK;
 }
 template <int DT, int DPAD>
 int choose_attention(const Attention& p, AttentionShape shape, hipStream_t s) {
-    constexpr int NB = DT == SC_F32 && DPAD == 256 ? 1 : 2;
-    if (shape == ATTENTION_FEW) return start_attention<DT, DPAD, 4, 1, true>(p, s);
-    if (shape == ATTENTION_SHORT) return start_attention<DT, DPAD, 1, NB, false>(p, s);
-    return start_attention<DT, DPAD, 4, NB, false>(p, s);
+    constexpr int NB = DT == SC_F32 && DPAD == 256 ? 1 : 2, WIDE = DPAD * ELEM<DT> <= 128 ? 4 : NB;
+    if (shape == ATTENTION_FEW) return start_attention<DT, DPAD, 1, SPLIT>(p, s);
+    if (shape == ATTENTION_SHORT) return start_attention<DT, DPAD, NB, ALONE>(p, s);
+    if (shape == ATTENTION_SHORT_64) return start_attention<DT, DPAD, WIDE, ALONE>(p, s);
+    return start_attention<DT, DPAD, NB, SHARED>(p, s);
 }
 template <int DT>
 int launch_attention(const Attention& p, AttentionShape shape, hipStream_t s) {
@@ -849,42 +990,49 @@ int launch_attention(const Attention& p, AttentionShape shape, hipStream_t s) {
                  : p.D <= 128 ? choose_attention<DT, 128>(p, shape, s) : choose_attention<DT, 256>(p, shape, s);
     if (rc != SC_OK || p.parts == 1) return rc;
     const int q_heads = p.k_heads * p.per;
-    const int64_t entries = p.q_rows * q_heads, blocks = (entries * ((p.D + 3) / 4) + 255) / 256;
-    if (blocks > INT32_MAX / 256) return SC_EINVAL;
-    SC_LAUNCH(KID_ATTENTION_JOIN, k_attention_join<DT>, dim3((unsigned)blocks), dim3(256), 0, s, p, entries, q_heads);
+    const int64_t entries = p.q_rows * q_heads;
+    if (entries > BLOCKS_MAX) return SC_EINVAL;
+    SC_LAUNCH(KID_ATTENTION_JOIN, k_attention_join<DT>, grid_of(entries), dim3(256), 0, s, p, entries, q_heads);
     return SC_OK;
 }
 
-template <int DT, int DPAD, int WAVES, int NB>
+template <int DT, int DPAD, int NB, int SHARE>
 int start_attention_grad(Attention p, hipStream_t s) {
-    constexpr auto of_queries = k_attention_dq<DT, DPAD, WAVES, NB>;
-    constexpr auto of_keys = k_attention_dkv<DT, DPAD, WAVES, NB>;
-    constexpr size_t lds = grad_lds<DT, DPAD>();
-    static bool done_queries[MAX_DEVICES], done_keys[MAX_DEVICES];
-    int rc = allow_lds((const void*)of_queries, lds, done_queries);
-    if (rc == SC_OK) rc = allow_lds((const void*)of_keys, lds, done_keys);
-    if (rc != SC_OK) return rc;
-    constexpr int COLUMNS = 16 * NB * WAVES;
+    constexpr auto of_queries = k_attention_dq<DT, DPAD, NB, SHARE>;
+    constexpr auto of_keys = k_attention_dkv<DT, DPAD, NB, SHARE>;
+    constexpr int WAVES = wavefronts<DT, DPAD, SHARE>(), COLUMNS = 16 * NB * (SHARE == SHARED ? WAVES : 1);
+    constexpr size_t lds = (size_t)(SHARE == SHARED ? 1 : WAVES) * walked_bytes<DT, DPAD, SHARE>(), lds_keys = lds + (SHARE == SHARED ? 1 : WAVES) * SUMS_BYTES;
+    static_assert(lds_keys <= 163840, "of a CU");
     p.units = scene_units(p.q_rows * p.per, p.scenes, COLUMNS);
     p.k_units = scene_units(p.k_rows, p.scenes, COLUMNS);
-    const int64_t blocks = p.units * p.k_heads, key_blocks = p.k_units * p.k_heads;
-    if (blocks > INT32_MAX - 2 * GRID_COLUMNS || key_blocks > INT32_MAX - 2 * GRID_COLUMNS) return SC_EINVAL;
-    if (p.q_rows > 0)
-        SC_LAUNCH(KID_ATTENTION_DQ, of_queries, dim3((unsigned)grid_columns(blocks), (unsigned)grid_rows(blocks)), dim3(64 * WAVES), lds, s, p);
-    if (p.k_rows > 0)
-        SC_LAUNCH(KID_ATTENTION_DKV, of_keys, dim3((unsigned)grid_columns(key_blocks), (unsigned)grid_rows(key_blocks)), dim3(64 * WAVES), lds, s, p);
+    const int64_t blocks = blocks_for<SHARE, WAVES>(p.units * p.k_heads * p.parts), key_blocks = blocks_for<SHARE, WAVES>(p.k_units * p.k_heads * p.k_parts);
+    if (blocks > BLOCKS_MAX || key_blocks > BLOCKS_MAX) return SC_EINVAL;
+    static bool done_queries[MAX_DEVICES], done_keys[MAX_DEVICES];
+    int rc = allow_lds((const void*)of_queries, lds, done_queries);
+    if (rc == SC_OK) rc = allow_lds((const void*)of_keys, lds_keys, done_keys);
+    if (rc != SC_OK) return rc;
+    if (p.q_rows > 0) SC_LAUNCH(KID_ATTENTION_DQ, of_queries, grid_of(blocks), dim3(64 * WAVES), lds, s, p);
+    if (p.k_rows > 0) SC_LAUNCH(KID_ATTENTION_DKV, of_keys, grid_of(key_blocks), dim3(64 * WAVES), lds_keys, s, p);
     return SC_OK;
 }
 template <int DT, int DPAD>
-int choose_attention_grad(const Attention& p, bool shorts, hipStream_t s) {
-    constexpr int NB = DT == SC_F32 && DPAD == 256 ? 1 : 2;
-    if (shorts) return start_attention_grad<DT, DPAD, 1, NB>(p, s);
-    return start_attention_grad<DT, DPAD, 4, NB>(p, s);
+int choose_attention_grad(const Attention& p, bool alone, hipStream_t s) {
+    constexpr int NB = DPAD == 256 ? 1 : 2;
+    return alone ? start_attention_grad<DT, DPAD, NB, ALONE>(p, s) : start_attention_grad<DT, DPAD, NB, SHARED>(p, s);
 }
 template <int DT>
-int launch_attention_grad(const Attention& p, bool shorts, hipStream_t s) {
-    return p.D <= 32 ? choose_attention_grad<DT, 32>(p, shorts, s) : p.D <= 64 ? choose_attention_grad<DT, 64>(p, shorts, s)
-           : p.D <= 128 ? choose_attention_grad<DT, 128>(p, shorts, s) : choose_attention_grad<DT, 256>(p, shorts, s);
+int launch_attention_grad(const Attention& p, bool alone, hipStream_t s) {
+    const int rc = p.D <= 32 ? choose_attention_grad<DT, 32>(p, alone, s) : p.D <= 64 ? choose_attention_grad<DT, 64>(p, alone, s)
+                 : p.D <= 128 ? choose_attention_grad<DT, 128>(p, alone, s) : choose_attention_grad<DT, 256>(p, alone, s);
+    if (rc != SC_OK) return rc;
+    const int q_heads = p.k_heads * p.per;
+    if (p.parts > 1 && p.q_rows > 0)
+        SC_LAUNCH(KID_ATTENTION_JOIN, k_attention_grad_join<DT>, grid_of(scene_units(p.q_rows, p.scenes, 16)), dim3(256), 0, s, p.q_starts, (const int32_t*)nullptr,
+                  p.scenes, p.q_rows, q_heads, p.D, p.parts, p.part_out, p.dq, p.scale, (const float*)nullptr, p.dq);
+    if (p.k_parts > 1 && p.k_rows > 0)
+        SC_LAUNCH(KID_ATTENTION_JOIN, k_attention_grad_join<DT>, grid_of(scene_units(p.k_rows, p.scenes, 16)), dim3(256), 0, s, p.k_starts, p.k_lens, p.scenes,
+                  p.k_rows, p.k_heads, p.D, p.k_parts, p.part_dk, p.dk, p.scale, p.part_dv, p.dv);
+    return SC_OK;
 }
 
 }  // namespace sc

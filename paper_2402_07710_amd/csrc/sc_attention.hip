@@ -1,4 +1,6 @@
 // Attention over packed scenes: checks of the calls and the choice of kernels (sc_attention.h).
+#include <initializer_list>
+
 #include "sc_heads.h"
 #include "sc_attention.h"
 
@@ -6,9 +8,9 @@ namespace sc {
 int launch_attention_f16(const Attention& p, AttentionShape shape, hipStream_t s);
 int launch_attention_bf16(const Attention& p, AttentionShape shape, hipStream_t s);
 int launch_attention_f32(const Attention& p, AttentionShape shape, hipStream_t s);
-int launch_attention_grad_f16(const Attention& p, bool shorts, hipStream_t s);
-int launch_attention_grad_bf16(const Attention& p, bool shorts, hipStream_t s);
-int launch_attention_grad_f32(const Attention& p, bool shorts, hipStream_t s);
+int launch_attention_grad_f16(const Attention& p, bool alone, hipStream_t s);
+int launch_attention_grad_bf16(const Attention& p, bool alone, hipStream_t s);
+int launch_attention_grad_f32(const Attention& p, bool alone, hipStream_t s);
 
 namespace {
 
@@ -24,11 +26,34 @@ struct Plan {
 };
 Plan plan_of(int64_t q_rows, int64_t k_rows, int scenes, int q_heads, int k_heads) {
     const int64_t columns = q_rows * (q_heads / k_heads);
-    Plan plan{attention_shape(columns, scenes, k_rows), 1};
+    Plan plan{attention_shape(columns, scenes, k_heads, k_rows), 1};
     plan.parts = q_rows == 0 ? 1 : attention_parts(plan.shape, columns, scenes, k_heads, k_rows);
     return plan;
 }
+struct GradPlan {
+    bool alone;
+    int parts, k_parts;
+    size_t sums, part, k_part;         // bytes in the workspace: exponents or deltas, partial gradients of queries, of keys (and as much of values)
+};
 size_t up16(size_t n) { return (n + 15) / 16 * 16; }
+GradPlan grad_plan_of(int64_t q_rows, int64_t k_rows, int scenes, int q_heads, int k_heads, int D) {
+    const int64_t per = q_heads / k_heads, columns = q_rows * per;
+    GradPlan plan{attention_grad_alone(columns, scenes, k_heads, k_rows), 1, 1, 0, 0, 0};
+    if (q_rows > 0 && k_rows > 0) {
+        plan.parts = attention_grad_parts(plan.alone, columns, scenes, k_heads, k_rows);
+        plan.k_parts = attention_grad_parts(plan.alone, k_rows, scenes, k_heads, columns);
+    }
+    plan.sums = up16((size_t)q_rows * q_heads * sizeof(float));
+    plan.part = plan.parts > 1 ? up16((size_t)plan.parts * q_rows * q_heads * D * sizeof(float)) : 0;
+    plan.k_part = plan.k_parts > 1 ? up16((size_t)plan.k_parts * k_rows * k_heads * D * sizeof(float)) : 0;
+    return plan;
+}
+// A tile's rows are 63 strides apart at most, in an offset of 32 bits.
+bool strides_ok(std::initializer_list<const sc_heads*> all) {
+    for (const sc_heads* h : all)
+        if (h->row > SC_ATTENTION_LD_MAX) return false;
+    return true;
+}
 HeadRows rows_of(const sc_heads* h, int dtype) {
     const int size = dtype == SC_F32 ? 4 : 2;
     return HeadRows{(char*)h->data, h->row * size, h->head * size};
@@ -38,6 +63,7 @@ int check_attention(const sc_heads* q, const sc_heads* k, const sc_heads* v, int
     if (dtype != SC_F32 && dtype != SC_F16 && dtype != SC_BF16) return SC_EINVAL;
     if (!heads_ok(q, dtype) || !heads_ok(k, dtype) || !heads_ok(v, dtype) || !heads_ok(out, dtype)) return SC_EINVAL;
     if (!sizes_ok(q_rows, k_rows, scenes, q->heads, k->heads, D, dtype) || v->heads != k->heads || out->heads != q->heads) return SC_EINVAL;
+    if (!strides_ok({q, k, v, out})) return SC_EINVAL;
     if (((uintptr_t)q_starts & 3) != 0 || ((uintptr_t)k_starts & 3) != 0 || ((uintptr_t)k_lens & 3) != 0 || ((uintptr_t)lse & 3) != 0) return SC_EINVAL;
     if (q_starts == nullptr && (k_starts != nullptr || scenes != 1)) return SC_EINVAL;
     if (q_starts != nullptr && k_starts == nullptr && q_rows != k_rows) return SC_EINVAL;
@@ -93,7 +119,7 @@ extern "C" int sc_attention_fwd(const sc_heads* q, const sc_heads* k, const sc_h
     const Plan plan = plan_of(q_rows, k_rows, scenes, q->heads, k->heads);
     Attention p = attention_of(q, k, v, q_rows, k_rows, D, d_q_starts, d_k_starts, d_k_lens, scenes, causal, scale, out, d_lse, dtype);
     p.parts = plan.parts;
-    p.part_keys = attention_part_keys(plan.shape);
+    p.part_keys = ATTENTION_PART_KEYS;
     if (plan.parts > 1) {
         p.part_sums = (float2*)d_workspace;
         p.part_out = (float*)((char*)d_workspace + up16((size_t)plan.parts * q_rows * q->heads * sizeof(float2)));
@@ -104,7 +130,8 @@ extern "C" int sc_attention_fwd(const sc_heads* q, const sc_heads* k, const sc_h
 
 extern "C" size_t sc_attention_bwd_workspace_bytes(int64_t q_rows, int64_t k_rows, int scenes, int q_heads, int k_heads, int D, int dtype) {
     if (!sizes_ok(q_rows, k_rows, scenes, q_heads, k_heads, D, dtype)) return 0;
-    return 2 * up16((size_t)q_rows * q_heads * sizeof(float));
+    const GradPlan plan = grad_plan_of(q_rows, k_rows, scenes, q_heads, k_heads, D);
+    return 2 * plan.sums + plan.part + 2 * plan.k_part;
 }
 
 extern "C" int sc_attention_bwd(const sc_heads* dout, const sc_heads* q, const sc_heads* k, const sc_heads* v, const sc_heads* out, const float* d_lse, int64_t q_rows,
@@ -114,6 +141,7 @@ extern "C" int sc_attention_bwd(const sc_heads* dout, const sc_heads* q, const s
     if (rc != SC_OK) return rc;
     if (d_lse == nullptr || !heads_ok(dout, dtype) || !heads_ok(dq, dtype) || !heads_ok(dk, dtype) || !heads_ok(dv, dtype)) return SC_EINVAL;
     if (dout->heads != q->heads || dq->heads != q->heads || dk->heads != k->heads || dv->heads != k->heads) return SC_EINVAL;
+    if (!strides_ok({dout, dq, dk, dv})) return SC_EINVAL;
     if (!heads_apart(dq, q_rows, D) || !heads_apart(dk, k_rows, D) || !heads_apart(dv, k_rows, D)) return SC_EINVAL;
     const size_t need = sc_attention_bwd_workspace_bytes(q_rows, k_rows, scenes, q->heads, k->heads, D, dtype);
     if (need > 0 && (d_workspace == nullptr || !aligned16(d_workspace))) return SC_EINVAL;
@@ -123,9 +151,16 @@ extern "C" int sc_attention_bwd(const sc_heads* dout, const sc_heads* q, const s
     p.dq = rows_of(dq, dtype);
     p.dk = rows_of(dk, dtype);
     p.dv = rows_of(dv, dtype);
-    p.against = (float*)d_workspace;
-    p.delta = (float*)((char*)d_workspace + need / 2);
-    const bool shorts = q_rows * p.per <= 64 * (int64_t)scenes && k_rows <= 64 * (int64_t)scenes;
+    const GradPlan plan = grad_plan_of(q_rows, k_rows, scenes, q->heads, k->heads, D);
+    char* const space = (char*)d_workspace;
+    p.against = (float*)space;
+    p.delta = (float*)(space + plan.sums);
+    p.part_out = (float*)(space + 2 * plan.sums);
+    p.part_dk = (float*)(space + 2 * plan.sums + plan.part);
+    p.part_dv = (float*)(space + 2 * plan.sums + plan.part + plan.k_part);
+    p.parts = plan.parts;
+    p.k_parts = plan.k_parts;
+    p.part_keys = p.part_rows = plan.alone ? ATTENTION_PART_KEYS : ATTENTION_PART_ROWS;
     hipStream_t s = (hipStream_t)stream;
-    return dtype == SC_F32 ? launch_attention_grad_f32(p, shorts, s) : dtype == SC_F16 ? launch_attention_grad_f16(p, shorts, s) : launch_attention_grad_bf16(p, shorts, s);
+    return dtype == SC_F32 ? launch_attention_grad_f32(p, plan.alone, s) : dtype == SC_F16 ? launch_attention_grad_f16(p, plan.alone, s) : launch_attention_grad_bf16(p, plan.alone, s);
 }

@@ -14,7 +14,7 @@
 namespace sc {
 namespace {
 
-constexpr int NORM_THREADS = 256, CHUNK = 8;
+constexpr int NORM_THREADS = 256, JOIN_THREADS = 1024, CHUNK = 8;
 constexpr int SLICE = NORM_THREADS * CHUNK;          // channels that a workgroup has at most
 
 struct Norm {
@@ -31,7 +31,7 @@ struct Norm {
     float2* stats;                     // [scene][group]: mean, 1 / deviation
     float2* sums;                      // [unit][C]: mean and squares about it, or backward the sums of dz and of dz u
     float2* means;                     // backward: [scene][group]
-    int per;                           // rows of a unit
+    int per, per_log2;                 // rows of a unit
     int64_t units;
 };
 
@@ -43,7 +43,7 @@ struct NormUnit {
 __device__ inline NormUnit unit_of(const Norm& p, int64_t u) {
     int64_t first = 0;
     int count = 0, scene = 0;
-    const int tile = __builtin_amdgcn_readfirstlane(find_scene(p.starts, p.scenes, p.rows, 1, p.per, u, first, count, scene).tile);
+    const int tile = __builtin_amdgcn_readfirstlane(find_scene(p.starts, p.scenes, p.rows, 1, p.per_log2, u, first, count, scene).tile);
     if (tile < 0) return NormUnit{0, 0, 0};
     first = uniform64(first) + (int64_t)tile * p.per;
     const int left = __builtin_amdgcn_readfirstlane(count) - tile * p.per;
@@ -125,18 +125,26 @@ k_norm_sums(const Norm p) {
     });
 }
 
-// A double that is the same in every thread of the workgroup: sum over the threads, in their order of lanes and wavefronts.
-__device__ inline double sum_of_threads(double v) {
-    __shared__ double shared[NORM_THREADS / WAVE];
+// Two sums over the threads of a workgroup, the same in all of them, in the order of lanes and wavefronts.
+template <int THREADS>
+__device__ inline void sum_of_threads(double& a, double& b) {
+    __shared__ double shared[2][THREADS / WAVE];
 #pragma unroll
-    for (int d = 1; d < WAVE; d <<= 1) v += __shfl_xor(v, d);
+    for (int d = 1; d < WAVE; d <<= 1) {
+        a += __shfl_xor(a, d);
+        b += __shfl_xor(b, d);
+    }
+    if ((threadIdx.x & 63) == 0) {
+        shared[0][threadIdx.x >> 6] = a;
+        shared[1][threadIdx.x >> 6] = b;
+    }
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v;
-    __syncthreads();
-    double total = 0.0;
+    a = b = 0.0;
 #pragma unroll
-    for (int w = 0; w < NORM_THREADS / WAVE; ++w) total += shared[w];
-    return total;
+    for (int w = 0; w < THREADS / WAVE; ++w) {
+        a += shared[0][w];
+        b += shared[1][w];
+    }
 }
 // A scene's rows and the units that hold them.
 __device__ inline void scene_units_of(const Norm& p, int scene, int64_t& first_unit, int& rows) {
@@ -146,7 +154,7 @@ __device__ inline void scene_units_of(const Norm& p, int scene, int64_t& first_u
 }
 
 // Mean and deviation of a scene's group from its units' sums.
-__global__ void __launch_bounds__(NORM_THREADS)
+__global__ void __launch_bounds__(JOIN_THREADS)
 k_norm_join(const Norm p) {
     const int scene = blockIdx.x / (unsigned)p.groups, group = blockIdx.x - scene * p.groups;
     int64_t unit = 0;
@@ -158,15 +166,14 @@ k_norm_join(const Norm p) {
     double sum = 0.0, square = 0.0;
     const int64_t items = (int64_t)units * p.channels;
 #pragma unroll 4
-    for (int64_t i = threadIdx.x; i < items; i += NORM_THREADS) {
+    for (int64_t i = threadIdx.x; i < items; i += JOIN_THREADS) {
         const int u = (int)(i / p.channels), c = (int)(i - (int64_t)u * p.channels);
         const float2 s = sums[(int64_t)u * p.C + c];
         const double n = rows - u * p.per < p.per ? rows - u * p.per : p.per, d = (double)s.x - pivot;
         sum += n * d;
         square += s.y + n * d * d;
     }
-    sum = sum_of_threads(sum);
-    square = sum_of_threads(square);
+    sum_of_threads<JOIN_THREADS>(sum, square);
     if (threadIdx.x != 0) return;
     const double n = (double)rows * p.channels, mean = rows > 0 ? sum / n : 0.0, var = rows > 0 ? square / n - mean * mean : 0.0;
     p.stats[blockIdx.x] = make_float2((float)(pivot + mean), (float)(1.0 / sqrt((var > 0.0 ? var : var != var ? var : 0.0) + (double)p.eps)));
@@ -235,8 +242,7 @@ k_norm_few(const Norm p) {
         sum += d;
         square += d * d;
     }
-    sum = sum_of_threads(sum);
-    square = sum_of_threads(square);
+    sum_of_threads<NORM_THREADS>(sum, square);
     const double mean = rows > 0 ? sum / items : 0.0, var = rows > 0 ? square / items - mean * mean : 0.0;
     const float2 s = make_float2((float)(pivot + mean), (float)(1.0 / sqrt((var > 0.0 ? var : var != var ? var : 0.0) + (double)p.eps)));
     if (p.stats != nullptr && threadIdx.x == 0) p.stats[blockIdx.x] = s;
@@ -297,7 +303,7 @@ k_norm_grad_sums(const Norm p) {
 }
 // The means of a scene's group, and in the workgroups behind those the gradients of 16 channels' gain and bias.
 template <int DT>
-__global__ void __launch_bounds__(NORM_THREADS)
+__global__ void __launch_bounds__(JOIN_THREADS)
 k_norm_grad_join(const Norm p) {
     const int pairs = p.scenes * p.groups;
     if ((int)blockIdx.x < pairs) {
@@ -310,25 +316,24 @@ k_norm_grad_join(const Norm p) {
         double sum = 0.0, along = 0.0;
         const int64_t items = (int64_t)units * p.channels;
 #pragma unroll 4
-        for (int64_t i = threadIdx.x; i < items; i += NORM_THREADS) {
+        for (int64_t i = threadIdx.x; i < items; i += JOIN_THREADS) {
             const int u = (int)(i / p.channels), c = (int)(i - (int64_t)u * p.channels);
             const float2 s = sums[(int64_t)u * p.C + c];
             const double gain = p.gain != nullptr ? load_elem<DT>(p.gain, group * p.channels + c) : 1.f;
             sum += gain * s.x;
             along += gain * s.y;
         }
-        sum = sum_of_threads(sum);
-        along = sum_of_threads(along);
+        sum_of_threads<JOIN_THREADS>(sum, along);
         const double n = (double)rows * p.channels;
         if (threadIdx.x == 0) p.means[blockIdx.x] = rows > 0 ? make_float2((float)(sum / n), (float)(along / n)) : make_float2(0.f, 0.f);
         return;
     }
-    __shared__ double shared[2][16][16];
+    __shared__ double shared[2][64][16];
     const int c = ((int)blockIdx.x - pairs) * 16 + (threadIdx.x & 15), which = threadIdx.x >> 4;
     double sum = 0.0, along = 0.0;
     if (c < p.C) {
 #pragma unroll 8
-        for (int64_t u = which; u < p.units; u += 16) {
+        for (int64_t u = which; u < p.units; u += 64) {
             const float2 s = p.sums[u * p.C + c];
             sum += s.x;
             along += s.y;
@@ -340,7 +345,7 @@ k_norm_grad_join(const Norm p) {
     if (which != 0 || c >= p.C) return;
     sum = along = 0.0;
 #pragma unroll
-    for (int w = 0; w < 16; ++w) {
+    for (int w = 0; w < 64; ++w) {
         sum += shared[0][w][threadIdx.x];
         along += shared[1][w][threadIdx.x];
     }
@@ -398,7 +403,7 @@ int launch_norm(const Norm& p, bool few, hipStream_t s) {
     }
     const dim3 grid((unsigned)p.units, (unsigned)slices_of(p.C));
     SC_LAUNCH(KID_NORM_SUMS, k_norm_sums<DT>, grid, dim3(NORM_THREADS), 0, s, p);
-    SC_LAUNCH(KID_NORM_JOIN, k_norm_join, pairs, dim3(NORM_THREADS), 0, s, p);
+    SC_LAUNCH(KID_NORM_JOIN, k_norm_join, pairs, dim3(JOIN_THREADS), 0, s, p);
     SC_LAUNCH(KID_NORM, k_norm<DT>, grid, dim3(NORM_THREADS), 0, s, p);
     return SC_OK;
 }
@@ -407,7 +412,7 @@ int launch_norm_grad(const Norm& p, hipStream_t s) {
     const dim3 grid((unsigned)p.units, (unsigned)slices_of(p.C));
     const int gains = p.dgain != nullptr || p.dbias != nullptr ? (p.C + 15) / 16 : 0;
     SC_LAUNCH(KID_NORM_SUMS, k_norm_grad_sums<DT>, grid, dim3(NORM_THREADS), 0, s, p);
-    SC_LAUNCH(KID_NORM_JOIN, k_norm_grad_join<DT>, dim3((unsigned)(p.scenes * p.groups + gains)), dim3(NORM_THREADS), 0, s, p);
+    SC_LAUNCH(KID_NORM_JOIN, k_norm_grad_join<DT>, dim3((unsigned)(p.scenes * p.groups + gains)), dim3(JOIN_THREADS), 0, s, p);
     if (p.y != nullptr) SC_LAUNCH(KID_NORM_GRAD, k_norm_grad<DT>, grid, dim3(NORM_THREADS), 0, s, p);
     return SC_OK;
 }
@@ -447,6 +452,7 @@ extern "C" int sc_group_norm_fwd(const void* d_x, int64_t ldx, int64_t rows, con
     p.eps = eps;
     p.act = act;
     p.per = norm_rows(rows, C);
+    p.per_log2 = __builtin_ctz(p.per);
     p.units = scene_units(rows, scenes, p.per);
     p.sums = (float2*)d_workspace;
     p.stats = d_stats != nullptr ? (float2*)d_stats : (float2*)((char*)d_workspace + up16((size_t)p.units * C * sizeof(float2)));
@@ -488,6 +494,7 @@ extern "C" int sc_group_norm_bwd(const void* d_dy, int64_t lddy, const void* d_x
     p.act = act;
     p.stats = (float2*)const_cast<float*>(d_stats);
     p.per = norm_rows(rows, C);
+    p.per_log2 = __builtin_ctz(p.per);
     p.units = scene_units(rows, scenes, p.per);
     p.sums = (float2*)d_workspace;
     p.means = (float2*)((char*)d_workspace + up16((size_t)p.units * C * sizeof(float2)));

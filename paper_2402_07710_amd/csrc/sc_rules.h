@@ -285,32 +285,53 @@ constexpr int64_t ROPE_BLOCKS_MAX = 1024;
 // Units of work of scenes' columns cut into tiles: scene s has those from start(s) / tile + s on, one more than it needs at most.
 constexpr int64_t scene_units(int64_t columns, int64_t scenes, int64_t tile) { return columns / tile + scenes; }
 
-// FEW: 16 columns a workgroup, whose four wavefronts share the keys; SHORT: a wavefront alone; WIDE: four wavefronts, 128 columns.
-enum AttentionShape { ATTENTION_FEW, ATTENTION_SHORT, ATTENTION_WIDE };
-constexpr AttentionShape attention_shape(int64_t columns, int64_t scenes, int64_t k_rows) {
-    if (columns <= 32 * scenes && k_rows >= 256 * scenes) return ATTENTION_FEW;
-    return columns <= 64 * scenes ? ATTENTION_SHORT : ATTENTION_WIDE;
+// FEW: 16 columns a workgroup, whose wavefronts share the keys; SHORT: a wavefront has 32 or 64 columns and the keys to itself; WIDE: four
+// wavefronts, 128 columns.
+enum AttentionShape { ATTENTION_FEW, ATTENTION_SHORT, ATTENTION_SHORT_64, ATTENTION_WIDE };
+constexpr int attention_columns(AttentionShape shape) {
+    return shape == ATTENTION_FEW ? 16 : shape == ATTENTION_SHORT ? 32 : shape == ATTENTION_SHORT_64 ? 64 : 128;
 }
-constexpr int attention_columns(AttentionShape shape) { return shape == ATTENTION_FEW ? 16 : shape == ATTENTION_SHORT ? 32 : 128; }
+constexpr int64_t attention_tiles(AttentionShape shape, int64_t columns, int64_t scenes) {       // about as many as there are
+    const int64_t full = (columns + attention_columns(shape) - 1) / attention_columns(shape);
+    return full > scenes ? full : scenes;
+}
+constexpr AttentionShape attention_shape(int64_t columns, int64_t scenes, int64_t k_heads, int64_t k_rows) {
+    if (columns <= 32 * scenes && k_rows >= 256 * scenes) return ATTENTION_FEW;
+    if (columns <= 32 * scenes) return ATTENTION_SHORT;
+    if (columns <= 96 * scenes) return ATTENTION_SHORT_64;
+    return attention_tiles(ATTENTION_WIDE, columns, scenes) * k_heads < 256 ? ATTENTION_SHORT : ATTENTION_WIDE;
+}
 // Parts that the keys of a scene are cut into where its columns alone do not fill the chip, and the keys that a part has at least.
-constexpr int ATTENTION_PARTS_MAX = 256;
-constexpr int attention_part_keys(AttentionShape) { return 256; }
+constexpr int ATTENTION_PARTS_MAX = 256, ATTENTION_PART_KEYS = 256;
 constexpr int attention_parts(AttentionShape shape, int64_t columns, int64_t scenes, int64_t k_heads, int64_t k_rows) {
-    const int64_t wanted = shape == ATTENTION_FEW ? 1024 : shape == ATTENTION_SHORT ? 2048 : 512;
-    const int64_t most = (k_rows / scenes + attention_part_keys(shape) - 1) / attention_part_keys(shape);
-    const int64_t there = (columns + attention_columns(shape) - 1) / attention_columns(shape) > scenes ? (columns + attention_columns(shape) - 1) / attention_columns(shape) : scenes;
-    int64_t parts = (wanted + there * k_heads - 1) / (there * k_heads);
+    const int64_t wanted = shape == ATTENTION_WIDE ? 512 : 1024;
+    const int64_t most = (k_rows / scenes + ATTENTION_PART_KEYS - 1) / ATTENTION_PART_KEYS, there = attention_tiles(shape, columns, scenes) * k_heads;
+    int64_t parts = (wanted + there - 1) / there;
     parts = parts < most ? parts : most;
     return (int)(parts < 1 ? 1 : parts < ATTENTION_PARTS_MAX ? parts : ATTENTION_PARTS_MAX);
 }
+// Backward: a wavefront ALONE has 32 columns, or four share 128, of queries and of keys.
+constexpr bool attention_grad_alone(int64_t columns, int64_t scenes, int64_t k_heads, int64_t k_rows) {
+    const int64_t most = columns > k_rows ? columns : k_rows;
+    return most <= 96 * scenes || attention_tiles(ATTENTION_WIDE, most, scenes) * k_heads < 256;
+}
+constexpr int ATTENTION_GRAD_PARTS_MAX = 16, ATTENTION_PART_ROWS = 1024;
+// Parts of what `columns` of a scene walk, `rows` of the scenes together.
+constexpr int attention_grad_parts(bool alone, int64_t columns, int64_t scenes, int64_t k_heads, int64_t rows) {
+    const int64_t there = attention_tiles(alone ? ATTENTION_SHORT : ATTENTION_WIDE, columns, scenes) * k_heads, wanted = 1536, least = alone ? 256 : ATTENTION_PART_ROWS;
+    const int64_t most = (rows / scenes + least - 1) / least;
+    int64_t parts = (wanted + there - 1) / there;
+    parts = parts < most ? parts : most;
+    return (int)(parts < 1 ? 1 : parts < ATTENTION_GRAD_PARTS_MAX ? parts : ATTENTION_GRAD_PARTS_MAX);
+}
 
 // ---- group norm (sc_norm.hip) -------------------------------------------------------------------------------
-// Rows of a unit: some eight chunks of eight channels a thread, and no more than about 4096 units, whose sums are joined.
+// Rows of a unit: a chunk of eight channels a thread at least, eight where that leaves 1024 units, and no more than about 4096 units, whose sums are joined.
 constexpr int norm_rows(int64_t rows, int C) {
     const int chunks = (C + 7) / 8;
     int64_t per = 1;
-    while (per * chunks < 2048 && per < 1024) per *= 2;
-    while (rows / per > 4096) per *= 2;
+    while (per * chunks < 256 && per < 1024) per *= 2;
+    while ((per * chunks < 2048 && per < 1024 && rows / per > 1024) || rows / per > 4096) per *= 2;
     return (int)per;
 }
 // One launch, a workgroup for a scene's group, whose rows may all be of one scene.

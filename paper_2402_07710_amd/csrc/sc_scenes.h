@@ -12,47 +12,42 @@ struct Scene {
 };
 __device__ inline int64_t clamp_row(int64_t v, int64_t rows) { return v < 0 ? 0 : v > rows ? rows : v; }
 
-// Unit u of the scenes' columns cut into tiles of `tile` columns, `per` columns a row.  Scene s has the units from A(s) = start(s) per / tile + s on: at least as many as
+// Unit u of the scenes' columns cut into tiles of 2^log2 columns, `per` columns a row.  Scene s has the units from A(s) = start(s) per / 2^log2 + s on: at least as many as
 // it has tiles, one too many at most, so the host knows how many units there can be without the starts, and the device finds a unit's scene by a search
-// 64 wide, one trip to memory up to 64 scenes and two up to 4096.  Called by whole wavefronts.  Starts that do not ascend give wrong scenes, but never rows outside [0, rows).
-__device__ inline Scene find_scene(const int32_t* __restrict__ starts, int scenes, int64_t rows, int per, int tile, int64_t u, int64_t& first, int& count, int& scene) {
-    Scene none{0, 0, 0, 0, -1};
+// 63 wide, one trip to memory up to 63 scenes and two up to 3969.  Called by whole wavefronts.  Starts that do not ascend give wrong scenes, but never rows outside [0, rows).
+__device__ inline Scene find_scene(const int32_t* __restrict__ starts, int scenes, int64_t rows, int per, int log2, int64_t u, int64_t& first, int& count, int& scene) {
+    Scene found{0, 0, 0, 0, -1};
     const int lane = threadIdx.x & 63;
     scene = 0;
     if (starts == nullptr) {
         first = 0;
         count = (int)rows;
-        if (u * tile >= rows * per) return none;
-        none.tile = (int)u;
-        return none;
+        if (u << log2 < rows * per) found.tile = (int)u;
+        return found;
     }
     int lo = 0, hi = scenes;
-    int64_t at_lo = 0;
-    bool found = false;
-    while (!found || hi - lo > 1) {
-        const int step = (hi - lo + 63) / 64;
-        const int s = lo + lane * step;
-        int64_t at = 0;
+    for (;;) {
+        const int step = (hi - lo + 62) / 63, s = lo + lane * step;
+        int start = 0;
         bool below = false;
-        if (s < hi) {
-            at = clamp_row(starts[s], rows) * per / tile + s;
-            below = at <= u;
+        if (s < hi || (s == hi && step == 1)) {
+            start = (int)clamp_row(starts[s], rows);
+            below = s < hi && ((int64_t)start * per >> log2) + s <= u;
         }
         const int n = __popcll(__ballot(below));
-        if (n == 0) return none;
-        at_lo = ((int64_t)__builtin_amdgcn_readlane((int)(at >> 32), n - 1) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)at, n - 1);
+        if (n == 0) return found;
+        if (step == 1) {
+            const int begin = __builtin_amdgcn_readlane(start, n - 1), stop = __builtin_amdgcn_readlane(start, n);
+            scene = lo + n - 1;
+            first = begin;
+            count = stop > begin ? stop - begin : 0;
+            const int64_t nth = u - (((int64_t)begin * per >> log2) + scene);
+            if (nth << log2 < (int64_t)count * per) found.tile = (int)nth;
+            return found;
+        }
         lo += (n - 1) * step;
         hi = lo + step < hi ? lo + step : hi;
-        found = true;
     }
-    scene = lo;
-    first = clamp_row(starts[lo], rows);
-    const int64_t stop = clamp_row(starts[lo + 1], rows);
-    count = (int)(stop > first ? stop - first : 0);
-    const int64_t nth = u - at_lo;
-    if (nth < 0 || nth * tile >= (int64_t)count * per) return none;
-    none.tile = (int)nth;
-    return none;
 }
 __device__ inline void scene_rows(const int32_t* __restrict__ starts, const int32_t* __restrict__ lens, int64_t rows, int scene, int64_t& first, int& count) {
     if (starts == nullptr) {
