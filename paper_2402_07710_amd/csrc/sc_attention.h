@@ -46,7 +46,7 @@ constexpr int log2_of(int tile) { return tile == 16 ? 4 : tile == 32 ? 5 : tile 
 __device__ inline Scene scene_of_queries(const Attention& p, int log2, int64_t u) {
     int64_t first = 0, first_k = 0;
     int count = 0, count_k = 0, scene;
-    Scene s = find_scene(p.q_starts, p.scenes, p.q_rows, p.per, log2, u, first, count, scene);
+    Scene s = find_scene(p.q_starts, p.scenes, p.q_rows, p.per, log2, u, p.units, first, count, scene);
     s.tile = __builtin_amdgcn_readfirstlane(s.tile);
     if (s.tile < 0) return s;
     first_k = first;
@@ -80,9 +80,11 @@ struct HeadShape {
     static constexpr int STEP = DT == SC_F32 ? 16 : 32;   // rows that a step of the second product takes
 };
 
-// 16 bytes a lane straight into LDS as load_to_lds, from an address that the wavefront shares and an offset of the lane's.
+// 16 bytes a lane straight into LDS as load_to_lds, from an address that the wavefront shares and an offset of the lane's.  A vector instruction (v_readfirstlane)
+// may have written that address just before, and a load that takes it from scalar registers needs five wait states behind such a write, which the compiler does not
+// see to inside assembly.
 __device__ inline void load_to_lds_at(const void* base, uint32_t offset, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "m0", "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "m0", "memory");
 }
 // The loads of one operand's tiles by NTH threads: rows first .. of a scene's head.  Zeros stand for rows that are not there and for channels beyond D: whole chunks of those
 // are cleared once, by clear(), and never written again.
@@ -137,46 +139,44 @@ struct TileLoader {
         }
     }
 };
-// What a lane reads of a tile: rows as they lie (16 rows, 64 bytes of channels a step) ...
+// What a lane reads of a tile, whose first byte lies at a multiple of 1024: the chunk's number is in bits of its own of the address, so others of a line follow by an exclusive or.
+// Rows as they lie (16 rows, 64 bytes of channels a step) ...
 template <int DT, int DPAD>
 struct RowReader {
     using H = HeadShape<DT, DPAD>;
-    uint32_t at[H::KS];
+    uint32_t at;
     __device__ explicit RowReader(uint32_t lds) {
         const int i = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
-#pragma unroll
-        for (int k = 0; k < H::KS; ++k) at[k] = lds + (i * H::LINE + ((4 * k + g) ^ tile_turn<DT, H::LINE>(i))) * 16;
+        at = lds + i * H::BYTES + (g ^ tile_turn<DT, H::LINE>(i)) * 16;
     }
     __device__ __forceinline__ uint4 read(uint32_t tile, int block, int k) const {
-        return __builtin_bit_cast(uint4, *(lds_u32x4)(at[k] + tile + block * (16 * H::BYTES)));
+        return __builtin_bit_cast(uint4, *(lds_u32x4)(((at + tile) ^ (k * 64)) + block * (16 * H::BYTES)));
     }
 };
 // ... or across them: a block of 16 channels, of the rows 4 g .. 4 g + 3 of each 16, which are the rows that the quarter g of the lanes holds of S.
 template <int DT, int DPAD>
 struct ChannelReader {
     using H = HeadShape<DT, DPAD>;
-    uint32_t at[H::CB];
+    static constexpr int N = DT == SC_F32 ? 4 : 1;
+    uint32_t at[N];
     __device__ explicit ChannelReader(uint32_t lds) {
         const int i = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
+        if constexpr (DT == SC_F32) {
 #pragma unroll
-        for (int c = 0; c < H::CB; ++c) {
-            if constexpr (DT == SC_F32) {          // the turn of rows 4 g + 0 .. 3 differs in its lowest bits: read() adds them
-                at[c] = lds + 4 * g * H::BYTES + (i & 3) * 4;
-            } else {                               // a lane hands in 4 channels of row 4 g + i / 4 and gets channel i of the four rows
-                const int line = 4 * g + (i >> 2);
-                at[c] = lds + line * H::BYTES + ((2 * c + ((i >> 1) & 1)) ^ tile_turn<DT, H::LINE>(line)) * 16 + (i & 1) * 8;
-            }
+            for (int j = 0; j < 4; ++j) at[j] = lds + (4 * g + j) * H::BYTES + ((i >> 2) ^ tile_turn<DT, H::LINE>(4 * g + j)) * 16 + (i & 3) * 4;
+        } else {                                   // a lane hands in 4 channels of row 4 g + i / 4 and gets channel i of the four rows
+            const int line = 4 * g + (i >> 2);
+            at[0] = lds + line * H::BYTES + (((i >> 1) & 1) ^ tile_turn<DT, H::LINE>(line)) * 16 + (i & 1) * 8;
         }
     }
     __device__ __forceinline__ uint4 read(uint32_t tile, int step, int c) const {
-        const uint32_t p = at[c] + tile + step * (H::STEP * H::BYTES);
         if constexpr (DT == SC_F32) {
-            const int i = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
             uint32_t v[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = *(lds_uint32)(p + j * H::BYTES + ((4 * c + (i >> 2)) ^ tile_turn<DT, H::LINE>(4 * g + j)) * 16);
+            for (int j = 0; j < 4; ++j) v[j] = *(lds_uint32)(((at[j] + tile) ^ (c * 64)) + step * (H::STEP * H::BYTES));
             return make_uint4(v[0], v[1], v[2], v[3]);
         } else {
+            const uint32_t p = ((at[0] + tile) ^ (c * 32)) + step * (H::STEP * H::BYTES);
             const uint2 a = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p));
             const uint2 b = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(p + 16 * H::BYTES)));
             return make_uint4(a.x, a.y, b.x, b.y);
@@ -259,13 +259,23 @@ struct Running {
     float sum;
 };
 
+// A larger score: what sums and results are scaled by.
+template <int DT>
+__device__ __forceinline__ float follow(Running& run, float score) {
+    const float top = fmaxf(run.top, score), against = top == NO_SCORE ? 0.f : top - LIFT<DT>;
+    const float factor = run.top == NO_SCORE ? 0.f : __builtin_amdgcn_exp2f(run.against - against);
+    run.top = top;
+    run.against = against;
+    run.sum *= factor;
+    return factor;
+}
 // SHARED: a wavefront has 16 NB columns of its own, and all walk the same tiles.  SPLIT: the wavefronts share 16 NB columns and take every WAVES-th tile each.
 // ALONE: a wavefront has columns and tiles to itself, neighbours the next head of the same scene: rows of short heads share lines of memory.
 enum Share { SHARED, SPLIT, ALONE };
 template <int DT, int DPAD, int SHARE>
 constexpr int walked_tile() {          // rows
     constexpr int BYTES = DPAD * ELEM<DT>;
-    if (SHARE == SHARED) return BYTES >= 512 ? 32 : 64;
+    if (SHARE == SHARED) return BYTES >= 1024 ? 16 : BYTES >= 512 ? 32 : 64;
     return DT == SC_F32 && BYTES >= 512 ? 16 : 32;
 }
 template <int DT, int DPAD, int SHARE>
@@ -301,12 +311,12 @@ __device__ inline void part_of(int all, int part, int parts, int64_t used, int& 
 }
 
 template <int DT, int DPAD, int NB, int SHARE>
-__global__ void __launch_bounds__((64 * wavefronts<DT, DPAD, SHARE>()), (DT == SC_F32 && DPAD >= 128 ? 1 : 2))
+__global__ void __launch_bounds__((64 * wavefronts<DT, DPAD, SHARE>()), (NB * HeadShape<DT, DPAD>::BYTES >= 1024 ? 1 : SHARE == ALONE && HeadShape<DT, DPAD>::BYTES <= 64 ? 3 : 2))
 k_attention(const Attention p) {
     using H = HeadShape<DT, DPAD>;
     constexpr int WAVES = wavefronts<DT, DPAD, SHARE>(), KT = walked_tile<DT, DPAD, SHARE>(), ST = KT / 16, TILE_BYTES = KT * H::BYTES;
     constexpr int COLUMNS = 16 * NB * (SHARE == SHARED ? WAVES : 1);
-    extern __shared__ __align__(16) uint4 attention_lds_words[];
+    extern __shared__ __align__(1024) uint4 attention_lds_words[];
     const Item item = item_of<SHARE, WAVES>(p.k_heads, p.parts);
     const int head_k = item.head, part = item.part;
     const int64_t unit = p.units - 1 - item.unit;                 // the last first: behind a causal mask they take longest
@@ -376,7 +386,52 @@ k_attention(const Attention p) {
         else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (t + STRIDE < to) bring(t + STRIDE, buffer ^ (2 * TILE_BYTES));
         const int key0 = t * KT;
-        if (key0 < wave_limit) {
+        if constexpr (SHARE == ALONE) {                           // block by block, and those only that have columns
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                if (column0 + 16 * n >= columns) break;
+                f32x4 s[ST];
+#pragma unroll
+                for (int b = 0; b < ST; ++b) s[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < H::KS; ++k)
+#pragma unroll
+                    for (int b = 0; b < ST; ++b) s[b] = multiply<DT>(rows.read(buffer, b, k), q[n][k], s[b]);
+                if (key0 + KT > first_limit) {
+                    const int least = p.causal ? limit[n] : scene.nk;
+#pragma unroll
+                    for (int b = 0; b < ST; ++b)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[b][r] = key0 + 16 * b + 4 * g + r < least ? s[b][r] : NO_SCORE;
+                }
+                float most = s[0][0];
+#pragma unroll
+                for (int b = 0; b < ST; ++b)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) most = fmaxf(most, s[b][r]);
+                most *= p.scale_log2;
+                if (!__all(most <= run[n].top + CALM)) {
+                    const float factor = follow<DT>(run[n], over_quarters_max(most));
+#pragma unroll
+                    for (int c = 0; c < H::CB; ++c)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) out[n][c][r] *= factor;
+                }
+#pragma unroll
+                for (int b = 0; b < ST; ++b)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], p.scale_log2, -run[n].against));
+                        run[n].sum += s[b][r];
+                    }
+#pragma unroll
+                for (int u = 0; u < KT / H::STEP; ++u) {
+                    const uint4 w = weights_of<DT, ST>(s, u);
+#pragma unroll
+                    for (int c = 0; c < H::CB; ++c) out[n][c] = multiply<DT>(channels.read(buffer, u, c), w, out[n][c]);
+                }
+            }
+        } else if (key0 < wave_limit) {
             f32x4 s[NB][ST];
 #pragma unroll
             for (int n = 0; n < NB; ++n)
@@ -413,12 +468,7 @@ k_attention(const Attention p) {
             if (!__all(calm)) {
 #pragma unroll
                 for (int n = 0; n < NB; ++n) {
-                    const float top = fmaxf(run[n].top, over_quarters_max(most[n]));
-                    const float against = top == NO_SCORE ? 0.f : top - LIFT<DT>;
-                    const float factor = run[n].top == NO_SCORE ? 0.f : __builtin_amdgcn_exp2f(run[n].against - against);
-                    run[n].top = top;
-                    run[n].against = against;
-                    run[n].sum *= factor;
+                    const float factor = follow<DT>(run[n], over_quarters_max(most[n]));
 #pragma unroll
                     for (int c = 0; c < H::CB; ++c)
 #pragma unroll
@@ -529,7 +579,7 @@ constexpr int SUB = walked_tile<DT, DPAD, SHARE>() < 32 ? 16 : 32;
 
 template <int DT, int DPAD, int NB>
 constexpr int grad_waves(int rows, int results) {                 // wavefronts on a SIMD that the registers leave room for
-    return NB * (rows * HeadShape<DT, DPAD>::KS * 4 + results * HeadShape<DT, DPAD>::CB * 4) > (DT == SC_F32 ? 180 : 200) ? 1 : 2;
+    return NB * (rows * HeadShape<DT, DPAD>::KS * 4 + results * HeadShape<DT, DPAD>::CB * 4) > (DT == SC_F32 ? 120 : 180) ? 1 : 2;
 }
 
 template <int DT, int DPAD, int NB, int SHARE>
@@ -538,7 +588,7 @@ k_attention_dq(const Attention p) {
     using H = HeadShape<DT, DPAD>;
     constexpr int WAVES = wavefronts<DT, DPAD, SHARE>(), KT = walked_tile<DT, DPAD, SHARE>(), TILE_BYTES = KT * H::BYTES, COLUMNS = 16 * NB * (SHARE == SHARED ? WAVES : 1);
     constexpr int SUB = sc::SUB<DT, DPAD, SHARE>, SUB_BLOCKS = SUB / 16;
-    extern __shared__ __align__(16) uint4 attention_lds_words[];
+    extern __shared__ __align__(1024) uint4 attention_lds_words[];
     const Item item = item_of<SHARE, WAVES>(p.k_heads, p.parts);
     const int head_k = item.head, part = item.part;
     const int64_t unit = p.units - 1 - item.unit;
@@ -705,14 +755,14 @@ k_attention_dkv(const Attention p) {
     using H = HeadShape<DT, DPAD>;
     constexpr int WAVES = wavefronts<DT, DPAD, SHARE>(), RT = walked_tile<DT, DPAD, SHARE>(), TILE_BYTES = RT * H::BYTES, COLUMNS = 16 * NB * (SHARE == SHARED ? WAVES : 1);
     constexpr int SUB = sc::SUB<DT, DPAD, SHARE>, SUB_BLOCKS = SUB / 16;
-    extern __shared__ __align__(16) uint4 attention_lds_words[];
+    extern __shared__ __align__(1024) uint4 attention_lds_words[];
     const Item item = item_of<SHARE, WAVES>(p.k_heads, p.k_parts);
     const int head_k = item.head, part = item.part;
     const int64_t unit = item.unit;                               // behind a causal mask the first take longest
     if (unit >= p.k_units) return;
     int64_t k0 = 0, q0 = 0, first_all = 0;
     int nk = 0, nq = 0, all = 0, scene_at;
-    const int at = __builtin_amdgcn_readfirstlane(find_scene(p.k_starts, p.scenes, p.k_rows, 1, log2_of(COLUMNS), unit, first_all, all, scene_at).tile);
+    const int at = __builtin_amdgcn_readfirstlane(find_scene(p.k_starts, p.scenes, p.k_rows, 1, log2_of(COLUMNS), unit, p.k_units, first_all, all, scene_at).tile);
     if (at < 0) return;
     k0 = q0 = first_all;
     nk = nq = all;
@@ -758,10 +808,11 @@ k_attention_dkv(const Attention p) {
         queries.fetch(t * RT, left, lds0 + which * (2 * TILE_BYTES));
         grads.fetch(t * RT, left, lds0 + which * (2 * TILE_BYTES) + TILE_BYTES);
         const int64_t from = (int64_t)head * p.q_rows + q0 + t * RT + lane;
-        if ((SHARE != SHARED || wave == 0) && lane < RT)
-            load_word_to_lds(lane < left ? (const void*)(p.against + from) : (const void*)&g_no_weight, __builtin_amdgcn_readfirstlane(lds0 + SUMS + which * 512));
-        if ((SHARE != SHARED || wave == WAVES - 1) && lane < RT)
-            load_word_to_lds(lane < left ? (const void*)(p.delta + from) : (const void*)&g_no_chunk, __builtin_amdgcn_readfirstlane(lds0 + SUMS + which * 512 + 256));
+        // all lanes, with nothing for those beyond the tile: a branch of some lanes would be one more place where the compiler may save registers for them alone
+        if (SHARE != SHARED || wave == 0)
+            load_word_to_lds(lane < RT && lane < left ? (const void*)(p.against + from) : (const void*)&g_no_weight, __builtin_amdgcn_readfirstlane(lds0 + SUMS + which * 512));
+        if (SHARE != SHARED || wave == WAVES - 1)
+            load_word_to_lds(lane < RT && lane < left ? (const void*)(p.delta + from) : (const void*)&g_no_chunk, __builtin_amdgcn_readfirstlane(lds0 + SUMS + which * 512 + 256));
     };
     if (p.D < DPAD) {
         const TileLoader<DT, DPAD, RT, SHARE == SHARED ? 64 * WAVES : 64> tile{nullptr, 0, p.D};
@@ -871,7 +922,7 @@ k_attention_grad_join(const int32_t* __restrict__ starts, const int32_t* __restr
                       const float* __restrict__ a, HeadRows to_a, float scale_a, const float* __restrict__ b, HeadRows to_b) {
     int64_t first = 0;
     int count = 0, scene;
-    const int tile = __builtin_amdgcn_readfirstlane(find_scene(starts, scenes, rows, 1, 4, (int64_t)blockIdx.y * gridDim.x + blockIdx.x, first, count, scene).tile);
+    const int tile = __builtin_amdgcn_readfirstlane(find_scene(starts, scenes, rows, 1, 4, (int64_t)blockIdx.y * gridDim.x + blockIdx.x, (rows >> 4) + scenes, first, count, scene).tile);
     if (tile < 0) return;
     if (lens != nullptr) scene_rows(starts, lens, rows, scene, first, count);
     const int here = count - tile * 16 < 16 ? count - tile * 16 : 16, fours = (D + 3) / 4, row_items = heads * fours;
@@ -898,6 +949,39 @@ k_attention_grad_join(const int32_t* __restrict__ starts, const int32_t* __restr
     }
 }
 
+// A few parts joined: a thread has four channels of a row's head.
+constexpr int PARTS_FEW = 8;
+template <int DT>
+__global__ void __launch_bounds__(256)
+k_attention_join_few(const Attention p, int64_t entries, int q_heads) {
+    const int fours = (p.D + 3) / 4;
+    const int64_t item = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x, entry = item / fours;
+    if (entry >= entries) return;
+    const int64_t row = entry / q_heads;
+    if (p.q_starts != nullptr && (row < p.q_starts[0] || row >= p.q_starts[p.scenes])) return;        // a row of no scene stays as it is
+    const int channel = (int)(item - entry * fours) * 4;
+    float2 s[PARTS_FEW];
+    float top = NO_SCORE, sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < PARTS_FEW; ++k) s[k] = k < p.parts ? p.part_sums[k * entries + entry] : make_float2(0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < PARTS_FEW; ++k) top = s[k].y == 0.f ? top : fmaxf(top, s[k].x);
+    f32x4 v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < PARTS_FEW; ++k) {
+        if (s[k].y == 0.f) continue;                             // nothing seen: its results were not written
+        const float factor = __builtin_amdgcn_exp2f(s[k].x - top);
+        sum = fmaf(factor, s[k].y, sum);
+        const float* const from = p.part_out + (k * entries + entry) * p.D + channel;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = channel + j < p.D ? fmaf(factor, from[j], v[j]) : 0.f;
+    }
+    const float inverse = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] *= inverse;
+    store4<DT>(p.out.data + row * p.out.row + (entry - row * q_heads) * p.out.head, channel, p.D, v);
+    if (p.lse != nullptr && channel == 0) p.lse[entry] = sum == 0.f ? NO_SCORE : (__log2f(sum) + top) * 0.69314718055994531f;
+}
 // Parts joined: a workgroup has a row's head, its threads four channels and every so many of the parts.
 template <int DT>
 __global__ void __launch_bounds__(256)
@@ -978,9 +1062,9 @@ int start_attention(Attention p, hipStream_t s) {
 }
 template <int DT, int DPAD>
 int choose_attention(const Attention& p, AttentionShape shape, hipStream_t s) {
-    constexpr int NB = DT == SC_F32 && DPAD == 256 ? 1 : 2, WIDE = DPAD * ELEM<DT> <= 128 ? 4 : NB;
+    constexpr int NB = DT == SC_F32 && DPAD == 256 ? 1 : 2, LONE = DPAD == 256 ? 1 : 2, WIDE = DPAD * ELEM<DT> <= 128 ? 4 : LONE;
     if (shape == ATTENTION_FEW) return start_attention<DT, DPAD, 1, SPLIT>(p, s);
-    if (shape == ATTENTION_SHORT) return start_attention<DT, DPAD, NB, ALONE>(p, s);
+    if (shape == ATTENTION_SHORT) return start_attention<DT, DPAD, LONE, ALONE>(p, s);
     if (shape == ATTENTION_SHORT_64) return start_attention<DT, DPAD, WIDE, ALONE>(p, s);
     return start_attention<DT, DPAD, NB, SHARED>(p, s);
 }
@@ -992,6 +1076,10 @@ int launch_attention(const Attention& p, AttentionShape shape, hipStream_t s) {
     const int q_heads = p.k_heads * p.per;
     const int64_t entries = p.q_rows * q_heads;
     if (entries > BLOCKS_MAX) return SC_EINVAL;
+    if (p.parts <= PARTS_FEW) {
+        SC_LAUNCH(KID_ATTENTION_JOIN, k_attention_join_few<DT>, grid_of((entries * ((p.D + 3) / 4) + 255) / 256), dim3(256), 0, s, p, entries, q_heads);
+        return SC_OK;
+    }
     SC_LAUNCH(KID_ATTENTION_JOIN, k_attention_join<DT>, grid_of(entries), dim3(256), 0, s, p, entries, q_heads);
     return SC_OK;
 }
@@ -1017,7 +1105,7 @@ int start_attention_grad(Attention p, hipStream_t s) {
 }
 template <int DT, int DPAD>
 int choose_attention_grad(const Attention& p, bool alone, hipStream_t s) {
-    constexpr int NB = DPAD == 256 ? 1 : 2;
+    constexpr int NB = DPAD == 256 || (DT == SC_F32 && DPAD == 128) ? 1 : 2;
     return alone ? start_attention_grad<DT, DPAD, NB, ALONE>(p, s) : start_attention_grad<DT, DPAD, NB, SHARED>(p, s);
 }
 template <int DT>

@@ -119,7 +119,7 @@ extern "C" int sc_attention_fwd(const sc_heads* q, const sc_heads* k, const sc_h
     const Plan plan = plan_of(q_rows, k_rows, scenes, q->heads, k->heads);
     Attention p = attention_of(q, k, v, q_rows, k_rows, D, d_q_starts, d_k_starts, d_k_lens, scenes, causal, scale, out, d_lse, dtype);
     p.parts = plan.parts;
-    p.part_keys = ATTENTION_PART_KEYS;
+    p.part_keys = attention_part_keys(plan.shape);
     if (plan.parts > 1) {
         p.part_sums = (float2*)d_workspace;
         p.part_out = (float*)((char*)d_workspace + up16((size_t)plan.parts * q_rows * q->heads * sizeof(float2)));
@@ -160,7 +160,7 @@ extern "C" int sc_attention_bwd(const sc_heads* dout, const sc_heads* q, const s
     p.part_dv = (float*)(space + 2 * plan.sums + plan.part + plan.k_part);
     p.parts = plan.parts;
     p.k_parts = plan.k_parts;
-    p.part_keys = p.part_rows = plan.alone ? ATTENTION_PART_KEYS : ATTENTION_PART_ROWS;
+    p.part_keys = p.part_rows = attention_part_rows(plan.alone);
     hipStream_t s = (hipStream_t)stream;
     return dtype == SC_F32 ? launch_attention_grad_f32(p, plan.alone, s) : dtype == SC_F16 ? launch_attention_grad_f16(p, plan.alone, s) : launch_attention_grad_bf16(p, plan.alone, s);
 }

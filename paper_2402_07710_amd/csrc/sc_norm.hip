@@ -43,7 +43,7 @@ struct NormUnit {
 __device__ inline NormUnit unit_of(const Norm& p, int64_t u) {
     int64_t first = 0;
     int count = 0, scene = 0;
-    const int tile = __builtin_amdgcn_readfirstlane(find_scene(p.starts, p.scenes, p.rows, 1, p.per_log2, u, first, count, scene).tile);
+    const int tile = __builtin_amdgcn_readfirstlane(find_scene(p.starts, p.scenes, p.rows, 1, p.per_log2, u, p.units, first, count, scene).tile);
     if (tile < 0) return NormUnit{0, 0, 0};
     first = uniform64(first) + (int64_t)tile * p.per;
     const int left = __builtin_amdgcn_readfirstlane(count) - tile * p.per;
@@ -344,7 +344,7 @@ k_norm_grad_join(const Norm p) {
     __syncthreads();
     if (which != 0 || c >= p.C) return;
     sum = along = 0.0;
-#pragma unroll
+#pragma unroll 8
     for (int w = 0; w < 64; ++w) {
         sum += shared[0][w][threadIdx.x];
         along += shared[1][w][threadIdx.x];

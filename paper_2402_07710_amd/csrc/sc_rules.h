@@ -302,10 +302,11 @@ constexpr AttentionShape attention_shape(int64_t columns, int64_t scenes, int64_
     return attention_tiles(ATTENTION_WIDE, columns, scenes) * k_heads < 256 ? ATTENTION_SHORT : ATTENTION_WIDE;
 }
 // Parts that the keys of a scene are cut into where its columns alone do not fill the chip, and the keys that a part has at least.
-constexpr int ATTENTION_PARTS_MAX = 256, ATTENTION_PART_KEYS = 256;
+constexpr int ATTENTION_PARTS_MAX = 256;
+constexpr int attention_part_keys(AttentionShape shape) { return shape == ATTENTION_FEW || shape == ATTENTION_WIDE ? 256 : 64; }
 constexpr int attention_parts(AttentionShape shape, int64_t columns, int64_t scenes, int64_t k_heads, int64_t k_rows) {
     const int64_t wanted = shape == ATTENTION_WIDE ? 512 : 1024;
-    const int64_t most = (k_rows / scenes + ATTENTION_PART_KEYS - 1) / ATTENTION_PART_KEYS, there = attention_tiles(shape, columns, scenes) * k_heads;
+    const int64_t most = (k_rows / scenes + attention_part_keys(shape) - 1) / attention_part_keys(shape), there = attention_tiles(shape, columns, scenes) * k_heads;
     int64_t parts = (wanted + there - 1) / there;
     parts = parts < most ? parts : most;
     return (int)(parts < 1 ? 1 : parts < ATTENTION_PARTS_MAX ? parts : ATTENTION_PARTS_MAX);
@@ -315,10 +316,11 @@ constexpr bool attention_grad_alone(int64_t columns, int64_t scenes, int64_t k_h
     const int64_t most = columns > k_rows ? columns : k_rows;
     return most <= 96 * scenes || attention_tiles(ATTENTION_WIDE, most, scenes) * k_heads < 256;
 }
-constexpr int ATTENTION_GRAD_PARTS_MAX = 16, ATTENTION_PART_ROWS = 1024;
+constexpr int ATTENTION_GRAD_PARTS_MAX = 16;
+constexpr int attention_part_rows(bool alone) { return alone ? 64 : 1024; }
 // Parts of what `columns` of a scene walk, `rows` of the scenes together.
 constexpr int attention_grad_parts(bool alone, int64_t columns, int64_t scenes, int64_t k_heads, int64_t rows) {
-    const int64_t there = attention_tiles(alone ? ATTENTION_SHORT : ATTENTION_WIDE, columns, scenes) * k_heads, wanted = 1536, least = alone ? 256 : ATTENTION_PART_ROWS;
+    const int64_t there = attention_tiles(alone ? ATTENTION_SHORT : ATTENTION_WIDE, columns, scenes) * k_heads, wanted = 1536, least = attention_part_rows(alone);
     const int64_t most = (rows / scenes + least - 1) / least;
     int64_t parts = (wanted + there - 1) / there;
     parts = parts < most ? parts : most;

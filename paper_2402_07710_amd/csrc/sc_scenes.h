@@ -13,9 +13,10 @@ struct Scene {
 __device__ inline int64_t clamp_row(int64_t v, int64_t rows) { return v < 0 ? 0 : v > rows ? rows : v; }
 
 // Unit u of the scenes' columns cut into tiles of 2^log2 columns, `per` columns a row.  Scene s has the units from A(s) = start(s) per / 2^log2 + s on: at least as many as
-// it has tiles, one too many at most, so the host knows how many units there can be without the starts, and the device finds a unit's scene by a search
-// 63 wide, one trip to memory up to 63 scenes and two up to 3969.  Called by whole wavefronts.  Starts that do not ascend give wrong scenes, but never rows outside [0, rows).
-__device__ inline Scene find_scene(const int32_t* __restrict__ starts, int scenes, int64_t rows, int per, int log2, int64_t u, int64_t& first, int& count, int& scene) {
+// it has tiles, one too many at most, so the host knows how many units there can be without the starts (`units`), and the device finds a unit's scene by a search
+// 63 wide: one trip to memory up to 63 scenes; with more of them the first one looks about the place that scenes of equal length would give, and mostly finds it there, else two
+// more do up to 3969.  Called by whole wavefronts.  Starts that do not ascend give wrong scenes, but never rows outside [0, rows).
+__device__ inline Scene find_scene(const int32_t* __restrict__ starts, int scenes, int64_t rows, int per, int log2, int64_t u, int64_t units, int64_t& first, int& count, int& scene) {
     Scene found{0, 0, 0, 0, -1};
     const int lane = threadIdx.x & 63;
     scene = 0;
@@ -26,15 +27,32 @@ __device__ inline Scene find_scene(const int32_t* __restrict__ starts, int scene
         return found;
     }
     int lo = 0, hi = scenes;
+    bool guess = scenes > 63;
+    if (guess) {
+        lo = (int)((float)u / (float)units * (float)scenes) - 31;
+        lo = lo < 0 ? 0 : lo > scenes - 63 ? scenes - 63 : lo;
+        hi = lo + 63;
+    }
     for (;;) {
         const int step = (hi - lo + 62) / 63, s = lo + lane * step;
         int start = 0;
         bool below = false;
         if (s < hi || (s == hi && step == 1)) {
             start = (int)clamp_row(starts[s], rows);
-            below = s < hi && ((int64_t)start * per >> log2) + s <= u;
+            below = ((int64_t)start * per >> log2) + s <= u;
         }
-        const int n = __popcll(__ballot(below));
+        const uint64_t vote = __ballot(below);
+        if (guess && ((vote & 1) == 0 || (vote >> 63 != 0 && hi < scenes))) {      // before these, or behind them
+            guess = false;
+            if ((vote & 1) == 0) hi = lo;
+            else lo = hi;
+            if ((vote & 1) == 0) lo = 0;
+            else hi = scenes;
+            if (lo >= hi) return found;
+            continue;
+        }
+        int n = __popcll(vote);
+        if (step == 1 && n > hi - lo) n = hi - lo;
         if (n == 0) return found;
         if (step == 1) {
             const int begin = __builtin_amdgcn_readlane(start, n - 1), stop = __builtin_amdgcn_readlane(start, n);
@@ -42,7 +60,7 @@ __device__ inline Scene find_scene(const int32_t* __restrict__ starts, int scene
             first = begin;
             count = stop > begin ? stop - begin : 0;
             const int64_t nth = u - (((int64_t)begin * per >> log2) + scene);
-            if (nth << log2 < (int64_t)count * per) found.tile = (int)nth;
+            if (nth >= 0 && nth << log2 < (int64_t)count * per) found.tile = (int)nth;
             return found;
         }
         lo += (n - 1) * step;

@@ -164,3 +164,25 @@ def test_scenes(lens, key_lens, causal, dt):
 @pytest.mark.parametrize("hq,hk,D,causal", [(1, 1, 64, True), (6, 2, 40, True), (16, 1, 64, True), (7, 7, 24, False), (5, 1, 128, False), (64, 2, 16, True), (3, 1, 256, True)])
 def test_heads(hq, hk, D, causal, dt):
     both([1, 90, 31], [200, 90, 31], hq, hk, D, dt, causal)
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("D", [40, 128, 256])
+@pytest.mark.parametrize("causal", [False, True])
+def test_few_queries_over_many_keys(D, causal, dt):
+    """The keys are cut into parts, forward and backward, some of which a scene does not need."""
+    both([1, 2, 1], [1900, 0, 300], 4, 2, D, dt, causal)
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("causal", [False, True])
+def test_long_scenes(causal, dt):
+    """Four wavefronts share the tiles; queries are cut into parts backward."""
+    both([2500, 1, 1500], [2500, 1, 1500], 8, 4, 16, dt, causal, together=True)
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("lens", [[7, 40, 0, 64, 33] * 60, [1] * 300, [0] * 100 + [50] + [0] * 100, [900] + [3] * 150, [3] * 150 + [900], [40] * 64])
+def test_many_scenes(lens, dt):
+    """More scenes than one search looks at."""
+    both(lens, lens, 3, 3, 24, dt, False, lead=2, trail=1)
