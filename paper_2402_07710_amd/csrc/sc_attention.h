@@ -26,6 +26,8 @@ struct Attention {
     int scenes;
     int64_t q_rows, k_rows;
     int D, per, k_heads;               // per: heads of queries that share one of keys
+    uint32_t per_magic;                // ceil(2^(31 + s) / per), 2^s >= per > 2^(s - 1): c / per is the high word of c per_magic, s - 1 bits down, for c < 2^31
+    int per_shift;                     // s - 1
     int causal;
     float scale, scale_log2;           // ... times log2 e
     int64_t units;                     // column tiles there can be at most
@@ -41,6 +43,7 @@ struct Attention {
     float *against, *delta;            // [q_heads][q_rows]: lse times log2 e, infinite for a row that sees nothing; sum(do o)
 };
 
+__device__ __forceinline__ int row_of_column(const Attention& p, int c) { return p.per == 1 ? c : (int)(__umulhi((uint32_t)c, p.per_magic) >> p.per_shift); }
 // log2 of a tile of columns
 constexpr int log2_of(int tile) { return tile == 16 ? 4 : tile == 32 ? 5 : tile == 64 ? 6 : tile == 128 ? 7 : 8; }
 __device__ inline Scene scene_of_queries(const Attention& p, int log2, int64_t u) {
@@ -232,14 +235,24 @@ __device__ __forceinline__ void store4(char* row, int channel, int D, f32x4 v) {
             if (channel + j < D) store_elem<DT>(row, channel + j, v[j]);
     }
 }
+// Over the four quarters of the lanes, the same bits in all of them: two registers that hold a number and each other's halves, or neighbouring quarters, after a swap.
+template <class F>
+__device__ inline float over_quarters(float v, F&& join) {
+    const uint32_t bits = __builtin_bit_cast(uint32_t, v);
+    const auto a = __builtin_amdgcn_permlane16_swap(bits, bits, false, false);
+    v = join(__builtin_bit_cast(float, (uint32_t)a[0]), __builtin_bit_cast(float, (uint32_t)a[1]));
+    const uint32_t half = __builtin_bit_cast(uint32_t, v);
+    const auto b = __builtin_amdgcn_permlane32_swap(half, half, false, false);
+    return join(__builtin_bit_cast(float, (uint32_t)b[0]), __builtin_bit_cast(float, (uint32_t)b[1]));
+}
 __device__ inline float over_quarters_max(float v) {
-    v = fmaxf(v, __shfl_xor(v, 16));
-    return fmaxf(v, __shfl_xor(v, 32));
+    return over_quarters(v, [](float a, float b) { return fmaxf(a, b); });
 }
 __device__ inline float over_quarters_sum(float v) {
-    v += __shfl_xor(v, 16);
-    return v + __shfl_xor(v, 32);
+    return over_quarters(v, [](float a, float b) { return a + b; });
 }
+// Row r of a head whose first row is at `base`: strides of rows are below 2^32 bytes.
+__device__ __forceinline__ char* row_at(char* base, int r, int64_t row) { return base + (uint64_t)(uint32_t)r * (uint32_t)row; }
 __device__ inline void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 constexpr float NO_SCORE = -__builtin_inff();
@@ -331,20 +344,23 @@ k_attention(const Attention p) {
     // keys that a column sees: those below its limit
     auto limit_of = [&](int column) {
         if (!p.causal) return scene.nk;
-        const int n = column / p.per + ahead + 1;
+        const int n = row_of_column(p, column) + ahead + 1;
         return n < 0 ? 0 : n < scene.nk ? n : scene.nk;
     };
-    int row_of[NB], head_of[NB], limit[NB];
-    bool there[NB];
+    // row and head of a column, -1 where there is none; found again behind the loop, which has other use for the registers
+    auto place_of = [&](int c, int& row, int& head) __attribute__((always_inline)) {
+        row = c < columns ? row_of_column(p, c) : -1;
+        head = head_k * p.per + (c < columns ? c - row * p.per : 0);
+    };
+    int limit[NB];
     uint4 q[NB][H::KS];
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
         const int c = column0 + 16 * n + i;
-        there[n] = c < columns;
-        row_of[n] = there[n] ? c / p.per : 0;
-        head_of[n] = head_k * p.per + (there[n] ? c % p.per : 0);
-        limit[n] = there[n] ? limit_of(c) : 0;
-        load_columns<DT, DPAD>(there[n] ? p.q.data + (scene.q0 + row_of[n]) * p.q.row + head_of[n] * p.q.head : nullptr, p.D, q[n]);
+        int row, head;
+        place_of(c, row, head);
+        limit[n] = row >= 0 ? limit_of(c) : 0;
+        load_columns<DT, DPAD>(row >= 0 ? row_at(p.q.data + scene.q0 * p.q.row + head * p.q.head, row, p.q.row) : nullptr, p.D, q[n]);
     }
     const int first_limit = column0 < columns ? __builtin_amdgcn_readfirstlane(limit_of(column0)) : 0;          // of the wavefront's columns the least and the largest
     const int last_column = column0 + 16 * NB < columns ? column0 + 16 * NB - 1 : columns - 1;
@@ -544,8 +560,11 @@ k_attention(const Attention p) {
     }
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
-        if (!there[n]) continue;
-        const int64_t row = scene.q0 + row_of[n], entry = row * (p.k_heads * p.per) + head_of[n];
+        int c = column0 + 16 * n + i, row_there, head;
+        asm volatile("" : "+v"(c));
+        place_of(c, row_there, head);
+        if (row_there < 0) continue;
+        const int64_t row = scene.q0 + row_there, entry = row * (p.k_heads * p.per) + head;
         const bool first_writer = g == 0 && (SHARE != SPLIT || wave == 0);
         if (p.parts > 1) {
             const int64_t at = (int64_t)part * p.q_rows * (p.k_heads * p.per) + entry;
@@ -557,7 +576,7 @@ k_attention(const Attention p) {
             }
         } else {
             const float inverse = run[n].sum == 0.f ? 0.f : 1.f / run[n].sum;
-            char* const to_row = p.out.data + row * p.out.row + head_of[n] * p.out.head;
+            char* const to_row = row_at(p.out.data + scene.q0 * p.out.row + head * p.out.head, row_there, p.out.row);
 #pragma unroll
             for (int c = 0; c < H::CB; ++c)
                 if (SHARE != SPLIT || c % WAVES == wave) {
@@ -602,7 +621,7 @@ k_attention_dq(const Attention p) {
     const int ahead = scene.nk - scene.nq;
     auto limit_of = [&](int column) {
         if (!p.causal) return scene.nk;
-        const int n = column / p.per + ahead + 1;
+        const int n = row_of_column(p, column) + ahead + 1;
         return n < 0 ? 0 : n < scene.nk ? n : scene.nk;
     };
     int row_of[NB], head_of[NB], limit[NB];
@@ -614,16 +633,16 @@ k_attention_dq(const Attention p) {
     for (int n = 0; n < NB; ++n) {
         const int c = column0 + 16 * n + i;
         there[n] = c < columns;
-        row_of[n] = there[n] ? c / p.per : 0;
-        head_of[n] = head_k * p.per + (there[n] ? c % p.per : 0);
+        row_of[n] = there[n] ? row_of_column(p, c) : 0;
+        head_of[n] = head_k * p.per + (there[n] ? c - row_of[n] * p.per : 0);
         limit[n] = there[n] ? limit_of(c) : 0;
         const int64_t row = scene.q0 + row_of[n];
-        load_columns<DT, DPAD>(there[n] ? p.q.data + row * p.q.row + head_of[n] * p.q.head : nullptr, p.D, q[n]);
-        load_columns<DT, DPAD>(there[n] ? p.dout.data + row * p.dout.row + head_of[n] * p.dout.head : nullptr, p.D, dout[n]);
+        load_columns<DT, DPAD>(there[n] ? row_at(p.q.data + scene.q0 * p.q.row + head_of[n] * p.q.head, row_of[n], p.q.row) : nullptr, p.D, q[n]);
+        load_columns<DT, DPAD>(there[n] ? row_at(p.dout.data + scene.q0 * p.dout.row + head_of[n] * p.dout.head, row_of[n], p.dout.row) : nullptr, p.D, dout[n]);
         const float lse = there[n] ? p.lse[row * (p.k_heads * p.per) + head_of[n]] : NO_SCORE;
         against[n] = lse == NO_SCORE ? -NO_SCORE : lse * 1.4426950408889634f;
         uint4 out[H::KS];
-        load_columns<DT, DPAD>(there[n] ? p.out.data + row * p.out.row + head_of[n] * p.out.head : nullptr, p.D, out);
+        load_columns<DT, DPAD>(there[n] ? row_at(p.out.data + scene.q0 * p.out.row + head_of[n] * p.out.head, row_of[n], p.out.row) : nullptr, p.D, out);
         float sum = 0.f;
 #pragma unroll
         for (int k = 0; k < H::KS; ++k) {
@@ -731,7 +750,7 @@ k_attention_dq(const Attention p) {
         if (!there[n]) continue;
         const int64_t row = scene.q0 + row_of[n];
         float* const to_part = p.parts > 1 ? p.part_out + (((int64_t)part * p.q_rows + row) * (p.k_heads * p.per) + head_of[n]) * p.D : nullptr;
-        char* const to_row = p.dq.data + row * p.dq.row + head_of[n] * p.dq.head;
+        char* const to_row = row_at(p.dq.data + scene.q0 * p.dq.row + head_of[n] * p.dq.head, row_of[n], p.dq.row);
 #pragma unroll
         for (int c = 0; c < H::CB; ++c) {
             if (p.parts > 1) {
@@ -782,8 +801,8 @@ k_attention_dkv(const Attention p) {
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
         const int c = column0 + 16 * n + i;
-        load_columns<DT, DPAD>(c < nk ? p.k.data + (k0 + c) * p.k.row + head_k * p.k.head : nullptr, p.D, k[n]);
-        load_columns<DT, DPAD>(c < nk ? p.v.data + (k0 + c) * p.v.row + head_k * p.v.head : nullptr, p.D, v[n]);
+        load_columns<DT, DPAD>(c < nk ? row_at(p.k.data + k0 * p.k.row + head_k * p.k.head, c, p.k.row) : nullptr, p.D, k[n]);
+        load_columns<DT, DPAD>(c < nk ? row_at(p.v.data + k0 * p.v.row + head_k * p.v.head, c, p.v.row) : nullptr, p.D, v[n]);
 #pragma unroll
         for (int c = 0; c < H::CB; ++c) dk[n][c] = dv[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -899,8 +918,8 @@ k_attention_dkv(const Attention p) {
         const int c = column0 + 16 * n + i;
         if (c >= nk) continue;
         const int64_t at_part = (((int64_t)part * p.k_rows + k0 + c) * p.k_heads + head_k) * p.D;
-        char* const to_k = p.dk.data + (k0 + c) * p.dk.row + head_k * p.dk.head;
-        char* const to_v = p.dv.data + (k0 + c) * p.dv.row + head_k * p.dv.head;
+        char* const to_k = row_at(p.dk.data + k0 * p.dk.row + head_k * p.dk.head, c, p.dk.row);
+        char* const to_v = row_at(p.dv.data + k0 * p.dv.row + head_k * p.dv.head, c, p.dv.row);
 #pragma unroll
         for (int b = 0; b < H::CB; ++b) {
             if (p.k_parts > 1) {

@@ -86,6 +86,10 @@ Attention attention_of(const sc_heads* q, const sc_heads* k, const sc_heads* v, 
     p.k_rows = k_rows;
     p.D = D;
     p.per = q->heads / k->heads;
+    int log2 = 1;
+    while (1 << log2 < p.per) ++log2;
+    p.per_magic = (uint32_t)((((uint64_t)1 << (31 + log2)) + p.per - 1) / p.per);
+    p.per_shift = log2 - 1;
     p.k_heads = k->heads;
     p.causal = causal;
     p.scale = scale;

@@ -296,7 +296,7 @@ constexpr int64_t attention_tiles(AttentionShape shape, int64_t columns, int64_t
     return full > scenes ? full : scenes;
 }
 constexpr AttentionShape attention_shape(int64_t columns, int64_t scenes, int64_t k_heads, int64_t k_rows) {
-    if (columns <= 32 * scenes && k_rows >= 256 * scenes) return ATTENTION_FEW;
+    if (columns <= 32 * scenes && (k_rows >= 256 * scenes || scenes * k_heads < 512)) return ATTENTION_FEW;
     if (columns <= 32 * scenes) return ATTENTION_SHORT;
     if (columns <= 96 * scenes) return ATTENTION_SHORT_64;
     return attention_tiles(ATTENTION_WIDE, columns, scenes) * k_heads < 256 ? ATTENTION_SHORT : ATTENTION_WIDE;
