@@ -201,6 +201,14 @@ template <int DT, int DPAD>
 __device__ __forceinline__ void load_columns(const char* row, int D, uint4 (&q)[HeadShape<DT, DPAD>::KS]) {
     using H = HeadShape<DT, DPAD>;
     const int g = (threadIdx.x >> 4) & 3;
+    if (D % H::PER == 0) {
+#pragma unroll
+        for (int k = 0; k < H::KS; ++k) {
+            const int chunk = 4 * k + g;
+            q[k] = load_chunk(row != nullptr && chunk * H::PER < D ? row + chunk * 16 : (const char*)&g_no_chunk);
+        }
+        return;
+    }
 #pragma unroll
     for (int k = 0; k < H::KS; ++k) {
         const int chunk = 4 * k + g, there = row != nullptr ? D - chunk * H::PER : 0;
@@ -253,7 +261,12 @@ __device__ inline float over_quarters_sum(float v) {
 }
 // Row r of a head whose first row is at `base`: strides of rows are below 2^32 bytes.
 __device__ __forceinline__ char* row_at(char* base, int r, int64_t row) { return base + (uint64_t)(uint32_t)r * (uint32_t)row; }
-__device__ inline void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// All loads have arrived.  Said to the compiler too, which otherwise waits in the loop for the columns' loads ahead of it, and with them for the next tile's.
+__device__ inline void loads_done() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0f70);            // vmcnt(0)
+    asm volatile("" ::: "memory");
+}
 
 constexpr float NO_SCORE = -__builtin_inff();
 
