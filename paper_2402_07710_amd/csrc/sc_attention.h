@@ -90,8 +90,8 @@ __device__ inline void load_to_lds_at(const void* base, uint32_t offset, uint32_
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(lds) : "m0", "memory");
 }
 // The loads of one operand's tiles by NTH threads: rows first .. of a scene's head.  Zeros stand for rows that are not there and for channels beyond D: whole chunks of those
-// are cleared once, by clear(), and never written again.
-template <int DT, int DPAD, int ROWS, int NTH>
+// are cleared once, by clear(), and never written again.  WHOLE: D is a multiple of a chunk's channels.
+template <int DT, int DPAD, int ROWS, int NTH, bool WHOLE>
 struct TileLoader {
     using H = HeadShape<DT, DPAD>;
     static constexpr int PASSES = ROWS * H::LINE / NTH, LINES = NTH / H::LINE;       // lines of a pass
@@ -113,7 +113,7 @@ struct TileLoader {
     __device__ __forceinline__ void fetch(int first, int left, uint32_t lds) const {
         const int tid = (int)threadIdx.x % NTH, wave = __builtin_amdgcn_readfirstlane(tid >> 6), line = tid / H::LINE;
         const char* const from = (const char*)uniform64((int64_t)(base + (int64_t)first * row));
-        if (left >= ROWS && D % H::PER == 0) {
+        if (left >= ROWS && (WHOLE || D % H::PER == 0)) {
             const uint32_t offset = (uint32_t)line * (uint32_t)row;
 #pragma unroll
             for (int i = 0; i < PASSES; ++i) {
@@ -127,7 +127,7 @@ struct TileLoader {
         for (int i = 0; i < PASSES; ++i) {
             const int at = line + i * LINES, chunk = (tid % H::LINE) ^ tile_turn<DT, H::LINE>(at), there = at < left ? D - chunk * H::PER : 0;
             const char* const src = from + (int64_t)at * row + chunk * 16;
-            if (there >= H::PER || there <= 0) {
+            if (WHOLE || there >= H::PER || there <= 0) {
                 load_to_lds(there > 0 ? (const void*)src : (const void*)&g_no_chunk, __builtin_amdgcn_readfirstlane(lds + (i * NTH + wave * 64) * 16));
             } else {
                 uint32_t w[4] = {0, 0, 0, 0};
@@ -197,11 +197,11 @@ __device__ __forceinline__ uint4 weights_of(const f32x4 (&p)[ST], int step) {
     }
 }
 // A row's channels as the first product's second operand; zeros for channels beyond D and for a column that is none (null).
-template <int DT, int DPAD>
+template <int DT, int DPAD, bool WHOLE>
 __device__ __forceinline__ void load_columns(const char* row, int D, uint4 (&q)[HeadShape<DT, DPAD>::KS]) {
     using H = HeadShape<DT, DPAD>;
     const int g = (threadIdx.x >> 4) & 3;
-    if (D % H::PER == 0) {
+    if (WHOLE || D % H::PER == 0) {
 #pragma unroll
         for (int k = 0; k < H::KS; ++k) {
             const int chunk = 4 * k + g;
@@ -228,16 +228,16 @@ __device__ __forceinline__ void load_columns(const char* row, int D, uint4 (&q)[
     }
 }
 // Four consecutive channels of a row, those from D on left alone.
-template <int DT>
+template <int DT, bool WHOLE = false>
 __device__ __forceinline__ void store4(char* row, int channel, int D, f32x4 v) {
-    if (channel + 4 <= D) {
+    if (WHOLE ? channel < D : channel + 4 <= D) {
         if constexpr (DT == SC_F32) {
             store_chunk(row + channel * 4, __builtin_bit_cast(uint4, v));
         } else {
             typedef uint32_t half_chunk __attribute__((ext_vector_type(2), aligned(2)));
             *reinterpret_cast<half_chunk*>(row + channel * 2) = half_chunk{round2<DT>(v[0], v[1]), round2<DT>(v[2], v[3])};
         }
-    } else {
+    } else if (!WHOLE) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             if (channel + j < D) store_elem<DT>(row, channel + j, v[j]);
@@ -315,6 +315,9 @@ constexpr int wavefronts() {
     if (SHARE == SPLIT) return BYTES > 32768 ? 2 : 4;
     return BYTES > 32768 ? 1 : BYTES > 16384 ? 2 : 4;
 }
+// Blocks of 16 columns that go through a tile together, each row read from LDS once for all of them; ALONE one by one, and those only that have columns.
+template <int NB, int SHARE>
+constexpr int blocks_together() { return SHARE == ALONE ? 1 : NB; }
 // What a workgroup, or a wavefront ALONE, works on: neighbours have the heads of one unit.
 struct Item {
     int64_t unit;
@@ -336,12 +339,12 @@ __device__ inline void part_of(int all, int part, int parts, int64_t used, int& 
     to = part < used ? (int)((int64_t)all * (part + 1) / used) : 0;
 }
 
-template <int DT, int DPAD, int NB, int SHARE>
-__global__ void __launch_bounds__((64 * wavefronts<DT, DPAD, SHARE>()), (NB * HeadShape<DT, DPAD>::BYTES >= 1024 ? 1 : SHARE == ALONE && HeadShape<DT, DPAD>::BYTES <= 64 ? 3 : 2))
+template <int DT, int DPAD, int NB, int SHARE, bool WHOLE>
+__global__ void __launch_bounds__((64 * wavefronts<DT, DPAD, SHARE>()), (NB * HeadShape<DT, DPAD>::BYTES >= 1024 ? 1 : SHARE == ALONE && HeadShape<DT, DPAD>::BYTES <= 64 ? 4 : 2))
 k_attention(const Attention p) {
     using H = HeadShape<DT, DPAD>;
     constexpr int WAVES = wavefronts<DT, DPAD, SHARE>(), KT = walked_tile<DT, DPAD, SHARE>(), ST = KT / 16, TILE_BYTES = KT * H::BYTES;
-    constexpr int COLUMNS = 16 * NB * (SHARE == SHARED ? WAVES : 1);
+    constexpr int COLUMNS = 16 * NB * (SHARE == SHARED ? WAVES : 1), TOGETHER = blocks_together<NB, SHARE>();
     extern __shared__ __align__(1024) uint4 attention_lds_words[];
     const Item item = item_of<SHARE, WAVES>(p.k_heads, p.parts);
     const int head_k = item.head, part = item.part;
@@ -373,7 +376,7 @@ k_attention(const Attention p) {
         int row, head;
         place_of(c, row, head);
         limit[n] = row >= 0 ? limit_of(c) : 0;
-        load_columns<DT, DPAD>(row >= 0 ? row_at(p.q.data + scene.q0 * p.q.row + head * p.q.head, row, p.q.row) : nullptr, p.D, q[n]);
+        load_columns<DT, DPAD, WHOLE>(row >= 0 ? row_at(p.q.data + scene.q0 * p.q.row + head * p.q.head, row, p.q.row) : nullptr, p.D, q[n]);
     }
     const int first_limit = column0 < columns ? __builtin_amdgcn_readfirstlane(limit_of(column0)) : 0;          // of the wavefront's columns the least and the largest
     const int last_column = column0 + 16 * NB < columns ? column0 + 16 * NB - 1 : columns - 1;
@@ -385,7 +388,7 @@ k_attention(const Attention p) {
 
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)attention_lds_words;
     const uint32_t mine = lds0 + (SHARE == SHARED ? 0 : wave * (4 * TILE_BYTES));
-    const TileLoader<DT, DPAD, KT, SHARE == SHARED ? 64 * WAVES : 64> keys{p.k.data + scene.k0 * p.k.row + head_k * p.k.head, p.k.row, p.D},
+    const TileLoader<DT, DPAD, KT, SHARE == SHARED ? 64 * WAVES : 64, WHOLE> keys{p.k.data + scene.k0 * p.k.row + head_k * p.k.head, p.k.row, p.D},
         values{p.v.data + scene.k0 * p.v.row + head_k * p.v.head, p.v.row, p.D};
     const RowReader<DT, DPAD> rows(mine);
     const ChannelReader<DT, DPAD> channels(mine + TILE_BYTES);
@@ -415,114 +418,73 @@ k_attention(const Attention p) {
         else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (t + STRIDE < to) bring(t + STRIDE, buffer ^ (2 * TILE_BYTES));
         const int key0 = t * KT;
-        if constexpr (SHARE == ALONE) {                           // block by block, and those only that have columns
+        if (SHARE == ALONE || key0 < wave_limit) {
 #pragma unroll
-            for (int n = 0; n < NB; ++n) {
-                if (column0 + 16 * n >= columns) break;
-                f32x4 s[ST];
+            for (int n0 = 0; n0 < NB; n0 += TOGETHER) {
+                if (SHARE == ALONE && column0 + 16 * n0 >= columns) break;
+                f32x4 s[TOGETHER][ST];
 #pragma unroll
-                for (int b = 0; b < ST; ++b) s[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int n = 0; n < TOGETHER; ++n)
+#pragma unroll
+                    for (int b = 0; b < ST; ++b) s[n][b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int k = 0; k < H::KS; ++k)
 #pragma unroll
-                    for (int b = 0; b < ST; ++b) s[b] = multiply<DT>(rows.read(buffer, b, k), q[n][k], s[b]);
+                    for (int b = 0; b < ST; ++b) {
+                        const uint4 a = rows.read(buffer, b, k);
+#pragma unroll
+                        for (int n = 0; n < TOGETHER; ++n) s[n][b] = multiply<DT>(a, q[n0 + n][k], s[n][b]);
+                    }
                 if (key0 + KT > first_limit) {
-                    const int least = p.causal ? limit[n] : scene.nk;
+#pragma unroll
+                    for (int n = 0; n < TOGETHER; ++n)
+#pragma unroll
+                        for (int b = 0; b < ST; ++b)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) s[n][b][r] = key0 + 16 * b + 4 * g + r < limit[n0 + n] ? s[n][b][r] : NO_SCORE;
+                }
+                float most[TOGETHER];
+                bool calm = true;
+#pragma unroll
+                for (int n = 0; n < TOGETHER; ++n) {
+                    most[n] = s[n][0][0];
 #pragma unroll
                     for (int b = 0; b < ST; ++b)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) s[b][r] = key0 + 16 * b + 4 * g + r < least ? s[b][r] : NO_SCORE;
+                        for (int r = 0; r < 4; ++r) most[n] = fmaxf(most[n], s[n][b][r]);
+                    most[n] *= p.scale_log2;
+                    calm = calm && most[n] <= run[n0 + n].top + CALM;
                 }
-                float most = s[0][0];
+                if (!__all(calm)) {
 #pragma unroll
-                for (int b = 0; b < ST; ++b)
+                    for (int n = 0; n < TOGETHER; ++n) {
+                        const float factor = follow<DT>(run[n0 + n], over_quarters_max(most[n]));
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) most = fmaxf(most, s[b][r]);
-                most *= p.scale_log2;
-                if (!__all(most <= run[n].top + CALM)) {
-                    const float factor = follow<DT>(run[n], over_quarters_max(most));
+                        for (int c = 0; c < H::CB; ++c)
 #pragma unroll
-                    for (int c = 0; c < H::CB; ++c)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) out[n][c][r] *= factor;
-                }
-#pragma unroll
-                for (int b = 0; b < ST; ++b)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        s[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], p.scale_log2, -run[n].against));
-                        run[n].sum += s[b][r];
+                            for (int r = 0; r < 4; ++r) out[n0 + n][c][r] *= factor;
                     }
+                }
+#pragma unroll
+                for (int n = 0; n < TOGETHER; ++n)
+#pragma unroll
+                    for (int b = 0; b < ST; ++b)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            s[n][b][r] = __builtin_amdgcn_exp2f(fmaf(s[n][b][r], p.scale_log2, -run[n0 + n].against));
+                            run[n0 + n].sum += s[n][b][r];
+                        }
 #pragma unroll
                 for (int u = 0; u < KT / H::STEP; ++u) {
-                    const uint4 w = weights_of<DT, ST>(s, u);
+                    uint4 w[TOGETHER];
 #pragma unroll
-                    for (int c = 0; c < H::CB; ++c) out[n][c] = multiply<DT>(channels.read(buffer, u, c), w, out[n][c]);
-                }
-            }
-        } else if (key0 < wave_limit) {
-            f32x4 s[NB][ST];
+                    for (int n = 0; n < TOGETHER; ++n) w[n] = weights_of<DT, ST>(s[n], u);
 #pragma unroll
-            for (int n = 0; n < NB; ++n)
+                    for (int c = 0; c < H::CB; ++c) {
+                        const uint4 a = channels.read(buffer, u, c);
 #pragma unroll
-                for (int b = 0; b < ST; ++b) s[n][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int k = 0; k < H::KS; ++k)
-#pragma unroll
-                for (int b = 0; b < ST; ++b) {
-                    const uint4 a = rows.read(buffer, b, k);
-#pragma unroll
-                    for (int n = 0; n < NB; ++n) s[n][b] = multiply<DT>(a, q[n][k], s[n][b]);
-                }
-            if (key0 + KT > first_limit) {
-#pragma unroll
-                for (int n = 0; n < NB; ++n)
-#pragma unroll
-                    for (int b = 0; b < ST; ++b)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) s[n][b][r] = key0 + 16 * b + 4 * g + r < limit[n] ? s[n][b][r] : NO_SCORE;
-            }
-            float most[NB];
-            bool calm = true;
-#pragma unroll
-            for (int n = 0; n < NB; ++n) {
-                most[n] = s[n][0][0];
-#pragma unroll
-                for (int b = 0; b < ST; ++b)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) most[n] = fmaxf(most[n], s[n][b][r]);
-                most[n] *= p.scale_log2;
-                calm = calm && most[n] <= run[n].top + CALM;
-            }
-            if (!__all(calm)) {
-#pragma unroll
-                for (int n = 0; n < NB; ++n) {
-                    const float factor = follow<DT>(run[n], over_quarters_max(most[n]));
-#pragma unroll
-                    for (int c = 0; c < H::CB; ++c)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) out[n][c][r] *= factor;
-                }
-            }
-#pragma unroll
-            for (int n = 0; n < NB; ++n)
-#pragma unroll
-                for (int b = 0; b < ST; ++b)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        s[n][b][r] = __builtin_amdgcn_exp2f(fmaf(s[n][b][r], p.scale_log2, -run[n].against));
-                        run[n].sum += s[n][b][r];
+                        for (int n = 0; n < TOGETHER; ++n) out[n0 + n][c] = multiply<DT>(a, w[n], out[n0 + n][c]);
                     }
-#pragma unroll
-            for (int u = 0; u < KT / H::STEP; ++u) {
-                uint4 w[NB];
-#pragma unroll
-                for (int n = 0; n < NB; ++n) w[n] = weights_of<DT, ST>(s[n], u);
-#pragma unroll
-                for (int c = 0; c < H::CB; ++c) {
-                    const uint4 a = channels.read(buffer, u, c);
-#pragma unroll
-                    for (int n = 0; n < NB; ++n) out[n][c] = multiply<DT>(a, w[n], out[n][c]);
                 }
             }
         }
@@ -585,7 +547,7 @@ k_attention(const Attention p) {
             if (from < to) {
 #pragma unroll
                 for (int c = 0; c < H::CB; ++c)
-                    if (SHARE != SPLIT || c % WAVES == wave) store4<SC_F32>((char*)(p.part_out + at * p.D), 16 * c + 4 * g, p.D, out[n][c]);
+                    if (SHARE != SPLIT || c % WAVES == wave) store4<SC_F32, WHOLE>((char*)(p.part_out + at * p.D), 16 * c + 4 * g, p.D, out[n][c]);
             }
         } else {
             const float inverse = run[n].sum == 0.f ? 0.f : 1.f / run[n].sum;
@@ -595,7 +557,7 @@ k_attention(const Attention p) {
                 if (SHARE != SPLIT || c % WAVES == wave) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) out[n][c][r] *= inverse;
-                    store4<DT>(to_row, 16 * c + 4 * g, p.D, out[n][c]);
+                    store4<DT, WHOLE>(to_row, 16 * c + 4 * g, p.D, out[n][c]);
                 }
             if (p.lse != nullptr && first_writer) p.lse[entry] = run[n].sum == 0.f ? NO_SCORE : (__log2f(run[n].sum) + run[n].against) * 0.69314718055994531f;
         }
@@ -614,12 +576,12 @@ constexpr int grad_waves(int rows, int results) {                 // wavefronts 
     return NB * (rows * HeadShape<DT, DPAD>::KS * 4 + results * HeadShape<DT, DPAD>::CB * 4) > (DT == SC_F32 ? 120 : 180) ? 1 : 2;
 }
 
-template <int DT, int DPAD, int NB, int SHARE>
+template <int DT, int DPAD, int NB, int SHARE, bool WHOLE>
 __global__ void __launch_bounds__((64 * wavefronts<DT, DPAD, SHARE>()), (grad_waves<DT, DPAD, NB>(2, 1)))
 k_attention_dq(const Attention p) {
     using H = HeadShape<DT, DPAD>;
     constexpr int WAVES = wavefronts<DT, DPAD, SHARE>(), KT = walked_tile<DT, DPAD, SHARE>(), TILE_BYTES = KT * H::BYTES, COLUMNS = 16 * NB * (SHARE == SHARED ? WAVES : 1);
-    constexpr int SUB = sc::SUB<DT, DPAD, SHARE>, SUB_BLOCKS = SUB / 16;
+    constexpr int SUB = sc::SUB<DT, DPAD, SHARE>, SUB_BLOCKS = SUB / 16, TOGETHER = blocks_together<NB, SHARE>();
     extern __shared__ __align__(1024) uint4 attention_lds_words[];
     const Item item = item_of<SHARE, WAVES>(p.k_heads, p.parts);
     const int head_k = item.head, part = item.part;
@@ -650,12 +612,12 @@ k_attention_dq(const Attention p) {
         head_of[n] = head_k * p.per + (there[n] ? c - row_of[n] * p.per : 0);
         limit[n] = there[n] ? limit_of(c) : 0;
         const int64_t row = scene.q0 + row_of[n];
-        load_columns<DT, DPAD>(there[n] ? row_at(p.q.data + scene.q0 * p.q.row + head_of[n] * p.q.head, row_of[n], p.q.row) : nullptr, p.D, q[n]);
-        load_columns<DT, DPAD>(there[n] ? row_at(p.dout.data + scene.q0 * p.dout.row + head_of[n] * p.dout.head, row_of[n], p.dout.row) : nullptr, p.D, dout[n]);
+        load_columns<DT, DPAD, WHOLE>(there[n] ? row_at(p.q.data + scene.q0 * p.q.row + head_of[n] * p.q.head, row_of[n], p.q.row) : nullptr, p.D, q[n]);
+        load_columns<DT, DPAD, WHOLE>(there[n] ? row_at(p.dout.data + scene.q0 * p.dout.row + head_of[n] * p.dout.head, row_of[n], p.dout.row) : nullptr, p.D, dout[n]);
         const float lse = there[n] ? p.lse[row * (p.k_heads * p.per) + head_of[n]] : NO_SCORE;
         against[n] = lse == NO_SCORE ? -NO_SCORE : lse * 1.4426950408889634f;
         uint4 out[H::KS];
-        load_columns<DT, DPAD>(there[n] ? row_at(p.out.data + scene.q0 * p.out.row + head_of[n] * p.out.head, row_of[n], p.out.row) : nullptr, p.D, out);
+        load_columns<DT, DPAD, WHOLE>(there[n] ? row_at(p.out.data + scene.q0 * p.out.row + head_of[n] * p.out.head, row_of[n], p.out.row) : nullptr, p.D, out);
         float sum = 0.f;
 #pragma unroll
         for (int k = 0; k < H::KS; ++k) {
@@ -688,7 +650,7 @@ k_attention_dq(const Attention p) {
     if (p.parts > 1) part_of(tiles, part, p.parts, ((int64_t)tiles * KT + p.part_keys - 1) / p.part_keys, from, to);
 
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)attention_lds_words + (SHARE == SHARED ? 0 : wave * (4 * TILE_BYTES));
-    const TileLoader<DT, DPAD, KT, SHARE == SHARED ? 64 * WAVES : 64> keys{p.k.data + scene.k0 * p.k.row + head_k * p.k.head, p.k.row, p.D},
+    const TileLoader<DT, DPAD, KT, SHARE == SHARED ? 64 * WAVES : 64, WHOLE> keys{p.k.data + scene.k0 * p.k.row + head_k * p.k.head, p.k.row, p.D},
         values{p.v.data + scene.k0 * p.v.row + head_k * p.v.head, p.v.row, p.D};
     const RowReader<DT, DPAD> rows(lds0);
     const ChannelReader<DT, DPAD> channels(lds0);
@@ -712,47 +674,51 @@ k_attention_dq(const Attention p) {
             const int key0 = t * KT + h * SUB;
             const uint32_t tile = buffer + h * (SUB * H::BYTES);
             if (key0 >= wave_limit) break;
-            f32x4 s[NB][SUB_BLOCKS], dp[NB][SUB_BLOCKS];
 #pragma unroll
-            for (int n = 0; n < NB; ++n)
+            for (int n0 = 0; n0 < NB; n0 += TOGETHER) {
+                if (SHARE == ALONE && column0 + 16 * n0 >= columns) break;
+                f32x4 s[TOGETHER][SUB_BLOCKS], dp[TOGETHER][SUB_BLOCKS];
 #pragma unroll
-                for (int b = 0; b < SUB_BLOCKS; ++b) s[n][b] = dp[n][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int n = 0; n < TOGETHER; ++n)
 #pragma unroll
-            for (int k = 0; k < H::KS; ++k)
+                    for (int b = 0; b < SUB_BLOCKS; ++b) s[n][b] = dp[n][b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int b = 0; b < SUB_BLOCKS; ++b) {
-                    const uint4 a = rows.read(tile, b, k), v = rows.read(tile + TILE_BYTES, b, k);
+                for (int k = 0; k < H::KS; ++k)
 #pragma unroll
-                    for (int n = 0; n < NB; ++n) {
-                        s[n][b] = multiply<DT>(a, q[n][k], s[n][b]);
-                        dp[n][b] = multiply<DT>(v, dout[n][k], dp[n][b]);
+                    for (int b = 0; b < SUB_BLOCKS; ++b) {
+                        const uint4 a = rows.read(tile, b, k), v = rows.read(tile + TILE_BYTES, b, k);
+#pragma unroll
+                        for (int n = 0; n < TOGETHER; ++n) {
+                            s[n][b] = multiply<DT>(a, q[n0 + n][k], s[n][b]);
+                            dp[n][b] = multiply<DT>(v, dout[n0 + n][k], dp[n][b]);
+                        }
                     }
-                }
 #pragma unroll
-            for (int n = 0; n < NB; ++n)
-#pragma unroll
-                for (int b = 0; b < SUB_BLOCKS; ++b)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        s[n][b][r] = __builtin_amdgcn_exp2f(fmaf(s[n][b][r], p.scale_log2, -against[n])) * (dp[n][b][r] - delta[n]);
-            if (key0 + SUB > first_limit) {
-#pragma unroll
-                for (int n = 0; n < NB; ++n)
+                for (int n = 0; n < TOGETHER; ++n)
 #pragma unroll
                     for (int b = 0; b < SUB_BLOCKS; ++b)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) s[n][b][r] = key0 + 16 * b + 4 * g + r < limit[n] ? s[n][b][r] : 0.f;
-            }
+                        for (int r = 0; r < 4; ++r)
+                            s[n][b][r] = __builtin_amdgcn_exp2f(fmaf(s[n][b][r], p.scale_log2, -against[n0 + n])) * (dp[n][b][r] - delta[n0 + n]);
+                if (key0 + SUB > first_limit) {
 #pragma unroll
-            for (int u = 0; u < SUB / H::STEP; ++u) {
-                uint4 w[NB];
+                    for (int n = 0; n < TOGETHER; ++n)
 #pragma unroll
-                for (int n = 0; n < NB; ++n) w[n] = weights_of<DT, SUB_BLOCKS>(s[n], u);
+                        for (int b = 0; b < SUB_BLOCKS; ++b)
 #pragma unroll
-                for (int c = 0; c < H::CB; ++c) {
-                    const uint4 a = channels.read(tile, u, c);
+                            for (int r = 0; r < 4; ++r) s[n][b][r] = key0 + 16 * b + 4 * g + r < limit[n0 + n] ? s[n][b][r] : 0.f;
+                }
 #pragma unroll
-                    for (int n = 0; n < NB; ++n) dq[n][c] = multiply<DT>(a, w[n], dq[n][c]);
+                for (int u = 0; u < SUB / H::STEP; ++u) {
+                    uint4 w[TOGETHER];
+#pragma unroll
+                    for (int n = 0; n < TOGETHER; ++n) w[n] = weights_of<DT, SUB_BLOCKS>(s[n], u);
+#pragma unroll
+                    for (int c = 0; c < H::CB; ++c) {
+                        const uint4 a = channels.read(tile, u, c);
+#pragma unroll
+                        for (int n = 0; n < TOGETHER; ++n) dq[n0 + n][c] = multiply<DT>(a, w[n], dq[n0 + n][c]);
+                    }
                 }
             }
         }
@@ -767,12 +733,12 @@ k_attention_dq(const Attention p) {
 #pragma unroll
         for (int c = 0; c < H::CB; ++c) {
             if (p.parts > 1) {
-                store4<SC_F32>((char*)to_part, 16 * c + 4 * g, p.D, dq[n][c]);
+                store4<SC_F32, WHOLE>((char*)to_part, 16 * c + 4 * g, p.D, dq[n][c]);
                 continue;
             }
 #pragma unroll
             for (int r = 0; r < 4; ++r) dq[n][c][r] *= p.scale;
-            store4<DT>(to_row, 16 * c + 4 * g, p.D, dq[n][c]);
+            store4<DT, WHOLE>(to_row, 16 * c + 4 * g, p.D, dq[n][c]);
         }
     }
 }
@@ -781,12 +747,12 @@ k_attention_dq(const Attention p) {
 __device__ float g_no_weight = __builtin_inff();
 
 constexpr int SUMS_BYTES = 4 * 64 * sizeof(float);
-template <int DT, int DPAD, int NB, int SHARE>
+template <int DT, int DPAD, int NB, int SHARE, bool WHOLE>
 __global__ void __launch_bounds__((64 * wavefronts<DT, DPAD, SHARE>()), (grad_waves<DT, DPAD, NB>(2, 2)))
 k_attention_dkv(const Attention p) {
     using H = HeadShape<DT, DPAD>;
     constexpr int WAVES = wavefronts<DT, DPAD, SHARE>(), RT = walked_tile<DT, DPAD, SHARE>(), TILE_BYTES = RT * H::BYTES, COLUMNS = 16 * NB * (SHARE == SHARED ? WAVES : 1);
-    constexpr int SUB = sc::SUB<DT, DPAD, SHARE>, SUB_BLOCKS = SUB / 16;
+    constexpr int SUB = sc::SUB<DT, DPAD, SHARE>, SUB_BLOCKS = SUB / 16, TOGETHER = blocks_together<NB, SHARE>();
     extern __shared__ __align__(1024) uint4 attention_lds_words[];
     const Item item = item_of<SHARE, WAVES>(p.k_heads, p.k_parts);
     const int head_k = item.head, part = item.part;
@@ -814,8 +780,8 @@ k_attention_dkv(const Attention p) {
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
         const int c = column0 + 16 * n + i;
-        load_columns<DT, DPAD>(c < nk ? row_at(p.k.data + k0 * p.k.row + head_k * p.k.head, c, p.k.row) : nullptr, p.D, k[n]);
-        load_columns<DT, DPAD>(c < nk ? row_at(p.v.data + k0 * p.v.row + head_k * p.v.head, c, p.v.row) : nullptr, p.D, v[n]);
+        load_columns<DT, DPAD, WHOLE>(c < nk ? row_at(p.k.data + k0 * p.k.row + head_k * p.k.head, c, p.k.row) : nullptr, p.D, k[n]);
+        load_columns<DT, DPAD, WHOLE>(c < nk ? row_at(p.v.data + k0 * p.v.row + head_k * p.v.head, c, p.v.row) : nullptr, p.D, v[n]);
 #pragma unroll
         for (int c = 0; c < H::CB; ++c) dk[n][c] = dv[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -835,7 +801,7 @@ k_attention_dkv(const Attention p) {
     if (p.k_parts > 1) part_of(total, part, p.k_parts, ((int64_t)total * RT + p.part_rows - 1) / p.part_rows, from, to);
     auto bring = [&](int n, int which) __attribute__((always_inline)) {
         const int h = n / each, t = first_tile + n - h * each, head = head_k * p.per + h, left = nq - t * RT;
-        const TileLoader<DT, DPAD, RT, SHARE == SHARED ? 64 * WAVES : 64> queries{p.q.data + q0 * p.q.row + head * p.q.head, p.q.row, p.D},
+        const TileLoader<DT, DPAD, RT, SHARE == SHARED ? 64 * WAVES : 64, WHOLE> queries{p.q.data + q0 * p.q.row + head * p.q.head, p.q.row, p.D},
             grads{p.dout.data + q0 * p.dout.row + head * p.dout.head, p.dout.row, p.D};
         queries.fetch(t * RT, left, lds0 + which * (2 * TILE_BYTES));
         grads.fetch(t * RT, left, lds0 + which * (2 * TILE_BYTES) + TILE_BYTES);
@@ -847,7 +813,7 @@ k_attention_dkv(const Attention p) {
             load_word_to_lds(lane < RT && lane < left ? (const void*)(p.delta + from) : (const void*)&g_no_chunk, __builtin_amdgcn_readfirstlane(lds0 + SUMS + which * 512 + 256));
     };
     if (p.D < DPAD) {
-        const TileLoader<DT, DPAD, RT, SHARE == SHARED ? 64 * WAVES : 64> tile{nullptr, 0, p.D};
+        const TileLoader<DT, DPAD, RT, SHARE == SHARED ? 64 * WAVES : 64, WHOLE> tile{nullptr, 0, p.D};
 #pragma unroll
         for (int b = 0; b < 4; ++b) tile.clear(lds0 + b * TILE_BYTES);
     }
@@ -865,62 +831,66 @@ k_attention_dkv(const Attention p) {
             const uint32_t tile = which * (2 * TILE_BYTES) + h * (SUB * H::BYTES);
             if (p.causal && row0 + SUB - 1 + ahead < column0) continue;       // none of the rows sees any of the keys
             if (row0 >= nq || column0 >= nk) break;
-            f32x4 s[NB][SUB_BLOCKS], dp[NB][SUB_BLOCKS];
-#pragma unroll
-            for (int m = 0; m < NB; ++m)
-#pragma unroll
-                for (int b = 0; b < SUB_BLOCKS; ++b) s[m][b] = dp[m][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int c = 0; c < H::KS; ++c)
-#pragma unroll
-                for (int b = 0; b < SUB_BLOCKS; ++b) {
-                    const uint4 a = rows.read(tile, b, c), d = rows.read(tile + TILE_BYTES, b, c);
-#pragma unroll
-                    for (int m = 0; m < NB; ++m) {
-                        s[m][b] = multiply<DT>(a, k[m][c], s[m][b]);
-                        dp[m][b] = multiply<DT>(d, v[m][c], dp[m][b]);
-                    }
-                }
             const bool masked = p.causal && row0 + ahead < last_column;
 #pragma unroll
-            for (int b = 0; b < SUB_BLOCKS; ++b) {
-                const uint32_t sums = lds0 + SUMS + which * 512 + (h * SUB + 16 * b + 4 * g) * 4;
-                const f32x4 against = __builtin_bit_cast(f32x4, *(lds_u32x4)sums), delta = __builtin_bit_cast(f32x4, *(lds_u32x4)(sums + 256));
+            for (int m0 = 0; m0 < NB; m0 += TOGETHER) {
+                if (SHARE == ALONE && column0 + 16 * m0 >= nk) break;
+                f32x4 s[TOGETHER][SUB_BLOCKS], dp[TOGETHER][SUB_BLOCKS];
 #pragma unroll
-                for (int m = 0; m < NB; ++m)
+                for (int m = 0; m < TOGETHER; ++m)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        s[m][b][r] = __builtin_amdgcn_exp2f(fmaf(s[m][b][r], p.scale_log2, -against[r]));
-                        dp[m][b][r] = s[m][b][r] * (dp[m][b][r] - delta[r]);
+                    for (int b = 0; b < SUB_BLOCKS; ++b) s[m][b] = dp[m][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < H::KS; ++c)
+#pragma unroll
+                    for (int b = 0; b < SUB_BLOCKS; ++b) {
+                        const uint4 a = rows.read(tile, b, c), d = rows.read(tile + TILE_BYTES, b, c);
+#pragma unroll
+                        for (int m = 0; m < TOGETHER; ++m) {
+                            s[m][b] = multiply<DT>(a, k[m0 + m][c], s[m][b]);
+                            dp[m][b] = multiply<DT>(d, v[m0 + m][c], dp[m][b]);
+                        }
                     }
-            }
-            if (masked) {
 #pragma unroll
-                for (int m = 0; m < NB; ++m)
+                for (int b = 0; b < SUB_BLOCKS; ++b) {
+                    const uint32_t sums = lds0 + SUMS + which * 512 + (h * SUB + 16 * b + 4 * g) * 4;
+                    const f32x4 against = __builtin_bit_cast(f32x4, *(lds_u32x4)sums), delta = __builtin_bit_cast(f32x4, *(lds_u32x4)(sums + 256));
 #pragma unroll
-                    for (int b = 0; b < SUB_BLOCKS; ++b)
+                    for (int m = 0; m < TOGETHER; ++m)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
-                            const bool seen = row0 + 16 * b + 4 * g + r + ahead >= column0 + 16 * m + i;
-                            s[m][b][r] = seen ? s[m][b][r] : 0.f;
-                            dp[m][b][r] = seen ? dp[m][b][r] : 0.f;
+                            s[m][b][r] = __builtin_amdgcn_exp2f(fmaf(s[m][b][r], p.scale_log2, -against[r]));
+                            dp[m][b][r] = s[m][b][r] * (dp[m][b][r] - delta[r]);
                         }
-            }
+                }
+                if (masked) {
 #pragma unroll
-            for (int u = 0; u < SUB / H::STEP; ++u) {
-                uint4 w[NB], z[NB];
+                    for (int m = 0; m < TOGETHER; ++m)
 #pragma unroll
-                for (int m = 0; m < NB; ++m) {
-                    w[m] = weights_of<DT, SUB_BLOCKS>(s[m], u);
-                    z[m] = weights_of<DT, SUB_BLOCKS>(dp[m], u);
+                        for (int b = 0; b < SUB_BLOCKS; ++b)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                const bool seen = row0 + 16 * b + 4 * g + r + ahead >= column0 + 16 * (m0 + m) + i;
+                                s[m][b][r] = seen ? s[m][b][r] : 0.f;
+                                dp[m][b][r] = seen ? dp[m][b][r] : 0.f;
+                            }
                 }
 #pragma unroll
-                for (int c = 0; c < H::CB; ++c) {
-                    const uint4 a = channels.read(tile + TILE_BYTES, u, c), b = channels.read(tile, u, c);
+                for (int u = 0; u < SUB / H::STEP; ++u) {
+                    uint4 w[TOGETHER], z[TOGETHER];
 #pragma unroll
-                    for (int m = 0; m < NB; ++m) {
-                        dv[m][c] = multiply<DT>(a, w[m], dv[m][c]);
-                        dk[m][c] = multiply<DT>(b, z[m], dk[m][c]);
+                    for (int m = 0; m < TOGETHER; ++m) {
+                        w[m] = weights_of<DT, SUB_BLOCKS>(s[m], u);
+                        z[m] = weights_of<DT, SUB_BLOCKS>(dp[m], u);
+                    }
+#pragma unroll
+                    for (int c = 0; c < H::CB; ++c) {
+                        const uint4 a = channels.read(tile + TILE_BYTES, u, c), b = channels.read(tile, u, c);
+#pragma unroll
+                        for (int m = 0; m < TOGETHER; ++m) {
+                            dv[m0 + m][c] = multiply<DT>(a, w[m], dv[m0 + m][c]);
+                            dk[m0 + m][c] = multiply<DT>(b, z[m], dk[m0 + m][c]);
+                        }
                     }
                 }
             }
@@ -936,14 +906,14 @@ k_attention_dkv(const Attention p) {
 #pragma unroll
         for (int b = 0; b < H::CB; ++b) {
             if (p.k_parts > 1) {
-                store4<SC_F32>((char*)(p.part_dk + at_part), 16 * b + 4 * g, p.D, dk[n][b]);
-                store4<SC_F32>((char*)(p.part_dv + at_part), 16 * b + 4 * g, p.D, dv[n][b]);
+                store4<SC_F32, WHOLE>((char*)(p.part_dk + at_part), 16 * b + 4 * g, p.D, dk[n][b]);
+                store4<SC_F32, WHOLE>((char*)(p.part_dv + at_part), 16 * b + 4 * g, p.D, dv[n][b]);
                 continue;
             }
 #pragma unroll
             for (int r = 0; r < 4; ++r) dk[n][b][r] *= p.scale;
-            store4<DT>(to_k, 16 * b + 4 * g, p.D, dk[n][b]);
-            store4<DT>(to_v, 16 * b + 4 * g, p.D, dv[n][b]);
+            store4<DT, WHOLE>(to_k, 16 * b + 4 * g, p.D, dk[n][b]);
+            store4<DT, WHOLE>(to_v, 16 * b + 4 * g, p.D, dv[n][b]);
         }
     }
 }
@@ -1077,9 +1047,9 @@ inline int64_t blocks_for(int64_t items) {
 inline dim3 grid_of(int64_t blocks) { return dim3((unsigned)grid_columns(blocks), (unsigned)grid_rows(blocks)); }
 constexpr int64_t BLOCKS_MAX = INT32_MAX / 4 - 2 * GRID_COLUMNS;
 
-template <int DT, int DPAD, int NB, int SHARE>
+template <int DT, int DPAD, int NB, int SHARE, bool WHOLE>
 int start_attention(Attention p, hipStream_t s) {
-    constexpr auto kernel = k_attention<DT, DPAD, NB, SHARE>;
+    constexpr auto kernel = k_attention<DT, DPAD, NB, SHARE, WHOLE>;
     constexpr int WAVES = wavefronts<DT, DPAD, SHARE>();
     constexpr size_t lds = (size_t)(SHARE == SHARED ? 1 : WAVES) * walked_bytes<DT, DPAD, SHARE>();
     static_assert(lds <= 163840, "of a CU");
@@ -1092,18 +1062,22 @@ int start_attention(Attention p, hipStream_t s) {
     SC_LAUNCH(KID_ATTENTION, kernel, grid_of(blocks), dim3(64 * WAVES), lds, s, p);
     return SC_OK;
 }
-template <int DT, int DPAD>
+template <int DT, int DPAD, bool WHOLE>
 int choose_attention(const Attention& p, AttentionShape shape, hipStream_t s) {
     constexpr int NB = DT == SC_F32 && DPAD == 256 ? 1 : 2, LONE = DPAD == 256 ? 1 : 2, WIDE = DPAD * ELEM<DT> <= 128 ? 4 : LONE;
-    if (shape == ATTENTION_FEW) return start_attention<DT, DPAD, 1, SPLIT>(p, s);
-    if (shape == ATTENTION_SHORT) return start_attention<DT, DPAD, LONE, ALONE>(p, s);
-    if (shape == ATTENTION_SHORT_64) return start_attention<DT, DPAD, WIDE, ALONE>(p, s);
-    return start_attention<DT, DPAD, NB, SHARED>(p, s);
+    if (shape == ATTENTION_FEW) return start_attention<DT, DPAD, 1, SPLIT, WHOLE>(p, s);
+    if (shape == ATTENTION_SHORT) return start_attention<DT, DPAD, LONE, ALONE, WHOLE>(p, s);
+    if (shape == ATTENTION_SHORT_64) return start_attention<DT, DPAD, WIDE, ALONE, WHOLE>(p, s);
+    return start_attention<DT, DPAD, NB, SHARED, WHOLE>(p, s);
+}
+template <int DT, bool WHOLE>
+int choose_head(const Attention& p, AttentionShape shape, hipStream_t s) {
+    return p.D <= 32 ? choose_attention<DT, 32, WHOLE>(p, shape, s) : p.D <= 64 ? choose_attention<DT, 64, WHOLE>(p, shape, s)
+           : p.D <= 128 ? choose_attention<DT, 128, WHOLE>(p, shape, s) : choose_attention<DT, 256, WHOLE>(p, shape, s);
 }
 template <int DT>
 int launch_attention(const Attention& p, AttentionShape shape, hipStream_t s) {
-    const int rc = p.D <= 32 ? choose_attention<DT, 32>(p, shape, s) : p.D <= 64 ? choose_attention<DT, 64>(p, shape, s)
-                 : p.D <= 128 ? choose_attention<DT, 128>(p, shape, s) : choose_attention<DT, 256>(p, shape, s);
+    const int rc = p.D * ELEM<DT> % 16 == 0 ? choose_head<DT, true>(p, shape, s) : choose_head<DT, false>(p, shape, s);
     if (rc != SC_OK || p.parts == 1) return rc;
     const int q_heads = p.k_heads * p.per;
     const int64_t entries = p.q_rows * q_heads;
@@ -1116,10 +1090,10 @@ int launch_attention(const Attention& p, AttentionShape shape, hipStream_t s) {
     return SC_OK;
 }
 
-template <int DT, int DPAD, int NB, int SHARE>
+template <int DT, int DPAD, int NB, int SHARE, bool WHOLE>
 int start_attention_grad(Attention p, hipStream_t s) {
-    constexpr auto of_queries = k_attention_dq<DT, DPAD, NB, SHARE>;
-    constexpr auto of_keys = k_attention_dkv<DT, DPAD, NB, SHARE>;
+    constexpr auto of_queries = k_attention_dq<DT, DPAD, NB, SHARE, WHOLE>;
+    constexpr auto of_keys = k_attention_dkv<DT, DPAD, NB, SHARE, WHOLE>;
     constexpr int WAVES = wavefronts<DT, DPAD, SHARE>(), COLUMNS = 16 * NB * (SHARE == SHARED ? WAVES : 1);
     constexpr size_t lds = (size_t)(SHARE == SHARED ? 1 : WAVES) * walked_bytes<DT, DPAD, SHARE>(), lds_keys = lds + (SHARE == SHARED ? 1 : WAVES) * SUMS_BYTES;
     static_assert(lds_keys <= 163840, "of a CU");
@@ -1135,15 +1109,19 @@ int start_attention_grad(Attention p, hipStream_t s) {
     if (p.k_rows > 0) SC_LAUNCH(KID_ATTENTION_DKV, of_keys, grid_of(key_blocks), dim3(64 * WAVES), lds_keys, s, p);
     return SC_OK;
 }
-template <int DT, int DPAD>
+template <int DT, int DPAD, bool WHOLE>
 int choose_attention_grad(const Attention& p, bool alone, hipStream_t s) {
     constexpr int NB = DPAD == 256 || (DT == SC_F32 && DPAD == 128) ? 1 : 2;
-    return alone ? start_attention_grad<DT, DPAD, NB, ALONE>(p, s) : start_attention_grad<DT, DPAD, NB, SHARED>(p, s);
+    return alone ? start_attention_grad<DT, DPAD, NB, ALONE, WHOLE>(p, s) : start_attention_grad<DT, DPAD, NB, SHARED, WHOLE>(p, s);
+}
+template <int DT, bool WHOLE>
+int choose_head_grad(const Attention& p, bool alone, hipStream_t s) {
+    return p.D <= 32 ? choose_attention_grad<DT, 32, WHOLE>(p, alone, s) : p.D <= 64 ? choose_attention_grad<DT, 64, WHOLE>(p, alone, s)
+           : p.D <= 128 ? choose_attention_grad<DT, 128, WHOLE>(p, alone, s) : choose_attention_grad<DT, 256, WHOLE>(p, alone, s);
 }
 template <int DT>
 int launch_attention_grad(const Attention& p, bool alone, hipStream_t s) {
-    const int rc = p.D <= 32 ? choose_attention_grad<DT, 32>(p, alone, s) : p.D <= 64 ? choose_attention_grad<DT, 64>(p, alone, s)
-                 : p.D <= 128 ? choose_attention_grad<DT, 128>(p, alone, s) : choose_attention_grad<DT, 256>(p, alone, s);
+    const int rc = p.D * ELEM<DT> % 16 == 0 ? choose_head_grad<DT, true>(p, alone, s) : choose_head_grad<DT, false>(p, alone, s);
     if (rc != SC_OK) return rc;
     const int q_heads = p.k_heads * p.per;
     if (p.parts > 1 && p.q_rows > 0)
