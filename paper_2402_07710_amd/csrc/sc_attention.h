@@ -501,7 +501,7 @@ k_attention(const Attention p) {
         constexpr int APART = TILE_BYTES;                         // floats from wavefront to wavefront: its own four tiles
         float* const own = shared + wave * APART;
         if (g == 0) {
-            own[2 * i] = run[0].top == NO_SCORE ? NO_SCORE : run[0].against;
+            own[2 * i] = run[0].sum == 0.f ? NO_SCORE : run[0].against;       // a sum that is no number has seen keys
             own[2 * i + 1] = run[0].sum;
         }
 #pragma unroll

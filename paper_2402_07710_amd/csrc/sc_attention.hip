@@ -24,10 +24,12 @@ struct Plan {
     AttentionShape shape;
     int parts;
 };
-Plan plan_of(int64_t q_rows, int64_t k_rows, int scenes, int q_heads, int k_heads) {
+// bytes of a row in LDS
+int row_bytes(int D, int dtype) { return (D <= 32 ? 32 : D <= 64 ? 64 : D <= 128 ? 128 : 256) * (dtype == SC_F32 ? 4 : 2); }
+Plan plan_of(int64_t q_rows, int64_t k_rows, int scenes, int q_heads, int k_heads, int D, int dtype) {
     const int64_t columns = q_rows * (q_heads / k_heads);
-    Plan plan{attention_shape(columns, scenes, k_heads, k_rows), 1};
-    plan.parts = q_rows == 0 ? 1 : attention_parts(plan.shape, columns, scenes, k_heads, k_rows);
+    Plan plan{attention_shape(columns, scenes, k_heads, k_rows, row_bytes(D, dtype)), 1};
+    plan.parts = q_rows == 0 ? 1 : attention_parts(plan.shape, columns, scenes, k_heads, k_rows, dtype == SC_F32);
     return plan;
 }
 struct GradPlan {
@@ -36,12 +38,12 @@ struct GradPlan {
     size_t sums, part, k_part;         // bytes in the workspace: exponents or deltas, partial gradients of queries, of keys (and as much of values)
 };
 size_t up16(size_t n) { return (n + 15) / 16 * 16; }
-GradPlan grad_plan_of(int64_t q_rows, int64_t k_rows, int scenes, int q_heads, int k_heads, int D) {
+GradPlan grad_plan_of(int64_t q_rows, int64_t k_rows, int scenes, int q_heads, int k_heads, int D, int dtype) {
     const int64_t per = q_heads / k_heads, columns = q_rows * per;
-    GradPlan plan{attention_grad_alone(columns, scenes, k_heads, k_rows), 1, 1, 0, 0, 0};
+    GradPlan plan{attention_grad_alone(columns, scenes, k_heads, k_rows, row_bytes(D, dtype), dtype == SC_F32), 1, 1, 0, 0, 0};
     if (q_rows > 0 && k_rows > 0) {
-        plan.parts = attention_grad_parts(plan.alone, columns, scenes, k_heads, k_rows);
-        plan.k_parts = attention_grad_parts(plan.alone, k_rows, scenes, k_heads, columns);
+        plan.parts = attention_grad_parts(plan.alone, columns, scenes, k_heads, k_rows, dtype == SC_F32);
+        plan.k_parts = attention_grad_parts(plan.alone, k_rows, scenes, k_heads, columns, dtype == SC_F32);
     }
     plan.sums = up16((size_t)q_rows * q_heads * sizeof(float));
     plan.part = plan.parts > 1 ? up16((size_t)plan.parts * q_rows * q_heads * D * sizeof(float)) : 0;
@@ -104,7 +106,7 @@ using namespace sc;
 
 extern "C" size_t sc_attention_workspace_bytes(int64_t q_rows, int64_t k_rows, int scenes, int q_heads, int k_heads, int D, int dtype) {
     if (!sizes_ok(q_rows, k_rows, scenes, q_heads, k_heads, D, dtype)) return 0;
-    const Plan plan = plan_of(q_rows, k_rows, scenes, q_heads, k_heads);
+    const Plan plan = plan_of(q_rows, k_rows, scenes, q_heads, k_heads, D, dtype);
     if (plan.parts == 1) return 0;
     const size_t entries = (size_t)plan.parts * q_rows * q_heads;
     return up16(entries * sizeof(float2)) + entries * D * sizeof(float);
@@ -120,10 +122,10 @@ extern "C" int sc_attention_fwd(const sc_heads* q, const sc_heads* k, const sc_h
     if (need > 0 && (d_workspace == nullptr || !aligned16(d_workspace))) return SC_EINVAL;
     if (workspace_bytes < need) return SC_ECAP;
     if (q_rows == 0) return SC_OK;
-    const Plan plan = plan_of(q_rows, k_rows, scenes, q->heads, k->heads);
+    const Plan plan = plan_of(q_rows, k_rows, scenes, q->heads, k->heads, D, dtype);
     Attention p = attention_of(q, k, v, q_rows, k_rows, D, d_q_starts, d_k_starts, d_k_lens, scenes, causal, scale, out, d_lse, dtype);
     p.parts = plan.parts;
-    p.part_keys = attention_part_keys(plan.shape);
+    p.part_keys = attention_part_keys(dtype == SC_F32);
     if (plan.parts > 1) {
         p.part_sums = (float2*)d_workspace;
         p.part_out = (float*)((char*)d_workspace + up16((size_t)plan.parts * q_rows * q->heads * sizeof(float2)));
@@ -134,7 +136,7 @@ extern "C" int sc_attention_fwd(const sc_heads* q, const sc_heads* k, const sc_h
 
 extern "C" size_t sc_attention_bwd_workspace_bytes(int64_t q_rows, int64_t k_rows, int scenes, int q_heads, int k_heads, int D, int dtype) {
     if (!sizes_ok(q_rows, k_rows, scenes, q_heads, k_heads, D, dtype)) return 0;
-    const GradPlan plan = grad_plan_of(q_rows, k_rows, scenes, q_heads, k_heads, D);
+    const GradPlan plan = grad_plan_of(q_rows, k_rows, scenes, q_heads, k_heads, D, dtype);
     return 2 * plan.sums + plan.part + 2 * plan.k_part;
 }
 
@@ -155,7 +157,7 @@ extern "C" int sc_attention_bwd(const sc_heads* dout, const sc_heads* q, const s
     p.dq = rows_of(dq, dtype);
     p.dk = rows_of(dk, dtype);
     p.dv = rows_of(dv, dtype);
-    const GradPlan plan = grad_plan_of(q_rows, k_rows, scenes, q->heads, k->heads, D);
+    const GradPlan plan = grad_plan_of(q_rows, k_rows, scenes, q->heads, k->heads, D, dtype);
     char* const space = (char*)d_workspace;
     p.against = (float*)space;
     p.delta = (float*)(space + plan.sums);
@@ -164,7 +166,7 @@ extern "C" int sc_attention_bwd(const sc_heads* dout, const sc_heads* q, const s
     p.part_dv = (float*)(space + 2 * plan.sums + plan.part + plan.k_part);
     p.parts = plan.parts;
     p.k_parts = plan.k_parts;
-    p.part_keys = p.part_rows = attention_part_rows(plan.alone);
+    p.part_keys = p.part_rows = attention_part_rows(plan.alone, dtype == SC_F32);
     hipStream_t s = (hipStream_t)stream;
     return dtype == SC_F32 ? launch_attention_grad_f32(p, plan.alone, s) : dtype == SC_F16 ? launch_attention_grad_f16(p, plan.alone, s) : launch_attention_grad_bf16(p, plan.alone, s);
 }

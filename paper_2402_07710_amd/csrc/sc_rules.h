@@ -286,7 +286,11 @@ constexpr int64_t ROPE_BLOCKS_MAX = 1024;
 constexpr int64_t scene_units(int64_t columns, int64_t scenes, int64_t tile) { return columns / tile + scenes; }
 
 // FEW: 16 columns a workgroup, whose wavefronts share the keys; SHORT: a wavefront has 32 or 64 columns and the keys to itself; WIDE: four
-// wavefronts, 128 columns.
+// wavefronts, 128 columns.  us of the call, f16, 8 heads, on either side of each line:
+//   FEW / WIDE       a scene of 256 rows of 64 5.9 / 7.6, 512 7.1 / 11, 1024 22 / 17; one row and 2048 keys 13.1 / 13.5, 8192 10.8 / 12.2, eight scenes 8192 30 / 30; 16 heads of 128 over 4, eight
+//                    scenes of 32768 keys 116 / 109
+//   SHORT 64 / WIDE  32768 rows of 32 in scenes of 96 21 / 27, 128 22 / 30, 192 29 / 28; of 64 in scenes of 48 32 / 39, 64 41 / 31; of 128 in scenes of 16 93 / 167, 32 103 / 96, 48 87 / 75
+//   SHORT, 32 / 64   2048 rows of 32 in scenes of 48 5.2 / 6.4; 32768 in scenes of 48 21.7 / 18.9
 enum AttentionShape { ATTENTION_FEW, ATTENTION_SHORT, ATTENTION_SHORT_64, ATTENTION_WIDE };
 constexpr int attention_columns(AttentionShape shape) {
     return shape == ATTENTION_FEW ? 16 : shape == ATTENTION_SHORT ? 32 : shape == ATTENTION_SHORT_64 ? 64 : 128;
@@ -295,33 +299,39 @@ constexpr int64_t attention_tiles(AttentionShape shape, int64_t columns, int64_t
     const int64_t full = (columns + attention_columns(shape) - 1) / attention_columns(shape);
     return full > scenes ? full : scenes;
 }
-constexpr AttentionShape attention_shape(int64_t columns, int64_t scenes, int64_t k_heads, int64_t k_rows) {
-    if (columns <= 32 * scenes && (k_rows >= 256 * scenes || scenes * k_heads < 512)) return ATTENTION_FEW;
-    if (columns <= 32 * scenes) return ATTENTION_SHORT;
-    if (columns <= 96 * scenes) return ATTENTION_SHORT_64;
-    return attention_tiles(ATTENTION_WIDE, columns, scenes) * k_heads < 256 ? ATTENTION_SHORT : ATTENTION_WIDE;
+constexpr AttentionShape attention_shape(int64_t columns, int64_t scenes, int64_t k_heads, int64_t k_rows, int row_bytes) {
+    if (attention_tiles(ATTENTION_FEW, columns, scenes) * k_heads <= 256 && k_rows * k_heads <= 262144) return ATTENTION_FEW;
+    if (columns * row_bytes < 8192 * scenes && k_rows <= 256 * scenes) return attention_tiles(ATTENTION_SHORT_64, columns, scenes) * k_heads < 4096 ? ATTENTION_SHORT : ATTENTION_SHORT_64;
+    return ATTENTION_WIDE;
 }
-// Parts that the keys of a scene are cut into where its columns alone do not fill the chip, and the keys that a part has at least.
+// Parts that the keys of a scene are cut into where its columns alone do not fill the chip, and the keys that a part has at least.  Joining them is a launch of 4 to 6 us more: one row of 8 heads
+// of 64, f16, over 512 keys whole / in parts 6.8 / 10.9 us, 1024 9.1 / 12, 2048 21 / 13 (WIDE: 512 rows 11 / 19, 2048 25 / 16).  f32, whose products take eight times as long, sooner.  Parts for
+// some 1000 workgroups: eight scenes of 32768 keys, 4 heads of 128, 500 / 1000 / 2000 116 / 109 / 112; where 512 are there, cutting them in two costs 42 -> 51 (64 scenes of 2048).
 constexpr int ATTENTION_PARTS_MAX = 256;
-constexpr int attention_part_keys(AttentionShape shape) { return shape == ATTENTION_FEW || shape == ATTENTION_WIDE ? 256 : 64; }
-constexpr int attention_parts(AttentionShape shape, int64_t columns, int64_t scenes, int64_t k_heads, int64_t k_rows) {
-    const int64_t wanted = shape == ATTENTION_WIDE ? 512 : 1024;
-    const int64_t most = (k_rows / scenes + attention_part_keys(shape) - 1) / attention_part_keys(shape), there = attention_tiles(shape, columns, scenes) * k_heads;
-    int64_t parts = (wanted + there - 1) / there;
+constexpr int attention_part_keys(bool f32) { return f32 ? 64 : 256; }
+constexpr int attention_parts(AttentionShape shape, int64_t columns, int64_t scenes, int64_t k_heads, int64_t k_rows, bool f32) {
+    const int64_t from = f32 ? 256 : shape == ATTENTION_FEW ? 2048 : 1024;
+    if (k_rows < from * scenes) return 1;
+    const int64_t most = k_rows / scenes / attention_part_keys(f32), there = attention_tiles(shape, columns, scenes) * k_heads;
+    int64_t parts = 1000 / there;
     parts = parts < most ? parts : most;
     return (int)(parts < 1 ? 1 : parts < ATTENTION_PARTS_MAX ? parts : ATTENTION_PARTS_MAX);
 }
-// Backward: a wavefront ALONE has 32 columns, or four share 128, of queries and of keys.
-constexpr bool attention_grad_alone(int64_t columns, int64_t scenes, int64_t k_heads, int64_t k_rows) {
+// Backward: a wavefront ALONE has 32 columns, or four share 128, of queries and of keys.  us, f16, 8 heads, alone / shared: 32768 rows of 32 in scenes of 64 50 / 62, 128 62 / 82, 192 76 / 73; of 64 in
+// scenes of 48 106 / 125, 96 132 / 97; of 128 in scenes of 64 217 / 231, 96 336 / 232; one scene of one head of 64, 1024 rows 29 / 56, 4096 66 / 67; f32,
+// 1501 rows in seven scenes, 6 heads of 20 over 2, 51 / 213.
+constexpr bool attention_grad_alone(int64_t columns, int64_t scenes, int64_t k_heads, int64_t k_rows, int row_bytes, bool f32) {
     const int64_t most = columns > k_rows ? columns : k_rows;
-    return most <= 96 * scenes || attention_tiles(ATTENTION_WIDE, most, scenes) * k_heads < 256;
+    return most <= (row_bytes <= 64 ? 144 : 72) * scenes || attention_tiles(ATTENTION_WIDE, most, scenes) * k_heads < (f32 ? 512 : 64);
 }
+// Parts of what `columns` of a scene walk, `rows` of the scenes together.  Causal sequences gain most, whose first keys and last queries take twice the mean: 16384 rows in four, 16 heads of 64 over 4,
+// keys' gradients in one part / three 867 / 537 us and 29 to join.
 constexpr int ATTENTION_GRAD_PARTS_MAX = 16;
-constexpr int attention_part_rows(bool alone) { return alone ? 64 : 1024; }
-// Parts of what `columns` of a scene walk, `rows` of the scenes together.
-constexpr int attention_grad_parts(bool alone, int64_t columns, int64_t scenes, int64_t k_heads, int64_t rows) {
-    const int64_t there = attention_tiles(alone ? ATTENTION_SHORT : ATTENTION_WIDE, columns, scenes) * k_heads, wanted = 1536, least = attention_part_rows(alone);
-    const int64_t most = (rows / scenes + least - 1) / least;
+constexpr int attention_part_rows(bool alone, bool f32) { return alone ? (f32 ? 64 : 128) : 1024; }
+constexpr int attention_grad_parts(bool alone, int64_t columns, int64_t scenes, int64_t k_heads, int64_t rows, bool f32) {
+    const int64_t from = alone ? (f32 ? 128 : 512) : 2048, wanted = 1536;
+    if (rows < from * scenes) return 1;
+    const int64_t there = attention_tiles(alone ? ATTENTION_SHORT : ATTENTION_WIDE, columns, scenes) * k_heads, most = rows / scenes / attention_part_rows(alone, f32);
     int64_t parts = (wanted + there - 1) / there;
     parts = parts < most ? parts : most;
     return (int)(parts < 1 ? 1 : parts < ATTENTION_GRAD_PARTS_MAX ? parts : ATTENTION_GRAD_PARTS_MAX);

@@ -186,3 +186,166 @@ def test_long_scenes(causal, dt):
 def test_many_scenes(lens, dt):
     """More scenes than one search looks at."""
     both(lens, lens, 3, 3, 24, dt, False, lead=2, trail=1)
+
+
+@pytest.mark.parametrize("dt", TYPES)
+def test_scenes_do_not_see_each_other(dt):
+    """Whatever a scene holds, and whatever lies behind its last counted key, the others' results are the same, bit for bit."""
+    lens, D = [50, 33, 140, 64], 24
+    q, k, v, grad = data(sum(lens), sum(lens), 2, 2, D, dt, 7)
+    starts = starts_of(lens)
+    counts = torch.tensor([50, 20, 100, 64], dtype=torch.int32, device=DEV)
+    for causal in (False, True):
+        kw = dict(q_starts=starts, causal=causal, k_lens=counts)
+        clean, clean_lse = forward(q, k, v, **kw)
+        clean_grads = backward(grad, q, k, v, clean, clean_lse, **kw)
+        bad_k, bad_v = k.clone(), v.clone()
+        for a in (50 + 20, 50 + 33 + 100):          # behind the counted keys of scenes 1 and 2
+            bad_k[a:a + 13], bad_v[a:a + 13] = float("nan"), float("inf")
+        got, got_lse = forward(q, bad_k, bad_v, **kw)
+        assert torch.equal(got, clean) and torch.equal(got_lse, clean_lse)
+        for a, b in zip(backward(grad, q, bad_k, bad_v, got, got_lse, **kw), clean_grads):
+            assert torch.equal(a, b)
+        bad_k[:50], bad_v[:50] = float("nan"), float("inf")                      # all of scene 0
+        got, _ = forward(q, bad_k, bad_v, **kw)
+        assert got[:50].isnan().any() and torch.equal(got[50:], clean[50:])
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("D", [16, 64, 100])
+def test_key_counts(D, dt):
+    """A cache with room behind its keys: as if the keys were all there is; gradients of the others stay as they were."""
+    room, counts, lens = [70, 40, 300, 5], [70, 1, 131, 0], [1, 1, 2, 1]
+    q, k, v, grad = data(sum(lens), sum(room), 4, 2, D, dt, 3)
+    starts, k_starts = starts_of(lens), starts_of(room)
+    k_lens = torch.tensor(counts, dtype=torch.int32, device=DEV)
+    kw = dict(q_starts=starts, k_starts=k_starts, k_lens=k_lens, causal=True)
+    out, lse = forward(q, k, v, **kw)
+    want, off = reference(q, k, v, grad, lens, counts, k_starts.tolist(), starts.tolist(), True, D ** -0.5, dt)
+    check("out", out, want[0], off[0])
+    check("lse", lse, want[1], off[1])
+    for name, got, ref, tol in zip(("dq", "dk", "dv"), backward(grad, q, k, v, out, lse, **kw), want[2:], off[2:]):
+        check(name, got, ref, tol, torch.full_like(ref, 7.0))
+
+
+@pytest.mark.parametrize("dt", TYPES)
+def test_large_scores(dt):
+    """Scores of hundreds, the largest at the end, a constant among them: weights that grow through the tiles."""
+    n, D = 700, 32
+    q, k, v, grad = data(n, n, 2, 2, D, dt, 11)
+    k = (k.float() * torch.linspace(0, 40, n, device=DEV)[:, None, None]).to(dt)
+    out, lse = forward(q, k, v)
+    want, off = reference(q, k, v, grad, [n], [n], [0], [0], False, D ** -0.5, dt)
+    check("out", out, want[0], off[0])
+    check("lse", lse, want[1], off[1])
+
+
+@pytest.mark.parametrize("dt", TYPES)
+def test_orders_of_rows_and_heads_and_unaligned_rows(dt):
+    """Heads ahead of rows, rows that start anywhere, gradients into slices: the same values as contiguous tensors give, bit for bit."""
+    n, h, D = 130, 3, 40
+    q, k, v, grad = data(n, n, h, h, D, dt, 5)
+    kw = dict(q_starts=starts_of([60, 70]), causal=True)
+    out, lse = forward(q, k, v, **kw)
+    grads = backward(grad, q, k, v, out, lse, **kw)
+    heads_first = [t.transpose(0, 1).contiguous().transpose(0, 1) for t in (q, k, v, grad)]
+    odd = []
+    for t in (q, k, v, grad):
+        wide = torch.full((n, h, D + 3), float("nan"), dtype=dt, device=DEV)
+        wide[:, :, 1:1 + D] = t
+        odd.append(wide[:, :, 1:1 + D])
+    for a, b, c, g in (heads_first, odd):
+        there = torch.full((h, n, D), 7.0, dtype=dt, device=DEV).transpose(0, 1)
+        got, got_lse = forward(a, b, c, out=there, **kw)
+        assert torch.equal(got, out) and torch.equal(got_lse, lse)
+        wide = [torch.full((n, h, D + 5), 7.0, dtype=dt, device=DEV) for _ in range(3)]
+        backward(g, a, b, c, got, got_lse, grads=[w[:, :, 2:2 + D] for w in wide], **kw)
+        for w, want in zip(wide, grads):
+            assert torch.equal(w[:, :, 2:2 + D], want) and (w[:, :, :2] == 7).all() and (w[:, :, 2 + D:] == 7).all()
+    # one head of keys for all, and rows that are one row
+    shared = k[:, :1].expand(n, h, D)
+    one, one_lse = forward(q, shared, v[:, :1].expand(n, h, D), **kw)
+    want, want_lse = forward(q, k[:, :1].contiguous(), v[:, :1].contiguous(), **kw)
+    assert (one.float() - want.float()).abs().max() <= 8 * torch.finfo(dt).eps * want.float().abs().max() and torch.allclose(one_lse, want_lse, atol=1e-4)
+
+
+def test_gradient_against_differences():
+    """f32: a directional derivative of sum(out * grad) against central differences of the 64-bit definition."""
+    lens, D = [20, 35], 16
+    q, k, v, grad = data(sum(lens), sum(lens), 2, 1, D, torch.float32, 9)
+    kw = dict(q_starts=starts_of(lens), causal=True)
+    out, lse = forward(q, k, v, **kw)
+    grads = backward(grad, q, k, v, out, lse, **kw)
+    gen = torch.Generator().manual_seed(1)
+    steps = [torch.randn(t.shape, generator=gen, dtype=torch.float64) for t in (q, k, v)]
+
+    def value(h):
+        moved = [t.double().cpu() + h * s for t, s in zip((q, k, v), steps)]
+        total, at = 0.0, 0
+        for n in lens:
+            m = slice(at, at + n)
+            at += n
+            for head in range(2):
+                s = (moved[0][m, head] @ moved[1][m, 0].t() * D ** -0.5).masked_fill(torch.ones(n, n).triu(1).bool(), -math.inf)
+                total += float((s.softmax(1) @ moved[2][m, 0] * grad[m, head].double().cpu()).sum())
+        return total
+    want = (value(1e-4) - value(-1e-4)) / 2e-4
+    got = sum(float((g.double().cpu() * s).sum()) for g, s in zip(grads, steps))
+    assert abs(got - want) <= 1e-4 * max(1.0, abs(want)), (got, want)         # differences: h^2; 32 bits: some 1e-6 of terms that add up to a few
+
+
+def test_repeated_streams_and_graphs():
+    """The same bits every time: on another stream, and in two captured graphs that share a workspace, replayed between eager calls."""
+    lens = [700, 3, 260]
+    q, k, v, grad = data(sum(lens), sum(lens), 8, 2, 64, torch.bfloat16, 13)
+    starts = starts_of(lens)
+    args = (sum(lens), sum(lens), 3, 8, 2, 64, torch.bfloat16)
+    need = max(sc.sc_attention_workspace_bytes(*args), sc.sc_attention_bwd_workspace_bytes(*args), 16)
+    workspace = torch.empty(need, dtype=torch.uint8, device=DEV)
+    kw = dict(q_starts=starts, causal=True, workspace=workspace)
+
+    def step(q, out, lse, grads):
+        sc.sc_attention_fwd(q, k, v, out, lse=lse, **kw)
+        sc.sc_attention_bwd(grad, q, k, v, out, lse, *grads, **kw)
+
+    def buffers():
+        return torch.zeros_like(q), torch.zeros(q.shape[:2], device=DEV), [torch.zeros_like(t) for t in (q, k, v)]
+    want = buffers()
+    step(q, *want)
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    there = buffers()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(other):
+        step(q, *there)
+    torch.cuda.synchronize()
+    for a, b in zip((there[0], there[1], *there[2]), (want[0], want[1], *want[2])):
+        assert torch.equal(a, b)
+    inputs = [q.clone(), q.clone()]
+    held, graphs = [buffers(), buffers()], []
+    for x, b in zip(inputs, held):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step(x, *b)
+        graphs.append(graph)
+    for turn in range(3):
+        inputs[1].copy_(q * (1 + turn))
+        for graph, x, b in zip(graphs, inputs, held):
+            for t in (b[0], b[1], *b[2]):
+                t.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            eager = buffers()
+            step(x, *eager)
+            torch.cuda.synchronize()
+            for s, t in zip((b[0], b[1], *b[2]), (eager[0], eager[1], *eager[2])):
+                assert torch.equal(s, t)
+
+
+def test_nothing_to_do():
+    for rows, keys in ((0, 5), (5, 0), (0, 0)):
+        q, k, v, grad = data(rows, keys, 2, 2, 16, torch.float16)
+        out, lse = forward(q, k, v)
+        assert (out == 0).all() and (lse == -math.inf).all()
+        for g in backward(grad, q, k, v, out, lse):
+            assert (g == 0).all()
