@@ -479,7 +479,8 @@ int sc_qk_rope_bwd(const sc_heads* dq_out, const sc_heads* dk_out, const sc_head
  *   d_lse      [q_rows][q->heads] or NULL: what sc_attention_bwd needs
  *   D          1 to SC_ATTENTION_HEAD_MAX; scenes 1 to SC_SCENES_MAX; rows up to SC_N_MAX, q_rows (q->heads / k->heads) below 2^31 - 4096
  *   d_workspace  workspace_bytes >= sc_attention_workspace_bytes(...), which may be 0; 16-byte aligned
- * 16-bit weights are rounded to the rows' type ahead of their product with the values; sums are in 32 bits. */
+ * 16-bit weights are rounded to the rows' type ahead of their product with the values; sums are in 32 bits.  Scenes, and keys that do not count, never reach each other's results; inside a
+ * causal scene a v that is not finite may also reach queries up to 63 rows ahead of it (zero times infinity), backward any row that is not finite. */
 #define SC_ATTENTION_HEAD_MAX 256
 #define SC_ATTENTION_LD_MAX   16777216LL    /* 2^24 */
 #define SC_SCENES_MAX         SC_N_MAX

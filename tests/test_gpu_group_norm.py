@@ -131,3 +131,110 @@ def test_far_from_zero_and_without_gains(dt):
     run([800, 500], 32, 4, dt, "none", mean=100.0, spread=0.5)
     run([800], 32, 32, dt, "gelu", gains=False, use_starts=False)
     run([4000], 32, 2, dt, "silu", spread=1e-3, mean=0.0, eps=1e-3)
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("lens,C,groups", [([33], 256, 32), ([3000, 0, 2000], 64, 8)])
+def test_rectifier(lens, C, groups, dt):
+    """Forward as the others'; backward the slope of what the forward call stored: 0 or 1, so it is compared where the value ahead of it is no closer to zero than its error."""
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(2)
+    rows, starts = sum(lens), starts_of(lens)
+    x, grad = (torch.randn((rows, C), generator=gen, device=DEV).to(dt) for _ in range(2))
+    workspace = torch.empty(sc.sc_group_norm_workspace_bytes(rows, len(lens), C, groups), dtype=torch.uint8, device=DEV)
+    plain, out, stats = torch.empty_like(x), torch.empty_like(x), torch.empty((len(lens), groups, 2), device=DEV)
+    sc.sc_group_norm_fwd(x, plain, groups, starts, workspace=workspace)
+    sc.sc_group_norm_fwd(x, out, groups, starts, act="relu", stats=stats, workspace=workspace)
+    assert torch.equal(out, plain.clamp(min=0))
+    # with its slope put into the gradient by hand the layer without an activation gives the same
+    by_hand, got = torch.empty_like(x), torch.empty_like(x)
+    sc.sc_group_norm_bwd(grad, x, stats, got, groups, starts, act="relu", workspace=workspace)
+    sc.sc_group_norm_bwd(torch.where(plain > 0, grad, torch.zeros_like(grad)), x, stats, by_hand, groups, starts, workspace=workspace)
+    assert torch.equal(got, by_hand)
+
+
+@pytest.mark.parametrize("rows", [40, 5000])
+def test_gradients_one_by_one(rows):
+    """Each gradient alone is what it is among the others."""
+    x, grad = (torch.randn((rows, 48), device=DEV).bfloat16() for _ in range(2))
+    gain, bias, stats = torch.ones(48, device=DEV).bfloat16(), torch.zeros(48, device=DEV).bfloat16(), torch.empty((1, 6, 2), device=DEV)
+    workspace = torch.empty(sc.sc_group_norm_workspace_bytes(rows, 1, 48, 6), dtype=torch.uint8, device=DEV)
+    sc.sc_group_norm_fwd(x, torch.empty_like(x), 6, gain=gain, bias=bias, act="silu", stats=stats, workspace=workspace)
+    names = ("grad_x", "grad_gain", "grad_bias")
+    every = dict(grad_x=torch.empty_like(x), grad_gain=torch.empty_like(gain), grad_bias=torch.empty_like(bias))
+
+    def call(grad_x=None, **kw):
+        sc.sc_group_norm_bwd(grad, x, stats, grad_x, 6, gain=gain, bias=bias, act="silu", workspace=workspace, **kw)
+    call(**every)
+    for name in names:
+        one = {name: torch.empty_like(every[name])}
+        call(**one)
+        assert torch.equal(one[name], every[name])
+
+
+def test_repeated_streams_and_graphs():
+    """The same bits every time: on another stream, and in two captured graphs that share a workspace, replayed between eager calls."""
+    lens, C, groups = [3000, 17, 900], 64, 8
+    rows, starts = sum(lens), starts_of([3000, 17, 900])
+    x, grad = (torch.randn((rows, C), device=DEV).half() for _ in range(2))
+    gain, bias = torch.randn(C, device=DEV).half(), torch.randn(C, device=DEV).half()
+    workspace = torch.empty(sc.sc_group_norm_workspace_bytes(rows, 3, C, groups), dtype=torch.uint8, device=DEV)
+
+    def buffers():
+        return [torch.zeros_like(x), torch.zeros((3, groups, 2), device=DEV), torch.zeros_like(x), torch.zeros_like(gain), torch.zeros_like(bias)]
+
+    def step(x, b):
+        sc.sc_group_norm_fwd(x, b[0], groups, starts, gain, bias, "gelu", stats=b[1], workspace=workspace)
+        sc.sc_group_norm_bwd(grad, x, b[1], b[2], groups, starts, gain, bias, "gelu", b[3], b[4], workspace)
+    want, there = buffers(), buffers()
+    step(x, want)
+    torch.cuda.synchronize()
+    other = torch.cuda.Stream()
+    with torch.cuda.stream(other):
+        step(x, there)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, there))
+    inputs, held, graphs = [x.clone(), x.clone()], [buffers(), buffers()], []
+    for v, b in zip(inputs, held):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step(v, b)
+        graphs.append(graph)
+    for turn in range(3):
+        inputs[1].copy_(x * (1 + turn))
+        for graph, v, b in zip(graphs, inputs, held):
+            for t in b:
+                t.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            eager = buffers()
+            step(v, eager)
+            torch.cuda.synchronize()
+            assert all(torch.equal(s, t) for s, t in zip(b, eager))
+
+
+def test_scenes_do_not_see_each_other():
+    lens = [200, 55, 3000]
+    starts = starts_of(lens)
+    for lens in ([200, 55, 3000], [20, 5, 30]):
+        starts = starts_of(lens)
+        x = torch.randn((sum(lens), 24), device=DEV)
+        workspace = torch.empty(sc.sc_group_norm_workspace_bytes(len(x), 3, 24, 3), dtype=torch.uint8, device=DEV)
+        clean, got, bad = torch.empty_like(x), torch.empty_like(x), x.clone()
+        sc.sc_group_norm_fwd(x, clean, 3, starts, act="silu", workspace=workspace)
+        bad[lens[0] + 1, 0], bad[lens[0] + 2, 9] = float("nan"), float("inf")
+        sc.sc_group_norm_fwd(bad, got, 3, starts, act="silu", workspace=workspace)
+        m = slice(lens[0], lens[0] + lens[1])
+        assert torch.equal(got[:m.start], clean[:m.start]) and torch.equal(got[m.stop:], clean[m.stop:])
+        assert got[m, :16].isnan().all() and torch.equal(got[m, 16:], clean[m, 16:])
+
+
+def test_no_rows():
+    x = torch.empty((0, 16), device=DEV)
+    stats, gain = torch.full((2, 4, 2), 7.0, device=DEV), torch.full((16,), 7.0, device=DEV)
+    workspace = torch.empty(sc.sc_group_norm_workspace_bytes(0, 2, 16, 4), dtype=torch.uint8, device=DEV)
+    starts = torch.zeros(3, dtype=torch.int32, device=DEV)
+    sc.sc_group_norm_fwd(x, x, 4, starts, stats=stats, eps=0.25, workspace=workspace)
+    assert (stats[..., 0] == 0).all() and (stats[..., 1] == 2).all()
+    sc.sc_group_norm_bwd(x, x, stats, x, 4, starts, grad_gain=gain, grad_bias=gain.clone(), workspace=workspace)
+    assert (gain == 0).all()
