@@ -134,6 +134,7 @@ __device__ inline void sum_of_threads(double& a, double& b) {
         a += __shfl_xor(a, d);
         b += __shfl_xor(b, d);
     }
+    if (THREADS == WAVE) return;
     if ((threadIdx.x & 63) == 0) {
         shared[0][threadIdx.x >> 6] = a;
         shared[1][threadIdx.x >> 6] = b;
@@ -153,10 +154,16 @@ __device__ inline void scene_units_of(const Norm& p, int scene, int64_t& first_u
     first_unit = first / p.per + scene;
 }
 
+// A scene and a group of THREADS threads: one workgroup's, or one wavefront's of the four in a workgroup where there are many of them.
+template <int THREADS>
+__device__ inline int pair_of_threads() { return THREADS == WAVE ? (int)(blockIdx.x * 4 + (threadIdx.x >> 6)) : (int)blockIdx.x; }
 // Mean and deviation of a scene's group from its units' sums.
-__global__ void __launch_bounds__(JOIN_THREADS)
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS == WAVE ? 256 : THREADS)
 k_norm_join(const Norm p) {
-    const int scene = blockIdx.x / (unsigned)p.groups, group = blockIdx.x - scene * p.groups;
+    const int pair = pair_of_threads<THREADS>(), tid = (int)threadIdx.x % THREADS;
+    if (pair >= p.scenes * p.groups) return;
+    const int scene = pair / p.groups, group = pair - scene * p.groups;
     int64_t unit = 0;
     int rows = 0;
     scene_units_of(p, scene, unit, rows);
@@ -166,17 +173,17 @@ k_norm_join(const Norm p) {
     double sum = 0.0, square = 0.0;
     const int64_t items = (int64_t)units * p.channels;
 #pragma unroll 4
-    for (int64_t i = threadIdx.x; i < items; i += JOIN_THREADS) {
-        const int u = (int)(i / p.channels), c = (int)(i - (int64_t)u * p.channels);
+    for (int64_t i = tid; i < items; i += THREADS) {
+        const int u = (int)((uint32_t)i / (uint32_t)p.channels), c = (int)(i - (int64_t)u * p.channels);
         const float2 s = sums[(int64_t)u * p.C + c];
         const double n = rows - u * p.per < p.per ? rows - u * p.per : p.per, d = (double)s.x - pivot;
         sum += n * d;
         square += s.y + n * d * d;
     }
-    sum_of_threads<JOIN_THREADS>(sum, square);
-    if (threadIdx.x != 0) return;
+    sum_of_threads<THREADS>(sum, square);
+    if (tid != 0) return;
     const double n = (double)rows * p.channels, mean = rows > 0 ? sum / n : 0.0, var = rows > 0 ? square / n - mean * mean : 0.0;
-    p.stats[blockIdx.x] = make_float2((float)(pivot + mean), (float)(1.0 / sqrt((var > 0.0 ? var : var != var ? var : 0.0) + (double)p.eps)));
+    p.stats[pair] = make_float2((float)(pivot + mean), (float)(1.0 / sqrt((var > 0.0 ? var : var != var ? var : 0.0) + (double)p.eps)));
 }
 
 // mean, 1 / deviation, gain and bias of a thread's channels
@@ -223,8 +230,8 @@ k_norm(const Norm p) {
 }
 
 // Few rows: a workgroup has a scene's group to itself, and its rows stay in the caches between the passes.
-template <int DT>
-__global__ void __launch_bounds__(NORM_THREADS)
+template <int DT, int THREADS>
+__global__ void __launch_bounds__(THREADS)
 k_norm_few(const Norm p) {
     const int scene = blockIdx.x / (unsigned)p.groups, group = blockIdx.x - scene * p.groups;
     int64_t first = 0;
@@ -235,19 +242,19 @@ k_norm_few(const Norm p) {
     const int c0 = group * p.channels, items = rows * p.channels;
     const float pivot = rows > 0 ? load_elem<DT>(x, c0) : 0.f;
     double sum = 0.0, square = 0.0;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < items; i += NORM_THREADS) {
+#pragma unroll 8
+    for (int i = threadIdx.x; i < items; i += THREADS) {
         const int r = i / p.channels;
         const double d = (double)load_elem<DT>(x + r * p.ldx, c0 + i - r * p.channels) - pivot;
         sum += d;
         square += d * d;
     }
-    sum_of_threads<NORM_THREADS>(sum, square);
+    sum_of_threads<THREADS>(sum, square);
     const double mean = rows > 0 ? sum / items : 0.0, var = rows > 0 ? square / items - mean * mean : 0.0;
     const float2 s = make_float2((float)(pivot + mean), (float)(1.0 / sqrt((var > 0.0 ? var : var != var ? var : 0.0) + (double)p.eps)));
     if (p.stats != nullptr && threadIdx.x == 0) p.stats[blockIdx.x] = s;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < items; i += NORM_THREADS) {
+#pragma unroll 8
+    for (int i = threadIdx.x; i < items; i += THREADS) {
         const int r = i / p.channels, c = c0 + i - r * p.channels;
         const float gain = p.gain != nullptr ? load_elem<DT>(p.gain, c) : 1.f, bias = p.bias != nullptr ? load_elem<DT>(p.bias, c) : 0.f;
         const float v = fmaf(load_elem<DT>(x + r * p.ldx, c) - s.x, s.y * gain, bias);
@@ -301,39 +308,16 @@ k_norm_grad_sums(const Norm p) {
     }
     join_threads(sum, along, width, [&](int c, float a, float b) { sums[c] = make_float2(a, b); });
 }
-// The means of a scene's group, and in the workgroups behind those the gradients of 16 channels' gain and bias.
-template <int DT>
-__global__ void __launch_bounds__(JOIN_THREADS)
-k_norm_grad_join(const Norm p) {
-    const int pairs = p.scenes * p.groups;
-    if ((int)blockIdx.x < pairs) {
-        const int scene = blockIdx.x / (unsigned)p.groups, group = blockIdx.x - scene * p.groups;
-        int64_t unit = 0;
-        int rows = 0;
-        scene_units_of(p, scene, unit, rows);
-        const int units = (rows + p.per - 1) / p.per;
-        const float2* const sums = p.sums + unit * p.C + group * p.channels;
-        double sum = 0.0, along = 0.0;
-        const int64_t items = (int64_t)units * p.channels;
-#pragma unroll 4
-        for (int64_t i = threadIdx.x; i < items; i += JOIN_THREADS) {
-            const int u = (int)(i / p.channels), c = (int)(i - (int64_t)u * p.channels);
-            const float2 s = sums[(int64_t)u * p.C + c];
-            const double gain = p.gain != nullptr ? load_elem<DT>(p.gain, group * p.channels + c) : 1.f;
-            sum += gain * s.x;
-            along += gain * s.y;
-        }
-        sum_of_threads<JOIN_THREADS>(sum, along);
-        const double n = (double)rows * p.channels;
-        if (threadIdx.x == 0) p.means[blockIdx.x] = rows > 0 ? make_float2((float)(sum / n), (float)(along / n)) : make_float2(0.f, 0.f);
-        return;
-    }
-    __shared__ double shared[2][64][16];
-    const int c = ((int)blockIdx.x - pairs) * 16 + (threadIdx.x & 15), which = threadIdx.x >> 4;
+// The gradients of 16 channels' gain and bias from the sums of all units, by a workgroup.
+template <int DT, int THREADS>
+__device__ inline void join_gains(const Norm& p, int first) {
+    constexpr int SHARES = THREADS / 16;
+    __shared__ double shared[2][SHARES][16];
+    const int c = first + (threadIdx.x & 15), which = threadIdx.x >> 4;
     double sum = 0.0, along = 0.0;
     if (c < p.C) {
 #pragma unroll 8
-        for (int64_t u = which; u < p.units; u += 64) {
+        for (int64_t u = which; u < p.units; u += SHARES) {
             const float2 s = p.sums[u * p.C + c];
             sum += s.x;
             along += s.y;
@@ -345,12 +329,42 @@ k_norm_grad_join(const Norm p) {
     if (which != 0 || c >= p.C) return;
     sum = along = 0.0;
 #pragma unroll 8
-    for (int w = 0; w < 64; ++w) {
+    for (int w = 0; w < SHARES; ++w) {
         sum += shared[0][w][threadIdx.x];
         along += shared[1][w][threadIdx.x];
     }
     if (p.dbias != nullptr) store_elem<DT>(p.dbias, c, (float)sum);
     if (p.dgain != nullptr) store_elem<DT>(p.dgain, c, (float)along);
+}
+// The means of a scene's group, and in the workgroups behind `pair_blocks` the gradients of the gains.
+template <int DT, int THREADS>
+__global__ void __launch_bounds__(THREADS == WAVE ? 256 : THREADS)
+k_norm_grad_join(const Norm p, int pair_blocks) {
+    if ((int)blockIdx.x >= pair_blocks) {
+        join_gains<DT, THREADS == WAVE ? 256 : THREADS>(p, ((int)blockIdx.x - pair_blocks) * 16);
+        return;
+    }
+    const int pair = pair_of_threads<THREADS>(), tid = (int)threadIdx.x % THREADS;
+    if (pair >= p.scenes * p.groups) return;
+    const int scene = pair / p.groups, group = pair - scene * p.groups;
+    int64_t unit = 0;
+    int rows = 0;
+    scene_units_of(p, scene, unit, rows);
+    const int units = (rows + p.per - 1) / p.per;
+    const float2* const sums = p.sums + unit * p.C + group * p.channels;
+    double sum = 0.0, along = 0.0;
+    const int64_t items = (int64_t)units * p.channels;
+#pragma unroll 4
+    for (int64_t i = tid; i < items; i += THREADS) {
+        const int u = (int)((uint32_t)i / (uint32_t)p.channels), c = (int)(i - (int64_t)u * p.channels);
+        const float2 s = sums[(int64_t)u * p.C + c];
+        const double gain = p.gain != nullptr ? load_elem<DT>(p.gain, group * p.channels + c) : 1.f;
+        sum += gain * s.x;
+        along += gain * s.y;
+    }
+    sum_of_threads<THREADS>(sum, along);
+    const double n = (double)rows * p.channels;
+    if (tid == 0) p.means[pair] = rows > 0 ? make_float2((float)(sum / n), (float)(along / n)) : make_float2(0.f, 0.f);
 }
 template <int DT>
 __global__ void __launch_bounds__(NORM_THREADS)
@@ -396,23 +410,29 @@ int slices_of(int C) { return (C + SLICE - 1) / SLICE; }
 
 template <int DT>
 int launch_norm(const Norm& p, bool few, hipStream_t s) {
-    const dim3 pairs((unsigned)(p.scenes * p.groups));
+    const int pairs = p.scenes * p.groups;
     if (few) {
-        SC_LAUNCH(KID_NORM, k_norm_few<DT>, pairs, dim3(NORM_THREADS), 0, s, p);
+        if (p.rows * p.channels <= 1024) SC_LAUNCH(KID_NORM, (k_norm_few<DT, 256>), dim3((unsigned)pairs), dim3(256), 0, s, p);
+        else SC_LAUNCH(KID_NORM, (k_norm_few<DT, 1024>), dim3((unsigned)pairs), dim3(1024), 0, s, p);
         return SC_OK;
     }
     const dim3 grid((unsigned)p.units, (unsigned)slices_of(p.C));
     SC_LAUNCH(KID_NORM_SUMS, k_norm_sums<DT>, grid, dim3(NORM_THREADS), 0, s, p);
-    SC_LAUNCH(KID_NORM_JOIN, k_norm_join, pairs, dim3(JOIN_THREADS), 0, s, p);
+    if (norm_join_by_wavefronts(pairs)) SC_LAUNCH(KID_NORM_JOIN, k_norm_join<WAVE>, dim3((unsigned)(pairs + 3) / 4), dim3(256), 0, s, p);
+    else SC_LAUNCH(KID_NORM_JOIN, k_norm_join<JOIN_THREADS>, dim3((unsigned)pairs), dim3(JOIN_THREADS), 0, s, p);
     SC_LAUNCH(KID_NORM, k_norm<DT>, grid, dim3(NORM_THREADS), 0, s, p);
     return SC_OK;
 }
 template <int DT>
 int launch_norm_grad(const Norm& p, hipStream_t s) {
+    const int pairs = p.scenes * p.groups;
     const dim3 grid((unsigned)p.units, (unsigned)slices_of(p.C));
-    const int gains = p.dgain != nullptr || p.dbias != nullptr ? (p.C + 15) / 16 : 0;
     SC_LAUNCH(KID_NORM_SUMS, k_norm_grad_sums<DT>, grid, dim3(NORM_THREADS), 0, s, p);
-    SC_LAUNCH(KID_NORM_JOIN, k_norm_grad_join<DT>, dim3((unsigned)(p.scenes * p.groups + gains)), dim3(JOIN_THREADS), 0, s, p);
+    const int gains = p.dgain != nullptr || p.dbias != nullptr ? (p.C + 15) / 16 : 0, by_wavefronts = (pairs + 3) / 4;
+    if (norm_join_by_wavefronts(pairs))
+        SC_LAUNCH(KID_NORM_JOIN, (k_norm_grad_join<DT, WAVE>), dim3((unsigned)(by_wavefronts + gains)), dim3(256), 0, s, p, by_wavefronts);
+    else
+        SC_LAUNCH(KID_NORM_JOIN, (k_norm_grad_join<DT, JOIN_THREADS>), dim3((unsigned)(pairs + gains)), dim3(JOIN_THREADS), 0, s, p, pairs);
     if (p.y != nullptr) SC_LAUNCH(KID_NORM_GRAD, k_norm_grad<DT>, grid, dim3(NORM_THREADS), 0, s, p);
     return SC_OK;
 }

@@ -317,6 +317,8 @@ constexpr int attention_parts(AttentionShape shape, int64_t columns, int64_t sce
     parts = parts < most ? parts : most;
     return (int)(parts < 1 ? 1 : parts < ATTENTION_PARTS_MAX ? parts : ATTENTION_PARTS_MAX);
 }
+// Joined by a thread for four channels, or by a workgroup for each row's head: 10449 heads of 32 in 12 parts JOIN_ROWS / JOIN_HEADS us, 128 of 128 in 32 36 / 7.
+constexpr bool join_by_rows(int parts, int64_t items) { return parts <= 8 || items >= 32768; }
 // Backward: a wavefront ALONE has 32 columns, or four share 128, of queries and of keys.  us, f16, 8 heads, alone / shared: 32768 rows of 32 in scenes of 64 50 / 62, 128 62 / 82, 192 76 / 73; of 64 in
 // scenes of 48 106 / 125, 96 132 / 97; of 128 in scenes of 64 217 / 231, 96 336 / 232; one scene of one head of 64, 1024 rows 29 / 56, 4096 66 / 67; f32,
 // 1501 rows in seven scenes, 6 heads of 20 over 2, 51 / 213.
@@ -346,6 +348,8 @@ constexpr int norm_rows(int64_t rows, int C) {
     while ((per * chunks < 2048 && per < 1024 && rows / per > 1024) || rows / per > 4096) per *= 2;
     return (int)per;
 }
+// Sums joined by a wavefront for each scene's group, or by a workgroup of sixteen.
+constexpr bool norm_join_by_wavefronts(int64_t pairs) { return pairs >= 1024; }
 // One launch, a workgroup for a scene's group, whose rows may all be of one scene.
 constexpr bool norm_few(int64_t rows, int channels) { return rows * channels <= 8192; }
 
