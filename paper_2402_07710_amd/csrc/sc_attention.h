@@ -8,6 +8,16 @@
 // two buffers deep, 16 bytes a lane straight from global memory.  S comes out transposed, rows of the walked side down a lane's registers, its column along the lanes:
 // the maximum and the sum of a column are then a lane's own (of its quarter of the rows), and four registers are four consecutive rows, which is how the
 // transposing LDS read hands out the second product's first operand.  So weights go from one product to the next without leaving their registers.
+//
+// What bounds it: the matrix cores for long scenes, next to the vector unit (an exponential, two multiplications, an addition and a share of a comparison and of a conversion for every
+// score); vector instructions ahead of and behind the products for scenes of tens; memory for single rows over long caches; a few trips to memory, one after the other, for little of everything.
+// us of the call, a copy on this card 5.1 TB/s, the library's largest product 1120 TFLOP/s in 16 bits and 152 in 32:
+//     one row, 77 keys, 8 heads of 32, bf16                     4.9
+//     8 rows, 262144 keys, 16 heads of 128 over 4, f16          111    537 MB, 4.8 TB/s with the parts' join of 7; the walk alone 5.2
+//     53373 rows in 1112 scenes, 8 heads of 16, f16              31    55 MB; 11 million vector instructions, 18 us of every SIMD's time
+//     16384 rows in 3 causal scenes, 16 heads of 128 over 4, bf16  427    915 TFLOP/s
+//     backward 110545 rows in 2303 scenes, 8 heads of 16, f16   156    230 MB; 53 million vector instructions, 86 us
+//     backward 16384 rows in 4 causal scenes, 16 heads of 64 over 4, bf16  910    590 TFLOP/s of the five products that it cannot do without, 825 of the seven that it does
 #pragma once
 
 #include "sc_product.h"
@@ -267,6 +277,15 @@ __device__ inline float over_quarters(float v, F&& join) {
 }
 __device__ inline float over_quarters_max(float v) {
     return over_quarters(v, [](float a, float b) { return fmaxf(a, b); });
+}
+template <int CONTROL>
+__device__ inline float from_lane(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CONTROL, 0xf, 0xf, true)); }
+__device__ inline float over_lanes_max(float v) {                 // the other of two, the other two of four, mirrored in eight and in sixteen; the quarters
+    v = fmaxf(v, from_lane<0xb1>(v));
+    v = fmaxf(v, from_lane<0x4e>(v));
+    v = fmaxf(v, from_lane<0x141>(v));
+    v = fmaxf(v, from_lane<0x140>(v));
+    return over_quarters_max(v);
 }
 __device__ inline float over_quarters_sum(float v) {
     return over_quarters(v, [](float a, float b) { return a + b; });
@@ -580,7 +599,7 @@ k_attention(const Attention p) {
 
 // ---- backward -------------------------------------------------------------------------------------------
 // Two kernels, so that every gradient is summed by one wavefront in one order: queries' columns walk the keys, keys' columns walk the queries.  The weights are made
-// again in both from lse: seven products where five would do, and no atomics, no sums in memory.
+// again in both from lse: seven products where five would do, and no atomics, no sums in memory.  (Gradients of queries added up over blocks of 128 keys would be 56 parts of a scene of 7069.)
 // The walked rows go through the registers 32 at a time.
 template <int DT, int DPAD, int SHARE>
 constexpr int SUB = walked_tile<DT, DPAD, SHARE>() < 32 ? 16 : 32;
@@ -588,6 +607,27 @@ constexpr int SUB = walked_tile<DT, DPAD, SHARE>() < 32 ? 16 : 32;
 template <int DT, int DPAD, int NB, bool WHOLE>
 constexpr int grad_waves(int rows, int results) {                 // wavefronts on a SIMD that the registers leave room for
     return NB * (rows * HeadShape<DT, DPAD>::KS * 4 + results * HeadShape<DT, DPAD>::CB * 4) > (DT == SC_F32 || !WHOLE ? 120 : 180) ? 1 : 2;
+}
+
+// Gradients of scores are a weight, some 1 / keys, times what may be small itself: in f16, whose least normal number is 2^-14, most of a long scene's would be rounded off.
+// A wavefront therefore holds them times a power of two, `factor`, that its first ones set, and sets it anew, with what is summed so far, when some come near f16's end.  The weights
+// themselves are at most 1 and are lifted by 2^14 in the keys' kernel.
+template <int DT>
+constexpr float WEIGHT_LIFT = DT == SC_F16 ? 14.f : 0.f;
+struct GradScale {
+    float factor = 1.f;
+    bool set = false;
+};
+// What sums and the gradients at hand, of which `most` is the lane's largest, are to be multiplied by: 1 almost always.
+__device__ __forceinline__ float rescale(GradScale& scale, float most) {
+    if (scale.set ? __all(most <= 32768.f) : !__any(most > 0.f)) return 1.f;
+    most = over_lanes_max(most);
+    scale.set = true;
+    if (!(most < __builtin_inff())) return 1.f;
+    const float by = ldexpf(1.f, 8 - __builtin_amdgcn_frexp_expf(most)), factor = scale.factor * by;
+    if (!(factor > 1e-30f && factor < 1e30f)) return 1.f;
+    scale.factor = factor;
+    return by;
 }
 
 template <int DT, int DPAD, int NB, int SHARE, bool WHOLE>
@@ -648,7 +688,7 @@ k_attention_dq(const Attention p) {
         }
         delta[n] = over_quarters_sum(sum);
         if (there[n] && g == 0 && part == 0) {                    // for the keys' kernel, a head's rows together
-            p.against[(int64_t)head_of[n] * p.q_rows + row] = against[n];
+            p.against[(int64_t)head_of[n] * p.q_rows + row] = against[n] - WEIGHT_LIFT<DT>;
             p.delta[(int64_t)head_of[n] * p.q_rows + row] = delta[n];
         }
 #pragma unroll
@@ -677,6 +717,7 @@ k_attention_dq(const Attention p) {
         for (int b = 0; b < 4; ++b) keys.clear(lds0 + b * TILE_BYTES);
     }
     uint32_t buffer = 0;
+    GradScale scale;
     if (from < to) bring(from, 0);
     for (int t = from; t < to; ++t) {
         loads_done();
@@ -715,7 +756,8 @@ k_attention_dq(const Attention p) {
                     for (int b = 0; b < SUB_BLOCKS; ++b)
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
-                            s[n][b][r] = __builtin_amdgcn_exp2f(fmaf(s[n][b][r], p.scale_log2, -against[n0 + n])) * (dp[n][b][r] - delta[n0 + n]);
+                            s[n][b][r] = __builtin_amdgcn_exp2f(fmaf(s[n][b][r], p.scale_log2, -against[n0 + n])) *
+                                         (DT == SC_F16 ? fmaf(dp[n][b][r], scale.factor, -delta[n0 + n] * scale.factor) : dp[n][b][r] - delta[n0 + n]);
                 if (key0 + SUB > first_limit) {
 #pragma unroll
                     for (int n = 0; n < TOGETHER; ++n)
@@ -723,6 +765,29 @@ k_attention_dq(const Attention p) {
                         for (int b = 0; b < SUB_BLOCKS; ++b)
 #pragma unroll
                             for (int r = 0; r < 4; ++r) s[n][b][r] = key0 + 16 * b + 4 * g + r < limit[n0 + n] ? s[n][b][r] : 0.f;
+                }
+                if constexpr (DT == SC_F16) {
+                    float most = 0.f;
+#pragma unroll
+                    for (int n = 0; n < TOGETHER; ++n)
+#pragma unroll
+                        for (int b = 0; b < SUB_BLOCKS; ++b)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) most = fmaxf(most, fabsf(s[n][b][r]));
+                    const bool summed = scale.set;                // or nothing but zeros so far
+                    const float by = rescale(scale, most);
+                    if (by != 1.f) {
+#pragma unroll
+                        for (int n = 0; n < TOGETHER; ++n)
+#pragma unroll
+                            for (int b = 0; b < SUB_BLOCKS; ++b) s[n][b] *= by;
+                        if (summed) {
+#pragma unroll
+                            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                                for (int c = 0; c < H::CB; ++c) dq[n][c] *= by;
+                        }
+                    }
                 }
 #pragma unroll
                 for (int u = 0; u < SUB / H::STEP; ++u) {
@@ -748,6 +813,7 @@ k_attention_dq(const Attention p) {
         char* const to_row = row_at(p.dq.data + scene.q0 * p.dq.row + head_of[n] * p.dq.head, row_of[n], p.dq.row);
 #pragma unroll
         for (int c = 0; c < H::CB; ++c) {
+            if constexpr (DT == SC_F16) dq[n][c] *= 1.f / scale.factor;
             if (p.parts > 1) {
                 store4<SC_F32, WHOLE>((char*)to_part, 16 * c + 4 * g, p.D, dq[n][c]);
                 continue;
@@ -835,6 +901,7 @@ k_attention_dkv(const Attention p) {
     }
     if (from < to) bring(from, 0);
     int which = 0;
+    GradScale scale;
     for (int n = from; n < to; ++n, which ^= 1) {
         loads_done();
         queries.settle(lds0 + which * (2 * TILE_BYTES));
@@ -869,6 +936,7 @@ k_attention_dkv(const Attention p) {
                             dp[m][b] = multiply<DT>(d, v[m0 + m][c], dp[m][b]);
                         }
                     }
+                const float lowered = DT == SC_F16 ? scale.factor * 0x1p-14f : 1.f;         // the weights' lift taken back
 #pragma unroll
                 for (int b = 0; b < SUB_BLOCKS; ++b) {
                     const uint32_t sums = lds0 + SUMS + which * 512 + (h * SUB + 16 * b + 4 * g) * 4;
@@ -878,7 +946,7 @@ k_attention_dkv(const Attention p) {
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
                             s[m][b][r] = __builtin_amdgcn_exp2f(fmaf(s[m][b][r], p.scale_log2, -against[r]));
-                            dp[m][b][r] = s[m][b][r] * (dp[m][b][r] - delta[r]);
+                            dp[m][b][r] = s[m][b][r] * (DT == SC_F16 ? fmaf(dp[m][b][r], lowered, -delta[r] * lowered) : dp[m][b][r] - delta[r]);
                         }
                 }
                 if (masked) {
@@ -892,6 +960,29 @@ k_attention_dkv(const Attention p) {
                                 s[m][b][r] = seen ? s[m][b][r] : 0.f;
                                 dp[m][b][r] = seen ? dp[m][b][r] : 0.f;
                             }
+                }
+                if constexpr (DT == SC_F16) {
+                    float most = 0.f;
+#pragma unroll
+                    for (int m = 0; m < TOGETHER; ++m)
+#pragma unroll
+                        for (int b = 0; b < SUB_BLOCKS; ++b)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) most = fmaxf(most, fabsf(dp[m][b][r]));
+                    const bool summed = scale.set;                // or nothing but zeros so far
+                    const float by = rescale(scale, most);
+                    if (by != 1.f) {
+#pragma unroll
+                        for (int m = 0; m < TOGETHER; ++m)
+#pragma unroll
+                            for (int b = 0; b < SUB_BLOCKS; ++b) dp[m][b] *= by;
+                        if (summed) {
+#pragma unroll
+                            for (int m = 0; m < NB; ++m)
+#pragma unroll
+                                for (int c = 0; c < H::CB; ++c) dk[m][c] *= by;
+                        }
+                    }
                 }
 #pragma unroll
                 for (int u = 0; u < SUB / H::STEP; ++u) {
@@ -923,6 +1014,10 @@ k_attention_dkv(const Attention p) {
         char* const to_v = row_at(p.dv.data + k0 * p.dv.row + head_k * p.dv.head, c, p.dv.row);
 #pragma unroll
         for (int b = 0; b < H::CB; ++b) {
+            if constexpr (DT == SC_F16) {
+                dk[n][b] *= 1.f / scale.factor;
+                dv[n][b] *= 0x1p-14f;
+            }
             if (p.k_parts > 1) {
                 store4<SC_F32, WHOLE>((char*)(p.part_dk + at_part), 16 * b + 4 * g, p.D, dk[n][b]);
                 store4<SC_F32, WHOLE>((char*)(p.part_dv + at_part), 16 * b + 4 * g, p.D, dv[n][b]);
@@ -944,18 +1039,19 @@ __device__ __forceinline__ f32x4 partial4(const float* p, int there) {
         if (j < there) v[j] = p[j];
     return v;
 }
-// Parts of a gradient added up, in their order: a workgroup has 16 rows of a scene.
+// Parts of a gradient added up, in their order: a workgroup has JOIN_ROWS rows of a scene.
+constexpr int JOIN_ROWS = 4, JOIN_ROWS_LOG2 = 2;
 template <int DT>
 __global__ void __launch_bounds__(256)
 k_attention_grad_join(const int32_t* __restrict__ starts, const int32_t* __restrict__ lens, int scenes, int64_t rows, int heads, int D, int parts,
                       const float* __restrict__ a, HeadRows to_a, float scale_a, const float* __restrict__ b, HeadRows to_b) {
     int64_t first = 0;
     int count = 0, scene;
-    const int tile = __builtin_amdgcn_readfirstlane(find_scene(starts, scenes, rows, 1, 4, (int64_t)blockIdx.y * gridDim.x + blockIdx.x, (rows >> 4) + scenes, first, count, scene).tile);
+    const int tile = __builtin_amdgcn_readfirstlane(find_scene(starts, scenes, rows, 1, JOIN_ROWS_LOG2, (int64_t)blockIdx.y * gridDim.x + blockIdx.x, scene_units(rows, scenes, JOIN_ROWS), first, count, scene).tile);
     if (tile < 0) return;
     if (lens != nullptr) scene_rows(starts, lens, rows, scene, first, count);
-    const int here = count - tile * 16 < 16 ? count - tile * 16 : 16, fours = (D + 3) / 4, row_items = heads * fours;
-    const int64_t row0 = first + tile * 16, apart = rows * heads * D;
+    const int here = count - tile * JOIN_ROWS < JOIN_ROWS ? count - tile * JOIN_ROWS : JOIN_ROWS, fours = (D + 3) / 4, row_items = heads * fours;
+    const int64_t row0 = first + tile * JOIN_ROWS, apart = rows * heads * D;
     for (int i = threadIdx.x; i < here * row_items; i += 256) {
         const int r = i / row_items, head = (i - r * row_items) / fours, channel = (i - r * row_items - head * fours) * 4;
         const int64_t at = ((row0 + r) * heads + head) * D + channel;
@@ -1151,10 +1247,10 @@ int launch_attention_grad(const Attention& p, bool alone, hipStream_t s) {
     if (rc != SC_OK) return rc;
     const int q_heads = p.k_heads * p.per;
     if (p.parts > 1 && p.q_rows > 0)
-        SC_LAUNCH(KID_ATTENTION_JOIN, k_attention_grad_join<DT>, grid_of(scene_units(p.q_rows, p.scenes, 16)), dim3(256), 0, s, p.q_starts, (const int32_t*)nullptr,
+        SC_LAUNCH(KID_ATTENTION_JOIN, k_attention_grad_join<DT>, grid_of(scene_units(p.q_rows, p.scenes, JOIN_ROWS)), dim3(256), 0, s, p.q_starts, (const int32_t*)nullptr,
                   p.scenes, p.q_rows, q_heads, p.D, p.parts, p.part_out, p.dq, p.scale, (const float*)nullptr, p.dq);
     if (p.k_parts > 1 && p.k_rows > 0)
-        SC_LAUNCH(KID_ATTENTION_JOIN, k_attention_grad_join<DT>, grid_of(scene_units(p.k_rows, p.scenes, 16)), dim3(256), 0, s, p.k_starts, p.k_lens, p.scenes,
+        SC_LAUNCH(KID_ATTENTION_JOIN, k_attention_grad_join<DT>, grid_of(scene_units(p.k_rows, p.scenes, JOIN_ROWS)), dim3(256), 0, s, p.k_starts, p.k_lens, p.scenes,
                   p.k_rows, p.k_heads, p.D, p.k_parts, p.part_dk, p.dk, p.scale, p.part_dv, p.dv);
     return SC_OK;
 }

@@ -349,3 +349,34 @@ def test_nothing_to_do():
         assert (out == 0).all() and (lse == -math.inf).all()
         for g in backward(grad, q, k, v, out, lse):
             assert (g == 0).all()
+
+
+@pytest.mark.parametrize("which", ["dq", "dk"])
+@pytest.mark.parametrize("lens", [[4000], [30] * 40])
+def test_small_gradients_in_f16(lens, which):
+    """Gradients of scores far below f16's normal numbers (2^-14) whose sums are not: some 2^-20 here.  Of a random sum each of whose terms is rounded by half a step at
+    most, and which is rounded once, the error is within 2 half steps of its size in the mean square; a term that was rounded as a number of 2^-20, in steps of 2^-24, would be off by a 64th."""
+    n, D = sum(lens), 32
+    q, k, v, grad = data(n, n, 2, 2, D, torch.float16, 17)
+    wide, narrow = (k, q) if which == "dq" else (q, k)
+    wide.mul_(32), narrow.mul_(1 / 32)
+    grad.mul_(2.0 ** -6 if len(lens) == 1 else 2.0 ** -11)
+    grad[0] *= 16                                   # a row of larger ones among them
+    starts = starts_of(lens)
+    kw = dict(q_starts=starts)
+    out, lse = forward(q, k, v, **kw)
+    got = backward(grad, q, k, v, out, lse, **kw)[0 if which == "dq" else 1]
+    want = torch.zeros(n, 2, D, dtype=torch.float64)
+    at = 0
+    for m in lens:
+        s = slice(at, at + m)
+        at += m
+        for h in range(2):
+            Q, K, V, G = (t[s, h].double().cpu() for t in (q, k, v, grad))
+            P = (Q @ K.t() * D ** -0.5).softmax(1)
+            dP = G @ V.t()
+            dS = P * (dP - (G * out[s, h].double().cpu()).sum(1, keepdim=True)) * D ** -0.5      # of the output as it was given
+            want[s, h] = dS @ K if which == "dq" else dS.t() @ Q
+    rel = float((got.double().cpu() - want).norm() / want.norm())
+    print(f"{rel:.1e}", flush=True)
+    assert rel <= 2 * 2.0 ** -11
