@@ -50,7 +50,7 @@ struct Attention {
     int64_t k_units;
     int k_parts, part_rows;            // of the queries that the keys' columns walk
     float *part_dk, *part_dv;          // [part][k_rows][k_heads][D]
-    float *against, *delta;            // [q_heads][q_rows]: lse times log2 e, infinite for a row that sees nothing; sum(do o)
+    float *against, *delta;            // [q_heads][q_rows]: lse times log2 e, infinite for a row that sees nothing; -sum(do o)
 };
 
 __device__ __forceinline__ int row_of_column(const Attention& p, int c) { return p.per == 1 ? c : (int)(__umulhi((uint32_t)c, p.per_magic) >> p.per_shift); }
@@ -177,6 +177,14 @@ struct TileLoader {
     }
 };
 // What a lane reads of a tile, whose first byte lies at a multiple of 1024: the chunk's number is in bits of its own of the address, so others of a line follow by an exclusive or.
+// `apart`, the way to the other operand's tile, goes into the instruction's offset: added to the address it cost an addition a read, and the compiler took 16 bytes as two reads of 8
+// that met banks twice.
+template <int DT>
+__device__ __forceinline__ f32x4 multiply(u32x4 a, uint4 b, f32x4 c) {
+    if constexpr (DT == SC_F32) return multiply<DT>(__builtin_bit_cast(uint4, a), b, c);
+    else if constexpr (DT == SC_F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
 // Rows as they lie (16 rows, 64 bytes of channels a step) ...
 template <int DT, int DPAD>
 struct RowReader {
@@ -186,8 +194,9 @@ struct RowReader {
         const int i = threadIdx.x & 15, g = (threadIdx.x >> 4) & 3;
         at = lds + i * H::BYTES + (g ^ tile_turn<DT, H::LINE>(i)) * 16;
     }
-    __device__ __forceinline__ uint4 read(uint32_t tile, int block, int k) const {
-        return __builtin_bit_cast(uint4, *(lds_u32x4)(((at + tile) ^ (k * 64)) + block * (16 * H::BYTES)));
+    __device__ __forceinline__ u32x4 read(uint32_t tile, int block, int k, int apart = 0) const {
+        const uint32_t p = ((at + tile) ^ (k * 64)) + (block * (16 * H::BYTES) + apart);
+        return *(lds_u32x4)p;
     }
 };
 // ... or across them: a block of 16 channels, of the rows 4 g .. 4 g + 3 of each 16, which are the rows that the quarter g of the lanes holds of S.
@@ -206,14 +215,14 @@ struct ChannelReader {
             at[0] = lds + line * H::BYTES + (((i >> 1) & 1) ^ tile_turn<DT, H::LINE>(line)) * 16 + (i & 1) * 8;
         }
     }
-    __device__ __forceinline__ uint4 read(uint32_t tile, int step, int c) const {
+    __device__ __forceinline__ uint4 read(uint32_t tile, int step, int c, int apart = 0) const {
         if constexpr (DT == SC_F32) {
             uint32_t v[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = *(lds_uint32)(((at[j] + tile) ^ (c * 64)) + step * (H::STEP * H::BYTES));
+            for (int j = 0; j < 4; ++j) v[j] = *(lds_uint32)(((at[j] + tile) ^ (c * 64)) + (step * (H::STEP * H::BYTES) + apart));
             return make_uint4(v[0], v[1], v[2], v[3]);
         } else {
-            const uint32_t p = ((at[0] + tile) ^ (c * 32)) + step * (H::STEP * H::BYTES);
+            const uint32_t p = ((at[0] + tile) ^ (c * 32)) + (step * (H::STEP * H::BYTES) + apart);
             const uint2 a = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p));
             const uint2 b = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(p + 16 * H::BYTES)));
             return make_uint4(a.x, a.y, b.x, b.y);
@@ -464,7 +473,7 @@ k_attention(const Attention p) {
                 for (int k = 0; k < H::KS; ++k)
 #pragma unroll
                     for (int b = 0; b < ST; ++b) {
-                        const uint4 a = rows.read(buffer, b, k);
+                        const u32x4 a = rows.read(buffer, b, k);
 #pragma unroll
                         for (int n = 0; n < TOGETHER; ++n) s[n][b] = multiply<DT>(a, q[n0 + n][k], s[n][b]);
                     }
@@ -615,18 +624,19 @@ constexpr int grad_waves(int rows, int results) {                 // wavefronts 
 template <int DT>
 constexpr float WEIGHT_LIFT = DT == SC_F16 ? 14.f : 0.f;
 struct GradScale {
+    int log2 = 0;
     float factor = 1.f;
     bool set = false;
 };
-// What sums and the gradients at hand, of which `most` is the lane's largest, are to be multiplied by: 1 almost always.
+// What sums and the gradients at hand, of which `most` is the lane's largest, are to be multiplied by: 1 almost always.  Past 2^60 there is nothing to win: a result of
+// f16 has no use for what is smaller, and gradients to come have to fit.
 __device__ __forceinline__ float rescale(GradScale& scale, float most) {
     if (scale.set ? __all(most <= 32768.f) : !__any(most > 0.f)) return 1.f;
-    most = over_lanes_max(most);
-    scale.set = true;
-    if (!(most < __builtin_inff())) return 1.f;
-    const float by = ldexpf(1.f, 8 - __builtin_amdgcn_frexp_expf(most)), factor = scale.factor * by;
-    if (!(factor > 1e-30f && factor < 1e30f)) return 1.f;
-    scale.factor = factor;
+    most = over_lanes_max(most < __builtin_inff() ? most : 0.f);              // what is not finite stays so
+    if (scale.set ? most <= 32768.f : most == 0.f) return 1.f;
+    const int log2 = max(-60, min(60, scale.log2 + 8 - __builtin_amdgcn_frexp_expf(most)));
+    const float by = ldexpf(1.f, log2 - scale.log2);
+    scale = GradScale{log2, ldexpf(1.f, log2), true};
     return by;
 }
 
@@ -689,7 +699,7 @@ k_attention_dq(const Attention p) {
         delta[n] = over_quarters_sum(sum);
         if (there[n] && g == 0 && part == 0) {                    // for the keys' kernel, a head's rows together
             p.against[(int64_t)head_of[n] * p.q_rows + row] = against[n] - WEIGHT_LIFT<DT>;
-            p.delta[(int64_t)head_of[n] * p.q_rows + row] = delta[n];
+            p.delta[(int64_t)head_of[n] * p.q_rows + row] = -delta[n];
         }
 #pragma unroll
         for (int c = 0; c < H::CB; ++c) dq[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -738,12 +748,15 @@ k_attention_dq(const Attention p) {
 #pragma unroll
                 for (int n = 0; n < TOGETHER; ++n)
 #pragma unroll
-                    for (int b = 0; b < SUB_BLOCKS; ++b) s[n][b] = dp[n][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    for (int b = 0; b < SUB_BLOCKS; ++b) {
+                        s[n][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+                        dp[n][b] = f32x4{-delta[n0 + n], -delta[n0 + n], -delta[n0 + n], -delta[n0 + n]};      // taken away here it costs no instruction
+                    }
 #pragma unroll
                 for (int k = 0; k < H::KS; ++k)
 #pragma unroll
                     for (int b = 0; b < SUB_BLOCKS; ++b) {
-                        const uint4 a = rows.read(tile, b, k), v = rows.read(tile + TILE_BYTES, b, k);
+                        const u32x4 a = rows.read(tile, b, k), v = rows.read(tile, b, k, TILE_BYTES);
 #pragma unroll
                         for (int n = 0; n < TOGETHER; ++n) {
                             s[n][b] = multiply<DT>(a, q[n0 + n][k], s[n][b]);
@@ -756,8 +769,7 @@ k_attention_dq(const Attention p) {
                     for (int b = 0; b < SUB_BLOCKS; ++b)
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
-                            s[n][b][r] = __builtin_amdgcn_exp2f(fmaf(s[n][b][r], p.scale_log2, -against[n0 + n])) *
-                                         (DT == SC_F16 ? fmaf(dp[n][b][r], scale.factor, -delta[n0 + n] * scale.factor) : dp[n][b][r] - delta[n0 + n]);
+                            s[n][b][r] = __builtin_amdgcn_exp2f(fmaf(s[n][b][r], p.scale_log2, scale.log2 - against[n0 + n])) * dp[n][b][r];
                 if (key0 + SUB > first_limit) {
 #pragma unroll
                     for (int n = 0; n < TOGETHER; ++n)
@@ -924,12 +936,21 @@ k_attention_dkv(const Attention p) {
 #pragma unroll
                 for (int m = 0; m < TOGETHER; ++m)
 #pragma unroll
-                    for (int b = 0; b < SUB_BLOCKS; ++b) s[m][b] = dp[m][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    for (int b = 0; b < SUB_BLOCKS; ++b) s[m][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+                f32x4 against[SUB_BLOCKS];
+#pragma unroll
+                for (int b = 0; b < SUB_BLOCKS; ++b) {
+                    const uint32_t sums = lds0 + SUMS + which * 512 + (h * SUB + 16 * b + 4 * g) * 4;
+                    against[b] = __builtin_bit_cast(f32x4, *(lds_u32x4)sums);
+                    const f32x4 delta = __builtin_bit_cast(f32x4, *(lds_u32x4)(sums + 256));
+#pragma unroll
+                    for (int m = 0; m < TOGETHER; ++m) dp[m][b] = delta;
+                }
 #pragma unroll
                 for (int c = 0; c < H::KS; ++c)
 #pragma unroll
                     for (int b = 0; b < SUB_BLOCKS; ++b) {
-                        const uint4 a = rows.read(tile, b, c), d = rows.read(tile + TILE_BYTES, b, c);
+                        const u32x4 a = rows.read(tile, b, c), d = rows.read(tile, b, c, TILE_BYTES);
 #pragma unroll
                         for (int m = 0; m < TOGETHER; ++m) {
                             s[m][b] = multiply<DT>(a, k[m0 + m][c], s[m][b]);
@@ -938,17 +959,14 @@ k_attention_dkv(const Attention p) {
                     }
                 const float lowered = DT == SC_F16 ? scale.factor * 0x1p-14f : 1.f;         // the weights' lift taken back
 #pragma unroll
-                for (int b = 0; b < SUB_BLOCKS; ++b) {
-                    const uint32_t sums = lds0 + SUMS + which * 512 + (h * SUB + 16 * b + 4 * g) * 4;
-                    const f32x4 against = __builtin_bit_cast(f32x4, *(lds_u32x4)sums), delta = __builtin_bit_cast(f32x4, *(lds_u32x4)(sums + 256));
+                for (int m = 0; m < TOGETHER; ++m)
 #pragma unroll
-                    for (int m = 0; m < TOGETHER; ++m)
+                    for (int b = 0; b < SUB_BLOCKS; ++b)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
-                            s[m][b][r] = __builtin_amdgcn_exp2f(fmaf(s[m][b][r], p.scale_log2, -against[r]));
-                            dp[m][b][r] = s[m][b][r] * (DT == SC_F16 ? fmaf(dp[m][b][r], lowered, -delta[r] * lowered) : dp[m][b][r] - delta[r]);
+                            s[m][b][r] = __builtin_amdgcn_exp2f(fmaf(s[m][b][r], p.scale_log2, -against[b][r]));
+                            dp[m][b][r] = s[m][b][r] * (DT == SC_F16 ? dp[m][b][r] * lowered : dp[m][b][r]);
                         }
-                }
                 if (masked) {
 #pragma unroll
                     for (int m = 0; m < TOGETHER; ++m)
@@ -994,7 +1012,7 @@ k_attention_dkv(const Attention p) {
                     }
 #pragma unroll
                     for (int c = 0; c < H::CB; ++c) {
-                        const uint4 a = channels.read(tile + TILE_BYTES, u, c), b = channels.read(tile, u, c);
+                        const uint4 a = channels.read(tile, u, c, TILE_BYTES), b = channels.read(tile, u, c);
 #pragma unroll
                         for (int m = 0; m < TOGETHER; ++m) {
                             dv[m0 + m][c] = multiply<DT>(a, w[m], dv[m0 + m][c]);

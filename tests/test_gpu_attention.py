@@ -380,3 +380,33 @@ def test_small_gradients_in_f16(lens, which):
     rel = float((got.double().cpu() - want).norm() / want.norm())
     print(f"{rel:.1e}", flush=True)
     assert rel <= 2 * 2.0 ** -11
+
+
+@pytest.mark.parametrize("which", ["dq", "dk"])
+@pytest.mark.parametrize("n", [300, 4000])
+@pytest.mark.parametrize("wide", [1, 32])
+def test_small_gradients_in_f16_behind_vanishing_ones(n, which, wide):
+    """As above, behind 64 rows whose weights are some e^-85, whose gradients are hardly numbers of 32 bits.  The bound is that of the test above, and half a step of f16
+    where results are below 2^-14 (all steps there are 2^-24): without the factor of 32 some 10^-5 here."""
+    D = 32
+    q, k, v, grad = data(n, n, 2, 2, D, torch.float16, 19)
+    grad.mul_(2.0 ** -6 if n == 4000 else 2.0 ** -10)
+    summed, other = (k, q) if which == "dq" else (q, k)
+    summed.mul_(wide), other.mul_(1 / wide)
+    q[..., 0], k[..., 0] = 0, 0
+    if which == "dq":
+        q[..., 0], k[:64, :, 0] = 16, -30           # keys that no query has a weight for
+    else:
+        q[:64, :, 0], k[-1, :, 0] = 16, 30          # queries that have a weight for the last key only
+    out, lse = forward(q, k, v)
+    got = backward(grad, q, k, v, out, lse)[0 if which == "dq" else 1].double().cpu()
+    want = torch.zeros(n, 2, D, dtype=torch.float64)
+    for h in range(2):
+        Q, K, V, G, O = (t[:, h].double().cpu() for t in (q, k, v, grad, out))
+        P = (Q @ K.t() * D ** -0.5).softmax(1)
+        dS = P * (G @ V.t() - (G * O).sum(1, keepdim=True)) * D ** -0.5
+        want[:, h] = dS @ K if which == "dq" else dS.t() @ Q
+    got, want = got[:-1], want[:-1]                 # of the last key dP is delta but for roundings
+    error, bound = float((got - want).norm()), 2 * 2.0 ** -11 * float(want.norm()) + float((want.abs() < 2.0 ** -14).double().sum().sqrt()) * 2.0 ** -25
+    print(f"{error / float(want.norm()):.1e} {error / bound:.2f}", flush=True)
+    assert error <= bound
