@@ -878,16 +878,6 @@ k_attention_dkv(const Attention p) {
     const int lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int column0 = at * COLUMNS + (SHARE == SHARED ? wave * 16 * NB : 0), ahead = nk - nq;
-    uint4 k[NB][H::KS], v[NB][H::KS];
-    f32x4 dk[NB][H::CB], dv[NB][H::CB];
-#pragma unroll
-    for (int n = 0; n < NB; ++n) {
-        const int c = column0 + 16 * n + i;
-        load_columns<DT, DPAD, WHOLE>(c < nk ? row_at(p.k.data + k0 * p.k.row + head_k * p.k.head, c, p.k.row) : nullptr, p.D, k[n]);
-        load_columns<DT, DPAD, WHOLE>(c < nk ? row_at(p.v.data + k0 * p.v.row + head_k * p.v.head, c, p.v.row) : nullptr, p.D, v[n]);
-#pragma unroll
-        for (int c = 0; c < H::CB; ++c) dk[n][c] = dv[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
     // rows that see key c: c - ahead on
     const int tiles = (nq + RT - 1) / RT;
     int first_row = p.causal ? at * COLUMNS - ahead : 0;
@@ -903,8 +893,13 @@ k_attention_dkv(const Attention p) {
     int from = 0, to = total;
     if (p.k_parts > 1) part_of(total, RT, part, p.k_parts, p.part_rows, from, to);
     TileLoader<DT, DPAD, RT, SHARE == SHARED ? 64 * WAVES : 64, WHOLE> queries{nullptr, p.q.row, p.D}, grads{nullptr, p.dout.row, p.D};
-    auto bring = [&](int n, int which) __attribute__((always_inline)) {
-        const int h = n / each, t = first_tile + n - h * each, head = head_k * p.per + h, left = nq - t * RT;
+    int next_head = 0, next = 0;                                  // of the tile to bring
+    if (p.k_parts > 1 && from < to) {
+        next_head = (int)((uint32_t)from / (uint32_t)each);
+        next = from - next_head * each;
+    }
+    auto bring = [&](int which) __attribute__((always_inline)) {
+        const int t = first_tile + next, head = head_k * p.per + next_head, left = nq - t * RT;
         queries.base = p.q.data + q0 * p.q.row + head * p.q.head;
         grads.base = p.dout.data + q0 * p.dout.row + head * p.dout.head;
         queries.fetch(t * RT, left, lds0 + which * (2 * TILE_BYTES));
@@ -920,7 +915,17 @@ k_attention_dkv(const Attention p) {
 #pragma unroll
         for (int b = 0; b < 4; ++b) queries.clear(lds0 + b * TILE_BYTES);
     }
-    if (from < to) bring(from, 0);
+    if (from < to) bring(0);
+    uint4 k[NB][H::KS], v[NB][H::KS];
+    f32x4 dk[NB][H::CB], dv[NB][H::CB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+        const int c = column0 + 16 * n + i;
+        load_columns<DT, DPAD, WHOLE>(c < nk ? row_at(p.k.data + k0 * p.k.row + head_k * p.k.head, c, p.k.row) : nullptr, p.D, k[n]);
+        load_columns<DT, DPAD, WHOLE>(c < nk ? row_at(p.v.data + k0 * p.v.row + head_k * p.v.head, c, p.v.row) : nullptr, p.D, v[n]);
+#pragma unroll
+        for (int c = 0; c < H::CB; ++c) dk[n][c] = dv[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
     int which = 0;
     GradScale scale;
     for (int n = from; n < to; ++n, which ^= 1) {
@@ -929,8 +934,12 @@ k_attention_dkv(const Attention p) {
         grads.settle(lds0 + which * (2 * TILE_BYTES) + TILE_BYTES);
         if constexpr (SHARE == SHARED) lds_barrier();
         else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (n + 1 < to) bring(n + 1, which ^ 1);
-        const int row_tile = (first_tile + n % each) * RT;
+        const int row_tile = (first_tile + next) * RT;
+        if (++next == each) {
+            next = 0;
+            ++next_head;
+        }
+        if (n + 1 < to) bring(which ^ 1);
 #pragma unroll 1
         for (int h = 0; h < RT / SUB; ++h) {
             const int row0 = row_tile + h * SUB;
