@@ -412,7 +412,7 @@ template <int DT>
 int launch_norm(const Norm& p, bool few, hipStream_t s) {
     const int pairs = p.scenes * p.groups;
     if (few) {
-        if (p.rows * p.channels <= 1024) SC_LAUNCH(KID_NORM, (k_norm_few<DT, 256>), dim3((unsigned)pairs), dim3(256), 0, s, p);
+        if (norm_few_threads(p.rows, p.channels, p.scenes) == 256) SC_LAUNCH(KID_NORM, (k_norm_few<DT, 256>), dim3((unsigned)pairs), dim3(256), 0, s, p);
         else SC_LAUNCH(KID_NORM, (k_norm_few<DT, 1024>), dim3((unsigned)pairs), dim3(1024), 0, s, p);
         return SC_OK;
     }
@@ -476,7 +476,7 @@ extern "C" int sc_group_norm_fwd(const void* d_x, int64_t ldx, int64_t rows, con
     p.units = scene_units(rows, scenes, p.per);
     p.sums = (float2*)d_workspace;
     p.stats = d_stats != nullptr ? (float2*)d_stats : (float2*)((char*)d_workspace + up16((size_t)p.units * C * sizeof(float2)));
-    const bool few = norm_few(rows, p.channels);
+    const bool few = norm_few(rows, p.channels) && (int64_t)scenes * groups <= NORM_FEW_PAIRS_MAX;
     hipStream_t s = (hipStream_t)stream;
     return dtype == SC_F32 ? launch_norm<SC_F32>(p, few, s) : dtype == SC_F16 ? launch_norm<SC_F16>(p, few, s) : launch_norm<SC_BF16>(p, few, s);
 }

@@ -356,5 +356,9 @@ constexpr int norm_rows(int64_t rows, int C) {
 constexpr bool norm_join_by_wavefronts(int64_t pairs) { return pairs >= 1024; }
 // One launch, a workgroup for a scene's group, whose rows may all be of one scene: 33 rows of 8 channels a group 4.0 us, 898 12.1 (three launches of 4 to 5 each).
 constexpr bool norm_few(int64_t rows, int channels) { return rows * channels <= 8192; }
+// ... of 1024 threads, or of 256 where a scene's group is small: 1000 rows of 32 groups of 8 channels, 31 scenes, 12.7 / 4.7 us; 8000 of 64 of one, 15, 15.8 / 9.2.  Many groups are taken by
+// units: 200 rows, 8192 groups 13.1 / 14.4 us; 8000 rows, 64000 groups 88 / 40.  A launch of 1024 threads each is below 2^32 threads.
+constexpr int norm_few_threads(int64_t rows, int channels, int64_t scenes) { return rows * channels > 1024 * scenes ? 1024 : 256; }
+constexpr int64_t NORM_FEW_PAIRS_MAX = 8192;
 
 }  // namespace sc

@@ -17,6 +17,7 @@ static_assert(attention_parts(ATTENTION_FEW, 8, 1, 8, 77, false) == 1 && attenti
 static_assert(attention_grad_alone(110545, 2303, 8, 110545, 64, false) && !attention_grad_alone(65536, 4, 4, 16384, 128, false) && attention_grad_alone(4503, 7, 2, 1501, 128, true), "alone");
 static_assert(norm_rows(261574, 64) == 256 && norm_rows(110545, 256) == 64 && norm_rows(3001, 45) == 64 && norm_rows(67108864, 8) <= 67108864, "rows of a unit");
 static_assert(norm_few(33, 8) && !norm_few(261574, 8), "few rows");
+static_assert(norm_few_threads(898, 8, 1) == 1024 && norm_few_threads(33, 8, 1) == 256 && norm_few_threads(1000, 8, 16) == 256, "threads of a group");
 
 #define HOLDS(what)                                                                            \
     if (!(what)) {                                                                             \

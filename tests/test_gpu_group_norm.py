@@ -238,3 +238,22 @@ def test_no_rows():
     assert (stats[..., 0] == 0).all() and (stats[..., 1] == 2).all()
     sc.sc_group_norm_bwd(x, x, stats, x, 4, starts, grad_gain=gain, grad_bias=gain.clone(), workspace=workspace)
     assert (gain == 0).all()
+
+
+@pytest.mark.parametrize("scenes", [8192, 8193, 4194400])
+def test_few_rows_in_many_scenes(scenes):
+    """Nearly all of them empty; of the most, a workgroup of 1024 threads each would be 2^32 threads.  Sums of n = 120 numbers d up to 8 in 32 bits, and of their squares, in any order: the mean is off by
+    n 8 2^-24 at most, the variance by (n + 2) 2^-24 of the mean square about a row, at most 65 of a variance near 1, 1 / deviation by half of that; a result of at most 5 by their sum."""
+    rows, C, eps = 200, 16, 1e-5
+    x = torch.randn(rows, C, generator=torch.Generator().manual_seed(3)).cuda()
+    starts = torch.full((scenes + 1,), 80, dtype=torch.int32, device="cuda")
+    starts[0], starts[-1] = 0, rows
+    y, stats = torch.empty_like(x), torch.empty(scenes, 1, 2, device="cuda")
+    sc.sc_group_norm_fwd(x, y, 1, starts, eps=eps, stats=stats, workspace=torch.empty(sc.sc_group_norm_workspace_bytes(rows, scenes, C, 1), dtype=torch.uint8, device="cuda"))
+    of_mean, of_rstd = 120 * 8 * 2.0 ** -24, 122 * 65 * 2.0 ** -25 * 1.1
+    for part, s in ((slice(0, 80), 0), (slice(80, rows), scenes - 1)):
+        a = x[part].double().cpu()
+        mean, rstd = a.mean(), (a.var(unbiased=False) + eps).rsqrt()
+        assert ((y[part].double().cpu() - (a - mean) * rstd).abs() <= 5 * of_rstd + 1.1 * of_mean + 8 * 2.0 ** -23).all()
+        assert abs(float(stats[s, 0, 0]) - float(mean)) <= of_mean and abs(float(stats[s, 0, 1]) - float(rstd)) <= of_rstd
+    assert (stats[1:-1, 0, 0] == 0).all() and (stats[1:-1, 0, 1] - eps ** -0.5).abs().max() <= eps ** -0.5 * 2.0 ** -23
