@@ -479,6 +479,7 @@ int sc_qk_rope_bwd(const sc_heads* dq_out, const sc_heads* dk_out, const sc_head
  *   d_lse      [q_rows][q->heads] or NULL: what sc_attention_bwd needs
  *   D          1 to SC_ATTENTION_HEAD_MAX; scenes 1 to SC_SCENES_MAX; rows up to SC_N_MAX, q_rows (q->heads / k->heads) below 2^31 - 4096
  *   d_workspace  workspace_bytes >= sc_attention_workspace_bytes(...), which may be 0; 16-byte aligned
+ * SC_EINVAL also where scenes, heads and rows together make more than some 2^29 workgroups.
  * 16-bit weights are rounded to the rows' type ahead of their product with the values; sums are in 32 bits.  Scenes, and keys that do not count, never reach each other's results; inside a
  * causal scene a v that is not finite may also reach queries up to 63 rows ahead of it (zero times infinity), backward any row that is not finite. */
 #define SC_ATTENTION_HEAD_MAX 256
@@ -491,7 +492,8 @@ int sc_attention_fwd(const sc_heads* q, const sc_heads* k, const sc_heads* v, in
                      int dtype, void* d_workspace, size_t workspace_bytes, void* stream);
 
 /* Gradients of sc_attention_fwd: of q, k and v from that of out.  `out` and d_lse are what the forward call stored.  Heads of keys get the sum over their queries' heads;
- * a key that no query sees gets zeros.  Rows of no scene, and keys beyond d_k_lens, are left untouched.  16-bit weights and their gradients are rounded to the rows' type ahead of their products. */
+ * a key that no query sees gets zeros.  Rows of no scene, and keys beyond d_k_lens, are left untouched.  16-bit weights and their gradients are rounded to the rows' type ahead of their products;
+ * in f16 they are held times powers of two meanwhile, so that small ones keep their eleven bits.  As forward, SC_EINVAL for more than some 2^29 workgroups. */
 size_t sc_attention_bwd_workspace_bytes(int64_t q_rows, int64_t k_rows, int scenes, int q_heads, int k_heads, int D, int dtype);
 int sc_attention_bwd(const sc_heads* dout, const sc_heads* q, const sc_heads* k, const sc_heads* v, const sc_heads* out, const float* d_lse,
                      int64_t q_rows, int64_t k_rows, int D,

@@ -15,9 +15,9 @@
 //     one row, 77 keys, 8 heads of 32, bf16                     4.9
 //     8 rows, 262144 keys, 16 heads of 128 over 4, f16          111    537 MB, 4.8 TB/s with the parts' join of 7; the walk alone 5.2
 //     53373 rows in 1112 scenes, 8 heads of 16, f16              31    55 MB; 11 million vector instructions, 18 us of every SIMD's time
-//     16384 rows in 3 causal scenes, 16 heads of 128 over 4, bf16  427    915 TFLOP/s
-//     backward 110545 rows in 2303 scenes, 8 heads of 16, f16   156    230 MB; 53 million vector instructions, 86 us
-//     backward 16384 rows in 4 causal scenes, 16 heads of 64 over 4, bf16  910    590 TFLOP/s of the five products that it cannot do without, 825 of the seven that it does
+//     16384 rows in 3 causal scenes, 16 heads of 128 over 4, bf16  387 to 427 by the card's clock    915 to 1010 TFLOP/s
+//     backward 110545 rows in 2303 scenes, 8 heads of 16, f16   163    230 MB; 53 million vector instructions, 86 us
+//     backward 16384 rows in 4 causal scenes, 16 heads of 64 over 4, bf16  817    656 TFLOP/s of the five products that it cannot do without, 918 of the seven that it does
 #pragma once
 
 #include "sc_product.h"
@@ -229,7 +229,8 @@ struct ChannelReader {
         }
     }
 };
-// Weights of a step as the second product's second operand: rounded once to the rows' type (f32: as they are).
+// Weights of a step as the second product's second operand: rounded once to the rows' type (f32: as they are), or the matrix cores would need two products, of a weight and of
+// what rounding left of it.  An error of a result's own rounding comes to it: of dq in bf16 0.0025 of its norm in place of the 0.0017 that the result's type costs.
 template <int DT, int ST>
 __device__ __forceinline__ uint4 weights_of(const f32x4 (&p)[ST], int step) {
     if constexpr (DT == SC_F32) {
