@@ -999,13 +999,16 @@ k_attention_dkv(const Attention p) {
                             }
                 }
                 if constexpr (DT == SC_F16) {
-                    float most = 0.f;
+                    float most = 0.f;                             // of columns that are keys: the weight of one that is none is exp(-lse), however large
 #pragma unroll
-                    for (int m = 0; m < TOGETHER; ++m)
+                    for (int m = 0; m < TOGETHER; ++m) {
+                        float of_column = 0.f;
 #pragma unroll
                         for (int b = 0; b < SUB_BLOCKS; ++b)
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) most = fmaxf(most, fabsf(dp[m][b][r]));
+                            for (int r = 0; r < 4; ++r) of_column = fmaxf(of_column, fabsf(dp[m][b][r]));
+                        most = i < nk - column0 - 16 * (m0 + m) ? fmaxf(most, of_column) : most;
+                    }
                     const bool summed = scale.set;                // or nothing but zeros so far
                     const float by = rescale(scale, most);
                     if (by != 1.f) {

@@ -410,3 +410,23 @@ def test_small_gradients_in_f16_behind_vanishing_ones(n, which, wide):
     error, bound = float((got - want).norm()), 2 * 2.0 ** -11 * float(want.norm()) + float((want.abs() < 2.0 ** -14).double().sum().sqrt()) * 2.0 ** -25
     print(f"{error / float(want.norm()):.1e} {error / bound:.2f}", flush=True)
     assert error <= bound
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("below", [20, 30, 60])
+@pytest.mark.parametrize("lens,key_lens,heads,D", [
+    ([10], [10], 2, 16), ([37, 10, 130, 1], [37, 10, 130, 1], 2, 64), ([1, 33, 2], [130, 37, 10], 2, 64), ([1037], [1037], 8, 64), ([2437], [2437], 4, 16)])
+def test_scores_far_below_zero(lens, key_lens, heads, D, below, causal, dt):
+    """All scores some 20 to 60 below zero, which softmax does not feel: a weight against such a sum that belongs to no key would be e^20 to e^60.  Wavefronts
+    alone, shared tiles, and queries in parts; the last block of keys is never full, and is seen whole by single rows behind a causal mask."""
+    q, k, v, grad = data(sum(lens), sum(key_lens), heads, heads, D, dt, 23)
+    q[..., 0], k[..., 0] = 16, -below * D ** 0.5 / 16
+    starts, k_starts = starts_of(lens), starts_of(key_lens)
+    kw = dict(q_starts=starts, k_starts=k_starts, causal=causal)
+    out, lse = forward(q, k, v, **kw)
+    want, off = reference(q, k, v, grad, lens, key_lens, k_starts.tolist(), starts.tolist(), causal, D ** -0.5, dt)
+    check("out", out, want[0], off[0])
+    check("lse", lse, want[1], off[1])
+    for name, got, ref, tol in zip(("dq", "dk", "dv"), backward(grad, q, k, v, out, lse, **kw), want[2:], off[2:]):
+        check(name, got, ref, tol)
