@@ -356,10 +356,10 @@ int sc_conv_up_fwd(const void* d_feat_coarse, int64_t n_map,
  * Conventions beside those above: rows are `ld` elements apart (the row's channels <= ld <= SC_LD_MAX, so a row may be
  * a slice of a wider one), every pointer needs the alignment of its elements only, and any number
  * of channels 1 <= C <= SC_CHANNELS_MAX is taken.  16-byte alignment of rows and channels that are multiples of 16
- * bytes are faster.  Types are SC_F32, SC_F16 and SC_BF16; sums are held in 32 bits.  Outputs must not overlap inputs,
- * except that d_y may be d_residual.  Every sum's order is fixed by the sizes: repeated calls give the same bits.
+ * bytes are faster.  Types are SC_F32, SC_F16 and SC_BF16; sums are held in 32 bits.  Outputs must not overlap inputs
+ * or each other, except that d_y may be d_residual and where a call says so.  Every sum's order is fixed by the sizes: repeated calls give the same bits.
  * No rows, no entries: nothing is written but the gradients of weights, biases and gains, which are zeros.  Rows may then be NULL in the linear
- * and grouped calls, but not a gradient that is asked for, nor the data of queries and keys and d_pos in sc_qk_rope_*. */
+ * and grouped calls, but not a gradient that is asked for, nor the data of queries and keys in sc_qk_rope_* and sc_attention_*, nor d_pos. */
 #define SC_CHANNELS_MAX 65536
 #define SC_LD_MAX       536870912LL    /* 2^29 */
 #define SC_GROUPS_MAX   65536
@@ -479,6 +479,7 @@ int sc_qk_rope_bwd(const sc_heads* dq_out, const sc_heads* dk_out, const sc_head
  *   d_lse      [q_rows][q->heads] or NULL: what sc_attention_bwd needs
  *   D          1 to SC_ATTENTION_HEAD_MAX; scenes 1 to SC_SCENES_MAX; rows up to SC_N_MAX, q_rows (q->heads / k->heads) below 2^31 - 4096
  *   d_workspace  workspace_bytes >= sc_attention_workspace_bytes(...), which may be 0; 16-byte aligned
+ * `out` may be q itself (same strides); where it meets q otherwise, or k or v, the call answers SC_EINVAL as far as that follows from places and strides (the same strides, or the same first element).
  * SC_EINVAL also where scenes, heads and rows together make more than some 2^29 workgroups.
  * 16-bit weights are rounded to the rows' type ahead of their product with the values; sums are in 32 bits.  Scenes, and keys that do not count, never reach each other's results; inside a
  * causal scene a v that is not finite may also reach queries up to 63 rows ahead of it (zero times infinity), backward any row that is not finite. */
@@ -492,7 +493,8 @@ int sc_attention_fwd(const sc_heads* q, const sc_heads* k, const sc_heads* v, in
                      int dtype, void* d_workspace, size_t workspace_bytes, void* stream);
 
 /* Gradients of sc_attention_fwd: of q, k and v from that of out.  `out` and d_lse are what the forward call stored.  Heads of keys get the sum over their queries' heads;
- * a key that no query sees gets zeros.  Rows of no scene, and keys beyond d_k_lens, are left untouched.  16-bit weights and their gradients are rounded to the rows' type ahead of their products;
+ * a key that no query sees gets zeros.  Rows of no scene, and keys beyond d_k_lens, are left untouched.  Gradients share no element with each other or with an operand, but dq may be `out` itself,
+ * dk and dv may be k and v themselves: others are refused with SC_EINVAL as forward.  16-bit weights and their gradients are rounded to the rows' type ahead of their products;
  * in f16 they are held times powers of two meanwhile, so that small ones keep their eleven bits.  As forward, SC_EINVAL for more than some 2^29 workgroups. */
 size_t sc_attention_bwd_workspace_bytes(int64_t q_rows, int64_t k_rows, int scenes, int q_heads, int k_heads, int D, int dtype);
 int sc_attention_bwd(const sc_heads* dout, const sc_heads* q, const sc_heads* k, const sc_heads* v, const sc_heads* out, const float* d_lse,

@@ -454,7 +454,7 @@ def sc_attention_bwd_workspace_bytes(q_rows: int, k_rows: int, scenes: int, q_he
 
 def sc_attention_bwd(grad_out, q, k, v, out, lse, grad_q, grad_k, grad_v, q_starts=None, k_starts=None, k_lens=None, causal=False, scale=None,
                      workspace=None, stream=None):
-    """Gradients of sc_attention_fwd, whose out and lse these are; workspace uint8 [>= sc_attention_bwd_workspace_bytes(...)]."""
+    """Gradients of sc_attention_fwd, whose out and lse these are, in tensors, or slices, of their own; workspace uint8 [>= sc_attention_bwd_workspace_bytes(...)]."""
     rc = _native.attention_bwd(grad_out, q, k, v, out, lse, grad_q, grad_k, grad_v, q_starts, k_starts, k_lens, 1 if causal else 0,
                                q.shape[-1] ** -0.5 if scale is None else scale, workspace, stream)
     if rc:

@@ -72,6 +72,25 @@ int check_attention(const sc_heads* q, const sc_heads* k, const sc_heads* v, int
     if (causal != 0 && causal != 1) return SC_EINVAL;
     return scale > 0.f && scale <= 3.0e38f ? SC_OK : SC_EINVAL;
 }
+// An output that shares elements with what other workgroups still read, or with another output, is refused; one in the very place of an operand that only its own
+// columns are read from is not.
+bool output_apart(const sc_heads* out, const sc_heads* q, const sc_heads* k, const sc_heads* v, int64_t q_rows, int64_t k_rows, int D, int dtype) {
+    return !heads_meet(out, q_rows, k, k_rows, D, dtype) && !heads_meet(out, q_rows, v, k_rows, D, dtype) &&
+           (heads_same(out, q, q_rows) || !heads_meet(out, q_rows, q, q_rows, D, dtype));
+}
+bool gradients_apart(const sc_heads* dout, const sc_heads* q, const sc_heads* k, const sc_heads* v, const sc_heads* out, const sc_heads* dq, const sc_heads* dk,
+                     const sc_heads* dv, int64_t q_rows, int64_t k_rows, int D, int dtype) {
+    if (heads_meet(dk, k_rows, dv, k_rows, D, dtype) || heads_meet(dq, q_rows, q, q_rows, D, dtype) || heads_meet(dq, q_rows, dout, q_rows, D, dtype)) return false;
+    if (!heads_same(dq, out, q_rows) && heads_meet(dq, q_rows, out, q_rows, D, dtype)) return false;
+    for (const sc_heads* of_keys : {k, v, dk, dv})
+        if (heads_meet(dq, q_rows, of_keys, k_rows, D, dtype)) return false;
+    for (const sc_heads* grad : {dk, dv}) {
+        if (heads_meet(grad, k_rows, q, q_rows, D, dtype) || heads_meet(grad, k_rows, dout, q_rows, D, dtype)) return false;
+        for (const sc_heads* own : {k, v})
+            if (!heads_same(grad, own, k_rows) && heads_meet(grad, k_rows, own, k_rows, D, dtype)) return false;
+    }
+    return true;
+}
 Attention attention_of(const sc_heads* q, const sc_heads* k, const sc_heads* v, int64_t q_rows, int64_t k_rows, int D, const int32_t* q_starts, const int32_t* k_starts,
                        const int32_t* k_lens, int scenes, int causal, float scale, const sc_heads* out, float* lse, int dtype) {
     Attention p{};
@@ -121,6 +140,7 @@ extern "C" int sc_attention_fwd(const sc_heads* q, const sc_heads* k, const sc_h
     const size_t need = sc_attention_workspace_bytes(q_rows, k_rows, scenes, q->heads, k->heads, D, dtype);
     if (need > 0 && (d_workspace == nullptr || !aligned16(d_workspace))) return SC_EINVAL;
     if (workspace_bytes < need) return SC_ECAP;
+    if (!output_apart(out, q, k, v, q_rows, k_rows, D, dtype)) return SC_EINVAL;
     if (q_rows == 0) return SC_OK;
     const Plan plan = plan_of(q_rows, k_rows, scenes, q->heads, k->heads, D, dtype);
     Attention p = attention_of(q, k, v, q_rows, k_rows, D, d_q_starts, d_k_starts, d_k_lens, scenes, causal, scale, out, d_lse, dtype);
@@ -152,6 +172,7 @@ extern "C" int sc_attention_bwd(const sc_heads* dout, const sc_heads* q, const s
     const size_t need = sc_attention_bwd_workspace_bytes(q_rows, k_rows, scenes, q->heads, k->heads, D, dtype);
     if (need > 0 && (d_workspace == nullptr || !aligned16(d_workspace))) return SC_EINVAL;
     if (workspace_bytes < need) return SC_ECAP;
+    if (!gradients_apart(dout, q, k, v, out, dq, dk, dv, q_rows, k_rows, D, dtype)) return SC_EINVAL;
     Attention p = attention_of(q, k, v, q_rows, k_rows, D, d_q_starts, d_k_starts, d_k_lens, scenes, causal, scale, out, const_cast<float*>(d_lse), dtype);
     p.dout = rows_of(dout, dtype);
     p.dq = rows_of(dq, dtype);

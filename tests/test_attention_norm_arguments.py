@@ -145,3 +145,22 @@ def test_group_norm_tensors():
             sc.sc_group_norm_bwd(*args, stream=0, **kw)
     with pytest.raises(KeyError):
         sc.sc_group_norm_fwd(x, x, 4, act="tanh", stream=0)
+
+
+def test_attention_refuses_outputs_that_meet_operands(lib):
+    """Slices of one row [5][20 heads of 64], 2 bytes a channel: two heads of queries, one of keys.  An output may share no element with what other workgroups still read, or
+    with another output."""
+    def at(head, n, byte=0):
+        return heads(data=(1 << 20) + 128 * head + byte, row=1280, head=64, n=n)
+    need = max(lib.sc_attention_bwd_workspace_bytes(5, 5, 1, 2, 1, 64, F16), lib.sc_attention_workspace_bytes(5, 5, 1, 2, 1, 64, F16))
+    q, k, v, out, dout, dq, dk, dv = (dict(q=at(0, 2)), dict(k=at(2, 1)), dict(v=at(3, 1)), dict(out=at(4, 2)), dict(dout=at(6, 2)), dict(dq=at(8, 2)), dict(dk=at(10, 1)), dict(dv=at(11, 1)))
+    good = dict(**q, **k, **v, **out, q_rows=5, k_rows=5, ws=16, bytes=need)
+    for bad in (dict(out=at(2, 2)), dict(out=at(1, 2)), dict(out=at(0, 2, 2)), dict(out=at(2, 2, 64)), dict(out=at(22, 2)), dict(out=heads(data=(1 << 20) + 256, row=2560, head=64))):
+        assert fwd(lib, **{**good, **bad}) == EINVAL, bad
+    good.update(**dout, **dq, **dk, **dv, lse=16)
+    for name in ("q", "dout", "k", "v", "dk", "dv"):
+        assert bwd(lib, **{**good, "dq": {**q, **dout, "k": at(1, 2), "v": at(3, 2), "dk": at(9, 2), "dv": at(11, 2)}[name]}) == EINVAL, name
+    for name in ("dk", "dv"):
+        for other in (at(0, 1), at(1, 1), at(7, 1), at(2, 1, 2), at(3, 1, 126), at(9, 1), at(10 if name == "dv" else 11, 1)):
+            assert bwd(lib, **{**good, name: other}) == EINVAL, name
+    assert bwd(lib, **{**good, "dq": at(5, 2)}) == EINVAL                        # half of out

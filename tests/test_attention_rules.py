@@ -11,3 +11,12 @@ def test_rules_of_attention_and_norm(tmp_path):
     assert made.returncode == 0, made.stderr[-3000:]
     run = subprocess.run([program], capture_output=True, text=True, timeout=60)
     assert run.returncode == 0, run.stdout
+
+
+def test_operands_that_meet(tmp_path):
+    source, program = os.path.join(os.path.dirname(os.path.abspath(__file__)), "native", "heads.cpp"), str(tmp_path / "heads")
+    include = os.path.join(build.ROOT, "include")
+    made = subprocess.run([build.CXX, "-std=c++17", "-O1", "-Wall", "-Werror", "-I", build.CSRC, "-I", include, source, "-o", program], capture_output=True, text=True)
+    assert made.returncode == 0, made.stderr[-3000:]
+    run = subprocess.run([program], capture_output=True, text=True, timeout=60)
+    assert run.returncode == 0, run.stdout

@@ -430,3 +430,27 @@ def test_scores_far_below_zero(lens, key_lens, heads, D, below, causal, dt):
     check("lse", lse, want[1], off[1])
     for name, got, ref, tol in zip(("dq", "dk", "dv"), backward(grad, q, k, v, out, lse, **kw), want[2:], off[2:]):
         check(name, got, ref, tol)
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("lens", [[60, 70], [1, 2, 1], [2100]])
+def test_outputs_between_and_in_place_of_operands(lens, dt):
+    """Queries, keys and values, and their gradients, one head of each behind the other; results in the place of rows that nothing else reads.  The same bits as in tensors of their own."""
+    n, h, D = sum(lens), 4, 16
+    q, k, v, grad = data(n, n, h, h, D, dt, 29)
+    kw = dict(q_starts=starts_of(lens), causal=True)
+    out, lse = forward(q, k, v, **kw)
+    grads = backward(grad, q, k, v, out, lse, **kw)
+    between, there = torch.stack([q, k, v], 2), torch.full((n, h, 3, D), 7.0, dtype=dt, device=DEV)
+    got, got_lse = forward(*between.unbind(2), **kw)
+    assert torch.equal(got, out) and torch.equal(got_lse, lse)
+    backward(grad, *between.unbind(2), got, lse, grads=list(there.unbind(2)), **kw)
+    for a, b in zip(there.unbind(2), grads):
+        assert torch.equal(a, b)
+    x, y, z = k.clone(), v.clone(), out.clone()
+    backward(grad, q, x, y, z, lse, grads=[z, x, y], **kw)
+    for a, b in zip((z, x, y), grads):
+        assert torch.equal(a, b)
+    x = q.clone()
+    forward(x, k, v, out=x, **kw)
+    assert torch.equal(x, out)
