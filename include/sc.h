@@ -475,7 +475,7 @@ int sc_qk_rope_bwd(const sc_heads* dq_out, const sc_heads* dk_out, const sc_head
  *   d_q_starts, d_k_starts  [scenes + 1] as d_starts above, in rows of queries and of keys; d_k_starts NULL: the same (then q_rows == k_rows); both NULL: one scene of all rows.
  *              Rows of `out` and d_lse of no scene are left untouched
  *   d_k_lens   [scenes] or NULL: only that many of a scene's keys count, the first ones (a cache with room behind them, which is not read)
- *   scale      above 0
+ *   scale      above 0, at most SC_ATTENTION_SCALE_MAX: times the logarithm of e to base 2 it is a number of 32 bits
  *   d_lse      [q_rows][q->heads] or NULL: what sc_attention_bwd needs
  *   D          1 to SC_ATTENTION_HEAD_MAX; scenes 1 to SC_SCENES_MAX; rows up to SC_N_MAX, q_rows (q->heads / k->heads) below 2^31 - 4096
  *   d_workspace  workspace_bytes >= sc_attention_workspace_bytes(...), which may be 0; 16-byte aligned
@@ -485,6 +485,7 @@ int sc_qk_rope_bwd(const sc_heads* dq_out, const sc_heads* dk_out, const sc_head
  * causal scene a v that is not finite may also reach queries up to 63 rows ahead of it (zero times infinity), backward any row that is not finite. */
 #define SC_ATTENTION_HEAD_MAX 256
 #define SC_ATTENTION_LD_MAX   16777216LL    /* 2^24 */
+#define SC_ATTENTION_SCALE_MAX 2.3e38f
 #define SC_SCENES_MAX         SC_N_MAX
 size_t sc_attention_workspace_bytes(int64_t q_rows, int64_t k_rows, int scenes, int q_heads, int k_heads, int D, int dtype);
 int sc_attention_fwd(const sc_heads* q, const sc_heads* k, const sc_heads* v, int64_t q_rows, int64_t k_rows, int D,

@@ -70,7 +70,7 @@ int check_attention(const sc_heads* q, const sc_heads* k, const sc_heads* v, int
     if (q_starts == nullptr && (k_starts != nullptr || scenes != 1)) return SC_EINVAL;
     if (q_starts != nullptr && k_starts == nullptr && q_rows != k_rows) return SC_EINVAL;
     if (causal != 0 && causal != 1) return SC_EINVAL;
-    return scale > 0.f && scale <= 3.0e38f ? SC_OK : SC_EINVAL;
+    return scale > 0.f && scale <= SC_ATTENTION_SCALE_MAX ? SC_OK : SC_EINVAL;
 }
 // An output that shares elements with what other workgroups still read, or with another output, is refused; one in the very place of an operand that only its own
 // columns are read from is not.

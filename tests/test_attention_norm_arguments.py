@@ -164,3 +164,12 @@ def test_attention_refuses_outputs_that_meet_operands(lib):
         for other in (at(0, 1), at(1, 1), at(7, 1), at(2, 1, 2), at(3, 1, 126), at(9, 1), at(10 if name == "dv" else 11, 1)):
             assert bwd(lib, **{**good, name: other}) == EINVAL, name
     assert bwd(lib, **{**good, "dq": at(5, 2)}) == EINVAL                        # half of out
+
+
+def test_attention_refuses_scales_that_are_infinite_to_base_2(lib):
+    """Kernels take exponentials to base 2: scale log2(e) is above the largest number of 32 bits, 3.4028e38, from 2.3587e38 on."""
+    for call in (fwd, bwd):
+        for scale in (2.36e38, 2.9e38, 3.4e38):
+            assert call(lib, scale=scale) == EINVAL, scale
+    for scale in (1e-45, 1.0, sc.SC_ATTENTION_SCALE_MAX):
+        assert fwd(lib, scale=scale) == OK, scale

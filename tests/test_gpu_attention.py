@@ -454,3 +454,16 @@ def test_outputs_between_and_in_place_of_operands(lens, dt):
     x = q.clone()
     forward(x, k, v, out=x, **kw)
     assert torch.equal(x, out)
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("scale", [1e-45, sc.SC_ATTENTION_SCALE_MAX])
+def test_least_and_largest_scale(scale, dt):
+    """Scores of zero are zero whatever they are scaled by: every row gets the mean of the values, and the logarithm of their number."""
+    lens = [40, 1, 130]
+    q, k, v, grad = data(sum(lens), sum(lens), 2, 2, 20, dt, 31)
+    kw = dict(q_starts=starts_of(lens), scale=scale)
+    out, lse = forward(q * 0, k, v, **kw)
+    want, off = reference(q * 0, k, v, grad, lens, lens, kw["q_starts"].tolist(), kw["q_starts"].tolist(), False, 1.0, dt)
+    check("out", out, want[0], off[0])
+    check("lse", lse, want[1], off[1])
