@@ -482,10 +482,12 @@ int sc_qk_rope_bwd(const sc_heads* dq_out, const sc_heads* dk_out, const sc_head
  * `out` may be q itself (same strides); where it meets q otherwise, or k or v, the call answers SC_EINVAL as far as that follows from places and strides (the same strides, or the same first element).
  * SC_EINVAL also where scenes, heads and rows together make more than some 2^29 workgroups.
  * 16-bit weights are rounded to the rows' type ahead of their product with the values; sums are in 32 bits.  Scenes, and keys that do not count, never reach each other's results; inside a
- * causal scene a v that is not finite may also reach queries up to 63 rows ahead of it (zero times infinity), backward any row that is not finite. */
+ * causal scene a v that is not finite may also reach queries that it lies behind, by SC_ATTENTION_REACH keys behind the last that they see at most (zero times infinity); backward any row of the scene that
+ * is not finite may reach any other. */
 #define SC_ATTENTION_HEAD_MAX 256
 #define SC_ATTENTION_LD_MAX   16777216LL    /* 2^24 */
 #define SC_ATTENTION_SCALE_MAX 2.3e38f
+#define SC_ATTENTION_REACH    94
 #define SC_SCENES_MAX         SC_N_MAX
 size_t sc_attention_workspace_bytes(int64_t q_rows, int64_t k_rows, int scenes, int q_heads, int k_heads, int D, int dtype);
 int sc_attention_fwd(const sc_heads* q, const sc_heads* k, const sc_heads* v, int64_t q_rows, int64_t k_rows, int D,

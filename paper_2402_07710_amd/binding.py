@@ -32,7 +32,7 @@ DTYPES = {"f32": SC_F32, "f16": SC_F16, "bf16": SC_BF16,
 TORCH_DTYPES = {SC_F32: torch.float32, SC_F16: torch.float16, SC_BF16: torch.bfloat16}
 
 SC_CHANNELS_MAX, SC_GROUPS_MAX, SC_ENTRIES_MAX, SC_HEAD_MAX, SC_AXES_MAX = 65536, 65536, (1 << 31) - 1, 1024, 4
-SC_ATTENTION_HEAD_MAX, SC_ATTENTION_SCALE_MAX, SC_SCENES_MAX = 256, 2.3e38, SC_N_MAX
+SC_ATTENTION_HEAD_MAX, SC_ATTENTION_SCALE_MAX, SC_ATTENTION_REACH, SC_SCENES_MAX = 256, 2.3e38, 94, SC_N_MAX
 ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, 0: 0, 1: 1, 2: 2, 3: 3}
 PAIRINGS = {"halves": 0, "adjacent": 1, 0: 0, 1: 1}
 

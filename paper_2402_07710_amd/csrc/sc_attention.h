@@ -393,6 +393,8 @@ k_attention(const Attention p) {
     using H = HeadShape<DT, DPAD>;
     constexpr int WAVES = wavefronts<DT, DPAD, SHARE>(), KT = walked_tile<DT, DPAD, SHARE>(), ST = KT / 16, TILE_BYTES = KT * H::BYTES;
     constexpr int COLUMNS = 16 * NB * (SHARE == SHARED ? WAVES : 1), TOGETHER = blocks_together<NB, SHARE>();
+    // A wavefront's columns all go through a tile that its last one sees a key of: behind the last key that its first one sees there are 16 NB - 1 more, and the rest of a tile.
+    static_assert(16 * NB - 1 + KT - 1 <= SC_ATTENTION_REACH, "keys with a weight of zero meet their values no further");
     extern __shared__ __align__(1024) uint4 attention_lds_words[];
     const Item item = item_of<SHARE, WAVES>(p.k_heads, p.parts);
     const int head_k = item.head, part = item.part;

@@ -467,3 +467,31 @@ def test_least_and_largest_scale(scale, dt):
     want, off = reference(q * 0, k, v, grad, lens, lens, kw["q_starts"].tolist(), kw["q_starts"].tolist(), False, 1.0, dt)
     check("out", out, want[0], off[0])
     check("lse", lse, want[1], off[1])
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("lens,more,heads,D", [([130], 1, 1, 32), ([200, 180], 33, 8, 32), ([100] * 10, 1, 8, 32), ([95] * 80, 1, 8, 32), ([1300], 1, 30, 64), ([1300], 5, 30, 64), ([260], 64, 2, 256)])
+def test_values_that_are_not_finite_behind_a_causal_mask(lens, more, heads, D, dt):
+    """Queries that are further from them than SC_ATTENTION_REACH keys, the columns of a wavefront and the rest of a tile, do not feel them.  `more` keys than queries, so that
+    what a wavefront's rows see does not end with tiles; few columns, wavefronts alone with 32 and 64, shared tiles."""
+    key_lens = [n + more for n in lens]
+    q, k, v, _ = data(sum(lens), sum(key_lens), heads, heads, D, dt, 37)
+    starts, k_starts = starts_of(lens), starts_of(key_lens)
+    kw = dict(q_starts=starts, k_starts=k_starts, causal=True)
+    clean, clean_lse = forward(q, k, v, **kw)
+    furthest = 0
+    for place in (more, 31, 63, 64, 95, 127, 1023, min(key_lens) - 1):             # the key of every scene; the ends of tiles
+        if not more <= place < min(key_lens):
+            continue
+        bad = v.clone()
+        for at in k_starts.tolist()[:-1]:
+            bad[at + place] = float("inf")
+        got, lse = forward(q, k, bad, **kw)
+        assert torch.equal(lse, clean_lse)
+        for at, n in zip(starts.tolist(), lens):
+            mine = slice(at, at + n)
+            assert not got[mine][place - more:].isfinite().any(), "queries that see it"
+            reached = (got[mine] != clean[mine]).flatten(1).any(1)
+            furthest = max(furthest, place - more - int(reached.nonzero()[0]))     # from the last key that the query sees
+    print(f"{furthest} keys behind", flush=True)
+    assert furthest <= sc.SC_ATTENTION_REACH
