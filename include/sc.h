@@ -478,7 +478,8 @@ int sc_qk_rope_bwd(const sc_heads* dq_out, const sc_heads* dk_out, const sc_head
  *   scale      above 0, at most SC_ATTENTION_SCALE_MAX: times the logarithm of e to base 2 it is a number of 32 bits
  *   d_lse      [q_rows][q->heads] or NULL: what sc_attention_bwd needs
  *   D          1 to SC_ATTENTION_HEAD_MAX; scenes 1 to SC_SCENES_MAX; rows up to SC_N_MAX, q_rows (q->heads / k->heads) below 2^31 - 4096
- *   d_workspace  workspace_bytes >= sc_attention_workspace_bytes(...), which may be 0; 16-byte aligned
+ *   d_workspace  workspace_bytes >= sc_attention_workspace_bytes(...), which may be 0; 16-byte aligned.  The size is that of these rows and scenes: fewer of them may need more, because keys are
+ *              cut into parts where there are few columns.  For any rows, heads and scenes SC_ATTENTION_WORKSPACE_MAX(D) is enough
  * `out` may be q itself (same strides); where it meets q otherwise, or k or v, the call answers SC_EINVAL as far as that follows from places and strides (the same strides, or the same first element).
  * SC_EINVAL also where scenes, heads and rows together make more than some 2^29 workgroups.
  * 16-bit weights are rounded to the rows' type ahead of their product with the values; sums are in 32 bits.  Scenes, and keys that do not count, never reach each other's results; inside a
@@ -488,6 +489,7 @@ int sc_qk_rope_bwd(const sc_heads* dq_out, const sc_heads* dk_out, const sc_head
 #define SC_ATTENTION_LD_MAX   16777216LL    /* 2^24 */
 #define SC_ATTENTION_SCALE_MAX 2.3e38f
 #define SC_ATTENTION_REACH    94
+#define SC_ATTENTION_WORKSPACE_MAX(D) ((size_t)128000 * (4 * (D) + 8) + 16)
 #define SC_SCENES_MAX         SC_N_MAX
 size_t sc_attention_workspace_bytes(int64_t q_rows, int64_t k_rows, int scenes, int q_heads, int k_heads, int D, int dtype);
 int sc_attention_fwd(const sc_heads* q, const sc_heads* k, const sc_heads* v, int64_t q_rows, int64_t k_rows, int D,
@@ -498,7 +500,9 @@ int sc_attention_fwd(const sc_heads* q, const sc_heads* k, const sc_heads* v, in
 /* Gradients of sc_attention_fwd: of q, k and v from that of out.  `out` and d_lse are what the forward call stored.  Heads of keys get the sum over their queries' heads;
  * a key that no query sees gets zeros.  Rows of no scene, and keys beyond d_k_lens, are left untouched.  Gradients share no element with each other or with an operand, but dq may be `out` itself,
  * dk and dv may be k and v themselves: others are refused with SC_EINVAL as forward.  16-bit weights and their gradients are rounded to the rows' type ahead of their products;
- * in f16 they are held times powers of two meanwhile, so that small ones keep their eleven bits.  As forward, SC_EINVAL for more than some 2^29 workgroups. */
+ * in f16 they are held times powers of two meanwhile, so that small ones keep their eleven bits.  As forward, SC_EINVAL for more than some 2^29 workgroups.
+ * The workspace's size, too, is that of these rows and scenes, and fewer may need more: SC_ATTENTION_BWD_WORKSPACE_MAX is enough for up to as many rows and heads of queries, any of keys and any scenes. */
+#define SC_ATTENTION_BWD_WORKSPACE_MAX(q_rows, q_heads, D) ((size_t)8 * (q_rows) * (q_heads) + (size_t)4715520 * (D) + 80)
 size_t sc_attention_bwd_workspace_bytes(int64_t q_rows, int64_t k_rows, int scenes, int q_heads, int k_heads, int D, int dtype);
 int sc_attention_bwd(const sc_heads* dout, const sc_heads* q, const sc_heads* k, const sc_heads* v, const sc_heads* out, const float* d_lse,
                      int64_t q_rows, int64_t k_rows, int D,
@@ -514,7 +518,8 @@ int sc_attention_bwd(const sc_heads* dout, const sc_heads* q, const sc_heads* k,
  *   eps        above 0
  *   d_stats    [scenes][groups][2] or NULL: receives mean and 1 / sqrt(var + eps), what sc_group_norm_bwd needs; of a scene without rows 0 and 1 / sqrt(eps). 8-byte aligned
  *   groups divides C <= SC_CHANNELS_MAX; scenes * groups <= SC_NORM_PAIRS_MAX
- *   d_workspace  workspace_bytes >= sc_group_norm_workspace_bytes(...), 16-byte aligned, for both calls */
+ *   d_workspace  workspace_bytes >= sc_group_norm_workspace_bytes(...), 16-byte aligned, for both calls.  Fewer rows may need more; SC_NORM_WORKSPACE_MAX is enough for any rows and up to as many scenes */
+#define SC_NORM_WORKSPACE_MAX(scenes, C, groups) ((size_t)8 * ((size_t)(4096 + (scenes)) * (C) + (size_t)(scenes) * (groups)) + 32)
 #define SC_NORM_PAIRS_MAX 8388608    /* 2^23 */
 size_t sc_group_norm_workspace_bytes(int64_t rows, int scenes, int C, int groups);
 int sc_group_norm_fwd(const void* d_x, int64_t ldx, int64_t rows, const int32_t* d_starts, int scenes, int C, int groups,

@@ -438,11 +438,17 @@ def sc_attention_workspace_bytes(q_rows: int, k_rows: int, scenes: int, q_heads:
     return load().sc_attention_workspace_bytes(q_rows, k_rows, scenes, q_heads, k_heads, D, DTYPES[dtype])
 
 
+def sc_attention_workspace_max(D: int) -> int:
+    """Bytes of a workspace for sc_attention_fwd of any rows, heads and scenes."""
+    return 128000 * (4 * D + 8) + 16
+
+
 def sc_attention_fwd(q, k, v, out, q_starts=None, k_starts=None, k_lens=None, causal=False, scale=None, lse=None, workspace=None, stream=None):
     """Attention of queries [rows, heads, D] to keys and values [key rows, heads of keys, D] of their scene: starts int32 [scenes + 1] of queries
     and keys (k_starts None: the same; both None: one scene), k_lens int32 [scenes] where only the first keys of a scene count.  causal: a scene's queries are
     its last rows, and see no key behind them.  scale: 1/sqrt(D) if None.  lse float32 [rows, heads] receives what sc_attention_bwd needs;
-    workspace uint8 [>= sc_attention_workspace_bytes(...)], which may be 0."""
+    workspace uint8 [>= sc_attention_workspace_bytes(...)], which may be 0 and may grow where rows or scenes get fewer: one for all
+    of them has sc_attention_workspace_max(D)."""
     rc = _native.attention_fwd(q, k, v, out, q_starts, k_starts, k_lens, 1 if causal else 0, q.shape[-1] ** -0.5 if scale is None else scale, lse, workspace, stream)
     if rc:
         _check(rc, "sc_attention_fwd")
@@ -450,6 +456,11 @@ def sc_attention_fwd(q, k, v, out, q_starts=None, k_starts=None, k_lens=None, ca
 
 def sc_attention_bwd_workspace_bytes(q_rows: int, k_rows: int, scenes: int, q_heads: int, k_heads: int, D: int, dtype) -> int:
     return load().sc_attention_bwd_workspace_bytes(q_rows, k_rows, scenes, q_heads, k_heads, D, DTYPES[dtype])
+
+
+def sc_attention_bwd_workspace_max(q_rows: int, q_heads: int, D: int) -> int:
+    """Bytes of a workspace for sc_attention_bwd of up to as many rows and heads of queries, any of keys and any scenes."""
+    return 8 * q_rows * q_heads + 4715520 * D + 80
 
 
 def sc_attention_bwd(grad_out, q, k, v, out, lse, grad_q, grad_k, grad_v, q_starts=None, k_starts=None, k_lens=None, causal=False, scale=None,
@@ -463,6 +474,11 @@ def sc_attention_bwd(grad_out, q, k, v, out, lse, grad_q, grad_k, grad_v, q_star
 
 def sc_group_norm_workspace_bytes(rows: int, scenes: int, C: int, groups: int) -> int:
     return load().sc_group_norm_workspace_bytes(rows, scenes, C, groups)
+
+
+def sc_group_norm_workspace_max(scenes: int, C: int, groups: int) -> int:
+    """Bytes of a workspace for sc_group_norm_fwd and sc_group_norm_bwd of any rows and up to as many scenes."""
+    return 8 * ((4096 + scenes) * C + scenes * groups) + 32
 
 
 def sc_group_norm_fwd(x, out, groups, starts=None, gain=None, bias=None, act="none", eps=1e-5, stats=None, workspace=None, stream=None):

@@ -307,6 +307,7 @@ constexpr AttentionShape attention_shape(int64_t columns, int64_t scenes, int64_
 // Parts that the keys of a scene are cut into where its columns alone do not fill the chip, and the keys that a part has at least.  Joining them is a launch of 4 to 6 us more: one row of 8 heads
 // of 64, f16, over 512 keys whole / in parts 6.8 / 10.9 us, 1024 9.1 / 12, 2048 21 / 13 (WIDE: 512 rows 11 / 19, 2048 25 / 16).  f32, whose products take eight times as long, sooner.  Parts for
 // some 1000 workgroups: eight scenes of 32768 keys, 4 heads of 128, 500 / 1000 / 2000 116 / 109 / 112; where 512 are there, cutting them in two costs 42 -> 51 (64 scenes of 2048).
+// Parts times tiles times heads is at most 1000, so there are no more than 128000 partial results, which SC_ATTENTION_WORKSPACE_MAX counts on.
 constexpr int ATTENTION_PARTS_MAX = 256;
 constexpr int attention_part_keys(bool f32) { return f32 ? 64 : 256; }
 constexpr int attention_parts(AttentionShape shape, int64_t columns, int64_t scenes, int64_t k_heads, int64_t k_rows, bool f32) {
@@ -328,7 +329,7 @@ constexpr bool attention_grad_alone(int64_t columns, int64_t scenes, int64_t k_h
     return most <= (row_bytes <= 64 ? 144 : 72) * scenes || attention_tiles(ATTENTION_WIDE, most, scenes) * k_heads < (f32 ? 512 : 64);
 }
 // Parts of what `columns` of a scene walk, `rows` of the scenes together.  Causal sequences gain most, whose first keys and last queries take twice the mean: 16384 rows in four, 16 heads of 64 over 4,
-// keys' gradients in one part / three 867 / 537 us and 29 to join.
+// keys' gradients in one part / three 867 / 537 us and 29 to join.  Two parts or more are at most 1535 + 1535 workgroups of 128 columns, 392960 partial results, which SC_ATTENTION_BWD_WORKSPACE_MAX counts on.
 constexpr int ATTENTION_GRAD_PARTS_MAX = 16;
 constexpr int attention_part_rows(bool alone, bool f32) { return alone ? (f32 ? 64 : 128) : 1024; }
 constexpr int attention_grad_parts(bool alone, int64_t columns, int64_t scenes, int64_t k_heads, int64_t rows, bool f32) {

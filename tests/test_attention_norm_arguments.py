@@ -1,5 +1,8 @@
 """CPU tests of what attention and the group norm refuse, at the C boundary and in the marshalling of tensors, before anything is launched; and of their size queries."""
 import ctypes
+import os
+import random
+import re
 
 import pytest
 import torch
@@ -173,3 +176,31 @@ def test_attention_refuses_scales_that_are_infinite_to_base_2(lib):
             assert call(lib, scale=scale) == EINVAL, scale
     for scale in (1e-45, 1.0, sc.SC_ATTENTION_SCALE_MAX):
         assert fwd(lib, scale=scale) == OK, scale
+
+
+def test_workspaces_for_all_sizes(lib):
+    """Sizes shrink and grow with rows; the bounds, which the header and the binding give alike, hold for all of them."""
+    size, grad, norm = lib.sc_attention_workspace_bytes, lib.sc_attention_bwd_workspace_bytes, lib.sc_group_norm_workspace_bytes
+    assert size(2048, 2048, 1, 8, 8, 64, F16) > size(8192, 8192, 1, 8, 8, 64, F16) and grad(16384, 16384, 1, 8, 8, 64, F16) > grad(32768, 32768, 1, 8, 8, 64, F16)
+    assert norm(32000, 1, 64, 8) > norm(33000, 1, 64, 8)
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "sc.h")).read()
+
+    def macro(name):
+        found = re.search(r"#define " + name + r"\(([^)]*)\) (.*)", text)
+        return eval(f"lambda {found.group(1)}: " + found.group(2).replace("(size_t)", ""))
+    most, most_grad, most_norm = macro("SC_ATTENTION_WORKSPACE_MAX"), macro("SC_ATTENTION_BWD_WORKSPACE_MAX"), macro("SC_NORM_WORKSPACE_MAX")
+    rng, nearest = random.Random(3), [0.0, 0.0, 0.0]
+    for i in range(200000):
+        rows, keys, scenes, k_heads, per, D = (int(2 ** rng.uniform(0, bits)) for bits in (26, 26, 12, 6, 5, 8.001))
+        if i % 3 == 0:
+            keys = rows
+        dt, heads_q, scenes = rng.choice([F16, F32]), k_heads * per, 1 if i % 2 else scenes
+        need, need_grad = size(rows, keys, scenes, heads_q, k_heads, D, dt), grad(rows, keys, scenes, heads_q, k_heads, D, dt)
+        C, groups = k_heads * per, per
+        need_norm = norm(rows, scenes, C, groups)
+        for j, (n, m, m2) in enumerate(((need, most(D), sc.sc_attention_workspace_max(D)), (need_grad, most_grad(rows, heads_q, D), sc.sc_attention_bwd_workspace_max(rows, heads_q, D)),
+                                        (need_norm, most_norm(scenes, C, groups), sc.sc_group_norm_workspace_max(scenes, C, groups)))):
+            assert n <= m == m2, (j, rows, keys, scenes, heads_q, k_heads, D, dt)
+            nearest[j] = max(nearest[j], n / m)
+    print(nearest)
+    assert min(nearest) > 0.5, nearest
