@@ -495,3 +495,37 @@ def test_values_that_are_not_finite_behind_a_causal_mask(lens, more, heads, D, d
             furthest = max(furthest, place - more - int(reached.nonzero()[0]))     # from the last key that the query sees
     print(f"{furthest} keys behind", flush=True)
     assert furthest <= sc.SC_ATTENTION_REACH
+
+
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("hk,D", [(2, 64), (1, 128)])
+def test_sequences_of_many_rows(hk, D, causal, dt):
+    """20004 rows in two scenes, heads that share keys, all gradients.  Each result is a sum of terms that are rounded by half a step at most, and is rounded once, so as of a random sum its
+    error is within 2 half steps of its size in the mean square."""
+    lens, hq = [14001, 6003], 4
+    q, k, v, grad = data(sum(lens), sum(lens), hq, hk, D, dt, 41)
+    kw = dict(q_starts=starts_of(lens), causal=causal)
+    out, lse = forward(q, k, v, **kw)
+    got = [out, *backward(grad, q, k, v, out, lse, **kw)]
+    want, at = [torch.zeros(t.shape, dtype=torch.float64, device=DEV) for t in got], 0
+    for n in lens:
+        rows = slice(at, at + n)
+        at += n
+        for h in range(hq):
+            j = h // (hq // hk)
+            Q, K, V, G = q[rows, h].double(), k[rows, j].double(), v[rows, j].double(), grad[rows, h].double()
+            P = Q @ K.t() * D ** -0.5
+            if causal:
+                P = P.masked_fill_(torch.ones((n, n), dtype=torch.bool, device=DEV).triu_(1), -math.inf)
+            P = P.softmax(1)
+            dS = G @ V.t()
+            dS = P * dS.sub_((P * dS).sum(1, keepdim=True)) * D ** -0.5
+            want[0][rows, h] = P @ V
+            want[1][rows, h] = dS @ K
+            want[2][rows, j] += dS.t() @ Q
+            want[3][rows, j] += P.t() @ G
+    for name, a, b in zip(("out", "dq", "dk", "dv"), got, want):
+        rel = float((a.double() - b).norm() / b.norm())
+        print(f"{name} {rel:.1e}", flush=True)
+        assert rel <= 2 * half_step(dt), name

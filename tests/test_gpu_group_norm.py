@@ -5,6 +5,7 @@ so the mean is off by (per + 8) 2 K f and its own rounding, 2 f |mean|, and the 
 Activations of 16-bit rows are off by 1e-6 (1 + |v|), f32's by 8 f (1 + |v|), their slopes as much; no slope is above 1.13 or steeper than 1.  Then one rounding to the rows' type.
 """
 import math
+import sys
 
 import pytest
 import torch
@@ -257,3 +258,10 @@ def test_few_rows_in_many_scenes(scenes):
         assert ((y[part].double().cpu() - (a - mean) * rstd).abs() <= 5 * of_rstd + 1.1 * of_mean + 8 * 2.0 ** -23).all()
         assert abs(float(stats[s, 0, 0]) - float(mean)) <= of_mean and abs(float(stats[s, 0, 1]) - float(rstd)) <= of_rstd
     assert (stats[1:-1, 0, 0] == 0).all() and (stats[1:-1, 0, 1] - eps ** -0.5).abs().max() <= eps ** -0.5 * 2.0 ** -23
+
+
+@pytest.mark.parametrize("dt", TYPES)
+def test_units_of_more_than_1024_rows(dt, monkeypatch):
+    """Beyond 4.2 million rows a unit has more than PER of them: 2048 here."""
+    monkeypatch.setattr(sys.modules[__name__], "PER", 2048)
+    run([4100000, 0, 100001], 4, 2, dt, "silu", lead=1, trail=3)
