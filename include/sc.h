@@ -482,7 +482,7 @@ int sc_qk_rope_bwd(const sc_heads* dq_out, const sc_heads* dk_out, const sc_head
  *              cut into parts where there are few columns.  For any rows, heads and scenes SC_ATTENTION_WORKSPACE_MAX(D) is enough
  * `out` may be q itself (same strides); where it meets q otherwise, or k or v, the call answers SC_EINVAL as far as that follows from places and strides (the same strides, or the same first element).
  * SC_EINVAL also where scenes, heads and rows together make more than some 2^29 workgroups.
- * 16-bit weights are rounded to the rows' type ahead of their product with the values; sums are in 32 bits.  Scenes, and keys that do not count, never reach each other's results; inside a
+ * 16-bit weights are rounded to the rows' type ahead of their product with the values, not ahead of their sum; sums are in 32 bits.  Scenes, and keys that do not count, never reach each other's results; inside a
  * causal scene a v that is not finite may also reach queries that it lies behind, by SC_ATTENTION_REACH keys behind the last that they see at most (zero times infinity); backward any row of the scene that
  * is not finite may reach any other. */
 #define SC_ATTENTION_HEAD_MAX 256
@@ -500,7 +500,8 @@ int sc_attention_fwd(const sc_heads* q, const sc_heads* k, const sc_heads* v, in
 /* Gradients of sc_attention_fwd: of q, k and v from that of out.  `out` and d_lse are what the forward call stored.  Heads of keys get the sum over their queries' heads;
  * a key that no query sees gets zeros.  Rows of no scene, and keys beyond d_k_lens, are left untouched.  Gradients share no element with each other or with an operand, but dq may be `out` itself,
  * dk and dv may be k and v themselves: others are refused with SC_EINVAL as forward.  16-bit weights and their gradients are rounded to the rows' type ahead of their products;
- * in f16 they are held times powers of two meanwhile, so that small ones keep their eleven bits.  As forward, SC_EINVAL for more than some 2^29 workgroups.
+ * in f16 they are held times a power of two that 16 or 32
+ * neighbours share (queries' rows and heads, or keys), so that small ones keep their eleven bits down to 2^-21 of the largest among them.  As forward, SC_EINVAL for more than some 2^29 workgroups.
  * The workspace's size, too, is that of these rows and scenes, and fewer may need more: SC_ATTENTION_BWD_WORKSPACE_MAX is enough for up to as many rows and heads of queries, any of keys and any scenes. */
 #define SC_ATTENTION_BWD_WORKSPACE_MAX(q_rows, q_heads, D) ((size_t)8 * (q_rows) * (q_heads) + (size_t)4715520 * (D) + 80)
 size_t sc_attention_bwd_workspace_bytes(int64_t q_rows, int64_t k_rows, int scenes, int q_heads, int k_heads, int D, int dtype);

@@ -12,12 +12,12 @@
 // What bounds it: the matrix cores for long scenes, next to the vector unit (an exponential, two multiplications, an addition and a share of a comparison and of a conversion for every
 // score); vector instructions ahead of and behind the products for scenes of tens; memory for single rows over long caches; a few trips to memory, one after the other, for little of everything.
 // us of the call, a copy on this card 5.1 TB/s, the library's largest product 1120 TFLOP/s in 16 bits and 152 in 32:
-//     one row, 77 keys, 8 heads of 32, bf16                     4.9
-//     8 rows, 262144 keys, 16 heads of 128 over 4, f16          111    537 MB, 4.8 TB/s with the parts' join of 7; the walk alone 5.2
-//     53373 rows in 1112 scenes, 8 heads of 16, f16              31    55 MB; 11 million vector instructions, 18 us of every SIMD's time
-//     16384 rows in 3 causal scenes, 16 heads of 128 over 4, bf16  387 to 427 by the card's clock    915 to 1010 TFLOP/s
+//     one row, 77 keys, 8 heads of 32, bf16                     5.1
+//     8 rows, 262144 keys, 16 heads of 128 over 4, f16          111    537 MB, 4.8 TB/s with the parts' join of 8; the walk alone 5.1
+//     53373 rows in 1112 scenes, 8 heads of 16, f16              29.6  55 MB; 10 million vector instructions, 16 us of every SIMD's time
+//     16384 rows in 3 causal scenes, 16 heads of 128 over 4, bf16  381 to 427 by the card's clock    915 to 1026 TFLOP/s
 //     backward 110545 rows in 2303 scenes, 8 heads of 16, f16   163    230 MB; 53 million vector instructions, 86 us
-//     backward 16384 rows in 4 causal scenes, 16 heads of 64 over 4, bf16  817    656 TFLOP/s of the five products that it cannot do without, 918 of the seven that it does
+//     backward 16384 rows in 4 causal scenes, 16 heads of 64 over 4, bf16  806 to 817    656 to 665 TFLOP/s of the five products that it cannot do without, 918 to 931 of the seven that it does
 #pragma once
 
 #include "sc_product.h"
@@ -75,7 +75,8 @@ __device__ inline Scene scene_of_queries(const Attention& p, int log2, int64_t u
 // ---- tiles in LDS ---------------------------------------------------------------------------------------
 // A tile is rows of LINE chunks of 16 bytes.  Where a chunk lies in its line is turned by the line's number so that both reads meet every bank once: 16-byte reads along
 // the lines go 16 lanes a cycle, a chunk of lines 0-3 and 12-15 and its neighbour of lines 4-11; transposing reads 32 lanes, two chunks of eight consecutive lines;
-// 32-bit reads across 64 bytes of lines 0, 4, 8 and 12.
+// 32-bit reads across 64 bytes of lines 0, 4, 8 and 12.  Not so in lines of 128 bytes of f32: those four all begin in the same half of the banks, so that 32-bit reads across them meet every bank of it
+// twice (the counters have a cycle for each matrix instruction of the keys' gradients).
 template <int DT, int LINE>
 __device__ constexpr int tile_turn(int line) {
     constexpr int WIDE = LINE < 16 ? LINE : 16;
@@ -231,6 +232,8 @@ struct ChannelReader {
 };
 // Weights of a step as the second product's second operand: rounded once to the rows' type (f32: as they are), or the matrix cores would need two products, of a weight and of
 // what rounding left of it.  An error of a result's own rounding comes to it: of dq in bf16 0.0025 of its norm in place of the 0.0017 that the result's type costs.
+// Forward the sum is of the weights ahead of that rounding, which spares turning them back.  So where one key has nearly all the weight of a row, and came at less than 2^CALM above
+// the exponent that was followed, its rounding does not cancel: the row is its value times a factor that is off 1 by half a step of the type at most (2^-8 bf16, 2^-11 f16).
 template <int DT, int ST>
 __device__ __forceinline__ uint4 weights_of(const f32x4 (&p)[ST], int step) {
     if constexpr (DT == SC_F32) {
@@ -629,7 +632,8 @@ constexpr int grad_waves(int rows, int results) {                 // wavefronts 
 }
 
 // Gradients of scores are a weight, some 1 / keys, times what may be small itself: in f16, whose least normal number is 2^-14, most of a long scene's would be rounded off.
-// A wavefront therefore holds them times a power of two, `factor`, that its first ones set, and sets it anew, with what is summed so far, when some come near f16's end.  The weights
+// A wavefront therefore holds them times a power of two, `factor`, that its first ones set (the largest comes to 2^7 to 2^8, so those down to 2^-21 of it are normal), and sets it anew, with what is summed so far,
+// when some come near f16's end.  The weights
 // themselves are at most 1 and are lifted by 2^14 in the keys' kernel.
 template <int DT>
 constexpr float WEIGHT_LIFT = DT == SC_F16 ? 14.f : 0.f;

@@ -291,6 +291,8 @@ constexpr int64_t scene_units(int64_t columns, int64_t scenes, int64_t tile) { r
 //                    scenes of 32768 keys 116 / 109
 //   SHORT 64 / WIDE  32768 rows of 32 in scenes of 96 21 / 27, 128 22 / 30, 192 29 / 28; of 64 in scenes of 48 32 / 39, 64 41 / 31; of 128 in scenes of 16 93 / 167, 32 103 / 96, 48 87 / 75
 //   SHORT, 32 / 64   2048 rows of 32 in scenes of 48 5.2 / 6.4; 32768 in scenes of 48 21.7 / 18.9
+// The columns are those of heads of up to 128 channels.  Of wider ones a wavefront has 16 at a time and a workgroup 64, and SHORT_64 is SHORT where a row has more than 128 bytes, so parts are chosen for half as many
+// workgroups as there are, and may be up to twice as many as intended; backward as much for f32 heads above 64 channels.
 enum AttentionShape { ATTENTION_FEW, ATTENTION_SHORT, ATTENTION_SHORT_64, ATTENTION_WIDE };
 constexpr int attention_columns(AttentionShape shape) {
     return shape == ATTENTION_FEW ? 16 : shape == ATTENTION_SHORT ? 32 : shape == ATTENTION_SHORT_64 ? 64 : 128;
